@@ -339,6 +339,104 @@ int32_t pctc_grouped_backward(pctc_dtype dtype, const void* H, int32_t M, int32_
                               size_t workspace_bytes, void* stream);
 
 /* ----------------------------------------------------------------------------------
+ * Readout with beams: CTC prefix beam search over the head's classes.
+ * ---------------------------------------------------------------------------------- */
+
+#define PCTC_MAX_BEAMS 32       /* beams per utterance */
+#define PCTC_MAX_CANDIDATES 64  /* candidate classes per frame */
+
+/* Frame candidates: for each frame the C most probable classes other than blank, with their log
+ * probabilities and blank's, over the full vocabulary (Eq. lognorm); the logits are not stored.
+ * H, D, W, bias, V: as for pruned_ctc_fwd_bwd_ex; M >= 0 frames; 0 <= blank < V;
+ * 1 <= C <= PCTC_MAX_CANDIDATES.
+ * ids  device int32 [M, C], logp device float [M, C]: classes by falling logit (the lowest id first
+ *      among equal ones) and float(z - lambda); where fewer than C classes have a logit above -inf,
+ *      the rest are -1 and -inf.  NaN or +inf logits give unspecified rows.
+ * blank_logp  device float [M].
+ * workspace: pctc_frame_candidates_workspace_size() bytes, 256-byte aligned; at most about 256 MiB
+ *      (kept per frame and block of 32 classes; more frames than fit take another pass over W) beside
+ *      the normaliser's partial sums.  Returns 0 for invalid arguments.
+ * Asynchronous. */
+size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C);
+int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W,
+                              const float* bias, int32_t V, int32_t blank, int32_t C, int32_t* ids,
+                              float* logp, float* blank_logp, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* Prefix beam search.  Up to K label prefixes per utterance, each with the mass of its alignments
+ * that end in blank (pb) and in its last label (pn).  With b a frame's blank score, l(c) the score of
+ * class c (-inf if it is not among the frame's candidates), s = pb (+) pn, (+) adding masses of logs,
+ * and w the token bonus, a frame turns prefix y into
+ *   y itself:  pb' = s + b;  pn' = (pn + l(last)) (+) (x + l(last) + w), the second term where y without
+ *              its last label is a prefix p of the beam: x = pb_p if p ends in that label too, else s_p;
+ *   y c, for each candidate c for which y c is not in the beam:  pb' = -inf, pn' = x + l(c) + w,
+ *              x = pb if c is y's last label, else s;
+ * and the K largest pb' (+) pn' above -inf are kept, in falling order; equal ones: prefixes of the beam
+ * first, then the others, by beam and then candidate.  Scores are held in float relative to the best
+ * prefix, whose total is kept in double.  Prefixes are compared by length and a 64-bit hash of their
+ * labels.
+ *
+ * The state between frames is caller memory of pctc_beam_state_bytes(N, K, max_frames) bytes, 256-byte
+ * aligned: it holds the beams and, for up to max_frames frames per utterance, K label records of 12 bytes
+ * a frame (0 for invalid arguments: N < 0, K outside [1, PCTC_MAX_BEAMS], max_frames < 0, or
+ * K max_frames >= 2^31).  pctc_beam_reset starts every utterance with the empty prefix.
+ *
+ * pctc_beam_advance: `frames` more frames of each utterance.  ids, logp [sum frames, C], blank_logp
+ * [sum frames]: device, utterance after utterance, as pctc_frame_candidates writes them (classes
+ * distinct and not blank, scores falling; an id below 0, or a score of -inf or NaN, is no candidate).
+ * frames: HOST int32 [N], >= 0.  frames_done: HOST int32 [N], in and out: the frames each utterance
+ * has had since the reset (zeros then); an utterance that would pass max_frames is PCTC_ELENGTH, before
+ * any work.  token_bonus: finite.  parents: device int32 [N, K] or NULL: the beam at the start of
+ * the call that each beam descends from (-1: no prefix in that place).
+ * pctc_beam_result: tokens device int32 [N, K, max_tokens] (labels; -1 past a prefix's end, and only the
+ * first max_tokens of a longer one), token_lengths device int32 [N, K] (-1: no prefix), scores device
+ * float [N, K] (total log mass with the bonuses; -inf: no prefix).  The state stays as it is.
+ * N = 0 is allowed.  All three are asynchronous; they copy nothing from host memory to the device (lengths
+ * go as kernel arguments), so a captured graph replays them with the lengths of the capture. */
+size_t pctc_beam_state_bytes(int32_t N, int32_t K, int32_t max_frames);
+int32_t pctc_beam_reset(int32_t N, int32_t K, int32_t max_frames, void* state, size_t state_bytes, void* stream);
+int32_t pctc_beam_advance(const int32_t* ids, const float* logp, const float* blank_logp, int32_t C,
+                          const int32_t* frames, int32_t N, int32_t K, int32_t max_frames, float token_bonus,
+                          int32_t* frames_done, void* state, size_t state_bytes, int32_t* parents, void* stream);
+int32_t pctc_beam_result(int32_t N, int32_t K, int32_t max_frames, const void* state, size_t state_bytes,
+                         int32_t max_tokens, int32_t* tokens, int32_t* token_lengths, float* scores, void* stream);
+
+/* Reorders a caller's per-beam state (a predictor's, a language model's cache) after an advance:
+ * out_i[n][k] = in_i[n][parents[n][k]] for each of ntensors contiguous device buffers [N, K, ...] of
+ * beam_bytes[i] bytes per beam (any size and alignment, at most 2^36).  A parent outside [0, K) leaves
+ * the beam's own state.  in, out, beam_bytes: HOST arrays; out NULL (or out[i] == in[i]): in place; other
+ * overlaps are not allowed.  parents: device int32 [N, K].  1 <= K <= PCTC_MAX_BEAMS.  Asynchronous. */
+int32_t pctc_beam_reorder(int32_t ntensors, const void* const* in, void* const* out, const int64_t* beam_bytes,
+                          const int32_t* parents, int32_t N, int32_t K, void* stream);
+
+/* Whole utterances from frames to label sequences: candidates, reset, advance and result in one call.
+ * H .. V, input_lengths, N, blank: as for pctc_greedy_decode; K, C, token_bonus, max_tokens and the
+ * outputs as above.  ids, logp [M, C] and blank_logp [M]: the frames' candidates, each may be NULL.
+ * workspace: pctc_beam_decode_workspace_size() bytes, 256-byte aligned.  Asynchronous. */
+size_t pctc_beam_decode_workspace_size(pctc_dtype dtype, const int32_t* input_lengths, int32_t N, int32_t D,
+                                       int32_t V, int32_t K, int32_t C);
+int32_t pctc_beam_decode(pctc_dtype dtype, const void* H, int32_t D, const void* W, const float* bias, int32_t V,
+                         const int32_t* input_lengths, int32_t N, int32_t blank, int32_t K, int32_t C,
+                         float token_bonus, int32_t max_tokens, int32_t* tokens, int32_t* token_lengths,
+                         float* scores, int32_t* ids, float* logp, float* blank_logp, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* ----------------------------------------------------------------------------------
+ * Training step: the global norm of a list of gradients, and clipping.
+ *   norm = sqrt(sum of squares over all tensors),  s = min(1, max_norm / (norm + 1e-6)),
+ *   out_i = s grads_i, rounded once to the tensor's type
+ * grads, out: HOST arrays of ntensors device pointers; out NULL: in place (nothing is written where s
+ * is 1).  n: HOST, values of each tensor (0 .. 2^36); dtypes: HOST, PCTC_F32 or PCTC_BF16; pointers
+ * aligned to their type.  max_norm >= 0 (+inf: the norm alone, and copies).  Squares are summed in
+ * double, in an order that depends on the sizes only.  norm: device float [1]; scale: device float [1] or
+ * NULL.  A norm that is not finite is reported as it is and scales by 1.
+ * workspace: pctc_clip_workspace_size(ntensors) bytes, 256-byte aligned.  Asynchronous. */
+size_t pctc_clip_workspace_size(int32_t ntensors);
+int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* const* out, const int64_t* n,
+                            const int32_t* dtypes, float max_norm, float* norm, float* scale, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* ----------------------------------------------------------------------------------
  * Kernel timing for benchmarks.  When enabled, every kernel the library launches is
  * bracketed by HIP events on its stream; the times are accumulated per kernel name when
  * they are read (pctc_prof_count / pctc_prof_get, which wait for the recorded launches to

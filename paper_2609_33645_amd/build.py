@@ -22,7 +22,7 @@ LIB = os.path.join(HERE, "libprunedctc.so")
 ROOT = os.path.dirname(HERE)
 
 SOURCES = ["pctc_api.hip", "union_remap.hip", "head_gemm.hip", "head_gemm_bf16.hip", "head_gemm_f32.hip",
-           "ctc_dp.hip", "grouped_head.hip"]
+           "ctc_dp.hip", "grouped_head.hip", "frame_candidates.hip", "beam_search.hip", "grad_clip.hip"]
 
 
 def hipcc() -> str:

@@ -1,0 +1,275 @@
+// Frame candidates (gfx950): the C most probable classes of every frame other than blank, with
+// their log probabilities and blank's, over the full vocabulary; the frame x vocabulary logits are
+// never stored.
+//
+//   z = H W^T + b,  lambda_m = log sum_v exp z_mv,  logp = float(z - lambda_m), z and lambda in the order
+//   of falling z, the lowest class first among equal ones
+//
+// One vocabulary pass on the matrix cores gives the normaliser's partial pairs and the largest logit
+// of every block of 32 classes.  A class among a frame's C best lies in one of the C + 1 blocks with
+// the largest maxima (one more for blank, which is left out), so a second kernel forms those blocks'
+// logits again, 32 (C + 1) dot products a frame, and orders them.  A block of 32 classes is where the
+// two sides meet: M V / 32 maxima are written and read (96 MB at 4,215 frames of 180,000 classes),
+// and W rows for 32 (C + 1) classes a frame are read again, from the L2s.  The scratch for the maxima is
+// held to 256 MB by passing over the vocabulary once per that many frames.
+#include <algorithm>
+
+#include "pctc_internal.h"
+
+namespace pctc {
+
+namespace {
+
+constexpr size_t kMaxBlockBytes = static_cast<size_t>(256) << 20;
+constexpr int kThreads = 256;
+constexpr int kList = 256;  // blocks kept for ordering; more only where maxima are equal
+constexpr int kValues = (kMaxCandidates + 1) * kCandRows;
+
+// Floats in the order of unsigned integers.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+
+// The largest key t (its low 12 bits zero) that at least `need` of the workgroup's 256 keys reach;
+// 0 when there are fewer.  Every wavefront searches by itself.
+__device__ __forceinline__ uint32_t reach(const uint32_t* keys, int need, int lane) {
+  uint32_t k[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k[i] = keys[64 * i + lane];
+  uint32_t t = 0;
+  for (int bit = 31; bit >= 12; --bit) {
+    const uint32_t c = t | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += __popcll(__ballot(k[i] >= c));
+    if (n >= need) t = c;
+  }
+  return t;
+}
+
+__device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, uint16_t) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    s = fmaf(__uint_as_float(w[q] << 16), __uint_as_float(h[q] << 16), s);
+    s = fmaf(__uint_as_float(w[q] & 0xffff0000u), __uint_as_float(h[q] & 0xffff0000u), s);
+  }
+  return s;
+}
+__device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, float) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) s = fmaf(__uint_as_float(w[q]), __uint_as_float(h[q]), s);
+  return s;
+}
+
+}  // namespace
+
+// One workgroup per frame.
+template <class T>
+__global__ void __launch_bounds__(kThreads)
+cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
+                   int V, int blank, int C, const float* __restrict__ bmax, int nb, const double* __restrict__ lam,
+                   int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
+  constexpr int kPer = 16 / sizeof(T);
+  __shared__ uint32_t keys[kThreads];
+  __shared__ float list_v[kList];
+  __shared__ int list_b[kList];
+  __shared__ int count;
+  __shared__ int sel[kMaxCandidates + 1];
+  __shared__ float z[kValues];
+  __shared__ float val_v[kValues];
+  __shared__ int val_i[kValues];
+  __shared__ float zblank;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int m = m0 + blockIdx.x;
+  const float* const row = bmax + static_cast<int64_t>(blockIdx.x) * nb;
+  const int nsel = min(C + 1, (V + kCandRows - 1) / kCandRows);
+
+  // ---- the nsel blocks with the largest maxima (ties: the lowest) ----
+  float mx = -INFINITY;
+  for (int i = tid * 4; i < nb; i += kThreads * 4) {
+    const float4 v = *reinterpret_cast<const float4*>(row + i);
+    mx = fmaxf(mx, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+  }
+  keys[tid] = order_key(mx);
+  if (tid == 0) count = 0;
+  __syncthreads();
+  uint32_t t = reach(keys, nsel, lane);
+  for (int i = tid * 4; i < nb; i += kThreads * 4) {
+    const float4 v4 = *reinterpret_cast<const float4*>(row + i);
+    const float v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (v[e] > -INFINITY && order_key(v[e]) >= t) {
+        const int q = atomicAdd(&count, 1);
+        if (q < kList) {
+          list_v[q] = v[e];
+          list_b[q] = i + e;
+        }
+      }
+    }
+  }
+  __syncthreads();
+  int n = count;
+  if (n <= kList) {
+    // the list in the order of (maximum, block): a block's place is the number of those before it
+    if (tid < n) {
+      const float v = list_v[tid];
+      const int b = list_b[tid];
+      int rank = 0;
+      for (int q = 0; q < n; ++q) rank += list_v[q] > v || (list_v[q] == v && list_b[q] < b);
+      if (rank < nsel) sel[rank] = b;
+    }
+    n = min(n, nsel);
+  } else {
+    // many equal maxima: the key of the nsel-th block exactly, the blocks above it in any order, then
+    // those at it from the lowest on
+    t = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t c = t | (1u << bit);
+      __syncthreads();
+      if (tid == 0) count = 0;
+      __syncthreads();
+      int mine = 0;
+      for (int i = tid; i < nb; i += kThreads) mine += row[i] > -INFINITY && order_key(row[i]) >= c;
+      if (mine) atomicAdd(&count, mine);
+      __syncthreads();
+      if (count >= nsel) t = c;
+    }
+    __syncthreads();
+    if (tid == 0) count = 0;
+    __syncthreads();
+    for (int i = tid; i < nb; i += kThreads)
+      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = i;
+    __syncthreads();
+    n = count;
+    if (wave == 0) {
+      for (int i0 = 0; i0 < nb && n < nsel; i0 += 64) {
+        const bool at = i0 + lane < nb && row[i0 + lane] > -INFINITY && order_key(row[i0 + lane]) == t;
+        const uint64_t who = __ballot(at);
+        const int q = n + __popcll(who & ((uint64_t{1} << lane) - 1));
+        if (at && q < nsel) sel[q] = i0 + lane;
+        n += __popcll(who);
+      }
+      if (lane == 0) count = min(n, nsel);
+    }
+    __syncthreads();
+    n = count;
+  }
+  __syncthreads();
+
+  // ---- their logits: eight lanes a class, eight classes of a wavefront at a time ----
+  const T* const h = H + static_cast<int64_t>(m) * D;
+  const int part = lane & 7;
+  auto dots = [&](int v) {  // class v's logit without bias, in each of its eight lanes (v >= V: 0)
+    float s = 0.f;
+    if (v < V) {
+      const T* const w = W + static_cast<int64_t>(v) * D;
+      for (int k = part * kPer; k < D; k += 8 * kPer)
+        s = dot16(*reinterpret_cast<const u32x4*>(w + k), *reinterpret_cast<const u32x4*>(h + k), s, T{});
+    }
+#pragma unroll
+    for (int o = 4; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+    return s;
+  };
+  for (int g = wave; g < n * 4; g += kThreads / 64) {  // groups of eight classes
+    const int v = sel[g >> 2] * kCandRows + (g & 3) * 8 + (lane >> 3);
+    float s = dots(v);
+    if (part == 0) {
+      if (bias && v < V) s += bias[v];
+      z[g * 8 + (lane >> 3)] = (v < V && v != blank) ? s : -INFINITY;
+    }
+  }
+  if (wave == kThreads / 64 - 1) {
+    float s = dots(blank);
+    if (lane == 0) zblank = bias ? s + bias[blank] : s;
+  }
+  if (tid == 0) count = 0;
+  __syncthreads();
+
+  // ---- the C best of them ----
+  const int nz = n * kCandRows;
+  mx = -INFINITY;
+  for (int i = tid; i < nz; i += kThreads) mx = fmaxf(mx, z[i]);
+  keys[tid] = order_key(mx);
+  __syncthreads();
+  t = reach(keys, C, lane);
+  for (int i = tid; i < nz; i += kThreads) {
+    const float v = z[i];
+    if (v > -INFINITY && order_key(v) >= t) {
+      const int q = atomicAdd(&count, 1);
+      val_v[q] = v;
+      val_i[q] = sel[i / kCandRows] * kCandRows + i % kCandRows;
+    }
+  }
+  __syncthreads();
+  const int nv = count;
+  const double l = lam[blockIdx.x];
+  for (int i = tid; i < nv; i += kThreads) {
+    const float v = val_v[i];
+    const int id = val_i[i];
+    int rank = 0;
+    for (int q = 0; q < nv; ++q) rank += val_v[q] > v || (val_v[q] == v && val_i[q] < id);
+    if (rank < C) {
+      ids[static_cast<int64_t>(m) * C + rank] = id;
+      logp[static_cast<int64_t>(m) * C + rank] = static_cast<float>(v - l);
+    }
+  }
+  for (int r = nv + tid; r < C; r += kThreads) {
+    ids[static_cast<int64_t>(m) * C + r] = -1;
+    logp[static_cast<int64_t>(m) * C + r] = -INFINITY;
+  }
+  if (tid == 0) blank_logp[m] = static_cast<float>(zblank - l);
+}
+
+int cand_pass_frames(int M, int V) {
+  const size_t per = static_cast<size_t>(cand_blocks(V)) * sizeof(float);
+  const int most = static_cast<int>(std::min<size_t>(kMaxBlockBytes / per / 256 * 256, 1 << 30));
+  return std::min(M, std::max(most, 256));
+}
+
+// lambda, its pair, the normaliser's partial pairs and the block maxima of one pass.
+size_t cand_scratch_bytes(int M, int D, int V) {
+  const int F = std::max(1, cand_pass_frames(M, V));
+  return 2 * align_up(static_cast<size_t>(F) * 8, 256) + lse_partial_bytes(F, D) +
+         align_up(static_cast<size_t>(F) * cand_blocks(V) * sizeof(float), 256);
+}
+
+hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
+                                   int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
+                                   hipStream_t stream) {
+  const int F = cand_pass_frames(M, V), nb = cand_blocks(V);
+  char* s = static_cast<char*>(scratch);
+  double* lam = reinterpret_cast<double*>(s);
+  s += align_up(static_cast<size_t>(F) * 8, 256);
+  float2* lam2 = reinterpret_cast<float2*>(s);
+  s += align_up(static_cast<size_t>(F) * 8, 256);
+  float2* partials = reinterpret_cast<float2*>(s);
+  float* bmax = reinterpret_cast<float*>(s + lse_partial_bytes(F, D));
+  for (int m0 = 0; m0 < M; m0 += F) {
+    const int here = std::min(F, M - m0);
+    int P = 0;
+    hipError_t e;
+    if (dtype == 1)
+      e = launch_cand_partial_bf16(static_cast<const uint16_t*>(H) + static_cast<int64_t>(m0) * D, here, D,
+                                   static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, stream);
+    else
+      e = launch_cand_partial_f32(static_cast<const float*>(H) + static_cast<int64_t>(m0) * D, here, D,
+                                  static_cast<const float*>(W), bias, V, partials, &P, bmax, stream);
+    if (e != hipSuccess) return e;
+    e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
+    if (e != hipSuccess) return e;
+    Prof pr("cand_select", stream);
+    if (dtype == 1)
+      hipLaunchKernelGGL(cand_select_kernel<uint16_t>, dim3(here), dim3(kThreads), 0, stream,
+                         static_cast<const uint16_t*>(H), m0, D, static_cast<const uint16_t*>(W), bias, V, blank, C,
+                         bmax, nb, lam, ids, logp, blank_logp);
+    else
+      hipLaunchKernelGGL(cand_select_kernel<float>, dim3(here), dim3(kThreads), 0, stream,
+                         static_cast<const float*>(H), m0, D, static_cast<const float*>(W), bias, V, blank, C, bmax,
+                         nb, lam, ids, logp, blank_logp);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace pctc

@@ -262,6 +262,49 @@ lse_partial_e_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ 
   lse_store_partials<G>(run_max, run_sum, stg_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
 
+// The normaliser with each frame's block maxima beside it (frame candidates), in the argmax's tile
+// order.
+template <class G, bool BIAS>
+__global__ void __launch_bounds__(G::kThreads, 1)
+cand_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __restrict__ W,
+                  const float* __restrict__ bias, int V, int P, int vper, float2* __restrict__ partials, int nb,
+                  float* __restrict__ bmax) {
+  extern __shared__ float bsh[];  // BIAS: b over this partition's rows
+  constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
+  PCTC_STAGES_G(G)
+  int mt, p;
+  if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), (M + TC - 1) / TC, P, mt, p)) return;
+  const int m0 = mt * TC;
+  const int vbeg = p * vper;
+  const int vend = min(V, vbeg + vper);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int ntiles = (vend - vbeg + TR - 1) / TR;
+  if (BIAS) {
+    for (int r = tid; r < ntiles * TR; r += G::kThreads) bsh[r] = (vbeg + r < vend) ? bias[vbeg + r] : 0.f;
+    __syncthreads();
+  }
+  const GOp A{W, D, vend, D, nullptr};
+  const GOp B{H, D, M, D, nullptr};
+  float run_max[FC], run_sum[FC];
+#pragma unroll
+  for (int j = 0; j < FC; ++j) {
+    run_max[j] = -INFINITY;
+    run_sum[j] = 0.f;
+  }
+  f32x16 acc[FR][FC];
+  auto epi = [&](int it, f32x16 (&a)[FR][FC]) {
+    const int v0 = vbeg + it * TR;
+    if (v0 + TR > vend) mask_rows_inf<FR, FC, G>(a, v0, vend, wave, lane);
+    const float4 blocks = lse_block_update<FR, FC, G>(a, lane, run_max, run_sum);
+    store_block_max<G>(blocks, v0, wave, lane, m0, M, nb, bmax);
+  };
+  G::run_seq(A, B, vbeg, m0, ntiles, D, st, acc, epi, [&](int it, f32x16 (&a)[FR][FC]) {
+    if constexpr (BIAS) bias_init<FR, FC, G>(a, bsh + it * TR, wave, lane);
+    else G::zero(a);
+  });
+  lse_store_partials<G>(run_max, run_sum, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
+}
+
 // ---------------------------------------------------------------------------------------
 // Greedy emission head: framewise argmax of H W^T (+ b) over a vocabulary partition, on the
 // same pipelined tiles as the normaliser.  Within a lane the rows are visited in
@@ -1200,6 +1243,27 @@ hipError_t launch_amax_partial_bf16(const uint16_t* H, int M, int D, const uint1
     PCTC_AMAX(GMid)
   }
 #undef PCTC_AMAX
+  return hipGetLastError();
+}
+
+hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
+                                    float2* partials, int* P_out, float* bmax, hipStream_t stream) {
+  const LseSplit sp = lse_split_bf16(M, D, V, SplitFor::kAmax);
+  *P_out = sp.P;
+  Prof pr("cand_partial", stream);
+  const size_t bsh = bias ? static_cast<size_t>(sp.vper) * sizeof(float) : 0;
+  const dim3 grid(grouped_grid(sp.nM, sp.P));
+#define PCTC_CAND(G, BIAS)                                                                                       \
+  hipLaunchKernelGGL((cand_partial_bf16<G, BIAS>), grid, dim3(G::kThreads), bsh, stream, H, M, D, W, bias, V, sp.P, \
+                     sp.vper, partials, cand_blocks(V), bmax)
+  if (sp.wide) {
+    if (bias) PCTC_CAND(GWide, true);
+    else PCTC_CAND(GWide, false);
+  } else {
+    if (bias) PCTC_CAND(GMid, true);
+    else PCTC_CAND(GMid, false);
+  }
+#undef PCTC_CAND
   return hipGetLastError();
 }
 

@@ -132,6 +132,30 @@ amax_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
   amax_store_partials<GZ>(bv, bi, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
 
+// The normaliser with each frame's block maxima beside it (frame candidates).
+template <bool BIAS>
+__global__ void __launch_bounds__(512, 1)
+cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restrict__ W,
+                 const float* __restrict__ bias, int V, int P, int vper, float2* __restrict__ partials, int nb,
+                 float* __restrict__ bmax) {
+  PCTC_F3_STAGES
+  int mt, p;
+  if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), (M + kTile - 1) / kTile, P, mt, p)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int m0 = mt * kTile, vbeg = p * vper, vend = min(V, vbeg + vper);
+  float run_max[GZ::FC], run_sum[GZ::FC];
+#pragma unroll
+  for (int j = 0; j < GZ::FC; ++j) {
+    run_max[j] = -INFINITY;
+    run_sum[j] = 0.f;
+  }
+  vocab_tiles<BIAS>(H, M, D, W, bias, m0, vbeg, vend, st, [&](int v0, int el, f32x16 (&a)[GZ::FR][GZ::FC]) {
+    const float4 blocks = lse_block_update<GZ::FR, GZ::FC, GZ>(a, el, run_max, run_sum);
+    store_block_max<GZ>(blocks, v0, wave, el, m0, M, nb, bmax);
+  });
+  lse_store_partials<GZ>(run_max, run_sum, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
+}
+
 __global__ void __launch_bounds__(512, 1)
 gather_s_f32(const float* __restrict__ H, int M, int D, const float* __restrict__ W, const float* __restrict__ bias,
              const int32_t* __restrict__ u_ids, const int32_t* __restrict__ Kdev, const double* __restrict__ lam,
@@ -457,6 +481,22 @@ hipError_t launch_amax_partial_f32(const float* H, int M, int D, const float* W,
                        vper, partials);
   else
     hipLaunchKernelGGL(amax_partial_f32<false>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials);
+  return hipGetLastError();
+}
+
+hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
+                                   float2* partials, int* P_out, float* bmax, hipStream_t stream) {
+  int vper, P;
+  lse_split_f32(D, V, &vper, &P);
+  *P_out = P;
+  const dim3 grid(grouped_grid((M + kTile - 1) / kTile, P));
+  Prof pr("cand_partial", stream);
+  if (bias)
+    hipLaunchKernelGGL(cand_partial_f32<true>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,
+                       cand_blocks(V), bmax);
+  else
+    hipLaunchKernelGGL(cand_partial_f32<false>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,
+                       cand_blocks(V), bmax);
   return hipGetLastError();
 }
 

@@ -126,6 +126,64 @@ __device__ __forceinline__ void lse_tile_update(const f32x16 (&acc)[FR][FC], flo
   }
 }
 
+// The same; returns the largest logit of each of the wavefront's four 32-row blocks (all 32 rows) for
+// the frame of the lane's half: lanes [0, 32) frame column 0, the others column 1.
+template <int FR, int FC, class G>
+__device__ __forceinline__ float4 lse_block_update(const f32x16 (&acc)[FR][FC], int lane, float (&run_max)[FC],
+                                                   float (&run_sum)[FC]) {
+  static_assert(FR == 4 && FC == 2, "four blocks of 32 rows by two frame columns");
+  float4 blocks = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < FC; ++j) {
+    float bm[FR];
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < FR; ++i) {
+      float x = acc[i][j][0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) x = fmaxf(x, acc[i][j][r]);
+      bm[i] = fmaxf(x, swap_halves(x));
+      tmax = fmaxf(tmax, bm[i]);
+    }
+    const bool mine = (lane >> 5) == j;
+    blocks.x = mine ? bm[0] : blocks.x;
+    blocks.y = mine ? bm[1] : blocks.y;
+    blocks.z = mine ? bm[2] : blocks.z;
+    blocks.w = mine ? bm[3] : blocks.w;
+    const float nmax = fmaxf(run_max[j], tmax);
+    // a column with no finite logit yet (rows masked by a -inf bias) adds nothing
+    const float ms = (nmax == -INFINITY) ? 0.f : nmax * kLog2e;
+    float s = 0.f;
+    if (__builtin_expect(__any(fabsf(nmax) > 1e37f && nmax > -INFINITY), 0)) {
+      // a column of masked classes only, the mask a type's lowest value: its products with log2(e)
+      // overflow, the differences do not
+#pragma unroll
+      for (int i = 0; i < FR; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += fast_exp2((acc[i][j][r] - (nmax == -INFINITY ? 0.f : nmax)) * kLog2e);
+    } else {
+#pragma unroll
+      for (int i = 0; i < FR; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += fast_exp2(fmaf(acc[i][j][r], kLog2e, -ms));
+    }
+    s += swap_halves(s);
+    const float scale = (run_max[j] == -INFINITY) ? 0.f : fast_exp2((run_max[j] - nmax) * kLog2e);
+    run_sum[j] = fmaf(run_sum[j], scale, s);
+    run_max[j] = nmax;
+  }
+  return blocks;
+}
+
+// Writes the block maxima of a tile whose first class is v0 (a frame's row has nb of them).
+template <class G>
+__device__ __forceinline__ void store_block_max(const float4& blocks, int v0, int wave, int lane, int m0, int M,
+                                                int nb, float* __restrict__ bmax) {
+  const int m = m0 + G::col_of(wave, lane, 0) + 32 * (lane >> 5);
+  const int blk = (v0 + G::row_of(wave, 0, 0, 0)) >> 5;
+  if (m < M) *reinterpret_cast<float4*>(bmax + static_cast<int64_t>(m) * nb + blk) = blocks;
+}
+
 // The two wavefronts of each frame column (row halves) combine their running (max, sum)
 // pairs through LDS (xch: any drained stage) and write the partition's pair of every frame.
 template <class G>

@@ -957,6 +957,204 @@ int32_t pctc_greedy_decode(pctc_dtype dtype, const void* H, int32_t D, const voi
   return PCTC_OK;
 }
 
+// ---- readout with beams ----------------------------------------------------------------------
+
+static bool head_args_ok(pctc_dtype dtype, int32_t D, int32_t V) {
+  return (dtype == PCTC_F32 || dtype == PCTC_BF16) && D > 0 && D % 8 == 0 && D <= PCTC_MAX_DIM && V > 1 &&
+         V <= PCTC_MAX_VOCAB;
+}
+static bool misaligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255) != 0; }
+constexpr int32_t kMaxFrames = 1 << 30;  // of a batch, as for the loss
+constexpr int32_t kMaxUtts = 1 << 24;    // with PCTC_MAX_BEAMS beams each, a grid of one workgroup per beam
+
+size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C) {
+  if (!head_args_ok(dtype, D, V) || M < 0 || M > kMaxFrames || C < 1 || C > PCTC_MAX_CANDIDATES) return 0;
+  return cand_scratch_bytes(M, D, V);
+}
+
+int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W, const float* bias,
+                              int32_t V, int32_t blank, int32_t C, int32_t* ids, float* logp, float* blank_logp,
+                              void* workspace, size_t workspace_bytes, void* stream_ptr) {
+  const size_t need = pctc_frame_candidates_workspace_size(dtype, M, D, V, C);
+  if (need == 0 || blank < 0 || blank >= V || !W || misaligned16(W) || misaligned16(H)) return PCTC_EINVAL;
+  if (M > 0 && (!H || !ids || !logp || !blank_logp)) return PCTC_EINVAL;
+  if (M == 0) return PCTC_OK;
+  if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
+  if (misaligned256(workspace)) return PCTC_EINVAL;
+  PCTC_HIP(launch_frame_candidates(dtype == PCTC_BF16 ? 1 : 0, H, M, D, W, bias, V, blank, C, ids, logp, blank_logp,
+                                   workspace, static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
+size_t pctc_beam_state_bytes(int32_t N, int32_t K, int32_t max_frames) {
+  if (N < 0 || N > kMaxUtts || K < 1 || K > PCTC_MAX_BEAMS || max_frames < 0 ||
+      static_cast<int64_t>(K) * max_frames > INT32_MAX)
+    return 0;
+  size_t at[12];
+  return beam_state_layout(N, K, max_frames, at);
+}
+
+static int32_t check_beam_state(int32_t N, int32_t K, int32_t max_frames, const void* state, size_t bytes) {
+  const size_t need = pctc_beam_state_bytes(N, K, max_frames);
+  if (need == 0) return PCTC_EINVAL;
+  if (N == 0) return PCTC_OK;
+  if (!state || bytes < need) return PCTC_EWORKSPACE;
+  return misaligned256(state) ? PCTC_EINVAL : PCTC_OK;
+}
+
+int32_t pctc_beam_reset(int32_t N, int32_t K, int32_t max_frames, void* state, size_t state_bytes, void* stream_ptr) {
+  const int32_t rc = check_beam_state(N, K, max_frames, state, state_bytes);
+  if (rc != PCTC_OK) return rc;
+  PCTC_HIP(launch_beam_reset(state, N, K, max_frames, static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
+int32_t pctc_beam_advance(const int32_t* ids, const float* logp, const float* blank_logp, int32_t C,
+                          const int32_t* frames, int32_t N, int32_t K, int32_t max_frames, float token_bonus,
+                          int32_t* frames_done, void* state, size_t state_bytes, int32_t* parents, void* stream_ptr) {
+  const int32_t rc = check_beam_state(N, K, max_frames, state, state_bytes);
+  if (rc != PCTC_OK) return rc;
+  if (C < 1 || C > PCTC_MAX_CANDIDATES || !(fabsf(token_bonus) < INFINITY)) return PCTC_EINVAL;
+  if (N > 0 && (!frames || !frames_done)) return PCTC_EINVAL;
+  int64_t M = 0;
+  for (int n = 0; n < N; ++n) {
+    if (frames[n] < 0 || frames_done[n] < 0 || frames[n] > max_frames || frames_done[n] > max_frames - frames[n])
+      return PCTC_ELENGTH;
+    M += frames[n];
+  }
+  if (M > kMaxFrames || (M > 0 && (!ids || !logp || !blank_logp))) return PCTC_EINVAL;
+  if (N == 0) return PCTC_OK;
+  PCTC_HIP(launch_beam_advance(ids, logp, blank_logp, C, frames, N, K, max_frames, token_bonus, frames_done, state,
+                               parents, static_cast<hipStream_t>(stream_ptr)));
+  for (int n = 0; n < N; ++n) frames_done[n] += frames[n];
+  prof_flush();
+  return PCTC_OK;
+}
+
+int32_t pctc_beam_result(int32_t N, int32_t K, int32_t max_frames, const void* state, size_t state_bytes,
+                         int32_t max_tokens, int32_t* tokens, int32_t* token_lengths, float* scores,
+                         void* stream_ptr) {
+  const int32_t rc = check_beam_state(N, K, max_frames, state, state_bytes);
+  if (rc != PCTC_OK) return rc;
+  if (max_tokens < 0) return PCTC_EINVAL;
+  if (N == 0) return PCTC_OK;
+  if (!token_lengths || !scores || (max_tokens > 0 && !tokens)) return PCTC_EINVAL;
+  PCTC_HIP(launch_beam_result(const_cast<void*>(state), N, K, max_frames, max_tokens, tokens, token_lengths, scores,
+                              static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
+int32_t pctc_beam_reorder(int32_t ntensors, const void* const* in, void* const* out, const int64_t* beam_bytes,
+                          const int32_t* parents, int32_t N, int32_t K, void* stream_ptr) {
+  if (ntensors < 0 || N < 0 || N > kMaxUtts || K < 1 || K > PCTC_MAX_BEAMS) return PCTC_EINVAL;
+  if (ntensors > 0 && (!in || !beam_bytes)) return PCTC_EINVAL;
+  bool any = false;
+  for (int i = 0; i < ntensors; ++i) {
+    if (beam_bytes[i] < 0 || beam_bytes[i] > (int64_t{1} << 36)) return PCTC_EINVAL;
+    if (beam_bytes[i] > 0 && N > 0 && (!in[i] || (out && !out[i]))) return PCTC_EINVAL;
+    any |= beam_bytes[i] > 0;
+  }
+  if (N == 0 || !any) return PCTC_OK;
+  if (!parents) return PCTC_EINVAL;
+  PCTC_HIP(launch_beam_reorder(ntensors, in, out, beam_bytes, parents, N, K, static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
+namespace {
+// Workspace of a whole decode: the beams' state, the candidates that are not returned, and the
+// candidates' scratch.
+struct DecodeLayout {
+  int32_t M = 0, max_frames = 0;
+  size_t o_ids, o_logp, o_blank, o_scratch, total;
+};
+int32_t decode_layout(pctc_dtype dtype, const int32_t* T, int32_t N, int32_t D, int32_t V, int32_t K, int32_t C,
+                      DecodeLayout* L) {
+  if (!head_args_ok(dtype, D, V) || N < 0 || N > kMaxUtts || K < 1 || K > PCTC_MAX_BEAMS || C < 1 ||
+      C > PCTC_MAX_CANDIDATES || (N > 0 && !T))
+    return PCTC_EINVAL;
+  int64_t M = 0;
+  for (int n = 0; n < N; ++n) {
+    if (T[n] < 1) return PCTC_ELENGTH;
+    M += T[n];
+    L->max_frames = std::max(L->max_frames, T[n]);
+  }
+  if (M > kMaxFrames) return PCTC_EINVAL;
+  L->M = static_cast<int32_t>(M);
+  const size_t state = pctc_beam_state_bytes(N, K, L->max_frames);
+  if (state == 0) return PCTC_EINVAL;
+  L->o_ids = align_up(state, 256);
+  L->o_logp = L->o_ids + align_up(static_cast<size_t>(M) * C * 4, 256);
+  L->o_blank = L->o_logp + align_up(static_cast<size_t>(M) * C * 4, 256);
+  L->o_scratch = L->o_blank + align_up(static_cast<size_t>(M) * 4, 256);
+  L->total = L->o_scratch + cand_scratch_bytes(L->M, D, V);
+  return PCTC_OK;
+}
+}  // namespace
+
+size_t pctc_beam_decode_workspace_size(pctc_dtype dtype, const int32_t* input_lengths, int32_t N, int32_t D, int32_t V,
+                                       int32_t K, int32_t C) {
+  DecodeLayout L;
+  return decode_layout(dtype, input_lengths, N, D, V, K, C, &L) == PCTC_OK ? L.total : 0;
+}
+
+int32_t pctc_beam_decode(pctc_dtype dtype, const void* H, int32_t D, const void* W, const float* bias, int32_t V,
+                         const int32_t* input_lengths, int32_t N, int32_t blank, int32_t K, int32_t C,
+                         float token_bonus, int32_t max_tokens, int32_t* tokens, int32_t* token_lengths, float* scores,
+                         int32_t* ids, float* logp, float* blank_logp, void* workspace, size_t workspace_bytes,
+                         void* stream_ptr) {
+  DecodeLayout L;
+  const int32_t rc = decode_layout(dtype, input_lengths, N, D, V, K, C, &L);
+  if (rc != PCTC_OK) return rc;
+  if (blank < 0 || blank >= V || !W || misaligned16(W) || misaligned16(H) || max_tokens < 0 ||
+      !(fabsf(token_bonus) < INFINITY))
+    return PCTC_EINVAL;
+  if (N == 0) return PCTC_OK;
+  if (!H || !token_lengths || !scores || (max_tokens > 0 && !tokens)) return PCTC_EINVAL;
+  if (!workspace || workspace_bytes < L.total) return PCTC_EWORKSPACE;
+  if (misaligned256(workspace)) return PCTC_EINVAL;
+  hipStream_t stream = static_cast<hipStream_t>(stream_ptr);
+  char* ws = static_cast<char*>(workspace);
+  if (!ids) ids = reinterpret_cast<int32_t*>(ws + L.o_ids);
+  if (!logp) logp = reinterpret_cast<float*>(ws + L.o_logp);
+  if (!blank_logp) blank_logp = reinterpret_cast<float*>(ws + L.o_blank);
+  PCTC_HIP(launch_frame_candidates(dtype == PCTC_BF16 ? 1 : 0, H, L.M, D, W, bias, V, blank, C, ids, logp, blank_logp,
+                                   ws + L.o_scratch, stream));
+  PCTC_HIP(launch_beam_reset(ws, N, K, L.max_frames, stream));
+  PCTC_HIP(launch_beam_advance(ids, logp, blank_logp, C, input_lengths, N, K, L.max_frames, token_bonus, nullptr, ws,
+                               nullptr, stream));
+  PCTC_HIP(launch_beam_result(ws, N, K, L.max_frames, max_tokens, tokens, token_lengths, scores, stream));
+  prof_flush();
+  return PCTC_OK;
+}
+
+// ---- gradient norm and clipping --------------------------------------------------------------
+
+size_t pctc_clip_workspace_size(int32_t ntensors) { return ntensors < 0 ? 0 : clip_workspace_bytes(ntensors); }
+
+int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* const* out, const int64_t* n,
+                            const int32_t* dtypes, float max_norm, float* norm, float* scale, void* workspace,
+                            size_t workspace_bytes, void* stream_ptr) {
+  if (ntensors < 0 || !(max_norm >= 0.f) || !norm) return PCTC_EINVAL;
+  if (ntensors > 0 && (!grads || !n || !dtypes)) return PCTC_EINVAL;
+  for (int i = 0; i < ntensors; ++i) {
+    if ((dtypes[i] != PCTC_F32 && dtypes[i] != PCTC_BF16) || n[i] < 0 || n[i] > clip_max_values()) return PCTC_EINVAL;
+    const uintptr_t mask = dtypes[i] == PCTC_F32 ? 3 : 1;
+    if (n[i] > 0 && (!grads[i] || (out && !out[i]))) return PCTC_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(grads[i]) & mask) || (out && (reinterpret_cast<uintptr_t>(out[i]) & mask)))
+      return PCTC_EINVAL;
+  }
+  if (!workspace || workspace_bytes < clip_workspace_bytes(ntensors)) return PCTC_EWORKSPACE;
+  if (misaligned256(workspace)) return PCTC_EINVAL;
+  PCTC_HIP(launch_clip_grad_norm(ntensors, grads, out, n, dtypes, max_norm, norm, scale, workspace,
+                                 static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
 size_t pctc_discarded_mass_scratch_bytes(int32_t N, const int32_t* input_lengths, const int32_t* target_lengths) {
   if (N < 0 || (N > 0 && (!input_lengths || !target_lengths))) return 0;
   for (int n = 0; n < N; ++n)

@@ -254,6 +254,50 @@ hipError_t launch_grouped_finalize(float* logp, int K, int M, const double* lse_
 hipError_t launch_grouped_adapter(const float* logp, const float* dlogp, int K, int M, float* G, float* g,
                                   hipStream_t stream);
 
+// ---- frame candidates (frame_candidates.hip; products in head_gemm_bf16.hip, head_gemm_f32.hip) ----
+constexpr int kCandRows = 32;      // classes of a block: the products keep a block's largest logit per frame
+constexpr int kMaxCandidates = 64;
+inline int cand_blocks(int V) { return (V + 255) / 256 * (256 / kCandRows); }  // a frame's block maxima
+// The normaliser's partial pairs and bmax[m * cand_blocks(V) + i], the largest logit of classes
+// [32 i, 32 i + 32) (-inf past V).
+hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
+                                    float2* partials, int* P_out, float* bmax, hipStream_t stream);
+hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
+                                   float2* partials, int* P_out, float* bmax, hipStream_t stream);
+// Frames of one pass over the vocabulary, and the scratch of a call.
+int cand_pass_frames(int M, int V);
+size_t cand_scratch_bytes(int M, int D, int V);
+hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
+                                   int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
+                                   hipStream_t stream);
+
+// ---- prefix beam search (beam_search.hip) --------------------------------------------------
+constexpr int kMaxBeams = 32;
+constexpr int kBeamGroup = 256;  // utterances of a launch: their rows are a kernel argument
+struct FrameRows {
+  int32_t off[kBeamGroup + 1];  // first row of each utterance's frames, and the end
+  int32_t done[kBeamGroup];     // frames each has had before
+};
+size_t beam_state_layout(int N, int K, int max_frames, size_t (&at)[12]);
+hipError_t launch_beam_reset(void* state, int N, int K, int max_frames, hipStream_t stream);
+// done: frames consumed before (null: none); parents [N][K] or null.
+hipError_t launch_beam_advance(const int32_t* ids, const float* logp, const float* blank_logp, int C,
+                               const int32_t* frames, int N, int K, int max_frames, float bonus,
+                               const int32_t* done, void* state, int32_t* parents, hipStream_t stream);
+hipError_t launch_beam_result(void* state, int N, int K, int max_frames, int max_tokens, int32_t* tokens,
+                              int32_t* lengths, float* scores, hipStream_t stream);
+// out null: in place.
+hipError_t launch_beam_reorder(int tensors, const void* const* in, void* const* out, const int64_t* beam_bytes,
+                               const int32_t* parents, int N, int K, hipStream_t stream);
+
+// ---- gradient norm and clipping (grad_clip.hip) ---------------------------------------------
+size_t clip_workspace_bytes(int tensors);
+int64_t clip_max_values();  // of one tensor
+// out null: in place; scale may be null.
+hipError_t launch_clip_grad_norm(int tensors, const void* const* grads, void* const* out, const int64_t* n,
+                                 const int32_t* dtypes, float max_norm, float* norm, float* scale, void* workspace,
+                                 hipStream_t stream);
+
 // ---- alignment lattice ------------------------------------------------------------------
 struct DpPlan {
   int N, M, Y, Smax;

@@ -8,6 +8,7 @@ raises ``PrunedCTCError``; there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 from typing import Dict, Optional, Sequence
@@ -23,6 +24,8 @@ STATUS = {0: "ok", -1: "invalid argument", -2: "bad label", -3: "bad length", -4
           -5: "HIP error", -6: "target too long"}
 UTT_OK, UTT_NOT_ALIGNABLE, UTT_NONFINITE = 0, 1, 2
 MAX_TARGET = 1023
+MAX_BEAMS = 32
+MAX_CANDIDATES = 64
 
 
 class PrunedCTCError(RuntimeError):
@@ -107,6 +110,30 @@ def lib() -> ctypes.CDLL:
     L.pctc_grouped_backward.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_i32, c_p, c_p, c_p, c_i32,
                                         c_p, c_p, c_p, c_p, c_sz, c_p]
     L.pctc_grouped_backward.restype = c_i32
+    L.pctc_frame_candidates_workspace_size.argtypes = [c_i32, c_i32, c_i32, c_i32, c_i32]
+    L.pctc_frame_candidates_workspace_size.restype = c_sz
+    L.pctc_frame_candidates.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_i32, c_i32, c_p, c_p, c_p, c_p, c_sz,
+                                        c_p]
+    L.pctc_frame_candidates.restype = c_i32
+    L.pctc_beam_state_bytes.argtypes = [c_i32, c_i32, c_i32]
+    L.pctc_beam_state_bytes.restype = c_sz
+    L.pctc_beam_reset.argtypes = [c_i32, c_i32, c_i32, c_p, c_sz, c_p]
+    L.pctc_beam_reset.restype = c_i32
+    L.pctc_beam_advance.argtypes = [c_p, c_p, c_p, c_i32, i32p, c_i32, c_i32, c_i32, c_f, i32p, c_p, c_sz, c_p, c_p]
+    L.pctc_beam_advance.restype = c_i32
+    L.pctc_beam_result.argtypes = [c_i32, c_i32, c_i32, c_p, c_sz, c_i32, c_p, c_p, c_p, c_p]
+    L.pctc_beam_result.restype = c_i32
+    L.pctc_beam_reorder.argtypes = [c_i32, c_p, c_p, c_p, c_p, c_i32, c_i32, c_p]
+    L.pctc_beam_reorder.restype = c_i32
+    L.pctc_beam_decode_workspace_size.argtypes = [c_i32, i32p, c_i32, c_i32, c_i32, c_i32, c_i32]
+    L.pctc_beam_decode_workspace_size.restype = c_sz
+    L.pctc_beam_decode.argtypes = [c_i32, c_p, c_i32, c_p, c_p, c_i32, i32p, c_i32, c_i32, c_i32, c_i32, c_f, c_i32, c_p,
+                                   c_p, c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
+    L.pctc_beam_decode.restype = c_i32
+    L.pctc_clip_workspace_size.argtypes = [c_i32]
+    L.pctc_clip_workspace_size.restype = c_sz
+    L.pctc_clip_grad_norm.argtypes = [c_i32, c_p, c_p, c_p, c_p, c_f, c_p, c_p, c_p, c_sz, c_p]
+    L.pctc_clip_grad_norm.restype = c_i32
     L.pctc_prof_enable.argtypes = [c_i32]
     L.pctc_prof_select.argtypes = [ctypes.c_char_p]
     L.pctc_prof_reset.argtypes = []
@@ -571,6 +598,238 @@ class GroupedHead(torch.autograd.Function):
 
 def grouped_head(H: torch.Tensor, W: torch.Tensor, u_ids: torch.Tensor, bias: Optional[torch.Tensor] = None):
     return GroupedHead.apply(H, W, bias, u_ids)
+
+
+# ---- readout with beams ------------------------------------------------------------------
+
+def _asynchronous(fn):
+    """For calls that return before the device is done: with stream=..., the whole call, its
+    allocations among it, is made on that stream, so that memory it lets go of is not handed out
+    to another stream while the kernels still use it."""
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
+    return call
+
+
+def _head_args(H: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]):
+    """Checked and contiguous H, W and bias of a readout, and the library's type code."""
+    dt = _dtype_code(H)
+    if W.dtype != H.dtype:
+        raise PrunedCTCError(-1, "H and W must have the same dtype")
+    if not (H.is_cuda and W.device == H.device):
+        raise PrunedCTCError(-1, "H and W must be tensors of one device")
+    if H.dim() != 2 or W.dim() != 2 or H.shape[1] != W.shape[1]:
+        raise PrunedCTCError(-1, "H must be [M, D] and W [V, D]")
+    if bias is not None:
+        bias = _bias_vector(bias, int(W.shape[0]), H.device)
+    return H.contiguous(), W.contiguous(), bias, dt
+
+
+@_asynchronous
+def frame_candidates(H: torch.Tensor, W: torch.Tensor, candidates: int, blank: int = 0,
+                     bias: Optional[torch.Tensor] = None, *, stream=None) -> Dict[str, torch.Tensor]:
+    """The most probable classes of every frame other than blank, by falling log probability over
+    the full vocabulary: ids [M, C] (int32; -1 past the classes of non-zero probability), logp
+    [M, C] and blank_logp [M] (float32)."""
+    L = lib()
+    H, W, bias, dt = _head_args(H, W, bias)
+    M, D = H.shape
+    V, C, dev = int(W.shape[0]), int(candidates), H.device
+    nbytes = int(L.pctc_frame_candidates_workspace_size(dt, M, D, V, C))
+    if nbytes == 0:
+        _check(-1, "pctc_frame_candidates")
+    ids = torch.empty((M, C), dtype=torch.int32, device=dev)
+    logp = torch.empty((M, C), dtype=torch.float32, device=dev)
+    blank_logp = torch.empty(M, dtype=torch.float32, device=dev)
+    ws = _workspace(nbytes, dev)
+    code = L.pctc_frame_candidates(dt, _ptr(H), M, D, _ptr(W), _ptr(bias), V, int(blank), C, _ptr(ids), _ptr(logp),
+                                   _ptr(blank_logp), ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()),
+                                   _stream(None))
+    _check(code, "pctc_frame_candidates")
+    return {"ids": ids, "logp": logp, "blank_logp": blank_logp}
+
+
+class BeamSearch:
+    """CTC prefix beam search of N utterances (or live streams) with up to beam_size prefixes
+    each, on candidate classes as frame_candidates gives them; the state stays on the device.
+
+    max_frames bounds the frames an utterance may have in all (memory: 12 bytes a frame and
+    beam).  token_bonus is added to a prefix's score per label (negative: a penalty).  Calls are
+    asynchronous on the current stream (or `stream`), and one search's calls belong on one stream."""
+
+    @_asynchronous
+    def __init__(self, N: int, beam_size: int, max_frames: int, token_bonus: float = 0.0, device=None, *, stream=None):
+        self.N, self.beam_size, self.max_frames = int(N), int(beam_size), int(max_frames)
+        self.token_bonus = float(token_bonus)
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        nbytes = int(lib().pctc_beam_state_bytes(self.N, self.beam_size, self.max_frames))
+        if nbytes == 0:
+            _check(-1, "pctc_beam_state_bytes")
+        self._state = _workspace(nbytes, self.device)
+        self._done = np.zeros(max(self.N, 1), np.int32)
+        self.reset()
+
+    @property
+    def frames_done(self) -> np.ndarray:
+        """Frames that each utterance has had since the reset."""
+        return self._done[:self.N].copy()
+
+    def _mem(self):
+        return ctypes.c_void_p(self._state.data_ptr()), ctypes.c_size_t(self._state.numel())
+
+    @_asynchronous
+    def reset(self, *, stream=None) -> None:
+        """Starts every utterance anew with the empty prefix."""
+        mem, size = self._mem()
+        _check(lib().pctc_beam_reset(self.N, self.beam_size, self.max_frames, mem, size, _stream(None)),
+               "pctc_beam_reset")
+        self._done[:] = 0
+
+    @_asynchronous
+    def advance(self, ids: torch.Tensor, logp: torch.Tensor, blank_logp: torch.Tensor, frames: Sequence[int],
+                *, stream=None) -> torch.Tensor:
+        """frames[n] more frames of utterance n (0: none), packed utterance after utterance: ids and
+        logp [sum frames, C], blank_logp [sum frames].  Returns parents [N, beam_size] (int32): the
+        beam before the call that each beam descends from, -1 where there is no prefix (for
+        beam_reorder)."""
+        fr = _host_i32(frames)
+        if fr.shape != (self.N,):
+            raise PrunedCTCError(-1, f"frames must have {self.N} entries")
+        M = int(fr.sum(dtype=np.int64))
+        if logp.dim() != 2 or logp.shape[0] != M or ids.shape != logp.shape or tuple(blank_logp.shape) != (M,):
+            raise PrunedCTCError(-1, f"ids and logp must be [{M}, C] and blank_logp [{M}]")
+        if any(t.device != self.device for t in (ids, logp, blank_logp)):
+            raise PrunedCTCError(-1, f"candidates must be on {self.device}")
+        ids = ids.to(torch.int32).contiguous()
+        logp = logp.to(torch.float32).contiguous()
+        blank_logp = blank_logp.to(torch.float32).contiguous()
+        parents = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=self.device)
+        mem, size = self._mem()
+        code = lib().pctc_beam_advance(_ptr(ids), _ptr(logp), _ptr(blank_logp), int(logp.shape[1]), _i32p(fr), self.N,
+                                       self.beam_size, self.max_frames, self.token_bonus, _i32p(self._done), mem, size,
+                                       _ptr(parents), _stream(None))
+        _check(code, "pctc_beam_advance")
+        return parents
+
+    @_asynchronous
+    def result(self, max_tokens: Optional[int] = None, *, stream=None) -> Dict[str, torch.Tensor]:
+        """The prefixes so far, best first: tokens [N, beam_size, max_tokens] (int32, -1 past the
+        end; by default as many as the utterance with most frames so far could have),
+        token_lengths [N, beam_size] (int32, -1: no prefix) and scores [N, beam_size] (float32)."""
+        if max_tokens is None:
+            max_tokens = int(self._done.max())
+        tokens = torch.empty((self.N, self.beam_size, int(max_tokens)), dtype=torch.int32, device=self.device)
+        lengths = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=self.device)
+        scores = torch.empty((self.N, self.beam_size), dtype=torch.float32, device=self.device)
+        mem, size = self._mem()
+        code = lib().pctc_beam_result(self.N, self.beam_size, self.max_frames, mem, size, int(max_tokens), _ptr(tokens),
+                                      _ptr(lengths), _ptr(scores), _stream(None))
+        _check(code, "pctc_beam_result")
+        return {"tokens": tokens, "token_lengths": lengths, "scores": scores}
+
+
+def _ptr_array(tensors):
+    return (ctypes.c_void_p * max(len(tensors), 1))(*[t.data_ptr() for t in tensors])
+
+
+@_asynchronous
+def beam_reorder(states: Sequence[torch.Tensor], parents: torch.Tensor, out: Optional[Sequence[torch.Tensor]] = None,
+                 *, stream=None):
+    """Per-beam state tensors [N, K, ...] of any type in the order of the surviving beams: state[n, k]
+    becomes state[n, parents[n, k]] (a parent outside [0, K) leaves it).  In place, or into the
+    tensors `out`; returns those written.  Tensors must be contiguous."""
+    if parents.dim() != 2 or parents.dtype != torch.int32 or not parents.is_cuda:
+        raise PrunedCTCError(-1, "parents must be a device int32 [N, K]")
+    N, K = parents.shape
+    parents = parents.contiguous()
+    dest = states if out is None else out
+    if len(dest) != len(states):
+        raise PrunedCTCError(-1, "out must have a tensor for each state")
+    for t, o in zip(states, dest):
+        if t.dim() < 2 or tuple(t.shape[:2]) != (N, K):
+            raise PrunedCTCError(-1, f"a state must be [{N}, {K}, ...]")
+        if o.shape != t.shape or o.dtype != t.dtype:
+            raise PrunedCTCError(-1, "out must have the states' shapes and types")
+        if any(not x.is_contiguous() or x.device != parents.device for x in (t, o)):
+            raise PrunedCTCError(-1, f"states must be contiguous tensors on {parents.device}")
+    n = max(len(states), 1)
+    sizes = (ctypes.c_int64 * n)(*[(t.numel() // max(N * K, 1)) * t.element_size() for t in states])
+    code = lib().pctc_beam_reorder(len(states), _ptr_array(states), None if out is None else _ptr_array(dest), sizes,
+                                   _ptr(parents), N, K, _stream(None))
+    _check(code, "pctc_beam_reorder")
+    return list(dest)
+
+
+@_asynchronous
+def beam_decode(H: torch.Tensor, W: torch.Tensor, input_lengths, beam_size: int = 8, candidates: int = 16,
+                blank: int = 0, bias: Optional[torch.Tensor] = None, token_bonus: float = 0.0,
+                max_tokens: Optional[int] = None, *, stream=None) -> Dict[str, torch.Tensor]:
+    """The beam_size best label sequences of each utterance under the head H W^T (+ bias): prefix beam
+    search over each frame's `candidates` most probable classes and blank.  Returns tokens [N,
+    beam_size, max_tokens] (by default the longest utterance's frames), token_lengths and scores [N,
+    beam_size] (see BeamSearch.result), and the candidates ids, logp, blank_logp (see
+    frame_candidates).  Asynchronous."""
+    L = lib()
+    H, W, bias, dt = _head_args(H, W, bias)
+    T = _host_i32(input_lengths)
+    N, (M, D), V, K, C, dev = int(T.size), H.shape, int(W.shape[0]), int(beam_size), int(candidates), H.device
+    if int(T.sum(dtype=np.int64)) != M:
+        raise PrunedCTCError(-1, "sum of input lengths differs from the rows of H")
+    nbytes = int(L.pctc_beam_decode_workspace_size(dt, _i32p(T), N, D, V, K, C))
+    if nbytes == 0:
+        _check(-3 if (T < 1).any() else -1, "pctc_beam_decode")
+    if max_tokens is None:
+        max_tokens = int(T.max()) if N else 0
+    i32 = dict(dtype=torch.int32, device=dev)
+    f32 = dict(dtype=torch.float32, device=dev)
+    out = {"tokens": torch.empty((N, K, int(max_tokens)), **i32), "token_lengths": torch.empty((N, K), **i32),
+           "scores": torch.empty((N, K), **f32), "ids": torch.empty((M, C), **i32),
+           "logp": torch.empty((M, C), **f32), "blank_logp": torch.empty(M, **f32)}
+    ws = _workspace(nbytes, dev)
+    code = L.pctc_beam_decode(dt, _ptr(H), D, _ptr(W), _ptr(bias), V, _i32p(T), N, int(blank), K, C, float(token_bonus),
+                              int(max_tokens), _ptr(out["tokens"]), _ptr(out["token_lengths"]), _ptr(out["scores"]),
+                              _ptr(out["ids"]), _ptr(out["logp"]), _ptr(out["blank_logp"]),
+                              ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), _stream(None))
+    _check(code, "pctc_beam_decode")
+    return out
+
+
+# ---- training step -----------------------------------------------------------------------
+
+@_asynchronous
+def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None,
+                   *, stream=None) -> Dict[str, torch.Tensor]:
+    """The global 2-norm over a list of float32 and bfloat16 gradients, and every gradient scaled by
+    min(1, max_norm / (norm + 1e-6)), in place or into the tensors `out`.  Returns norm and scale
+    (float32 [1], on the device).  A norm that is not finite scales by 1: test it before the step.
+    Tensors must be contiguous."""
+    grads = list(grads)
+    if not grads:
+        raise PrunedCTCError(-1, "no gradients")
+    dev = grads[0].device
+    dest = grads if out is None else list(out)
+    if len(dest) != len(grads):
+        raise PrunedCTCError(-1, "out must have a tensor for each gradient")
+    for g, o in zip(grads, dest):
+        if not (g.is_cuda and g.device == dev and o.device == dev and g.is_contiguous() and o.is_contiguous()):
+            raise PrunedCTCError(-1, "gradients must be contiguous tensors of one device")
+        if o.dtype != g.dtype or o.numel() != g.numel():
+            raise PrunedCTCError(-1, "out must have the gradients' types and sizes")
+    n = len(grads)
+    codes = (ctypes.c_int32 * n)(*[_dtype_code(g) for g in grads])
+    sizes = (ctypes.c_int64 * n)(*[g.numel() for g in grads])
+    L = lib()
+    res = torch.empty(2, dtype=torch.float32, device=dev)
+    ws = _workspace(int(L.pctc_clip_workspace_size(n)), dev)
+    code = L.pctc_clip_grad_norm(n, _ptr_array(grads), None if out is None else _ptr_array(dest), sizes, codes,
+                                 float(max_norm), _ptr(res), ctypes.c_void_p(res.data_ptr() + 4),
+                                 ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), _stream(None))
+    _check(code, "pctc_clip_grad_norm")
+    return {"norm": res[:1], "scale": res[1:]}
 
 
 # ---- kernel timing -----------------------------------------------------------------------

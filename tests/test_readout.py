@@ -1,0 +1,209 @@
+"""Readout with beams and gradient clipping, without a GPU: the 64-bit reference search against
+enumeration of all alignments, and the library's host-side argument checks and sizes."""
+import ctypes
+import itertools
+import math
+import os
+
+import numpy as np
+import pytest
+
+from tests import readout_ref as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_2609_33645_amd", "libprunedctc.so")
+built = pytest.mark.skipif(not os.path.exists(LIB), reason="library not built")
+
+
+def collapse(path, blank):
+    out, prev = [], None
+    for c in path:
+        if c != prev and c != blank:
+            out.append(c)
+        prev = c
+    return tuple(out)
+
+
+@pytest.mark.parametrize("T,V,bonus", [(1, 3, 0.0), (3, 3, 0.0), (5, 3, -0.7), (4, 4, 0.3)])
+def test_reference_search_is_the_sum_over_alignments(T, V, bonus):
+    """With room for every prefix, a prefix's score is the log mass of all alignments that collapse
+    to it (Sec. 3.1), plus the bonus of its labels."""
+    rng = np.random.default_rng(T * 10 + V)
+    z = rng.normal(size=(T, V)) * 2
+    ids, logp, blank = ref.candidates(z, V - 1, 0)
+    lp = z - np.log(np.exp(z).sum(1, keepdims=True))
+    mass = {}
+    for path in itertools.product(range(V), repeat=T):
+        y = collapse(path, 0)
+        mass[y] = mass.get(y, 0.0) + math.exp(sum(lp[t, c] for t, c in enumerate(path)))
+    got = dict(ref.Search(10 ** 6, bonus).run(ids, logp, blank).result())
+    assert set(got) == set(mass)
+    for y, p in mass.items():
+        assert got[y] == pytest.approx(math.log(p) + bonus * len(y), abs=1e-12)
+
+
+def test_reference_search_by_hand():
+    """K = 1 on two frames: the better of blank and label a at each frame, then merged mass."""
+    s = ref.Search(1)
+    s.step([5], [math.log(0.6)], math.log(0.4))
+    assert s.result() == [((5,), pytest.approx(math.log(0.6)))]
+    s.step([5], [math.log(0.5)], math.log(0.5))
+    assert s.result()[0][1] == pytest.approx(math.log(0.6))  # stays by blank and by its label
+
+
+def _lib():
+    import torch  # noqa: F401
+    from paper_2609_33645_amd import prunedctc
+    return prunedctc.lib()
+
+
+OK = 0x7f0000000000  # an aligned stand-in; never dereferenced where a check refuses the call
+
+
+def i32(*xs):
+    return np.array(xs, np.int32)
+
+
+def p(a):
+    return a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+
+@built
+def test_sizes():
+    L = _lib()
+    up = lambda x: (x + 255) // 256 * 256  # noqa: E731
+    assert L.pctc_beam_state_bytes(0, 8, 100) > 0
+    for bad in ((-1, 8, 100), (1, 0, 100), (1, 33, 100), (1, 8, -1), (1, 8, 1 << 28), ((1 << 24) + 1, 1, 1)):
+        assert L.pctc_beam_state_bytes(*bad) == 0, bad
+    # three masses, two hashes and four indices a beam; an offset an utterance; 12 bytes a frame and beam
+    nk = 3 * 8
+    assert L.pctc_beam_state_bytes(3, 8, 100) == \
+        7 * up(nk * 4) + 2 * up(nk * 8) + up(24) + up(nk * 100 * 8) + up(nk * 100 * 4)
+    assert L.pctc_clip_workspace_size(-1) == 0 and L.pctc_clip_workspace_size(0) > 0
+    c = L.pctc_frame_candidates_workspace_size
+    assert c(1, 0, 512, 180_000, 16) > 0
+    for bad in ((2, 4, 512, 1000, 16), (1, -1, 512, 1000, 16), (1, 4, 500, 1000, 16), (1, 4, 512, 1, 16),
+                (1, 4, 512, 1000, 0), (1, 4, 512, 1000, 65), (1, 4, 512, 524_289, 16)):
+        assert c(*bad) == 0, bad
+    # the block maxima are held to 256 MiB: more frames take more passes, not more memory (the
+    # normaliser's partial sums grow with the frames of a pass alone)
+    for D in (512, 4096):
+        assert c(1, 400_000, D, 180_000, 16) == c(0, 100_000, D, 180_000, 64) < (256 << 20) + 12_000 * 8 * 1030
+    d = L.pctc_beam_decode_workspace_size
+    T = i32(30, 20)
+    assert d(1, p(T), 2, 512, 1000, 8, 16) > c(1, 50, 512, 1000, 16)
+    assert d(1, p(i32(0, 20)), 2, 512, 1000, 8, 16) == 0
+    for bad in ((1, 2, 512, 1000, 0, 16), (1, 2, 512, 1000, 33, 16), (1, 2, 512, 1000, 8, 65), (1, -1, 512, 1000, 8, 16)):
+        assert d(bad[0], p(T), *bad[1:]) == 0, bad
+    assert d(1, p(T), 0, 512, 1000, 8, 16) > 0
+
+
+@built
+def test_candidates_refusals():
+    L = _lib()
+    big = 1 << 40
+
+    def call(dt=1, H=OK, M=4, D=64, W=OK, V=100, blank=0, C=8, ids=OK, logp=OK, bl=OK, ws=OK, n=big):
+        return L.pctc_frame_candidates(dt, H, M, D, W, None, V, blank, C, ids, logp, bl, ws, n, None)
+    for kw in (dict(dt=2), dict(H=OK + 8), dict(W=OK + 8), dict(W=None), dict(H=None), dict(M=-1), dict(D=60), dict(V=1),
+               dict(blank=-1), dict(blank=100), dict(C=0), dict(C=65), dict(ids=None), dict(logp=None), dict(bl=None),
+               dict(ws=OK + 16)):
+        assert call(**kw) == -1, kw
+    assert call(ws=None) == -4 and call(n=16) == -4
+    assert call(M=0, H=None, ids=None, logp=None, bl=None, ws=None) == 0
+
+
+@built
+def test_beam_refusals():
+    L = _lib()
+    big = 1 << 40
+    done = i32(0, 95)
+
+    def adv(ids=OK, logp=OK, bl=OK, C=8, frames=i32(3, 4), N=2, K=4, cap=100, bonus=0.0, dn=done, state=OK, n=big):
+        return L.pctc_beam_advance(ids, logp, bl, C, p(frames) if frames is not None else None, N, K, cap, bonus,
+                                   p(dn) if dn is not None else None, state, n, None, None)
+    for kw in (dict(ids=None), dict(logp=None), dict(bl=None), dict(C=0), dict(C=65), dict(N=-1), dict(K=0), dict(K=33),
+               dict(cap=-1), dict(bonus=math.nan), dict(bonus=math.inf), dict(frames=None), dict(dn=None),
+               dict(state=OK + 16)):
+        assert adv(**kw) == -1, kw
+    assert adv(state=None) == -4 and adv(n=64) == -4
+    for frames in (i32(-1, 2), i32(3, 6), i32(101, 0), i32(0, 2 ** 31 - 1)):
+        assert adv(frames=frames) == -3, frames
+    assert adv(dn=i32(-1, 0)) == -3
+    assert done.tolist() == [0, 95]  # refused calls count no frames
+    assert adv(N=0, frames=None, dn=None, state=None) == 0
+    assert L.pctc_beam_reset(2, 4, 100, None, big, None) == -4 and L.pctc_beam_reset(2, 40, 100, OK, big, None) == -1
+    assert L.pctc_beam_reset(0, 4, 100, None, 0, None) == 0
+
+    def res(N=2, K=4, cap=100, state=OK, n=big, mt=10, tokens=OK, lengths=OK, scores=OK):
+        return L.pctc_beam_result(N, K, cap, state, n, mt, tokens, lengths, scores, None)
+    for kw in (dict(mt=-1), dict(tokens=None), dict(lengths=None), dict(scores=None), dict(K=0), dict(state=OK + 8)):
+        assert res(**kw) == -1, kw
+    assert res(state=None) == -4 and res(N=0, state=None) == 0
+
+
+@built
+def test_decode_refusals():
+    L = _lib()
+    T = i32(30, 20)
+
+    def call(dt=1, H=OK, D=64, W=OK, V=100, T=T, N=2, blank=0, K=4, C=8, bonus=0.0, mt=10, tokens=OK, lengths=OK,
+             scores=OK, ws=OK, n=1 << 40):
+        return L.pctc_beam_decode(dt, H, D, W, None, V, p(T) if T is not None else None, N, blank, K, C, bonus, mt, tokens,
+                                  lengths, scores, None, None, None, ws, n, None)
+    for kw in (dict(dt=3), dict(H=None), dict(H=OK + 4), dict(D=0), dict(W=None), dict(V=1), dict(T=None), dict(N=-1),
+               dict(blank=100), dict(K=0), dict(K=33), dict(C=0), dict(C=65), dict(bonus=math.nan), dict(mt=-1),
+               dict(tokens=None), dict(lengths=None), dict(scores=None), dict(ws=OK + 64)):
+        assert call(**kw) == -1, kw
+    assert call(T=i32(0, 4)) == -3 and call(ws=None) == -4 and call(n=100) == -4
+    assert call(N=0, T=None) == 0
+
+
+@built
+def test_reorder_and_clip_refusals():
+    L = _lib()
+    vp = lambda *xs: (ctypes.c_void_p * max(len(xs), 1))(*xs)  # noqa: E731
+    i64 = lambda *xs: (ctypes.c_int64 * max(len(xs), 1))(*xs)  # noqa: E731
+    r = L.pctc_beam_reorder
+    assert r(-1, vp(OK), None, i64(4), OK, 2, 4, None) == -1
+    assert r(1, None, None, i64(4), OK, 2, 4, None) == -1 and r(1, vp(OK), None, None, OK, 2, 4, None) == -1
+    assert r(1, vp(OK), None, i64(-4), OK, 2, 4, None) == -1 and r(1, vp(None), None, i64(4), OK, 2, 4, None) == -1
+    assert r(1, vp(OK), vp(None), i64(4), OK, 2, 4, None) == -1 and r(1, vp(OK), None, i64(4), None, 2, 4, None) == -1
+    assert r(1, vp(OK), None, i64(4), OK, 2, 0, None) == -1 and r(1, vp(OK), None, i64(4), OK, 2, 33, None) == -1
+    assert r(1, vp(OK), None, i64((1 << 36) + 1), OK, 2, 4, None) == -1
+    assert r(0, None, None, None, None, 2, 4, None) == 0 and r(1, vp(None), None, i64(0), None, 2, 4, None) == 0
+    assert r(1, vp(OK), None, i64(4), None, 0, 4, None) == 0
+    c = L.pctc_clip_grad_norm
+    f32, bf = (ctypes.c_int32 * 1)(0), (ctypes.c_int32 * 1)(1)
+    big = 1 << 30
+    assert c(-1, vp(OK), None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1
+    for bad in (math.nan, -1.0):
+        assert c(1, vp(OK), None, i64(4), f32, bad, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), None, i64(4), f32, 1.0, None, None, OK, big, None) == -1
+    assert c(1, None, None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), None, i64(4), (ctypes.c_int32 * 1)(2), 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), None, i64(-1), f32, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), None, i64((1 << 36) + 1), f32, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(None), None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), vp(None), i64(4), f32, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK + 2), None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1  # off its type's alignment
+    assert c(1, vp(OK), vp(OK + 1), i64(4), bf, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), None, i64(4), f32, 1.0, OK, None, None, big, None) == -4
+    assert c(1, vp(OK), None, i64(4), f32, 1.0, OK, None, OK, 16, None) == -4
+    assert c(1, vp(OK), None, i64(4), f32, 1.0, OK, None, OK + 8, big, None) == -1
+
+
+@built
+def test_binding_refusals():
+    """The binding refuses what it can see without a device."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    x = torch.zeros(4, 8)
+    for call in (lambda: pc.frame_candidates(x, x, 2), lambda: pc.beam_decode(x, x, [4]),
+                 lambda: pc.clip_grad_norm([x], 1.0), lambda: pc.clip_grad_norm([], 1.0),
+                 lambda: pc.beam_reorder([x], torch.zeros(2, 2, dtype=torch.int32)),
+                 lambda: pc.frame_candidates(x.half(), x.half(), 2)):
+        with pytest.raises(pc.PrunedCTCError) as e:
+            call()
+        assert e.value.code == -1
