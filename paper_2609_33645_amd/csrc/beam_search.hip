@@ -11,13 +11,17 @@
 //           else s;  pb' = -inf
 // The K largest totals are kept, ties in the order: staying beams, then grown ones by (beam, class).
 //
-// What bounds it: a chain of dependent frames, each a chain of K selections; memory and arithmetic
-// are negligible.  One wavefront per utterance keeps everything in registers: lane i holds beam
-// i mod KT; lanes [0, KT) offer the staying beams, lanes [KT, 2 KT) the best class by which their beam
-// can still grow (the classes come sorted, so a beam's next best is the next bit of a mask of
-// classes, and only 2 KT values take part in a selection whatever C is).  Prefixes are compared by
-// 64-bit hashes of their labels and their lengths: two different ones meet with a probability of
-// about K^2 / 2^65 per frame.
+// What bounds it: a chain of dependent frames; memory and arithmetic are negligible.  One wavefront per
+// utterance holds the beams in registers (lane l: beam l mod KT, the copies share out the comparisons
+// over classes and beams), and every exchange is a cross-lane move or a wavefront's own LDS.
+// Of the K (C + 1) totals few have to be looked at.  Beams and classes come sorted: with beam i (from 0)
+// and class c (from 0), all of i' <= i, c' <= c but a beam's own last label have totals no smaller, as
+// prefixes of their own, so that (i, c) can only be kept where (i + 1) c <= K (28 pairs for K = 8, 66 for
+// 16, 151 for 32); and where all K beams can stay, only pairs above the least of their totals.  These
+// few are ordered by counting, each lane the totals above its own.  A frame that none of them enters and
+// that leaves the order as it is (most frames, where a head is sure) moves nothing.
+// Prefixes are compared by 64-bit hashes of their labels and their lengths: two different ones meet
+// with a probability of about K^2 / 2^65 per frame.
 #include <algorithm>
 #include <type_traits>
 
@@ -36,31 +40,41 @@ __device__ __forceinline__ float log_add(float a, float b) {
   return hi + kLn2 * fast_log2(1.f + fast_exp2((lo - hi) * kLog2e));
 }
 
-__device__ __forceinline__ uint64_t grow_hash(uint64_t h, int label) {
-  h = (h ^ static_cast<uint32_t>(label + 1)) * 0x9fb21c651e98df25ull;
-  h ^= h >> 29;
-  h = h * 0xd6e8feb86659fd93ull + 0x2545f4914f6cdd1dull;
+// The hash of a prefix with one more label.
+__device__ __forceinline__ uint64_t grow_hash(uint64_t hash, int label) {
+  uint64_t h = static_cast<uint32_t>(label + 1) * 0x9fb21c651e98df25ull;
+  h = (h ^ (h >> 29)) * 0xd6e8feb86659fd93ull;
+  h = (hash + (h ^ (h >> 32))) * 0x2545f4914f6cdd1dull;
   return h ^ (h >> 32);
 }
 
 __device__ __forceinline__ float lane_f(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
 }
+__device__ __forceinline__ uint64_t from_lane(uint64_t x, int lane) {
+  const uint32_t lo = __shfl(static_cast<int>(x), lane, 64), hi = __shfl(static_cast<int>(x >> 32), lane, 64);
+  return (static_cast<uint64_t>(hi) << 32) | lo;
+}
 
-// Maximum over lanes [0, W), W = 8, 16, 32 or 64, in every lane.
+// The value of the lane below in the row of 16 (the first lane of a row keeps its own).
+__device__ __forceinline__ float lane_below(float x) {
+  return __int_as_float(
+      __builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), 0x111, 0xf, 0xf, false));
+}
+
+// Minimum over lanes [0, W), W = 4, 8, 16 or 32.
 template <int W>
-__device__ __forceinline__ float lanes_max(float x) {
+__device__ __forceinline__ float lanes_min(float x) {
   auto step = [&](auto ctrl) {
     const int v = __builtin_amdgcn_update_dpp(__float_as_int(x), __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf,
                                               false);
-    x = fmaxf(x, __int_as_float(v));
+    x = fminf(x, __int_as_float(v));
   };
   step(std::integral_constant<int, 0x111>{});  // from one, two, four, eight lanes below in the row of 16
   step(std::integral_constant<int, 0x112>{});
-  step(std::integral_constant<int, 0x114>{});
+  if constexpr (W >= 8) step(std::integral_constant<int, 0x114>{});
   if constexpr (W >= 16) step(std::integral_constant<int, 0x118>{});
   if constexpr (W >= 32) step(std::integral_constant<int, 0x142>{});  // a row's last lane to the next row
-  if constexpr (W >= 64) step(std::integral_constant<int, 0x143>{});  // lane 31 to the upper half
   return lane_f(x, W - 1);
 }
 
@@ -134,18 +148,28 @@ __global__ void __launch_bounds__(64)
 beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restrict__ ids,
                     const float* __restrict__ logp, const float* __restrict__ blank_logp, float bonus, BeamFields f,
                     int32_t* __restrict__ parents) {
-  __shared__ float lp_s[64];
-  __shared__ int32_t id_s[64];
-  const int lane = threadIdx.x, i = lane & (KT - 1);
-  const bool stays = lane < KT, grows = lane >= KT && lane < 2 * KT;
+  constexpr int kCopies = 64 / KT;                        // lanes of a beam
+  constexpr int kPairs = KT <= 8 ? 1 : KT <= 16 ? 2 : 3;  // (beam, class) pairs a lane looks at
+  constexpr int kEntries = KT + 64 * kPairs;
+  constexpr uint64_t kEvery = KT == 4 ? 0x1111111111111111ull : KT == 8 ? 0x0101010101010101ull
+                              : KT == 16 ? 0x0001000100010001ull : 0x0000000100000001ull;  // a beam's lanes
+  __shared__ float lp_s[2][64];       // this frame's classes and the next one's
+  __shared__ __attribute__((aligned(16))) int32_t id_s[2][64];
+  __shared__ int first_s[KT + 1];     // pairs of the beams before
+  __shared__ int merged_s[64 * kPairs];  // frame (from 1) in which a pair's prefix was last a beam
+  __shared__ __attribute__((aligned(16))) float val_s[kEntries + 4];  // totals to be ordered: staying beams, pairs
+  __shared__ int what_s[kEntries];    // of a pair: beam + 256 class
+  __shared__ int place_s[KT];         // entry of each place
+  const int lane = threadIdx.x, i = lane & (KT - 1), copy = lane / KT;
   const int n = n0 + blockIdx.x;
   const int t0 = rows.off[blockIdx.x], t1 = rows.off[blockIdx.x + 1];
-  int frame = rows.done[blockIdx.x];  // frames before this one
+  const int done = rows.done[blockIdx.x];  // frames before this call
   const int64_t at = static_cast<int64_t>(n) * K + i;
+  const bool mine = i < K;
   float pb = kNegInf, pn = kNegInf, s = kNegInf;
   uint64_t hash = 0, phash = 0;
   int last = -2, len = -2, node = -1, ck = -1;
-  if (i < K) {
+  if (mine) {
     pb = f.pb[at];
     pn = f.pn[at];
     s = f.s[at];
@@ -161,8 +185,43 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   double offset = f.offset[n];
   int origin = i;
 
+  // the pairs that can be kept: classes c <= K / (i + 1) of beam i, beam by beam
+  int first = 0, pairs;  // pairs of the beams before, and of all
+  {
+    // (a quotient that is no whole number is at least 1/32 away from one)
+    const int here = lane < K ? min(C, static_cast<int>(static_cast<float>(K) / static_cast<float>(lane + 1) + 0.01f) + 1)
+                              : 0;
+    int sum = here;
+#pragma unroll
+    for (int o = 1; o < KT; o <<= 1) {
+      const int v = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += v;
+    }
+    pairs = __builtin_amdgcn_readlane(sum, K - 1);
+    first = sum - here;
+    if (lane < K) first_s[lane] = first;
+    if (lane == 0) first_s[K] = pairs;
+  }
+  int pi[kPairs], pc[kPairs];  // beam and class of this lane's pairs (beam -1: none)
+#pragma unroll
+  for (int q = 0; q < kPairs; ++q) {
+    const int e = lane + 64 * q;
+    merged_s[e] = 0;
+    pi[q] = -1;
+    pc[q] = 0;
+    for (int k = 0; k < K; ++k) {
+      const int a = __builtin_amdgcn_readlane(first, k);
+      if (e >= a && e < pairs) {
+        pi[q] = k;
+        pc[q] = e - a;
+      }
+    }
+  }
+
   // a frame's classes, one a lane; a score that is no number counts as -inf
-  auto fetch = [&](int m, int& id, float& l, float& b) {
+  int id;
+  float l, b;
+  auto fetch = [&](int m) {
     id = -1;
     l = b = kNegInf;
     if (m >= t1) return;
@@ -171,98 +230,161 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       l = logp[static_cast<int64_t>(m) * C + lane];
     }
     b = blank_logp[m];
+  };
+  auto stage = [&](int buf) {
     if (id < 0 || !(l > kNegInf)) {
       id = -1;
       l = kNegInf;
     }
     if (!(b > kNegInf)) b = kNegInf;
+    lp_s[buf][lane] = l;
+    id_s[buf][lane] = id;
+    return b;
   };
-  int id, nid;
-  float l, b, nl, nb;
-  fetch(t0, id, l, b);
-  for (int m = t0; m < t1; ++m, ++frame) {
-    fetch(m + 1, nid, nl, nb);
-    lp_s[lane] = l;
-    id_s[lane] = id;
-    __builtin_amdgcn_wave_barrier();
-    const uint64_t offered = __ballot(id >= 0);
-    // where each beam's last label stands among the classes, which beam is its prefix without that
-    // label, and the classes by which a beam would grow into another
-    uint64_t skip = 0;
-    int pos = -1, par = -1;
-#pragma unroll 8
-    for (int j = 0; j < KT; ++j) {
-      const int lj = __builtin_amdgcn_readlane(last, j), nj = __builtin_amdgcn_readlane(len, j);
-      const uint32_t hl = __builtin_amdgcn_readlane(static_cast<uint32_t>(phash), j);
-      const uint32_t hh = __builtin_amdgcn_readlane(static_cast<uint32_t>(phash >> 32), j);
-      const uint64_t pm = __ballot(id == lj);
-      const bool into = len + 1 == nj && hash == ((static_cast<uint64_t>(hh) << 32) | hl) && i != j;
-      const uint64_t im = __ballot(into) & ((uint64_t{1} << KT) - 1);
-      if (into) skip |= pm;
-      if (i == j) {
-        pos = pm ? __builtin_ctzll(pm) : -1;
-        par = im ? __builtin_ctzll(im) : -1;
-      }
+  // the beam whose prefix is this beam's without its last label
+  auto find_parent = [&]() {
+    int found = -1;
+#pragma unroll
+    for (int q = 0; q < (KT + kCopies - 1) / kCopies; ++q) {
+      const int o = q * kCopies + copy;
+      const uint64_t h = from_lane(hash, o & (KT - 1));
+      const int ln = __shfl(len, o & (KT - 1), 64);
+      if (o < KT && ln + 1 == len && h == phash) found = o;
     }
-    const float l_last = pos >= 0 ? lp_s[pos] : kNegInf;
-    const int p = par >= 0 ? par : 0;
+    const uint64_t who = (__ballot(found >= 0) >> i) & kEvery;
+    return __shfl(found, (who ? __builtin_ctzll(who) & ~(KT - 1) : 0) + i, 64);
+  };
+
+  fetch(t0);
+  float bl = stage(t0 & 1);
+  fetch(t0 + 1);
+  __builtin_amdgcn_wave_barrier();
+  int par = find_parent();
+  for (int m = t0; m < t1; ++m) {
+    const int buf = m & 1;
+    const float b_now = bl;
+    bl = stage(buf ^ 1);
+    fetch(m + 2);
+    // what the pairs and the joining prefixes need of other beams
+    float ps[kPairs], ppb[kPairs], pl[kPairs];
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) {
+      ps[q] = __shfl(s, pi[q] & 63, 64);
+      ppb[q] = __shfl(pb, pi[q] & 63, 64);
+      pl[q] = lp_s[buf][pc[q]] + bonus;
+    }
+    const int p = par >= 0 ? par : i;
     const float pb_p = __shfl(pb, p, 64), s_p = __shfl(s, p, 64);
     const int last_p = __shfl(last, p, 64);
-    const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
-    const float sb = s + b, sn = log_add(pn + l_last, join);
-    // this lane's offer: a staying beam's total, or the best class left to grow by
-    const uint64_t own = pos >= 0 ? uint64_t{1} << pos : 0;
-    uint64_t left = grows ? offered & ~skip & ~own : 0;
-    float again = grows && (own & ~skip) ? pb + (l_last + bonus) : kNegInf;  // its last label once more
-    int rank = 0;
-    float val = kNegInf;
-    auto offer = [&]() {
-      const int r = left ? __builtin_ctzll(left) : 63;
-      const float v = left ? s + (lp_s[r] + bonus) : kNegInf;
-      const bool rep = again > v || (again == v && pos < r);
-      rank = rep ? pos : r;
-      val = rep ? again : v;
-    };
-    if (grows) offer();
-    if (stays) val = log_add(sb, sn);
-    float best = kNegInf, won = kNegInf;
-    int src = -1, wrank = 0;
-    for (int r = 0; r < K; ++r) {
-      const float top = lanes_max<2 * KT>(val);
-      const uint64_t who = __ballot(val == top) & (2 * KT == 64 ? ~uint64_t{0} : (uint64_t{1} << (2 * KT)) - 1);
-      if (!(top > kNegInf) || who == 0) break;
-      const int w = __builtin_ctzll(who);
-      const int wr = __builtin_amdgcn_readlane(rank, w);
-      if (r == 0) best = top;
-      if (i == r) {
-        src = w;
-        won = top;
-        wrank = wr;
-      }
-      if (lane == w) {
-        if (stays) {
-          val = kNegInf;
-        } else {
-          if (rank == pos) again = kNegInf;
-          else left &= left - 1;
-          offer();
-        }
-      }
+    // where the beam's last label stands among the classes
+    int pos = -1;
+#pragma unroll
+    for (int q = 0; q < KT; q += 4) {
+      const int4 v = *reinterpret_cast<const int4*>(&id_s[buf][copy * KT + q]);
+      pos = v.x == last ? copy * KT + q : pos;
+      pos = v.y == last ? copy * KT + q + 1 : pos;
+      pos = v.z == last ? copy * KT + q + 2 : pos;
+      pos = v.w == last ? copy * KT + q + 3 : pos;
     }
-    // the new beam i descends from beam src mod KT
-    const bool grown = src >= KT, live = src >= 0;
-    const int from = live ? src & (KT - 1) : 0;
-    const float f_sb = __shfl(sb, from, 64), f_sn = __shfl(sn, from, 64);
-    const uint64_t f_hash = __shfl(hash, from, 64), f_phash = __shfl(phash, from, 64);
-    const int f_last = __shfl(last, from, 64), f_len = __shfl(len, from, 64), f_node = __shfl(node, from, 64);
-    const int f_ck = __shfl(ck, from, 64), f_origin = __shfl(origin, from, 64);
-    if (!live) {
+    {
+      const uint64_t who = (__ballot(pos >= 0) >> i) & kEvery;
+      pos = __shfl(pos, (who ? __builtin_ctzll(who) & ~(KT - 1) : 0) + i, 64);
+    }
+    const float l_last = pos >= 0 ? lp_s[buf][pos] : kNegInf;
+    const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
+    const float sb = s + b_now, again = pn + l_last;
+    // pb' (+) pn' of a staying beam
+    const float top = fmaxf(sb, fmaxf(again, join));
+    const float total =
+        top > kNegInf ? top + kLn2 * fast_log2(fast_exp2((sb - top) * kLog2e) + fast_exp2((again - top) * kLog2e) +
+                                               fast_exp2((join - top) * kLog2e))
+                      : kNegInf;
+    const float sn = log_add(again, join);
+    // a pair whose prefix is a beam already is no new one
+    const bool joins = par >= 0 && pos >= 0;
+    if (__any(joins) && joins && copy == 0) {
+      const int e = first_s[par] + pos;
+      if (e < first_s[par + 1]) merged_s[e] = m - t0 + 1;
+    }
+    __builtin_amdgcn_wave_barrier();
+    const float least = lanes_min<KT>(mine ? total : INFINITY);
+    float pv[kPairs];
+    uint64_t enter[kPairs], any = 0;
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) {
+      const int own = __shfl(pos, pi[q] & 63, 64);
+      pv[q] = (own == pc[q] ? ppb[q] : ps[q]) + pl[q];
+      enter[q] = __ballot(pi[q] >= 0 && pv[q] > least && merged_s[lane + 64 * q] != m - t0 + 1);
+      any |= enter[q];
+    }
+    // no pair enters, no beam leaves, and their order stands
+    const float before = KT <= 16 ? lane_below(total) : __shfl(total, lane > 0 ? lane - 1 : 0, 64);
+    const bool moves = mine && ((i > 0 && total > before) || (len >= 0 && !(total > kNegInf)));
+    const float lead = lane_f(total, 0);
+    if (any == 0 && lead > kNegInf && __ballot(moves) == 0) {
+      pb = sb - lead;
+      pn = sn - lead;
+      s = total - lead;
+      offset += lead;
+      continue;
+    }
+
+    // the totals to be ordered, in the order of ties
+    int count = K;
+    if (copy == 0 && mine) val_s[i] = total;
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) {
+      if ((enter[q] >> lane) & 1) {
+        const int e = count + __popcll(enter[q] & ((uint64_t{1} << lane) - 1));
+        val_s[e] = pv[q];
+        what_s[e] = pi[q] + 256 * pc[q];
+      }
+      count += __popcll(enter[q]);
+    }
+    if (lane < 4) val_s[count + lane] = kNegInf;
+    __builtin_amdgcn_wave_barrier();
+    int live = 0;  // entries above -inf
+    for (int e0 = 0; e0 < count; e0 += 64) {
+      const int e = e0 + lane;
+      const float v = e < count ? val_s[e] : kNegInf;
+      int place = 0;
+      for (int o = 0; o < count; o += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(&val_s[o]);
+        place += (w.x > v) + (w.y > v) + (w.z > v) + (w.w > v);
+      }
+      const bool in = v > kNegInf;
+      live += __popcll(__ballot(in));
+      // equal totals land on one place: where someone finds another there (and past the first 64
+      // entries, whose places may be taken), the entries' order tells them apart
+      if (e0 == 0) {
+        if (in && place < K) place_s[place] = e;
+        __builtin_amdgcn_wave_barrier();
+      }
+      if (e0 > 0 || __any(in && place < K && place_s[place] != e)) {
+        for (int o = 0; o < e && in; ++o) place += val_s[o] == v;
+        if (in && place < K) place_s[place] = e;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    // the new beam i
+    const bool lives = i < min(live, K);
+    const int e = lives ? place_s[i] : 0;
+    const bool grown = lives && e >= K;
+    const int what = grown ? what_s[e] : e;
+    const int src = what & 255, c = grown ? what >> 8 : 0;
+    const float won = val_s[e];
+    const float best = live > 0 ? lane_f(won, 0) : 0.f;
+    const float f_sb = __shfl(sb, src, 64), f_sn = __shfl(sn, src, 64);
+    const uint64_t f_hash = from_lane(hash, src), f_phash = from_lane(phash, src);
+    const int f_last = __shfl(last, src, 64), f_len = __shfl(len, src, 64), f_node = __shfl(node, src, 64);
+    const int f_ck = __shfl(ck, src, 64), f_origin = __shfl(origin, src, 64);
+    if (!lives) {
       pb = pn = s = kNegInf;
       len = last = -2;
       origin = -1;
     } else {
-      const int label = id_s[wrank];
-      const int fresh = frame * K + i;
+      const int label = id_s[buf][c];
+      const int fresh = (done + m - t0) * K + i;
       pb = grown ? kNegInf : f_sb - best;
       pn = (grown ? won : f_sn) - best;
       s = won - best;
@@ -274,19 +396,17 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       ck = f_ck;
       origin = f_origin;
       if (grown) {
-        if (lane < KT) nodes[fresh] = make_int2(f_node, label);
+        if (copy == 0) nodes[fresh] = make_int2(f_node, label);
         if (len % kCkStep == 0) {
-          if (lane < KT) cks[fresh] = f_ck;
+          if (copy == 0) cks[fresh] = f_ck;
           ck = fresh;
         }
       }
     }
-    if (best > kNegInf) offset += best;
-    id = nid;
-    l = nl;
-    b = nb;
+    offset += best;
+    par = find_parent();
   }
-  if (lane < KT && i < K) {
+  if (copy == 0 && mine) {
     f.pb[at] = pb;
     f.pn[at] = pn;
     f.s[at] = s;
