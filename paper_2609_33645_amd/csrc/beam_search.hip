@@ -19,7 +19,9 @@
 // prefixes of their own, so that (i, c) can only be kept where (i + 1) c <= K (28 pairs for K = 8, 66 for
 // 16, 151 for 32); and where all K beams can stay, only pairs above the least of their totals.  These
 // few are ordered by counting, each lane the totals above its own.  A frame that none of them enters and
-// that leaves the order as it is (most frames, where a head is sure) moves nothing.
+// that leaves the order as it is (most frames, where a head is sure) moves nothing, and one that does not
+// offer any beam's last label either adds blank's score to every beam.  Frames come from memory eight at
+// a time, a wait of eight frames ahead of their use.
 // Prefixes are compared by 64-bit hashes of their labels and their lengths: two different ones meet
 // with a probability of about K^2 / 2^65 per frame.
 #include <algorithm>
@@ -151,10 +153,12 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   constexpr int kCopies = 64 / KT;                        // lanes of a beam
   constexpr int kPairs = KT <= 8 ? 1 : KT <= 16 ? 2 : 3;  // (beam, class) pairs a lane looks at
   constexpr int kEntries = KT + 64 * kPairs;
+  constexpr int kAhead = 8;                               // frames fetched at a time
   constexpr uint64_t kEvery = KT == 4 ? 0x1111111111111111ull : KT == 8 ? 0x0101010101010101ull
                               : KT == 16 ? 0x0001000100010001ull : 0x0000000100000001ull;  // a beam's lanes
-  __shared__ float lp_s[2][64];       // this frame's classes and the next one's
-  __shared__ __attribute__((aligned(16))) int32_t id_s[2][64];
+  __shared__ float lp_s[2 * kAhead][64];  // the classes of this and the next eight frames
+  __shared__ int32_t id_s[2 * kAhead][64];
+  __shared__ float bl_s[2 * kAhead];
   __shared__ int first_s[KT + 1];     // pairs of the beams before
   __shared__ int merged_s[64 * kPairs];  // frame (from 1) in which a pair's prefix was last a beam
   __shared__ __attribute__((aligned(16))) float val_s[kEntries + 4];  // totals to be ordered: staying beams, pairs
@@ -218,28 +222,31 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     }
   }
 
-  // a frame's classes, one a lane; a score that is no number counts as -inf
-  int id;
-  float l, b;
+  // eight frames' classes, one a lane, and (lanes [0, 8)) blank scores; a score that is no number
+  // counts as -inf
+  int fid[kAhead];
+  float fl[kAhead], fb;
   auto fetch = [&](int m) {
-    id = -1;
-    l = b = kNegInf;
-    if (m >= t1) return;
-    if (lane < C) {
-      id = ids[static_cast<int64_t>(m) * C + lane];
-      l = logp[static_cast<int64_t>(m) * C + lane];
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) {
+      fid[g] = -1;
+      fl[g] = kNegInf;
+      if (m + g < t1 && lane < C) {
+        fid[g] = ids[static_cast<int64_t>(m + g) * C + lane];
+        fl[g] = logp[static_cast<int64_t>(m + g) * C + lane];
+      }
     }
-    b = blank_logp[m];
+    fb = lane < kAhead && m + lane < t1 ? blank_logp[m + lane] : kNegInf;
   };
-  auto stage = [&](int buf) {
-    if (id < 0 || !(l > kNegInf)) {
-      id = -1;
-      l = kNegInf;
+  auto stage = [&](int half) {
+#pragma unroll
+    for (int g = 0; g < kAhead; ++g) {
+      const bool ok = fid[g] >= 0 && fl[g] > kNegInf;
+      lp_s[half * kAhead + g][lane] = ok ? fl[g] : kNegInf;
+      id_s[half * kAhead + g][lane] = ok ? fid[g] : -1;
     }
-    if (!(b > kNegInf)) b = kNegInf;
-    lp_s[buf][lane] = l;
-    id_s[buf][lane] = id;
-    return b;
+    if (lane < kAhead) bl_s[half * kAhead + lane] = fb > kNegInf ? fb : kNegInf;
+    __builtin_amdgcn_wave_barrier();
   };
   // the beam whose prefix is this beam's without its last label
   auto find_parent = [&]() {
@@ -256,77 +263,118 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   };
 
   fetch(t0);
-  float bl = stage(t0 & 1);
-  fetch(t0 + 1);
-  __builtin_amdgcn_wave_barrier();
+  stage(0);
+  fetch(t0 + kAhead);
   int par = find_parent();
-  for (int m = t0; m < t1; ++m) {
-    const int buf = m & 1;
-    const float b_now = bl;
-    bl = stage(buf ^ 1);
-    fetch(m + 2);
-    // what the pairs and the joining prefixes need of other beams
-    float ps[kPairs], ppb[kPairs], pl[kPairs];
+  int lasts[KT];  // every beam's last label, in scalar registers
+  float ps[kPairs], ppb[kPairs];  // s and pb of the pairs' beams
+  auto spread = [&]() {
+#pragma unroll
+    for (int j = 0; j < KT; ++j) lasts[j] = __builtin_amdgcn_readlane(last, j);
+  };
+  auto spread_masses = [&]() {
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) {
       ps[q] = __shfl(s, pi[q] & 63, 64);
       ppb[q] = __shfl(pb, pi[q] & 63, 64);
-      pl[q] = lp_s[buf][pc[q]] + bonus;
     }
-    const int p = par >= 0 ? par : i;
-    const float pb_p = __shfl(pb, p, 64), s_p = __shfl(s, p, 64);
-    const int last_p = __shfl(last, p, 64);
-    // where the beam's last label stands among the classes
-    int pos = -1;
+  };
+  spread();
+  spread_masses();
+  // the frame at hand: this lane's class, its pairs' scores, blank's score
+  int id = id_s[0][lane];
+  float pl[kPairs], bl = bl_s[0];
 #pragma unroll
-    for (int q = 0; q < KT; q += 4) {
-      const int4 v = *reinterpret_cast<const int4*>(&id_s[buf][copy * KT + q]);
-      pos = v.x == last ? copy * KT + q : pos;
-      pos = v.y == last ? copy * KT + q + 1 : pos;
-      pos = v.z == last ? copy * KT + q + 2 : pos;
-      pos = v.w == last ? copy * KT + q + 3 : pos;
+  for (int q = 0; q < kPairs; ++q) pl[q] = lp_s[0][pc[q]] + bonus;
+  for (int m = t0; m < t1; ++m) {
+    const int row = (m - t0) & (2 * kAhead - 1), row1 = (row + 1) & (2 * kAhead - 1);
+    const float b = bl;
+    const int id_now = id;
+    float plb[kPairs];
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) plb[q] = pl[q];
+    if ((row & (kAhead - 1)) == kAhead - 1) {
+      stage(row1 / kAhead);
+      fetch(m + 1 + kAhead);
     }
-    {
-      const uint64_t who = (__ballot(pos >= 0) >> i) & kEvery;
-      pos = __shfl(pos, (who ? __builtin_ctzll(who) & ~(KT - 1) : 0) + i, 64);
-    }
-    const float l_last = pos >= 0 ? lp_s[buf][pos] : kNegInf;
-    const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
-    const float sb = s + b_now, again = pn + l_last;
-    // pb' (+) pn' of a staying beam
-    const float top = fmaxf(sb, fmaxf(again, join));
-    const float total =
-        top > kNegInf ? top + kLn2 * fast_log2(fast_exp2((sb - top) * kLog2e) + fast_exp2((again - top) * kLog2e) +
-                                               fast_exp2((join - top) * kLog2e))
-                      : kNegInf;
-    const float sn = log_add(again, join);
-    // a pair whose prefix is a beam already is no new one
-    const bool joins = par >= 0 && pos >= 0;
-    if (__any(joins) && joins && copy == 0) {
-      const int e = first_s[par] + pos;
-      if (e < first_s[par + 1]) merged_s[e] = m - t0 + 1;
-    }
-    __builtin_amdgcn_wave_barrier();
-    const float least = lanes_min<KT>(mine ? total : INFINITY);
-    float pv[kPairs];
+    id = id_s[row1][lane];
+    bl = bl_s[row1];
+#pragma unroll
+    for (int q = 0; q < kPairs; ++q) pl[q] = lp_s[row1][pc[q]] + bonus;
+
+    // the classes that are some beam's last label
+    uint64_t met = 0;
+#pragma unroll
+    for (int j = 0; j < KT; ++j) met |= __ballot(id_now == lasts[j]);
+    const float sb = s + b;
+    float total, sn, pv[kPairs];
     uint64_t enter[kPairs], any = 0;
+    if (met == 0) {
+      // every beam can only end in blank, and their order stands
+      const float least = lane_f(sb, K - 1), lead = lane_f(sb, 0);
 #pragma unroll
-    for (int q = 0; q < kPairs; ++q) {
-      const int own = __shfl(pos, pi[q] & 63, 64);
-      pv[q] = (own == pc[q] ? ppb[q] : ps[q]) + pl[q];
-      enter[q] = __ballot(pi[q] >= 0 && pv[q] > least && merged_s[lane + 64 * q] != m - t0 + 1);
-      any |= enter[q];
-    }
-    // no pair enters, no beam leaves, and their order stands
-    const float before = KT <= 16 ? lane_below(total) : __shfl(total, lane > 0 ? lane - 1 : 0, 64);
-    const bool moves = mine && ((i > 0 && total > before) || (len >= 0 && !(total > kNegInf)));
-    const float lead = lane_f(total, 0);
-    if (any == 0 && lead > kNegInf && __ballot(moves) == 0) {
-      pb = sb - lead;
-      pn = sn - lead;
-      s = total - lead;
-      offset += lead;
-      continue;
+      for (int q = 0; q < kPairs; ++q) {
+        pv[q] = ps[q] + plb[q];
+        enter[q] = __ballot(pi[q] >= 0 && pv[q] > least);
+        any |= enter[q];
+      }
+      if (any == 0 && lead > kNegInf) {
+        pb = s = sb - lead;
+        pn = kNegInf;
+#pragma unroll
+        for (int q = 0; q < kPairs; ++q) ps[q] = ppb[q] = (ps[q] + b) - lead;
+        offset += lead;
+        continue;
+      }
+      total = sb;
+      sn = kNegInf;
+    } else {
+      const int p = par >= 0 ? par : i;
+      const float pb_p = __shfl(pb, p, 64), s_p = __shfl(s, p, 64);
+      const int last_p = __shfl(last, p, 64);
+      // where the beam's last label stands among the classes
+      int pos = -1;
+#pragma unroll
+      for (int j = 0; j < KT; ++j) {
+        const uint64_t who = __ballot(id_now == lasts[j]);
+        const int c = who ? __builtin_ctzll(who) : -1;
+        pos = i == j ? c : pos;
+      }
+      const float l_last = pos >= 0 ? lp_s[row][pos] : kNegInf;
+      const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
+      const float again = pn + l_last;
+      // pb' (+) pn' of a staying beam
+      const float top = fmaxf(sb, fmaxf(again, join));
+      total = top > kNegInf ? top + kLn2 * fast_log2(fast_exp2((sb - top) * kLog2e) + fast_exp2((again - top) * kLog2e) +
+                                                     fast_exp2((join - top) * kLog2e))
+                            : kNegInf;
+      sn = log_add(again, join);
+      // a pair whose prefix is a beam already is no new one
+      if (par >= 0 && pos >= 0 && copy == 0) {
+        const int e = first_s[par] + pos;
+        if (e < first_s[par + 1]) merged_s[e] = m - t0 + 1;
+      }
+      __builtin_amdgcn_wave_barrier();
+      const float least = lanes_min<KT>(mine ? total : INFINITY);
+#pragma unroll
+      for (int q = 0; q < kPairs; ++q) {
+        const int own = __shfl(pos, pi[q] & 63, 64);
+        pv[q] = (own == pc[q] ? ppb[q] : ps[q]) + plb[q];
+        enter[q] = __ballot(pi[q] >= 0 && pv[q] > least && merged_s[lane + 64 * q] != m - t0 + 1);
+        any |= enter[q];
+      }
+      // no pair enters, no beam leaves, and their order stands
+      const float before = KT <= 16 ? lane_below(total) : __shfl(total, lane > 0 ? lane - 1 : 0, 64);
+      const bool moves = mine && ((i > 0 && total > before) || (len >= 0 && !(total > kNegInf)));
+      const float lead = lane_f(total, 0);
+      if (any == 0 && lead > kNegInf && __ballot(moves) == 0) {
+        pb = sb - lead;
+        pn = sn - lead;
+        s = total - lead;
+        spread_masses();
+        offset += lead;
+        continue;
+      }
     }
 
     // the totals to be ordered, in the order of ties
@@ -383,7 +431,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       len = last = -2;
       origin = -1;
     } else {
-      const int label = id_s[buf][c];
+      const int label = id_s[row][c];
       const int fresh = (done + m - t0) * K + i;
       pb = grown ? kNegInf : f_sb - best;
       pn = (grown ? won : f_sn) - best;
@@ -405,6 +453,8 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     }
     offset += best;
     par = find_parent();
+    spread();
+    spread_masses();
   }
   if (copy == 0 && mine) {
     f.pb[at] = pb;
