@@ -36,11 +36,20 @@ namespace {
 constexpr float kNegInf = -INFINITY;
 constexpr int kCkStep = 32;  // labels between two nodes that remember the one before (result kernel)
 
+constexpr float kLow = -1e30f;  // a reference that stays finite where all masses are zero
+
+// Sums of two and of three masses; -inf where all are zero.
 __device__ __forceinline__ float log_add(float a, float b) {
-  const float hi = fmaxf(a, b), lo = fminf(a, b);
-  if (hi == kNegInf) return kNegInf;
-  return hi + kLn2 * fast_log2(1.f + fast_exp2((lo - hi) * kLog2e));
+  const float hi = fmaxf(fmaxf(a, b), kLow);
+  return hi + kLn2 * fast_log2(fast_exp2((a - hi) * kLog2e) + fast_exp2((b - hi) * kLog2e));
 }
+__device__ __forceinline__ float log_add(float a, float b, float c) {
+  const float hi = fmaxf(fmaxf(a, b), fmaxf(c, kLow));
+  return hi + kLn2 * fast_log2(fast_exp2((a - hi) * kLog2e) + fast_exp2((b - hi) * kLog2e) +
+                               fast_exp2((c - hi) * kLog2e));
+}
+
+__device__ __forceinline__ uint64_t lanes_where(bool x) { return __builtin_amdgcn_ballot_w64(x); }
 
 // The hash of a prefix with one more label.
 __device__ __forceinline__ uint64_t grow_hash(uint64_t hash, int label) {
@@ -161,9 +170,9 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   __shared__ float bl_s[2 * kAhead];
   __shared__ int first_s[KT + 1];     // pairs of the beams before
   __shared__ int merged_s[64 * kPairs];  // frame (from 1) in which a pair's prefix was last a beam
-  __shared__ __attribute__((aligned(16))) float val_s[kEntries + 4];  // totals to be ordered: staying beams, pairs
+  __shared__ __attribute__((aligned(16))) float val_s[kEntries + 16];  // totals to be ordered: staying beams, pairs
   __shared__ int what_s[kEntries];    // of a pair: beam + 256 class
-  __shared__ int place_s[KT];         // entry of each place
+  __shared__ int2 place_s[KT];        // of each place: what, with bit 30 for a pair, and the total
   const int lane = threadIdx.x, i = lane & (KT - 1), copy = lane / KT;
   const int n = n0 + blockIdx.x;
   const int t0 = rows.off[blockIdx.x], t1 = rows.off[blockIdx.x + 1];
@@ -226,22 +235,20 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   // counts as -inf
   int fid[kAhead];
   float fl[kAhead], fb;
-  auto fetch = [&](int m) {
+  const int mine_c = min(lane, C - 1);
+  auto fetch = [&](int m) {  // (rows past the last are read as the last: they are not used)
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      fid[g] = -1;
-      fl[g] = kNegInf;
-      if (m + g < t1 && lane < C) {
-        fid[g] = ids[static_cast<int64_t>(m + g) * C + lane];
-        fl[g] = logp[static_cast<int64_t>(m + g) * C + lane];
-      }
+      const int64_t at_row = static_cast<int64_t>(min(m + g, t1 - 1)) * C;
+      fid[g] = (ids + at_row)[mine_c];
+      fl[g] = (logp + at_row)[mine_c];
     }
-    fb = lane < kAhead && m + lane < t1 ? blank_logp[m + lane] : kNegInf;
+    fb = blank_logp[min(m + (lane & (kAhead - 1)), t1 - 1)];
   };
   auto stage = [&](int half) {
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      const bool ok = fid[g] >= 0 && fl[g] > kNegInf;
+      const bool ok = lane < C && fid[g] >= 0 && fl[g] > kNegInf;
       lp_s[half * kAhead + g][lane] = ok ? fl[g] : kNegInf;
       id_s[half * kAhead + g][lane] = ok ? fid[g] : -1;
     }
@@ -258,14 +265,17 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       const int ln = __shfl(len, o & (KT - 1), 64);
       if (o < KT && ln + 1 == len && h == phash) found = o;
     }
-    const uint64_t who = (__ballot(found >= 0) >> i) & kEvery;
+    const uint64_t who = (lanes_where(found >= 0) >> i) & kEvery;
     return __shfl(found, (who ? __builtin_ctzll(who) & ~(KT - 1) : 0) + i, 64);
   };
 
-  fetch(t0);
-  stage(0);
-  fetch(t0 + kAhead);
-  int par = find_parent();
+  if (t0 < t1) {
+    fetch(t0);
+    stage(0);
+    fetch(t0 + kAhead);
+  }
+  int par = -1;
+  bool par_known = false;  // par is formed when a frame asks for it
   int lasts[KT];  // every beam's last label, in scalar registers
   float ps[kPairs], ppb[kPairs];  // s and pb of the pairs' beams
   auto spread = [&]() {
@@ -305,7 +315,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     // the classes that are some beam's last label
     uint64_t met = 0;
 #pragma unroll
-    for (int j = 0; j < KT; ++j) met |= __ballot(id_now == lasts[j]);
+    for (int j = 0; j < KT; ++j) met |= lanes_where(id_now == lasts[j]);
     const float sb = s + b;
     float total, sn, pv[kPairs];
     uint64_t enter[kPairs], any = 0;
@@ -315,7 +325,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
 #pragma unroll
       for (int q = 0; q < kPairs; ++q) {
         pv[q] = ps[q] + plb[q];
-        enter[q] = __ballot(pi[q] >= 0 && pv[q] > least);
+        enter[q] = lanes_where(pi[q] >= 0 && pv[q] > least);
         any |= enter[q];
       }
       if (any == 0 && lead > kNegInf) {
@@ -329,6 +339,8 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       total = sb;
       sn = kNegInf;
     } else {
+      if (!par_known) par = find_parent();
+      par_known = true;
       const int p = par >= 0 ? par : i;
       const float pb_p = __shfl(pb, p, 64), s_p = __shfl(s, p, 64);
       const int last_p = __shfl(last, p, 64);
@@ -336,21 +348,20 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       int pos = -1;
 #pragma unroll
       for (int j = 0; j < KT; ++j) {
-        const uint64_t who = __ballot(id_now == lasts[j]);
+        const uint64_t who = lanes_where(id_now == lasts[j]);
         const int c = who ? __builtin_ctzll(who) : -1;
         pos = i == j ? c : pos;
       }
-      const float l_last = pos >= 0 ? lp_s[row][pos] : kNegInf;
+      const float l_pos = lp_s[row][pos & 63];
+      const float l_last = pos >= 0 ? l_pos : kNegInf;
       const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
       const float again = pn + l_last;
       // pb' (+) pn' of a staying beam
-      const float top = fmaxf(sb, fmaxf(again, join));
-      total = top > kNegInf ? top + kLn2 * fast_log2(fast_exp2((sb - top) * kLog2e) + fast_exp2((again - top) * kLog2e) +
-                                                     fast_exp2((join - top) * kLog2e))
-                            : kNegInf;
+      total = log_add(sb, again, join);
       sn = log_add(again, join);
       // a pair whose prefix is a beam already is no new one
-      if (par >= 0 && pos >= 0 && copy == 0) {
+      const bool joins = par >= 0 && pos >= 0 && copy == 0, joined = lanes_where(joins) != 0;
+      if (joins) {
         const int e = first_s[par] + pos;
         if (e < first_s[par + 1]) merged_s[e] = m - t0 + 1;
       }
@@ -360,14 +371,15 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       for (int q = 0; q < kPairs; ++q) {
         const int own = __shfl(pos, pi[q] & 63, 64);
         pv[q] = (own == pc[q] ? ppb[q] : ps[q]) + plb[q];
-        enter[q] = __ballot(pi[q] >= 0 && pv[q] > least && merged_s[lane + 64 * q] != m - t0 + 1);
+        const bool is_beam = joined && merged_s[lane + 64 * q] == m - t0 + 1;
+        enter[q] = lanes_where(pi[q] >= 0 && pv[q] > least && !is_beam);
         any |= enter[q];
       }
       // no pair enters, no beam leaves, and their order stands
       const float before = KT <= 16 ? lane_below(total) : __shfl(total, lane > 0 ? lane - 1 : 0, 64);
       const bool moves = mine && ((i > 0 && total > before) || (len >= 0 && !(total > kNegInf)));
       const float lead = lane_f(total, 0);
-      if (any == 0 && lead > kNegInf && __ballot(moves) == 0) {
+      if (any == 0 && lead > kNegInf && lanes_where(moves) == 0) {
         pb = sb - lead;
         pn = sn - lead;
         s = total - lead;
@@ -389,38 +401,58 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       }
       count += __popcll(enter[q]);
     }
-    if (lane < 4) val_s[count + lane] = kNegInf;
+    if (lane < 16) val_s[count + lane] = kNegInf;
     __builtin_amdgcn_wave_barrier();
     int live = 0;  // entries above -inf
-    for (int e0 = 0; e0 < count; e0 += 64) {
-      const int e = e0 + lane;
-      const float v = e < count ? val_s[e] : kNegInf;
+    auto place_of = [&](float v) {
       int place = 0;
-      for (int o = 0; o < count; o += 4) {
-        const float4 w = *reinterpret_cast<const float4*>(&val_s[o]);
-        place += (w.x > v) + (w.y > v) + (w.z > v) + (w.w > v);
+      for (int o = 0; o < count; o += 16) {
+        float4 w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const float4*>(&val_s[o + 4 * k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) place += (w[k].x > v) + (w[k].y > v) + (w[k].z > v) + (w[k].w > v);
       }
-      const bool in = v > kNegInf;
-      live += __popcll(__ballot(in));
-      // equal totals land on one place: where someone finds another there (and past the first 64
-      // entries, whose places may be taken), the entries' order tells them apart
-      if (e0 == 0) {
-        if (in && place < K) place_s[place] = e;
-        __builtin_amdgcn_wave_barrier();
-      }
-      if (e0 > 0 || __any(in && place < K && place_s[place] != e)) {
-        for (int o = 0; o < e && in; ++o) place += val_s[o] == v;
-        if (in && place < K) place_s[place] = e;
-      }
+      return place;
+    };
+    // equal totals have one place: the entries' order tells them apart
+    auto untie = [&](int e, float v, int place) {
+      for (int o = 0; o < e; ++o) place += val_s[o] == v;
+      return place;
+    };
+    if (count <= 64) {
+      const float mine_v = val_s[lane];
+      const int pair = what_s[lane] | 1 << 30;
+      const float v = lane < count ? mine_v : kNegInf;
+      const int what = lane < K ? lane : pair;
+      int place = place_of(v);
+      const bool in = v > kNegInf, kept = in && place < K;
+      live = __popcll(lanes_where(in));
+      if (kept) place_s[place] = make_int2(what, __float_as_int(v));
       __builtin_amdgcn_wave_barrier();
+      if (__builtin_expect(lanes_where(kept && place_s[place & (KT - 1)].x != what) != 0, 0)) {
+        place = untie(lane, v, place);
+        if (in && place < K) place_s[place] = make_int2(what, __float_as_int(v));
+      }
+    } else {
+      for (int e0 = 0; e0 < count; e0 += 64) {
+        const int e = e0 + lane;
+        const float v = e < count ? val_s[e] : kNegInf;
+        const bool in = v > kNegInf;
+        live += __popcll(lanes_where(in));
+        if (in) {
+          const int place = untie(e, v, place_of(v));
+          if (place < K) place_s[place] = make_int2(e < K ? e : what_s[e] | 1 << 30, __float_as_int(v));
+        }
+      }
     }
+    __builtin_amdgcn_wave_barrier();
     // the new beam i
     const bool lives = i < min(live, K);
-    const int e = lives ? place_s[i] : 0;
-    const bool grown = lives && e >= K;
-    const int what = grown ? what_s[e] : e;
-    const int src = what & 255, c = grown ? what >> 8 : 0;
-    const float won = val_s[e];
+    const int2 here = place_s[lives ? i : 0];
+    const bool grown = lives && (here.x >> 30) != 0;
+    const int src = lives ? here.x & 255 : 0, c = grown ? (here.x >> 8) & 63 : 0;
+    const float won = __int_as_float(here.y);
     const float best = live > 0 ? lane_f(won, 0) : 0.f;
     const float f_sb = __shfl(sb, src, 64), f_sn = __shfl(sn, src, 64);
     const uint64_t f_hash = from_lane(hash, src), f_phash = from_lane(phash, src);
@@ -452,7 +484,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       }
     }
     offset += best;
-    par = find_parent();
+    par_known = false;
     spread();
     spread_masses();
   }
