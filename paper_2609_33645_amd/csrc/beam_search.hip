@@ -20,8 +20,10 @@
 // 16, 151 for 32); and where all K beams can stay, only pairs above the least of their totals.  These
 // few are ordered by counting, each lane the totals above its own.  A frame that none of them enters and
 // that leaves the order as it is (most frames, where a head is sure) moves nothing, and one that does not
-// offer any beam's last label either adds blank's score to every beam.  Frames come from memory eight at
-// a time, a wait of eight frames ahead of their use.
+// offer any beam's last label either leaves every beam as it is: blank's score goes to the utterance's
+// total.  Where the beams' last labels stand among the classes is looked up for 64 / KT frames at once
+// (at most eight), a lane for each beam and frame.  Frames come from memory eight at a time, eight frames
+// and more ahead of their use.
 // Prefixes are compared by 64-bit hashes of their labels and their lengths: two different ones meet
 // with a probability of about K^2 / 2^65 per frame.
 #include <algorithm>
@@ -161,17 +163,20 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
                     int32_t* __restrict__ parents) {
   constexpr int kCopies = 64 / KT;                        // lanes of a beam
   constexpr int kPairs = KT <= 8 ? 1 : KT <= 16 ? 2 : 3;  // (beam, class) pairs a lane looks at
-  constexpr int kEntries = KT + 64 * kPairs;
+  constexpr int kBatches = KT <= 8 ? 1 : KT <= 16 ? 2 : 3;  // of 64 totals to be ordered (36, 82, 183 at most)
   constexpr int kAhead = 8;                               // frames fetched at a time
+  constexpr int kRing = 32;                               // frames held
+  constexpr int kLook = kCopies < 8 ? kCopies : 8;        // frames looked up at a time
+  constexpr uint64_t kBeamBits = (uint64_t{1} << KT) - 1;
   constexpr uint64_t kEvery = KT == 4 ? 0x1111111111111111ull : KT == 8 ? 0x0101010101010101ull
                               : KT == 16 ? 0x0001000100010001ull : 0x0000000100000001ull;  // a beam's lanes
-  __shared__ float lp_s[2 * kAhead][64];  // the classes of this and the next eight frames
-  __shared__ int32_t id_s[2 * kAhead][64];
-  __shared__ float bl_s[2 * kAhead];
+  __shared__ float lp_s[kRing][64];  // the classes of frame t0 + f in row f mod kRing, and blank's score
+  __shared__ __attribute__((aligned(16))) int32_t id_s[kRing][64];
+  __shared__ float bl_s[kRing];
   __shared__ int first_s[KT + 1];     // pairs of the beams before
   __shared__ int merged_s[64 * kPairs];  // frame (from 1) in which a pair's prefix was last a beam
-  __shared__ __attribute__((aligned(16))) float val_s[kEntries + 16];  // totals to be ordered: staying beams, pairs
-  __shared__ int what_s[kEntries];    // of a pair: beam + 256 class
+  __shared__ __attribute__((aligned(16))) float val_s[64 * kBatches + 16];  // totals to be ordered: staying beams, pairs
+  __shared__ int what_s[64 * kBatches];  // of a pair: beam + 256 class
   __shared__ int2 place_s[KT];        // of each place: what, with bit 30 for a pair, and the total
   const int lane = threadIdx.x, i = lane & (KT - 1), copy = lane / KT;
   const int n = n0 + blockIdx.x;
@@ -245,14 +250,15 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     }
     fb = blank_logp[min(m + (lane & (kAhead - 1)), t1 - 1)];
   };
-  auto stage = [&](int half) {
+  auto stage = [&](int f) {  // frames t0 + f .. t0 + f + 7 (f a multiple of 8)
+    const int r0 = f & (kRing - 1);
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      const bool ok = lane < C && fid[g] >= 0 && fl[g] > kNegInf;
-      lp_s[half * kAhead + g][lane] = ok ? fl[g] : kNegInf;
-      id_s[half * kAhead + g][lane] = ok ? fid[g] : -1;
+      const bool ok = lane < C & fid[g] >= 0 & fl[g] > kNegInf;
+      lp_s[r0 + g][lane] = ok ? fl[g] : kNegInf;
+      id_s[r0 + g][lane] = ok ? fid[g] : -1;
     }
-    if (lane < kAhead) bl_s[half * kAhead + lane] = fb > kNegInf ? fb : kNegInf;
+    if (lane < kAhead) bl_s[r0 + lane] = fb > kNegInf ? fb : kNegInf;
     __builtin_amdgcn_wave_barrier();
   };
   // the beam whose prefix is this beam's without its last label
@@ -269,71 +275,85 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     return __shfl(found, (who ? __builtin_ctzll(who) & ~(KT - 1) : 0) + i, 64);
   };
 
-  if (t0 < t1) {
+  const int T = t1 - t0;
+  int staged = 0;  // frames in the ring
+  auto more = [&]() {
+    stage(staged);
+    staged += kAhead;
+    fetch(t0 + staged);
+  };
+  if (T > 0) {
     fetch(t0);
-    stage(0);
-    fetch(t0 + kAhead);
+    more();
   }
   int par = -1;
   bool par_known = false;  // par is formed when a frame asks for it
-  int lasts[KT];  // every beam's last label, in scalar registers
   float ps[kPairs], ppb[kPairs];  // s and pb of the pairs' beams
+  float floor_s;                  // s of the last beam
   auto spread = [&]() {
-#pragma unroll
-    for (int j = 0; j < KT; ++j) lasts[j] = __builtin_amdgcn_readlane(last, j);
-  };
-  auto spread_masses = [&]() {
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) {
       ps[q] = __shfl(s, pi[q] & 63, 64);
       ppb[q] = __shfl(pb, pi[q] & 63, 64);
     }
+    floor_s = lane_f(s, K - 1);
   };
   spread();
-  spread_masses();
-  // the frame at hand: this lane's class, its pairs' scores, blank's score
-  int id = id_s[0][lane];
+  // where beam lane mod KT's last label stands among the classes of frame looked + lane / KT (-1: nowhere)
+  int stand = -1, looked = -kLook;
+  uint64_t stands = 0;
+  auto look = [&](int fr) {
+    looked = fr;
+    stand = -1;
+    const int32_t* const r = id_s[(fr + copy) & (kRing - 1)];
+    for (int c = 0; c < C; c += 16) {
+      int4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const int4*>(r + c + 4 * k);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        stand = v[k].x == last ? c + 4 * k : stand;
+        stand = v[k].y == last ? c + 4 * k + 1 : stand;
+        stand = v[k].z == last ? c + 4 * k + 2 : stand;
+        stand = v[k].w == last ? c + 4 * k + 3 : stand;
+      }
+    }
+    stands = lanes_where(stand >= 0);
+  };
+  // the frame at hand: its pairs' scores and blank's
   float pl[kPairs], bl = bl_s[0];
 #pragma unroll
   for (int q = 0; q < kPairs; ++q) pl[q] = lp_s[0][pc[q]] + bonus;
-  for (int m = t0; m < t1; ++m) {
-    const int row = (m - t0) & (2 * kAhead - 1), row1 = (row + 1) & (2 * kAhead - 1);
+  for (int fr = 0; fr < T; ++fr) {
+    const int row = fr & (kRing - 1), row1 = (fr + 1) & (kRing - 1);
+    if (staged < fr + kLook + 1) more();
     const float b = bl;
-    const int id_now = id;
     float plb[kPairs];
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) plb[q] = pl[q];
-    if ((row & (kAhead - 1)) == kAhead - 1) {
-      stage(row1 / kAhead);
-      fetch(m + 1 + kAhead);
-    }
-    id = id_s[row1][lane];
     bl = bl_s[row1];
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) pl[q] = lp_s[row1][pc[q]] + bonus;
-
-    // the classes that are some beam's last label
-    uint64_t met = 0;
-#pragma unroll
-    for (int j = 0; j < KT; ++j) met |= lanes_where(id_now == lasts[j]);
+    if (fr >= looked + kLook) look(fr);
+    const uint64_t met = (stands >> ((fr - looked) * KT)) & kBeamBits;  // beams whose last label is offered
     const float sb = s + b;
     float total, sn, pv[kPairs];
     uint64_t enter[kPairs], any = 0;
     if (met == 0) {
       // every beam can only end in blank, and their order stands
-      const float least = lane_f(sb, K - 1), lead = lane_f(sb, 0);
+      const float least = floor_s + b;
 #pragma unroll
       for (int q = 0; q < kPairs; ++q) {
         pv[q] = ps[q] + plb[q];
-        enter[q] = lanes_where(pi[q] >= 0 && pv[q] > least);
+        enter[q] = lanes_where(pi[q] >= 0 & pv[q] > least);
         any |= enter[q];
       }
-      if (any == 0 && lead > kNegInf) {
-        pb = s = sb - lead;
+      if (any == 0 && b > kNegInf) {
+        pb = s;
         pn = kNegInf;
 #pragma unroll
-        for (int q = 0; q < kPairs; ++q) ps[q] = ppb[q] = (ps[q] + b) - lead;
-        offset += lead;
+        for (int q = 0; q < kPairs; ++q) ppb[q] = ps[q];
+        offset += b;
         continue;
       }
       total = sb;
@@ -344,26 +364,18 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       const int p = par >= 0 ? par : i;
       const float pb_p = __shfl(pb, p, 64), s_p = __shfl(s, p, 64);
       const int last_p = __shfl(last, p, 64);
-      // where the beam's last label stands among the classes
-      int pos = -1;
-#pragma unroll
-      for (int j = 0; j < KT; ++j) {
-        const uint64_t who = lanes_where(id_now == lasts[j]);
-        const int c = who ? __builtin_ctzll(who) : -1;
-        pos = i == j ? c : pos;
-      }
+      const int pos = __shfl(stand, (fr - looked) * KT + i, 64);
       const float l_pos = lp_s[row][pos & 63];
       const float l_last = pos >= 0 ? l_pos : kNegInf;
       const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
       const float again = pn + l_last;
-      // pb' (+) pn' of a staying beam
-      total = log_add(sb, again, join);
+      total = log_add(sb, again, join);  // pb' (+) pn' of a staying beam
       sn = log_add(again, join);
       // a pair whose prefix is a beam already is no new one
       const bool joins = par >= 0 && pos >= 0 && copy == 0, joined = lanes_where(joins) != 0;
       if (joins) {
         const int e = first_s[par] + pos;
-        if (e < first_s[par + 1]) merged_s[e] = m - t0 + 1;
+        if (e < first_s[par + 1]) merged_s[e] = fr + 1;
       }
       __builtin_amdgcn_wave_barrier();
       const float least = lanes_min<KT>(mine ? total : INFINITY);
@@ -371,7 +383,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       for (int q = 0; q < kPairs; ++q) {
         const int own = __shfl(pos, pi[q] & 63, 64);
         pv[q] = (own == pc[q] ? ppb[q] : ps[q]) + plb[q];
-        const bool is_beam = joined && merged_s[lane + 64 * q] == m - t0 + 1;
+        const bool is_beam = joined && merged_s[lane + 64 * q] == fr + 1;
         enter[q] = lanes_where(pi[q] >= 0 && pv[q] > least && !is_beam);
         any |= enter[q];
       }
@@ -383,7 +395,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
         pb = sb - lead;
         pn = sn - lead;
         s = total - lead;
-        spread_masses();
+        spread();
         offset += lead;
         continue;
       }
@@ -403,50 +415,50 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     }
     if (lane < 16) val_s[count + lane] = kNegInf;
     __builtin_amdgcn_wave_barrier();
+    // entry e = 64 q + lane in this lane's registers
+    float v[kBatches];
+    int what[kBatches], place[kBatches];
     int live = 0;  // entries above -inf
-    auto place_of = [&](float v) {
-      int place = 0;
-      for (int o = 0; o < count; o += 16) {
-        float4 w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const float4*>(&val_s[o + 4 * k]);
+    for (int q = 0; q < kBatches; ++q) {
+      const int e = 64 * q + lane;
+      const float x = val_s[e];
+      const int pair = what_s[e] | 1 << 30;
+      v[q] = e < count ? x : kNegInf;
+      what[q] = e < K ? e : pair;
+      place[q] = 0;
+      live += __popcll(lanes_where(v[q] > kNegInf));
+    }
+    for (int o = 0; o < count; o += 16) {
+      float4 w[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) place += (w[k].x > v) + (w[k].y > v) + (w[k].z > v) + (w[k].w > v);
-      }
-      return place;
-    };
-    // equal totals have one place: the entries' order tells them apart
-    auto untie = [&](int e, float v, int place) {
-      for (int o = 0; o < e; ++o) place += val_s[o] == v;
-      return place;
-    };
-    if (count <= 64) {
-      const float mine_v = val_s[lane];
-      const int pair = what_s[lane] | 1 << 30;
-      const float v = lane < count ? mine_v : kNegInf;
-      const int what = lane < K ? lane : pair;
-      int place = place_of(v);
-      const bool in = v > kNegInf, kept = in && place < K;
-      live = __popcll(lanes_where(in));
-      if (kept) place_s[place] = make_int2(what, __float_as_int(v));
-      __builtin_amdgcn_wave_barrier();
-      if (__builtin_expect(lanes_where(kept && place_s[place & (KT - 1)].x != what) != 0, 0)) {
-        place = untie(lane, v, place);
-        if (in && place < K) place_s[place] = make_int2(what, __float_as_int(v));
-      }
-    } else {
-      for (int e0 = 0; e0 < count; e0 += 64) {
-        const int e = e0 + lane;
-        const float v = e < count ? val_s[e] : kNegInf;
-        const bool in = v > kNegInf;
-        live += __popcll(lanes_where(in));
-        if (in) {
-          const int place = untie(e, v, place_of(v));
-          if (place < K) place_s[place] = make_int2(e < K ? e : what_s[e] | 1 << 30, __float_as_int(v));
-        }
+      for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const float4*>(&val_s[o + 4 * k]);
+#pragma unroll
+      for (int q = 0; q < kBatches; ++q) {
+        if (q > 0 && count <= 64 * q) break;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          place[q] += (w[k].x > v[q]) + (w[k].y > v[q]) + (w[k].z > v[q]) + (w[k].w > v[q]);
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    // equal totals have one place: who finds another there goes by the entries' order
+    auto put = [&]() {
+#pragma unroll
+      for (int q = 0; q < kBatches; ++q)
+        if (v[q] > kNegInf && place[q] < K) place_s[place[q]] = make_int2(what[q], __float_as_int(v[q]));
+      __builtin_amdgcn_wave_barrier();
+    };
+    put();
+    bool tied = false;
+#pragma unroll
+    for (int q = 0; q < kBatches; ++q)
+      tied |= v[q] > kNegInf && place[q] < K && place_s[place[q] & (KT - 1)].x != what[q];
+    if (__builtin_expect(lanes_where(tied) != 0, 0)) {
+#pragma unroll
+      for (int q = 0; q < kBatches; ++q)
+        for (int o = 0; o < 64 * q + lane && o < count; ++o) place[q] += val_s[o] == v[q];
+      put();
+    }
     // the new beam i
     const bool lives = i < min(live, K);
     const int2 here = place_s[lives ? i : 0];
@@ -464,7 +476,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       origin = -1;
     } else {
       const int label = id_s[row][c];
-      const int fresh = (done + m - t0) * K + i;
+      const int fresh = (done + fr) * K + i;
       pb = grown ? kNegInf : f_sb - best;
       pn = (grown ? won : f_sn) - best;
       s = won - best;
@@ -485,8 +497,8 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     }
     offset += best;
     par_known = false;
+    looked = -kLook;
     spread();
-    spread_masses();
   }
   if (copy == 0 && mine) {
     f.pb[at] = pb;
