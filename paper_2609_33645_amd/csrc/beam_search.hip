@@ -36,6 +36,7 @@ namespace pctc {
 namespace {
 
 constexpr float kNegInf = -INFINITY;
+constexpr int kBufWord3 = 0x00020000;  // word 3 of a raw buffer resource: 32-bit data, no swizzle
 constexpr int kCkStep = 32;  // labels between two nodes that remember the one before (result kernel)
 
 constexpr float kLow = -1e30f;  // a reference that stays finite where all masses are zero
@@ -50,6 +51,10 @@ __device__ __forceinline__ float log_add(float a, float b, float c) {
   return hi + kLn2 * fast_log2(fast_exp2((a - hi) * kLog2e) + fast_exp2((b - hi) * kLog2e) +
                                fast_exp2((c - hi) * kLog2e));
 }
+
+// 1 where x > y, for y above -inf (from the sign of the difference: a comparison's mask takes an addition
+// several times as long).
+__device__ __forceinline__ uint32_t above(float x, float y) { return __float_as_uint(y - x) >> 31; }
 
 __device__ __forceinline__ uint64_t lanes_where(bool x) { return __builtin_amdgcn_ballot_w64(x); }
 
@@ -236,29 +241,39 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     }
   }
 
-  // eight frames' classes, one a lane, and (lanes [0, 8)) blank scores; a score that is no number
-  // counts as -inf
+  // eight frames' classes, one a lane, and (lanes [0, 8)) blank scores, through buffer resources that
+  // end with the utterance (what lies past reads as zeros and is not used)
   int fid[kAhead];
   float fl[kAhead], fb;
-  const int mine_c = min(lane, C - 1);
-  auto fetch = [&](int m) {  // (rows past the last are read as the last: they are not used)
+  const int T = t1 - t0;
+  auto fetch = [&](int f) {  // frames t0 + f ..
+#if defined(__HIP_DEVICE_COMPILE__)  // the buffer-resource type exists on the device side only
+    const int left = f < T ? min(T - f, kAhead) : 0;
+    const int64_t at_row = static_cast<int64_t>(t0 + f) * C;
+    auto resource = [&](const void* p, int values) {
+      return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), static_cast<short>(0), values * 4, kBufWord3);
+    };
+    const __amdgpu_buffer_rsrc_t ri = resource(ids + at_row, left * C), rl = resource(logp + at_row, left * C),
+                                 rb = resource(blank_logp + t0 + f, left);
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      const int64_t at_row = static_cast<int64_t>(min(m + g, t1 - 1)) * C;
-      fid[g] = (ids + at_row)[mine_c];
-      fl[g] = (logp + at_row)[mine_c];
+      fid[g] = __builtin_amdgcn_raw_buffer_load_b32(ri, lane * 4, g * C * 4, 0);
+      fl[g] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rl, lane * 4, g * C * 4, 0));
     }
-    fb = blank_logp[min(m + (lane & (kAhead - 1)), t1 - 1)];
+    fb = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rb, lane * 4, 0, 0));
+#endif
   };
-  auto stage = [&](int f) {  // frames t0 + f .. t0 + f + 7 (f a multiple of 8)
+  const int no_class = lane < C ? 0 : -1;
+  auto stage = [&](int f) {  // the same frames (f a multiple of 8)
     const int r0 = f & (kRing - 1);
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      const bool ok = lane < C & fid[g] >= 0 & fl[g] > kNegInf;
-      lp_s[r0 + g][lane] = ok ? fl[g] : kNegInf;
-      id_s[r0 + g][lane] = ok ? fid[g] : -1;
+      const int id = fid[g] | no_class;
+      // all ones, no number, where the class is none; the maximum takes -inf for no number
+      lp_s[r0 + g][lane] = fmaxf(__int_as_float(__float_as_int(fl[g]) | (id >> 31)), kNegInf);
+      id_s[r0 + g][lane] = id;
     }
-    if (lane < kAhead) bl_s[r0 + lane] = fb > kNegInf ? fb : kNegInf;
+    if (lane < kAhead) bl_s[r0 + lane] = fmaxf(fb, kNegInf);
     __builtin_amdgcn_wave_barrier();
   };
   // the beam whose prefix is this beam's without its last label
@@ -275,15 +290,14 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     return __shfl(found, (who ? __builtin_ctzll(who) & ~(KT - 1) : 0) + i, 64);
   };
 
-  const int T = t1 - t0;
   int staged = 0;  // frames in the ring
   auto more = [&]() {
     stage(staged);
     staged += kAhead;
-    fetch(t0 + staged);
+    fetch(staged);
   };
   if (T > 0) {
-    fetch(t0);
+    fetch(0);
     more();
   }
   int par = -1;
@@ -299,12 +313,13 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
     floor_s = lane_f(s, K - 1);
   };
   spread();
-  // where beam lane mod KT's last label stands among the classes of frame looked + lane / KT (-1: nowhere)
-  int stand = -1, looked = -kLook;
+  // whether beam lane mod KT's last label is among the classes of frame looked + lane / KT, from differences
+  // and their minimum (a comparison's mask takes a select several times as long)
+  int looked = -kLook;
   uint64_t stands = 0;
   auto look = [&](int fr) {
     looked = fr;
-    stand = -1;
+    uint32_t x = 0xffffffffu;
     const int32_t* const r = id_s[(fr + copy) & (kRing - 1)];
     for (int c = 0; c < C; c += 16) {
       int4 v[4];
@@ -312,13 +327,11 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const int4*>(r + c + 4 * k);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        stand = v[k].x == last ? c + 4 * k : stand;
-        stand = v[k].y == last ? c + 4 * k + 1 : stand;
-        stand = v[k].z == last ? c + 4 * k + 2 : stand;
-        stand = v[k].w == last ? c + 4 * k + 3 : stand;
+        x = min(min(static_cast<uint32_t>(v[k].x ^ last), static_cast<uint32_t>(v[k].y ^ last)), x);
+        x = min(min(static_cast<uint32_t>(v[k].z ^ last), static_cast<uint32_t>(v[k].w ^ last)), x);
       }
     }
-    stands = lanes_where(stand >= 0);
+    stands = lanes_where(x == 0);
   };
   // the frame at hand: its pairs' scores and blank's
   float pl[kPairs], bl = bl_s[0];
@@ -364,7 +377,15 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
       const int p = par >= 0 ? par : i;
       const float pb_p = __shfl(pb, p, 64), s_p = __shfl(s, p, 64);
       const int last_p = __shfl(last, p, 64);
-      const int pos = __shfl(stand, (fr - looked) * KT + i, 64);
+      // where the beams' last labels stand, label by label
+      int pos = -1;
+      const int id_now = id_s[row][lane];
+      for (uint64_t todo = met; todo != 0;) {
+        const int label = __builtin_amdgcn_readlane(last, __builtin_ctzll(todo));
+        const uint64_t at_class = lanes_where(id_now == label), has = lanes_where(last == label);
+        pos = last == label ? __builtin_ctzll(at_class) : pos;
+        todo &= ~has;
+      }
       const float l_pos = lp_s[row][pos & 63];
       const float l_last = pos >= 0 ? l_pos : kNegInf;
       const float join = par >= 0 ? (last_p == last ? pb_p : s_p) + (l_last + bonus) : kNegInf;
@@ -438,7 +459,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
         if (q > 0 && count <= 64 * q) break;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          place[q] += (w[k].x > v[q]) + (w[k].y > v[q]) + (w[k].z > v[q]) + (w[k].w > v[q]);
+          place[q] += above(w[k].x, v[q]) + above(w[k].y, v[q]) + above(w[k].z, v[q]) + above(w[k].w, v[q]);
       }
     }
     // equal totals have one place: who finds another there goes by the entries' order
