@@ -6,12 +6,12 @@
 //   of falling z, the lowest class first among equal ones
 //
 // One vocabulary pass on the matrix cores gives the normaliser's partial pairs and the largest logit
-// of every block of 32 classes.  A class among a frame's C best lies in one of the C + 1 blocks with
-// the largest maxima (one more for blank, which is left out), so a second kernel forms those blocks'
-// logits again, 32 (C + 1) dot products a frame, and orders them.  A block of 32 classes is where the
-// two sides meet: M V / 32 maxima are written and read (96 MB at 4,215 frames of 180,000 classes),
-// and W rows for 32 (C + 1) classes a frame are read again, from the L2s.  The scratch for the maxima is
-// held to 256 MB by passing over the vocabulary once per that many frames.
+// of every block of 16 classes.  A class among a frame's C best lies in one of the C + 1 blocks with the
+// largest maxima (one more for blank, which is left out; and one for the block whose classes lie between
+// the last one's, where maxima are equal), so a second kernel forms those blocks' logits again, 16 (C + 2)
+// dot products a frame, and orders them.  M V / 16 maxima are written and read (190 MB at 4,215 frames of
+// 180,000 classes) and W rows for 16 (C + 2) classes a frame are read again, through the L2s.  The scratch for
+// the maxima is held to 256 MB by passing over the vocabulary once per that many frames.
 #include <algorithm>
 
 #include "pctc_internal.h"
@@ -23,7 +23,8 @@ namespace {
 constexpr size_t kMaxBlockBytes = static_cast<size_t>(256) << 20;
 constexpr int kThreads = 256;
 constexpr int kList = 256;  // blocks kept for ordering; more only where maxima are equal
-constexpr int kValues = (kMaxCandidates + 1) * kCandRows;
+constexpr int kMaxSel = kMaxCandidates + 2;
+constexpr int kValues = kMaxSel * kCandRows;
 
 // Floats in the order of unsigned integers.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -75,7 +76,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   __shared__ float list_v[kList];
   __shared__ int list_b[kList];
   __shared__ int count;
-  __shared__ int sel[kMaxCandidates + 1];
+  __shared__ int sel[kMaxSel];
   __shared__ float z[kValues];
   __shared__ float val_v[kValues];
   __shared__ int val_i[kValues];
@@ -83,9 +84,9 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int m = m0 + blockIdx.x;
   const float* const row = bmax + static_cast<int64_t>(blockIdx.x) * nb;
-  const int nsel = min(C + 1, (V + kCandRows - 1) / kCandRows);
+  const int nsel = min(C + 2, nb);
 
-  // ---- the nsel blocks with the largest maxima (ties: the lowest) ----
+  // ---- the nsel blocks with the largest maxima (equal ones: the lowest) ----
   float mx = -INFINITY;
   for (int i = tid * 4; i < nb; i += kThreads * 4) {
     const float4 v = *reinterpret_cast<const float4*>(row + i);
@@ -104,7 +105,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
         const int q = atomicAdd(&count, 1);
         if (q < kList) {
           list_v[q] = v[e];
-          list_b[q] = i + e;
+          list_b[q] = CandBlocks::at(i + e);
         }
       }
     }
@@ -140,12 +141,13 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     if (tid == 0) count = 0;
     __syncthreads();
     for (int i = tid; i < nb; i += kThreads)
-      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = i;
+      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = CandBlocks::at(i);
     __syncthreads();
     n = count;
     if (wave == 0) {
       for (int i0 = 0; i0 < nb && n < nsel; i0 += 64) {
-        const bool at = i0 + lane < nb && row[i0 + lane] > -INFINITY && order_key(row[i0 + lane]) == t;
+        const float v = i0 + lane < nb ? row[CandBlocks::place(i0 + lane)] : -INFINITY;
+        const bool at = v > -INFINITY && order_key(v) == t;
         const uint64_t who = __ballot(at);
         const int q = n + __popcll(who & ((uint64_t{1} << lane) - 1));
         if (at && q < nsel) sel[q] = i0 + lane;
@@ -172,8 +174,9 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     for (int o = 4; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
     return s;
   };
-  for (int g = wave; g < n * 4; g += kThreads / 64) {  // groups of eight classes
-    const int v = sel[g >> 2] * kCandRows + (g & 3) * 8 + (lane >> 3);
+  constexpr int kParts = kCandRows / 8;
+  for (int g = wave; g < n * kParts; g += kThreads / 64) {  // groups of eight classes
+    const int v = CandBlocks::class_of(sel[g / kParts], g % kParts * 8 + (lane >> 3));
     float s = dots(v);
     if (part == 0) {
       if (bias && v < V) s += bias[v];
@@ -199,7 +202,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     if (v > -INFINITY && order_key(v) >= t) {
       const int q = atomicAdd(&count, 1);
       val_v[q] = v;
-      val_i[q] = sel[i / kCandRows] * kCandRows + i % kCandRows;
+      val_i[q] = CandBlocks::class_of(sel[i / kCandRows], i % kCandRows);
     }
   }
   __syncthreads();
@@ -228,34 +231,53 @@ int cand_pass_frames(int M, int V) {
   return std::min(M, std::max(most, 256));
 }
 
-// lambda, its pair, the normaliser's partial pairs and the block maxima of one pass.
-size_t cand_scratch_bytes(int M, int D, int V) {
-  const int F = std::max(1, cand_pass_frames(M, V));
-  return 2 * align_up(static_cast<size_t>(F) * 8, 256) + lse_partial_bytes(F, D) +
-         align_up(static_cast<size_t>(F) * cand_blocks(V) * sizeof(float), 256);
+namespace {
+// Scratch of a pass: lambda, its pair, the normaliser's partial pairs, the block maxima and, where the
+// product reads it, H transposed.
+struct CandLayout {
+  int frames, blocks;
+  size_t o_lam2, o_part, o_bmax, o_ht, total;
+};
+CandLayout cand_layout(int dtype, int M, int D, int V) {
+  CandLayout L;
+  L.frames = std::max(1, cand_pass_frames(M, V));
+  L.blocks = cand_blocks(V);
+  L.o_lam2 = align_up(static_cast<size_t>(L.frames) * 8, 256);
+  L.o_part = 2 * L.o_lam2;
+  L.o_bmax = L.o_part + lse_partial_bytes(L.frames, D);
+  L.o_ht = L.o_bmax + align_up(static_cast<size_t>(L.frames) * L.blocks * sizeof(float), 256);
+  L.total = L.o_ht + (dtype == 1 && frames_from_ht_bf16(L.frames, D, V) ? lse_ht_bytes_bf16(L.frames, D) : 0);
+  return L;
 }
+}  // namespace
+
+size_t cand_scratch_bytes(int dtype, int M, int D, int V) { return cand_layout(dtype, M, D, V).total; }
 
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
                                    int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
                                    hipStream_t stream) {
-  const int F = cand_pass_frames(M, V), nb = cand_blocks(V);
+  const CandLayout L = cand_layout(dtype, M, D, V);
+  const int F = L.frames, nb = L.blocks;
   char* s = static_cast<char*>(scratch);
   double* lam = reinterpret_cast<double*>(s);
-  s += align_up(static_cast<size_t>(F) * 8, 256);
-  float2* lam2 = reinterpret_cast<float2*>(s);
-  s += align_up(static_cast<size_t>(F) * 8, 256);
-  float2* partials = reinterpret_cast<float2*>(s);
-  float* bmax = reinterpret_cast<float*>(s + lse_partial_bytes(F, D));
+  float2* lam2 = reinterpret_cast<float2*>(s + L.o_lam2);
+  float2* partials = reinterpret_cast<float2*>(s + L.o_part);
+  float* bmax = reinterpret_cast<float*>(s + L.o_bmax);
   for (int m0 = 0; m0 < M; m0 += F) {
     const int here = std::min(F, M - m0);
     int P = 0;
     hipError_t e;
-    if (dtype == 1)
-      e = launch_cand_partial_bf16(static_cast<const uint16_t*>(H) + static_cast<int64_t>(m0) * D, here, D,
-                                   static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, stream);
-    else
+    if (dtype == 1) {
+      const uint16_t* Hm = static_cast<const uint16_t*>(H) + static_cast<int64_t>(m0) * D;
+      const int Mp = (here + 63) / 64 * 64;
+      uint16_t* Ht = frames_from_ht_bf16(here, D, V) ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
+      if (Ht && (e = launch_ht_build_bf16(Hm, here, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
+      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, stream,
+                                   Ht, Mp);
+    } else {
       e = launch_cand_partial_f32(static_cast<const float*>(H) + static_cast<int64_t>(m0) * D, here, D,
                                   static_cast<const float*>(W), bias, V, partials, &P, bmax, stream);
+    }
     if (e != hipSuccess) return e;
     e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
     if (e != hipSuccess) return e;

@@ -266,12 +266,14 @@ lse_partial_e_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ 
 // order.
 template <class G, bool BIAS>
 __global__ void __launch_bounds__(G::kThreads, 1)
-cand_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __restrict__ W,
-                  const float* __restrict__ bias, int V, int P, int vper, float2* __restrict__ partials, int nb,
-                  float* __restrict__ bmax) {
+cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ Ht, int Mp, int M, int D,
+                  const uint16_t* __restrict__ W, const float* __restrict__ bias, int V, int P, int vper,
+                  float2* __restrict__ partials, int nb, float* __restrict__ bmax) {
   extern __shared__ float bsh[];  // BIAS: b over this partition's rows
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
+  constexpr bool HT = std::is_same_v<G, GMidTW>;  // frames from Ht [D][Mp]
   PCTC_STAGES_G(G)
+  __shared__ char xch_[HT ? 4096 : 16];
   int mt, p;
   if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), (M + TC - 1) / TC, P, mt, p)) return;
   const int m0 = mt * TC;
@@ -284,7 +286,7 @@ cand_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* 
     __syncthreads();
   }
   const GOp A{W, D, vend, D, nullptr};
-  const GOp B{H, D, M, D, nullptr};
+  const GOp B = HT ? GOp{Ht, Mp, M, D, nullptr} : GOp{H, D, M, D, nullptr};
   float run_max[FC], run_sum[FC];
 #pragma unroll
   for (int j = 0; j < FC; ++j) {
@@ -295,14 +297,17 @@ cand_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* 
   auto epi = [&](int it, f32x16 (&a)[FR][FC]) {
     const int v0 = vbeg + it * TR;
     if (v0 + TR > vend) mask_rows_inf<FR, FC, G>(a, v0, vend, wave, lane);
-    const float4 blocks = lse_block_update<FR, FC, G>(a, lane, run_max, run_sum);
-    store_block_max<G>(blocks, v0, wave, lane, m0, M, nb, bmax);
+    float bm[FC][FR * 16 / kCandRows];
+    lse_block_update<FR, FC, G, kCandRows>(a, run_max, run_sum, bm);
+    store_block_max<G, kCandRows>(bm, v0, wave, lane, m0, M, nb, bmax);
   };
-  G::run_seq(A, B, vbeg, m0, ntiles, D, st, acc, epi, [&](int it, f32x16 (&a)[FR][FC]) {
+  auto init = [&](int it, f32x16 (&a)[FR][FC]) {
     if constexpr (BIAS) bias_init<FR, FC, G>(a, bsh + it * TR, wave, lane);
     else G::zero(a);
-  });
-  lse_store_partials<G>(run_max, run_sum, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
+  };
+  if constexpr (HT) G::template seq_aligned<0>(A, B, vbeg, m0, ntiles, D, acc, epi, init);
+  else G::run_seq(A, B, vbeg, m0, ntiles, D, st, acc, epi, init);
+  lse_store_partials<G>(run_max, run_sum, HT ? xch_ : st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1247,21 +1252,26 @@ hipError_t launch_amax_partial_bf16(const uint16_t* H, int M, int D, const uint1
 }
 
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                    float2* partials, int* P_out, float* bmax, hipStream_t stream) {
+                                    float2* partials, int* P_out, float* bmax, hipStream_t stream, const uint16_t* Ht,
+                                    int Mp) {
   const LseSplit sp = lse_split_bf16(M, D, V, SplitFor::kAmax);
   *P_out = sp.P;
   Prof pr("cand_partial", stream);
   const size_t bsh = bias ? static_cast<size_t>(sp.vper) * sizeof(float) : 0;
   const dim3 grid(grouped_grid(sp.nM, sp.P));
-#define PCTC_CAND(G, BIAS)                                                                                       \
-  hipLaunchKernelGGL((cand_partial_bf16<G, BIAS>), grid, dim3(G::kThreads), bsh, stream, H, M, D, W, bias, V, sp.P, \
-                     sp.vper, partials, cand_blocks(V), bmax)
+#define PCTC_CAND(G)                                                                                               \
+  if (bias)                                                                                                        \
+    hipLaunchKernelGGL((cand_partial_bf16<G, true>), grid, dim3(G::kThreads), bsh, stream, H, Ht, Mp, M, D, W,     \
+                       bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);                                    \
+  else                                                                                                             \
+    hipLaunchKernelGGL((cand_partial_bf16<G, false>), grid, dim3(G::kThreads), 0, stream, H, Ht, Mp, M, D, W,      \
+                       bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);
   if (sp.wide) {
-    if (bias) PCTC_CAND(GWide, true);
-    else PCTC_CAND(GWide, false);
+    PCTC_CAND(GWide)
+  } else if (Ht) {
+    PCTC_CAND(GMidTW)
   } else {
-    if (bias) PCTC_CAND(GMid, true);
-    else PCTC_CAND(GMid, false);
+    PCTC_CAND(GMid)
   }
 #undef PCTC_CAND
   return hipGetLastError();

@@ -150,8 +150,9 @@ cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
     run_sum[j] = 0.f;
   }
   vocab_tiles<BIAS>(H, M, D, W, bias, m0, vbeg, vend, st, [&](int v0, int el, f32x16 (&a)[GZ::FR][GZ::FC]) {
-    const float4 blocks = lse_block_update<GZ::FR, GZ::FC, GZ>(a, el, run_max, run_sum);
-    store_block_max<GZ>(blocks, v0, wave, el, m0, M, nb, bmax);
+    float bm[GZ::FC][GZ::FR * 16 / kCandRows];
+    lse_block_update<GZ::FR, GZ::FC, GZ, kCandRows>(a, run_max, run_sum, bm);
+    store_block_max<GZ, kCandRows>(bm, v0, wave, el, m0, M, nb, bmax);
   });
   lse_store_partials<GZ>(run_max, run_sum, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }

@@ -126,30 +126,27 @@ __device__ __forceinline__ void lse_tile_update(const f32x16 (&acc)[FR][FC], flo
   }
 }
 
-// The same; returns the largest logit of each of the wavefront's four 32-row blocks (all 32 rows) for
-// the frame of the lane's half: lanes [0, 32) frame column 0, the others column 1.
-template <int FR, int FC, class G>
-__device__ __forceinline__ float4 lse_block_update(const f32x16 (&acc)[FR][FC], int lane, float (&run_max)[FC],
-                                                   float (&run_sum)[FC]) {
-  static_assert(FR == 4 && FC == 2, "four blocks of 32 rows by two frame columns");
-  float4 blocks = make_float4(0.f, 0.f, 0.f, 0.f);
+// The same, and bm[j][..]: the largest logits of the lane's blocks of frame column j.  A block is ROWS
+// of the 16 rows that a lane holds of 32: of rows 8 q + 4 h + e (h the lane's half, e < 4) those of ROWS / 4
+// consecutive q.
+template <int FR, int FC, class G, int ROWS>
+__device__ __forceinline__ void lse_block_update(const f32x16 (&acc)[FR][FC], float (&run_max)[FC],
+                                                 float (&run_sum)[FC], float (&bm)[FC][FR * 16 / ROWS]) {
+  constexpr int kSub = 16 / ROWS;
 #pragma unroll
   for (int j = 0; j < FC; ++j) {
-    float bm[FR];
     float tmax = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < FR; ++i) {
-      float x = acc[i][j][0];
+    for (int i = 0; i < FR; ++i)
 #pragma unroll
-      for (int r = 1; r < 16; ++r) x = fmaxf(x, acc[i][j][r]);
-      bm[i] = fmaxf(x, swap_halves(x));
-      tmax = fmaxf(tmax, bm[i]);
-    }
-    const bool mine = (lane >> 5) == j;
-    blocks.x = mine ? bm[0] : blocks.x;
-    blocks.y = mine ? bm[1] : blocks.y;
-    blocks.z = mine ? bm[2] : blocks.z;
-    blocks.w = mine ? bm[3] : blocks.w;
+      for (int u = 0; u < kSub; ++u) {
+        float x = acc[i][j][u * ROWS];
+#pragma unroll
+        for (int r = 1; r < ROWS; ++r) x = fmaxf(x, acc[i][j][u * ROWS + r]);
+        bm[j][i * kSub + u] = x;
+        tmax = fmaxf(tmax, x);
+      }
+    tmax = fmaxf(tmax, swap_halves(tmax));
     const float nmax = fmaxf(run_max[j], tmax);
     // a column with no finite logit yet (rows masked by a -inf bias) adds nothing
     const float ms = (nmax == -INFINITY) ? 0.f : nmax * kLog2e;
@@ -172,16 +169,25 @@ __device__ __forceinline__ float4 lse_block_update(const f32x16 (&acc)[FR][FC], 
     run_sum[j] = fmaf(run_sum[j], scale, s);
     run_max[j] = nmax;
   }
-  return blocks;
 }
 
-// Writes the block maxima of a tile whose first class is v0 (a frame's row has nb of them).
-template <class G>
-__device__ __forceinline__ void store_block_max(const float4& blocks, int v0, int wave, int lane, int m0, int M,
-                                                int nb, float* __restrict__ bmax) {
-  const int m = m0 + G::col_of(wave, lane, 0) + 32 * (lane >> 5);
-  const int blk = (v0 + G::row_of(wave, 0, 0, 0)) >> 5;
-  if (m < M) *reinterpret_cast<float4*>(bmax + static_cast<int64_t>(m) * nb + blk) = blocks;
+// Writes the block maxima of a tile whose first class is v0; a frame's row has nb of them, a lane's
+// side by side (CandBlocks in pctc_internal.h has the order).
+template <class G, int ROWS>
+__device__ __forceinline__ void store_block_max(const float (&bm)[G::FC][G::FR * 16 / ROWS], int v0, int wave, int lane,
+                                                int m0, int M, int nb, float* __restrict__ bmax) {
+  constexpr int kRun = G::FR * 16 / ROWS;
+  static_assert(G::FR == 4 && kRun % 4 == 0, "wavefronts of 128 rows");
+  const int at = ((v0 + G::row_of(wave, 0, 0, 0)) >> 7) * 2 * kRun + (lane >> 5) * kRun;
+#pragma unroll
+  for (int j = 0; j < G::FC; ++j) {
+    const int m = m0 + G::col_of(wave, lane, j);
+    if (m >= M) continue;
+    float4* const out = reinterpret_cast<float4*>(bmax + static_cast<int64_t>(m) * nb + at);
+#pragma unroll
+    for (int k = 0; k < kRun / 4; ++k)
+      out[k] = make_float4(bm[j][4 * k], bm[j][4 * k + 1], bm[j][4 * k + 2], bm[j][4 * k + 3]);
+  }
 }
 
 // The two wavefronts of each frame column (row halves) combine their running (max, sum)

@@ -255,18 +255,36 @@ hipError_t launch_grouped_adapter(const float* logp, const float* dlogp, int K, 
                                   hipStream_t stream);
 
 // ---- frame candidates (frame_candidates.hip; products in head_gemm_bf16.hip, head_gemm_f32.hip) ----
-constexpr int kCandRows = 32;      // classes of a block: the products keep a block's largest logit per frame
+constexpr int kCandRows = 16;  // classes of a block: the products keep a block's largest logit per frame
 constexpr int kMaxCandidates = 64;
 inline int cand_blocks(int V) { return (V + 255) / 256 * (256 / kCandRows); }  // a frame's block maxima
-// The normaliser's partial pairs and bmax[m * cand_blocks(V) + i], the largest logit of classes
-// [32 i, 32 i + 32) (-inf past V).
+// The blocks.  Two of them share 2 kCandRows consecutive classes, four and four in turn (what the two
+// lane halves of a matrix-core accumulator hold); block 2 g + h has the h-th fours of group g.  In a
+// frame's row of maxima they lie as the lanes write them: per 128 classes the first halves' blocks, then the
+// second halves'.
+struct CandBlocks {
+  static constexpr int kRun = 64 / kCandRows;  // groups of 128 classes
+  static __host__ __device__ __forceinline__ int place(int block) {
+    const int g = block >> 1;
+    return (g / kRun * 2 + (block & 1)) * kRun + g % kRun;
+  }
+  static __host__ __device__ __forceinline__ int at(int place) {
+    return (place / (2 * kRun) * kRun + place % kRun) * 2 + (place / kRun & 1);
+  }
+  static __host__ __device__ __forceinline__ int class_of(int block, int k) {  // the k-th of a block
+    return (block >> 1) * 2 * kCandRows + (k >> 2) * 8 + (block & 1) * 4 + (k & 3);
+  }
+};
+// The normaliser's partial pairs and bmax[m * cand_blocks(V) + i], the block maxima of frame m (-inf
+// past V).  Ht (null: none): H transposed [D][Mp], as for the argmax.
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                    float2* partials, int* P_out, float* bmax, hipStream_t stream);
+                                    float2* partials, int* P_out, float* bmax, hipStream_t stream,
+                                    const uint16_t* Ht = nullptr, int Mp = 0);
 hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
                                    float2* partials, int* P_out, float* bmax, hipStream_t stream);
 // Frames of one pass over the vocabulary, and the scratch of a call.
 int cand_pass_frames(int M, int V);
-size_t cand_scratch_bytes(int M, int D, int V);
+size_t cand_scratch_bytes(int dtype, int M, int D, int V);
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
                                    int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
                                    hipStream_t stream);

@@ -86,9 +86,11 @@ def test_sizes():
                 (1, 4, 512, 1000, 0), (1, 4, 512, 1000, 65), (1, 4, 512, 524_289, 16)):
         assert c(*bad) == 0, bad
     # the block maxima are held to 256 MiB: more frames take more passes, not more memory (the
-    # normaliser's partial sums grow with the frames of a pass alone)
+    # normaliser's partial sums and a transposed H grow with the frames of a pass alone)
     for D in (512, 4096):
-        assert c(1, 400_000, D, 180_000, 16) == c(0, 100_000, D, 180_000, 64) < (256 << 20) + 12_000 * 8 * 1030
+        for dt in (0, 1):
+            assert c(dt, 400_000, D, 180_000, 16) == c(dt, 100_000, D, 180_000, 64) \
+                < (256 << 20) + 6_144 * (8 * 1030 + 2 * D)
     d = L.pctc_beam_decode_workspace_size
     T = i32(30, 20)
     assert d(1, p(T), 2, 512, 1000, 8, 16) > c(1, 50, 512, 1000, 16)
