@@ -6,11 +6,11 @@
 //   of falling z, the lowest class first among equal ones
 //
 // One vocabulary pass on the matrix cores gives the normaliser's partial pairs and the largest logit
-// of every block of 16 classes.  A class among a frame's C best lies in one of the C + 1 blocks with the
+// of every block of R classes, R = 16, or 8 for long rows of W.  A class among a frame's C best lies in one of the C + 1 blocks with the
 // largest maxima (one more for blank, which is left out; and one for the block whose classes lie between
-// the last one's, where maxima are equal), so a second kernel forms those blocks' logits again, 16 (C + 2)
-// dot products a frame, and orders them.  M V / 16 maxima are written and read (190 MB at 4,215 frames of
-// 180,000 classes) and W rows for 16 (C + 2) classes a frame are read again, through the L2s.  The scratch for
+// the last one's, where maxima are equal), so a second kernel forms those blocks' logits again, R (C + 2)
+// dot products a frame, and orders them.  M V / R maxima are written and read (190 MB at 4,215 frames of
+// 180,000 classes) and W rows for R (C + 2) classes a frame are read again, through the L2s.  The scratch for
 // the maxima is held to 256 MB by passing over the vocabulary once per that many frames.
 #include <algorithm>
 
@@ -24,7 +24,6 @@ constexpr size_t kMaxBlockBytes = static_cast<size_t>(256) << 20;
 constexpr int kThreads = 256;
 constexpr int kList = 256;  // blocks kept for ordering; more only where maxima are equal
 constexpr int kMaxSel = kMaxCandidates + 2;
-constexpr int kValues = kMaxSel * kCandRows;
 
 // Floats in the order of unsigned integers.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -49,11 +48,12 @@ __device__ __forceinline__ uint32_t reach(const uint32_t* keys, int need, int la
   return t;
 }
 
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, uint16_t) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    s = fmaf(__uint_as_float(w[q] << 16), __uint_as_float(h[q] << 16), s);
-    s = fmaf(__uint_as_float(w[q] & 0xffff0000u), __uint_as_float(h[q] & 0xffff0000u), s);
+    const uint32_t a = w[q], b = h[q];
+    s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), s, false);
   }
   return s;
 }
@@ -66,12 +66,14 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 }  // namespace
 
 // One workgroup per frame.
-template <class T>
+template <class T, int ROWS>
 __global__ void __launch_bounds__(kThreads)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
                    int V, int blank, int C, const float* __restrict__ bmax, int nb, const double* __restrict__ lam,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
+  using Blocks = CandBlocks<ROWS>;
   constexpr int kPer = 16 / sizeof(T);
+  constexpr int kValues = kMaxSel * ROWS;
   __shared__ uint32_t keys[kThreads];
   __shared__ float list_v[kList];
   __shared__ int list_b[kList];
@@ -96,7 +98,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   if (tid == 0) count = 0;
   __syncthreads();
   uint32_t t = reach(keys, nsel, lane);
-  for (int i = tid * 4; i < nb; i += kThreads * 4) {
+  // (most threads have no block that large)
+  for (int i = order_key(mx) >= t ? tid * 4 : nb; i < nb; i += kThreads * 4) {
     const float4 v4 = *reinterpret_cast<const float4*>(row + i);
     const float v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
@@ -105,7 +108,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
         const int q = atomicAdd(&count, 1);
         if (q < kList) {
           list_v[q] = v[e];
-          list_b[q] = CandBlocks::at(i + e);
+          list_b[q] = Blocks::at(i + e);
         }
       }
     }
@@ -141,12 +144,12 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     if (tid == 0) count = 0;
     __syncthreads();
     for (int i = tid; i < nb; i += kThreads)
-      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = CandBlocks::at(i);
+      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = Blocks::at(i);
     __syncthreads();
     n = count;
     if (wave == 0) {
       for (int i0 = 0; i0 < nb && n < nsel; i0 += 64) {
-        const float v = i0 + lane < nb ? row[CandBlocks::place(i0 + lane)] : -INFINITY;
+        const float v = i0 + lane < nb ? row[Blocks::place(i0 + lane)] : -INFINITY;
         const bool at = v > -INFINITY && order_key(v) == t;
         const uint64_t who = __ballot(at);
         const int q = n + __popcll(who & ((uint64_t{1} << lane) - 1));
@@ -160,38 +163,50 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   }
   __syncthreads();
 
-  // ---- their logits: eight lanes a class, eight classes of a wavefront at a time ----
+  // ---- their logits: eight lanes a class, a block of a wavefront at a time ----
   const T* const h = H + static_cast<int64_t>(m) * D;
   const int part = lane & 7;
-  auto dots = [&](int v) {  // class v's logit without bias, in each of its eight lanes (v >= V: 0)
-    float s = 0.f;
-    if (v < V) {
-      const T* const w = W + static_cast<int64_t>(v) * D;
-      for (int k = part * kPer; k < D; k += 8 * kPer)
-        s = dot16(*reinterpret_cast<const u32x4*>(w + k), *reinterpret_cast<const u32x4*>(h + k), s, T{});
+  constexpr int kSets = ROWS / 8;  // of eight classes
+  auto dots = [&](const int (&v)[kSets], float (&s)[kSets]) {  // in each of a class's eight lanes (v >= V: as V - 1)
+    const T* w[kSets];
+#pragma unroll
+    for (int e = 0; e < kSets; ++e) {
+      w[e] = W + static_cast<int64_t>(min(v[e], V - 1)) * D;
+      s[e] = 0.f;
+    }
+#pragma unroll 4
+    for (int k = part * kPer; k < D; k += 8 * kPer) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(h + k);
+#pragma unroll
+      for (int e = 0; e < kSets; ++e) s[e] = dot16(*reinterpret_cast<const u32x4*>(w[e] + k), x, s[e], T{});
     }
 #pragma unroll
-    for (int o = 4; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
-    return s;
+    for (int o = 4; o >= 1; o >>= 1)
+#pragma unroll
+      for (int e = 0; e < kSets; ++e) s[e] += __shfl_xor(s[e], o, 64);
   };
-  constexpr int kParts = kCandRows / 8;
-  for (int g = wave; g < n * kParts; g += kThreads / 64) {  // groups of eight classes
-    const int v = CandBlocks::class_of(sel[g / kParts], g % kParts * 8 + (lane >> 3));
-    float s = dots(v);
-    if (part == 0) {
-      if (bias && v < V) s += bias[v];
-      z[g * 8 + (lane >> 3)] = (v < V && v != blank) ? s : -INFINITY;
+  for (int g = wave; g <= n; g += kThreads / 64) {  // (the last: blank)
+    int v[kSets];
+    float s[kSets];
+#pragma unroll
+    for (int e = 0; e < kSets; ++e) v[e] = g < n ? Blocks::class_of(sel[g], e * 8 + (lane >> 3)) : blank;
+    dots(v, s);
+#pragma unroll
+    for (int e = 0; e < kSets; ++e) {
+      if (part != 0 || v[e] >= V) {
+        if (part == 0) z[g * ROWS + e * 8 + (lane >> 3)] = -INFINITY;
+        continue;
+      }
+      if (bias) s[e] += bias[v[e]];
+      if (g == n) zblank = s[e];  // every class's first lane holds it
+      else z[g * ROWS + e * 8 + (lane >> 3)] = v[e] == blank ? -INFINITY : s[e];
     }
-  }
-  if (wave == kThreads / 64 - 1) {
-    float s = dots(blank);
-    if (lane == 0) zblank = bias ? s + bias[blank] : s;
   }
   if (tid == 0) count = 0;
   __syncthreads();
 
   // ---- the C best of them ----
-  const int nz = n * kCandRows;
+  const int nz = n * ROWS;
   mx = -INFINITY;
   for (int i = tid; i < nz; i += kThreads) mx = fmaxf(mx, z[i]);
   keys[tid] = order_key(mx);
@@ -202,7 +217,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     if (v > -INFINITY && order_key(v) >= t) {
       const int q = atomicAdd(&count, 1);
       val_v[q] = v;
-      val_i[q] = CandBlocks::class_of(sel[i / kCandRows], i % kCandRows);
+      val_i[q] = Blocks::class_of(sel[i / ROWS], i % ROWS);
     }
   }
   __syncthreads();
@@ -225,8 +240,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   if (tid == 0) blank_logp[m] = static_cast<float>(zblank - l);
 }
 
-int cand_pass_frames(int M, int V) {
-  const size_t per = static_cast<size_t>(cand_blocks(V)) * sizeof(float);
+int cand_pass_frames(int dtype, int M, int D, int V) {
+  const size_t per = static_cast<size_t>(cand_blocks(V, cand_rows(dtype, D))) * sizeof(float);
   const int most = static_cast<int>(std::min<size_t>(kMaxBlockBytes / per / 256 * 256, 1 << 30));
   return std::min(M, std::max(most, 256));
 }
@@ -240,8 +255,8 @@ struct CandLayout {
 };
 CandLayout cand_layout(int dtype, int M, int D, int V) {
   CandLayout L;
-  L.frames = std::max(1, cand_pass_frames(M, V));
-  L.blocks = cand_blocks(V);
+  L.frames = std::max(1, cand_pass_frames(dtype, M, D, V));
+  L.blocks = cand_blocks(V, cand_rows(dtype, D));
   L.o_lam2 = align_up(static_cast<size_t>(L.frames) * 8, 256);
   L.o_part = 2 * L.o_lam2;
   L.o_bmax = L.o_part + lse_partial_bytes(L.frames, D);
@@ -282,14 +297,18 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
     e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
     if (e != hipSuccess) return e;
     Prof pr("cand_select", stream);
-    if (dtype == 1)
-      hipLaunchKernelGGL(cand_select_kernel<uint16_t>, dim3(here), dim3(kThreads), 0, stream,
-                         static_cast<const uint16_t*>(H), m0, D, static_cast<const uint16_t*>(W), bias, V, blank, C,
-                         bmax, nb, lam, ids, logp, blank_logp);
-    else
-      hipLaunchKernelGGL(cand_select_kernel<float>, dim3(here), dim3(kThreads), 0, stream,
-                         static_cast<const float*>(H), m0, D, static_cast<const float*>(W), bias, V, blank, C, bmax,
-                         nb, lam, ids, logp, blank_logp);
+    const bool short_blocks = cand_rows(dtype, D) == 8;
+#define PCTC_SELECT(T, ROWS)                                                                                       \
+  hipLaunchKernelGGL((cand_select_kernel<T, ROWS>), dim3(here), dim3(kThreads), 0, stream, static_cast<const T*>(H), \
+                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, lam, ids, logp, blank_logp)
+    if (dtype == 1) {
+      if (short_blocks) PCTC_SELECT(uint16_t, 8);
+      else PCTC_SELECT(uint16_t, 16);
+    } else {
+      if (short_blocks) PCTC_SELECT(float, 8);
+      else PCTC_SELECT(float, 16);
+    }
+#undef PCTC_SELECT
   }
   return hipGetLastError();
 }
