@@ -353,8 +353,8 @@ int32_t pctc_grouped_backward(pctc_dtype dtype, const void* H, int32_t M, int32_
  *      among equal ones) and float(z - lambda); where fewer than C classes have a logit above -inf,
  *      the rest are -1 and -inf.  NaN or +inf logits give unspecified rows.
  * blank_logp  device float [M].
- * workspace: pctc_frame_candidates_workspace_size() bytes, 256-byte aligned; at most about 256 MiB
- *      (kept per frame and block of 32 classes; more frames than fit take another pass over W) beside
+ * workspace: pctc_frame_candidates_workspace_size() bytes, 256-byte aligned; at most about 512 MiB
+ *      (kept per frame and block of 8 classes; more frames than fit take another pass over W) beside
  *      the normaliser's partial sums.  Returns 0 for invalid arguments.
  * Asynchronous. */
 size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C);

@@ -6,12 +6,12 @@
 //   of falling z, the lowest class first among equal ones
 //
 // One vocabulary pass on the matrix cores gives the normaliser's partial pairs and the largest logit
-// of every block of R classes, R = 16, or 8 for long rows of W.  A class among a frame's C best lies in one of the C + 1 blocks with the
+// of every block of 8 classes.  A class among a frame's C best lies in one of the C + 1 blocks with the
 // largest maxima (one more for blank, which is left out; and one for the block whose classes lie between
-// the last one's, where maxima are equal), so a second kernel forms those blocks' logits again, R (C + 2)
-// dot products a frame, and orders them.  M V / R maxima are written and read (190 MB at 4,215 frames of
-// 180,000 classes) and W rows for R (C + 2) classes a frame are read again, through the L2s.  The scratch for
-// the maxima is held to 256 MB by passing over the vocabulary once per that many frames.
+// the last one's, where maxima are equal), so a second kernel forms those blocks' logits again, 8 (C + 2)
+// dot products a frame, and orders them.  M V / 8 maxima are written and read (380 MB at 4,215 frames of
+// 180,000 classes) and W rows for 8 (C + 2) classes a frame are read again, through the L2s.  The scratch for
+// the maxima is held to 512 MB by passing over the vocabulary once per that many frames.
 #include <algorithm>
 
 #include "pctc_internal.h"
@@ -20,7 +20,7 @@ namespace pctc {
 
 namespace {
 
-constexpr size_t kMaxBlockBytes = static_cast<size_t>(256) << 20;
+constexpr size_t kMaxBlockBytes = static_cast<size_t>(512) << 20;
 constexpr int kThreads = 256;
 constexpr int kList = 256;  // blocks kept for ordering; more only where maxima are equal
 constexpr int kMaxSel = kMaxCandidates + 2;
@@ -66,14 +66,13 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 }  // namespace
 
 // One workgroup per frame.
-template <class T, int ROWS>
+template <class T>
 __global__ void __launch_bounds__(kThreads)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
                    int V, int blank, int C, const float* __restrict__ bmax, int nb, const double* __restrict__ lam,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
-  using Blocks = CandBlocks<ROWS>;
   constexpr int kPer = 16 / sizeof(T);
-  constexpr int kValues = kMaxSel * ROWS;
+  constexpr int kValues = kMaxSel * kCandRows;
   __shared__ uint32_t keys[kThreads];
   __shared__ float list_v[kList];
   __shared__ int list_b[kList];
@@ -108,7 +107,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
         const int q = atomicAdd(&count, 1);
         if (q < kList) {
           list_v[q] = v[e];
-          list_b[q] = Blocks::at(i + e);
+          list_b[q] = CandBlocks::at(i + e);
         }
       }
     }
@@ -144,12 +143,12 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     if (tid == 0) count = 0;
     __syncthreads();
     for (int i = tid; i < nb; i += kThreads)
-      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = Blocks::at(i);
+      if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = CandBlocks::at(i);
     __syncthreads();
     n = count;
     if (wave == 0) {
       for (int i0 = 0; i0 < nb && n < nsel; i0 += 64) {
-        const float v = i0 + lane < nb ? row[Blocks::place(i0 + lane)] : -INFINITY;
+        const float v = i0 + lane < nb ? row[CandBlocks::place(i0 + lane)] : -INFINITY;
         const bool at = v > -INFINITY && order_key(v) == t;
         const uint64_t who = __ballot(at);
         const int q = n + __popcll(who & ((uint64_t{1} << lane) - 1));
@@ -166,7 +165,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   // ---- their logits: eight lanes a class, a block of a wavefront at a time ----
   const T* const h = H + static_cast<int64_t>(m) * D;
   const int part = lane & 7;
-  constexpr int kSets = ROWS / 8;  // of eight classes
+  constexpr int kSets = kCandRows / 8;  // of eight classes
   auto dots = [&](const int (&v)[kSets], float (&s)[kSets]) {  // in each of a class's eight lanes (v >= V: as V - 1)
     const T* w[kSets];
 #pragma unroll
@@ -189,24 +188,24 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     int v[kSets];
     float s[kSets];
 #pragma unroll
-    for (int e = 0; e < kSets; ++e) v[e] = g < n ? Blocks::class_of(sel[g], e * 8 + (lane >> 3)) : blank;
+    for (int e = 0; e < kSets; ++e) v[e] = g < n ? CandBlocks::class_of(sel[g], e * 8 + (lane >> 3)) : blank;
     dots(v, s);
 #pragma unroll
     for (int e = 0; e < kSets; ++e) {
       if (part != 0 || v[e] >= V) {
-        if (part == 0) z[g * ROWS + e * 8 + (lane >> 3)] = -INFINITY;
+        if (part == 0) z[g * kCandRows + e * 8 + (lane >> 3)] = -INFINITY;
         continue;
       }
       if (bias) s[e] += bias[v[e]];
       if (g == n) zblank = s[e];  // every class's first lane holds it
-      else z[g * ROWS + e * 8 + (lane >> 3)] = v[e] == blank ? -INFINITY : s[e];
+      else z[g * kCandRows + e * 8 + (lane >> 3)] = v[e] == blank ? -INFINITY : s[e];
     }
   }
   if (tid == 0) count = 0;
   __syncthreads();
 
   // ---- the C best of them ----
-  const int nz = n * ROWS;
+  const int nz = n * kCandRows;
   mx = -INFINITY;
   for (int i = tid; i < nz; i += kThreads) mx = fmaxf(mx, z[i]);
   keys[tid] = order_key(mx);
@@ -217,7 +216,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     if (v > -INFINITY && order_key(v) >= t) {
       const int q = atomicAdd(&count, 1);
       val_v[q] = v;
-      val_i[q] = Blocks::class_of(sel[i / ROWS], i % ROWS);
+      val_i[q] = CandBlocks::class_of(sel[i / kCandRows], i % kCandRows);
     }
   }
   __syncthreads();
@@ -240,8 +239,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   if (tid == 0) blank_logp[m] = static_cast<float>(zblank - l);
 }
 
-int cand_pass_frames(int dtype, int M, int D, int V) {
-  const size_t per = static_cast<size_t>(cand_blocks(V, cand_rows(dtype, D))) * sizeof(float);
+int cand_pass_frames(int M, int V) {
+  const size_t per = static_cast<size_t>(cand_blocks(V)) * sizeof(float);
   const int most = static_cast<int>(std::min<size_t>(kMaxBlockBytes / per / 256 * 256, 1 << 30));
   return std::min(M, std::max(most, 256));
 }
@@ -255,8 +254,8 @@ struct CandLayout {
 };
 CandLayout cand_layout(int dtype, int M, int D, int V) {
   CandLayout L;
-  L.frames = std::max(1, cand_pass_frames(dtype, M, D, V));
-  L.blocks = cand_blocks(V, cand_rows(dtype, D));
+  L.frames = std::max(1, cand_pass_frames(M, V));
+  L.blocks = cand_blocks(V);
   L.o_lam2 = align_up(static_cast<size_t>(L.frames) * 8, 256);
   L.o_part = 2 * L.o_lam2;
   L.o_bmax = L.o_part + lse_partial_bytes(L.frames, D);
@@ -297,18 +296,14 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
     e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
     if (e != hipSuccess) return e;
     Prof pr("cand_select", stream);
-    const bool short_blocks = cand_rows(dtype, D) == 8;
-#define PCTC_SELECT(T, ROWS)                                                                                       \
-  hipLaunchKernelGGL((cand_select_kernel<T, ROWS>), dim3(here), dim3(kThreads), 0, stream, static_cast<const T*>(H), \
-                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, lam, ids, logp, blank_logp)
-    if (dtype == 1) {
-      if (short_blocks) PCTC_SELECT(uint16_t, 8);
-      else PCTC_SELECT(uint16_t, 16);
-    } else {
-      if (short_blocks) PCTC_SELECT(float, 8);
-      else PCTC_SELECT(float, 16);
-    }
-#undef PCTC_SELECT
+    if (dtype == 1)
+      hipLaunchKernelGGL(cand_select_kernel<uint16_t>, dim3(here), dim3(kThreads), 0, stream,
+                         static_cast<const uint16_t*>(H), m0, D, static_cast<const uint16_t*>(W), bias, V, blank, C,
+                         bmax, nb, lam, ids, logp, blank_logp);
+    else
+      hipLaunchKernelGGL(cand_select_kernel<float>, dim3(here), dim3(kThreads), 0, stream,
+                         static_cast<const float*>(H), m0, D, static_cast<const float*>(W), bias, V, blank, C, bmax,
+                         nb, lam, ids, logp, blank_logp);
   }
   return hipGetLastError();
 }

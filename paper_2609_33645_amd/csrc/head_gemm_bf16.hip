@@ -272,7 +272,6 @@ cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ H
   extern __shared__ float bsh[];  // BIAS: b over this partition's rows
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   constexpr bool HT = std::is_same_v<G, GMidTW>;  // frames from Ht [D][Mp]
-  constexpr int kRows = std::is_same_v<G, GWide> ? 8 : 16;  // cand_rows
   PCTC_STAGES_G(G)
   __shared__ char xch_[HT ? 4096 : 16];
   int mt, p;
@@ -298,9 +297,9 @@ cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ H
   auto epi = [&](int it, f32x16 (&a)[FR][FC]) {
     const int v0 = vbeg + it * TR;
     if (v0 + TR > vend) mask_rows_inf<FR, FC, G>(a, v0, vend, wave, lane);
-    float bm[FC][FR * 16 / kRows];
-    lse_block_update<FR, FC, G, kRows>(a, run_max, run_sum, bm);
-    store_block_max<G, kRows>(bm, v0, wave, lane, m0, M, nb, bmax);
+    float bm[FC][FR * 16 / kCandRows];
+    lse_block_update<FR, FC, G, kCandRows>(a, run_max, run_sum, bm);
+    store_block_max<G, kCandRows>(bm, v0, wave, lane, m0, M, nb, bmax);
   };
   auto init = [&](int it, f32x16 (&a)[FR][FC]) {
     if constexpr (BIAS) bias_init<FR, FC, G>(a, bsh + it * TR, wave, lane);
@@ -1263,10 +1262,10 @@ hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint1
 #define PCTC_CAND(G)                                                                                               \
   if (bias)                                                                                                        \
     hipLaunchKernelGGL((cand_partial_bf16<G, true>), grid, dim3(G::kThreads), bsh, stream, H, Ht, Mp, M, D, W,     \
-                       bias, V, sp.P, sp.vper, partials, cand_blocks(V, cand_rows(1, D)), bmax);                                    \
+                       bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);                                    \
   else                                                                                                             \
     hipLaunchKernelGGL((cand_partial_bf16<G, false>), grid, dim3(G::kThreads), 0, stream, H, Ht, Mp, M, D, W,      \
-                       bias, V, sp.P, sp.vper, partials, cand_blocks(V, cand_rows(1, D)), bmax);
+                       bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);
   if (sp.wide) {
     PCTC_CAND(GWide)
   } else if (Ht) {

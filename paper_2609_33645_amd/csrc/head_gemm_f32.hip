@@ -132,8 +132,8 @@ amax_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
   amax_store_partials<GZ>(bv, bi, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
 
-// The normaliser with each frame's block maxima beside it (frame candidates; ROWS: cand_rows).
-template <bool BIAS, int ROWS>
+// The normaliser with each frame's block maxima beside it (frame candidates).
+template <bool BIAS>
 __global__ void __launch_bounds__(512, 1)
 cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restrict__ W,
                  const float* __restrict__ bias, int V, int P, int vper, float2* __restrict__ partials, int nb,
@@ -150,9 +150,9 @@ cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
     run_sum[j] = 0.f;
   }
   vocab_tiles<BIAS>(H, M, D, W, bias, m0, vbeg, vend, st, [&](int v0, int el, f32x16 (&a)[GZ::FR][GZ::FC]) {
-    float bm[GZ::FC][GZ::FR * 16 / ROWS];
-    lse_block_update<GZ::FR, GZ::FC, GZ, ROWS>(a, run_max, run_sum, bm);
-    store_block_max<GZ, ROWS>(bm, v0, wave, el, m0, M, nb, bmax);
+    float bm[GZ::FC][GZ::FR * 16 / kCandRows];
+    lse_block_update<GZ::FR, GZ::FC, GZ, kCandRows>(a, run_max, run_sum, bm);
+    store_block_max<GZ, kCandRows>(bm, v0, wave, el, m0, M, nb, bmax);
   });
   lse_store_partials<GZ>(run_max, run_sum, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
@@ -492,18 +492,12 @@ hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W,
   *P_out = P;
   const dim3 grid(grouped_grid((M + kTile - 1) / kTile, P));
   Prof pr("cand_partial", stream);
-  const int rows = cand_rows(0, D);
-#define PCTC_CAND(BIAS, ROWS)                                                                                       \
-  hipLaunchKernelGGL((cand_partial_f32<BIAS, ROWS>), grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper,       \
-                     partials, cand_blocks(V, ROWS), bmax)
-  if (bias) {
-    if (rows == 8) PCTC_CAND(true, 8);
-    else PCTC_CAND(true, 16);
-  } else {
-    if (rows == 8) PCTC_CAND(false, 8);
-    else PCTC_CAND(false, 16);
-  }
-#undef PCTC_CAND
+  if (bias)
+    hipLaunchKernelGGL(cand_partial_f32<true>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,
+                       cand_blocks(V), bmax);
+  else
+    hipLaunchKernelGGL(cand_partial_f32<false>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,
+                       cand_blocks(V), bmax);
   return hipGetLastError();
 }
 

@@ -256,18 +256,18 @@ hipError_t launch_grouped_adapter(const float* logp, const float* dlogp, int K, 
 
 // ---- frame candidates (frame_candidates.hip; products in head_gemm_bf16.hip, head_gemm_f32.hip) ----
 constexpr int kMaxCandidates = 64;
-// Classes of a block (the products keep a block's largest logit per frame): 16, and 8 where a class's
-// row of W is 4 KB and more, so that reading a block's rows again costs more than twice as many maxima.
-// D = 4,096, V = 151,936, 2,500 frames, 8 classes: selection PCTC_A us with 8, PCTC_B with 16.
-inline int cand_rows(int dtype, int D) { return static_cast<int64_t>(D) * (dtype == 1 ? 2 : 4) >= 4096 ? 8 : 16; }
-inline int cand_blocks(int V, int rows) { return (V + 255) / 256 * (256 / rows); }  // a frame's block maxima
-// The blocks.  Two of them share 2 ROWS consecutive classes, four and four in turn (what the two
+// Classes of a block: the products keep a block's largest logit per frame.  With 8, half the rows of W
+// are read again that 16 take, for twice the maxima: selection and product, 4,215 frames, D = 512,
+// V = 180,000: 185 + 853 us, with 16 250 + 825; 2,500 frames, D = 4,096, V = 151,936: 307 + 3,214, with 16
+// 670 + 3,190; fp32, 1,600 frames, D = 512, V = 5,000: 46 + 70, with 16 74 + 69.
+constexpr int kCandRows = 8;
+inline int cand_blocks(int V) { return (V + 255) / 256 * (256 / kCandRows); }  // a frame's block maxima
+// The blocks.  Two of them share 2 kCandRows consecutive classes, four and four in turn (what the two
 // lane halves of a matrix-core accumulator hold); block 2 g + h has the h-th fours of group g.  In a
 // frame's row of maxima they lie as the lanes write them: per 128 classes the first halves' blocks, then the
 // second halves'.
-template <int ROWS>
 struct CandBlocks {
-  static constexpr int kRun = 64 / ROWS;  // groups of 128 classes
+  static constexpr int kRun = 64 / kCandRows;  // groups of 128 classes
   static __host__ __device__ __forceinline__ int place(int block) {
     const int g = block >> 1;
     return (g / kRun * 2 + (block & 1)) * kRun + g % kRun;
@@ -276,18 +276,18 @@ struct CandBlocks {
     return (place / (2 * kRun) * kRun + place % kRun) * 2 + (place / kRun & 1);
   }
   static __host__ __device__ __forceinline__ int class_of(int block, int k) {  // the k-th of a block
-    return (block >> 1) * 2 * ROWS + (k >> 2) * 8 + (block & 1) * 4 + (k & 3);
+    return (block >> 1) * 2 * kCandRows + (k >> 2) * 8 + (block & 1) * 4 + (k & 3);
   }
 };
-// The normaliser's partial pairs and bmax[m * cand_blocks(V, rows) + i], the block maxima of frame m (-inf
-// past V), with rows = cand_rows.  Ht (null: none): H transposed [D][Mp], as for the argmax.
+// The normaliser's partial pairs and bmax[m * cand_blocks(V) + i], the block maxima of frame m (-inf
+// past V).  Ht (null: none): H transposed [D][Mp], as for the argmax.
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                     float2* partials, int* P_out, float* bmax, hipStream_t stream,
                                     const uint16_t* Ht = nullptr, int Mp = 0);
 hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
                                    float2* partials, int* P_out, float* bmax, hipStream_t stream);
 // Frames of one pass over the vocabulary, and the scratch of a call.
-int cand_pass_frames(int dtype, int M, int D, int V);
+int cand_pass_frames(int M, int V);
 size_t cand_scratch_bytes(int dtype, int M, int D, int V);
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
                                    int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,

@@ -162,7 +162,7 @@ def test_candidates_passes():
     import torch
 
     from paper_2609_33645_amd import prunedctc as pc
-    M, D, V = 700, 64, 524_288  # a pass takes 4,096 frames
+    M, D, V = 700, 64, 524_288  # a pass takes 2,048 frames
     r = torch.Generator(device="cuda")
     r.manual_seed(1)
     H = torch.randn(M, D, generator=r, device="cuda").to(torch.bfloat16)

@@ -85,12 +85,12 @@ def test_sizes():
     for bad in ((2, 4, 512, 1000, 16), (1, -1, 512, 1000, 16), (1, 4, 500, 1000, 16), (1, 4, 512, 1, 16),
                 (1, 4, 512, 1000, 0), (1, 4, 512, 1000, 65), (1, 4, 512, 524_289, 16)):
         assert c(*bad) == 0, bad
-    # the block maxima are held to 256 MiB: more frames take more passes, not more memory (the
+    # the block maxima are held to 512 MiB: more frames take more passes, not more memory (the
     # normaliser's partial sums and a transposed H grow with the frames of a pass alone)
     for D in (512, 4096):
         for dt in (0, 1):
             assert c(dt, 400_000, D, 180_000, 16) == c(dt, 100_000, D, 180_000, 64) \
-                < (256 << 20) + 6_144 * (8 * 1030 + 2 * D)
+                < (512 << 20) + 6_144 * (8 * 1030 + 2 * D)
     d = L.pctc_beam_decode_workspace_size
     T = i32(30, 20)
     assert d(1, p(T), 2, 512, 1000, 8, 16) > c(1, 50, 512, 1000, 16)
