@@ -119,7 +119,7 @@ def lib() -> ctypes.CDLL:
     L.pctc_beam_state_bytes.restype = c_sz
     L.pctc_beam_reset.argtypes = [c_i32, c_i32, c_i32, c_p, c_sz, c_p]
     L.pctc_beam_reset.restype = c_i32
-    L.pctc_beam_advance.argtypes = [c_p, c_p, c_p, c_i32, i32p, c_i32, c_i32, c_i32, c_f, i32p, c_p, c_sz, c_p, c_p]
+    L.pctc_beam_advance.argtypes = [c_p, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_i32, c_f, c_p, c_p, c_sz, c_p, c_p]
     L.pctc_beam_advance.restype = c_i32
     L.pctc_beam_result.argtypes = [c_i32, c_i32, c_i32, c_p, c_sz, c_i32, c_p, c_p, c_p, c_p]
     L.pctc_beam_result.restype = c_i32
@@ -615,6 +615,21 @@ def _asynchronous(fn):
     return call
 
 
+def _raw_stream(dev: torch.device) -> int:
+    """The current stream's handle (without the stream object that current_stream makes, 2 us)."""
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
+def _scratch(nbytes: int, dev: torch.device) -> torch.Tensor:
+    """_workspace without its slice where the allocation is aligned already, as torch's are."""
+    t = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    return t if t.data_ptr() % 256 == 0 else _workspace(nbytes, dev)
+
+
+def _as(t: torch.Tensor, dtype: torch.dtype) -> torch.Tensor:
+    return t if t.dtype is dtype and t.is_contiguous() else t.to(dtype).contiguous()
+
+
 def _head_args(H: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]):
     """Checked and contiguous H, W and bias of a readout, and the library's type code."""
     dt = _dtype_code(H)
@@ -670,7 +685,11 @@ class BeamSearch:
         if nbytes == 0:
             _check(-1, "pctc_beam_state_bytes")
         self._state = _workspace(nbytes, self.device)
+        self.device = self._state.device
+        self._mem = self._state.data_ptr(), self._state.numel()
         self._done = np.zeros(max(self.N, 1), np.int32)
+        self._frames = np.zeros(max(self.N, 1), np.int32)
+        self._host = self._frames.ctypes.data, self._done.ctypes.data
         self.reset()
 
     @property
@@ -678,15 +697,12 @@ class BeamSearch:
         """Frames that each utterance has had since the reset."""
         return self._done[:self.N].copy()
 
-    def _mem(self):
-        return ctypes.c_void_p(self._state.data_ptr()), ctypes.c_size_t(self._state.numel())
-
     @_asynchronous
     def reset(self, *, stream=None) -> None:
         """Starts every utterance anew with the empty prefix."""
-        mem, size = self._mem()
-        _check(lib().pctc_beam_reset(self.N, self.beam_size, self.max_frames, mem, size, _stream(None)),
-               "pctc_beam_reset")
+        code = lib().pctc_beam_reset(self.N, self.beam_size, self.max_frames, *self._mem, _raw_stream(self.device))
+        if code:
+            _check(code, "pctc_beam_reset")
         self._done[:] = 0
 
     @_asynchronous
@@ -696,23 +712,24 @@ class BeamSearch:
         logp [sum frames, C], blank_logp [sum frames].  Returns parents [N, beam_size] (int32): the
         beam before the call that each beam descends from, -1 where there is no prefix (for
         beam_reorder)."""
-        fr = _host_i32(frames)
-        if fr.shape != (self.N,):
+        if isinstance(frames, torch.Tensor):
+            frames = frames.detach().cpu().numpy()
+        if len(frames) != self.N:
             raise PrunedCTCError(-1, f"frames must have {self.N} entries")
-        M = int(fr.sum(dtype=np.int64))
-        if logp.dim() != 2 or logp.shape[0] != M or ids.shape != logp.shape or tuple(blank_logp.shape) != (M,):
+        fr = self._frames
+        fr[:self.N] = frames
+        M, dev = int(fr.sum()), self.device
+        if logp.dim() != 2 or logp.shape[0] != M or ids.shape != logp.shape or blank_logp.shape != logp.shape[:1]:
             raise PrunedCTCError(-1, f"ids and logp must be [{M}, C] and blank_logp [{M}]")
-        if any(t.device != self.device for t in (ids, logp, blank_logp)):
-            raise PrunedCTCError(-1, f"candidates must be on {self.device}")
-        ids = ids.to(torch.int32).contiguous()
-        logp = logp.to(torch.float32).contiguous()
-        blank_logp = blank_logp.to(torch.float32).contiguous()
-        parents = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=self.device)
-        mem, size = self._mem()
-        code = lib().pctc_beam_advance(_ptr(ids), _ptr(logp), _ptr(blank_logp), int(logp.shape[1]), _i32p(fr), self.N,
-                                       self.beam_size, self.max_frames, self.token_bonus, _i32p(self._done), mem, size,
-                                       _ptr(parents), _stream(None))
-        _check(code, "pctc_beam_advance")
+        if ids.device != dev or logp.device != dev or blank_logp.device != dev:
+            raise PrunedCTCError(-1, f"candidates must be on {dev}")
+        ids, logp, blank_logp = _as(ids, torch.int32), _as(logp, torch.float32), _as(blank_logp, torch.float32)
+        parents = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=dev)
+        code = lib().pctc_beam_advance(ids.data_ptr(), logp.data_ptr(), blank_logp.data_ptr(), logp.shape[1],
+                                       self._host[0], self.N, self.beam_size, self.max_frames, self.token_bonus,
+                                       self._host[1], *self._mem, parents.data_ptr(), _raw_stream(dev))
+        if code:
+            _check(code, "pctc_beam_advance")
         return parents
 
     @_asynchronous
@@ -725,9 +742,8 @@ class BeamSearch:
         tokens = torch.empty((self.N, self.beam_size, int(max_tokens)), dtype=torch.int32, device=self.device)
         lengths = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=self.device)
         scores = torch.empty((self.N, self.beam_size), dtype=torch.float32, device=self.device)
-        mem, size = self._mem()
-        code = lib().pctc_beam_result(self.N, self.beam_size, self.max_frames, mem, size, int(max_tokens), _ptr(tokens),
-                                      _ptr(lengths), _ptr(scores), _stream(None))
+        code = lib().pctc_beam_result(self.N, self.beam_size, self.max_frames, *self._mem, int(max_tokens),
+                                      tokens.data_ptr(), lengths.data_ptr(), scores.data_ptr(), _raw_stream(self.device))
         _check(code, "pctc_beam_result")
         return {"tokens": tokens, "token_lengths": lengths, "scores": scores}
 
@@ -742,25 +758,28 @@ def beam_reorder(states: Sequence[torch.Tensor], parents: torch.Tensor, out: Opt
     """Per-beam state tensors [N, K, ...] of any type in the order of the surviving beams: state[n, k]
     becomes state[n, parents[n, k]] (a parent outside [0, K) leaves it).  In place, or into the
     tensors `out`; returns those written.  Tensors must be contiguous."""
-    if parents.dim() != 2 or parents.dtype != torch.int32 or not parents.is_cuda:
+    dev = parents.device
+    if parents.dim() != 2 or parents.dtype is not torch.int32 or dev.type != "cuda":
         raise PrunedCTCError(-1, "parents must be a device int32 [N, K]")
     N, K = parents.shape
     parents = parents.contiguous()
     dest = states if out is None else out
     if len(dest) != len(states):
         raise PrunedCTCError(-1, "out must have a tensor for each state")
+    sizes = []
     for t, o in zip(states, dest):
-        if t.dim() < 2 or tuple(t.shape[:2]) != (N, K):
+        if t.dim() < 2 or t.shape[:2] != parents.shape:
             raise PrunedCTCError(-1, f"a state must be [{N}, {K}, ...]")
-        if o.shape != t.shape or o.dtype != t.dtype:
-            raise PrunedCTCError(-1, "out must have the states' shapes and types")
-        if any(not x.is_contiguous() or x.device != parents.device for x in (t, o)):
-            raise PrunedCTCError(-1, f"states must be contiguous tensors on {parents.device}")
-    n = max(len(states), 1)
-    sizes = (ctypes.c_int64 * n)(*[(t.numel() // max(N * K, 1)) * t.element_size() for t in states])
-    code = lib().pctc_beam_reorder(len(states), _ptr_array(states), None if out is None else _ptr_array(dest), sizes,
-                                   _ptr(parents), N, K, _stream(None))
-    _check(code, "pctc_beam_reorder")
+        if t.device != dev or not t.is_contiguous():
+            raise PrunedCTCError(-1, f"states must be contiguous tensors on {dev}")
+        if o is not t and (o.shape != t.shape or o.dtype is not t.dtype or o.device != dev or not o.is_contiguous()):
+            raise PrunedCTCError(-1, f"out must be contiguous tensors of the states' shapes and types on {dev}")
+        sizes.append(t.nbytes // (N * K) if N * K else 0)
+    code = lib().pctc_beam_reorder(len(sizes), _ptr_array(states), None if out is None else _ptr_array(dest),
+                                   (ctypes.c_int64 * max(len(sizes), 1))(*sizes), parents.data_ptr(), N, K,
+                                   _raw_stream(dev))
+    if code:
+        _check(code, "pctc_beam_reorder")
     return list(dest)
 
 
@@ -811,25 +830,36 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional
     if not grads:
         raise PrunedCTCError(-1, "no gradients")
     dev = grads[0].device
+    if dev.type != "cuda":
+        raise PrunedCTCError(-1, "gradients must be device tensors")
     dest = grads if out is None else list(out)
     if len(dest) != len(grads):
         raise PrunedCTCError(-1, "out must have a tensor for each gradient")
+    codes, sizes = [], []
     for g, o in zip(grads, dest):
-        if not (g.is_cuda and g.device == dev and o.device == dev and g.is_contiguous() and o.is_contiguous()):
+        dt = g.dtype
+        if dt is not torch.float32 and dt is not torch.bfloat16:
+            raise PrunedCTCError(-1, f"unsupported dtype {dt}")
+        if g.device != dev or not g.is_contiguous():
             raise PrunedCTCError(-1, "gradients must be contiguous tensors of one device")
-        if o.dtype != g.dtype or o.numel() != g.numel():
-            raise PrunedCTCError(-1, "out must have the gradients' types and sizes")
+        n = g.numel()
+        if o is not g and (o.dtype is not dt or o.numel() != n or o.device != dev or not o.is_contiguous()):
+            raise PrunedCTCError(-1, "out must be contiguous tensors of the gradients' types and sizes on their device")
+        codes.append(PCTC_F32 if dt is torch.float32 else PCTC_BF16)
+        sizes.append(n)
     n = len(grads)
-    codes = (ctypes.c_int32 * n)(*[_dtype_code(g) for g in grads])
-    sizes = (ctypes.c_int64 * n)(*[g.numel() for g in grads])
     L = lib()
+    nbytes = L.pctc_clip_workspace_size(n)
+    ws = _scratch(nbytes, dev)
     res = torch.empty(2, dtype=torch.float32, device=dev)
-    ws = _workspace(int(L.pctc_clip_workspace_size(n)), dev)
-    code = L.pctc_clip_grad_norm(n, _ptr_array(grads), None if out is None else _ptr_array(dest), sizes, codes,
-                                 float(max_norm), _ptr(res), ctypes.c_void_p(res.data_ptr() + 4),
-                                 ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), _stream(None))
-    _check(code, "pctc_clip_grad_norm")
-    return {"norm": res[:1], "scale": res[1:]}
+    at = res.data_ptr()
+    code = L.pctc_clip_grad_norm(n, _ptr_array(grads), None if out is None else _ptr_array(dest),
+                                 (ctypes.c_int64 * n)(*sizes), (ctypes.c_int32 * n)(*codes), max_norm, at, at + 4,
+                                 ws.data_ptr(), nbytes, _raw_stream(dev))
+    if code:
+        _check(code, "pctc_clip_grad_norm")
+    norm, scale = res.split(1)
+    return {"norm": norm, "scale": scale}
 
 
 # ---- kernel timing -----------------------------------------------------------------------

@@ -122,8 +122,8 @@ def test_beam_refusals():
     done = i32(0, 95)
 
     def adv(ids=OK, logp=OK, bl=OK, C=8, frames=i32(3, 4), N=2, K=4, cap=100, bonus=0.0, dn=done, state=OK, n=big):
-        return L.pctc_beam_advance(ids, logp, bl, C, p(frames) if frames is not None else None, N, K, cap, bonus,
-                                   p(dn) if dn is not None else None, state, n, None, None)
+        at = lambda a: None if a is None else a.ctypes.data  # noqa: E731
+        return L.pctc_beam_advance(ids, logp, bl, C, at(frames), N, K, cap, bonus, at(dn), state, n, None, None)
     for kw in (dict(ids=None), dict(logp=None), dict(bl=None), dict(C=0), dict(C=65), dict(N=-1), dict(K=0), dict(K=33),
                dict(cap=-1), dict(bonus=math.nan), dict(bonus=math.inf), dict(frames=None), dict(dn=None),
                dict(state=OK + 16)):
@@ -185,7 +185,7 @@ def test_reorder_and_clip_refusals():
     assert c(1, None, None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1
     assert c(1, vp(OK), None, i64(4), (ctypes.c_int32 * 1)(2), 1.0, OK, None, OK, big, None) == -1
     assert c(1, vp(OK), None, i64(-1), f32, 1.0, OK, None, OK, big, None) == -1
-    assert c(1, vp(OK), None, i64((1 << 36) + 1), f32, 1.0, OK, None, OK, big, None) == -1
+    assert c(1, vp(OK), None, i64((1 << 34) + 1), f32, 1.0, OK, None, OK, big, None) == -1
     assert c(1, vp(None), None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1
     assert c(1, vp(OK), vp(None), i64(4), f32, 1.0, OK, None, OK, big, None) == -1
     assert c(1, vp(OK + 2), None, i64(4), f32, 1.0, OK, None, OK, big, None) == -1  # off its type's alignment
