@@ -11,6 +11,7 @@ import ctypes
 import functools
 import math
 import os
+from array import array
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -748,8 +749,13 @@ class BeamSearch:
         return {"tokens": tokens, "token_lengths": lengths, "scores": scores}
 
 
-def _ptr_array(tensors):
-    return (ctypes.c_void_p * max(len(tensors), 1))(*[t.data_ptr() for t in tensors])
+def _pointers(tensors) -> array:
+    return array("Q", map(torch.Tensor.data_ptr, tensors))
+
+
+def _at(a: Optional[array]) -> Optional[int]:
+    """Address of a host array's values (the caller keeps the array until the call is over)."""
+    return None if a is None else a.buffer_info()[0]
 
 
 @_asynchronous
@@ -775,8 +781,8 @@ def beam_reorder(states: Sequence[torch.Tensor], parents: torch.Tensor, out: Opt
         if o is not t and (o.shape != t.shape or o.dtype is not t.dtype or o.device != dev or not o.is_contiguous()):
             raise PrunedCTCError(-1, f"out must be contiguous tensors of the states' shapes and types on {dev}")
         sizes.append(t.nbytes // (N * K) if N * K else 0)
-    code = lib().pctc_beam_reorder(len(sizes), _ptr_array(states), None if out is None else _ptr_array(dest),
-                                   (ctypes.c_int64 * max(len(sizes), 1))(*sizes), parents.data_ptr(), N, K,
+    src, dst, nbytes = _pointers(states), None if out is None else _pointers(dest), array("q", sizes)
+    code = lib().pctc_beam_reorder(len(sizes), _at(src), _at(dst), _at(nbytes), parents.data_ptr(), N, K,
                                    _raw_stream(dev))
     if code:
         _check(code, "pctc_beam_reorder")
@@ -835,27 +841,27 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional
     dest = grads if out is None else list(out)
     if len(dest) != len(grads):
         raise PrunedCTCError(-1, "out must have a tensor for each gradient")
-    codes, sizes = [], []
-    for g, o in zip(grads, dest):
-        dt = g.dtype
-        if dt is not torch.float32 and dt is not torch.bfloat16:
-            raise PrunedCTCError(-1, f"unsupported dtype {dt}")
-        if g.device != dev or not g.is_contiguous():
-            raise PrunedCTCError(-1, "gradients must be contiguous tensors of one device")
-        n = g.numel()
-        if o is not g and (o.dtype is not dt or o.numel() != n or o.device != dev or not o.is_contiguous()):
-            raise PrunedCTCError(-1, "out must be contiguous tensors of the gradients' types and sizes on their device")
-        codes.append(PCTC_F32 if dt is torch.float32 else PCTC_BF16)
-        sizes.append(n)
+    # list-wide checks (lists of hundreds of tensors are ordinary)
+    T = torch.Tensor
+    dtypes, sizes, devs = [g.dtype for g in grads], list(map(T.numel, grads)), set(map(T.get_device, grads))
+    if not all(map(T.is_contiguous, grads)) or devs != {dev.index}:
+        raise PrunedCTCError(-1, "gradients must be contiguous tensors of one device")
+    if not set(dtypes) <= {torch.float32, torch.bfloat16}:
+        raise PrunedCTCError(-1, "gradients must be float32 or bfloat16")
+    if out is not None and (
+            [o.dtype for o in dest] != dtypes or list(map(T.numel, dest)) != sizes
+            or set(map(T.get_device, dest)) != devs or not all(map(T.is_contiguous, dest))):
+        raise PrunedCTCError(-1, "out must be contiguous tensors of the gradients' types and sizes on their device")
     n = len(grads)
     L = lib()
+    src, dst, counts = _pointers(grads), None if out is None else _pointers(dest), array("q", sizes)
+    codes = array("i", [PCTC_F32 if d is torch.float32 else PCTC_BF16 for d in dtypes])
     nbytes = L.pctc_clip_workspace_size(n)
     ws = _scratch(nbytes, dev)
     res = torch.empty(2, dtype=torch.float32, device=dev)
     at = res.data_ptr()
-    code = L.pctc_clip_grad_norm(n, _ptr_array(grads), None if out is None else _ptr_array(dest),
-                                 (ctypes.c_int64 * n)(*sizes), (ctypes.c_int32 * n)(*codes), max_norm, at, at + 4,
-                                 ws.data_ptr(), nbytes, _raw_stream(dev))
+    code = L.pctc_clip_grad_norm(n, _at(src), _at(dst), _at(counts), _at(codes), max_norm, at, at + 4, ws.data_ptr(),
+                                 nbytes, _raw_stream(dev))
     if code:
         _check(code, "pctc_clip_grad_norm")
     norm, scale = res.split(1)
