@@ -756,3 +756,14 @@ def test_clip_head_gradients():
     r = pc.clip_grad_norm(grads, 1.0)
     check_clip(before, grads, r, 1.0)
     assert float(pc.clip_grad_norm(grads, math.inf)["norm"]) == pytest.approx(1.0, rel=1e-5)
+
+
+def test_fit_and_decode_example():
+    """The example end to end: the loss falls, and every beam's predictor state, reordered through all
+    of its frames, is the one its labels define (sums of at most 80 vectors in another order)."""
+    from paper_2609_33645_amd import fit_and_decode
+    r = fit_and_decode.run(steps=120, beams=4, classes=100, N=6)
+    say(r)
+    assert r["loss_last"] < 0.1 * r["loss_first"] and 0 < r["norm_last"] < r["norm_max"]
+    assert r["errors best of beams"] <= r["errors beam"] < r["labels"]
+    assert r["predictor off by"] < 1e-4
