@@ -378,7 +378,7 @@ int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_
  *
  * The state between frames is caller memory of pctc_beam_state_bytes(N, K, max_frames) bytes, 256-byte
  * aligned: it holds the beams and, for up to max_frames frames per utterance, K label records of 12 bytes
- * a frame (0 for invalid arguments: N < 0, K outside [1, PCTC_MAX_BEAMS], max_frames < 0, or
+ * a frame (0 for invalid arguments: N outside [0, 2^20], K outside [1, PCTC_MAX_BEAMS], max_frames < 0, or
  * K max_frames >= 2^31).  pctc_beam_reset starts every utterance with the empty prefix.
  *
  * pctc_beam_advance: `frames` more frames of each utterance.  ids, logp [sum frames, C], blank_logp

@@ -37,7 +37,7 @@ namespace {
 
 constexpr float kNegInf = -INFINITY;
 constexpr int kBufWord3 = 0x00020000;  // word 3 of a raw buffer resource: 32-bit data, no swizzle
-constexpr int kCkStep = 32;  // labels between two nodes that remember the one before (result kernel)
+constexpr int kCkStep = 16;  // labels between two nodes that remember the one before (result kernel)
 
 constexpr float kLow = -1e30f;  // a reference that stays finite where all masses are zero
 
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(256) beam_reset_kernel(BeamFields f, int N, in
 // KT: beams rounded up to 4, 8, 16 or 32.
 template <int KT>
 __global__ void __launch_bounds__(64)
-beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restrict__ ids,
+beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, const int32_t* __restrict__ ids,
                     const float* __restrict__ logp, const float* __restrict__ blank_logp, float bonus, BeamFields f,
                     int32_t* __restrict__ parents) {
   constexpr int kCopies = 64 / KT;                        // lanes of a beam
@@ -192,7 +192,14 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   float pb = kNegInf, pn = kNegInf, s = kNegInf;
   uint64_t hash = 0, phash = 0;
   int last = -2, len = -2, node = -1, ck = -1;
-  if (mine) {
+  double offset = 0.0;
+  if (fresh_start) {  // as beam_reset_kernel leaves it
+    if (i == 0) {
+      pb = s = 0.f;
+      len = 0;
+    }
+  } else if (mine) {
+    offset = f.offset[n];
     pb = f.pb[at];
     pn = f.pn[at];
     s = f.s[at];
@@ -205,7 +212,6 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
   }
   int2* const nodes = f.nodes + n * f.cap;
   int32_t* const cks = f.cks + n * f.cap;
-  double offset = f.offset[n];
   int origin = i;
 
   // the pairs that can be kept: classes c <= K / (i + 1) of beam i, beam by beam
@@ -257,8 +263,9 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, const int32_t* __restr
                                  rb = resource(blank_logp + t0 + f, left);
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      fid[g] = __builtin_amdgcn_raw_buffer_load_b32(ri, lane * 4, g * C * 4, 0);
-      fl[g] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rl, lane * 4, g * C * 4, 0));
+      const int at_class = (g * C + lane) * 4;  // (the whole offset takes part in the range check)
+      fid[g] = __builtin_amdgcn_raw_buffer_load_b32(ri, at_class, 0, 0);
+      fl[g] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rl, at_class, 0, 0));
     }
     fb = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rb, lane * 4, 0, 0));
 #endif
@@ -617,8 +624,8 @@ constexpr int kColBytes = 256 * 16;
 // before any is written, so that input and output may be the same memory.
 template <int KT>
 __global__ void __launch_bounds__(256)
-beam_reorder_kernel(ReorderTable t, const int32_t* __restrict__ parents, int n0, int K) {
-  const int64_t col = static_cast<int64_t>(blockIdx.x);
+beam_reorder_kernel(ReorderTable t, int64_t col0, const int32_t* __restrict__ parents, int n0, int K) {
+  const int64_t col = col0 + blockIdx.x;
   const int n = n0 + blockIdx.y;
   int lo = 0, hi = t.tensors - 1;
   while (lo < hi) {
@@ -675,7 +682,8 @@ hipError_t launch_beam_reset(void* state, int N, int K, int max_frames, hipStrea
 
 hipError_t launch_beam_advance(const int32_t* ids, const float* logp, const float* blank_logp, int C,
                                const int32_t* frames, int N, int K, int max_frames, float bonus,
-                               const int32_t* done, void* state, int32_t* parents, hipStream_t stream) {
+                               const int32_t* done, bool fresh_start, void* state, int32_t* parents,
+                               hipStream_t stream) {
   const BeamFields f = beam_fields(state, N, K, max_frames);
   int32_t row = 0;
   for (int n0 = 0; n0 < N; n0 += kBeamGroup) {
@@ -689,7 +697,7 @@ hipError_t launch_beam_advance(const int32_t* ids, const float* logp, const floa
     rows.off[here] = row;
     Prof pr("beam_advance", stream);
 #define PCTC_ADVANCE(KT)                                                                                        \
-  hipLaunchKernelGGL(beam_advance_kernel<KT>, dim3(here), dim3(64), 0, stream, rows, n0, K, C, ids, logp,       \
+  hipLaunchKernelGGL(beam_advance_kernel<KT>, dim3(here), dim3(64), 0, stream, rows, n0, K, C, fresh_start, ids, logp, \
                      blank_logp, bonus, f, parents)
     if (K <= 4) PCTC_ADVANCE(4);
     else if (K <= 8) PCTC_ADVANCE(8);
@@ -726,14 +734,17 @@ hipError_t launch_beam_reorder(int tensors, const void* const* in, void* const* 
     if (c == 0) continue;
     Prof pr("beam_reorder", stream);
     for (int n0 = 0; n0 < N; n0 += 65535) {
-      const dim3 grid(static_cast<unsigned>(c), static_cast<unsigned>(std::min(65535, N - n0)));
+      for (int64_t col0 = 0; col0 < c; col0 += kMaxGrid) {
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(kMaxGrid, c - col0)),
+                        static_cast<unsigned>(std::min(65535, N - n0)));
 #define PCTC_REORDER(KT) \
-  hipLaunchKernelGGL(beam_reorder_kernel<KT>, grid, dim3(256), 0, stream, t, parents, n0, K)
-      if (K <= 4) PCTC_REORDER(4);
-      else if (K <= 8) PCTC_REORDER(8);
-      else if (K <= 16) PCTC_REORDER(16);
-      else PCTC_REORDER(32);
+  hipLaunchKernelGGL(beam_reorder_kernel<KT>, grid, dim3(256), 0, stream, t, col0, parents, n0, K)
+        if (K <= 4) PCTC_REORDER(4);
+        else if (K <= 8) PCTC_REORDER(8);
+        else if (K <= 16) PCTC_REORDER(16);
+        else PCTC_REORDER(32);
 #undef PCTC_REORDER
+      }
     }
   }
   return hipGetLastError();

@@ -236,7 +236,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     ids[static_cast<int64_t>(m) * C + r] = -1;
     logp[static_cast<int64_t>(m) * C + r] = -INFINITY;
   }
-  if (tid == 0) blank_logp[m] = static_cast<float>(zblank - l);
+  if (tid == 0) blank_logp[m] = zblank == -INFINITY ? -INFINITY : static_cast<float>(zblank - l);
 }
 
 int cand_pass_frames(int M, int V) {
@@ -260,7 +260,7 @@ CandLayout cand_layout(int dtype, int M, int D, int V) {
   L.o_part = 2 * L.o_lam2;
   L.o_bmax = L.o_part + lse_partial_bytes(L.frames, D);
   L.o_ht = L.o_bmax + align_up(static_cast<size_t>(L.frames) * L.blocks * sizeof(float), 256);
-  L.total = L.o_ht + (dtype == 1 && frames_from_ht_bf16(L.frames, D, V) ? lse_ht_bytes_bf16(L.frames, D) : 0);
+  L.total = L.o_ht + (dtype == 1 ? cand_ht_bytes(L.frames, D, V) : 0);
   return L;
 }
 }  // namespace
@@ -284,7 +284,7 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
     if (dtype == 1) {
       const uint16_t* Hm = static_cast<const uint16_t*>(H) + static_cast<int64_t>(m0) * D;
       const int Mp = (here + 63) / 64 * 64;
-      uint16_t* Ht = frames_from_ht_bf16(here, D, V) ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
+      uint16_t* Ht = cand_ht_bytes(here, D, V) > 0 ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
       if (Ht && (e = launch_ht_build_bf16(Hm, here, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
       e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, stream,
                                    Ht, Mp);

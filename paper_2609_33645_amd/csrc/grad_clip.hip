@@ -326,11 +326,13 @@ hipError_t launch_clip_grad_norm(int tensors, const void* const* grads, void* co
     hipLaunchKernelGGL(grad_norm, dim3(1), dim3(kNormThreads), 0, stream, parts, nparts, max_norm, norm, scale, factor);
   }
   for (int g = 0; g < groups; ++g) {
-    const int chunks = table(g, out ? kOutBytes : kInPlaceBytes);
+    int chunks = out ? table(g, kOutBytes) : 0;
+    const bool small = out && chunks <= kMaxGrid;
+    if (!small) chunks = table(g, kInPlaceBytes);  // (of 96 tensors at most 0.27 TB)
     if (chunks == 0) continue;
     Prof pr("grad_scale", stream);
-    if (out) hipLaunchKernelGGL(grad_scale<kOutBytes>, dim3(chunks), dim3(kThreads), 0, stream, t, factor, false);
-    else hipLaunchKernelGGL(grad_scale<kInPlaceBytes>, dim3(chunks), dim3(kThreads), 0, stream, t, factor, true);
+    if (small) hipLaunchKernelGGL(grad_scale<kOutBytes>, dim3(chunks), dim3(kThreads), 0, stream, t, factor, false);
+    else hipLaunchKernelGGL(grad_scale<kInPlaceBytes>, dim3(chunks), dim3(kThreads), 0, stream, t, factor, !out);
   }
   return hipGetLastError();
 }

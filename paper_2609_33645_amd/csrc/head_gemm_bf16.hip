@@ -1251,6 +1251,14 @@ hipError_t launch_amax_partial_bf16(const uint16_t* H, int M, int D, const uint1
   return hipGetLastError();
 }
 
+// Bytes of H transposed where the candidates' product reads its frames from it (0: it does not), from the
+// size on at which the argmax does; wide heads too, whose product takes 32-deep tiles here.
+size_t cand_ht_bytes(int M, int D, int V) {
+  const size_t bytes = static_cast<size_t>(D) * ((M + 63) / 64 * 64) * sizeof(uint16_t);
+  if (M <= 0 || D % 128 != 0 || bytes >= (1ull << 31) || static_cast<double>(M) * V * D < 8e10) return 0;
+  return align_up(bytes, 256);
+}
+
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                     float2* partials, int* P_out, float* bmax, hipStream_t stream, const uint16_t* Ht,
                                     int Mp) {
@@ -1266,9 +1274,7 @@ hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint1
   else                                                                                                             \
     hipLaunchKernelGGL((cand_partial_bf16<G, false>), grid, dim3(G::kThreads), 0, stream, H, Ht, Mp, M, D, W,      \
                        bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);
-  if (sp.wide) {
-    PCTC_CAND(GWide)
-  } else if (Ht) {
+  if (Ht) {
     PCTC_CAND(GMidTW)
   } else {
     PCTC_CAND(GMid)

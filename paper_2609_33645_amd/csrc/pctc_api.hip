@@ -965,7 +965,7 @@ static bool head_args_ok(pctc_dtype dtype, int32_t D, int32_t V) {
 }
 static bool misaligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255) != 0; }
 constexpr int32_t kMaxFrames = 1 << 30;  // of a batch, as for the loss
-constexpr int32_t kMaxUtts = 1 << 24;    // with PCTC_MAX_BEAMS beams each, a grid of one workgroup per beam
+constexpr int32_t kMaxUtts = 1 << 20;    // with PCTC_MAX_BEAMS beams each, a grid of one wavefront per beam
 
 size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C) {
   if (!head_args_ok(dtype, D, V) || M < 0 || M > kMaxFrames || C < 1 || C > PCTC_MAX_CANDIDATES) return 0;
@@ -1026,8 +1026,8 @@ int32_t pctc_beam_advance(const int32_t* ids, const float* logp, const float* bl
   }
   if (M > kMaxFrames || (M > 0 && (!ids || !logp || !blank_logp))) return PCTC_EINVAL;
   if (N == 0) return PCTC_OK;
-  PCTC_HIP(launch_beam_advance(ids, logp, blank_logp, C, frames, N, K, max_frames, token_bonus, frames_done, state,
-                               parents, static_cast<hipStream_t>(stream_ptr)));
+  PCTC_HIP(launch_beam_advance(ids, logp, blank_logp, C, frames, N, K, max_frames, token_bonus, frames_done, false,
+                               state, parents, static_cast<hipStream_t>(stream_ptr)));
   for (int n = 0; n < N; ++n) frames_done[n] += frames[n];
   prof_flush();
   return PCTC_OK;
@@ -1123,9 +1123,8 @@ int32_t pctc_beam_decode(pctc_dtype dtype, const void* H, int32_t D, const void*
   if (!blank_logp) blank_logp = reinterpret_cast<float*>(ws + L.o_blank);
   PCTC_HIP(launch_frame_candidates(dtype == PCTC_BF16 ? 1 : 0, H, L.M, D, W, bias, V, blank, C, ids, logp, blank_logp,
                                    ws + L.o_scratch, stream));
-  PCTC_HIP(launch_beam_reset(ws, N, K, L.max_frames, stream));
-  PCTC_HIP(launch_beam_advance(ids, logp, blank_logp, C, input_lengths, N, K, L.max_frames, token_bonus, nullptr, ws,
-                               nullptr, stream));
+  PCTC_HIP(launch_beam_advance(ids, logp, blank_logp, C, input_lengths, N, K, L.max_frames, token_bonus, nullptr, true,
+                               ws, nullptr, stream));
   PCTC_HIP(launch_beam_result(ws, N, K, L.max_frames, max_tokens, tokens, token_lengths, scores, stream));
   prof_flush();
   return PCTC_OK;

@@ -27,6 +27,7 @@ constexpr int kDefaultChunk = 16384;
 constexpr float kKeepSlack = 1e-3f;  // nats added to the beam threshold (tie/rounding rule)
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of 256 threads along a grid axis (threads stay below 2^32)
 
 // ---- union / relabel -------------------------------------------------------------------
 // u_ids[remap[v]] = v for remap[v] >= 0 and K = 1 + max remap (K zeroed here).
@@ -280,13 +281,14 @@ struct CandBlocks {
   }
 };
 // The normaliser's partial pairs and bmax[m * cand_blocks(V) + i], the block maxima of frame m (-inf
-// past V).  Ht (null: none): H transposed [D][Mp], as for the argmax.
+// past V).  Ht (null: none): H transposed [D][Mp] of cand_ht_bytes.
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                     float2* partials, int* P_out, float* bmax, hipStream_t stream,
                                     const uint16_t* Ht = nullptr, int Mp = 0);
 hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
                                    float2* partials, int* P_out, float* bmax, hipStream_t stream);
 // Frames of one pass over the vocabulary, and the scratch of a call.
+size_t cand_ht_bytes(int M, int D, int V);
 int cand_pass_frames(int M, int V);
 size_t cand_scratch_bytes(int dtype, int M, int D, int V);
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
@@ -302,10 +304,12 @@ struct FrameRows {
 };
 size_t beam_state_layout(int N, int K, int max_frames, size_t (&at)[12]);
 hipError_t launch_beam_reset(void* state, int N, int K, int max_frames, hipStream_t stream);
-// done: frames consumed before (null: none); parents [N][K] or null.
+// done: frames consumed before (null: none); fresh_start: every utterance starts anew, whatever the state
+// holds; parents [N][K] or null.
 hipError_t launch_beam_advance(const int32_t* ids, const float* logp, const float* blank_logp, int C,
                                const int32_t* frames, int N, int K, int max_frames, float bonus,
-                               const int32_t* done, void* state, int32_t* parents, hipStream_t stream);
+                               const int32_t* done, bool fresh_start, void* state, int32_t* parents,
+                               hipStream_t stream);
 hipError_t launch_beam_result(void* state, int N, int K, int max_frames, int max_tokens, int32_t* tokens,
                               int32_t* lengths, float* scores, hipStream_t stream);
 // out null: in place.

@@ -73,7 +73,7 @@ def test_sizes():
     L = _lib()
     up = lambda x: (x + 255) // 256 * 256  # noqa: E731
     assert L.pctc_beam_state_bytes(0, 8, 100) > 0
-    for bad in ((-1, 8, 100), (1, 0, 100), (1, 33, 100), (1, 8, -1), (1, 8, 1 << 28), ((1 << 24) + 1, 1, 1)):
+    for bad in ((-1, 8, 100), (1, 0, 100), (1, 33, 100), (1, 8, -1), (1, 8, 1 << 28), ((1 << 20) + 1, 1, 1)):
         assert L.pctc_beam_state_bytes(*bad) == 0, bad
     # three masses, two hashes and four indices a beam; an offset an utterance; 12 bytes a frame and beam
     nk = 3 * 8
