@@ -82,6 +82,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   __shared__ float val_v[kValues];
   __shared__ int val_i[kValues];
   __shared__ float zblank;
+  __shared__ unsigned long long moved;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int m = m0 + blockIdx.x;
   const float* const row = bmax + static_cast<int64_t>(blockIdx.x) * nb;
@@ -94,7 +95,10 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     mx = fmaxf(mx, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
   }
   keys[tid] = order_key(mx);
-  if (tid == 0) count = 0;
+  if (tid == 0) {
+    count = 0;
+    moved = 0;
+  }
   __syncthreads();
   uint32_t t = reach(keys, nsel, lane);
   // (most threads have no block that large)
@@ -163,6 +167,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   __syncthreads();
 
   // ---- their logits: eight lanes a class, a block of a wavefront at a time ----
+  const float was = tid < n ? row[CandBlocks::place(sel[tid])] : 0.f;
+  const double lam0 = lam[blockIdx.x];
   const T* const h = H + static_cast<int64_t>(m) * D;
   const int part = lane & 7;
   constexpr int kSets = kCandRows / 8;  // of eight classes
@@ -204,6 +210,19 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   if (tid == 0) count = 0;
   __syncthreads();
 
+  // The vocabulary pass rounded these logits in another order.  Where one class has nearly all of the
+  // probability, the difference would be the whole of logp = z - lambda, so lambda takes the largest of each
+  // block as they are here: lambda + log(1 + sum over the blocks (exp(z' - lambda) - exp(z - lambda))), the
+  // sum in integers of 2^-56, which have the same sum in any order.
+  if (tid < n) {
+    float top = sel[tid] == CandBlocks::block_of(blank) ? zblank : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kCandRows; ++k) top = fmaxf(top, z[tid * kCandRows + k]);
+    const float d = expf(static_cast<float>(was - lam0)) * expm1f(top - was);
+    if (fabsf(d) < 0.5f)  // (not where a logit is infinite or NaN)
+      atomicAdd(&moved, static_cast<unsigned long long>(llrint(static_cast<double>(d) * 0x1p56)));
+  }
+
   // ---- the C best of them ----
   const int nz = n * kCandRows;
   mx = -INFINITY;
@@ -221,7 +240,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   }
   __syncthreads();
   const int nv = count;
-  const double l = lam[blockIdx.x];
+  const float by = static_cast<float>(static_cast<double>(static_cast<long long>(moved)) * 0x1p-56);
+  const double l = lam0 + (fabsf(by) < 0.5f ? static_cast<double>(log1pf(by)) : 0.);
   for (int i = tid; i < nv; i += kThreads) {
     const float v = val_v[i];
     const int id = val_i[i];

@@ -287,18 +287,18 @@ cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ H
   }
   const GOp A{W, D, vend, D, nullptr};
   const GOp B = HT ? GOp{Ht, Mp, M, D, nullptr} : GOp{H, D, M, D, nullptr};
-  float run_max[FC], run_sum[FC];
+  float run_max[FC], run_sum[FC], run_lo[FC];
 #pragma unroll
   for (int j = 0; j < FC; ++j) {
     run_max[j] = -INFINITY;
-    run_sum[j] = 0.f;
+    run_sum[j] = run_lo[j] = 0.f;
   }
   f32x16 acc[FR][FC];
   auto epi = [&](int it, f32x16 (&a)[FR][FC]) {
     const int v0 = vbeg + it * TR;
     if (v0 + TR > vend) mask_rows_inf<FR, FC, G>(a, v0, vend, wave, lane);
     float bm[FC][FR * 16 / kCandRows];
-    lse_block_update<FR, FC, G, kCandRows>(a, run_max, run_sum, bm);
+    lse_block_update<FR, FC, G, kCandRows>(a, run_max, run_sum, run_lo, bm);
     store_block_max<G, kCandRows>(bm, v0, wave, lane, m0, M, nb, bmax);
   };
   auto init = [&](int it, f32x16 (&a)[FR][FC]) {
@@ -307,6 +307,8 @@ cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ H
   };
   if constexpr (HT) G::template seq_aligned<0>(A, B, vbeg, m0, ntiles, D, acc, epi, init);
   else G::run_seq(A, B, vbeg, m0, ntiles, D, st, acc, epi, init);
+#pragma unroll
+  for (int j = 0; j < FC; ++j) run_sum[j] += run_lo[j];
   lse_store_partials<G>(run_max, run_sum, HT ? xch_ : st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
 

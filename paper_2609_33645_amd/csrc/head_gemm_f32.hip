@@ -143,17 +143,19 @@ cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
   if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), (M + kTile - 1) / kTile, P, mt, p)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int m0 = mt * kTile, vbeg = p * vper, vend = min(V, vbeg + vper);
-  float run_max[GZ::FC], run_sum[GZ::FC];
+  float run_max[GZ::FC], run_sum[GZ::FC], run_lo[GZ::FC];
 #pragma unroll
   for (int j = 0; j < GZ::FC; ++j) {
     run_max[j] = -INFINITY;
-    run_sum[j] = 0.f;
+    run_sum[j] = run_lo[j] = 0.f;
   }
   vocab_tiles<BIAS>(H, M, D, W, bias, m0, vbeg, vend, st, [&](int v0, int el, f32x16 (&a)[GZ::FR][GZ::FC]) {
     float bm[GZ::FC][GZ::FR * 16 / kCandRows];
-    lse_block_update<GZ::FR, GZ::FC, GZ, kCandRows>(a, run_max, run_sum, bm);
+    lse_block_update<GZ::FR, GZ::FC, GZ, kCandRows>(a, run_max, run_sum, run_lo, bm);
     store_block_max<GZ, kCandRows>(bm, v0, wave, el, m0, M, nb, bmax);
   });
+#pragma unroll
+  for (int j = 0; j < GZ::FC; ++j) run_sum[j] += run_lo[j];
   lse_store_partials<GZ>(run_max, run_sum, st0_, wave, lane, m0, M, partials + static_cast<int64_t>(p) * M);
 }
 

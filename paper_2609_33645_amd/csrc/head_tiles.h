@@ -128,10 +128,13 @@ __device__ __forceinline__ void lse_tile_update(const f32x16 (&acc)[FR][FC], flo
 
 // The same, and bm[j][..]: the largest logits of the lane's blocks of frame column j.  A block is ROWS
 // of the 16 rows that a lane holds of 32: of rows 8 q + 4 h + e (h the lane's half, e < 4) those of ROWS / 4
-// consecutive q.
+// consecutive q.  Where one class has nearly all of a frame's probability, the classes beside it are each below
+// the sum's last bit and would all be lost to it: a block's eight are added among themselves first, and run_lo
+// holds what the running sum's roundings left.
 template <int FR, int FC, class G, int ROWS>
 __device__ __forceinline__ void lse_block_update(const f32x16 (&acc)[FR][FC], float (&run_max)[FC],
-                                                 float (&run_sum)[FC], float (&bm)[FC][FR * 16 / ROWS]) {
+                                                 float (&run_sum)[FC], float (&run_lo)[FC],
+                                                 float (&bm)[FC][FR * 16 / ROWS]) {
   constexpr int kSub = 16 / ROWS;
 #pragma unroll
   for (int j = 0; j < FC; ++j) {
@@ -162,11 +165,20 @@ __device__ __forceinline__ void lse_block_update(const f32x16 (&acc)[FR][FC], fl
 #pragma unroll
       for (int i = 0; i < FR; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s += fast_exp2(fmaf(acc[i][j][r], kLog2e, -ms));
+        for (int u = 0; u < 16; u += 8) {
+          float e[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) e[r] = fast_exp2(fmaf(acc[i][j][u + r], kLog2e, -ms));
+          s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+        }
+      // ms is nmax log2(e) rounded; its rounding, up to 1e-6 at a logit of 20, is taken off the sum again
+      if (nmax > -INFINITY) s *= fast_exp2(-fmaf(nmax, kLog2e, -ms));
     }
     s += swap_halves(s);
     const float scale = (run_max[j] == -INFINITY) ? 0.f : fast_exp2((run_max[j] - nmax) * kLog2e);
-    run_sum[j] = fmaf(run_sum[j], scale, s);
+    const float was = run_sum[j] * scale, sum = was + s, of_s = sum - was;
+    run_lo[j] = fmaf(run_lo[j], scale, (was - (sum - of_s)) + (s - of_s));
+    run_sum[j] = sum;
     run_max[j] = nmax;
   }
 }

@@ -279,6 +279,9 @@ struct CandBlocks {
   static __host__ __device__ __forceinline__ int class_of(int block, int k) {  // the k-th of a block
     return (block >> 1) * 2 * kCandRows + (k >> 2) * 8 + (block & 1) * 4 + (k & 3);
   }
+  static __host__ __device__ __forceinline__ int block_of(int cls) {
+    return cls / (2 * kCandRows) * 2 + (cls >> 2 & 1);
+  }
 };
 // The normaliser's partial pairs and bmax[m * cand_blocks(V) + i], the block maxima of frame m (-inf
 // past V).  Ht (null: none): H transposed [D][Mp] of cand_ht_bytes.

@@ -148,6 +148,34 @@ def test_candidates_masked_blank_and_all():
     assert (got["ids"].cpu().numpy() == -1).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("top", [0, 700])
+def test_candidates_certain_frames(dtype, top):
+    """Frames of one nearly certain class, its logit near 200, where a logit's own rounding is 1e-5: the class's
+    log-probability holds neither that rounding nor the loss of 5,000 classes that are each below a sum's last
+    bit.  The normaliser rounds the sum of such a frame some 16 times, at 2^-24 each at most, and its terms'
+    exponents at 4 x 2^-24 together."""
+    from paper_2609_33645_amd import prunedctc as pc
+    say("certain", dtype, top)
+    M, D, V, C, blank = 70, 512, 5000, 8, 0
+    r = np.random.default_rng(top)
+    h = r.standard_normal(D)
+    z = r.uniform(165.0, 183.0, V)
+    z[top] = 200.0
+    W = z[:, None] * h[None, :] / (h @ h) + 0.002 * r.standard_normal((V, D))
+    H = h[None, :] * r.uniform(0.97, 1.03, M)[:, None]
+    H, W = (bf16_round(x) if dtype == "bf16" else x.astype(np.float32) for x in (H, W))
+    got = pc.frame_candidates(dev(H, dtype), dev(W, dtype), C, blank)
+    z = H.astype(np.float64) @ W.astype(np.float64).T
+    x = z - z[:, top:top + 1]
+    x[:, top] = -np.inf
+    want = -np.log1p(np.exp(x).sum(1))
+    out = got["blank_logp"] if top == blank else got["logp"][:, 0]
+    if top != blank:
+        assert (got["ids"][:, 0] == top).all()
+    assert np.abs(out.cpu().numpy().astype(np.float64) - want).max() <= 20 * 2.0**-24
+
+
 def test_candidates_without_frames():
     import torch
 
