@@ -21,7 +21,10 @@ namespace pctc {
 namespace {
 
 constexpr size_t kMaxBlockBytes = static_cast<size_t>(512) << 20;
-constexpr int kThreads = 256;
+// Up to two workgroups a compute unit: 1024 threads each, whose loads cover one another (150 frames of 180,000
+// classes, D = 512: 14.9 us, with 256 threads 26; 109 frames, D = 3512, C = 24: 39 and 56).  More frames fill the
+// card as workgroups of 256 (2,155 frames of 6,700 classes: 18 us, with 1024 threads 50).
+constexpr int kFewFrames = 512;
 constexpr int kList = 256;  // blocks kept for ordering; more only where maxima are equal
 constexpr int kMaxSel = kMaxCandidates + 2;
 
@@ -31,12 +34,18 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-// The largest key t (its low 12 bits zero) that at least `need` of the workgroup's 256 keys reach;
-// 0 when there are fewer.  Every wavefront searches by itself.
+// The largest key t (its low 12 bits zero) that at least `need` of 256 groups of threads reach (thread
+// tid is of group tid mod 256; keys of NT threads); 0 when there are fewer.  For one wavefront: the
+// others' issue slots are for other workgroups.
+template <int NT>
 __device__ __forceinline__ uint32_t reach(const uint32_t* keys, int need, int lane) {
   uint32_t k[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) k[i] = keys[64 * i + lane];
+  for (int i = 0; i < 4; ++i) {
+    k[i] = keys[64 * i + lane];
+#pragma unroll
+    for (int j = 256; j < NT; j += 256) k[i] = max(k[i], keys[j + 64 * i + lane]);
+  }
   uint32_t t = 0;
   for (int bit = 31; bit >= 12; --bit) {
     const uint32_t c = t | (1u << bit);
@@ -65,18 +74,19 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 
 }  // namespace
 
-// One workgroup per frame.
-template <class T>
-__global__ void __launch_bounds__(kThreads)
+// One workgroup of NT threads per frame.
+template <class T, int NT>
+__global__ void __launch_bounds__(NT)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
                    int V, int blank, int C, const float* __restrict__ bmax, int nb, const double* __restrict__ lam,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
   constexpr int kPer = 16 / sizeof(T);
   constexpr int kValues = kMaxSel * kCandRows;
-  __shared__ uint32_t keys[kThreads];
+  __shared__ uint32_t keys[NT];
   __shared__ float list_v[kList];
   __shared__ int list_b[kList];
   __shared__ int count;
+  __shared__ uint32_t bound;
   __shared__ int sel[kMaxSel];
   __shared__ float z[kValues];
   __shared__ float val_v[kValues];
@@ -90,7 +100,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
 
   // ---- the nsel blocks with the largest maxima (equal ones: the lowest) ----
   float mx = -INFINITY;
-  for (int i = tid * 4; i < nb; i += kThreads * 4) {
+  for (int i = tid * 4; i < nb; i += NT * 4) {
     const float4 v = *reinterpret_cast<const float4*>(row + i);
     mx = fmaxf(mx, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
   }
@@ -100,9 +110,14 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     moved = 0;
   }
   __syncthreads();
-  uint32_t t = reach(keys, nsel, lane);
+  if (wave == 0) {
+    const uint32_t r = reach<NT>(keys, nsel, lane);
+    if (lane == 0) bound = r;
+  }
+  __syncthreads();
+  uint32_t t = bound;
   // (most threads have no block that large)
-  for (int i = order_key(mx) >= t ? tid * 4 : nb; i < nb; i += kThreads * 4) {
+  for (int i = order_key(mx) >= t ? tid * 4 : nb; i < nb; i += NT * 4) {
     const float4 v4 = *reinterpret_cast<const float4*>(row + i);
     const float v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
@@ -124,6 +139,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
       const float v = list_v[tid];
       const int b = list_b[tid];
       int rank = 0;
+#pragma unroll 4
       for (int q = 0; q < n; ++q) rank += list_v[q] > v || (list_v[q] == v && list_b[q] < b);
       if (rank < nsel) sel[rank] = b;
     }
@@ -138,7 +154,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
       if (tid == 0) count = 0;
       __syncthreads();
       int mine = 0;
-      for (int i = tid; i < nb; i += kThreads) mine += row[i] > -INFINITY && order_key(row[i]) >= c;
+      for (int i = tid; i < nb; i += NT) mine += row[i] > -INFINITY && order_key(row[i]) >= c;
       if (mine) atomicAdd(&count, mine);
       __syncthreads();
       if (count >= nsel) t = c;
@@ -146,7 +162,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
     __syncthreads();
     if (tid == 0) count = 0;
     __syncthreads();
-    for (int i = tid; i < nb; i += kThreads)
+    for (int i = tid; i < nb; i += NT)
       if (row[i] > -INFINITY && order_key(row[i]) > t) sel[atomicAdd(&count, 1)] = CandBlocks::at(i);
     __syncthreads();
     n = count;
@@ -190,7 +206,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
 #pragma unroll
       for (int e = 0; e < kSets; ++e) s[e] += __shfl_xor(s[e], o, 64);
   };
-  for (int g = wave; g <= n; g += kThreads / 64) {  // (the last: blank)
+  for (int g = wave; g <= n; g += NT / 64) {  // (the last: blank)
     int v[kSets];
     float s[kSets];
 #pragma unroll
@@ -226,11 +242,16 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   // ---- the C best of them ----
   const int nz = n * kCandRows;
   mx = -INFINITY;
-  for (int i = tid; i < nz; i += kThreads) mx = fmaxf(mx, z[i]);
+  for (int i = tid; i < nz; i += NT) mx = fmaxf(mx, z[i]);
   keys[tid] = order_key(mx);
   __syncthreads();
-  t = reach(keys, C, lane);
-  for (int i = tid; i < nz; i += kThreads) {
+  if (wave == 0) {
+    const uint32_t r = reach<NT>(keys, C, lane);
+    if (lane == 0) bound = r;
+  }
+  __syncthreads();
+  t = bound;
+  for (int i = tid; i < nz; i += NT) {
     const float v = z[i];
     if (v > -INFINITY && order_key(v) >= t) {
       const int q = atomicAdd(&count, 1);
@@ -242,17 +263,18 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   const int nv = count;
   const float by = static_cast<float>(static_cast<double>(static_cast<long long>(moved)) * 0x1p-56);
   const double l = lam0 + (fabsf(by) < 0.5f ? static_cast<double>(log1pf(by)) : 0.);
-  for (int i = tid; i < nv; i += kThreads) {
+  for (int i = tid; i < nv; i += NT) {
     const float v = val_v[i];
     const int id = val_i[i];
     int rank = 0;
+#pragma unroll 4
     for (int q = 0; q < nv; ++q) rank += val_v[q] > v || (val_v[q] == v && val_i[q] < id);
     if (rank < C) {
       ids[static_cast<int64_t>(m) * C + rank] = id;
       logp[static_cast<int64_t>(m) * C + rank] = static_cast<float>(v - l);
     }
   }
-  for (int r = nv + tid; r < C; r += kThreads) {
+  for (int r = nv + tid; r < C; r += NT) {
     ids[static_cast<int64_t>(m) * C + r] = -1;
     logp[static_cast<int64_t>(m) * C + r] = -INFINITY;
   }
@@ -316,14 +338,17 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
     e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
     if (e != hipSuccess) return e;
     Prof pr("cand_select", stream);
-    if (dtype == 1)
-      hipLaunchKernelGGL(cand_select_kernel<uint16_t>, dim3(here), dim3(kThreads), 0, stream,
-                         static_cast<const uint16_t*>(H), m0, D, static_cast<const uint16_t*>(W), bias, V, blank, C,
-                         bmax, nb, lam, ids, logp, blank_logp);
-    else
-      hipLaunchKernelGGL(cand_select_kernel<float>, dim3(here), dim3(kThreads), 0, stream,
-                         static_cast<const float*>(H), m0, D, static_cast<const float*>(W), bias, V, blank, C, bmax,
-                         nb, lam, ids, logp, blank_logp);
+#define PCTC_SELECT(T, NT)                                                                                            \
+  hipLaunchKernelGGL((cand_select_kernel<T, NT>), dim3(here), dim3(NT), 0, stream, static_cast<const T*>(H), m0, D,     \
+                     static_cast<const T*>(W), bias, V, blank, C, bmax, nb, lam, ids, logp, blank_logp)
+    if (dtype == 1) {
+      if (here <= kFewFrames) PCTC_SELECT(uint16_t, 1024);
+      else PCTC_SELECT(uint16_t, 256);
+    } else {
+      if (here <= kFewFrames) PCTC_SELECT(float, 1024);
+      else PCTC_SELECT(float, 256);
+    }
+#undef PCTC_SELECT
   }
   return hipGetLastError();
 }
