@@ -1,6 +1,5 @@
 // Frame candidates (gfx950): the C most probable classes of every frame other than blank, with
-// their log probabilities and blank's, over the full vocabulary; the frame x vocabulary logits are
-// never stored.
+// their log probabilities and blank's, over the full vocabulary.
 //
 //   z = H W^T + b,  lambda_m = log sum_v exp z_mv,  logp = float(z - lambda_m), z and lambda in the order
 //   of falling z, the lowest class first among equal ones
@@ -8,10 +7,14 @@
 // One vocabulary pass on the matrix cores gives the normaliser's partial pairs and the largest logit
 // of every block of 8 classes.  A class among a frame's C best lies in one of the C + 1 blocks with the
 // largest maxima (one more for blank, which is left out; and one for the block whose classes lie between
-// the last one's, where maxima are equal), so a second kernel forms those blocks' logits again, 8 (C + 2)
-// dot products a frame, and orders them.  M V / 8 maxima are written and read (380 MB at 4,215 frames of
-// 180,000 classes) and W rows for 8 (C + 2) classes a frame are read again, through the L2s.  The scratch for
-// the maxima is held to 512 MB by passing over the vocabulary once per that many frames.
+// the last one's, where maxima are equal), so a second kernel needs 8 (C + 2) logits a frame, and orders
+// them.  Where the vocabulary is long beside the rows that those take, they are formed again from H and W
+// and the frame x vocabulary logits are never stored; where it is short, the pass keeps them (keeps_logits).
+// The scratch is held to 512 MB by passing over the vocabulary once per that many frames.
+//
+// The product is bound by the matrix cores from some 600 frames on (4,215 frames, D = 512, V = 180,000, bf16:
+// 860 us, 0.90 PFLOP/s of 1.20 in a large library product) and by the reading of W below (150 frames: 53 us, 3.5
+// TB/s).  The choice reads M V / 8 maxima (380 MB there) and 8 (C + 2) rows of W a frame (620 MB): 187 us.
 #include <algorithm>
 
 #include "pctc_internal.h"
@@ -20,7 +23,7 @@ namespace pctc {
 
 namespace {
 
-constexpr size_t kMaxBlockBytes = static_cast<size_t>(512) << 20;
+constexpr size_t kMaxPassBytes = static_cast<size_t>(512) << 20;
 // Up to two workgroups a compute unit: 1024 threads each, whose loads cover one another (150 frames of 180,000
 // classes, D = 512: 14.9 us, with 256 threads 26; 109 frames, D = 3512, C = 24: 39 and 56).  More frames fill the
 // card as workgroups of 256 (2,155 frames of 6,700 classes: 18 us, with 1024 threads 50).
@@ -75,10 +78,11 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 }  // namespace
 
 // One workgroup of NT threads per frame.
-template <class T, int NT>
+template <class T, int NT, bool KEPT>
 __global__ void __launch_bounds__(NT)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
                    int V, int blank, int C, const float* __restrict__ bmax, int nb, const double* __restrict__ lam,
+                   const float* __restrict__ Z, int ldz,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
   constexpr int kPer = 16 / sizeof(T);
   constexpr int kValues = kMaxSel * kCandRows;
@@ -182,45 +186,34 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   }
   __syncthreads();
 
-  // ---- their logits: eight lanes a class, a block of a wavefront at a time ----
-  const float was = tid < n ? row[CandBlocks::place(sel[tid])] : 0.f;
+  // ---- their logits ----
   const double lam0 = lam[blockIdx.x];
-  const T* const h = H + static_cast<int64_t>(m) * D;
-  const int part = lane & 7;
-  constexpr int kSets = kCandRows / 8;  // of eight classes
-  auto dots = [&](const int (&v)[kSets], float (&s)[kSets]) {  // in each of a class's eight lanes (v >= V: as V - 1)
-    const T* w[kSets];
-#pragma unroll
-    for (int e = 0; e < kSets; ++e) {
-      w[e] = W + static_cast<int64_t>(min(v[e], V - 1)) * D;
-      s[e] = 0.f;
+  const float was = !KEPT && tid < n ? row[CandBlocks::place(sel[tid])] : 0.f;
+  if constexpr (KEPT) {
+    const float* const zrow = Z + static_cast<int64_t>(blockIdx.x) * ldz;
+    for (int i = tid; i < n * kCandRows; i += NT) {
+      const int v = CandBlocks::class_of(sel[i / kCandRows], i % kCandRows);
+      z[i] = v == blank ? -INFINITY : zrow[v];  // (-inf from V on)
     }
+    if (tid == 0) zblank = zrow[blank];
+  } else {
+    // eight lanes a class, a block of a wavefront at a time
+    static_assert(kCandRows == 8, "a wavefront's classes");
+    const T* const h = H + static_cast<int64_t>(m) * D;
+    const int part = lane & 7;
+    for (int g = wave; g <= n; g += NT / 64) {  // (the last: blank)
+      const int v = g < n ? CandBlocks::class_of(sel[g], lane >> 3) : blank;
+      const T* const w = W + static_cast<int64_t>(min(v, V - 1)) * D;
+      float x = 0.f;
 #pragma unroll 4
-    for (int k = part * kPer; k < D; k += 8 * kPer) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(h + k);
+      for (int k = part * kPer; k < D; k += 8 * kPer)
+        x = dot16(*reinterpret_cast<const u32x4*>(w + k), *reinterpret_cast<const u32x4*>(h + k), x, T{});
 #pragma unroll
-      for (int e = 0; e < kSets; ++e) s[e] = dot16(*reinterpret_cast<const u32x4*>(w[e] + k), x, s[e], T{});
-    }
-#pragma unroll
-    for (int o = 4; o >= 1; o >>= 1)
-#pragma unroll
-      for (int e = 0; e < kSets; ++e) s[e] += __shfl_xor(s[e], o, 64);
-  };
-  for (int g = wave; g <= n; g += NT / 64) {  // (the last: blank)
-    int v[kSets];
-    float s[kSets];
-#pragma unroll
-    for (int e = 0; e < kSets; ++e) v[e] = g < n ? CandBlocks::class_of(sel[g], e * 8 + (lane >> 3)) : blank;
-    dots(v, s);
-#pragma unroll
-    for (int e = 0; e < kSets; ++e) {
-      if (part != 0 || v[e] >= V) {
-        if (part == 0) z[g * kCandRows + e * 8 + (lane >> 3)] = -INFINITY;
-        continue;
-      }
-      if (bias) s[e] += bias[v[e]];
-      if (g == n) zblank = s[e];  // every class's first lane holds it
-      else z[g * kCandRows + e * 8 + (lane >> 3)] = v[e] == blank ? -INFINITY : s[e];
+      for (int o = 4; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+      if (part != 0) continue;
+      if (bias && v < V) x += bias[v];
+      if (g == n) zblank = x;  // every class's first lane holds it
+      else z[g * kCandRows + (lane >> 3)] = v >= V || v == blank ? -INFINITY : x;
     }
   }
   if (tid == 0) count = 0;
@@ -230,7 +223,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   // probability, the difference would be the whole of logp = z - lambda, so lambda takes the largest of each
   // block as they are here: lambda + log(1 + sum over the blocks (exp(z' - lambda) - exp(z - lambda))), the
   // sum in integers of 2^-56, which have the same sum in any order.
-  if (tid < n) {
+  if (!KEPT && tid < n) {
     float top = sel[tid] == CandBlocks::block_of(blank) ? zblank : -INFINITY;
 #pragma unroll
     for (int k = 0; k < kCandRows; ++k) top = fmaxf(top, z[tid * kCandRows + k]);
@@ -281,44 +274,52 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   if (tid == 0) blank_logp[m] = zblank == -INFINITY ? -INFINITY : static_cast<float>(zblank - l);
 }
 
-int cand_pass_frames(int M, int V) {
-  const size_t per = static_cast<size_t>(cand_blocks(V)) * sizeof(float);
-  const int most = static_cast<int>(std::min<size_t>(kMaxBlockBytes / per / 256 * 256, 1 << 30));
-  return std::min(M, std::max(most, 256));
-}
-
 namespace {
-// Scratch of a pass: lambda, its pair, the normaliser's partial pairs, the block maxima and, where the
-// product reads it, H transposed.
+// Whether the product writes its logits for the choice to read (4 V bytes a frame, and 32 (C + 2) of them
+// back) instead of the choice forming them again from 8 (C + 2) rows of W, which come through the L2s at twice
+// the rate.  Product and choice, kept and formed again: fp32, 1,600 frames, D = 512, V = 5,000, C = 16: 81 + 12
+// us, 73 + 48; 753 frames, D = 2480, V = 17,052, C = 7: 373 + 10, 364 + 77; bf16, 138 frames, D = 448,
+// V = 29,197, C = 29 (near the rule's edge): 23.6 + 13.7, 18.3 + 20.2; 205 frames, D = 3008, V = 157,375, C = 14
+// (past it): 322 + 16, 279 + 40; 798 frames, D = 160, V = 11,099, C = 12 (past it): 24 + 11, 14 + 16.
+bool keeps_logits(int dtype, int D, int V, int C) {
+  return V < static_cast<int64_t>(C + 2) * D * (dtype == 1 ? 2 : 4);
+}
+// Scratch of a pass: lambda, its pair, the normaliser's partial pairs, the block maxima, the logits where they
+// are kept and, where the product reads it, H transposed.
 struct CandLayout {
-  int frames, blocks;
-  size_t o_lam2, o_part, o_bmax, o_ht, total;
+  int frames, blocks, ldz;
+  size_t o_lam2, o_part, o_bmax, o_z, o_ht, total;
 };
-CandLayout cand_layout(int dtype, int M, int D, int V) {
+CandLayout cand_layout(int dtype, int M, int D, int V, int C) {
   CandLayout L;
-  L.frames = std::max(1, cand_pass_frames(M, V));
   L.blocks = cand_blocks(V);
+  L.ldz = keeps_logits(dtype, D, V, C) ? L.blocks * kCandRows : 0;
+  const size_t per = static_cast<size_t>(L.blocks + L.ldz) * sizeof(float);
+  const int most = static_cast<int>(std::min<size_t>(kMaxPassBytes / per / 256 * 256, 1 << 30));
+  L.frames = std::max(1, std::min(M, std::max(most, 256)));
   L.o_lam2 = align_up(static_cast<size_t>(L.frames) * 8, 256);
   L.o_part = 2 * L.o_lam2;
   L.o_bmax = L.o_part + lse_partial_bytes(L.frames, D);
-  L.o_ht = L.o_bmax + align_up(static_cast<size_t>(L.frames) * L.blocks * sizeof(float), 256);
+  L.o_z = L.o_bmax + align_up(static_cast<size_t>(L.frames) * L.blocks * sizeof(float), 256);
+  L.o_ht = L.o_z + align_up(static_cast<size_t>(L.frames) * L.ldz * sizeof(float), 256);
   L.total = L.o_ht + (dtype == 1 ? cand_ht_bytes(L.frames, D, V) : 0);
   return L;
 }
 }  // namespace
 
-size_t cand_scratch_bytes(int dtype, int M, int D, int V) { return cand_layout(dtype, M, D, V).total; }
+size_t cand_scratch_bytes(int dtype, int M, int D, int V, int C) { return cand_layout(dtype, M, D, V, C).total; }
 
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
                                    int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
                                    hipStream_t stream) {
-  const CandLayout L = cand_layout(dtype, M, D, V);
+  const CandLayout L = cand_layout(dtype, M, D, V, C);
   const int F = L.frames, nb = L.blocks;
   char* s = static_cast<char*>(scratch);
   double* lam = reinterpret_cast<double*>(s);
   float2* lam2 = reinterpret_cast<float2*>(s + L.o_lam2);
   float2* partials = reinterpret_cast<float2*>(s + L.o_part);
   float* bmax = reinterpret_cast<float*>(s + L.o_bmax);
+  float* Z = L.ldz ? reinterpret_cast<float*>(s + L.o_z) : nullptr;
   for (int m0 = 0; m0 < M; m0 += F) {
     const int here = std::min(F, M - m0);
     int P = 0;
@@ -328,25 +329,30 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
       const int Mp = (here + 63) / 64 * 64;
       uint16_t* Ht = cand_ht_bytes(here, D, V) > 0 ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
       if (Ht && (e = launch_ht_build_bf16(Hm, here, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
-      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, stream,
-                                   Ht, Mp);
+      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, Z, L.ldz,
+                                   stream, Ht, Mp);
     } else {
       e = launch_cand_partial_f32(static_cast<const float*>(H) + static_cast<int64_t>(m0) * D, here, D,
-                                  static_cast<const float*>(W), bias, V, partials, &P, bmax, stream);
+                                  static_cast<const float*>(W), bias, V, partials, &P, bmax, Z, L.ldz, stream);
     }
     if (e != hipSuccess) return e;
     e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
     if (e != hipSuccess) return e;
     Prof pr("cand_select", stream);
-#define PCTC_SELECT(T, NT)                                                                                            \
-  hipLaunchKernelGGL((cand_select_kernel<T, NT>), dim3(here), dim3(NT), 0, stream, static_cast<const T*>(H), m0, D,     \
-                     static_cast<const T*>(W), bias, V, blank, C, bmax, nb, lam, ids, logp, blank_logp)
-    if (dtype == 1) {
-      if (here <= kFewFrames) PCTC_SELECT(uint16_t, 1024);
-      else PCTC_SELECT(uint16_t, 256);
+#define PCTC_SELECT(T, NT, KEPT)                                                                                      \
+  hipLaunchKernelGGL((cand_select_kernel<T, NT, KEPT>), dim3(here), dim3(NT), 0, stream, static_cast<const T*>(H),    \
+                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, lam, Z, L.ldz, ids, logp,         \
+                     blank_logp)
+    const bool few = here <= kFewFrames;
+    if (Z) {  // (H and W are not read)
+      if (few) PCTC_SELECT(float, 1024, true);
+      else PCTC_SELECT(float, 256, true);
+    } else if (dtype == 1) {
+      if (few) PCTC_SELECT(uint16_t, 1024, false);
+      else PCTC_SELECT(uint16_t, 256, false);
     } else {
-      if (here <= kFewFrames) PCTC_SELECT(float, 1024);
-      else PCTC_SELECT(float, 256);
+      if (few) PCTC_SELECT(float, 1024, false);
+      else PCTC_SELECT(float, 256, false);
     }
 #undef PCTC_SELECT
   }

@@ -263,12 +263,12 @@ lse_partial_e_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ 
 }
 
 // The normaliser with each frame's block maxima beside it (frame candidates), in the argmax's tile
-// order.
-template <class G, bool BIAS>
+// order; and with KEEP the logits.
+template <class G, bool BIAS, bool KEEP>
 __global__ void __launch_bounds__(G::kThreads, 1)
 cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ Ht, int Mp, int M, int D,
                   const uint16_t* __restrict__ W, const float* __restrict__ bias, int V, int P, int vper,
-                  float2* __restrict__ partials, int nb, float* __restrict__ bmax) {
+                  float2* __restrict__ partials, int nb, float* __restrict__ bmax, float* __restrict__ Z, int ldz) {
   extern __shared__ float bsh[];  // BIAS: b over this partition's rows
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   constexpr bool HT = std::is_same_v<G, GMidTW>;  // frames from Ht [D][Mp]
@@ -300,6 +300,7 @@ cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ H
     float bm[FC][FR * 16 / kCandRows];
     lse_block_update<FR, FC, G, kCandRows>(a, run_max, run_sum, run_lo, bm);
     store_block_max<G, kCandRows>(bm, v0, wave, lane, m0, M, nb, bmax);
+    if constexpr (KEEP) store_logits<G>(a, v0, wave, lane, m0, M, ldz, Z);
   };
   auto init = [&](int it, f32x16 (&a)[FR][FC]) {
     if constexpr (BIAS) bias_init<FR, FC, G>(a, bsh + it * TR, wave, lane);
@@ -1262,25 +1263,27 @@ size_t cand_ht_bytes(int M, int D, int V) {
 }
 
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                    float2* partials, int* P_out, float* bmax, hipStream_t stream, const uint16_t* Ht,
-                                    int Mp) {
+                                    float2* partials, int* P_out, float* bmax, float* Z, int ldz, hipStream_t stream,
+                                    const uint16_t* Ht, int Mp) {
   const LseSplit sp = lse_split_bf16(M, D, V, SplitFor::kAmax);
   *P_out = sp.P;
   Prof pr("cand_partial", stream);
   const size_t bsh = bias ? static_cast<size_t>(sp.vper) * sizeof(float) : 0;
   const dim3 grid(grouped_grid(sp.nM, sp.P));
-#define PCTC_CAND(G)                                                                                               \
-  if (bias)                                                                                                        \
-    hipLaunchKernelGGL((cand_partial_bf16<G, true>), grid, dim3(G::kThreads), bsh, stream, H, Ht, Mp, M, D, W,     \
-                       bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);                                    \
-  else                                                                                                             \
-    hipLaunchKernelGGL((cand_partial_bf16<G, false>), grid, dim3(G::kThreads), 0, stream, H, Ht, Mp, M, D, W,      \
-                       bias, V, sp.P, sp.vper, partials, cand_blocks(V), bmax);
+#define PCTC_CAND1(G, B, K)                                                                                        \
+  hipLaunchKernelGGL((cand_partial_bf16<G, B, K>), grid, dim3(G::kThreads), bsh, stream, H, Ht, Mp, M, D, W, bias,   \
+                     V, sp.P, sp.vper, partials, cand_blocks(V), bmax, Z, ldz)
+#define PCTC_CAND(G)                    \
+  if (bias && Z) PCTC_CAND1(G, true, true);        \
+  else if (bias) PCTC_CAND1(G, true, false);       \
+  else if (Z) PCTC_CAND1(G, false, true);          \
+  else PCTC_CAND1(G, false, false);
   if (Ht) {
     PCTC_CAND(GMidTW)
   } else {
     PCTC_CAND(GMid)
   }
+#undef PCTC_CAND1
 #undef PCTC_CAND
   return hipGetLastError();
 }

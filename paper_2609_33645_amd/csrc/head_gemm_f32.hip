@@ -133,11 +133,11 @@ amax_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
 }
 
 // The normaliser with each frame's block maxima beside it (frame candidates).
-template <bool BIAS>
+template <bool BIAS, bool KEEP>
 __global__ void __launch_bounds__(512, 1)
 cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restrict__ W,
                  const float* __restrict__ bias, int V, int P, int vper, float2* __restrict__ partials, int nb,
-                 float* __restrict__ bmax) {
+                 float* __restrict__ bmax, float* __restrict__ Z, int ldz) {
   PCTC_F3_STAGES
   int mt, p;
   if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), (M + kTile - 1) / kTile, P, mt, p)) return;
@@ -153,6 +153,7 @@ cand_partial_f32(const float* __restrict__ H, int M, int D, const float* __restr
     float bm[GZ::FC][GZ::FR * 16 / kCandRows];
     lse_block_update<GZ::FR, GZ::FC, GZ, kCandRows>(a, run_max, run_sum, run_lo, bm);
     store_block_max<GZ, kCandRows>(bm, v0, wave, el, m0, M, nb, bmax);
+    if constexpr (KEEP) store_logits<GZ>(a, v0, wave, el, m0, M, ldz, Z);
   });
 #pragma unroll
   for (int j = 0; j < GZ::FC; ++j) run_sum[j] += run_lo[j];
@@ -488,18 +489,20 @@ hipError_t launch_amax_partial_f32(const float* H, int M, int D, const float* W,
 }
 
 hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
-                                   float2* partials, int* P_out, float* bmax, hipStream_t stream) {
+                                   float2* partials, int* P_out, float* bmax, float* Z, int ldz, hipStream_t stream) {
   int vper, P;
   lse_split_f32(D, V, &vper, &P);
   *P_out = P;
   const dim3 grid(grouped_grid((M + kTile - 1) / kTile, P));
   Prof pr("cand_partial", stream);
-  if (bias)
-    hipLaunchKernelGGL(cand_partial_f32<true>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,
-                       cand_blocks(V), bmax);
-  else
-    hipLaunchKernelGGL(cand_partial_f32<false>, grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,
-                       cand_blocks(V), bmax);
+#define PCTC_CAND(B, K)                                                                                             \
+  hipLaunchKernelGGL((cand_partial_f32<B, K>), grid, dim3(512), 0, stream, H, M, D, W, bias, V, P, vper, partials,  \
+                     cand_blocks(V), bmax, Z, ldz)
+  if (bias && Z) PCTC_CAND(true, true);
+  else if (bias) PCTC_CAND(true, false);
+  else if (Z) PCTC_CAND(false, true);
+  else PCTC_CAND(false, false);
+#undef PCTC_CAND
   return hipGetLastError();
 }
 

@@ -202,6 +202,24 @@ __device__ __forceinline__ void store_block_max(const float (&bm)[G::FC][G::FR *
   }
 }
 
+// Writes the logits of a tile whose first class is v0, ld (a whole number of tiles) to a frame.
+template <class G>
+__device__ __forceinline__ void store_logits(const f32x16 (&acc)[G::FR][G::FC], int v0, int wave, int lane, int m0, int M,
+                                             int ld, float* __restrict__ Z) {
+#pragma unroll
+  for (int j = 0; j < G::FC; ++j) {
+    const int m = m0 + G::col_of(wave, lane, j);
+    if (m >= M) continue;
+    float* const out = Z + static_cast<int64_t>(m) * ld + v0 + G::row_of(wave, lane, 0, 0);
+#pragma unroll
+    for (int i = 0; i < G::FR; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(out + 32 * i + 8 * q) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+  }
+}
+
 // The two wavefronts of each frame column (row halves) combine their running (max, sum)
 // pairs through LDS (xch: any drained stage) and write the partition's pair of every frame.
 template <class G>

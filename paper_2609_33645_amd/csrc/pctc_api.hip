@@ -969,7 +969,7 @@ constexpr int32_t kMaxUtts = 1 << 20;    // with PCTC_MAX_BEAMS beams each, a gr
 
 size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C) {
   if (!head_args_ok(dtype, D, V) || M < 0 || M > kMaxFrames || C < 1 || C > PCTC_MAX_CANDIDATES) return 0;
-  return cand_scratch_bytes(dtype == PCTC_BF16 ? 1 : 0, M, D, V);
+  return cand_scratch_bytes(dtype == PCTC_BF16 ? 1 : 0, M, D, V, C);
 }
 
 int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W, const float* bias,
@@ -1090,7 +1090,7 @@ int32_t decode_layout(pctc_dtype dtype, const int32_t* T, int32_t N, int32_t D, 
   L->o_logp = L->o_ids + align_up(static_cast<size_t>(M) * C * 4, 256);
   L->o_blank = L->o_logp + align_up(static_cast<size_t>(M) * C * 4, 256);
   L->o_scratch = L->o_blank + align_up(static_cast<size_t>(M) * 4, 256);
-  L->total = L->o_scratch + cand_scratch_bytes(dtype == PCTC_BF16 ? 1 : 0, L->M, D, V);
+  L->total = L->o_scratch + cand_scratch_bytes(dtype == PCTC_BF16 ? 1 : 0, L->M, D, V, C);
   return PCTC_OK;
 }
 }  // namespace

@@ -89,6 +89,20 @@ def test_candidates(dtype, M, D, V, C, blank, bias):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V,C,blank", [
+    (70, 8, 700, 3, 1), (513, 24, 5003, 16, 4999), (600, 64, 9001, 5, 0), (512, 128, 40_000, 64, 0),  # formed again
+    (513, 128, 1501, 9, 3), (700, 1032, 259, 64, 258)])                                               # kept
+def test_candidates_either_way(dtype, M, D, V, C, blank):
+    """Logits formed again and kept, for few frames and many."""
+    from paper_2609_33645_amd import prunedctc as pc
+    say("either way", dtype, M, D, V, C, blank)
+    H, W = head(M * V, M, D, V, dtype, 3.0)
+    b = np.random.default_rng(V).normal(size=V).astype(np.float32)
+    got = pc.frame_candidates(dev(H, dtype), dev(W, dtype), C, blank, dev(b))
+    check_candidates(H, W, C, blank, b, dtype, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", ["zero", "few", "steps"])
 def test_candidates_ties(dtype, kind):
     """Equal logits (exact sums of small whole numbers): the lowest classes first, also where more
@@ -199,6 +213,21 @@ def test_candidates_passes():
     one, many = pc.frame_candidates(H, W, 8), pc.frame_candidates(big, W, 8)
     for k in one:
         assert torch.allclose(many[k].float(), one[k].float().repeat(*([8] + [1] * (one[k].dim() - 1))), atol=2e-5), k
+
+
+def test_candidates_passes_with_logits():
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    M, D, V, C = 500, 512, 60_001, 64  # a pass takes 1,792 frames
+    r = torch.Generator(device="cuda")
+    r.manual_seed(2)
+    H = torch.randn(M, D, generator=r, device="cuda").to(torch.bfloat16)
+    W = (torch.randn(V, D, generator=r, device="cuda") / 8).to(torch.bfloat16)
+    one, many = pc.frame_candidates(H, W, C), pc.frame_candidates(H.repeat(4, 1), W, C)
+    assert torch.equal(many["ids"], one["ids"].repeat(4, 1))
+    for k in ("logp", "blank_logp"):
+        assert torch.allclose(many[k], one[k].repeat(*([4] + [1] * (one[k].dim() - 1))), atol=2e-5), k
 
 
 # ---- the search ----------------------------------------------------------------------------
