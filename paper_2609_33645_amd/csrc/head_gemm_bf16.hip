@@ -52,6 +52,9 @@ using GMid = bf::Gemm<256, 256, 32, LL::KC, LL::KC, 4, 2, 4, true>;
 // k-tiles ahead instead of three)
 using GMidT = bf::Gemm<256, 256, 32, LL::KC, LL::MC, 4, 2, 4, true>;
 using GMidTW = bf::GemmMidA64<2, 4>;
+// candidates of few frames: 64 frames a tile, as W's rows bound it (three stages and two workgroups per CU: the same
+// times)
+using GFew = bf::Gemm<256, 64, 32, LL::KC, LL::KC, 4>;
 constexpr int kMidRun = 8;
 constexpr int kRcCus = 224;  // workgroups of the dense recompute (one round)
 constexpr int kRcStores = 16;  // buffer stores per wave per 256 x 256 tile (recompute, E)
@@ -1265,7 +1268,18 @@ size_t cand_ht_bytes(int M, int D, int V) {
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                     float2* partials, int* P_out, float* bmax, float* Z, int ldz, hipStream_t stream,
                                     const uint16_t* Ht, int Mp) {
-  const LseSplit sp = lse_split_bf16(M, D, V, SplitFor::kAmax);
+  // Tiles of 64 frames while W's rows are what takes the time (up to two such tiles), and where all of them find
+  // a compute unit.  In us, with tiles of 256: D = 512, V = 180,000: 64 frames 34.5 (46.5), 100 46 (49), 150 68
+  // (50); D = 4096, V = 151,936: 64 252 (312), 128 328 (334); D = 512, V = 5,000: 64 12.6 (16.4), 400 16 (25);
+  // D = 1024, V = 30,000: 128 (236 tiles) 20.6 (27), 192 (354 tiles) 28.6 (28.7).
+  LseSplit sp = lse_split_bf16(M, D, V, SplitFor::kAmax);
+  const int vtiles = (V + GFew::kBR - 1) / GFew::kBR, ftiles = (M + GFew::kBC - 1) / GFew::kBC;
+  const bool few = !Ht && (ftiles <= 2 || static_cast<int64_t>(ftiles) * vtiles <= 256);
+  if (few) {
+    sp.nM = ftiles;
+    sp.vper = (vtiles + lse_max_parts(D) - 1) / lse_max_parts(D) * GFew::kBR;
+    sp.P = (V + sp.vper - 1) / sp.vper;
+  }
   *P_out = sp.P;
   Prof pr("cand_partial", stream);
   const size_t bsh = bias ? static_cast<size_t>(sp.vper) * sizeof(float) : 0;
@@ -1280,6 +1294,8 @@ hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint1
   else PCTC_CAND1(G, false, false);
   if (Ht) {
     PCTC_CAND(GMidTW)
+  } else if (few) {
+    PCTC_CAND(GFew)
   } else {
     PCTC_CAND(GMid)
   }
