@@ -81,16 +81,21 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 template <class T, int NT, bool KEPT>
 __global__ void __launch_bounds__(NT)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
-                   int V, int blank, int C, const float* __restrict__ bmax, int nb, const double* __restrict__ lam,
+                   int V, int blank, int C, const float* __restrict__ bmax, int nb, const float2* __restrict__ partials, int M, int P,
                    const float* __restrict__ Z, int ldz,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
   constexpr int kPer = 16 / sizeof(T);
   constexpr int kValues = kMaxSel * kCandRows;
+  constexpr int kParts = kMaxLseParts / NT;
   __shared__ uint32_t keys[NT];
   __shared__ float list_v[kList];
   __shared__ int list_b[kList];
   __shared__ int count;
   __shared__ uint32_t bound;
+  __shared__ float part_max[NT / 64];
+  __shared__ double part_sum[NT / 64];
+  __shared__ int part_nan[NT / 64];
+  __shared__ double lam_s;
   __shared__ int sel[kMaxSel];
   __shared__ float z[kValues];
   __shared__ float val_v[kValues];
@@ -101,6 +106,37 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   const int m = m0 + blockIdx.x;
   const float* const row = bmax + static_cast<int64_t>(blockIdx.x) * nb;
   const int nsel = min(C + 2, nb);
+
+  // ---- the normaliser of each wavefront's partitions ----
+  {
+    const float2* const q0 = partials + blockIdx.x;
+    float2 q[kParts];
+    float top = -INFINITY;
+    int nan = 0;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int p = tid + i * NT;
+      q[i] = p < P ? q0[static_cast<int64_t>(p) * M] : make_float2(-INFINITY, 0.f);
+      nan |= (q[i].x != q[i].x) | (q[i].y != q[i].y);
+      top = fmaxf(top, q[i].x);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i)
+      if (q[i].x > -INFINITY)
+        sum += static_cast<double>(q[i].y) *
+               static_cast<double>(fast_exp2(static_cast<float>(static_cast<double>(q[i].x) - top) * kLog2e));
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    nan = __any(nan);
+    if (lane == 0) {
+      part_max[wave] = top;
+      part_sum[wave] = sum;
+      part_nan[wave] = nan;
+    }
+  }
 
   // ---- the nsel blocks with the largest maxima (equal ones: the lowest) ----
   float mx = -INFINITY;
@@ -117,6 +153,22 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   if (wave == 0) {
     const uint32_t r = reach<NT>(keys, nsel, lane);
     if (lane == 0) bound = r;
+  } else if (wave == 1) {  // lambda meanwhile
+    float top = -INFINITY;
+    int nan = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      top = fmaxf(top, part_max[w]);
+      nan |= part_nan[w];
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w)
+      if (part_max[w] > -INFINITY)
+        sum += part_sum[w] *
+               static_cast<double>(fast_exp2(static_cast<float>(static_cast<double>(part_max[w]) - top) * kLog2e));
+    const double l = top > -INFINITY ? static_cast<double>(top) + log(sum) : -INFINITY;
+    if (lane == 0) lam_s = nan ? __longlong_as_double(0x7ff8000000000000LL) : l;
   }
   __syncthreads();
   uint32_t t = bound;
@@ -187,7 +239,7 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   __syncthreads();
 
   // ---- their logits ----
-  const double lam0 = lam[blockIdx.x];
+  const double lam0 = lam_s;
   const float was = !KEPT && tid < n ? row[CandBlocks::place(sel[tid])] : 0.f;
   if constexpr (KEPT) {
     const float* const zrow = Z + static_cast<int64_t>(blockIdx.x) * ldz;
@@ -284,11 +336,10 @@ namespace {
 bool keeps_logits(int dtype, int D, int V, int C) {
   return V < static_cast<int64_t>(C + 2) * D * (dtype == 1 ? 2 : 4);
 }
-// Scratch of a pass: lambda, its pair, the normaliser's partial pairs, the block maxima, the logits where they
-// are kept and, where the product reads it, H transposed.
+// Scratch of a pass: the normaliser's partial pairs, the block maxima, the logits where they are kept and, where the product reads it, H transposed.
 struct CandLayout {
   int frames, blocks, ldz;
-  size_t o_lam2, o_part, o_bmax, o_z, o_ht, total;
+  size_t o_bmax, o_z, o_ht, total;
 };
 CandLayout cand_layout(int dtype, int M, int D, int V, int C) {
   CandLayout L;
@@ -297,9 +348,7 @@ CandLayout cand_layout(int dtype, int M, int D, int V, int C) {
   const size_t per = static_cast<size_t>(L.blocks + L.ldz) * sizeof(float);
   const int most = static_cast<int>(std::min<size_t>(kMaxPassBytes / per / 256 * 256, 1 << 30));
   L.frames = std::max(1, std::min(M, std::max(most, 256)));
-  L.o_lam2 = align_up(static_cast<size_t>(L.frames) * 8, 256);
-  L.o_part = 2 * L.o_lam2;
-  L.o_bmax = L.o_part + lse_partial_bytes(L.frames, D);
+  L.o_bmax = lse_partial_bytes(L.frames, D);
   L.o_z = L.o_bmax + align_up(static_cast<size_t>(L.frames) * L.blocks * sizeof(float), 256);
   L.o_ht = L.o_z + align_up(static_cast<size_t>(L.frames) * L.ldz * sizeof(float), 256);
   L.total = L.o_ht + (dtype == 1 ? cand_ht_bytes(L.frames, D, V) : 0);
@@ -315,9 +364,7 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
   const CandLayout L = cand_layout(dtype, M, D, V, C);
   const int F = L.frames, nb = L.blocks;
   char* s = static_cast<char*>(scratch);
-  double* lam = reinterpret_cast<double*>(s);
-  float2* lam2 = reinterpret_cast<float2*>(s + L.o_lam2);
-  float2* partials = reinterpret_cast<float2*>(s + L.o_part);
+  float2* partials = reinterpret_cast<float2*>(s);
   float* bmax = reinterpret_cast<float*>(s + L.o_bmax);
   float* Z = L.ldz ? reinterpret_cast<float*>(s + L.o_z) : nullptr;
   for (int m0 = 0; m0 < M; m0 += F) {
@@ -336,13 +383,11 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
                                   static_cast<const float*>(W), bias, V, partials, &P, bmax, Z, L.ldz, stream);
     }
     if (e != hipSuccess) return e;
-    e = launch_lse_finalize(partials, here, P, lam, lam2, nullptr, nullptr, nullptr, 0, stream);
-    if (e != hipSuccess) return e;
     Prof pr("cand_select", stream);
 #define PCTC_SELECT(T, NT, KEPT)                                                                                      \
   hipLaunchKernelGGL((cand_select_kernel<T, NT, KEPT>), dim3(here), dim3(NT), 0, stream, static_cast<const T*>(H),    \
-                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, lam, Z, L.ldz, ids, logp,         \
-                     blank_logp)
+                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, partials, here, P, Z, L.ldz, ids, \
+                     logp, blank_logp)
     const bool few = here <= kFewFrames;
     if (Z) {  // (H and W are not read)
       if (few) PCTC_SELECT(float, 1024, true);
