@@ -332,9 +332,10 @@ namespace {
 // the rate.  Product and choice, kept and formed again: fp32, 1,600 frames, D = 512, V = 5,000, C = 16: 81 + 12
 // us, 73 + 48; 753 frames, D = 2480, V = 17,052, C = 7: 373 + 10, 364 + 77; bf16, 138 frames, D = 448,
 // V = 29,197, C = 29 (near the rule's edge): 23.6 + 13.7, 18.3 + 20.2; 205 frames, D = 3008, V = 157,375, C = 14
-// (past it): 322 + 16, 279 + 40; 798 frames, D = 160, V = 11,099, C = 12 (past it): 24 + 11, 14 + 16.
+// (past it): 322 + 16, 279 + 40; 798 frames, D = 160, V = 11,099, C = 12 (past it): 24 + 11, 14 + 16.  At 32,768
+// classes a pass's scratch holds 3,584 frames; fewer to a pass would read W more often than they save.
 bool keeps_logits(int dtype, int D, int V, int C) {
-  return V < static_cast<int64_t>(C + 2) * D * (dtype == 1 ? 2 : 4);
+  return V <= 32768 && V < static_cast<int64_t>(C + 2) * D * (dtype == 1 ? 2 : 4);
 }
 // Scratch of a pass: the normaliser's partial pairs, the block maxima, the logits where they are kept and, where the product reads it, H transposed.
 struct CandLayout {
