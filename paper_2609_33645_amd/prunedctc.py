@@ -126,9 +126,9 @@ def lib() -> ctypes.CDLL:
     L.pctc_beam_result.restype = c_i32
     L.pctc_beam_reorder.argtypes = [c_i32, c_p, c_p, c_p, c_p, c_i32, c_i32, c_p]
     L.pctc_beam_reorder.restype = c_i32
-    L.pctc_beam_decode_workspace_size.argtypes = [c_i32, i32p, c_i32, c_i32, c_i32, c_i32, c_i32]
+    L.pctc_beam_decode_workspace_size.argtypes = [c_i32, c_p, c_i32, c_i32, c_i32, c_i32, c_i32]
     L.pctc_beam_decode_workspace_size.restype = c_sz
-    L.pctc_beam_decode.argtypes = [c_i32, c_p, c_i32, c_p, c_p, c_i32, i32p, c_i32, c_i32, c_i32, c_i32, c_f, c_i32, c_p,
+    L.pctc_beam_decode.argtypes = [c_i32, c_p, c_i32, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_i32, c_i32, c_f, c_i32, c_p,
                                    c_p, c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
     L.pctc_beam_decode.restype = c_i32
     L.pctc_clip_workspace_size.argtypes = [c_i32]
@@ -661,11 +661,12 @@ def frame_candidates(H: torch.Tensor, W: torch.Tensor, candidates: int, blank: i
     ids = torch.empty((M, C), dtype=torch.int32, device=dev)
     logp = torch.empty((M, C), dtype=torch.float32, device=dev)
     blank_logp = torch.empty(M, dtype=torch.float32, device=dev)
-    ws = _workspace(nbytes, dev)
-    code = L.pctc_frame_candidates(dt, _ptr(H), M, D, _ptr(W), _ptr(bias), V, int(blank), C, _ptr(ids), _ptr(logp),
-                                   _ptr(blank_logp), ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()),
-                                   _stream(None))
-    _check(code, "pctc_frame_candidates")
+    ws = _scratch(nbytes, dev)
+    code = L.pctc_frame_candidates(dt, H.data_ptr(), M, D, W.data_ptr(), None if bias is None else bias.data_ptr(), V,
+                                   int(blank), C, ids.data_ptr(), logp.data_ptr(), blank_logp.data_ptr(), ws.data_ptr(),
+                                   ws.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_frame_candidates")
     return {"ids": ids, "logp": logp, "blank_logp": blank_logp}
 
 
@@ -804,22 +805,24 @@ def beam_decode(H: torch.Tensor, W: torch.Tensor, input_lengths, beam_size: int 
     N, (M, D), V, K, C, dev = int(T.size), H.shape, int(W.shape[0]), int(beam_size), int(candidates), H.device
     if int(T.sum(dtype=np.int64)) != M:
         raise PrunedCTCError(-1, "sum of input lengths differs from the rows of H")
-    nbytes = int(L.pctc_beam_decode_workspace_size(dt, _i32p(T), N, D, V, K, C))
+    Tp = T.ctypes.data
+    nbytes = int(L.pctc_beam_decode_workspace_size(dt, Tp, N, D, V, K, C))
     if nbytes == 0:
         _check(-3 if (T < 1).any() else -1, "pctc_beam_decode")
     if max_tokens is None:
         max_tokens = int(T.max()) if N else 0
-    i32 = dict(dtype=torch.int32, device=dev)
-    f32 = dict(dtype=torch.float32, device=dev)
-    out = {"tokens": torch.empty((N, K, int(max_tokens)), **i32), "token_lengths": torch.empty((N, K), **i32),
-           "scores": torch.empty((N, K), **f32), "ids": torch.empty((M, C), **i32),
-           "logp": torch.empty((M, C), **f32), "blank_logp": torch.empty(M, **f32)}
-    ws = _workspace(nbytes, dev)
-    code = L.pctc_beam_decode(dt, _ptr(H), D, _ptr(W), _ptr(bias), V, _i32p(T), N, int(blank), K, C, float(token_bonus),
-                              int(max_tokens), _ptr(out["tokens"]), _ptr(out["token_lengths"]), _ptr(out["scores"]),
-                              _ptr(out["ids"]), _ptr(out["logp"]), _ptr(out["blank_logp"]),
-                              ctypes.c_void_p(ws.data_ptr()), ctypes.c_size_t(ws.numel()), _stream(None))
-    _check(code, "pctc_beam_decode")
+    most = int(max_tokens)
+    i32, f32 = torch.int32, torch.float32
+    out = {"tokens": torch.empty((N, K, most), dtype=i32, device=dev),
+           "token_lengths": torch.empty((N, K), dtype=i32, device=dev),
+           "scores": torch.empty((N, K), dtype=f32, device=dev), "ids": torch.empty((M, C), dtype=i32, device=dev),
+           "logp": torch.empty((M, C), dtype=f32, device=dev), "blank_logp": torch.empty(M, dtype=f32, device=dev)}
+    ws = _scratch(nbytes, dev)
+    code = L.pctc_beam_decode(dt, H.data_ptr(), D, W.data_ptr(), None if bias is None else bias.data_ptr(), V, Tp, N,
+                              int(blank), K, C, float(token_bonus), most, *map(torch.Tensor.data_ptr, out.values()),
+                              ws.data_ptr(), ws.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_beam_decode")
     return out
 
 
