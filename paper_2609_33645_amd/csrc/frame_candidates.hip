@@ -13,8 +13,9 @@
 // The scratch is held to 512 MB by passing over the vocabulary once per that many frames.
 //
 // The product is bound by the matrix cores from some 600 frames on (4,215 frames, D = 512, V = 180,000, bf16:
-// 860 us, 0.90 PFLOP/s of 1.20 in a large library product) and by the reading of W below (150 frames: 53 us, 3.5
-// TB/s).  The choice reads M V / 8 maxima (380 MB there) and 8 (C + 2) rows of W a frame (620 MB): 193 us.
+// 860 us, 0.90 PFLOP/s of 1.20 in a large library product) and by the reading of W below (64 frames: 34.5 us, 5.3
+// TB/s).  The choice is bound by the rows of W that it reads again (8 (C + 2) a frame, 620 MB there: 104 us, 6
+// TB/s).
 #include <algorithm>
 
 #include "pctc_internal.h"
@@ -81,7 +82,7 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 template <class T, int NT, bool KEPT>
 __global__ void __launch_bounds__(NT)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
-                   int V, int blank, int C, const float* __restrict__ bmax, int nb, const float2* __restrict__ partials, int M, int P,
+                   int V, int blank, int C, const float* __restrict__ bmax, int nb, const float2* __restrict__ partials, int M, int P, int vper,
                    const float* __restrict__ Z, int ldz,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
   constexpr int kPer = 16 / sizeof(T);
@@ -96,6 +97,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   __shared__ double part_sum[NT / 64];
   __shared__ int part_nan[NT / 64];
   __shared__ double lam_s;
+  __shared__ uint16_t scan_s[kMaxLseParts];
+  __shared__ int scans;
   __shared__ int sel[kMaxSel];
   __shared__ float z[kValues];
   __shared__ float val_v[kValues];
@@ -108,18 +111,19 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   const int nsel = min(C + 2, nb);
 
   // ---- the normaliser of each wavefront's partitions ----
+  float2 q[kParts];  // the largest logit of partition tid + i NT, and its sum
+  float mx = -INFINITY;
   {
     const float2* const q0 = partials + blockIdx.x;
-    float2 q[kParts];
-    float top = -INFINITY;
     int nan = 0;
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
       const int p = tid + i * NT;
       q[i] = p < P ? q0[static_cast<int64_t>(p) * M] : make_float2(-INFINITY, 0.f);
       nan |= (q[i].x != q[i].x) | (q[i].y != q[i].y);
-      top = fmaxf(top, q[i].x);
+      mx = fmaxf(mx, q[i].x);
     }
+    float top = mx;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     double sum = 0.0;
@@ -139,14 +143,22 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   }
 
   // ---- the nsel blocks with the largest maxima (equal ones: the lowest) ----
-  float mx = -INFINITY;
-  for (int i = tid * 4; i < nb; i += NT * 4) {
-    const float4 v = *reinterpret_cast<const float4*>(row + i);
-    mx = fmaxf(mx, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+  // Where there are many partitions, those blocks lie in the ones whose largest logit is at least the nsel-th of
+  // theirs, a few of them, and only these are read (4,215 frames, V = 180,000 in 88 partitions: 104 us, by the
+  // threads' maxima 193; 2,500 frames, V = 151,936 in 594, D = 4096: 276 and 323); else the blocks of at least
+  // the nsel-th of the threads' maxima, from two readings of all.
+  const bool by_parts = P >= 2 * nsel;
+  if (!by_parts) {
+    mx = -INFINITY;
+    for (int i = tid * 4; i < nb; i += NT * 4) {
+      const float4 v = *reinterpret_cast<const float4*>(row + i);
+      mx = fmaxf(mx, fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)));
+    }
   }
   keys[tid] = order_key(mx);
   if (tid == 0) {
     count = 0;
+    scans = 0;
     moved = 0;
   }
   __syncthreads();
@@ -172,20 +184,33 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
   }
   __syncthreads();
   uint32_t t = bound;
-  // (most threads have no block that large)
-  for (int i = order_key(mx) >= t ? tid * 4 : nb; i < nb; i += NT * 4) {
+  auto take = [&](int i) {  // the blocks in places i .. i + 3 that are large enough
     const float4 v4 = *reinterpret_cast<const float4*>(row + i);
     const float v[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       if (v[e] > -INFINITY && order_key(v[e]) >= t) {
-        const int q = atomicAdd(&count, 1);
-        if (q < kList) {
-          list_v[q] = v[e];
-          list_b[q] = CandBlocks::at(i + e);
+        const int at = atomicAdd(&count, 1);
+        if (at < kList) {
+          list_v[at] = v[e];
+          list_b[at] = CandBlocks::at(i + e);
         }
       }
     }
+  };
+  if (by_parts) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i)
+      if (q[i].x > -INFINITY && order_key(q[i].x) >= t)
+        scan_s[atomicAdd(&scans, 1)] = static_cast<uint16_t>(tid + i * NT);
+    __syncthreads();
+    const int quads = vper / (4 * kCandRows), all = scans * quads;
+    for (int x = tid; x < all; x += NT) {
+      const int i = (scan_s[x / quads] * quads + x % quads) * 4;
+      if (i < nb) take(i);
+    }
+  } else {  // (most threads have no block that large)
+    for (int i = order_key(mx) >= t ? tid * 4 : nb; i < nb; i += NT * 4) take(i);
   }
   __syncthreads();
   int n = count;
@@ -370,24 +395,24 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
   float* Z = L.ldz ? reinterpret_cast<float*>(s + L.o_z) : nullptr;
   for (int m0 = 0; m0 < M; m0 += F) {
     const int here = std::min(F, M - m0);
-    int P = 0;
+    int P = 0, vper = 0;
     hipError_t e;
     if (dtype == 1) {
       const uint16_t* Hm = static_cast<const uint16_t*>(H) + static_cast<int64_t>(m0) * D;
       const int Mp = (here + 63) / 64 * 64;
       uint16_t* Ht = cand_ht_bytes(here, D, V) > 0 ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
       if (Ht && (e = launch_ht_build_bf16(Hm, here, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
-      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, bmax, Z, L.ldz,
+      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, &vper, bmax, Z, L.ldz,
                                    stream, Ht, Mp);
     } else {
       e = launch_cand_partial_f32(static_cast<const float*>(H) + static_cast<int64_t>(m0) * D, here, D,
-                                  static_cast<const float*>(W), bias, V, partials, &P, bmax, Z, L.ldz, stream);
+                                  static_cast<const float*>(W), bias, V, partials, &P, &vper, bmax, Z, L.ldz, stream);
     }
     if (e != hipSuccess) return e;
     Prof pr("cand_select", stream);
 #define PCTC_SELECT(T, NT, KEPT)                                                                                      \
   hipLaunchKernelGGL((cand_select_kernel<T, NT, KEPT>), dim3(here), dim3(NT), 0, stream, static_cast<const T*>(H),    \
-                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, partials, here, P, Z, L.ldz, ids, \
+                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, partials, here, P, vper, Z, L.ldz, ids, \
                      logp, blank_logp)
     const bool few = here <= kFewFrames;
     if (Z) {  // (H and W are not read)

@@ -1267,7 +1267,7 @@ size_t cand_ht_bytes(int M, int D, int V) {
 }
 
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                    float2* partials, int* P_out, float* bmax, float* Z, int ldz, hipStream_t stream,
+                                    float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz, hipStream_t stream,
                                     const uint16_t* Ht, int Mp) {
   // Tiles of 64 frames while W's rows are what takes the time (up to two such tiles), and where all of them find
   // a compute unit.  In us, with tiles of 256: D = 512, V = 180,000: 64 frames 34.5 (46.5), 100 46 (49), 150 68
@@ -1282,6 +1282,7 @@ hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint1
     sp.P = (V + sp.vper - 1) / sp.vper;
   }
   *P_out = sp.P;
+  *vper_out = sp.vper;
   Prof pr("cand_partial", stream);
   const size_t bsh = bias ? static_cast<size_t>(sp.vper) * sizeof(float) : 0;
   const dim3 grid(grouped_grid(sp.nM, sp.P));
