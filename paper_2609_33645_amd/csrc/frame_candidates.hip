@@ -13,7 +13,7 @@
 // The scratch is held to 512 MB by passing over the vocabulary once per that many frames.
 //
 // The product is bound by the matrix cores from some 600 frames on (4,215 frames, D = 512, V = 180,000, bf16:
-// 860 us, 0.90 PFLOP/s of 1.20 in a large library product) and by the reading of W below (64 frames: 34.5 us, 5.3
+// 843 us, 0.92 PFLOP/s of 1.20 in a large library product) and by the reading of W below (64 frames: 34.5 us, 5.3
 // TB/s).  The choice is bound by the rows of W that it reads again (8 (C + 2) a frame, 620 MB there: 104 us, 6
 // TB/s).
 #include <algorithm>

@@ -184,22 +184,32 @@ __device__ __forceinline__ void lse_block_update(const f32x16 (&acc)[FR][FC], fl
 }
 
 // Writes the block maxima of a tile whose first class is v0; a frame's row has nb of them, a lane's
-// side by side (CandBlocks in pctc_internal.h has the order).
+// side by side (CandBlocks in pctc_internal.h has the order).  kBlockStores stores in every wavefront, also where
+// its frames lie past M (the resource ends there), so that waits for copies in flight can count on them.
+constexpr int kRawBuffer = 0x00020000;  // word 3 of a raw buffer resource: 32-bit data, no swizzle
+template <class G, int ROWS>
+constexpr int kBlockStores = G::FC * G::FR * 4 / ROWS;
 template <class G, int ROWS>
 __device__ __forceinline__ void store_block_max(const float (&bm)[G::FC][G::FR * 16 / ROWS], int v0, int wave, int lane,
                                                 int m0, int M, int nb, float* __restrict__ bmax) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the buffer-resource type exists on the device side only
   constexpr int kRun = G::FR * 16 / ROWS;
   static_assert(G::FR == 4 && kRun % 4 == 0, "wavefronts of 128 rows");
+  const __amdgpu_buffer_rsrc_t rows =
+      __builtin_amdgcn_make_buffer_rsrc(bmax + static_cast<int64_t>(m0) * nb, static_cast<short>(0),
+                                        min(M - m0, G::kBC) * nb * 4, kRawBuffer);
   const int at = ((v0 + G::row_of(wave, 0, 0, 0)) >> 7) * 2 * kRun + (lane >> 5) * kRun;
 #pragma unroll
   for (int j = 0; j < G::FC; ++j) {
-    const int m = m0 + G::col_of(wave, lane, j);
-    if (m >= M) continue;
-    float4* const out = reinterpret_cast<float4*>(bmax + static_cast<int64_t>(m) * nb + at);
+    const int off = (G::col_of(wave, lane, j) * nb + at) * 4;
 #pragma unroll
-    for (int k = 0; k < kRun / 4; ++k)
-      out[k] = make_float4(bm[j][4 * k], bm[j][4 * k + 1], bm[j][4 * k + 2], bm[j][4 * k + 3]);
+    for (int k = 0; k < kRun / 4; ++k) {
+      const u32x4 v = {__float_as_uint(bm[j][4 * k]), __float_as_uint(bm[j][4 * k + 1]),
+                       __float_as_uint(bm[j][4 * k + 2]), __float_as_uint(bm[j][4 * k + 3])};
+      __builtin_amdgcn_raw_buffer_store_b128(v, rows, off + 16 * k, 0, 0);
+    }
   }
+#endif
 }
 
 // Writes the logits of a tile whose first class is v0, ld (a whole number of tiles) to a frame.
