@@ -346,7 +346,8 @@ int32_t pctc_grouped_backward(pctc_dtype dtype, const void* H, int32_t M, int32_
 #define PCTC_MAX_CANDIDATES 64  /* candidate classes per frame */
 
 /* Frame candidates: for each frame the C most probable classes other than blank, with their log
- * probabilities and blank's, over the full vocabulary (Eq. lognorm); the logits are not stored.
+ * probabilities and blank's, over the full vocabulary (Eq. lognorm); the logits of a long vocabulary
+ * are not stored.
  * H, D, W, bias, V: as for pruned_ctc_fwd_bwd_ex; M >= 0 frames; 0 <= blank < V;
  * 1 <= C <= PCTC_MAX_CANDIDATES.
  * ids  device int32 [M, C], logp device float [M, C]: classes by falling logit (the lowest id first
@@ -354,7 +355,8 @@ int32_t pctc_grouped_backward(pctc_dtype dtype, const void* H, int32_t M, int32_
  *      the rest are -1 and -inf.  NaN or +inf logits give unspecified rows.
  * blank_logp  device float [M].
  * workspace: pctc_frame_candidates_workspace_size() bytes, 256-byte aligned; at most about 512 MiB
- *      (kept per frame and block of 8 classes; more frames than fit take another pass over W) beside
+ *      (per frame a value for each block of 8 classes, and the logits of a short vocabulary; more
+ *      frames than fit take another pass over W) beside
  *      the normaliser's partial sums.  Returns 0 for invalid arguments.
  * Asynchronous. */
 size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C);

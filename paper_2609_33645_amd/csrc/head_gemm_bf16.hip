@@ -309,7 +309,7 @@ cand_partial_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ H
     if constexpr (BIAS) bias_init<FR, FC, G>(a, bsh + it * TR, wave, lane);
     else G::zero(a);
   };
-  // (copies are not waited for behind the stores: 860 -> 843 us at 4,215 frames, D = 512, V = 180,000)
+  // (copies are not waited for behind the stores: 860 -> 843 us at 4,347 frames, D = 512, V = 180,000)
   constexpr int kStores = KEEP ? 0 : kBlockStores<G, kCandRows>;
   if constexpr (HT) G::template seq_aligned<kStores>(A, B, vbeg, m0, ntiles, D, acc, epi, init);
   else G::run_seq(A, B, vbeg, m0, ntiles, D, st, acc, epi, init);
@@ -1260,7 +1260,7 @@ hipError_t launch_amax_partial_bf16(const uint16_t* H, int M, int D, const uint1
 }
 
 // Bytes of H transposed where the candidates' product reads its frames from it (0: it does not), from the
-// size on at which the argmax does; wide heads too, whose product takes 32-deep tiles here (2,500 frames,
+// size on at which the argmax does; wide heads too, whose product takes 32-deep tiles here (2,669 frames,
 // D = 4096, V = 151,936: 2,860 us, from 64-deep tiles of H 3,230).
 size_t cand_ht_bytes(int M, int D, int V) {
   const size_t bytes = static_cast<size_t>(D) * ((M + 63) / 64 * 64) * sizeof(uint16_t);

@@ -258,8 +258,8 @@ hipError_t launch_grouped_adapter(const float* logp, const float* dlogp, int K, 
 // ---- frame candidates (frame_candidates.hip; products in head_gemm_bf16.hip, head_gemm_f32.hip) ----
 constexpr int kMaxCandidates = 64;
 // Classes of a block: the products keep a block's largest logit per frame.  With 8, half the rows of W
-// are read again that 16 take, for twice the maxima: selection and product, 4,215 frames, D = 512,
-// V = 180,000: 185 + 853 us, with 16 250 + 825; 2,500 frames, D = 4,096, V = 151,936: 307 + 3,214, with 16
+// are read again that 16 take, for twice the maxima: selection and product, 4,347 frames, D = 512,
+// V = 180,000: 185 + 853 us, with 16 250 + 825; 2,669 frames, D = 4,096, V = 151,936: 307 + 3,214, with 16
 // 670 + 3,190; fp32, 1,600 frames, D = 512, V = 5,000: 46 + 70, with 16 74 + 69.
 constexpr int kCandRows = 8;
 inline int cand_blocks(int V) { return (V + 255) / 256 * (256 / kCandRows); }  // a frame's block maxima
