@@ -606,13 +606,19 @@ def grouped_head(H: torch.Tensor, W: torch.Tensor, u_ids: torch.Tensor, bias: Op
 def _asynchronous(fn):
     """For calls that return before the device is done: with stream=..., the whole call, its
     allocations among it, is made on that stream, so that memory it lets go of is not handed out
-    to another stream while the kernels still use it."""
+    to another stream while the kernels still use it; nor is that of the caller's tensors.  What
+    another stream writes into them the caller waits for."""
     @functools.wraps(fn)
     def call(*args, stream=None, **kw):
         if stream is None:
             return fn(*args, **kw)
         with torch.cuda.stream(stream):
-            return fn(*args, **kw)
+            result = fn(*args, **kw)
+        for arg in (*args, *kw.values()):
+            for t in arg if isinstance(arg, (list, tuple)) else (arg,):
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
+        return result
     return call
 
 

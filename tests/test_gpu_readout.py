@@ -612,6 +612,35 @@ def test_other_stream():
         del junk
 
 
+def test_other_stream_keeps_the_callers_tensors():
+    """Tensors let go of right after a call on a busy stream, their memory asked for again on the current one."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    T = [80, 60]
+    H, W = spoken(8, T, 256, 4000, "bf16")
+    want = pc.beam_decode(dev(H, "bf16"), dev(W, "bf16"), T, 8, 16)
+    grads = [torch.randn(300_000, device="cuda") for _ in range(3)]
+    norm = pc.clip_grad_norm(grads, 1.0, out=[torch.empty_like(g) for g in grads])["norm"].clone()
+    a = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        Hd, Wd, gs = dev(H, "bf16"), dev(W, "bf16"), [g.clone() for g in grads]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                torch.mm(a, a)
+        got = pc.beam_decode(Hd, Wd, T, 8, 16, stream=side)
+        clipped = pc.clip_grad_norm(gs, 1.0, out=[torch.empty_like(g) for g in gs], stream=side)
+        sizes = [(t.shape, t.dtype) for t in (Hd, Wd, *gs)]
+        del Hd, Wd, gs
+        junk = [torch.full(s, 7, dtype=d, device="cuda") for s, d in sizes]
+        torch.cuda.synchronize()
+        assert all(torch.equal(want[k], got[k]) for k in want)
+        assert torch.equal(clipped["norm"], norm)
+        del junk
+
+
 def test_graph_replays():
     """A captured step (candidates, one frame of search, reordering) replayed on new frames."""
     import torch
