@@ -698,6 +698,8 @@ class BeamSearch:
         self._done = np.zeros(max(self.N, 1), np.int32)
         self._frames = np.zeros(max(self.N, 1), np.int32)
         self._host = self._frames.ctypes.data, self._done.ctypes.data
+        self._ones = np.ones_like(self._frames)
+        self._beams = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=self.device)  # (a shape)
         self.reset()
 
     @property
@@ -726,14 +728,15 @@ class BeamSearch:
             raise PrunedCTCError(-1, f"frames must have {self.N} entries")
         fr = self._frames
         fr[:self.N] = frames
-        M, dev = int(fr.sum()), self.device
-        if logp.dim() != 2 or logp.shape[0] != M or ids.shape != logp.shape or blank_logp.shape != logp.shape[:1]:
+        # (a live stream calls this every frame: a dot product takes half of a sum, empty_like of empty)
+        M, shape, dev = int(fr.dot(self._ones)), logp.shape, self.device
+        if len(shape) != 2 or shape[0] != M or ids.shape != shape or blank_logp.shape != (M,):
             raise PrunedCTCError(-1, f"ids and logp must be [{M}, C] and blank_logp [{M}]")
         if ids.device != dev or logp.device != dev or blank_logp.device != dev:
             raise PrunedCTCError(-1, f"candidates must be on {dev}")
         ids, logp, blank_logp = _as(ids, torch.int32), _as(logp, torch.float32), _as(blank_logp, torch.float32)
-        parents = torch.empty((self.N, self.beam_size), dtype=torch.int32, device=dev)
-        code = lib().pctc_beam_advance(ids.data_ptr(), logp.data_ptr(), blank_logp.data_ptr(), logp.shape[1],
+        parents = torch.empty_like(self._beams)
+        code = lib().pctc_beam_advance(ids.data_ptr(), logp.data_ptr(), blank_logp.data_ptr(), shape[1],
                                        self._host[0], self.N, self.beam_size, self.max_frames, self.token_bonus,
                                        self._host[1], *self._mem, parents.data_ptr(), _raw_stream(dev))
         if code:
@@ -772,7 +775,7 @@ def beam_reorder(states: Sequence[torch.Tensor], parents: torch.Tensor, out: Opt
     becomes state[n, parents[n, k]] (a parent outside [0, K) leaves it).  In place, or into the
     tensors `out`; returns those written.  Tensors must be contiguous."""
     dev = parents.device
-    if parents.dim() != 2 or parents.dtype is not torch.int32 or dev.type != "cuda":
+    if parents.dim() != 2 or parents.dtype is not torch.int32 or not parents.is_cuda:
         raise PrunedCTCError(-1, "parents must be a device int32 [N, K]")
     N, K = parents.shape
     parents = parents.contiguous()
@@ -781,11 +784,12 @@ def beam_reorder(states: Sequence[torch.Tensor], parents: torch.Tensor, out: Opt
         raise PrunedCTCError(-1, "out must have a tensor for each state")
     sizes = []
     for t, o in zip(states, dest):
-        if t.dim() < 2 or t.shape[:2] != parents.shape:
+        shape = t.shape
+        if len(shape) < 2 or shape[0] != N or shape[1] != K:
             raise PrunedCTCError(-1, f"a state must be [{N}, {K}, ...]")
         if t.device != dev or not t.is_contiguous():
             raise PrunedCTCError(-1, f"states must be contiguous tensors on {dev}")
-        if o is not t and (o.shape != t.shape or o.dtype is not t.dtype or o.device != dev or not o.is_contiguous()):
+        if o is not t and (o.shape != shape or o.dtype is not t.dtype or o.device != dev or not o.is_contiguous()):
             raise PrunedCTCError(-1, f"out must be contiguous tensors of the states' shapes and types on {dev}")
         sizes.append(t.nbytes // (N * K) if N * K else 0)
     src, dst, nbytes = _pointers(states), None if out is None else _pointers(dest), array("q", sizes)
