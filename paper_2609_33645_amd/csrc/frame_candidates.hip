@@ -13,7 +13,7 @@
 // The scratch is held to 512 MB by passing over the vocabulary once per that many frames.
 //
 // The product is bound by the matrix cores from some 600 frames on (4,347 frames, D = 512, V = 180,000, bf16:
-// 843 us, 0.92 PFLOP/s of 1.20 in a large library product) and by the reading of W below (64 frames: 34.5 us, 5.3
+// 811 us, 0.99 PFLOP/s of 1.20 in a large library product) and by the reading of W below (64 frames: 34 us, 5.4
 // TB/s).  The choice is bound by the rows of W that it reads again (8 (C + 2) a frame, 640 MB there: 104 us, 6
 // TB/s).
 #include <algorithm>
@@ -144,8 +144,8 @@ cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__
 
   // ---- the nsel blocks with the largest maxima (equal ones: the lowest) ----
   // Where there are many partitions, those blocks lie in the ones whose largest logit is at least the nsel-th of
-  // theirs, a few of them, and only these are read (4,347 frames, V = 180,000 in 88 partitions: 104 us, by the
-  // threads' maxima 193; 2,669 frames, V = 151,936 in 594, D = 4096: 276 and 323); else the blocks of at least
+  // theirs, a few of them, and only these are read (4,347 frames, V = 180,000: 103 us, by the
+  // threads' maxima 193; 2,669 frames, V = 151,936, D = 4096: 270 and 323); else the blocks of at least
   // the nsel-th of the threads' maxima, from two readings of all.
   const bool by_parts = P >= 2 * nsel;
   if (!by_parts) {

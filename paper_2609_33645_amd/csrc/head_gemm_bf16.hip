@@ -55,6 +55,9 @@ using GMidTW = bf::GemmMidA64<2, 4>;
 // candidates of few frames: 64 frames a tile, as W's rows bound it (three stages and two workgroups per CU: the same
 // times)
 using GFew = bf::Gemm<256, 64, 32, LL::KC, LL::KC, 4>;
+// the same copied 64 deep (whole lines) for longer rows, and with 128 frames a tile
+using GFewLong = bf::Gemm<256, 64, 64, LL::KC, LL::KC, 3>;
+using GFewTwo = bf::Gemm<256, 128, 64, LL::KC, LL::KC, 3>;
 constexpr int kMidRun = 8;
 constexpr int kRcCus = 224;  // workgroups of the dense recompute (one round)
 constexpr int kRcStores = 16;  // buffer stores per wave per 256 x 256 tile (recompute, E)
@@ -1268,21 +1271,51 @@ size_t cand_ht_bytes(int M, int D, int V) {
   return align_up(bytes, 256);
 }
 
+namespace {
+// Tiles and vocabulary runs of the candidates' product, in us (beside them with tiles of 256 frames):
+//  * 64 frames a tile while W's rows are what takes the time, and where all tiles find a compute unit:
+//    D = 512, V = 180,000, 64 frames 34 (46.5); V = 5,000, 64 frames 12.6 (16.4), 400 16 (25); copied 64 deep
+//    for long rows: D = 4096, V = 151,936, 64 frames 224 (255 copied 32 deep; 312);
+//  * 128 a tile for one such tile: 128 frames, D = 512, V = 180,000 44 (two of 64 48; 49), D = 4096,
+//    V = 151,936 277 (two of 64 341; 334);
+//  * 256 a tile from there on, in runs of the length that a count of the rounds makes shortest, the longest
+//    of equal ones: D = 512, V = 180,000, 700 frames 159 (runs of 8 223), 1,700 317 (335), 4,347 775 (805).
+enum class CandTile { kFew, kFewLong, kFewTwo, kMid };
+struct CandSplit {
+  CandTile tile;
+  int nM, P, vper;
+};
+CandSplit cand_split(int M, int D, int V, bool from_ht) {
+  const int vtiles = (V + 255) / 256, least = (vtiles + lse_max_parts(D) - 1) / lse_max_parts(D);
+  const int few = (M + 63) / 64;
+  CandSplit s;
+  int run = least;
+  if (!from_ht && (few <= 2 || static_cast<int64_t>(few) * vtiles <= 256)) {
+    const bool two = few == 2 && 2 * vtiles > 256 && D >= 512;
+    s.tile = two ? CandTile::kFewTwo : D >= 1024 ? CandTile::kFewLong : CandTile::kFew;
+    s.nM = two ? 1 : few;
+  } else {
+    s.tile = CandTile::kMid;
+    s.nM = (M + 255) / 256;
+    double best = -1;
+    for (int r = least; r <= std::max(least, kMidRun); ++r) {
+      const double t = grouped_rounds(s.nM, (vtiles + r - 1) / r) * (r * (D / 32 * 0.53 + 4) + 4);
+      if (best < 0 || t <= best) {
+        best = t;
+        run = r;
+      }
+    }
+  }
+  s.vper = run * 256;
+  s.P = (V + s.vper - 1) / s.vper;
+  return s;
+}
+}  // namespace
+
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                     float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz, hipStream_t stream,
                                     const uint16_t* Ht, int Mp) {
-  // Tiles of 64 frames while W's rows are what takes the time (up to two such tiles), and where all of them find
-  // a compute unit.  In us, with tiles of 256: D = 512, V = 180,000: 64 frames 34.5 (46.5), 100 46 (49), 150 68
-  // (50); D = 4096, V = 151,936: 64 252 (312), 128 328 (334); D = 512, V = 5,000: 64 12.6 (16.4), 400 16 (25);
-  // D = 1024, V = 30,000: 128 (236 tiles) 20.6 (27), 192 (354 tiles) 28.6 (28.7).
-  LseSplit sp = lse_split_bf16(M, D, V, SplitFor::kAmax);
-  const int vtiles = (V + GFew::kBR - 1) / GFew::kBR, ftiles = (M + GFew::kBC - 1) / GFew::kBC;
-  const bool few = !Ht && (ftiles <= 2 || static_cast<int64_t>(ftiles) * vtiles <= 256);
-  if (few) {
-    sp.nM = ftiles;
-    sp.vper = (vtiles + lse_max_parts(D) - 1) / lse_max_parts(D) * GFew::kBR;
-    sp.P = (V + sp.vper - 1) / sp.vper;
-  }
+  const CandSplit sp = cand_split(M, D, V, Ht != nullptr);
   *P_out = sp.P;
   *vper_out = sp.vper;
   Prof pr("cand_partial", stream);
@@ -1298,8 +1331,12 @@ hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint1
   else PCTC_CAND1(G, false, false);
   if (Ht) {
     PCTC_CAND(GMidTW)
-  } else if (few) {
+  } else if (sp.tile == CandTile::kFew) {
     PCTC_CAND(GFew)
+  } else if (sp.tile == CandTile::kFewLong) {
+    PCTC_CAND(GFewLong)
+  } else if (sp.tile == CandTile::kFewTwo) {
+    PCTC_CAND(GFewTwo)
   } else {
     PCTC_CAND(GMid)
   }
