@@ -190,6 +190,25 @@ def test_candidates_certain_frames(dtype, top):
     assert np.abs(out.cpu().numpy().astype(np.float64) - want).max() <= 20 * 2.0**-24
 
 
+@pytest.mark.parametrize("M,D,V,C", [
+    (100, 520, 40_001, 16), (65, 4096, 33_003, 3), (128, 512, 70_001, 64),  # one tile of 128 frames
+    (64, 1032, 40_001, 5), (130, 1024, 12_000, 16),                         # rows copied 64 deep
+    (700, 512, 230_001, 16), (1025, 2048, 40_007, 8)])                      # frames from H transposed
+@pytest.mark.parametrize("bias", [False, True])
+def test_candidates_tiles(M, D, V, C, bias):
+    """The product's other tiles, up to 50 frames of them against the definition."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    say("tiles", M, D, V, C, bias)
+    H, W = head(M + V + D, M, D, V, "bf16", 3.0)
+    b = (np.random.default_rng(V).normal(size=V) * 2).astype(np.float32) if bias else None
+    got = pc.frame_candidates(dev(H, "bf16"), dev(W, "bf16"), C, 3, None if b is None else dev(b))
+    rows = np.unique(np.concatenate([[0, M - 1], np.random.default_rng(M).integers(0, M, 48)]))
+    at = torch.from_numpy(rows).cuda()
+    check_candidates(H[rows], W, C, 3, b, "bf16", {k: v[at] for k, v in got.items()})
+
+
 def test_candidates_without_frames():
     import torch
 
