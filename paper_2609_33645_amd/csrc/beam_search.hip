@@ -186,7 +186,8 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
   __shared__ float bl_s[kRing];
   __shared__ int first_s[KT + 1];     // pairs of the beams before
   __shared__ int merged_s[64 * kPairs];  // frame (from 1) in which a pair's prefix was last a beam
-  __shared__ __attribute__((aligned(16))) float val_s[64 * kBatches + 16];  // totals to be ordered: staying beams, pairs
+  // totals to be ordered: staying beams, pairs
+  __shared__ __attribute__((aligned(16))) float val_s[64 * kBatches + 16];
   __shared__ int what_s[64 * kBatches];  // of a pair: beam + 256 class
   __shared__ int2 place_s[KT];        // of each place: what, with bit 30 for a pair, and the total
   const int lane = threadIdx.x, i = lane & (KT - 1), copy = lane / KT;
@@ -224,8 +225,8 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
   int first = 0, pairs;  // pairs of the beams before, and of all
   {
     // (a quotient that is no whole number is at least 1/32 away from one)
-    const int here = lane < K ? min(C, static_cast<int>(static_cast<float>(K) / static_cast<float>(lane + 1) + 0.01f) + 1)
-                              : 0;
+    const int classes = static_cast<int>(static_cast<float>(K) / static_cast<float>(lane + 1) + 0.01f) + 1;
+    const int here = lane < K ? min(C, classes) : 0;
     int sum = here;
 #pragma unroll
     for (int o = 1; o < KT; o <<= 1) {

@@ -82,8 +82,8 @@ __device__ __forceinline__ float dot16(const u32x4& w, const u32x4& h, float s, 
 template <class T, int NT, bool KEPT>
 __global__ void __launch_bounds__(NT)
 cand_select_kernel(const T* __restrict__ H, int m0, int D, const T* __restrict__ W, const float* __restrict__ bias,
-                   int V, int blank, int C, const float* __restrict__ bmax, int nb, const float2* __restrict__ partials, int M, int P, int vper,
-                   const float* __restrict__ Z, int ldz,
+                   int V, int blank, int C, const float* __restrict__ bmax, int nb,
+                   const float2* __restrict__ partials, int M, int P, int vper, const float* __restrict__ Z, int ldz,
                    int32_t* __restrict__ ids, float* __restrict__ logp, float* __restrict__ blank_logp) {
   constexpr int kPer = 16 / sizeof(T);
   constexpr int kValues = kMaxSel * kCandRows;
@@ -362,7 +362,8 @@ namespace {
 bool keeps_logits(int dtype, int D, int V, int C) {
   return V <= 32768 && V < static_cast<int64_t>(C + 2) * D * (dtype == 1 ? 2 : 4);
 }
-// Scratch of a pass: the normaliser's partial pairs, the block maxima, the logits where they are kept and, where the product reads it, H transposed.
+// Scratch of a pass: the normaliser's partial pairs, the block maxima, the logits where they are kept and, where
+// the product reads it, H transposed.
 struct CandLayout {
   int frames, blocks, ldz;
   size_t o_bmax, o_z, o_ht, total;
@@ -402,8 +403,8 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
       const int Mp = (here + 63) / 64 * 64;
       uint16_t* Ht = cand_ht_bytes(here, D, V) > 0 ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
       if (Ht && (e = launch_ht_build_bf16(Hm, here, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
-      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, &vper, bmax, Z, L.ldz,
-                                   stream, Ht, Mp);
+      e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, &vper, bmax, Z,
+                                   L.ldz, stream, Ht, Mp);
     } else {
       e = launch_cand_partial_f32(static_cast<const float*>(H) + static_cast<int64_t>(m0) * D, here, D,
                                   static_cast<const float*>(W), bias, V, partials, &P, &vper, bmax, Z, L.ldz, stream);
@@ -412,8 +413,8 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
     Prof pr("cand_select", stream);
 #define PCTC_SELECT(T, NT, KEPT)                                                                                      \
   hipLaunchKernelGGL((cand_select_kernel<T, NT, KEPT>), dim3(here), dim3(NT), 0, stream, static_cast<const T*>(H),    \
-                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, partials, here, P, vper, Z, L.ldz, ids, \
-                     logp, blank_logp)
+                     m0, D, static_cast<const T*>(W), bias, V, blank, C, bmax, nb, partials, here, P, vper, Z, L.ldz, \
+                     ids, logp, blank_logp)
     const bool few = here <= kFewFrames;
     if (Z) {  // (H and W are not read)
       if (few) PCTC_SELECT(float, 1024, true);

@@ -1313,8 +1313,8 @@ CandSplit cand_split(int M, int D, int V, bool from_ht) {
 }  // namespace
 
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                    float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz, hipStream_t stream,
-                                    const uint16_t* Ht, int Mp) {
+                                    float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz,
+                                    hipStream_t stream, const uint16_t* Ht, int Mp) {
   const CandSplit sp = cand_split(M, D, V, Ht != nullptr);
   *P_out = sp.P;
   *vper_out = sp.vper;
@@ -1324,10 +1324,10 @@ hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint1
 #define PCTC_CAND1(G, B, K)                                                                                        \
   hipLaunchKernelGGL((cand_partial_bf16<G, B, K>), grid, dim3(G::kThreads), bsh, stream, H, Ht, Mp, M, D, W, bias,   \
                      V, sp.P, sp.vper, partials, cand_blocks(V), bmax, Z, ldz)
-#define PCTC_CAND(G)                    \
-  if (bias && Z) PCTC_CAND1(G, true, true);        \
-  else if (bias) PCTC_CAND1(G, true, false);       \
-  else if (Z) PCTC_CAND1(G, false, true);          \
+#define PCTC_CAND(G)                         \
+  if (bias && Z) PCTC_CAND1(G, true, true);  \
+  else if (bias) PCTC_CAND1(G, true, false); \
+  else if (Z) PCTC_CAND1(G, false, true);    \
   else PCTC_CAND1(G, false, false);
   if (Ht) {
     PCTC_CAND(GMidTW)

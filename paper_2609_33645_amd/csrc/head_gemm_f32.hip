@@ -489,7 +489,8 @@ hipError_t launch_amax_partial_f32(const float* H, int M, int D, const float* W,
 }
 
 hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
-                                   float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz, hipStream_t stream) {
+                                   float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz,
+                                   hipStream_t stream) {
   int vper, P;
   lse_split_f32(D, V, &vper, &P);
   *P_out = P;

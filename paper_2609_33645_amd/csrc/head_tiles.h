@@ -214,8 +214,8 @@ __device__ __forceinline__ void store_block_max(const float (&bm)[G::FC][G::FR *
 
 // Writes the logits of a tile whose first class is v0, ld (a whole number of tiles) to a frame.
 template <class G>
-__device__ __forceinline__ void store_logits(const f32x16 (&acc)[G::FR][G::FC], int v0, int wave, int lane, int m0, int M,
-                                             int ld, float* __restrict__ Z) {
+__device__ __forceinline__ void store_logits(const f32x16 (&acc)[G::FR][G::FC], int v0, int wave, int lane, int m0,
+                                             int M, int ld, float* __restrict__ Z) {
 #pragma unroll
   for (int j = 0; j < G::FC; ++j) {
     const int m = m0 + G::col_of(wave, lane, j);

@@ -287,10 +287,11 @@ struct CandBlocks {
 // past V); with Z (null: not kept) the logits, ldz a whole number of tiles to a frame.  Ht (null: none): H
 // transposed [D][Mp] of cand_ht_bytes.
 hipError_t launch_cand_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                    float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz, hipStream_t stream,
-                                    const uint16_t* Ht = nullptr, int Mp = 0);
+                                    float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz,
+                                    hipStream_t stream, const uint16_t* Ht = nullptr, int Mp = 0);
 hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W, const float* bias, int V,
-                                   float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz, hipStream_t stream);
+                                   float2* partials, int* P_out, int* vper_out, float* bmax, float* Z, int ldz,
+                                   hipStream_t stream);
 size_t cand_ht_bytes(int M, int D, int V);
 size_t cand_scratch_bytes(int dtype, int M, int D, int V, int C);  // of a call
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
