@@ -364,6 +364,11 @@ int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_
                               const float* bias, int32_t V, int32_t blank, int32_t C, int32_t* ids,
                               float* logp, float* blank_logp, void* workspace, size_t workspace_bytes,
                               void* stream);
+/* How such a call divides its frames: *frames is the number that the pass from frame m0 on takes (0 <= m0 < M),
+ * and the result the bytes of the workspace, from its start on, that this pass uses; 0 on invalid arguments.
+ * Host only; no device work. */
+size_t pctc_frame_candidates_pass(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C, int32_t m0,
+                                  int32_t* frames);
 
 /* Prefix beam search.  Up to K label prefixes per utterance, each with the mass of its alignments
  * that end in blank (pb) and in its last label (pn).  With b a frame's blank score, l(c) the score of

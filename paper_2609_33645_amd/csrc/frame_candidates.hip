@@ -381,9 +381,20 @@ CandLayout cand_layout(int dtype, int M, int D, int V, int C) {
   L.total = L.o_ht + (dtype == 1 ? cand_ht_bytes(L.frames, D, V) : 0);
   return L;
 }
+// Bytes of H transposed for a pass over `here` frames (0: the product reads H itself).  A full pass's are too many
+// to be addressed where D is large beside V; the layout then has no room for them, nor for a shorter last pass's.
+size_t pass_ht_bytes(const CandLayout& L, int here, int D, int V) {
+  return L.total > L.o_ht ? cand_ht_bytes(here, D, V) : 0;
+}
 }  // namespace
 
 size_t cand_scratch_bytes(int dtype, int M, int D, int V, int C) { return cand_layout(dtype, M, D, V, C).total; }
+
+size_t cand_pass_bytes(int dtype, int M, int D, int V, int C, int m0, int* frames) {
+  const CandLayout L = cand_layout(dtype, M, D, V, C);
+  *frames = std::min(L.frames, M - m0);
+  return L.o_ht + (dtype == 1 ? pass_ht_bytes(L, *frames, D, V) : 0);
+}
 
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
                                    int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
@@ -401,7 +412,7 @@ hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const
     if (dtype == 1) {
       const uint16_t* Hm = static_cast<const uint16_t*>(H) + static_cast<int64_t>(m0) * D;
       const int Mp = (here + 63) / 64 * 64;
-      uint16_t* Ht = cand_ht_bytes(here, D, V) > 0 ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
+      uint16_t* Ht = pass_ht_bytes(L, here, D, V) > 0 ? reinterpret_cast<uint16_t*>(s + L.o_ht) : nullptr;
       if (Ht && (e = launch_ht_build_bf16(Hm, here, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
       e = launch_cand_partial_bf16(Hm, here, D, static_cast<const uint16_t*>(W), bias, V, partials, &P, &vper, bmax, Z,
                                    L.ldz, stream, Ht, Mp);

@@ -972,6 +972,12 @@ size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t
   return cand_scratch_bytes(dtype == PCTC_BF16 ? 1 : 0, M, D, V, C);
 }
 
+size_t pctc_frame_candidates_pass(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C, int32_t m0,
+                                  int32_t* frames) {
+  if (pctc_frame_candidates_workspace_size(dtype, M, D, V, C) == 0 || m0 < 0 || m0 >= M || !frames) return 0;
+  return cand_pass_bytes(dtype == PCTC_BF16 ? 1 : 0, M, D, V, C, m0, frames);
+}
+
 int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W, const float* bias,
                               int32_t V, int32_t blank, int32_t C, int32_t* ids, float* logp, float* blank_logp,
                               void* workspace, size_t workspace_bytes, void* stream_ptr) {

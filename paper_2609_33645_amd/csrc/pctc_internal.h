@@ -294,6 +294,8 @@ hipError_t launch_cand_partial_f32(const float* H, int M, int D, const float* W,
                                    hipStream_t stream);
 size_t cand_ht_bytes(int M, int D, int V);
 size_t cand_scratch_bytes(int dtype, int M, int D, int V, int C);  // of a call
+// Of its pass over the frames from m0 on (*frames of them): the bytes from the scratch's start that it uses.
+size_t cand_pass_bytes(int dtype, int M, int D, int V, int C, int m0, int* frames);
 hipError_t launch_frame_candidates(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
                                    int blank, int C, int32_t* ids, float* logp, float* blank_logp, void* scratch,
                                    hipStream_t stream);

@@ -116,6 +116,8 @@ def lib() -> ctypes.CDLL:
     L.pctc_frame_candidates.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_i32, c_i32, c_p, c_p, c_p, c_p, c_sz,
                                         c_p]
     L.pctc_frame_candidates.restype = c_i32
+    L.pctc_frame_candidates_pass.argtypes = [c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, i32p]
+    L.pctc_frame_candidates_pass.restype = c_sz
     L.pctc_beam_state_bytes.argtypes = [c_i32, c_i32, c_i32]
     L.pctc_beam_state_bytes.restype = c_sz
     L.pctc_beam_reset.argtypes = [c_i32, c_i32, c_i32, c_p, c_sz, c_p]

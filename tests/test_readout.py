@@ -209,3 +209,34 @@ def test_binding_refusals():
         with pytest.raises(pc.PrunedCTCError) as e:
             call()
         assert e.value.code == -1
+
+
+@built
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_candidates_passes_stay_in_the_workspace(dtype):
+    """Every pass of a call uses no more than the workspace asked for: short and long vocabularies, narrow and
+    wide heads, and numbers of frames whose last pass is short while a full one is too large to be transposed."""
+    L = _lib()
+    frames = ctypes.c_int32()
+
+    def check(M, D, V, C):
+        size, m0, n = L.pctc_frame_candidates_workspace_size(dtype, M, D, V, C), 0, 0
+        assert size > 0
+        while m0 < M:
+            used = L.pctc_frame_candidates_pass(dtype, M, D, V, C, m0, ctypes.byref(frames))
+            assert 0 < used <= size and 0 < frames.value <= M - m0, (M, D, V, C, m0, frames.value, used - size)
+            m0, n = m0 + frames.value, n + 1
+        return n
+    assert check(252_500, 8192, 512, 8) == 2 and check(168_000, 8192, 768, 8) == 2
+    assert check(270_000, 5120, 512, 8) == 2
+    for D in (8, 128, 512, 640, 4096, 8192, 65_536, 1 << 20):
+        for V in (2, 300, 512, 768, 5000, 32_768, 180_000, 524_288):
+            for C in (1, 16, 64):
+                full = ctypes.c_int32()
+                assert L.pctc_frame_candidates_pass(dtype, 1 << 30, D, V, C, 0, ctypes.byref(full)) > 0
+                F = full.value
+                for M in (1, 63, F - 1, F, F + 1, F + 100, F + F // 16, F + F // 2, 2 * F, 2 * F + 3000, 5 * F + 7):
+                    check(M, D, V, C)
+    for bad in ((1, 512, 1000, 16, 1), (1, 512, 1000, 16, -1), (0, 512, 1000, 16, 0), (4, 500, 1000, 16, 0)):
+        assert L.pctc_frame_candidates_pass(dtype, *bad, ctypes.byref(frames)) == 0
+    assert L.pctc_frame_candidates_pass(dtype, 4, 512, 1000, 16, 0, None) == 0
