@@ -389,8 +389,10 @@ size_t pctc_frame_candidates_pass(pctc_dtype dtype, int32_t M, int32_t D, int32_
  * K max_frames >= 2^31).  pctc_beam_reset starts every utterance with the empty prefix.
  *
  * pctc_beam_advance: `frames` more frames of each utterance.  ids, logp [sum frames, C], blank_logp
- * [sum frames]: device, utterance after utterance, as pctc_frame_candidates writes them (classes
- * distinct and not blank, scores falling; an id below 0, or a score of -inf or NaN, is no candidate).
+ * [sum frames]: device, utterance after utterance, as pctc_frame_candidates writes them.  An id below 0, or a
+ * score of -inf or NaN, is no candidate, in any place of a row; the others' classes are distinct and not blank,
+ * and their scores fall along the row (a row in another order loses prefixes: only classes that can be among the
+ * K best by their place are looked at).
  * frames: HOST int32 [N], >= 0.  frames_done: HOST int32 [N], in and out: the frames each utterance
  * has had since the reset (zeros then); an utterance that would pass max_frames is PCTC_ELENGTH, before
  * any work.  token_bonus: finite.  parents: device int32 [N, K] or NULL: the beam at the start of

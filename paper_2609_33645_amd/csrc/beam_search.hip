@@ -278,14 +278,32 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
 #endif
   };
   const int no_class = lane < C ? 0 : -1;
+  const uint64_t places = ~uint64_t{0} >> (64 - C);
   auto stage = [&](int f) {  // the same frames (f a multiple of 8)
     const int r0 = f & (kRing - 1);
+    float x[kAhead], least = INFINITY;
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
-      const int id = fid[g] | no_class;
       // all ones, no number, where the class is none; the maximum takes -inf for no number
-      lp_s[r0 + g][lane] = fmaxf(__int_as_float(__float_as_int(fl[g]) | (id >> 31)), kNegInf);
-      id_s[r0 + g][lane] = id;
+      x[g] = fmaxf(__int_as_float(__float_as_int(fl[g]) | ((fid[g] | no_class) >> 31)), kNegInf);
+      least = fminf(least, x[g]);
+    }
+    // the pairs looked at go by a class's place among the classes there are, so empty places move behind them
+    if (__builtin_expect(lanes_where(least > kNegInf) == places, 1)) {
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) {
+        lp_s[r0 + g][lane] = x[g];
+        id_s[r0 + g][lane] = fid[g] | no_class;
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < kAhead; ++g) {
+        const uint64_t full = lanes_where(x[g] > kNegInf);
+        const int before = __popcll(full & ((uint64_t{1} << lane) - 1));
+        const int at = x[g] > kNegInf ? before : __popcll(full) + lane - before;
+        lp_s[r0 + g][at] = x[g];
+        id_s[r0 + g][at] = fid[g] | no_class;
+      }
     }
     if (lane < kAhead) bl_s[r0 + lane] = fmaxf(fb, kNegInf);
     __builtin_amdgcn_wave_barrier();

@@ -721,9 +721,11 @@ class BeamSearch:
     def advance(self, ids: torch.Tensor, logp: torch.Tensor, blank_logp: torch.Tensor, frames: Sequence[int],
                 *, stream=None) -> torch.Tensor:
         """frames[n] more frames of utterance n (0: none), packed utterance after utterance: ids and
-        logp [sum frames, C], blank_logp [sum frames].  Returns parents [N, beam_size] (int32): the
-        beam before the call that each beam descends from, -1 where there is no prefix (for
-        beam_reorder)."""
+        logp [sum frames, C], blank_logp [sum frames].  A row's classes are distinct and not blank, and
+        their scores fall (a row in another order loses prefixes: sort it again after adding scores of
+        your own); places with an id below 0 or a score of -inf or NaN, anywhere in a row, are left out.
+        Returns parents [N, beam_size] (int32): the beam before the call that each beam descends from,
+        -1 where there is no prefix (for beam_reorder)."""
         if isinstance(frames, torch.Tensor):
             frames = frames.detach().cpu().numpy()
         if len(frames) != self.N:

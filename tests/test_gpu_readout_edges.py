@@ -1,0 +1,66 @@
+"""Readout with beams and clipping on the GPU, where calls are out of the ordinary (references and
+tolerances as in test_gpu_readout)."""
+import numpy as np
+import pytest
+
+from tests import readout_ref as ref
+from tests.gpu_util import say
+from tests.test_gpu_readout import check_result, random_frames, run_search
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- rows with empty places ------------------------------------------------------------------
+
+def with_gaps(seed, ids, lp, share):
+    """The rows with places made empty in every way, whole runs at the beginning among them; and the same
+    rows with the empty places last."""
+    r = np.random.default_rng(seed)
+    ids, lp = ids.copy(), lp.copy()
+    T, C = ids.shape
+    gone = r.random((T, C)) < share
+    for t in range(0, T, 3):
+        gone[t, :r.integers(0, C)] = True
+    gone[T // 2] = False
+    kind = r.integers(0, 4, size=(T, C))
+    ids[gone & (kind == 0)] = -1
+    ids[gone & (kind == 1)] = -7
+    lp[gone & (kind == 2)] = -np.inf
+    lp[gone & (kind == 3)] = np.nan
+    order = np.argsort(gone, 1, kind="stable")
+    packed = np.sort(gone, 1)
+    return ids, lp, np.where(packed, -1, np.take_along_axis(ids, order, 1)), \
+        np.where(packed, -np.inf, np.take_along_axis(lp, order, 1)).astype(np.float32)
+
+
+@pytest.mark.parametrize("K,C", [(1, 3), (1, 64), (4, 8), (8, 16), (8, 64), (16, 24), (32, 40), (32, 64)])
+@pytest.mark.parametrize("share", [0.1, 0.6])
+def test_search_empty_places(K, C, share):
+    """An empty place is no candidate wherever it stands: rows with them are searched bit for bit as the rows
+    without them, and as the definition has it."""
+    say("empty places", K, C, share)
+    parts, packed, T = [], [], (1, 9, 30)
+    for n, t in enumerate(T):
+        for k in range(400):
+            ids, lp, bl = random_frames(100 * n + 7919 * k + K, t, C, C + 6)
+            a, b, c, d = with_gaps(k, ids, lp, share)
+            s = ref.Search(K).run(a, b, bl)
+            if s.gap > 2e-5:
+                break
+        parts.append((a, b, bl, s))
+        packed.append((c, d, bl))
+    got, same = run_search([q[:3] for q in parts], K), run_search(packed, K)
+    assert all(np.array_equal(got[k], same[k]) for k in got)
+    for n, q in enumerate(parts):
+        assert q[3].gap > 2e-5
+        check_result(got, n, q[3].result(), T[n])
+
+
+def test_search_empty_places_first():
+    """Candidates behind more empty places than there are beams."""
+    def one(K, ids, lp, bl):
+        ids, lp, bl = np.array([ids], np.int32), np.array([lp], np.float32), np.array([bl], np.float32)
+        check_result(run_search([(ids, lp, bl)], K), 0, ref.Search(K).run(ids, lp, bl).result(), 1)
+    one(1, [-1, -1, 9], [-.01, -.02, -.05], -4.0)
+    one(4, [-1] * 6 + [7, 8], [-.1 * k for k in range(1, 9)], -3.0)
+    one(2, [5, 6, 4, 7], [-np.inf, np.nan, -0.5, -1.0], -3.0)
