@@ -62,6 +62,13 @@ __device__ __forceinline__ float log_add(float a, float b, float c) {
 // several times as long).
 __device__ __forceinline__ uint32_t above(float x, float y) { return __float_as_uint(y - x) >> 31; }
 
+// What a lane wrote to the LDS before is there for the others after: a wavefront's LDS operations run in program
+// order, and the fence keeps the compiler from reordering them or from taking a lane's own value for what it reads.
+__device__ __forceinline__ void exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __device__ __forceinline__ uint64_t lanes_where(bool x) { return __builtin_amdgcn_ballot_w64(x); }
 
 // The hash of a prefix with one more label.
@@ -281,21 +288,21 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
   const uint64_t places = ~uint64_t{0} >> (64 - C);
   auto stage = [&](int f) {  // the same frames (f a multiple of 8)
     const int r0 = f & (kRing - 1);
+    exchange();  // (the rows' frames before have been read)
     float x[kAhead], least = INFINITY;
 #pragma unroll
     for (int g = 0; g < kAhead; ++g) {
+      const int id = fid[g] | no_class;
       // all ones, no number, where the class is none; the maximum takes -inf for no number
-      x[g] = fmaxf(__int_as_float(__float_as_int(fl[g]) | ((fid[g] | no_class) >> 31)), kNegInf);
+      x[g] = fmaxf(__int_as_float(__float_as_int(fl[g]) | (id >> 31)), kNegInf);
       least = fminf(least, x[g]);
+      lp_s[r0 + g][lane] = x[g];
+      id_s[r0 + g][lane] = id;
     }
+    if (lane < kAhead) bl_s[r0 + lane] = fmaxf(fb, kNegInf);
     // the pairs looked at go by a class's place among the classes there are, so empty places move behind them
-    if (__builtin_expect(lanes_where(least > kNegInf) == places, 1)) {
-#pragma unroll
-      for (int g = 0; g < kAhead; ++g) {
-        lp_s[r0 + g][lane] = x[g];
-        id_s[r0 + g][lane] = fid[g] | no_class;
-      }
-    } else {
+    if (__builtin_expect(lanes_where(least > kNegInf) != places, 0)) {
+      exchange();
 #pragma unroll
       for (int g = 0; g < kAhead; ++g) {
         const uint64_t full = lanes_where(x[g] > kNegInf);
@@ -305,8 +312,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
         id_s[r0 + g][at] = fid[g] | no_class;
       }
     }
-    if (lane < kAhead) bl_s[r0 + lane] = fmaxf(fb, kNegInf);
-    __builtin_amdgcn_wave_barrier();
+    exchange();
   };
   // the beam whose prefix is this beam's without its last label
   auto find_parent = [&]() {
@@ -426,11 +432,12 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
       sn = log_add(again, join);
       // a pair whose prefix is a beam already is no new one
       const bool joins = par >= 0 && pos >= 0 && copy == 0, joined = lanes_where(joins) != 0;
+      exchange();  // (the frame before has been read)
       if (joins) {
         const int e = first_s[par] + pos;
         if (e < first_s[par + 1]) merged_s[e] = fr + 1;
       }
-      __builtin_amdgcn_wave_barrier();
+      exchange();
       const float least = lanes_min<KT>(mine ? total : INFINITY);
 #pragma unroll
       for (int q = 0; q < kPairs; ++q) {
@@ -456,6 +463,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
 
     // the totals to be ordered, in the order of ties
     int count = K;
+    exchange();  // (the frame before has been read)
     if (copy == 0 && mine) val_s[i] = total;
 #pragma unroll
     for (int q = 0; q < kPairs; ++q) {
@@ -467,7 +475,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
       count += __popcll(enter[q]);
     }
     if (lane < 16) val_s[count + lane] = kNegInf;
-    __builtin_amdgcn_wave_barrier();
+    exchange();
     // entry e = 64 q + lane in this lane's registers
     float v[kBatches];
     int what[kBatches], place[kBatches];
@@ -499,7 +507,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
 #pragma unroll
       for (int q = 0; q < kBatches; ++q)
         if (v[q] > kNegInf && place[q] < K) place_s[place[q]] = make_int2(what[q], __float_as_int(v[q]));
-      __builtin_amdgcn_wave_barrier();
+      exchange();
     };
     put();
     bool tied = false;
@@ -507,6 +515,7 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
     for (int q = 0; q < kBatches; ++q)
       tied |= v[q] > kNegInf && place[q] < K && place_s[place[q] & (KT - 1)].x != what[q];
     if (__builtin_expect(lanes_where(tied) != 0, 0)) {
+      exchange();
 #pragma unroll
       for (int q = 0; q < kBatches; ++q)
         for (int o = 0; o < 64 * q + lane && o < count; ++o) place[q] += val_s[o] == v[q];

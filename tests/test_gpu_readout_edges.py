@@ -64,3 +64,23 @@ def test_search_empty_places_first():
     one(1, [-1, -1, 9], [-.01, -.02, -.05], -4.0)
     one(4, [-1] * 6 + [7, 8], [-.1 * k for k in range(1, 9)], -3.0)
     one(2, [5, 6, 4, 7], [-np.inf, np.nan, -0.5, -1.0], -3.0)
+
+
+# ---- equal totals ------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("K", [1, 2, 4, 7, 8, 16, 31, 32])
+@pytest.mark.parametrize("C", [1, 6, 64])
+@pytest.mark.parametrize("bonus", [0.0, -0.5, 0.25])
+def test_search_ties(K, C, bonus):
+    """Equal totals go by their order: beams that stay, then grown ones by beam and class.  Every frame has
+    classes of its own and scores of a few halves, so that all sums are exact."""
+    say("ties", K, C, bonus)
+    parts = []
+    for seed, T in ((1, 1), (2, 3), (3, 12), (4, 12)):
+        r = np.random.default_rng(seed + K)
+        ids = 1 + np.arange(T * C, dtype=np.int32).reshape(T, C)
+        lp = -np.sort(r.integers(1, 4, size=(T, C)) / 2.0, 1).astype(np.float32)
+        parts.append((ids, lp, -(r.integers(1, 4, size=T) / 2.0).astype(np.float32)))
+    got = run_search(parts, K, bonus)
+    for n, q in enumerate(parts):
+        check_result(got, n, ref.Search(K, bonus).run(*q).result(), len(q[2]), tol=0.0)
