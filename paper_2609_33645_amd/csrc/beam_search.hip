@@ -45,7 +45,7 @@ constexpr float kNegInf = -INFINITY;
 constexpr int kBufWord3 = 0x00020000;  // word 3 of a raw buffer resource: 32-bit data, no swizzle
 constexpr int kCkStep = 16;  // labels between two nodes that remember the one before (result kernel)
 
-constexpr float kLow = -1e30f;  // a reference that stays finite where all masses are zero
+constexpr float kLow = -3.4028235e38f;  // float's lowest: a reference that stays finite where all masses are zero
 
 // Sums of two and of three masses; -inf where all are zero.
 __device__ __forceinline__ float log_add(float a, float b) {

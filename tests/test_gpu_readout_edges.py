@@ -84,3 +84,23 @@ def test_search_ties(K, C, bonus):
     got = run_search(parts, K, bonus)
     for n, q in enumerate(parts):
         check_result(got, n, ref.Search(K, bonus).run(*q).result(), len(q[2]), tol=0.0)
+
+
+# ---- scores near float's lowest value ------------------------------------------------------------
+
+def test_search_scores_near_the_lowest_value():
+    """Masks of large finite scores: a total far below any other is still above -inf, and its prefix stays, also
+    where masses are added (a beam's last label is offered).  Every sum has one term above the others' last bits."""
+    f = np.float32
+    low = float(np.finfo(f).min)
+
+    def one(K, rows):
+        ids, lp, bl = (np.array([r[i] for r in rows], d) for i, d in ((0, np.int32), (1, f), (2, f)))
+        want = ref.Search(K).run(ids, lp.astype(np.float64), bl.astype(np.float64)).result()
+        got = run_search([(ids, lp, bl)], K)
+        check_result(got, 0, want, len(rows), tol=1e-6 * max(1.0, *(abs(s) for _, s in want)))
+    one(1, [([5], [-0.5], -50.0), ([5], [-2e38], -3e38)])             # its label, then blank far below
+    one(1, [([5], [-0.5], -50.0), ([5], [-3e38], -2e38)])             # the other way
+    one(1, [([5], [-0.5], -50.0), ([5], [low], low), ([5], [-1.0], -9.0)])
+    one(2, [([5, 6], [-1.0, -1e31], -1e33), ([5, 6], [-1e32, -2e35], -3e34)])
+    one(4, [([5, 6], [-1.0, -1e33], -1e31), ([5, 6], [-0.5, -1e36], -1e34)])
