@@ -401,7 +401,9 @@ size_t pctc_frame_candidates_pass(pctc_dtype dtype, int32_t M, int32_t D, int32_
  * first max_tokens of a longer one), token_lengths device int32 [N, K] (-1: no prefix), scores device
  * float [N, K] (total log mass with the bonuses; -inf: no prefix).  The state stays as it is.
  * N = 0 is allowed.  All three are asynchronous; they copy nothing from host memory to the device (lengths
- * go as kernel arguments), so a captured graph replays them with the lengths of the capture. */
+ * go as kernel arguments), so a captured graph replays them with the lengths of the capture: an advance belongs
+ * at the frames_done of its capture, and a replay elsewhere leaves unspecified labels.  A replay counts no
+ * frames on the host. */
 size_t pctc_beam_state_bytes(int32_t N, int32_t K, int32_t max_frames);
 int32_t pctc_beam_reset(int32_t N, int32_t K, int32_t max_frames, void* state, size_t state_bytes, void* stream);
 int32_t pctc_beam_advance(const int32_t* ids, const float* logp, const float* blank_logp, int32_t C,

@@ -581,14 +581,17 @@ beam_advance_kernel(FrameRows rows, int n0, int K, int C, bool fresh_start, cons
 // first, a load behind a load; the nodes at multiples of kCkStep labels are visited first, and from
 // each a lane of its own walks the kCkStep labels before it.  Bound by those loads, len / kCkStep + kCkStep
 // behind one another: prefixes of up to 190 labels 16.5 us, 60 labels 11.5 (with steps of 32 labels 20 and 17).
+// Lengths and nodes are held to the state's bounds: an advance that was captured at one position and replayed at
+// another writes over nodes in use, and a prefix's nodes may then end before its labels do.
 __global__ void __launch_bounds__(64)
-beam_result_kernel(BeamFields f, int K, int max_tokens, int32_t* __restrict__ tokens, int32_t* __restrict__ lengths,
+beam_result_kernel(BeamFields f, int K, int max_frames, int max_tokens, int32_t* __restrict__ tokens, int32_t* __restrict__ lengths,
                    float* __restrict__ scores) {
   __shared__ int32_t start[64];
   const int lane = threadIdx.x;
   const int64_t at = blockIdx.x;
   const int n = static_cast<int>(at / K);
-  const int len = f.len[at];
+  const int len = min(f.len[at], max_frames);
+  const uint32_t last_node = static_cast<uint32_t>(f.cap) - 1;  // (there are some where a prefix has labels)
   const int2* const nodes = f.nodes + n * f.cap;
   const int32_t* const cks = f.cks + n * f.cap;
   int32_t* const out = tokens + at * max_tokens;
@@ -606,7 +609,7 @@ beam_result_kernel(BeamFields f, int K, int max_tokens, int32_t* __restrict__ to
     if (lane == 0) {
       for (int q = 0; q < here; ++q) {
         start[q] = next;
-        next = cks[next];
+        next = cks[min(static_cast<uint32_t>(next), last_node)];
       }
     }
     __syncthreads();
@@ -621,7 +624,7 @@ beam_result_kernel(BeamFields f, int K, int max_tokens, int32_t* __restrict__ to
       to = whole * kCkStep;
     }
     for (int t = from - 1; t >= to; --t) {
-      const int2 v = nodes[node];
+      const int2 v = nodes[min(static_cast<uint32_t>(node), last_node)];
       if (t < max_tokens) out[t] = v.y;
       node = v.x;
     }
@@ -750,7 +753,7 @@ hipError_t launch_beam_result(void* state, int N, int K, int max_frames, int max
   if (N <= 0) return hipSuccess;
   Prof pr("beam_result", stream);
   hipLaunchKernelGGL(beam_result_kernel, dim3(static_cast<unsigned>(N * K)), dim3(64), 0, stream,
-                     beam_fields(state, N, K, max_frames), K, max_tokens, tokens, lengths, scores);
+                     beam_fields(state, N, K, max_frames), K, max_frames, max_tokens, tokens, lengths, scores);
   return hipGetLastError();
 }
 

@@ -684,7 +684,10 @@ class BeamSearch:
 
     max_frames bounds the frames an utterance may have in all (memory: 12 bytes a frame and
     beam).  token_bonus is added to a prefix's score per label (negative: a penalty).  Calls are
-    asynchronous on the current stream (or `stream`), and one search's calls belong on one stream."""
+    asynchronous on the current stream (or `stream`), and one search's calls belong on one stream.
+
+    In a captured graph an advance stays bound to the position of its capture (frames_done counts
+    there, not at replays): capture one for each, and give result its max_tokens."""
 
     @_asynchronous
     def __init__(self, N: int, beam_size: int, max_frames: int, token_bonus: float = 0.0, device=None, *, stream=None):

@@ -104,3 +104,49 @@ def test_search_scores_near_the_lowest_value():
     one(1, [([5], [-0.5], -50.0), ([5], [low], low), ([5], [-1.0], -9.0)])
     one(2, [([5, 6], [-1.0, -1e31], -1e33), ([5, 6], [-1e32, -2e35], -3e34)])
     one(4, [([5, 6], [-1.0, -1e33], -1e31), ([5, 6], [-0.5, -1e36], -1e34)])
+
+
+# ---- replays -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("K", [2, 4])
+def test_result_after_replays_at_another_position(K):
+    """One captured advance replayed frame after frame writes over its own nodes: the labels are unspecified, but
+    the lengths stay in bounds, nothing outside the state is read, and a reset makes the search right again."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    say("replays", K)
+    N, C, T = 3, 6, 50
+    parts = [random_frames(70 + n, T, C, 9) for n in range(N)]
+    frames = [torch.from_numpy(np.stack([q[i] for q in parts], 1)).cuda() for i in range(3)]
+    now = [f[0].clone() for f in frames]
+    b = pc.BeamSearch(N, K, T)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.advance(*now, [1] * N)
+    for t in range(T):
+        for x, f in zip(now, frames):
+            x.copy_(f[t])
+        graph.replay()
+        torch.cuda.synchronize()
+    r = b.result(T)
+    lengths = r["token_lengths"].cpu().numpy()
+    assert lengths.min() >= -1 and lengths.max() <= T
+    past = np.arange(T)[None, None, :] >= lengths[:, :, None]
+    assert (r["tokens"].cpu().numpy()[past] == -1).all()
+    b.reset()
+    b.advance(*(torch.cat([f[:, n] for n in range(N)]) for f in frames), [T] * N)
+    got = {k: v.cpu().numpy() for k, v in b.result(T).items()}
+    want = run_search(parts, K)
+    assert all(np.array_equal(got[k], want[k]) for k in want)
+    # more replays than the state has room for frames
+    small = pc.BeamSearch(N, K, 5)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        small.advance(*now, [1] * N)
+    for t in range(T):
+        for x, f in zip(now, frames):
+            x.copy_(f[t])
+        graph.replay()
+        torch.cuda.synchronize()
+    assert int(small.result(5)["token_lengths"].max()) <= 5
