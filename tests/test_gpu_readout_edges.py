@@ -150,3 +150,17 @@ def test_result_after_replays_at_another_position(K):
         graph.replay()
         torch.cuda.synchronize()
     assert int(small.result(5)["token_lengths"].max()) <= 5
+
+
+def test_long_prefix_cut_at_segments():
+    """The labels hang together in segments of 16: cuts on both sides of a segment's edge, and of 63 segments'."""
+    T = 1100
+    path = np.random.default_rng(1).integers(1, 500, size=T) * 2
+    path[1:] += (path[1:] == path[:-1])
+    ids = np.stack([path, path + 2000], 1).astype(np.int32)
+    lp = np.tile(np.array([[-0.01, -9.0]], np.float32), (T, 1))
+    bl = np.full(T, -12.0, np.float32)
+    for n in (15, 16, 17, 1007, 1008, 1009, 1100):
+        for cut in sorted({min(n, c) for c in (15, 16, 17, 1008, n)}):
+            got = run_search([(ids[:n], lp[:n], bl[:n])], 1, max_frames=T, max_tokens=cut)
+            assert got["tokens"][0, 0].tolist() == path[:cut].tolist() and got["token_lengths"][0, 0] == n
