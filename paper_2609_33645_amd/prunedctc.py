@@ -11,8 +11,9 @@ import ctypes
 import functools
 import math
 import os
+import threading
 from array import array
-from typing import Dict, Optional, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 import torch
@@ -605,17 +606,31 @@ def grouped_head(H: torch.Tensor, W: torch.Tensor, u_ids: torch.Tensor, bias: Op
 
 # ---- readout with beams ------------------------------------------------------------------
 
+_given: List[int] = []  # the threads whose running call was given a stream
+_moved: Dict[int, int] = {}  # by thread: the device that was current before its running call made another so
+_current_device = torch._C._cuda_getDevice  # (without the checks of torch.cuda.current_device)
+
+
 def _asynchronous(fn):
     """For calls that return before the device is done: with stream=..., the whole call, its
     allocations among it, is made on that stream, so that memory it lets go of is not handed out
     to another stream while the kernels still use it; nor is that of the caller's tensors.  What
-    another stream writes into them the caller waits for."""
+    another stream writes into them the caller waits for.  Kernels go to the device of the tensors,
+    whichever is current (see _raw_stream); `stream` must be one of it."""
     @functools.wraps(fn)
     def call(*args, stream=None, **kw):
         if stream is None:
-            return fn(*args, **kw)
-        with torch.cuda.stream(stream):
-            result = fn(*args, **kw)
+            try:
+                return fn(*args, **kw)
+            finally:
+                if _moved and threading.get_ident() in _moved:
+                    torch.cuda.set_device(_moved.pop(threading.get_ident()))
+        _given.append(threading.get_ident())
+        try:
+            with torch.cuda.stream(stream):
+                result = fn(*args, **kw)
+        finally:
+            _given.remove(threading.get_ident())
         for arg in (*args, *kw.values()):
             for t in arg if isinstance(arg, (list, tuple)) else (arg,):
                 if isinstance(t, torch.Tensor) and t.is_cuda:
@@ -625,8 +640,16 @@ def _asynchronous(fn):
 
 
 def _raw_stream(dev: torch.device) -> int:
-    """The current stream's handle (without the stream object that current_stream makes, 2 us)."""
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+    """The handle of dev's current stream (without the stream object that current_stream makes, 2 us),
+    for an _asynchronous call's launch.  A default stream's is the same on every device, and kernels go to
+    the current device's: dev becomes the current one until the call is over."""
+    index = dev.index
+    if _current_device() != index:
+        if threading.get_ident() in _given:
+            raise PrunedCTCError(-1, f"stream must be one of {dev}, where the tensors are")
+        _moved[threading.get_ident()] = torch.cuda.current_device()
+        torch.cuda.set_device(index)
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _scratch(nbytes: int, dev: torch.device) -> torch.Tensor:
@@ -694,6 +717,8 @@ class BeamSearch:
         self.N, self.beam_size, self.max_frames = int(N), int(beam_size), int(max_frames)
         self.token_bonus = float(token_bonus)
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+        if self.device.type != "cuda":
+            raise PrunedCTCError(-1, "a search runs on a GPU")
         nbytes = int(lib().pctc_beam_state_bytes(self.N, self.beam_size, self.max_frames))
         if nbytes == 0:
             _check(-1, "pctc_beam_state_bytes")
