@@ -13,6 +13,7 @@ import math
 import os
 import threading
 from array import array
+from collections.abc import Iterable
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -611,6 +612,12 @@ _moved: Dict[int, int] = {}  # by thread: the device that was current before its
 _current_device = torch._C._cuda_getDevice  # (without the checks of torch.cuda.current_device)
 
 
+def _sequence(x):
+    """A tuple in the place of an iterable that could only be gone through once or is no plain sequence."""
+    plain = isinstance(x, (torch.Tensor, np.ndarray, list, tuple, str, array)) or not isinstance(x, Iterable)
+    return x if plain else tuple(x)
+
+
 def _asynchronous(fn):
     """For calls that return before the device is done: with stream=..., the whole call, its
     allocations among it, is made on that stream, so that memory it lets go of is not handed out
@@ -625,6 +632,7 @@ def _asynchronous(fn):
             finally:
                 if _moved and threading.get_ident() in _moved:
                     torch.cuda.set_device(_moved.pop(threading.get_ident()))
+        args, kw = [_sequence(x) for x in args], {k: _sequence(x) for k, x in kw.items()}
         _given.append(threading.get_ident())
         try:
             with torch.cuda.stream(stream):
@@ -632,7 +640,7 @@ def _asynchronous(fn):
         finally:
             _given.remove(threading.get_ident())
         for arg in (*args, *kw.values()):
-            for t in arg if isinstance(arg, (list, tuple)) else (arg,):
+            for t in arg if isinstance(arg, (list, tuple)) else (getattr(arg, "_state", arg),):  # (a search's)
                 if isinstance(t, torch.Tensor) and t.is_cuda:
                     t.record_stream(stream)
         return result

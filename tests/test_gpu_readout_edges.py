@@ -164,3 +164,37 @@ def test_long_prefix_cut_at_segments():
         for cut in sorted({min(n, c) for c in (15, 16, 17, 1008, n)}):
             got = run_search([(ids[:n], lp[:n], bl[:n])], 1, max_frames=T, max_tokens=cut)
             assert got["tokens"][0, 0].tolist() == path[:cut].tolist() and got["token_lengths"][0, 0] == n
+
+
+# ---- other streams -------------------------------------------------------------------------------
+
+def test_other_stream_keeps_a_search_and_iterators_tensors():
+    """A search let go of right after its calls on a busy stream, and gradients that came as an iterator: their
+    memory, asked for again on the current stream, is not handed out before the work is done."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    parts = [random_frames(n, 40, 6, 9) for n in range(4)]
+    want = run_search(parts, 8, max_frames=40, max_tokens=40)
+    cat = [torch.from_numpy(np.concatenate([q[i] for q in parts])).cuda() for i in range(3)]
+    grads = [torch.randn(300_000, device="cuda") for _ in range(3)]
+    norm = pc.clip_grad_norm(grads, 1.0, out=[torch.empty_like(g) for g in grads])["norm"].clone()
+    a = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        b, gs = pc.BeamSearch(4, 8, 40), [g.clone() for g in grads]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                torch.mm(a, a)
+        b.advance(*cat, [40] * 4, stream=side)
+        got = b.result(40, stream=side)
+        clipped = pc.clip_grad_norm((g for g in gs), 1.0, out=(torch.empty_like(g) for g in grads), stream=side)
+        nbytes = b._state.untyped_storage().nbytes()
+        del b, gs
+        junk = [torch.full((nbytes,), 7, dtype=torch.uint8, device="cuda"),
+                *(torch.full((300_000,), 7.0, device="cuda") for _ in range(3))]
+        torch.cuda.synchronize()
+        assert all(np.array_equal(want[k], got[k].cpu().numpy()) for k in want)
+        assert torch.equal(clipped["norm"], norm)
+        del junk

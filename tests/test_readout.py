@@ -1,5 +1,6 @@
 """Readout with beams and gradient clipping, without a GPU: the 64-bit reference search against
 enumeration of all alignments, and the library's host-side argument checks and sizes."""
+import contextlib
 import ctypes
 import itertools
 import math
@@ -299,3 +300,38 @@ def test_search_on_no_gpu_is_refused():
     with pytest.raises(pc.PrunedCTCError) as e:
         pc.BeamSearch(1, 4, 10, device="cpu")
     assert e.value.code == -1
+
+
+def test_tensors_of_a_call_on_a_stream_are_kept(monkeypatch):
+    """Every device tensor that a call on a given stream works on is told to the allocator: single ones, those
+    of lists, of iterables of any kind (which the call still gets whole), and a search's own state."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+
+    class Device(torch.Tensor):
+        is_cuda = True
+
+        def record_stream(self, stream):
+            kept.append((self.mark, stream))
+
+    class Holder:
+        pass
+
+    def tensor(mark):
+        t = torch.zeros(1).as_subclass(Device)
+        t.mark = mark
+        return t
+    kept, seen = [], []
+    monkeypatch.setattr(torch.cuda, "stream", contextlib.nullcontext)
+
+    @pc._asynchronous
+    def call(*args, **kw):
+        seen.extend(len(list(a)) for a in args if not isinstance(a, Holder))
+    one, search = tensor(0), Holder()
+    search._state = tensor(1)
+    listed = {2: tensor(2), 3: tensor(3)}
+    call(search, one, [tensor(4)], (tensor(5),), listed.values(), (tensor(k) for k in (6, 7)), iter([tensor(8)]),
+         out=iter([tensor(9)]), stream="side")
+    assert sorted(k for k, _ in kept) == list(range(10)) and {s for _, s in kept} == {"side"}
+    assert seen == [1, 1, 1, 2, 2, 1]
