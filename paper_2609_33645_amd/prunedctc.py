@@ -666,6 +666,23 @@ def _scratch(nbytes: int, dev: torch.device) -> torch.Tensor:
     return t if t.data_ptr() % 256 == 0 else _workspace(nbytes, dev)
 
 
+_I32 = np.dtype(np.int32)
+
+
+def _counts(x):
+    """Numbers of frames as an array of int32: whole numbers that it holds, nothing cut off."""
+    if isinstance(x, torch.Tensor):
+        x = x.detach().cpu().numpy()
+    if isinstance(x, np.ndarray):
+        x = x.tolist()
+    try:
+        return array("i", x)
+    except TypeError:
+        raise PrunedCTCError(-1, "numbers of frames must be whole numbers, one for each utterance") from None
+    except OverflowError:
+        raise PrunedCTCError(-3, "more frames than an utterance can have") from None
+
+
 def _as(t: torch.Tensor, dtype: torch.dtype) -> torch.Tensor:
     return t if t.dtype is dtype and t.is_contiguous() else t.to(dtype).contiguous()
 
@@ -762,13 +779,14 @@ class BeamSearch:
         your own); places with an id below 0 or a score of -inf or NaN, anywhere in a row, are left out.
         Returns parents [N, beam_size] (int32): the beam before the call that each beam descends from,
         -1 where there is no prefix (for beam_reorder)."""
-        if isinstance(frames, torch.Tensor):
-            frames = frames.detach().cpu().numpy()
+        # (a live stream calls this every frame: an array of int32 is taken without a look at its values, a dot
+        # product takes half of a sum, empty_like of empty)
+        if type(frames) is not np.ndarray or frames.dtype is not _I32:
+            frames = _counts(frames)
         if len(frames) != self.N:
             raise PrunedCTCError(-1, f"frames must have {self.N} entries")
         fr = self._frames
         fr[:self.N] = frames
-        # (a live stream calls this every frame: a dot product takes half of a sum, empty_like of empty)
         M, shape, dev = int(fr.dot(self._ones)), logp.shape, self.device
         if len(shape) != 2 or shape[0] != M or ids.shape != shape or blank_logp.shape != (M,):
             raise PrunedCTCError(-1, f"ids and logp must be [{M}, C] and blank_logp [{M}]")
@@ -851,7 +869,7 @@ def beam_decode(H: torch.Tensor, W: torch.Tensor, input_lengths, beam_size: int 
     frame_candidates).  Asynchronous."""
     L = lib()
     H, W, bias, dt = _head_args(H, W, bias)
-    T = _host_i32(input_lengths)
+    T = np.array(_counts(input_lengths), np.int32)
     N, (M, D), V, K, C, dev = int(T.size), H.shape, int(W.shape[0]), int(beam_size), int(candidates), H.device
     if int(T.sum(dtype=np.int64)) != M:
         raise PrunedCTCError(-1, "sum of input lengths differs from the rows of H")

@@ -198,3 +198,32 @@ def test_other_stream_keeps_a_search_and_iterators_tensors():
         assert all(np.array_equal(want[k], got[k].cpu().numpy()) for k in want)
         assert torch.equal(clipped["norm"], norm)
         del junk
+
+
+# ---- numbers of frames ---------------------------------------------------------------------------
+
+def test_numbers_of_frames_that_no_call_takes():
+    """Numbers that are not whole, or that int32 does not hold, are refused where they would have been cut off to
+    numbers that fit the candidates."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    ids, lp, bl = (torch.from_numpy(x).cuda() for x in random_frames(1, 3, 4, 6))
+    b = pc.BeamSearch(2, 4, 10)
+    for frames, code in (([1.7, 2.0], -1), ([2 ** 32 + 1, 2], -3), (np.array([2 ** 32 + 1, 2]), -3),
+                         (torch.tensor([1.0, 2.0]), -1), ([1, 2, 0], -1), ([-1, 4], -3), (np.array([1.0, 2.0]), -1)):
+        with pytest.raises(pc.PrunedCTCError) as e:
+            b.advance(ids, lp, bl, frames)
+        assert e.value.code == code, frames
+    assert b.frames_done.tolist() == [0, 0]
+    first = b.advance(ids, lp, bl, [1, 2])
+    for frames in ((1, 2), np.array([1, 2]), torch.tensor([1, 2], device="cuda"), np.array([1, 2], np.int32)):
+        b.reset()
+        assert torch.equal(b.advance(ids, lp, bl, frames), first) and b.frames_done.tolist() == [1, 2]
+    H, W = torch.randn(3, 64, device="cuda"), torch.randn(9, 64, device="cuda")
+    for lengths, code in (([1.5, 2.9], -1), (np.array([2 ** 32 + 1, 2]), -3), ([0, 3], -3), ([3, 1], -1)):
+        with pytest.raises(pc.PrunedCTCError) as e:
+            pc.beam_decode(H, W, lengths)
+        assert e.value.code == code, lengths
+    for lengths in ([1, 2], torch.tensor([1, 2])):
+        assert pc.beam_decode(H, W, lengths)["token_lengths"].shape == (2, 8)

@@ -335,3 +335,23 @@ def test_tensors_of_a_call_on_a_stream_are_kept(monkeypatch):
          out=iter([tensor(9)]), stream="side")
     assert sorted(k for k, _ in kept) == list(range(10)) and {s for _, s in kept} == {"side"}
     assert seen == [1, 1, 1, 2, 2, 1]
+
+
+def test_numbers_of_frames_are_taken_as_they_are():
+    """Whole numbers of any integer type and container; a number that int32 does not hold, or that is no whole
+    one, is refused and not cut off."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    for x in ([3, 0, 7], (3, 0, 7), np.array([3, 0, 7]), np.array([3, 0, 7], np.int32), np.array([3, 0, 7], np.uint8),
+              torch.tensor([3, 0, 7]), [np.int64(3), np.int32(0), 7], np.array([[3, 0, 7]] * 2, np.int32).T[:, 0],
+              np.array([3, 9, 0, 9, 7], np.int32)[::2]):
+        assert list(pc._counts(x)) == [3, 0, 7]
+    assert len(pc._counts([])) == 0 and len(pc._counts(np.zeros(0))) == 0
+    assert list(pc._counts([-1])) == [-1]  # (refused where lengths are)
+    for x, code in (([1.7], -1), (np.array([2.0]), -1), (torch.tensor([1.0]), -1), ([2 ** 32], -3), ([2 ** 31], -3),
+                    (np.array([2 ** 32 + 1]), -3), (torch.tensor([2 ** 40]), -3), (5, -1), (None, -1), ([None], -1),
+                    (np.array([[1], [2]], np.int32), -1), (np.int32(4), -1)):
+        with pytest.raises(pc.PrunedCTCError) as e:
+            pc._counts(x)
+        assert e.value.code == code, x
