@@ -438,7 +438,9 @@ int32_t pctc_beam_decode(pctc_dtype dtype, const void* H, int32_t D, const void*
  *   out_i = s grads_i, rounded once to the tensor's type
  * grads, out: HOST arrays of ntensors device pointers; out NULL: in place (nothing is written where s
  * is 1).  n: HOST, values of each tensor (0 .. 2^34); dtypes: HOST, PCTC_F32 or PCTC_BF16; pointers
- * aligned to their type.  max_norm >= 0 (+inf: the norm alone, and copies).  Squares are summed in
+ * aligned to their type.  An out_i may be grads_i itself; other overlaps of what is written, with another
+ * out_j or grads_j (in place: of two gradients), are PCTC_EINVAL.  max_norm >= 0 (+inf: the norm alone, and
+ * copies; in place nothing is written then).  Squares are summed in
  * double, in an order that depends on the sizes only.  norm: device float [1]; scale: device float [1] or
  * NULL.  A norm that is not finite is reported as it is and scales by 1.
  * workspace: pctc_clip_workspace_size(ntensors) bytes, 256-byte aligned.  Asynchronous. */

@@ -7,7 +7,9 @@
 #include <algorithm>
 #include <functional>
 #include <map>
+#include <memory>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -365,6 +367,48 @@ static bool lattice_leads(const DpPlan& dp, int t_max, int D, int V) {
 }  // namespace pctc
 
 using namespace pctc;
+
+namespace {
+// Whether a list's call would write memory that it reads or writes for another tensor too, where the order would
+// decide: written ranges of bytes that meet, or one that meets another tensor's input.  out null: written are the
+// inputs.  1 yes, 0 no, -1 no host memory.  Lists in the order of their addresses, as views into flat buffers
+// are, are not sorted first.
+template <class Bytes>
+int lists_overlap(int32_t n, const void* const* in, void* const* out, const Bytes& bytes) {
+  struct Range {
+    uintptr_t at, end;
+    int32_t of;
+  };
+  auto before = [](const Range& a, const Range& b) { return a.at < b.at; };
+  auto collect = [&](const void* const* p, std::unique_ptr<Range[]>& r) {
+    r.reset(new (std::nothrow) Range[n]);
+    if (!r) return -1;
+    int32_t m = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(p[i]);
+      if (const uintptr_t b = bytes(i)) r[m++] = Range{at, at + b, i};
+    }
+    if (!std::is_sorted(r.get(), r.get() + m, before)) std::sort(r.get(), r.get() + m, before);
+    return m;
+  };
+  if (n < 1 || (n < 2 && !out)) return 0;
+  std::unique_ptr<Range[]> w, r;
+  const int32_t nw = collect(out ? out : in, w);
+  if (nw < 0) return -1;
+  for (int32_t i = 1; i < nw; ++i)
+    if (w[i].at < w[i - 1].end) return 1;
+  if (!out) return 0;
+  const int32_t nr = collect(in, r);
+  if (nr < 0) return -1;
+  // the written ranges fall apart, so their ends are in order too; inputs may meet one another
+  for (int32_t i = 0, j = 0; i < nr; ++i) {
+    while (j < nw && w[j].end <= r[i].at) ++j;
+    for (int32_t k = j; k < nw && w[k].at < r[i].end; ++k)
+      if (w[k].of != r[i].of || w[k].at != r[i].at) return 1;
+  }
+  return 0;
+}
+}  // namespace
 
 extern "C" {
 
@@ -1151,6 +1195,12 @@ int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* co
     if (n[i] > 0 && (!grads[i] || (out && !out[i]))) return PCTC_EINVAL;
     if ((reinterpret_cast<uintptr_t>(grads[i]) & mask) || (out && (reinterpret_cast<uintptr_t>(out[i]) & mask)))
       return PCTC_EINVAL;
+  }
+  if (out || max_norm < INFINITY) {  // (else nothing is written)
+    const int over = lists_overlap(ntensors, grads, out, [&](int32_t i) {
+      return static_cast<uintptr_t>(n[i]) * (dtypes[i] == PCTC_F32 ? 4 : 2);
+    });
+    if (over != 0) return over > 0 ? PCTC_EINVAL : PCTC_EWORKSPACE;
   }
   if (!workspace || workspace_bytes < clip_workspace_bytes(ntensors)) return PCTC_EWORKSPACE;
   if (misaligned256(workspace)) return PCTC_EINVAL;

@@ -355,3 +355,49 @@ def test_numbers_of_frames_are_taken_as_they_are():
         with pytest.raises(pc.PrunedCTCError) as e:
             pc._counts(x)
         assert e.value.code == code, x
+
+
+@built
+def test_clip_refuses_overlaps():
+    """Memory that would be written beside another reader or writer of the list is refused before any work;
+    the calls that are in order get as far as their missing workspace."""
+    L = _lib()
+
+    def call(grads, n, out=None, dtypes=None, max_norm=1.0):
+        vp = lambda xs: (ctypes.c_void_p * len(xs))(*xs)  # noqa: E731
+        k = len(grads)
+        return L.pctc_clip_grad_norm(k, vp(grads), None if out is None else vp(out), (ctypes.c_int64 * k)(*n),
+                                     (ctypes.c_int32 * k)(*(dtypes or [0] * k)), max_norm, OK, None, None, 0, None)
+    A, B, C = OK, OK + 400, OK + 800  # 100 float32 values apart
+    fine, refused = -4, -1
+    assert call([A, B, C], [100, 100, 100]) == fine and call([C, A, B], [100, 100, 100]) == fine
+    assert call([A], [100]) == fine and call([A, A], [100, 0]) == fine and call([A, None], [100, 0]) == fine
+    assert call([A, B, A], [100, 100, 100]) == refused  # the same gradient twice
+    assert call([C, A, B], [100, 101, 100]) == refused and call([B, A], [50, 100 + 1]) == refused
+    assert call([A, A + 200], [100, 100], dtypes=[1, 1]) == fine and call([A, A + 200], [101, 100], dtypes=[1, 1]) == refused
+    assert call([A, A], [100, 100], max_norm=math.inf) == fine  # nothing is written
+    # other tensors to write to
+    D, E, F = OK + 4000, OK + 4400, OK + 4800
+    assert call([A, A, B], [100, 100, 100], out=[D, E, F]) == fine  # read twice, written apart
+    assert call([A, B, C], [100] * 3, out=[A, B, C]) == fine and call([C, A, B], [100] * 3, out=[C, A, B]) == fine
+    assert call([A, B, C], [100] * 3, out=[F, B, D]) == fine
+    for out in ([D, D, F], [D, D + 4, F], [B, A, C], [A + 4, D, E], [D, E, A], [D, E, C + 396], [D, E, A + 796]):
+        assert call([A, B, C], [100] * 3, out=out) == refused, out
+    assert call([A], [100], out=[A + 4]) == refused and call([A], [100], out=[A]) == fine
+    assert call([A, B], [100, 100], out=[D, D], max_norm=math.inf) == refused  # copies are written
+    # against a plain search of all pairs
+    rng = np.random.default_rng(0)
+    seen = set()
+    for _ in range(4000):
+        k = int(rng.integers(1, 5))
+        n = rng.integers(0, 4, size=k)
+        g = rng.integers(0, 24, size=k)
+        o = None if rng.random() < 0.4 else np.where(rng.random(k) < 0.3, g, rng.integers(0, 24, size=k))
+        w = g if o is None else o
+        meet = lambda a, b, i, j: a < b + n[j] and b < a + n[i] and n[i] > 0 and n[j] > 0  # noqa: E731
+        bad = any(meet(w[i], w[j], i, j) for i in range(k) for j in range(i)) or (
+            o is not None and any(meet(o[i], g[j], i, j) and (i != j or o[i] != g[j]) for i in range(k) for j in range(k)))
+        seen.add(bad)
+        got = call([OK + 4 * int(x) for x in g], n.tolist(), None if o is None else [OK + 4 * int(x) for x in o])
+        assert got == (refused if bad else fine), (n, g, o)
+    assert seen == {False, True}
