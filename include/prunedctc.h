@@ -416,7 +416,8 @@ int32_t pctc_beam_result(int32_t N, int32_t K, int32_t max_frames, const void* s
  * out_i[n][k] = in_i[n][parents[n][k]] for each of ntensors contiguous device buffers [N, K, ...] of
  * beam_bytes[i] bytes per beam (any size and alignment, at most 2^36).  A parent outside [0, K) leaves
  * the beam's own state.  in, out, beam_bytes: HOST arrays; out NULL (or out[i] == in[i]): in place; other
- * overlaps are not allowed.  parents: device int32 [N, K].  1 <= K <= PCTC_MAX_BEAMS.  Asynchronous. */
+ * overlaps of what is written, with another out[j] or in[j] (in place: of two states), are PCTC_EINVAL.
+ * parents: device int32 [N, K].  1 <= K <= PCTC_MAX_BEAMS.  Asynchronous. */
 int32_t pctc_beam_reorder(int32_t ntensors, const void* const* in, void* const* out, const int64_t* beam_bytes,
                           const int32_t* parents, int32_t N, int32_t K, void* stream);
 

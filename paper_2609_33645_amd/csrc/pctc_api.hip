@@ -1109,6 +1109,10 @@ int32_t pctc_beam_reorder(int32_t ntensors, const void* const* in, void* const* 
   }
   if (N == 0 || !any) return PCTC_OK;
   if (!parents) return PCTC_EINVAL;
+  const int over = lists_overlap(ntensors, in, out, [&](int32_t i) {
+    return static_cast<uintptr_t>(beam_bytes[i]) * (static_cast<uintptr_t>(N) * K);
+  });
+  if (over != 0) return over > 0 ? PCTC_EINVAL : PCTC_EWORKSPACE;
   PCTC_HIP(launch_beam_reorder(ntensors, in, out, beam_bytes, parents, N, K, static_cast<hipStream_t>(stream_ptr)));
   prof_flush();
   return PCTC_OK;

@@ -831,7 +831,8 @@ def beam_reorder(states: Sequence[torch.Tensor], parents: torch.Tensor, out: Opt
                  *, stream=None):
     """Per-beam state tensors [N, K, ...] of any type in the order of the surviving beams: state[n, k]
     becomes state[n, parents[n, k]] (a parent outside [0, K) leaves it).  In place, or into the
-    tensors `out`; returns those written.  Tensors must be contiguous."""
+    tensors `out`; returns those written.  Tensors must be contiguous, and what is written must not
+    overlap another tensor of the call (in place: no state twice in the list)."""
     dev = parents.device
     if parents.dim() != 2 or parents.dtype is not torch.int32 or not parents.is_cuda:
         raise PrunedCTCError(-1, "parents must be a device int32 [N, K]")

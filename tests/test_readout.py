@@ -401,3 +401,19 @@ def test_clip_refuses_overlaps():
         got = call([OK + 4 * int(x) for x in g], n.tolist(), None if o is None else [OK + 4 * int(x) for x in o])
         assert got == (refused if bad else fine), (n, g, o)
     assert seen == {False, True}
+
+
+@built
+def test_reorder_refuses_overlaps():
+    """A state twice in a list that is reordered in place, or an out that overlaps another tensor."""
+    L = _lib()
+
+    def refused(states, sizes, out=None):
+        vp = lambda xs: (ctypes.c_void_p * len(xs))(*xs)  # noqa: E731
+        k = len(states)
+        return L.pctc_beam_reorder(k, vp(states), None if out is None else vp(out), (ctypes.c_int64 * k)(*sizes), OK, 2, 4,
+                                   None) == -1
+    A, B, D = OK + 1024, OK + 1024 + 8 * 16, OK + 4096  # two states of 2 x 4 beams of 16 bytes, side by side
+    assert refused([A, A], [16, 16]) and refused([A, B], [17, 16]) and refused([B, A, B], [16, 16, 16])
+    assert refused([A, B], [16, 16], out=[D, D]) and refused([A, B], [16, 16], out=[D, D + 127])
+    assert refused([A, B], [16, 16], out=[B, A]) and refused([A], [16], out=[A + 1])
