@@ -354,10 +354,11 @@ int32_t pctc_grouped_backward(pctc_dtype dtype, const void* H, int32_t M, int32_
  *      among equal ones) and float(z - lambda); where fewer than C classes have a logit above -inf,
  *      the rest are -1 and -inf.  NaN or +inf logits give unspecified rows.
  * blank_logp  device float [M].
- * workspace: pctc_frame_candidates_workspace_size() bytes, 256-byte aligned; at most about 512 MiB
+ * workspace: pctc_frame_candidates_workspace_size() bytes, 256-byte aligned: at most about 512 MiB
  *      (per frame a value for each block of 8 classes, and the logits of a short vocabulary; more
- *      frames than fit take another pass over W) beside
- *      the normaliser's partial sums.  Returns 0 for invalid arguments.
+ *      frames than fit take another pass over W), and beside it for the frames of a pass the normaliser's
+ *      partial sums (2 KiB a frame; 8 KiB from D = 2048 on) and, for large bf16 products, H transposed (2 D
+ *      bytes a frame, below 2 GiB).  Returns 0 for invalid arguments.
  * Asynchronous. */
 size_t pctc_frame_candidates_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t C);
 int32_t pctc_frame_candidates(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W,
@@ -443,7 +444,8 @@ int32_t pctc_beam_decode(pctc_dtype dtype, const void* H, int32_t D, const void*
  * out_j or grads_j (in place: of two gradients), are PCTC_EINVAL.  max_norm >= 0 (+inf: the norm alone, and
  * copies; in place nothing is written then).  Squares are summed in
  * double, in an order that depends on the sizes only.  norm: device float [1]; scale: device float [1] or
- * NULL.  A norm that is not finite is reported as it is and scales by 1.
+ * NULL.  A norm that is not finite is reported as it is and scales by 1; that of finite values beyond float's
+ * range is reported as +inf, and clips.
  * workspace: pctc_clip_workspace_size(ntensors) bytes, 256-byte aligned.  Asynchronous. */
 size_t pctc_clip_workspace_size(int32_t ntensors);
 int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* const* out, const int64_t* n,

@@ -12,9 +12,9 @@
 // The K largest totals are kept, ties in the order: staying beams, then grown ones by (beam, class).
 //
 // What bounds it: a chain of dependent frames; memory and arithmetic are negligible.  16 utterances of 150 to
-// 348 frames, K = 8, C = 16: 190 us, 0.55 us a frame of the longest (4 beams and 8 classes 0.51, 16 beams and 40
-// classes 0.85; a frame of a live stream by itself, launch included, 3.5 us).  A frame is
-// some 170 instructions of a wavefront alone on its SIMD, 7.5 cycles each (plain additions take 4, comparisons
+// 348 frames, K = 8, C = 16: 186 us (the median of 60), 0.53 us a frame of the longest (4 beams and 8 classes
+// 0.54, 16 beams and 40 classes 0.83; a frame of a live stream by itself, launch included, 3.5 us).  A frame is
+// 172 instructions of a wavefront alone on its SIMD, 7.6 cycles each (plain additions take 4, comparisons
 // whose masks are used, cross-lane reads and branches more), and fewer instructions are what makes it faster:
 // with the exchanges through the LDS taken off the chain it was no faster.  Several
 // wavefronts to an utterance would wait at a barrier for each exchange.  One wavefront per

@@ -2,7 +2,8 @@
 //
 //   n = sqrt(sum over all values g^2),  s = min(1, max_norm / (n + 1e-6)),  g <- s g
 //
-// Squares are taken and summed in double: no square of a finite value overflows, and the order of
+// Squares are taken and summed in double: no square of a finite value overflows (a norm beyond float's range
+// is reported as infinite, and its double still clips), and the order of
 // the sums, fixed by the sizes alone, moves the float result by at most its last bit.  Bound by
 // memory: the values are read twice (the scale is known only after the last of them) and written once.
 // Three kernels: partial sums on a fixed grid, one workgroup that adds them up, and the scaling; for
@@ -23,9 +24,9 @@ constexpr int kGroup = 96;       // tensors of a launch: their table is a kernel
 constexpr int kMaxParts = 2048;  // workgroups (8 a compute unit) of a launch of the sums
 constexpr int kPartsBudget = 16384;
 // Bytes of a tensor that a workgroup takes at a time.  Scaling runs
-// best in short workgroups: 2.5 GB fp32 out of place, 4 KB each 765 us, 16 KB 838, on a fixed grid of 2,048
-// 931; but 600,000 workgroups that find nothing to do take 128 us, so in place, where a scale of 1 is
-// ordinary, each takes 32 KB (821 us; 4 KB 838).
+// best in short workgroups: 2.5 GB fp32 out of place, 4 KB each 813 us, 16 KB 857; but 600,000 workgroups
+// that find nothing to do take 134 us, so in place, where a scale of 1 is ordinary, each takes 32 KB (20 us
+// then, and 898 where it clips; 4 KB 813).
 constexpr int kSumBytes = kThreads * 8 * 16;
 constexpr int kOutBytes = kThreads * 16;
 constexpr int kInPlaceBytes = kThreads * 8 * 16;
@@ -34,7 +35,7 @@ constexpr int kNormThreads = 1024;
 // the norm is 4.4 more); at 32 MB 1,024 workgroups add up as many partial sums each.
 constexpr int64_t kShortBytes = int64_t{32} << 20;
 // Lists of this size are still cached (256 MB beside the memory) when they are read again, and are
-// loaded as usual; longer ones past the caches: 2.5 GB summed in 349 us, as usual 394.
+// loaded as usual; longer ones past the caches: 2.5 GB summed in 370 us, as usual 415.
 constexpr int64_t kCachedBytes = int64_t{192} << 20;
 
 struct ClipTable {

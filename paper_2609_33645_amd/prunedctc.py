@@ -902,7 +902,8 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional
                    *, stream=None) -> Dict[str, torch.Tensor]:
     """The global 2-norm over a list of float32 and bfloat16 gradients, and every gradient scaled by
     min(1, max_norm / (norm + 1e-6)), in place or into the tensors `out`.  Returns norm and scale
-    (float32 [1], on the device).  A norm that is not finite scales by 1: test it before the step.
+    (float32 [1], on the device).  A norm that is not finite scales by 1: test it before the step (one of
+    finite values beyond float32's range is reported as infinite too, but clips).
     Tensors must be contiguous, and what is written must not overlap another tensor of the call (in place: no
     gradient twice in the list, unless max_norm is infinite)."""
     grads = list(grads)
