@@ -381,8 +381,8 @@ size_t pctc_frame_candidates_pass(pctc_dtype dtype, int32_t M, int32_t D, int32_
  *              x = pb if c is y's last label, else s;
  * and the K largest pb' (+) pn' above -inf are kept, in falling order; equal ones: prefixes of the beam
  * first, then the others, by beam and then candidate.  Scores are held in float relative to the best
- * prefix, whose total is kept in double.  Prefixes are compared by length and a 64-bit hash of their
- * labels.
+ * prefix, whose total is kept in double (totals below float's range are -inf).  Prefixes are compared by
+ * length and a 64-bit hash of their labels.
  *
  * The state between frames is caller memory of pctc_beam_state_bytes(N, K, max_frames) bytes, 256-byte
  * aligned: it holds the beams and, for up to max_frames frames per utterance, K label records of 12 bytes
@@ -417,7 +417,8 @@ int32_t pctc_beam_result(int32_t N, int32_t K, int32_t max_frames, const void* s
  * out_i[n][k] = in_i[n][parents[n][k]] for each of ntensors contiguous device buffers [N, K, ...] of
  * beam_bytes[i] bytes per beam (any size and alignment, at most 2^36).  A parent outside [0, K) leaves
  * the beam's own state.  in, out, beam_bytes: HOST arrays; out NULL (or out[i] == in[i]): in place; other
- * overlaps of what is written, with another out[j] or in[j] (in place: of two states), are PCTC_EINVAL.
+ * overlaps of what is written, with another out[j] or in[j] (in place: of two states) or with parents, are
+ * PCTC_EINVAL.
  * parents: device int32 [N, K].  1 <= K <= PCTC_MAX_BEAMS.  Asynchronous. */
 int32_t pctc_beam_reorder(int32_t ntensors, const void* const* in, void* const* out, const int64_t* beam_bytes,
                           const int32_t* parents, int32_t N, int32_t K, void* stream);

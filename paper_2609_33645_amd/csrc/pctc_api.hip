@@ -1113,6 +1113,14 @@ int32_t pctc_beam_reorder(int32_t ntensors, const void* const* in, void* const* 
     return static_cast<uintptr_t>(beam_bytes[i]) * (static_cast<uintptr_t>(N) * K);
   });
   if (over != 0) return over > 0 ? PCTC_EINVAL : PCTC_EWORKSPACE;
+  // (the parents are read again between the writes)
+  const uintptr_t p0 = reinterpret_cast<uintptr_t>(parents), p1 = p0 + sizeof(int32_t) * N * K;
+  for (int i = 0; i < ntensors; ++i) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(out ? out[i] : in[i]);
+    if (at < p1 && p0 < at + static_cast<uintptr_t>(beam_bytes[i]) * (static_cast<uintptr_t>(N) * K) &&
+        beam_bytes[i] > 0)
+      return PCTC_EINVAL;
+  }
   PCTC_HIP(launch_beam_reorder(ntensors, in, out, beam_bytes, parents, N, K, static_cast<hipStream_t>(stream_ptr)));
   prof_flush();
   return PCTC_OK;

@@ -286,3 +286,23 @@ def test_reorder_overlapping_tensors():
     got = pc.beam_reorder([a, b], parents, [a, at(0, spare)])  # in place and not
     assert got[0] is a and torch.equal(a, want[0])
     assert torch.equal(got[1], torch.stack([b[n][parents[n].long()] for n in range(N)]))
+
+
+def test_reorder_beside_its_parents():
+    """States that touch the parents' memory without meeting it are reordered; one that meets it is refused."""
+    import torch
+
+    from paper_2609_33645_amd import prunedctc as pc
+    flat = torch.zeros(24, dtype=torch.int32, device="cuda")
+    before, parents, after = (flat[i:i + 8].view(2, 4) for i in (0, 8, 16))
+    parents.copy_(torch.tensor([[3, 2, 1, 0], [1, 1, 0, 0]]))
+    for t in (before, after):
+        t.copy_(torch.arange(8, device="cuda").view(2, 4))
+    pc.beam_reorder([before, after], parents)
+    want = torch.tensor([[3, 2, 1, 0], [5, 5, 4, 4]], dtype=torch.int32, device="cuda")
+    assert torch.equal(before, want) and torch.equal(after, want)
+    for states, out in (([parents], None), ([flat[4:12].view(2, 4)], None), ([before], [parents])):
+        with pytest.raises(pc.PrunedCTCError):
+            pc.beam_reorder(states, parents, out)
+    assert pc.beam_reorder([parents], parents, [after])[0] is after  # only read
+    assert torch.equal(after, torch.tensor([[0, 1, 2, 3], [1, 1, 1, 1]], dtype=torch.int32, device="cuda"))

@@ -417,3 +417,16 @@ def test_reorder_refuses_overlaps():
     assert refused([A, A], [16, 16]) and refused([A, B], [17, 16]) and refused([B, A, B], [16, 16, 16])
     assert refused([A, B], [16, 16], out=[D, D]) and refused([A, B], [16, 16], out=[D, D + 127])
     assert refused([A, B], [16, 16], out=[B, A]) and refused([A], [16], out=[A + 1])
+
+
+@built
+def test_reorder_refuses_to_write_its_parents():
+    L = _lib()
+    vp = lambda x: (ctypes.c_void_p * 1)(x)  # noqa: E731
+
+    def refused(state, nbytes, parents, out=None):
+        return L.pctc_beam_reorder(1, vp(state), None if out is None else vp(out), (ctypes.c_int64 * 1)(nbytes), parents, 2, 4,
+                                   None) == -1
+    for at in (0, 4, 124, -28):  # parents of 32 bytes, states of 2 x 4 beams of 16
+        assert refused(OK, 16, OK + at)
+        assert refused(OK + 4096, 16, OK + at, out=OK)
