@@ -66,6 +66,31 @@ def test_search_empty_places_first():
     one(2, [5, 6, 4, 7], [-np.inf, np.nan, -0.5, -1.0], -3.0)
 
 
+@pytest.mark.parametrize("K", [1, 3, 8, 32])
+def test_search_empty_places_of_offered_classes(K):
+    """An empty place may hold a class that the row offers in another place."""
+    parts = []
+    for seed in range(6):
+        for k in range(400):
+            ids, lp, bl = random_frames(1000 * seed + k, 20, 8, 9)
+            r = np.random.default_rng(k)
+            for t in range(20):  # 4 of 8 places empty, with the classes of the others, scores gone
+                gone = np.sort(r.choice(8, 4, replace=False))
+                ids[t, gone] = ids[t, np.setdiff1d(np.arange(8), gone)]
+                lp[t, gone] = r.choice([-np.inf, np.nan], 4)
+            s = ref.Search(K)
+            for t in range(20):
+                keep = lp[t] > -np.inf
+                s.step(ids[t][keep], lp[t][keep], bl[t])
+            if s.gap > 2e-5:
+                break
+        parts.append((ids, lp, bl, s))
+    got = run_search([q[:3] for q in parts], K)
+    for n, q in enumerate(parts):
+        assert q[3].gap > 2e-5
+        check_result(got, n, q[3].result(), 20)
+
+
 # ---- equal totals ------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("K", [1, 2, 4, 7, 8, 16, 31, 32])
