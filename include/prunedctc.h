@@ -454,6 +454,39 @@ int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* co
                             size_t workspace_bytes, void* stream);
 
 /* ----------------------------------------------------------------------------------
+ * Below the head: dropout and token embedding, with their gradients.
+ *
+ * pctc_dropout: y_i = x_i 65536 / t where h_i < t, else 0, plus residual_i where residual is not NULL;
+ *   t = round((1 - p) 65536), computed in float and rounded once.  h_i is the 16-bit half i mod 8 (low half
+ *   first, word by word) of the four words of Philox4x32-10 (Salmon et al., 2011) with the 64-bit counter
+ *   offset + i / 8 (upper two words of the counter zero) and key seed.  The gradient of x is the same call on dy with
+ *   no residual.  A call uses the counters [offset, offset + (n + 7) / 8).  offset_dev: device uint64 added to
+ *   offset when the kernel runs (a captured graph's replays then take other masks), or NULL.
+ *   n: 0 .. 2^34; 0 <= p <= 1 - 2^-16.  x, residual, y: device, dtype, aligned to it; y may be x or residual
+ *   itself, other overlaps are PCTC_EINVAL.
+ *
+ * pctc_embedding: y[m] = scale table[tokens[m]], rounded once; zeros where tokens[m] lies outside [0, V).
+ *   table [V, D], y [N, D] device, dtype; tokens device int32 or int64 [N] (token_bytes 4 or 8).
+ *
+ * pctc_embedding_backward: dW[v] (+)= scale times the sum of dy[m] over the m with tokens[m] = v, in
+ *   float and in the order of m for each of a fixed number of consecutive tokens, whose sums are then added
+ *   in order: the same call gives the same bits.  accumulate 0: every row of dW is written; else the sums are
+ *   added to what dW holds (a tied head's gradient) and rows without a token are not touched.  dW [V, D]:
+ *   out_dtype.  1 <= V <= PCTC_MAX_VOCAB, 1 <= D <= PCTC_MAX_DIM, 0 <= N <= 2^30, scale finite.
+ *   workspace: pctc_embedding_backward_workspace_size() bytes, 256-byte aligned.
+ *
+ * What is written must not overlap an input but as said.  All are asynchronous.
+ * ---------------------------------------------------------------------------------- */
+int32_t pctc_dropout(pctc_dtype dtype, const void* x, const void* residual, void* y, int64_t n, double p,
+                     uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* stream);
+int32_t pctc_embedding(pctc_dtype dtype, const void* table, int32_t V, int32_t D, const void* tokens,
+                       int32_t token_bytes, int64_t N, float scale, void* y, void* stream);
+size_t pctc_embedding_backward_workspace_size(int64_t N, int32_t D);
+int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* tokens, int32_t token_bytes, int64_t N,
+                                int32_t V, int32_t D, float scale, pctc_dtype out_dtype, void* dW, int32_t accumulate,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* ----------------------------------------------------------------------------------
  * Kernel timing for benchmarks.  When enabled, every kernel the library launches is
  * bracketed by HIP events on its stream; the times are accumulated per kernel name when
  * they are read (pctc_prof_count / pctc_prof_get, which wait for the recorded launches to

@@ -1222,6 +1222,85 @@ int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* co
   return PCTC_OK;
 }
 
+// ---- below the head ----------------------------------------------------------------------------
+
+static bool is_dtype(pctc_dtype d) { return d == PCTC_F32 || d == PCTC_BF16; }
+static size_t value_bytes(int32_t d) { return d == PCTC_BF16 ? 2 : 4; }
+static bool misaligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+// Whether the `n` bytes at p and the `m` at q meet.
+static bool meets(const void* p, uint64_t n, const void* q, uint64_t m) {
+  const uint64_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return p && q && n && m && a < b + m && b < a + n;
+}
+
+int32_t pctc_dropout(pctc_dtype dtype, const void* x, const void* residual, void* y, int64_t n, double p, uint64_t seed,
+                     uint64_t offset, const uint64_t* offset_dev, void* stream_ptr) {
+  if (!is_dtype(dtype) || n < 0 || n > clip_max_values() || !(p >= 0.0) || !(p <= 1.0 - 1.0 / 65536)) return PCTC_EINVAL;
+  if (n == 0) return PCTC_OK;
+  const size_t e = value_bytes(dtype);
+  const uint64_t bytes = static_cast<uint64_t>(n) * e;
+  if (!x || !y || misaligned_to(x, e) || misaligned_to(y, e) || misaligned_to(residual, e) ||
+      misaligned_to(offset_dev, 8))
+    return PCTC_EINVAL;
+  if ((y != x && meets(y, bytes, x, bytes)) || (y != residual && meets(y, bytes, residual, bytes)) ||
+      meets(y, bytes, offset_dev, 8))
+    return PCTC_EINVAL;
+  const uint32_t t = static_cast<uint32_t>((1.0 - p) * 65536.0 + 0.5);
+  PCTC_HIP(launch_dropout(dtype == PCTC_BF16 ? 1 : 0, x, residual, y, n, t, seed, offset, offset_dev,
+                          static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
+static bool table_args_ok(pctc_dtype dtype, int32_t V, int32_t D, int64_t N, float scale) {
+  return is_dtype(dtype) && V >= 1 && V <= PCTC_MAX_VOCAB && D >= 1 && D <= PCTC_MAX_DIM && N >= 0 && N <= kMaxFrames &&
+         scale - scale == 0.f;
+}
+
+int32_t pctc_embedding(pctc_dtype dtype, const void* table, int32_t V, int32_t D, const void* tokens,
+                       int32_t token_bytes, int64_t N, float scale, void* y, void* stream_ptr) {
+  if (!table_args_ok(dtype, V, D, N, scale) || (token_bytes != 4 && token_bytes != 8)) return PCTC_EINVAL;
+  if (N == 0) return PCTC_OK;
+  const size_t e = value_bytes(dtype);
+  if (!table || !tokens || !y || misaligned_to(table, e) || misaligned_to(y, e) || misaligned_to(tokens, token_bytes))
+    return PCTC_EINVAL;
+  const uint64_t bytes = static_cast<uint64_t>(N) * D * e;
+  if (meets(y, bytes, table, static_cast<uint64_t>(V) * D * e) || meets(y, bytes, tokens, static_cast<uint64_t>(N) * token_bytes))
+    return PCTC_EINVAL;
+  PCTC_HIP(launch_embedding(dtype == PCTC_BF16 ? 1 : 0, table, V, D, tokens, token_bytes == 8, N, scale, y,
+                            static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
+size_t pctc_embedding_backward_workspace_size(int64_t N, int32_t D) {
+  if (N < 0 || N > kMaxFrames || D < 1 || D > PCTC_MAX_DIM) return 0;
+  return embedding_backward_bytes(static_cast<int>(N), D);
+}
+
+int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* tokens, int32_t token_bytes, int64_t N,
+                                int32_t V, int32_t D, float scale, pctc_dtype out_dtype, void* dW, int32_t accumulate,
+                                void* workspace, size_t workspace_bytes, void* stream_ptr) {
+  if (!table_args_ok(dtype, V, D, N, scale) || !is_dtype(out_dtype) || (token_bytes != 4 && token_bytes != 8))
+    return PCTC_EINVAL;
+  const size_t e = value_bytes(dtype), o = value_bytes(out_dtype);
+  const uint64_t bytes = static_cast<uint64_t>(V) * D * o;
+  if (!dW || misaligned_to(dW, o)) return PCTC_EINVAL;
+  if (N > 0) {
+    if (!dy || !tokens || misaligned_to(dy, e) || misaligned_to(tokens, token_bytes)) return PCTC_EINVAL;
+    if (meets(dW, bytes, dy, static_cast<uint64_t>(N) * D * e) || meets(dW, bytes, tokens, static_cast<uint64_t>(N) * token_bytes))
+      return PCTC_EINVAL;
+    const size_t need = pctc_embedding_backward_workspace_size(N, D);
+    if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
+    if (misaligned256(workspace) || meets(workspace, need, dW, bytes)) return PCTC_EINVAL;
+  }
+  PCTC_HIP(launch_embedding_backward(dtype == PCTC_BF16 ? 1 : 0, dy, tokens, token_bytes == 8, static_cast<int>(N), V, D,
+                                     scale, out_dtype == PCTC_BF16 ? 1 : 0, dW, accumulate != 0, workspace,
+                                     static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
 size_t pctc_discarded_mass_scratch_bytes(int32_t N, const int32_t* input_lengths, const int32_t* target_lengths) {
   if (N < 0 || (N > 0 && (!input_lengths || !target_lengths))) return 0;
   for (int n = 0; n < N; ++n)

@@ -329,6 +329,18 @@ hipError_t launch_clip_grad_norm(int tensors, const void* const* grads, void* co
                                  const int32_t* dtypes, float max_norm, float* norm, float* scale, void* workspace,
                                  hipStream_t stream);
 
+// ---- dropout (dropout.hip) and token embedding (embedding.hip) --------------------------------
+// Values are kept where their 16 random bits are below t, 1 <= t <= 65536.  residual may be null; offset_dev
+// (null: 0) is added to offset.
+hipError_t launch_dropout(int dtype, const void* x, const void* residual, void* y, int64_t n, uint32_t t,
+                          uint64_t seed, uint64_t offset, const uint64_t* offset_dev, hipStream_t stream);
+hipError_t launch_embedding(int dtype, const void* table, int V, int D, const void* tokens, bool i64, int64_t N,
+                            float scale, void* y, hipStream_t stream);
+size_t embedding_backward_bytes(int N, int D);
+hipError_t launch_embedding_backward(int dtype, const void* dy, const void* tokens, bool i64, int N, int V, int D,
+                                     float scale, int out_dtype, void* dW, bool accumulate, void* workspace,
+                                     hipStream_t stream);
+
 // ---- alignment lattice ------------------------------------------------------------------
 struct DpPlan {
   int N, M, Y, Smax;

@@ -139,6 +139,16 @@ def lib() -> ctypes.CDLL:
     L.pctc_clip_workspace_size.restype = c_sz
     L.pctc_clip_grad_norm.argtypes = [c_i32, c_p, c_p, c_p, c_p, c_f, c_p, c_p, c_p, c_sz, c_p]
     L.pctc_clip_grad_norm.restype = c_i32
+    c_i64, c_u64, c_d = ctypes.c_int64, ctypes.c_uint64, ctypes.c_double
+    L.pctc_dropout.argtypes = [c_i32, c_p, c_p, c_p, c_i64, c_d, c_u64, c_u64, c_p, c_p]
+    L.pctc_dropout.restype = c_i32
+    L.pctc_embedding.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_i32, c_i64, c_f, c_p, c_p]
+    L.pctc_embedding.restype = c_i32
+    L.pctc_embedding_backward_workspace_size.argtypes = [c_i64, c_i32]
+    L.pctc_embedding_backward_workspace_size.restype = c_sz
+    L.pctc_embedding_backward.argtypes = [c_i32, c_p, c_p, c_i32, c_i64, c_i32, c_i32, c_f, c_i32, c_p, c_i32, c_p, c_sz,
+                                          c_p]
+    L.pctc_embedding_backward.restype = c_i32
     L.pctc_prof_enable.argtypes = [c_i32]
     L.pctc_prof_select.argtypes = [ctypes.c_char_p]
     L.pctc_prof_reset.argtypes = []
@@ -940,6 +950,114 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional
         _check(code, "pctc_clip_grad_norm")
     norm, scale = res.split(1)
     return {"norm": norm, "scale": scale}
+
+
+# ---- below the head ----------------------------------------------------------------------
+
+def _out(out: Optional[torch.Tensor], shape, dtype: torch.dtype, dev: torch.device, what: str = "out") -> torch.Tensor:
+    """A new tensor, or the caller's, which must be one of that shape."""
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if out.dtype is not dtype or tuple(out.shape) != tuple(shape) or out.device != dev or not out.is_contiguous():
+        raise PrunedCTCError(-1, f"{what} must be contiguous {dtype} {tuple(shape)} on {dev}")
+    return out
+
+
+def _u64(x, what: str) -> int:
+    if isinstance(x, float) or int(x) != x or not 0 <= int(x) < 2 ** 64:
+        raise PrunedCTCError(-1, f"{what} must be a whole number below 2^64")
+    return int(x)
+
+
+@_asynchronous
+def dropout(x: torch.Tensor, p: float, seed: int, offset=0, residual: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None, *, stream=None) -> torch.Tensor:
+    """Each value of x (bfloat16 or float32, any shape) zero with probability p, else times the inverse of
+    the share kept, plus `residual`.  The mask is a function of seed, offset and the value's place alone
+    (see pctc_dropout) and is not kept anywhere: the gradient of x is dropout(dy, p, seed, offset).  A call uses
+    (x.numel() + 7) // 8 counters from offset on; calls that should differ take other offsets or seeds.
+    offset: a whole number, or a device int64 tensor of one, which a captured graph reads at each replay.
+    out may be x or residual."""
+    if not x.is_cuda:
+        raise PrunedCTCError(-1, "x must be a device tensor")
+    dt, dev = _dtype_code(x), x.device
+    x = x.contiguous()
+    if residual is not None:
+        if residual.dtype is not x.dtype or residual.shape != x.shape or residual.device != dev:
+            raise PrunedCTCError(-1, "residual must be a tensor like x")
+        residual = residual.contiguous()
+    counter = None
+    if isinstance(offset, torch.Tensor):
+        if offset.dtype is not torch.int64 or offset.numel() != 1 or offset.device != dev:
+            raise PrunedCTCError(-1, f"offset must be a whole number or an int64 tensor of one on {dev}")
+        counter, offset = offset, 0
+    y = _out(out, x.shape, x.dtype, dev)
+    code = lib().pctc_dropout(dt, x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(),
+                              float(p), _u64(seed, "seed"), _u64(offset, "offset"),
+                              None if counter is None else counter.data_ptr(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_dropout")
+    return y
+
+
+def _token_args(tokens: torch.Tensor, dev: torch.device):
+    if tokens.dtype not in (torch.int32, torch.int64) or tokens.device != dev:
+        raise PrunedCTCError(-1, f"tokens must be int32 or int64 on {dev}")
+    return tokens.contiguous(), 4 if tokens.dtype is torch.int32 else 8
+
+
+@_asynchronous
+def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+              *, stream=None) -> torch.Tensor:
+    """Rows of table [V, D] (bfloat16 or float32) by token, times scale: [*tokens.shape, D].  A token outside
+    [0, V) (a beam's -1 past its end) gives zeros.  tokens: int32 or int64, any shape."""
+    if table.dim() != 2 or not table.is_cuda:
+        raise PrunedCTCError(-1, "table must be a device tensor [V, D]")
+    dt, dev, (V, D) = _dtype_code(table), table.device, table.shape
+    table = table.contiguous()
+    tokens, size = _token_args(tokens, dev)
+    y = _out(out, (*tokens.shape, D), table.dtype, dev)
+    code = lib().pctc_embedding(dt, table.data_ptr(), V, D, tokens.data_ptr(), size, tokens.numel(), float(scale),
+                                y.data_ptr(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_embedding")
+    return y
+
+
+@_asynchronous
+def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, V: int, scale: float = 1.0,
+                       out: Optional[torch.Tensor] = None, accumulate: bool = False,
+                       dtype: Optional[torch.dtype] = None, *, stream=None) -> torch.Tensor:
+    """Gradient of embedding()'s table [V, D] from dy [*tokens.shape, D]: the scaled sum of dy's rows for
+    every class, summed in float in an order that the sizes fix.  New (in `dtype`, by default dy's), written
+    into `out`, or with accumulate added to what `out` holds (the gradient that a loss left in the
+    head tied to the table: float32 with a bfloat16 dy is ordinary)."""
+    if not dy.is_cuda:
+        raise PrunedCTCError(-1, "dy must be a device tensor")
+    dt, dev = _dtype_code(dy), dy.device
+    tokens, size = _token_args(tokens, dev)
+    if dy.dim() < 1 or dy.shape[:-1] != tokens.shape:
+        raise PrunedCTCError(-1, "dy must be [*tokens.shape, D]")
+    V, D, N = int(V), int(dy.shape[-1]), tokens.numel()
+    if accumulate and out is None:
+        raise PrunedCTCError(-1, "accumulate needs out")
+    kind = dtype if dtype is not None else dy.dtype if out is None else out.dtype
+    if kind not in (torch.float32, torch.bfloat16):
+        raise PrunedCTCError(-1, f"unsupported dtype {kind}")
+    if V < 1 or D < 1:
+        raise PrunedCTCError(-1, "V and D must be positive")
+    dW = _out(out, (V, D), kind, dev)
+    dy = dy.contiguous()
+    L = lib()
+    nbytes = L.pctc_embedding_backward_workspace_size(N, D)
+    if nbytes == 0:
+        _check(-1, "pctc_embedding_backward")
+    ws = _scratch(nbytes, dev)
+    code = L.pctc_embedding_backward(dt, dy.data_ptr(), tokens.data_ptr(), size, N, V, D, float(scale), _dtype_code(dW),
+                                     dW.data_ptr(), int(bool(accumulate)), ws.data_ptr(), ws.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_embedding_backward")
+    return dW
 
 
 # ---- kernel timing -----------------------------------------------------------------------
