@@ -487,6 +487,37 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
                                 void* workspace, size_t workspace_bytes, void* stream);
 
 /* ----------------------------------------------------------------------------------
+ * A clipped policy loss with a KL term on tokens of the head (rewards instead of transcripts), and
+ * its gradients.  Row m of H emits tokens[m] (of a CTC head: the class of frame m, blank or not):
+ *   lp = z[tokens[m]] - lambda,  z = W H_m + b, lambda = log sum exp z;   r = exp(lp - old_logp[m])
+ *   losses[m] = -min(r A, clip(r, 1 - clip_lo, 1 + clip_hi) A) + kl_weight (exp(d) - d - 1),
+ *               A = advantages[m], d = ref_logp[m] - lp
+ *   loss = sum over the counted rows of weights[m] losses[m];  dH, dW, db: its gradients
+ * (where r A is the smaller the row's gradient is that of r A, else of the KL term alone).  The frame x
+ * vocabulary logits are not stored: the backward recomputes them chunk by chunk as Pruned CTC's does.
+ *   H, W, bias, D, V, chunk: as for pruned_ctc_fwd_bwd_ex (M rows, bias NULL for none).  M = 0 is allowed.
+ *   tokens: device int32 [M]; advantages: device float [M].  old_logp NULL: the policy that sampled the tokens
+ *   is this one (r = 1).  ref_logp NULL: no KL term.  weights NULL: 1.  All three device float [M].
+ *   clip_lo, clip_hi >= 0 (+inf: not clipped), kl_weight finite and >= 0.
+ *   loss: device double [1]; losses, logp: device float [M]; status: device int32 [M]: PCTC_TOKEN_COUNTED;
+ *   PCTC_TOKEN_LEFT_OUT, a token outside [0, V) (a prompt's place), logp 0; PCTC_TOKEN_NONFINITE, a loss or
+ *   gradient factor that is not finite.  Rows that are not counted have losses 0 and take no part in loss
+ *   or gradients (their dH rows are zero).
+ *   dH [M, D], dW [V, D], db [V]: of the dtype of H, rounded once from float sums; each may be NULL, and with all
+ *   three NULL only the losses are formed.
+ *   workspace: pctc_policy_workspace_size() bytes (bias, grads: whether the call has a bias, asks for a
+ *   gradient), 256-byte aligned.  Asynchronous; the result does not change from call to call.
+ * ---------------------------------------------------------------------------------- */
+enum { PCTC_TOKEN_COUNTED = 0, PCTC_TOKEN_LEFT_OUT = 1, PCTC_TOKEN_NONFINITE = 2 };
+size_t pctc_policy_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t bias, int32_t grads,
+                                  int32_t chunk);
+int32_t pctc_policy_loss(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W, const float* bias,
+                         int32_t V, const int32_t* tokens, const float* advantages, const float* old_logp,
+                         const float* ref_logp, const float* weights, float clip_lo, float clip_hi, float kl_weight,
+                         int32_t chunk, double* loss, float* losses, float* logp, int32_t* status, void* dH, void* dW,
+                         void* db, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ----------------------------------------------------------------------------------
  * Kernel timing for benchmarks.  When enabled, every kernel the library launches is
  * bracketed by HIP events on its stream; the times are accumulated per kernel name when
  * they are read (pctc_prof_count / pctc_prof_get, which wait for the recorded launches to

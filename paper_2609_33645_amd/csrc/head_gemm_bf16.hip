@@ -780,7 +780,8 @@ struct DwOp {
 };
 
 // dW products of up to two operand sets in one launch: work ids below tiles0 take P0's output
-// tiles, the rest P1's (the union columns' dW_u in the last chunk's launch).
+// tiles, the rest P1's (the union columns' dW_u in the last chunk's launch).  O16: `out` holds bf16.
+template <bool O16>
 __global__ void __launch_bounds__(512, 1)
 dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int M, int D) {
   using G = GDw;
@@ -817,7 +818,11 @@ dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int 
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int v = v0 + G::row_of(wave, lane, i, r);
-        if (v < cw) dW[static_cast<int64_t>(P.c0 + v) * D + d] = acc[i][j][r];
+        const int64_t at = static_cast<int64_t>(P.c0 + v) * D + d;
+        if (v < cw) {
+          if constexpr (O16) reinterpret_cast<uint16_t*>(dW)[at] = static_cast<uint16_t>(pack_bf16x2(acc[i][j][r], 0.f));
+          else dW[at] = acc[i][j][r];
+        }
       }
     }
 }
@@ -1085,7 +1090,7 @@ hipError_t launch_union_part_bf16(const float* G, int ldG, const int32_t* Kdev, 
     const DwOp p{Gb, k2, 0, k2, reinterpret_cast<float*>(sc + L.o_dwu), L.nz, L.mslice,
                  static_cast<int64_t>(k2) * D, Kdev};
     Prof pr("union_dw", stream);
-    hipLaunchKernelGGL(dw_gemm_bf16, dim3(tiles), dim3(GDw::kThreads), 0, stream, p, p, tiles, Hs, M, D);
+    hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles), dim3(GDw::kThreads), 0, stream, p, p, tiles, Hs, M, D);
   }
   if (want_db) {
     const int mper = (M + kColSlices - 1) / kColSlices;
@@ -1361,7 +1366,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  const int32_t* remap, const float* S, int ldS, uint16_t* dZ, int chunk, float* part,
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra, const ChunkE* ce,
-                                 const uint16_t* Hst, int Mp) {
+                                 const uint16_t* Hst, int Mp, uint16_t* dW16) {
   // wide heads: one 8-wave 256 x 256 workgroup per CU (the long k loop hides the epilogue);
   // narrow heads: two 4-wave 256 x 128 workgroups per CU, so that one's epilogue (exp, pack,
   // staged stores: VALU-bound) overlaps the other's products
@@ -1419,7 +1424,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
   if (want_dW) {
     const int nDt = (D + kBC - 1) / kBC;
     const int tiles0 = ((cw + kBR - 1) / kBR) * nDt;
-    const DwOp p0{dZ, chunk, c0, cw, dW, 1, M, 0, nullptr};
+    DwOp p0{dZ, chunk, c0, cw, dW, 1, M, 0, nullptr};
     DwOp p1 = p0;
     int tiles1 = 0;
     if (extra && extra->Z) {  // the union columns' dW_u, in this launch's last round
@@ -1427,8 +1432,13 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
       tiles1 = ((extra->cols + kBR - 1) / kBR) * nDt;
     }
     Prof pr("dw_gemm", stream);
-    hipLaunchKernelGGL(dw_gemm_bf16, dim3(tiles0 + tiles1), dim3(GDw::kThreads), 0, stream, p0, p1, tiles0,
-                       ce ? ce->Hp : Hs, M, D);
+    if (dW16) {
+      p0.out = reinterpret_cast<float*>(dW16);
+      hipLaunchKernelGGL(dw_gemm_bf16<true>, dim3(tiles0), dim3(GDw::kThreads), 0, stream, p0, p0, tiles0, Hs, M, D);
+    } else {
+      hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles0 + tiles1), dim3(GDw::kThreads), 0, stream, p0, p1, tiles0,
+                         ce ? ce->Hp : Hs, M, D);
+    }
   }
   return hipGetLastError();
 }

@@ -222,7 +222,7 @@ recompute_dz_f32(const float* __restrict__ H, int M, int D, const float* __restr
   int jsel = -1;
   if (tid < kTile) {
     const bool in = vl0 + tid < cw;
-    jsel = in ? remap[c0 + vl0 + tid] : -1;
+    jsel = in && remap ? remap[c0 + vl0 + tid] : -1;  // no remap: -g p only
     sel[tid] = jsel;
     if (BIAS) bl[tid] = in ? bias[c0 + vl0 + tid] : 0.f;
   }
@@ -563,7 +563,7 @@ void plan_products_f32(int M, int D, int cols, int* splits, int* wsplits) {
 
 hipError_t head_bwd_f32(const float* H, int M, int D, const float* W, const float* bias, int V, const float2* lam2,
                         const float* G, int ldG, const float* g, const int32_t* remap, float* dH, float* dW, float* db,
-                        char* scratch, const BwdPlan& plan, hipStream_t stream) {
+                        char* scratch, const BwdPlan& plan, hipStream_t stream, const DzTokens* tokens) {
   float* dZ = reinterpret_cast<float*>(scratch);
   float* Hs = reinterpret_cast<float*>(scratch + plan.dz_bytes);
   // a single dH slice accumulates in the caller's dH
@@ -596,6 +596,10 @@ hipError_t head_bwd_f32(const float* H, int M, int D, const float* W, const floa
       else
         hipLaunchKernelGGL(recompute_dz_f32<false>, grid, dim3(512), 0, stream, H, M, D, W, bias, c0, cw, lam2, G, ldG,
                            g, remap, dZ, chunk);
+    }
+    if (tokens) {
+      const hipError_t e = launch_dz_tokens(0, dZ, chunk, M, c0, cw, *tokens, kDzScale, stream);
+      if (e != hipSuccess) return e;
     }
     auto col_sums = [&](int maxs, float* sums) {
       const int mper = ((M + maxs - 1) / maxs + 3) / 4 * 4;

@@ -1301,6 +1301,39 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
   return PCTC_OK;
 }
 
+// ---- policy loss on the head -----------------------------------------------------------------
+
+size_t pctc_policy_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t bias, int32_t grads,
+                                  int32_t chunk) {
+  if (!head_args_ok(dtype, D, V) || M < 0 || M > kMaxFrames || chunk < 0 || chunk % 256) return 0;
+  return policy_layout(dtype == PCTC_BF16 ? 1 : 0, M, D, V, bias != 0, grads != 0, chunk).total;
+}
+
+int32_t pctc_policy_loss(pctc_dtype dtype, const void* H, int32_t M, int32_t D, const void* W, const float* bias,
+                         int32_t V, const int32_t* tokens, const float* advantages, const float* old_logp,
+                         const float* ref_logp, const float* weights, float clip_lo, float clip_hi, float kl_weight,
+                         int32_t chunk, double* loss, float* losses, float* logp, int32_t* status, void* dH, void* dW,
+                         void* db, void* workspace, size_t workspace_bytes, void* stream_ptr) {
+  const bool grads = dH || dW || db;
+  const size_t need = pctc_policy_workspace_size(dtype, M, D, V, bias != nullptr, grads, chunk);
+  if (need == 0 || !(clip_lo >= 0.f) || !(clip_hi >= 0.f) || !(kl_weight >= 0.f) || !(kl_weight < INFINITY) || !loss ||
+      !W || misaligned16(W) || misaligned16(H) || misaligned16(dH) || misaligned16(dW))
+    return PCTC_EINVAL;
+  if (M > 0 && (!H || !tokens || !advantages || !losses || !logp || !status)) return PCTC_EINVAL;
+  const uint64_t e = value_bytes(dtype), nh = e * M * D, nw = e * V * D;
+  if (meets(dH, nh, H, nh) || meets(dH, nh, W, nw) || meets(dW, nw, H, nh) || meets(dW, nw, W, nw) || meets(dH, nh, dW, nw))
+    return PCTC_EINVAL;
+  if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
+  if (misaligned256(workspace)) return PCTC_EINVAL;
+  const int dt = dtype == PCTC_BF16 ? 1 : 0;
+  const PolicyArgs a{tokens, advantages, old_logp, ref_logp, weights, clip_lo, clip_hi, kl_weight, loss, losses, logp, status};
+  PCTC_HIP(launch_policy_loss(dt, H, M, D, W, bias, V, a, dH, dW, db, static_cast<char*>(workspace),
+                              policy_layout(dt, M, D, V, bias != nullptr, grads, chunk),
+                              static_cast<hipStream_t>(stream_ptr)));
+  prof_flush();
+  return PCTC_OK;
+}
+
 size_t pctc_discarded_mass_scratch_bytes(int32_t N, const int32_t* input_lengths, const int32_t* target_lengths) {
   if (N < 0 || (N > 0 && (!input_lengths || !target_lengths))) return 0;
   for (int n = 0; n < N; ++n)

@@ -158,6 +158,17 @@ hipError_t launch_lam2(const double* lam, int M, float2* lam2, hipStream_t strea
 hipError_t launch_dh_reduce(const float* part, int splits, int64_t n, const float* extra, float* dH,
                             hipStream_t stream);
 
+// One class per frame of a recomputed dZ (policy_loss.hip): dZ[m][token_m] = scale g_m (1 - p), p =
+// exp(logp_m), for the frames whose token lies in the chunk and g_m is not zero.  (Not -g p + g in the
+// chunk's type: of a nearly certain class that would leave nothing but its rounding.)
+struct DzTokens {
+  const int32_t* token;
+  const float* logp;
+  const float* g;
+};
+hipError_t launch_dz_tokens(int dtype, void* dZ, int pitch, int M, int c0, int cw, const DzTokens& t, float scale,
+                            hipStream_t stream);
+
 // ---- fp32 kernels on the split engine (head_gemm_f32.hip) --------------------------------
 constexpr int kDbSlicesF32 = 64;  // frame slices of db's column sums
 void plan_products_f32(int M, int D, int cols, int* splits, int* wsplits);
@@ -170,7 +181,7 @@ hipError_t launch_gather_s_f32(const float* H, int M, int D, const float* W, con
                                float* Gz = nullptr);
 hipError_t head_bwd_f32(const float* H, int M, int D, const float* W, const float* bias, int V, const float2* lam2,
                         const float* G, int ldG, const float* g, const int32_t* remap, float* dH, float* dW, float* db,
-                        char* scratch, const BwdPlan& plan, hipStream_t stream);
+                        char* scratch, const BwdPlan& plan, hipStream_t stream, const DzTokens* tokens = nullptr);
 
 // ---- bf16 kernels on the direct-to-LDS engine (head_gemm_bf16.hip) ---------------------
 hipError_t launch_lse_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
@@ -198,7 +209,8 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  const int32_t* remap, const float* S, int ldS, uint16_t* dZ, int chunk, float* part,
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra = nullptr,
-                                 const ChunkE* ce = nullptr, const uint16_t* Hst = nullptr, int Mp = 0);
+                                 const ChunkE* ce = nullptr, const uint16_t* Hst = nullptr, int Mp = 0,
+                                 uint16_t* dW16 = nullptr);  // dW16: dW is written there, rounded to bf16 (no extra, no ce)
 // Partitions of the normaliser that can write E for a first chunk of `chunk` columns (0: none;
 // narrow heads with D a multiple of 128, chunk a multiple of the partition width).
 int lse_e_parts_bf16(int M, int D, int V, int chunk);
@@ -340,6 +352,27 @@ size_t embedding_backward_bytes(int N, int D);
 hipError_t launch_embedding_backward(int dtype, const void* dy, const void* tokens, bool i64, int N, int V, int D,
                                      float scale, int out_dtype, void* dW, bool accumulate, void* workspace,
                                      hipStream_t stream);
+
+// ---- policy loss (policy_loss.hip) -----------------------------------------------------------
+struct PolicyArgs {
+  const int32_t* tokens;                         // [M]
+  const float *adv, *old_logp, *ref_logp, *weights;  // [M]; the last three may be null
+  float clip_lo, clip_hi, kl;
+  double* loss;     // [1]
+  float* losses;    // [M]
+  float* logp;      // [M]
+  int32_t* status;  // [M]
+};
+struct PolicyLayout {
+  BwdPlan bwd;
+  size_t o_lam, o_lam2, o_g, o_part, o_ht, o_dh, o_bwd, total;
+};
+// grads: the call asks for gradients.
+PolicyLayout policy_layout(int dtype, int M, int D, int V, bool bias, bool grads, int chunk);
+// dH [M][D], dW [V][D], db [V] in the dtype of H, each may be null.
+hipError_t launch_policy_loss(int dtype, const void* H, int M, int D, const void* W, const float* bias, int V,
+                              const PolicyArgs& a, void* dH, void* dW, void* db, char* ws, const PolicyLayout& L,
+                              hipStream_t stream);
 
 // ---- alignment lattice ------------------------------------------------------------------
 struct DpPlan {

@@ -26,6 +26,7 @@ PCTC_F32, PCTC_BF16 = 0, 1
 STATUS = {0: "ok", -1: "invalid argument", -2: "bad label", -3: "bad length", -4: "workspace too small",
           -5: "HIP error", -6: "target too long"}
 UTT_OK, UTT_NOT_ALIGNABLE, UTT_NONFINITE = 0, 1, 2
+TOKEN_COUNTED, TOKEN_LEFT_OUT, TOKEN_NONFINITE = 0, 1, 2
 MAX_TARGET = 1023
 MAX_BEAMS = 32
 MAX_CANDIDATES = 64
@@ -149,6 +150,11 @@ def lib() -> ctypes.CDLL:
     L.pctc_embedding_backward.argtypes = [c_i32, c_p, c_p, c_i32, c_i64, c_i32, c_i32, c_f, c_i32, c_p, c_i32, c_p, c_sz,
                                           c_p]
     L.pctc_embedding_backward.restype = c_i32
+    L.pctc_policy_workspace_size.argtypes = [c_i32] * 7
+    L.pctc_policy_workspace_size.restype = c_sz
+    L.pctc_policy_loss.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_p, c_p, c_p, c_p, c_f, c_f, c_f,
+                                   c_i32, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
+    L.pctc_policy_loss.restype = c_i32
     L.pctc_prof_enable.argtypes = [c_i32]
     L.pctc_prof_select.argtypes = [ctypes.c_char_p]
     L.pctc_prof_reset.argtypes = []
@@ -950,6 +956,63 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional
         _check(code, "pctc_clip_grad_norm")
     norm, scale = res.split(1)
     return {"norm": norm, "scale": scale}
+
+
+# ---- policy loss -------------------------------------------------------------------------
+
+def _per_token(x: Optional[torch.Tensor], M: int, dev: torch.device, what: str) -> Optional[torch.Tensor]:
+    if x is None:
+        return None
+    if x.numel() != M or x.device != dev or not x.dtype.is_floating_point:
+        raise PrunedCTCError(-1, f"{what} must hold a value for each of the {M} rows of H, on {dev}")
+    return _as(x.reshape(M), torch.float32)
+
+
+@_asynchronous
+def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantages: torch.Tensor,
+                old_logp: Optional[torch.Tensor] = None, ref_logp: Optional[torch.Tensor] = None,
+                weights: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, clip=(0.2, 0.2),
+                kl_weight: float = 0.0, chunk: int = 0, want_dH: bool = True, want_dW: bool = True,
+                want_db: bool = False, dH_out: Optional[torch.Tensor] = None, dW_out: Optional[torch.Tensor] = None,
+                *, stream=None) -> Dict[str, torch.Tensor]:
+    """Clipped policy loss with a KL term on the tokens that the head H W^T (+ bias) emits, row by row (see
+    pctc_policy_loss), and its gradients; the rows x vocabulary logits are never stored.  tokens [M]
+    int32 or int64, one outside [0, V) is left out (a prompt's places); advantages, old_logp (None: the
+    policy itself sampled), ref_logp (None: no KL term) and weights (None: 1; the loss is their
+    weighted sum) hold a value per row.  clip: how far below and above 1 the ratio counts (None: anywhere).
+    Returns loss (float64 [1]), losses and logp (float32 [M]), status (int32 [M], TOKEN_*) and, of the type
+    of H, dH [M, D], dW [V, D] and with want_db db [V].  dH_out / dW_out: the caller's tensors for them."""
+    L = lib()
+    H, W, bias, dt = _head_args(H, W, bias)
+    (M, D), V, dev = H.shape, int(W.shape[0]), H.device
+    if tokens.numel() != M or tokens.dtype not in (torch.int32, torch.int64) or tokens.device != dev:
+        raise PrunedCTCError(-1, f"tokens must be int32 or int64, one for each of the {M} rows of H, on {dev}")
+    if tokens.dtype is torch.int64:  # (nothing wraps into the vocabulary)
+        tokens = tokens.clamp(-1, V)
+    tokens = _as(tokens.reshape(M), torch.int32)
+    adv, old, ref, w = (_per_token(x, M, dev, what) for x, what in (
+        (advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights")))
+    if adv is None:
+        raise PrunedCTCError(-1, "no advantages")
+    lo, hi = (math.inf, math.inf) if clip is None else clip
+    dH = _out(dH_out, (M, D), H.dtype, dev, "dH_out") if want_dH else None
+    dW = _out(dW_out, (V, D), H.dtype, dev, "dW_out") if want_dW else None
+    db = torch.empty(V, dtype=H.dtype, device=dev) if want_db else None
+    nbytes = int(L.pctc_policy_workspace_size(dt, M, D, V, int(bias is not None), int(want_dH or want_dW or want_db),
+                                              int(chunk)))
+    if nbytes == 0:
+        _check(-1, "pctc_policy_loss")
+    loss = torch.empty(1, dtype=torch.float64, device=dev)
+    losses, logp = torch.empty((2, M), dtype=torch.float32, device=dev).unbind()
+    status = torch.empty(M, dtype=torch.int32, device=dev)
+    ws = _scratch(nbytes, dev)
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    code = L.pctc_policy_loss(dt, at(H), M, D, at(W), at(bias), V, at(tokens), at(adv), at(old), at(ref), at(w), float(lo),
+                              float(hi), float(kl_weight), int(chunk), at(loss), at(losses), at(logp), at(status), at(dH),
+                              at(dW), at(db), at(ws), ws.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_policy_loss")
+    return {"loss": loss, "losses": losses, "logp": logp, "status": status, "dH": dH, "dW": dW, "db": db}
 
 
 # ---- below the head ----------------------------------------------------------------------

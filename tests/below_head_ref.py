@@ -54,3 +54,33 @@ def embedding_backward(dy, tokens, V, scale):
     np.add.at(mag, t[ok], np.abs(dy[ok] * scale))
     np.add.at(n, t[ok], 1)
     return dW, mag, n
+
+
+def policy(H, W, bias, tokens, adv, old, ref, w, lo, hi, kl):
+    """Policy loss on the head and its gradients, in 64 bits (old, ref, w, bias: None as in the library)."""
+    H, W = np.asarray(H, np.float64), np.asarray(W, np.float64)
+    M, V = len(H), len(W)
+    z = H @ W.T + (0.0 if bias is None else np.asarray(bias, np.float64))
+    top = z.max(1, keepdims=True) if M else np.zeros((0, 1))
+    lam = top + np.log(np.exp(z - top).sum(1, keepdims=True))
+    p = np.exp(z - lam)
+    ok = (tokens >= 0) & (tokens < V)
+    rows = np.nonzero(ok)[0]
+    logp, losses, g = np.zeros(M), np.zeros(M), np.zeros(M)
+    w = np.ones(M) if w is None else np.asarray(w, np.float64)
+    for m in rows:
+        lp = logp[m] = z[m, tokens[m]] - lam[m, 0]
+        r = 1.0 if old is None else np.exp(lp - float(old[m]))
+        A = float(adv[m])
+        a, b = r * A, min(max(r, 1 - lo), 1 + hi) * A
+        losses[m] = -min(a, b)
+        g[m] = -A * r if a <= b else 0.0
+        if ref is not None:
+            d = float(ref[m]) - lp
+            losses[m] += kl * (np.exp(d) - d - 1)
+            g[m] += kl * (1 - np.exp(d))
+    g *= w
+    dZ = -g[:, None] * p
+    dZ[rows, tokens[rows]] += g[rows]
+    return {"loss": float((losses * w)[rows].sum()), "losses": losses, "logp": logp, "g": g, "p": p, "dZ": dZ,
+            "dH": dZ @ W, "dW": dZ.T @ H, "db": dZ.sum(0)}

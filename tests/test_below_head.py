@@ -86,3 +86,56 @@ def test_embedding_backward_refusals_and_sizes():
                 dict(dW=OK + BIG), dict(ws=OK + 3 * BIG + 8), dict(ws=OK + 2 * BIG)):
         assert call(**bad) == -1, bad
     assert call(ws=None) == call(bytes=100) == -4
+
+
+def test_policy_reference_against_differences():
+    rng = np.random.default_rng(3)
+    M, D, V = 6, 5, 7
+    H, W, b = rng.normal(size=(M, D)), rng.normal(size=(V, D)), rng.normal(size=V)
+    t = np.array([0, 3, 6, -1, 2, 2])
+    adv, old = rng.normal(size=M), np.full(M, -2.0)
+    ref_lp, w = rng.normal(size=M) - 2, rng.random(M)
+    f = lambda H, W, b: ref.policy(H, W, b, t, adv, old, ref_lp, w, 0.2, 0.3, 0.1)  # noqa: E731
+    r = f(H, W, b)
+    assert r["losses"][3] == 0 and not r["dH"][3].any()
+    h = 1e-6
+    for x, key in ((H, "dH"), (W, "dW"), (b, "db")):
+        for i in np.ndindex(x.shape):
+            keep = x[i]
+            x[i] = keep + h
+            up = f(H, W, b)["loss"]
+            x[i] = keep - h
+            down = f(H, W, b)["loss"]
+            x[i] = keep
+            # a loss of |L| = 2276 makes about 16 roundings of 2^-53 |L| on each side: 8e-6 over 2 h
+            assert abs((up - down) / (2 * h) - r[key][i]) < 1e-7 + 32 * 2.0 ** -53 * abs(r["loss"]) / h, (key, i)
+
+
+@built
+def test_policy_refusals_and_sizes():
+    lib = _lib()
+    size, f = lib.pctc_policy_workspace_size, lib.pctc_policy_loss
+    assert size(1, 100, 64, 300, 0, 1, 0) > size(1, 100, 64, 300, 0, 0, 0) > 0 and size(1, 0, 64, 300, 0, 1, 0) > 0
+    for bad in ((2, 1, 64, 300, 0, 1, 0), (1, -1, 64, 300, 0, 1, 0), (1, 1, 60, 300, 0, 1, 0), (1, 1, 0, 300, 0, 1, 0),
+                (1, 1, 64, 1, 0, 1, 0), (1, 1, 64, 524_289, 0, 1, 0), (1, 1, 64, 300, 0, 1, 100), (1, 1, 64, 300, 0, 1, -256),
+                (1, (1 << 30) + 1, 64, 300, 0, 1, 0)):
+        assert size(*bad) == 0, bad
+    # the gradients' room does not grow with the vocabulary
+    big = [size(1, 4000, 512, V, 0, 1, 0) for V in (150_000, 180_000, 400_000)]
+    assert max(big) - min(big) < 1 << 20
+    p = [OK + i * BIG for i in range(16)]
+    good = dict(dtype=1, H=p[0], M=10, D=64, W=p[1], bias=None, V=300, tokens=p[2], adv=p[3], old=None, ref=None, w=None, lo=0.2,
+                hi=0.2, kl=0.0, chunk=0, loss=p[4], losses=p[5], logp=p[6], status=p[7], dH=p[8], dW=p[9], db=None, ws=p[10],
+                bytes=1 << 34)
+
+    def call(**kw):
+        return f(*dict(good, **kw).values(), None)
+
+    nan, inf = float("nan"), float("inf")
+    for bad in (dict(dtype=2), dict(M=-1), dict(D=60), dict(V=1), dict(chunk=100), dict(lo=-0.1), dict(lo=nan), dict(hi=nan),
+                dict(hi=-1.0), dict(kl=-0.1), dict(kl=inf), dict(kl=nan), dict(loss=None), dict(W=None), dict(H=None),
+                dict(tokens=None), dict(adv=None), dict(losses=None), dict(logp=None), dict(status=None), dict(H=p[0] + 8),
+                dict(W=p[1] + 8), dict(dH=p[8] + 8), dict(dW=p[9] + 8), dict(dH=p[0]), dict(dH=p[1] + 16), dict(dW=p[1]),
+                dict(dW=p[8] + 1024), dict(ws=p[10] + 16)):
+        assert call(**bad) == -1, bad
+    assert call(ws=None) == call(bytes=1000) == -4

@@ -231,3 +231,199 @@ def test_embedding_backward_of_a_view_and_in_a_graph():
             g.replay()
             assert torch.equal(dW, pc.embedding_backward(dy, tok, 400)), i
         torch.cuda.synchronize()
+
+
+# ---- policy loss ---------------------------------------------------------------------------
+
+def policy_case(seed, M, D, V, dtype, bias=False, sure=4.0, clip=(0.2, 0.3)):
+    """H, W, bias, tokens (some left out), advantages, old and reference log probabilities (no ratio within
+    1e-3 of the clip's edges), weights."""
+    r = np.random.default_rng(seed)
+    W = r.normal(size=(V, D)) / math.sqrt(D)
+    t = r.integers(0, V, size=M)
+    H = r.normal(size=(M, D)) + W[t] * (r.random((M, 1)) * 2 * sure + math.log(V) - sure)
+    H, W = (host(dev(x.astype(np.float32), dtype)) for x in (H, W))
+    b = (r.normal(size=V) * 0.3).astype(np.float32) if bias else None
+    z = H @ W.T + (0 if b is None else b)
+    top = z.max(1)
+    lp = z[np.arange(M), t] - top - np.log(np.exp(z - top[:, None]).sum(1))
+    moved = r.normal(size=M) * 0.2
+    for edge in (math.log(1 - clip[0]), math.log(1 + clip[1])):
+        near = np.abs(moved - edge) < 1e-3
+        moved[near] += 3e-3
+    t = np.where(r.random(M) < 0.15, r.choice([-1, V, -7], size=M), t)
+    f = lambda x: x.astype(np.float32)  # noqa: E731
+    return dict(H=H, W=W, bias=b, tokens=t, adv=f(r.normal(size=M)), old=f(lp - moved), ref=f(lp + r.normal(size=M) * 0.5),
+                w=f(r.random(M) + 0.5))
+
+
+def policy_call(c, dtype, clip, kl, **kw):
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    d = lambda x: None if x is None else dev(x)  # noqa: E731
+    return pc.policy_loss(dev(c["H"].astype(np.float32), dtype), dev(c["W"].astype(np.float32), dtype),
+                          torch.from_numpy(c["tokens"]).cuda().int(), d(c["adv"]), d(c["old"]), d(c["ref"]), d(c["w"]),
+                          d(c["bias"]), clip=clip, kl_weight=kl, **kw)
+
+
+def check_policy(c, dtype, clip, kl, got, db=False, status=None):
+    """Errors to first order.  A logit: (D + 2) 2^-24 of the sum of its terms' magnitudes; lambda: the largest logit's
+    error and 2e-5, the normaliser's bar.  From these the token's log probability (one rounding more), its
+    ratio and KL factor, hence g; a probability by its logit's and lambda's errors and the exponential's
+    2^-21; dZ by these and one rounding to the products' type (of the token's own entry: of g (1 - p), whose p
+    is off by the log probability's error).  Products: magnitudes times the roundings of their sums, at most one
+    per 16 terms on the matrix cores and one per slice, taken as one per term; a rounding at the end.
+    float32 products drop 2^-24 of each term and round six times per 16 terms: the same bound."""
+    lo, hi = clip
+    w = ref.policy(c["H"], c["W"], c["bias"], c["tokens"], c["adv"], c["old"], c["ref"], c["w"], lo, hi, kl)
+    M, V = w["p"].shape
+    D = c["H"].shape[1]
+    mass = np.abs(c["H"]) @ np.abs(c["W"]).T + (0 if c["bias"] is None else np.abs(c["bias"]))
+    ez = (D + 2) * F * mass
+    el = ez.max(1) + 2e-5
+    ok = (c["tokens"] >= 0) & (c["tokens"] < V)
+    t = np.where(ok, c["tokens"], 0)
+    elp = np.where(ok, ez[np.arange(M), t] + el + F * np.abs(w["logp"]), 0.0)
+    if status is None:
+        within(got["logp"], w["logp"], elp, "logp")
+    assert (got["status"].cpu().numpy() == (np.where(ok, 0, 1) if status is None else status)).all()
+    A = np.abs(c["adv"].astype(np.float64))
+    r = np.ones(M) if c["old"] is None else np.exp(w["logp"] - c["old"])
+    x = np.zeros(M) if c["ref"] is None else np.exp(c["ref"] - w["logp"])
+    eloss = np.where(ok, (A * r + kl * (x + 1)) * elp * 1.01 + 2 * F * np.abs(w["losses"]), 0.0)
+    within(got["losses"], w["losses"], eloss, "losses")
+    wt = np.ones(M) if c["w"] is None else c["w"].astype(np.float64)
+    within(got["loss"], np.array([w["loss"]]), (eloss * wt).sum() + 1e-12, "loss")
+    eg = np.where(ok, wt * (A * r + kl * x) * elp * 1.01, 0.0) + 2 * F * np.abs(w["g"])
+    g = np.abs(w["g"])[:, None]
+    e = E["bf16"] if dtype == "bf16" else F
+    ep = w["p"] * ((ez + el[:, None]) * 1.01 + 2.0 ** -21)
+    edz = g * ep + eg[:, None] * w["p"] + e * np.abs(w["dZ"])
+    rows = np.nonzero(ok)[0]
+    own = (rows, t[rows])
+    edz[own] = (g[rows, 0] * w["p"][own] * elp[rows] * 1.01 + eg[rows] * (1 - w["p"][own]) + (e + 4 * F) * np.abs(w["dZ"][own]))
+    dz = np.abs(w["dZ"]) + edz
+    aW, aH = np.abs(c["W"]), np.abs(c["H"])
+    out = E[dtype]
+    tiny = 1e-37
+    within(got["dH"], w["dH"], edz @ aW + (V + 8) * F * (dz @ aW) + out * np.abs(w["dH"]) * 1.01 + tiny, "dH")
+    within(got["dW"], w["dW"], edz.T @ aH + (M + 8) * F * (dz.T @ aH) + out * np.abs(w["dW"]) * 1.01 + tiny, "dW")
+    if db:
+        within(got["db"], w["db"], edz.sum(0) + (M + 8) * F * dz.sum(0) + out * np.abs(w["db"]) * 1.01 + tiny, "db")
+    assert not got["dH"][dev(~ok)].any()
+    return w
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V,chunk", [(1, 8, 2, 0), (2, 24, 3, 0), (5, 64, 33, 0), (64, 64, 257, 256), (65, 72, 1000, 256),
+                                         (130, 512, 2000, 512), (257, 128, 3001, 0), (300, 2048, 700, 0), (40, 2056, 1500, 512),
+                                         (300, 128, 8931, 0), (513, 256, 520, 256)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_policy_loss(dtype, M, D, V, chunk, bias):
+    say("policy_loss", dtype, M, D, V, chunk, bias)
+    clip, kl = (0.2, 0.3), 0.07
+    c = policy_case(M + V, M, D, V, dtype, bias)
+    got = policy_call(c, dtype, clip, kl, chunk=chunk, want_db=True)
+    check_policy(c, dtype, clip, kl, got, db=True)
+    again = policy_call(c, dtype, clip, kl, chunk=chunk)
+    import torch
+    assert all(torch.equal(got[k], again[k]) for k in ("loss", "losses", "logp", "dH", "dW")) and again["db"] is None
+    alone = policy_call(c, dtype, clip, kl, chunk=chunk, want_dH=False)
+    assert alone["dH"] is None and torch.equal(alone["dW"], got["dW"])
+    none = policy_call(c, dtype, clip, kl, want_dH=False, want_dW=False)
+    assert torch.equal(none["losses"], got["losses"]) and torch.equal(none["loss"], got["loss"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_policy_loss_of_nearly_certain_tokens(dtype):
+    """Where p is near one, g (1 - p) is smaller than the rounding of g p."""
+    say("policy_loss certain", dtype)
+    c = policy_case(5, 200, 64, 300, dtype, sure=0.5)
+    ok = (c["tokens"] >= 0) & (c["tokens"] < 300)
+    c["H"][ok] += 6 * c["W"][c["tokens"][ok]]
+    c["H"] = host(dev(c["H"].astype(np.float32), dtype))
+    z = c["H"] @ c["W"].T
+    lp = z[np.arange(200), np.where(ok, c["tokens"], 0)] - np.log(np.exp(z).sum(1))
+    c["old"], c["ref"] = (lp - 0.05).astype(np.float32), (lp + 0.1).astype(np.float32)
+    w = check_policy(c, dtype, (0.2, 0.2), 0.05, policy_call(c, dtype, (0.2, 0.2), 0.05))
+    assert np.median(w["p"][np.nonzero(ok)[0], c["tokens"][ok]]) > 0.95  # (the inputs are what they are meant to be)
+
+
+@pytest.mark.parametrize("drop", ["old", "ref", "w", "old ref w", "clip"])
+def test_policy_loss_without(drop):
+    """No old policy (a ratio of one), no reference, unit weights, no clip."""
+    say("policy_loss without", drop)
+    c = policy_case(8, 100, 64, 400, "f32")
+    clip = (0.2, 0.3)
+    for k in drop.split():
+        if k == "clip":
+            clip = None
+        else:
+            c[k] = None
+    kl = 0.0 if c["ref"] is None else 0.1
+    got = policy_call(c, "f32", clip, kl)
+    check_policy(c, "f32", clip or (math.inf, math.inf), kl, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_policy_loss_of_rows_that_are_not_finite(dtype):
+    """Infinities and NaN in rows that are left out change nothing; in counted rows they take that row out
+    alone.  (float32 tiles with such values are taken on other instructions, which round otherwise: there the
+    others are checked against the reference instead of to the bit.)"""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss nonfinite", dtype)
+    M, D, V = 150, 64, 700
+    c = policy_case(9, M, D, V, dtype)
+    c["tokens"] = np.abs(c["tokens"]) % V
+    args = lambda H, t, adv, old: pc.policy_loss(H, W, t, adv, old, clip=(0.2, 0.3))  # noqa: E731
+    H, W = dev(c["H"].astype(np.float32), dtype), dev(c["W"].astype(np.float32), dtype)
+    t, adv, old = torch.from_numpy(c["tokens"]).cuda(), dev(c["adv"]), dev(c["old"])
+    bad = [3, 64, 65, 100, 149]
+    t0 = t.clone()
+    t0[bad] = -1
+    want = args(H, t0, adv, old)
+    H2 = H.clone()
+    H2[3], H2[64, 5], H2[65] = math.nan, math.inf, -math.inf
+    adv2, old2 = adv.clone(), old.clone()
+    adv2[100], old2[149] = math.nan, math.nan
+    c0 = dict(c, tokens=t0.cpu().numpy(), ref=None, w=None)
+    for tokens, code in ((t0, pc.TOKEN_LEFT_OUT), (t, pc.TOKEN_NONFINITE)):
+        got = args(H2, tokens, adv2, old2)
+        status = np.zeros(M, np.int32)
+        status[bad] = code
+        check_policy(c0, dtype, (0.2, 0.3), 0.0, got, status=status)
+        for k in ("loss", "losses", "dH", "dW") if dtype == "bf16" else ():
+            assert torch.equal(got[k], want[k]), k
+    # a ratio beyond every bound: clipped where that lowers the objective, left out where it does not
+    adv3, old3 = torch.ones_like(adv), old.clone()
+    old3[7] = old3[8] = -1e30
+    adv3[8] = -1
+    got = args(H, t, adv3, old3)
+    assert got["status"][7] == 0 and got["losses"][7] == -np.float32(1 + np.float64(np.float32(0.3))) and not got["dH"][7].any()
+    assert got["status"][8] == pc.TOKEN_NONFINITE and got["losses"][8] == 0 and torch.isfinite(got["dW"].float()).all()
+
+
+def test_policy_loss_without_rows_and_in_a_graph():
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss graph")
+    W = torch.randn(300, 64, device="cuda").bfloat16()
+    z = torch.zeros(0, device="cuda")
+    r = pc.policy_loss(W[:0], W, z.int(), z, want_db=True)
+    assert r["loss"].item() == 0 and not r["dW"].any() and not r["db"].any() and r["dH"].shape == (0, 64)
+    H = torch.randn(100, 64, device="cuda").bfloat16()
+    t, adv = torch.randint(-1, 300, (100,), device="cuda", dtype=torch.int32), torch.randn(100, device="cuda")
+    call = lambda: pc.policy_loss(H, W, t, adv, want_db=True, chunk=256)  # noqa: E731
+    call()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r = call()
+    for i in range(4):
+        H.normal_()
+        t.copy_(torch.randint(-1, 300, (100,), device="cuda"))
+        g.replay()
+        e = call()
+        torch.cuda.synchronize()
+        for k in e:
+            assert torch.equal(r[k], e[k]), (i, k)
