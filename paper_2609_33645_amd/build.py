@@ -23,7 +23,7 @@ ROOT = os.path.dirname(HERE)
 
 SOURCES = ["pctc_api.hip", "union_remap.hip", "head_gemm.hip", "head_gemm_bf16.hip", "head_gemm_f32.hip",
            "ctc_dp.hip", "grouped_head.hip", "frame_candidates.hip", "beam_search.hip", "grad_clip.hip",
-           "dropout.hip", "embedding.hip", "policy_loss.hip"]
+           "dropout.hip", "embedding.hip", "policy_loss.hip", "gated_ffn.hip"]
 
 
 def hipcc() -> str:

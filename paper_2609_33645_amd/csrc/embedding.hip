@@ -416,6 +416,14 @@ Layout layout(int N, int D) {
 
 }  // namespace
 
+hipError_t launch_clear(void* p, int64_t bytes, hipStream_t stream) {
+  Prof pr("clear", stream);
+  if (bytes > 0)
+    hipLaunchKernelGGL(fill_zero, dim3(static_cast<unsigned>(std::min<int64_t>((bytes + 4095) / 4096, kMaxGrid))),
+                       dim3(kThreads), 0, stream, p, bytes);
+  return hipGetLastError();
+}
+
 hipError_t launch_embedding(int dtype, const void* table, int V, int D, const void* tokens, bool i64, int64_t N,
                             float scale, void* y, hipStream_t stream) {
   const int per = dtype == 1 ? 8 : 4;
@@ -485,10 +493,8 @@ hipError_t launch_embedding_backward(int dtype, const void* dy, const void* toke
                                      float scale, int out_dtype, void* dW, bool accumulate, void* workspace,
                                      hipStream_t stream) {
   if (!accumulate) {
-    const int64_t bytes = static_cast<int64_t>(V) * D * (out_dtype == 1 ? 2 : 4);
-    Prof pr("embedding_fill", stream);
-    hipLaunchKernelGGL(fill_zero, dim3(static_cast<unsigned>(std::min<int64_t>((bytes + 4095) / 4096, kMaxGrid))),
-                       dim3(kThreads), 0, stream, dW, bytes);
+    const hipError_t e = launch_clear(dW, static_cast<int64_t>(V) * D * (out_dtype == 1 ? 2 : 4), stream);
+    if (e != hipSuccess) return e;
   }
   if (N == 0) return hipGetLastError();
   const Layout L = layout(N, D);

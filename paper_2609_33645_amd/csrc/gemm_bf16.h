@@ -31,6 +31,8 @@
 // a whole 128-byte line: a 64-byte piece costs the cache about as much as a whole line.
 #pragma once
 
+#include <type_traits>
+
 #include "pctc_device.h"
 
 namespace pctc {
@@ -46,6 +48,7 @@ struct GOp {
   int rows;             // valid rows
   int kmax;             // valid k (KC: kmax <= pitch)
   const int* rowidx;    // KC only: optional row gather table (needs a Gemm with BUF false)
+  const uint16_t* base2 = nullptr;  // PairCopy only: the second matrix
 };
 
 // Word 3 of a raw buffer resource on gfx9-family parts: 32-bit data format, no swizzle.
@@ -266,6 +269,60 @@ struct TileCopy<L, NR, BK, NW, true> {
   }
 };
 
+// Copies of a k-contiguous tile of two matrices of the same shape (base, base2): blocks of 64 tile rows
+// from the one and the other in turn, so that tile rows 128 q + r and 128 q + 64 + r (r < 64) hold rows
+// row0 + 64 q + r of each, and a wavefront that owns 128 tile rows has both products of the same rows.
+// NR tile rows are NR / 2 rows of each.  Otherwise as TileCopy with buffer resources.
+template <int NR, int BK, int NW>
+struct PairCopy {
+  using G = KC<BK>;
+  static constexpr int kBytes = NR * BK * 2;
+  static constexpr int kCopies = kBytes / 1024;
+  static constexpr int kPerWave = kCopies / NW;
+  static_assert(kBytes % 1024 == 0 && kCopies % NW == 0, "tile must be whole 1 KB copies per wave");
+  static_assert(NR % 128 == 0 && 64 % G::kRowsPerCopy == 0, "copies lie within blocks of 64 rows");
+  int row0_, rows_left, kpart;
+  uint32_t poob, off[kPerWave];
+
+  __device__ static __forceinline__ int block(int c) { return c * G::kRowsPerCopy / 64; }
+
+  __device__ __forceinline__ void init(const GOp& op, int row0, int w, int lane, int kbeg, int klim) {
+    const int rem = (klim > kbeg) ? (klim - kbeg) % BK : 0;
+    kpart = rem ? klim - rem : -1;
+#pragma unroll
+    for (int i = 0; i < kPerWave; ++i) {
+      const int c = w + NW * i;
+      const int r = c * G::kRowsPerCopy + lane / G::kSlots;
+      const int lc = (lane % G::kSlots) ^ G::swz(r);
+      off[i] = static_cast<uint32_t>(((block(c) >> 1) * 64 + (r & 63)) * op.pitch * 2 + lc * 16);
+      poob = (lc * 8 < rem) ? 0u : kOob;  // the same for every i
+    }
+    row0_ = row0;
+    rows_left = min(max(op.rows - row0, 0), NR / 2);
+  }
+
+  __device__ __forceinline__ void issue(const GOp& op, int k0, int klim, char* lds, int w) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int size = (k0 < klim) ? rows_left * static_cast<int>(op.pitch) * 2 - k0 * 2 : 0;
+    auto resource = [&](const uint16_t* m) {
+      const uint64_t ba = reinterpret_cast<uint64_t>(m + static_cast<int64_t>(row0_) * op.pitch + k0);
+      const uint64_t bu = (static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ba >> 32))) << 32) |
+                          static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ba)));
+      return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(bu), static_cast<short>(0),
+                                               __builtin_amdgcn_readfirstlane(max(size, 0)), kBufWord3);
+    };
+    uint32_t adj = (k0 == kpart) ? poob : 0u;
+    asm volatile("" : "+v"(adj));  // one register per issue, not a hoisted second offset set
+#pragma unroll
+    for (int i = 0; i < kPerWave; ++i) {
+      const int c = w + NW * i;
+      const __amdgpu_buffer_rsrc_t rs = resource((block(c) & 1) ? op.base2 : op.base);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + c * 1024), 16, off[i] | adj, 0, 0, 0);
+    }
+#endif
+  }
+};
+
 // 8-element bf16 fragment of row (or column) `rr` for k in [kk + 8h, kk + 8h + 8).
 template <LL L, int NR, int BK>
 __device__ __forceinline__ bf16x8 frag(const char* lds, int rr_base, int kk, int lane) {
@@ -298,7 +355,9 @@ __device__ __forceinline__ bf16x8 frag(const char* lds, int rr_base, int kk, int
 // tile's last k-step, half of the products are issued before the barrier (they need only
 // registers), so the matrix pipe has work while the wave waits there; this pays where one
 // workgroup fills the CU (no other workgroup's products to fill the wait).
-template <int BR, int BC, int BK, LL LA, LL LB, int NS, int WR = 2, int WC = 2, bool PRE = false, bool BUF = true>
+// CAX: A's copies, if not TileCopy's.
+template <int BR, int BC, int BK, LL LA, LL LB, int NS, int WR = 2, int WC = 2, bool PRE = false, bool BUF = true,
+          class CAX = void>
 struct Gemm {
   static constexpr int kNS = NS;
   static constexpr int kBR = BR, kBC = BC;
@@ -312,7 +371,7 @@ struct Gemm {
   // bytes of each stage array a kernel declares for this engine (engines that declare their
   // own stages set it to a stub)
   static constexpr int kKernelStageBytes = kStageBytes;
-  using CA = TileCopy<LA, BR, BK, NW, BUF>;
+  using CA = std::conditional_t<std::is_void_v<CAX>, TileCopy<LA, BR, BK, NW, BUF>, CAX>;
   using CB = TileCopy<LB, BC, BK, NW, BUF>;
   static constexpr int CPW = CA::kPerWave + CB::kPerWave;  // copies per wave per k-tile
   static_assert(NS >= 2 && NS <= 4, "stages");

@@ -48,6 +48,7 @@ struct GOp {
   int rows;       // valid rows
   int kmax;       // valid k
   const int* rowidx;  // KC only: row gather table (needs a Gemm with BUF false)
+  const float* base2 = nullptr;  // PairCopy only: the second matrix
 };
 
 constexpr int kT = 256;  // tile rows and columns
@@ -143,6 +144,46 @@ struct TileCopy {
   }
 };
 
+// The copies of bf::PairCopy: 256 tile rows are 128 rows of each of two matrices, blocks of 64 in turn.
+// Wave w's copies (16 rows each, 128 tile rows apart) are of one matrix.
+struct PairCopy {
+  static constexpr int kPerWave = 2;
+  const float* tbase;
+  int rows_left, kpart;
+  uint32_t poob, off[kPerWave];
+
+  __device__ __forceinline__ void init(const GOp& op, int row0, int w, int lane, int kbeg, int klim) {
+    const int rem = (klim > kbeg) ? (klim - kbeg) % kBK : 0;
+    kpart = rem ? klim - rem : -1;
+#pragma unroll
+    for (int i = 0; i < kPerWave; ++i) {
+      const int r = (w + 8 * i) * 16 + (lane >> 2);
+      const int slot = (lane & 3) ^ ((r >> 2) & 3);  // the same for every i
+      off[i] = static_cast<uint32_t>((64 * i + (r & 63)) * op.pitch * 4 + slot * 16);
+      poob = (slot * 4 < rem) ? 0u : bf::kOob;
+    }
+    tbase = ((w & 4) ? op.base2 : op.base) + static_cast<int64_t>(row0) * op.pitch;
+    rows_left = min(max(op.rows - row0, 0), kT / 2);
+  }
+
+  __device__ __forceinline__ void issue(const GOp& op, int k0, int klim, char* lds, int w) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int size = __builtin_amdgcn_readfirstlane(
+        max((k0 < klim) ? rows_left * static_cast<int>(op.pitch) * 4 - k0 * 4 : 0, 0));
+    const uint64_t ba = reinterpret_cast<uint64_t>(tbase + k0);
+    const uint64_t bu = (static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ba >> 32))) << 32) |
+                        static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ba)));
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(bu), static_cast<short>(0), size, bf::kBufWord3);
+    uint32_t adj = (k0 == kpart) ? poob : 0u;
+    asm volatile("" : "+v"(adj));  // one register per issue, not a hoisted second offset set
+#pragma unroll
+    for (int i = 0; i < kPerWave; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (bf::lds_void*)(lds + (w + 8 * i) * 1024), 16, off[i] | adj, 0, 0, 0);
+#endif
+  }
+};
+
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 // The three bf16 parts of a matrix-core fragment (8 values).  x0 and x1 are roundings to nearest of
@@ -190,15 +231,15 @@ __device__ __forceinline__ float value(const char* lds, int r, int k) {
   }
 }
 
-// BUF false: A's rows through its gather table.
-template <LL LA, LL LB, bool BUF = true>
+// BUF false: A's rows through its gather table.  CAX: A's copies, if not TileCopy's.
+template <LL LA, LL LB, bool BUF = true, class CAX = void>
 struct Gemm {
   static constexpr int kNS = 4;
   static constexpr int kBR = kT, kBC = kT;
   static constexpr int NW = 8, kThreads = 512, WR = 2, WC = 4;
   static constexpr int FR = 4, FC = 2;
   static constexpr int kABytes = kT * kBK * 4, kStageBytes = 2 * kABytes;
-  using CA = TileCopy<LA, BUF>;
+  using CA = std::conditional_t<std::is_void_v<CAX>, TileCopy<LA, BUF>, CAX>;
   using CB = TileCopy<LB, true>;
   static constexpr int CPW = CA::kPerWave + CB::kPerWave;
 

@@ -353,6 +353,24 @@ hipError_t launch_embedding_backward(int dtype, const void* dy, const void* toke
                                      float scale, int out_dtype, void* dW, bool accumulate, void* workspace,
                                      hipStream_t stream);
 
+// `bytes` (a multiple of 2) of zeros at an even address; a kernel, so that a captured graph holds no memset.
+hipError_t launch_clear(void* p, int64_t bytes, hipStream_t stream);
+
+// ---- gated feed-forward block (gated_ffn.hip) -------------------------------------------------
+struct FfnArgs {
+  const void *x, *wg, *wu, *wd;  // [M][D], [F][D] twice, [O][F]
+  void *a, *b;                   // [M][F]: written by the forward (null: not kept), read by the backward
+  void* y;                       // [M][O], forward
+  int M, D, F, O, act;
+};
+struct FfnGrads {
+  const void* dy;
+  void *dx, *dwg, *dwu, *dwd;  // null: not wanted (dwg and dwu go together)
+};
+size_t ffn_workspace_bytes(int dtype, int M, int F, bool back);
+hipError_t launch_gated_ffn(int dtype, const FfnArgs& q, void* ws, hipStream_t stream);
+hipError_t launch_gated_ffn_backward(int dtype, const FfnArgs& q, const FfnGrads& g, void* ws, hipStream_t stream);
+
 // ---- policy loss (policy_loss.hip) -----------------------------------------------------------
 struct PolicyArgs {
   const int32_t* tokens;                         // [M]

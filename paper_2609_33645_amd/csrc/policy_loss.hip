@@ -185,23 +185,6 @@ dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, uint16_t* _
   *reinterpret_cast<u32x2*>(dH + i) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
 }
 
-__global__ void __launch_bounds__(kThreads) zero_values(void* p, int64_t n16, int half) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= n16) return;
-  if (half) static_cast<uint16_t*>(p)[i] = 0;
-  else static_cast<u32x4*>(p)[i] = u32x4{0u, 0u, 0u, 0u};
-}
-
-// `bytes` (a multiple of 2) of zeros; a kernel, so that a graph holds no memset.
-hipError_t clear(void* p, int64_t bytes, hipStream_t stream) {
-  const int half = bytes % 16 != 0;
-  const int64_t n = half ? bytes / 2 : bytes / 16;
-  if (n > 0)
-    hipLaunchKernelGGL(zero_values, dim3(static_cast<unsigned>((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, stream,
-                       p, n, half);
-  return hipGetLastError();
-}
-
 constexpr int kDbSlices = 16;
 
 }  // namespace
@@ -299,9 +282,9 @@ hipError_t launch_policy_loss(int dtype, const void* H, int M, int D, const void
   hipError_t e;
   const int64_t es = dtype == 1 ? 2 : 4;
   if (M == 0) {
-    if ((e = clear(a.loss, sizeof(double), stream)) != hipSuccess) return e;
-    if (dW && (e = clear(dW, es * V * D, stream)) != hipSuccess) return e;
-    return db ? clear(db, es * V, stream) : hipSuccess;
+    if ((e = launch_clear(a.loss, sizeof(double), stream)) != hipSuccess) return e;
+    if (dW && (e = launch_clear(dW, es * V * D, stream)) != hipSuccess) return e;
+    return db ? launch_clear(db, es * V, stream) : hipSuccess;
   }
   double* lam = reinterpret_cast<double*>(ws + L.o_lam);
   float2* lam2 = reinterpret_cast<float2*>(ws + L.o_lam2);

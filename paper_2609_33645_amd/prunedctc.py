@@ -150,6 +150,14 @@ def lib() -> ctypes.CDLL:
     L.pctc_embedding_backward.argtypes = [c_i32, c_p, c_p, c_i32, c_i64, c_i32, c_i32, c_f, c_i32, c_p, c_i32, c_p, c_sz,
                                           c_p]
     L.pctc_embedding_backward.restype = c_i32
+    L.pctc_gated_ffn_workspace_size.argtypes = [c_i32] * 6
+    L.pctc_gated_ffn_workspace_size.restype = c_sz
+    L.pctc_gated_ffn.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_p, c_p, c_p, c_p, c_sz,
+                                 c_p]
+    L.pctc_gated_ffn.restype = c_i32
+    L.pctc_gated_ffn_backward.argtypes = [c_i32, c_p, c_p, c_i32, c_i32, c_p, c_p, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_p,
+                                          c_p, c_p, c_p, c_p, c_sz, c_p]
+    L.pctc_gated_ffn_backward.restype = c_i32
     L.pctc_policy_workspace_size.argtypes = [c_i32] * 7
     L.pctc_policy_workspace_size.restype = c_sz
     L.pctc_policy_loss.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_p, c_p, c_p, c_p, c_f, c_f, c_f,
@@ -1121,6 +1129,77 @@ def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, V: int, scale: fl
     if code:
         _check(code, "pctc_embedding_backward")
     return dW
+
+
+_ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def _ffn_args(x, w_gate, w_up, w_down, activation):
+    """Checked and contiguous tensors of a gated block, its sizes, type code and activation's code."""
+    dt, dev = _dtype_code(x), x.device
+    if activation not in _ACTIVATIONS:
+        raise PrunedCTCError(-1, f"activation must be one of {', '.join(_ACTIVATIONS)}")
+    if not x.is_cuda or any(w.dtype is not x.dtype or w.device != dev for w in (w_gate, w_up, w_down)):
+        raise PrunedCTCError(-1, "x and the weights must be tensors of one type on one device")
+    if x.dim() < 1 or any(w.dim() != 2 for w in (w_gate, w_up, w_down)):
+        raise PrunedCTCError(-1, "x must be [..., D] and the weights matrices")
+    D, F, O = int(x.shape[-1]), int(w_gate.shape[0]), int(w_down.shape[0])
+    if tuple(w_gate.shape) != (F, D) or w_up.shape != w_gate.shape or w_down.shape[1] != F:
+        raise PrunedCTCError(-1, "w_gate and w_up must be [F, D], w_down [O, F]")
+    M = x.numel() // D if D else 0
+    return x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), (M, D, F, O), dt, \
+        _ACTIVATIONS[activation]
+
+
+@_asynchronous
+def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+              activation: str = "silu", keep: bool = False, out: Optional[torch.Tensor] = None,
+              *, stream=None) -> Dict[str, Optional[torch.Tensor]]:
+    """Gated feed-forward block y = (act(x w_gate^T) * (x w_up^T)) w_down^T of x [..., D], bfloat16 or float32,
+    for activation "silu" or "gelu" (by the error function); D, F and O multiples of 8.  Returns y [..., O] and, with
+    keep, gate and up [..., F], the two projections, which the backward reads (else None)."""
+    L = lib()
+    x, wg, wu, wd, (M, D, F, O), dt, act = _ffn_args(x, w_gate, w_up, w_down, activation)
+    dev, lead = x.device, x.shape[:-1]
+    nbytes = L.pctc_gated_ffn_workspace_size(dt, M, D, F, O, 0)
+    if nbytes == 0:
+        _check(-1, "pctc_gated_ffn")
+    y = _out(out, (*lead, O), x.dtype, dev)
+    a, b = (torch.empty((*lead, F), dtype=x.dtype, device=dev) for _ in range(2)) if keep else (None, None)
+    ws = _scratch(nbytes, dev)
+    code = L.pctc_gated_ffn(dt, x.data_ptr(), M, D, wg.data_ptr(), wu.data_ptr(), F, wd.data_ptr(), O, act,
+                            a.data_ptr() if keep else None, b.data_ptr() if keep else None, y.data_ptr(), ws.data_ptr(),
+                            ws.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_gated_ffn")
+    return {"y": y, "gate": a, "up": b}
+
+
+@_asynchronous
+def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, w_gate: torch.Tensor,
+                       w_up: torch.Tensor, w_down: torch.Tensor, activation: str = "silu", want_dx: bool = True,
+                       want_dw: bool = True, *, stream=None) -> Dict[str, Optional[torch.Tensor]]:
+    """Gradients of gated_ffn from dy [..., O] and the forward's x, gate and up: dx, dw_gate, dw_up and dw_down, of
+    the type of x (None where not wanted)."""
+    L = lib()
+    x, wg, wu, wd, (M, D, F, O), dt, act = _ffn_args(x, w_gate, w_up, w_down, activation)
+    dev, lead = x.device, x.shape[:-1]
+    for t, n, what in ((dy, O, "dy"), (gate, F, "gate"), (up, F, "up")):
+        if t.dtype is not x.dtype or t.device != dev or tuple(t.shape) != (*lead, n):
+            raise PrunedCTCError(-1, f"{what} must be {x.dtype} {(*lead, n)} on {dev}")
+    dy, gate, up = dy.contiguous(), gate.contiguous(), up.contiguous()
+    nbytes = L.pctc_gated_ffn_workspace_size(dt, M, D, F, O, 1)
+    if nbytes == 0:
+        _check(-1, "pctc_gated_ffn_backward")
+    dx = torch.empty_like(x) if want_dx else None
+    dws = [torch.empty_like(w) if want_dw else None for w in (wg, wu, wd)]
+    ws = _scratch(nbytes, dev)
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    code = L.pctc_gated_ffn_backward(dt, at(dy), at(x), M, D, at(gate), at(up), at(wg), at(wu), F, at(wd), O, act, at(dx),
+                                     *map(at, dws), at(ws), ws.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "pctc_gated_ffn_backward")
+    return dict(zip(("dx", "dw_gate", "dw_up", "dw_down"), (dx, *dws)))
 
 
 # ---- kernel timing -----------------------------------------------------------------------

@@ -84,3 +84,26 @@ def policy(H, W, bias, tokens, adv, old, ref, w, lo, hi, kl):
     dZ[rows, tokens[rows]] += g[rows]
     return {"loss": float((losses * w)[rows].sum()), "losses": losses, "logp": logp, "g": g, "p": p, "dZ": dZ,
             "dH": dZ @ W, "dW": dZ.T @ H, "db": dZ.sum(0)}
+
+
+def _act(a, name):
+    """act(a) and its derivative."""
+    from scipy.special import erfc, expit
+    if name == "silu":
+        s = expit(a)
+        return a * s, s * (1 + a * (1 - s))
+    c = 0.5 * erfc(-a / np.sqrt(2.0))
+    return a * c, c + a * np.exp(-0.5 * a * a) / np.sqrt(2 * np.pi)
+
+
+def gated_ffn(x, wg, wu, wd, act, dy=None, r=lambda v, n: v):
+    """The block and, with dy, its gradients.  r(v, name): what is done to an intermediate result (nothing)."""
+    a, b = r(x @ wg.T, "gate"), r(x @ wu.T, "up")
+    f, df = _act(a, act)
+    h = r(f * b, "h")
+    out = {"gate": a, "up": b, "h": h, "y": h @ wd.T}
+    if dy is not None:
+        dh = dy @ wd
+        da, db = r(dh * b * df, "da"), r(dh * f, "db")
+        out.update(dh=dh, da=da, db=db, dx=da @ wg + db @ wu, dw_gate=da.T @ x, dw_up=db.T @ x, dw_down=dy.T @ h)
+    return out

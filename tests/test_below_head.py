@@ -139,3 +139,71 @@ def test_policy_refusals_and_sizes():
                 dict(dW=p[8] + 1024), dict(ws=p[10] + 16)):
         assert call(**bad) == -1, bad
     assert call(ws=None) == call(bytes=1000) == -4
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gated_ffn_reference_against_differences(act):
+    rng = np.random.default_rng(4)
+    M, D, F, O = 3, 4, 5, 2
+    c = {"x": rng.normal(size=(M, D)), "wg": rng.normal(size=(F, D)), "wu": rng.normal(size=(F, D)), "wd": rng.normal(size=(O, F))}
+    dy = rng.normal(size=(M, O))
+    r = ref.gated_ffn(*c.values(), act, dy)
+    h = 1e-6
+    for key, grad in (("x", "dx"), ("wg", "dw_gate"), ("wu", "dw_up"), ("wd", "dw_down")):
+        for i in np.ndindex(c[key].shape):
+            keep = c[key][i]
+            c[key][i] = keep + h
+            up = (ref.gated_ffn(*c.values(), act)["y"] * dy).sum()
+            c[key][i] = keep - h
+            down = (ref.gated_ffn(*c.values(), act)["y"] * dy).sum()
+            c[key][i] = keep
+            # a sum of magnitude below 100, some 100 roundings of 2^-53 each, over 2 h; truncation below 1e-9
+            assert abs((up - down) / (2 * h) - r[grad][i]) < 6e-7, (key, i)
+
+
+@built
+def test_gated_ffn_refusals_and_sizes():
+    lib = _lib()
+    size = lib.pctc_gated_ffn_workspace_size
+    assert size(1, 100, 64, 128, 64, 1) > size(1, 100, 64, 128, 64, 0) > 0 and size(0, 0, 8, 8, 8, 1) > 0
+    for bad in ((2, 1, 64, 64, 64, 0), (1, -1, 64, 64, 64, 0), (1, 1, 60, 64, 64, 0), (1, 1, 64, 0, 64, 0), (1, 1, 64, 64, 4, 0),
+                (1, (1 << 30) + 1, 64, 64, 64, 0), (1, 1, (1 << 20) + 8, 64, 64, 0)):
+        assert size(*bad) == 0, bad
+    p = [OK + i * BIG for i in range(16)]
+    good = dict(dtype=1, x=p[0], M=10, D=64, wg=p[1], wu=p[2], F=128, wd=p[3], O=72, act=0, gate=p[4], up=p[5], y=p[6], ws=p[7],
+                bytes=1 << 34)
+
+    def call(**kw):
+        return lib.pctc_gated_ffn(*dict(good, **kw).values(), None)
+
+    assert call(M=0) == 0
+    for bad in (dict(dtype=2), dict(M=-1), dict(D=60), dict(F=4), dict(O=0), dict(act=2), dict(gate=None), dict(up=None),
+                dict(x=None), dict(wg=None), dict(wu=None), dict(wd=None), dict(y=None), dict(x=p[0] + 8), dict(wd=p[3] + 2),
+                dict(gate=p[4] + 8), dict(y=p[0]), dict(gate=p[1] + 16), dict(up=p[4]), dict(y=p[5] + 16), dict(ws=p[7] + 8)):
+        assert call(**bad) == -1, bad
+    assert call(ws=None) == call(bytes=100) == -4
+    good = dict(dtype=1, dy=p[0], x=p[1], M=10, D=64, gate=p[2], up=p[3], wg=p[4], wu=p[5], F=128, wd=p[6], O=72, act=1, dx=p[7],
+                dwg=p[8], dwu=p[9], dwd=p[10], ws=p[11], bytes=1 << 34)
+
+    def back(**kw):
+        return lib.pctc_gated_ffn_backward(*dict(good, **kw).values(), None)
+
+    for bad in (dict(dtype=2), dict(M=-1), dict(D=60), dict(F=4), dict(O=0), dict(act=-1), dict(dwg=None), dict(dwu=None),
+                dict(dy=None), dict(x=None), dict(gate=None), dict(up=None), dict(wg=None), dict(wu=None), dict(wd=None),
+                dict(dx=p[7] + 8), dict(dx=p[1]), dict(dwg=p[4]), dict(dwg=p[9]), dict(dwd=p[8] + 256), dict(ws=p[11] + 16)):
+        assert back(**bad) == -1, bad
+    assert back(ws=None) == back(bytes=100) == -4
+
+
+@built
+def test_entry_points_check_their_tensors():
+    """The binding's own checks, on host tensors (nothing reaches the library)."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    x, w, t = torch.zeros(4, 8), torch.zeros(16, 8), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: pc.dropout(x, 0.1, 1), lambda: pc.embedding(w, t), lambda: pc.embedding_backward(x, t, 16),
+                 lambda: pc.gated_ffn(x, w, w, w.T), lambda: pc.gated_ffn_backward(x, x, x, x, w, w, w.T),
+                 lambda: pc.gated_ffn(x, w, w, w.T, "relu"), lambda: pc.policy_loss(x, w, t, x[:, 0]),
+                 lambda: pc.dropout(x.half(), 0.1, 1)):
+        with pytest.raises(pc.PrunedCTCError):
+            call()

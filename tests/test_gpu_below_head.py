@@ -427,3 +427,83 @@ def test_policy_loss_without_rows_and_in_a_graph():
         torch.cuda.synchronize()
         for k in e:
             assert torch.equal(r[k], e[k]), (i, k)
+
+
+# ---- gated block ---------------------------------------------------------------------------
+
+def ffn_case(seed, M, D, F_, O, dtype):
+    r = np.random.default_rng(seed)
+    c = {"x": r.normal(size=(M, D)), "wg": r.normal(size=(F_, D)) / math.sqrt(D), "wu": r.normal(size=(F_, D)) / math.sqrt(D),
+         "wd": r.normal(size=(O, F_)) / math.sqrt(F_), "dy": r.normal(size=(M, O)) * 0.1}
+    return {k: dev(v.astype(np.float32), dtype) for k, v in c.items()}
+
+
+def product_error(A, B, eA, eB, extra=0):
+    """Of A B^T with errors eA, eB in its operands: first order, the product of both, and a rounding of float per
+    term of the sum (there are at most one per 16 terms and six parts; see check_policy) and `extra` more."""
+    aA, aB = np.abs(A), np.abs(B)
+    n = A.shape[1] + 8 + extra
+    return eA @ aB.T + aA @ eB.T + eA @ eB.T + n * F * ((aA + eA) @ (aB + eB).T)
+
+
+def check_ffn(c, act, dtype, got, grads=None):
+    """Bounds carried through the block.  a, b: their products' errors and one rounding to the type (e).  The
+    activation's slope is at most 1.13 (and its derivative's at most 0.8), and it is itself computed to
+    within 2^-20 of its argument (exponential, error function and division of a few units in the last place
+    each).  Products of two factors: each one's error times the other."""
+    x, wg, wu, wd = (host(c[k]) for k in ("x", "wg", "wu", "wd"))
+    e = E[dtype]
+    dy = host(c["dy"])
+    w = ref.gated_ffn(x, wg, wu, wd, act, dy)
+    z = lambda v: np.zeros_like(v)  # noqa: E731
+    raw_a, raw_b = product_error(x, wg, z(x), z(wg)), product_error(x, wu, z(x), z(wu))
+    f, df = ref._act(w["gate"], act)
+    small = 2.0 ** -20
+
+    def h_error(ea, eb):
+        ef = 1.13 * ea + small * np.abs(w["gate"])
+        return (ef * np.abs(w["up"]) + np.abs(f) * eb + ef * eb) * (1 + e) + (e + 2 * F) * np.abs(w["h"]) + 1e-37, ef
+
+    eh, _ = h_error(raw_a, raw_b)  # the forward's h comes from unrounded projections
+    within(got["y"], w["y"], product_error(w["h"], wd, eh, z(wd)) * (1 + e) + e * np.abs(w["y"]) + 1e-37, "y")
+    ea, eb = raw_a * (1 + e) + e * np.abs(w["gate"]), raw_b * (1 + e) + e * np.abs(w["up"])
+    if got["gate"] is not None:
+        within(got["gate"], w["gate"], ea, "gate")
+        within(got["up"], w["up"], eb, "up")
+    if grads is None:
+        return
+    eh, ef = h_error(ea, eb)
+    edf = 0.8 * ea + small * (1 + np.abs(w["gate"]))
+    edh = product_error(dy, wd.T, z(dy), z(wd.T))
+    up, dh = np.abs(w["up"]), np.abs(w["dh"])
+    eda = ((dh + edh) * (up + eb) * (np.abs(df) + edf) - dh * up * np.abs(df)) * (1 + e) + (e + 3 * F) * np.abs(w["da"]) + 1e-37
+    edb = ((dh + edh) * (np.abs(f) + ef) - dh * np.abs(f)) * (1 + e) + (e + 2 * F) * np.abs(w["db"]) + 1e-37
+    tol = {"dx": product_error(w["da"], wg.T, eda, z(wg.T), w["db"].shape[1]) + product_error(w["db"], wu.T, edb, z(wu.T), w["da"].shape[1]),
+           "dw_gate": product_error(w["da"].T, x.T, eda.T, z(x.T)), "dw_up": product_error(w["db"].T, x.T, edb.T, z(x.T)),
+           "dw_down": product_error(dy.T, w["h"].T, z(dy.T), eh.T)}
+    for k, t in tol.items():
+        within(grads[k], w[k], t * (1 + e) + e * np.abs(w[k]) + 1e-37, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,F_,O", [(1, 8, 8, 8), (1, 264, 520, 72), (2, 64, 128, 64), (3, 16, 24, 40), (7, 512, 136, 8), (8, 40, 1032, 264),
+                                      (16, 256, 512, 256), (17, 1032, 264, 520), (31, 72, 200, 72), (33, 512, 384, 136), (64, 128, 264, 512),
+                                      (65, 264, 136, 520), (128, 136, 648, 264), (129, 8, 264, 8), (200, 392, 72, 392), (257, 512, 776, 264),
+                                      (300, 264, 1288, 520), (520, 72, 136, 1032)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gated_ffn(dtype, M, D, F_, O, act):
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("gated_ffn", dtype, M, D, F_, O, act)
+    c = ffn_case(M + D, M, D, F_, O, dtype)
+    got = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act, keep=True)
+    back = lambda **kw: pc.gated_ffn_backward(c["dy"], c["x"], got["gate"], got["up"], c["wg"], c["wu"], c["wd"], act, **kw)  # noqa: E731
+    grads = back()
+    check_ffn(c, act, dtype, got, grads)
+    plain = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act)
+    assert plain["gate"] is None and torch.equal(plain["y"], got["y"])
+    again = back()
+    assert all(torch.equal(grads[k], again[k]) for k in grads)
+    dx, dw = back(want_dw=False), back(want_dx=False)
+    assert torch.equal(dx["dx"], grads["dx"]) and dx["dw_gate"] is None and dw["dx"] is None
+    assert all(torch.equal(dw[k], grads[k]) for k in ("dw_gate", "dw_up", "dw_down"))
