@@ -4,13 +4,13 @@
 //   dh = dy Wd, da = dh b act'(a), db = dh act(a)
 //   dx = da Wg + db Wu,  dWg = da^T x,  dWu = db^T x,  dWd = dy^T h
 //
-// Four launches on the tile engines of gemm_bf16.h and gemm_f32.h:
-//   ffn_pair    both projections, the activation and the product: a tile holds 128 rows of Wg and the same
-//               rows of Wu in blocks of 64, so that a wavefront ends with a and b of the same places
-//               in its registers; what is written is h (and a, b for a backward);
-//   ffn_down    y;
-//   ffn_back    dh, whose epilogue reads a and b and writes da, db and h (formed again);
-//   ffn_grads   dx and the three weight gradients, which need only what is there by then, in one launch.
+// Launches on the tile engines of gemm_bf16.h and gemm_f32.h (bf16 on the ping-pong schedule: 1 to 4% faster here):
+//   ffn_pair      both projections, the activation and the product: a tile holds 128 rows of Wg and the same
+//                 rows of Wu in blocks of 64, so that a wavefront ends with a and b of the same places
+//                 in its registers; what is written is h (and a, b for a backward);
+//   ffn_products  y;
+//   ffn_back      dh, whose epilogue reads a and b and writes da, db and h (formed again);
+//   ffn_products  dx and the three weight gradients, which need only what is there by then, in one launch.
 // Every product is laid out with the output's contiguous dimension as the tile's rows, so that a lane's
 // accumulators are runs of 4 output values.  a, b, h, da and db are kept in the type of x: they are
 // operands of the next products.
@@ -28,7 +28,9 @@ namespace {
 
 using bf::LL;
 
+constexpr int kFew = 128;  // rows of x that the forward takes without tiles
 constexpr int kT = 256;  // tile rows and columns
+constexpr int kWc = 4;   // wavefronts across a tile's columns (two across its rows)
 
 struct B16 {
   using T = uint16_t;
@@ -60,67 +62,308 @@ static_assert(B16::Pair::kStageBytes == kStage && F32::Pair::kStageBytes == kSta
 
 constexpr int kSilu = 0, kGelu = 1;
 
+// A factor c of act(a) = a c, and what the derivative needs besides (silu: nothing; gelu: exp(-a^2 / 2)).
+// silu: c = 1 / (1 + exp(-a)).  gelu: c = (1 + erf(a / sqrt 2)) / 2, the error function by the rational
+// approximation 7.1.26 of Abramowitz and Stegun, off by at most 1.5e-7 (with float roundings 3.1e-7 of
+// c, 8e-8 of gelu root mean square over normal values): 15 instructions that share their exponential with the
+// derivative, where the library's erff, expf and division take 80, which is as long as a float product
+// 512 deep.
+template <int ACT>
+__device__ __forceinline__ float act_factor(float a, float& e) {
+  if constexpr (ACT == kSilu) {
+    e = 0.f;
+    return __builtin_amdgcn_rcpf(1.f + fast_exp2(a * -kLog2e));
+  } else {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(a), 0.3275911f * 0.70710678118654752f, 1.f));
+    float p = fmaf(t, 1.061405429f, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    e = fast_exp2(a * a * (-0.5f * kLog2e));
+    const float half = 0.5f * p * t * e;
+    return a < 0.f ? half : 1.f - half;
+  }
+}
 template <int ACT>
 __device__ __forceinline__ float act(float a) {
-  if constexpr (ACT == kSilu) return a / (1.f + expf(-a));
-  else return 0.5f * a * (1.f + erff(a * 0.70710678118654752f));
+  float e;
+  return a * act_factor<ACT>(a, e);
 }
 // f = act(a), d = act'(a)
 template <int ACT>
 __device__ __forceinline__ void act_grad(float a, float& f, float& d) {
-  if constexpr (ACT == kSilu) {
-    const float s = 1.f / (1.f + expf(-a));
-    f = a * s;
-    d = s * (1.f + a * (1.f - s));
-  } else {
-    const float c = 0.5f * (1.f + erff(a * 0.70710678118654752f));
-    f = a * c;
-    d = c + a * 0.3989422804014327f * expf(-0.5f * a * a);
-  }
+  float e;
+  const float c = act_factor<ACT>(a, e);
+  f = a * c;
+  if constexpr (ACT == kSilu) d = fmaf(f, 1.f - c, c);
+  else d = fmaf(a * 0.3989422804014327f, e, c);
 }
 
-// ---- four consecutive values ---------------------------------------------------------------
+// ---- eight consecutive values (16-byte aligned) --------------------------------------------
 
+template <class E>
+__device__ __forceinline__ void store8(typename E::T* p, const float (&v)[8]) {
+  if constexpr (E::kBf) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                                         pack_bf16x2(v[6], v[7])};
+  } else {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
 template <class E>
 __device__ __forceinline__ void store4(typename E::T* p, const float (&v)[4]) {
   if constexpr (E::kBf) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
   else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
 }
 template <class E>
-__device__ __forceinline__ void load4(const typename E::T* p, float (&v)[4]) {
+struct Raw;  // eight values as they lie in memory
+template <>
+struct Raw<B16> {
+  struct __attribute__((aligned(16))) Eight {
+    u32x4 w;
+  };
+  __device__ static __forceinline__ void values(const Eight& x, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(x.w[e] << 16);
+      v[2 * e + 1] = __uint_as_float(x.w[e] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Raw<F32> {
+  struct __attribute__((aligned(16))) Eight {
+    float4 a, b;
+  };
+  __device__ static __forceinline__ void values(const Eight& x, float (&v)[8]) {
+    v[0] = x.a.x;
+    v[1] = x.a.y;
+    v[2] = x.a.z;
+    v[3] = x.a.w;
+    v[4] = x.b.x;
+    v[5] = x.b.y;
+    v[6] = x.b.z;
+    v[7] = x.b.w;
+  }
+};
+template <class E>
+__device__ __forceinline__ void load8(const typename E::T* p, float (&v)[8]) {
+  Raw<E>::values(*reinterpret_cast<const typename Raw<E>::Eight*>(p), v);
+}
+
+// A wavefront's accumulators (128 tile rows x 64 columns) as rows of the output: 32 columns at a time go
+// through its own 16 KB of the drained stages (16-byte slots XORed with the column, so that neither
+// writes nor reads meet in a bank), and come back 8 consecutive tile rows a lane, 16 lanes a column, so that
+// memory is read and written in lines.  Straight from the accumulators a store is 32 pieces of 16 bytes: the
+// epilogue of ffn_back then took longer than its product (M = 2,567, 4,096 x 10,240: 419 us, now 238).
+// fn(block, col, v, x): tile rows 8 block .. 8 block + 7 of the wavefront's 128, column col of its 64; x is what
+// pre(block, col, x) read for these places, for 32 columns before any of them is used, so that many
+// reads are in flight (there is one workgroup on a compute unit, whose products are over).
+// A wavefront's LDS accesses are ordered; no barrier is needed.
+struct Nothing {};
+template <class G, class X = Nothing, class Fn, class Pre>
+__device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* const (&st)[4], Fn&& fn, Pre&& pre) {
+  static_assert(G::FR == 4 && G::FC == 2, "128 x 64");
+  int lane = threadIdx.x & 63;
+  // opaque: what is derived from it is not kept in registers through the product (it would spill there)
+  asm volatile("" : "+v"(lane));
+  const int wave = threadIdx.x >> 6;
+  char* const base = (wave < 2 ? st[0] : wave < 4 ? st[1] : wave < 6 ? st[2] : st[3]) + (wave & 1) * 16384;
+  constexpr int NB = sizeof(X) > 32 ? 4 : 8;  // places a lane reads ahead
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int c = lane & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int slot = 8 * i + 2 * q + (lane >> 5);  // tile rows 4 slot ..
+        *reinterpret_cast<float4*>(base + c * 512 + ((slot ^ (c & 31)) << 4)) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      }
+    const int block = lane & 15;
+#pragma unroll
+    for (int t0 = 0; t0 < 8; t0 += NB) {
+      X x[NB];
+#pragma unroll
+      for (int t = 0; t < NB; ++t) pre(block, 32 * j + 4 * (t0 + t) + (lane >> 4), x[t]);
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        const int col = 4 * (t0 + t) + (lane >> 4);
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 y = *reinterpret_cast<const float4*>(base + col * 512 + (((2 * block + h) ^ (col & 31)) << 4));
+          v[4 * h] = y.x;
+          v[4 * h + 1] = y.y;
+          v[4 * h + 2] = y.z;
+          v[4 * h + 3] = y.w;
+        }
+        fn(block, 32 * j + col, v, x[t]);
+      }
+    }
+  }
+}
+template <class G, class Fn>
+__device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* const (&st)[4], Fn&& fn) {
+  by_columns<G>(acc, st, [&](int block, int col, const float (&v)[8], const Nothing&) { fn(block, col, v); },
+                [](int, int, Nothing&) {});
+}
+
+// ---- few rows ------------------------------------------------------------------------------
+
+// The projections (MATS 2: the same rows of w0 and w1, then h = act(a) b) or a plain product (MATS 1) for up to
+// 16 NT rows of x.  A workgroup takes 16 rows of the weights, its wavefronts a share of k each, and adds the
+// shares up in order through LDS.  Weights and rows go from memory to the matrix instructions' registers
+// (16 x 16, 16 bytes a lane: 64 bytes of each of 16 rows an instruction) without LDS: every weight is used by
+// one wavefront only, and what bounds the kernel is reading the weights.  Rows past R or M repeat the
+// last one; what they give is not written.
+template <class E>
+struct FewArgs {
+  const typename E::T *x, *w0, *w1;
+  typename E::T *out, *a, *b;  // a and b null: not kept
+  int M, K, R;
+};
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+template <class E>
+__device__ __forceinline__ void few_step(const u32x4& w, const u32x4& x, f32x4& acc) {
   if constexpr (E::kBf) {
-    const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-    v[0] = __uint_as_float(w[0] << 16);
-    v[1] = __uint_as_float(w[0] & 0xffff0000u);
-    v[2] = __uint_as_float(w[1] << 16);
-    v[3] = __uint_as_float(w[1] & 0xffff0000u);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
   } else {
-    const float4 w = *reinterpret_cast<const float4*>(p);
-    v[0] = w.x;
-    v[1] = w.y;
-    v[2] = w.z;
-    v[3] = w.w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)  // k in another order, the same for both operands
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[e]), __uint_as_float(x[e]), acc, 0, 0, 0);
   }
 }
 
-// fn(row, col, values) for each run of 4 rows of this lane's accumulators (blocks I0 .. I1 - 1) inside
-// rows x cols; rows is a multiple of 4.
-template <class G, int I0, int I1, class Fn>
-__device__ __forceinline__ void for_runs(f32x16 (&acc)[G::FR][G::FC], int row0, int col0, int rows, int cols, Fn&& fn) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <class E, int MATS, int NT, int WAVES, int ACT>
+__global__ void __launch_bounds__(WAVES * 64) ffn_few(FewArgs<E> P) {
+  using T = typename E::T;
+  constexpr int kPer = E::kBf ? 8 : 4, kStep = 4 * kPer;  // values of a lane, k of a step
+  constexpr int U = NT >= 4 ? 2 : 4;                      // steps read ahead
+  __shared__ f32x4 sum[WAVES][MATS * NT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
+  const int row = min(r0 + (lane & 15), P.R - 1), ko = (lane >> 4) * kPer;
+  const T* w[MATS];
+  w[0] = P.w0 + static_cast<int64_t>(row) * P.K + ko;
+  if constexpr (MATS == 2) w[1] = P.w1 + static_cast<int64_t>(row) * P.K + ko;
+  const T* x[NT];
 #pragma unroll
-  for (int j = 0; j < G::FC; ++j) {
-    const int col = col0 + G::col_of(wave, lane, j);
-    if (col >= cols) continue;
+  for (int n = 0; n < NT; ++n) x[n] = P.x + static_cast<int64_t>(min(m0 + 16 * n + (lane & 15), P.M - 1)) * P.K + ko;
+  f32x4 acc[MATS][NT];
 #pragma unroll
-    for (int i = I0; i < I1; ++i)
+  for (int q = 0; q < MATS; ++q)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int row = row0 + G::row_of(wave, lane, i, 4 * q);
-        if (row >= rows) continue;
-        fn(i, j, q, row, col);
-      }
+    for (int n = 0; n < NT; ++n) acc[q][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int share = (P.K + WAVES * kStep - 1) / (WAVES * kStep) * kStep;
+  const int kb = min(P.K, wave * share), ke = min(P.K, kb + share);
+  auto piece = [](const T* p) { return *reinterpret_cast<const u32x4*>(p); };
+  int k = kb;
+  u32x4 wv[2][MATS][U], xv[2][NT][U];
+  auto read = [&](int s, int at) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int q = 0; q < MATS; ++q) wv[s][q][u] = piece(w[q] + at + u * kStep);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) xv[s][n][u] = piece(x[n] + at + u * kStep);
+    }
+  };
+  auto use = [&](int s) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int q = 0; q < MATS; ++q)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) few_step<E>(wv[s][q][u], xv[s][n][u], acc[q][n]);
+  };
+  constexpr int kBlock = U * kStep;
+  const int blocks = (ke - kb) / kBlock;
+  if (blocks > 0) {
+    read(0, k);
+    int i = 0;
+    for (; i + 2 < blocks; i += 2) {
+      read(1, k + kBlock);
+      use(0);
+      read(0, k + 2 * kBlock);
+      use(1);
+      k += 2 * kBlock;
+    }
+    if (i + 1 < blocks) {
+      read(1, k + kBlock);
+      use(0);
+      use(1);
+      k += 2 * kBlock;
+    } else {
+      use(0);
+      k += kBlock;
+    }
   }
+  for (; k < ke; k += kStep) {  // the last steps; lanes past K have zeros
+    const bool in = k + ko < P.K;
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    u32x4 xt[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) xt[n] = in ? piece(x[n] + k) : zero;
+#pragma unroll
+    for (int q = 0; q < MATS; ++q) {
+      const u32x4 wt = in ? piece(w[q] + k) : zero;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) few_step<E>(wt, xt[n], acc[q][n]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < MATS; ++q)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) sum[wave][q * NT + n][lane] = acc[q][n];
+  __syncthreads();
+  for (int i = threadIdx.x; i < NT * 64; i += WAVES * 64) {
+    const int n = i >> 6, l = i & 63;
+    const int m = m0 + 16 * n + (l & 15), r = r0 + 4 * (l >> 4);
+    if (m >= P.M || r >= P.R) continue;
+    float v[MATS][4] = {};
+#pragma unroll
+    for (int g = 0; g < WAVES; ++g)
+#pragma unroll
+      for (int q = 0; q < MATS; ++q) {
+        const f32x4 s = sum[g][q * NT + n][l];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q][e] += s[e];
+      }
+    const int64_t at = static_cast<int64_t>(m) * P.R + r;
+    if constexpr (MATS == 2) {
+      float h[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) h[e] = act<ACT>(v[0][e]) * v[1][e];
+      store4<E>(P.out + at, h);
+      if (P.a) {
+        store4<E>(P.a + at, v[0]);
+        store4<E>(P.b + at, v[1]);
+      }
+    } else {
+      store4<E>(P.out + at, v[0]);
+    }
+  }
+}
+
+// Rows of x a workgroup takes: all of them while that leaves workgroups for every compute unit twice; else
+// fewer, and the weights are read again from the caches.
+template <class E, int MATS, int ACT>
+void launch_few(const FewArgs<E>& P, hipStream_t stream) {
+  const int nr = (P.R + 15) / 16;
+  int nt = P.M <= 16 ? 1 : P.M <= 32 ? 2 : P.M <= 64 ? 4 : 8;
+  while (nt > 1 && nr * ((P.M + 16 * nt - 1) / (16 * nt)) < 512) nt /= 2;
+  const dim3 grid(nr, (P.M + 16 * nt - 1) / (16 * nt));
+#define PCTC_FEW(NT, WAVES) \
+  hipLaunchKernelGGL((ffn_few<E, MATS, NT, WAVES, ACT>), grid, dim3(WAVES * 64), 0, stream, P)
+  if (nt == 1) PCTC_FEW(1, 8);
+  else if (nt == 2) PCTC_FEW(2, 8);
+  else if (nt == 4) PCTC_FEW(4, 8);
+  else PCTC_FEW(8, 4);
+#undef PCTC_FEW
 }
 
 // ---- forward -------------------------------------------------------------------------------
@@ -143,56 +386,23 @@ __global__ void __launch_bounds__(512, 1) ffn_pair(PairArgs<E> P) {
   A.base2 = P.wu;
   const typename E::Op B{P.x, P.D, P.M, P.D, nullptr};
   f32x16 acc[G::FR][G::FC];
-  G::run(A, B, f0, m0, 0, P.D, st, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if constexpr (E::kBf) G::run_pp(A, B, f0, m0, 0, P.D, st, acc);
+  else G::run(A, B, f0, m0, 0, P.D, st, acc);
+  // 64 rows of Wg, then the same of Wu: lanes b and b + 8 of a column have a and b of the same places
+  const int wave = threadIdx.x >> 6;
+  const int fw = f0 + wave / kWc * 64, mw = m0 + wave % kWc * 64;
+  by_columns<G>(acc, st, [&](int block, int col, const float (&v)[8]) {
+    const int f = fw + (block & 7) * 8, m = mw + col;
+    const bool in = f < P.F && m < P.M;
+    const int64_t at = static_cast<int64_t>(m) * P.F + f;
+    float h[8];
 #pragma unroll
-  for (int j = 0; j < G::FC; ++j) {
-    const int m = m0 + G::col_of(wave, lane, j);
-    if (m >= P.M) continue;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)  // blocks i and i + 2: the same rows of Wg and Wu
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int r = G::row_of(wave, lane, i, 4 * q);  // tile rows 128 q + r hold rows 64 q + r
-        const int f = f0 + (r >> 7) * 64 + (r & 63);
-        if (f >= P.F) continue;
-        float a[4], b[4], h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          a[e] = acc[i][j][4 * q + e];
-          b[e] = acc[i + 2][j][4 * q + e];
-          h[e] = act<ACT>(a[e]) * b[e];
-        }
-        const int64_t at = static_cast<int64_t>(m) * P.F + f;
-        store4<E>(P.h + at, h);
-        if (P.a) {
-          store4<E>(P.a + at, a);
-          store4<E>(P.b + at, b);
-        }
-      }
-  }
-}
-
-template <class E>
-struct DownArgs {
-  const typename E::T *h, *wd;
-  typename E::T* y;
-  int M, F, O;
-};
-
-template <class E>
-__global__ void __launch_bounds__(512, 1) ffn_down(DownArgs<E> P) {
-  using G = typename E::template G<LL::KC, LL::KC>;
-  PCTC_FFN_STAGES
-  int mt, ot;
-  if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), (P.M + kT - 1) / kT, (P.O + kT - 1) / kT, mt, ot)) return;
-  const typename E::Op A{P.wd, P.F, P.O, P.F, nullptr};
-  const typename E::Op B{P.h, P.F, P.M, P.F, nullptr};
-  f32x16 acc[G::FR][G::FC];
-  G::run(A, B, ot * kT, mt * kT, 0, P.F, st, acc);
-  for_runs<G, 0, G::FR>(acc, ot * kT, mt * kT, P.O, P.M, [&](int i, int j, int q, int o, int m) {
-    const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    store4<E>(P.y + static_cast<int64_t>(m) * P.O + o, v);
+    for (int e = 0; e < 8; ++e) {
+      const float o = __shfl_xor(v[e], 8, 64);
+      h[e] = act<ACT>(block < 8 ? v[e] : o) * (block < 8 ? o : v[e]);
+    }
+    if (in && block < 8) store8<E>(P.h + at, h);
+    if (in && P.a) store8<E>((block < 8 ? P.a : P.b) + at, v);
   });
 }
 
@@ -214,117 +424,294 @@ __global__ void __launch_bounds__(512, 1) ffn_back(BackArgs<E> P) {
   const typename E::Op A{P.wd, P.F, P.F, P.O, nullptr};  // rows f, k-lines of Wd
   const typename E::Op B{P.dy, P.O, P.M, P.O, nullptr};
   f32x16 acc[G::FR][G::FC];
-  G::run(A, B, ft * kT, mt * kT, 0, P.O, st, acc);
-  for_runs<G, 0, G::FR>(acc, ft * kT, mt * kT, P.F, P.M, [&](int i, int j, int q, int f, int m) {
-    const int64_t at = static_cast<int64_t>(m) * P.F + f;
-    float a[4], b[4], h[4];
-    load4<E>(P.a + at, a);
-    load4<E>(P.b + at, b);
+  if constexpr (E::kBf) G::run_pp(A, B, ft * kT, mt * kT, 0, P.O, st, acc);
+  else G::run(A, B, ft * kT, mt * kT, 0, P.O, st, acc);
+  const int wave = threadIdx.x >> 6;
+  const int fw = ft * kT + wave / kWc * 128, mw = mt * kT + wave % kWc * 64;
+  struct AB {
+    typename Raw<E>::Eight a, b;
+  };
+  // (places outside read the tile's first: no branch between the reads)
+  by_columns<G, AB>(
+      acc, st,
+      [&](int block, int col, const float (&dh)[8], const AB& x) {
+        const int f = fw + block * 8, m = mw + col;
+        if (f >= P.F || m >= P.M) return;
+        const int64_t at = static_cast<int64_t>(m) * P.F + f;
+        float a[8], b[8], h[8];
+        Raw<E>::values(x.a, a);
+        Raw<E>::values(x.b, b);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float dh = acc[i][j][4 * q + e];
-      float fa, ga;
-      act_grad<ACT>(a[e], fa, ga);
-      h[e] = fa * b[e];
-      a[e] = dh * b[e] * ga;
-      b[e] = dh * fa;
-    }
-    store4<E>(P.da + at, a);
-    store4<E>(P.db + at, b);
-    store4<E>(P.h + at, h);
-  });
+        for (int e = 0; e < 8; ++e) {
+          float fa, ga;
+          act_grad<ACT>(a[e], fa, ga);
+          h[e] = fa * b[e];
+          a[e] = dh[e] * b[e] * ga;
+          b[e] = dh[e] * fa;
+        }
+        store8<E>(P.da + at, a);
+        store8<E>(P.db + at, b);
+        store8<E>(P.h + at, h);
+      },
+      [&](int block, int col, AB& x) {
+        const int f = fw + block * 8, m = mw + col;
+        const int64_t at = f < P.F && m < P.M ? static_cast<int64_t>(m) * P.F + f : 0;
+        x.a = *reinterpret_cast<const typename Raw<E>::Eight*>(P.a + at);
+        x.b = *reinterpret_cast<const typename Raw<E>::Eight*>(P.b + at);
+      });
 }
 
-template <class E>
-struct GradArgs {
-  const typename E::T *x, *dy, *wg, *wu, *da, *db, *h;
-  typename E::T *dx, *dwg, *dwu, *dwd;  // null: not wanted
-  int M, D, F, O;
-  int n_dx, n_w, n_d;  // tiles of dx, of dWg (and dWu), of dWd (0: not wanted)
+// ---- products -------------------------------------------------------------------------------
+
+// out[c][r] = sum over k of A[r][k] B[c][k] (+ A2[r][k] B2[c][k]), r < rows, c < cols, for up to four
+// products in one launch, each cut along k into `slices` of `depth` (a multiple of 32; the second operands' k
+// begins at kp, K rounded up to it).  A product of one slice is written as it is to be; of several, every
+// slice's float sums are written and ffn_join adds them in order.
+struct Product {
+  const void *A, *B, *A2, *B2;  // A2 null: none
+  void* out;
+  float* part;  // [slices][cols][rows]
+  int pa, pb;   // pitches
+  int rows, cols, K, kp, slices, depth;
+  int mc_b;     // B's columns are contiguous in memory (else its k)
+  int first;    // workgroups of the products before
+};
+struct Products {
+  Product p[4];
+  int n;
 };
 
-// out[col][row ..] = the tile's sums
-template <class E, class G>
-__device__ __forceinline__ void put_tile(f32x16 (&acc)[G::FR][G::FC], int row0, int col0, int rows, int cols,
-                                         typename E::T* out) {
-  for_runs<G, 0, G::FR>(acc, row0, col0, rows, cols, [&](int i, int j, int q, int r, int c) {
-    const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    store4<E>(out + static_cast<int64_t>(c) * rows + r, v);
+// LA: the layout of every A; MCB, KCB: which layouts of B there are.
+template <class E, LL LA, bool KCB, bool MCB>
+__global__ void __launch_bounds__(512, 1) ffn_products(Products Q) {
+  using T = typename E::T;
+  using Op = typename E::Op;
+  using GK = typename E::template G<LA, LL::KC>;
+  using GM = typename E::template G<LA, LL::MC>;
+  PCTC_FFN_STAGES
+  int which = 0;
+  while (which + 1 < Q.n && static_cast<int>(blockIdx.x) >= Q.p[which + 1].first) ++which;
+  const Product& P = Q.p[which];
+  const int nR = (P.rows + kT - 1) / kT, nC = (P.cols + kT - 1) / kT;
+  const int w = xcd_swz(blockIdx.x - P.first, nR * nC * P.slices);
+  const int slice = w / (nR * nC), rest = w % (nR * nC);
+  // the shorter side fastest: the workgroups of an XCD share what they read
+  const int rt = nR <= nC ? rest % nR : rest / nC, ct = nR <= nC ? rest / nR : rest % nC;
+  const int r0 = rt * kT, c0 = ct * kT;
+  const int kb = slice * P.depth, ke = kb + P.depth;
+  f32x16 acc[GK::FR][GK::FC];
+  const Op A{static_cast<const T*>(P.A), P.pa, P.rows, P.K, nullptr}, B{static_cast<const T*>(P.B), P.pb, P.cols, P.K, nullptr};
+  if (MCB && (!KCB || P.mc_b)) {
+    if constexpr (E::kBf) GM::run_pp(A, B, r0, c0, kb, min(ke, P.K), st, acc);
+    else GM::run(A, B, r0, c0, kb, min(ke, P.K), st, acc);
+  } else if constexpr (KCB) {
+    if constexpr (E::kBf) {
+      GK::run_pp(A, B, r0, c0, kb, min(ke, P.K), st, acc);  // (nothing where the slice begins past the first half)
+      if (P.A2) {
+        const Op A2{static_cast<const T*>(P.A2), P.pa, P.rows, P.K, nullptr};
+        const Op B2{static_cast<const T*>(P.B2), P.pb, P.cols, P.K, nullptr};
+        GK::template run_pp<false>(A2, B2, r0, c0, max(kb - P.kp, 0), min(ke - P.kp, P.K), st, acc);
+      }
+    } else {  // a slice of a float product lies in one half
+      const bool second = P.A2 && kb >= P.kp;
+      const Op A1{static_cast<const T*>(second ? P.A2 : P.A), P.pa, P.rows, P.K, nullptr};
+      const Op B1{static_cast<const T*>(second ? P.B2 : P.B), P.pb, P.cols, P.K, nullptr};
+      const int from = second ? kb - P.kp : kb;
+      GK::run(A1, B1, r0, c0, from, min(from + P.depth, P.K), st, acc);
+    }
+  }
+  const int wave = threadIdx.x >> 6;
+  const int rw = r0 + wave / kWc * 128, cw = c0 + wave % kWc * 64;
+  float* const part = P.slices > 1 ? P.part + static_cast<int64_t>(slice) * P.rows * P.cols : nullptr;
+  by_columns<GK>(acc, st, [&](int block, int col, const float (&v)[8]) {
+    const int r = rw + block * 8, c = cw + col;
+    if (r >= P.rows || c >= P.cols) return;
+    const int64_t at = static_cast<int64_t>(c) * P.rows + r;
+    if (part) store8<F32>(part + at, v);
+    else store8<E>(static_cast<T*>(P.out) + at, v);
   });
 }
 
-// dx's tiles first: they are the longest (2 F deep, the others M).
+// The sliced products' sums; blockIdx.y: product.
 template <class E>
-__global__ void __launch_bounds__(512, 1) ffn_grads(GradArgs<E> P) {
-  PCTC_FFN_STAGES
-  using Op = typename E::Op;
-  const int nD = (P.D + kT - 1) / kT, nF = (P.F + kT - 1) / kT, nM = (P.M + kT - 1) / kT;
-  int w = blockIdx.x;
-  if (w < P.n_dx) {
-    using G = typename E::template G<LL::MC, LL::KC>;
-    w = xcd_swz(w, P.n_dx);
-    const int d0 = w / nM * kT, m0 = w % nM * kT;
-    f32x16 acc[G::FR][G::FC];
-    const Op Ag{P.wg, P.D, P.D, P.F, nullptr}, Au{P.wu, P.D, P.D, P.F, nullptr};
-    const Op Bg{P.da, P.F, P.M, P.F, nullptr}, Bu{P.db, P.F, P.M, P.F, nullptr};
-    if constexpr (E::kBf) {
-      G::run(Ag, Bg, d0, m0, 0, P.F, st, acc);
-      G::template run<false>(Au, Bu, d0, m0, 0, P.F, st, acc);
-      put_tile<E, G>(acc, d0, m0, P.D, P.M, P.dx);
-    } else {
-      G::run(Ag, Bg, d0, m0, 0, P.F, st, acc);
-      put_tile<E, G>(acc, d0, m0, P.D, P.M, P.dx);
-      G::run(Au, Bu, d0, m0, 0, P.F, st, acc);
-      for_runs<G, 0, G::FR>(acc, d0, m0, P.D, P.M, [&](int i, int j, int q, int d, int m) {
-        float* const o = P.dx + static_cast<int64_t>(m) * P.D + d;
-        float v[4];
-        load4<E>(o, v);  // (this lane's own of the first product)
+__global__ void __launch_bounds__(256) ffn_join(Products Q) {
+  const Product& P = Q.p[blockIdx.y];
+  const int64_t n = static_cast<int64_t>(P.rows) * P.cols;
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (P.slices < 2 || i >= n) return;
+  float s[8];
+  load8<F32>(P.part + i, s);
+#pragma unroll 4
+  for (int k = 1; k < P.slices; ++k) {
+    float v[8];
+    load8<F32>(P.part + k * n + i, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += acc[i][j][4 * q + e];
-        store4<E>(o, v);
-      });
-    }
-    return;
+    for (int e = 0; e < 8; ++e) s[e] += v[e];
   }
-  w -= P.n_dx;
-  using G = typename E::template G<LL::MC, LL::MC>;
-  f32x16 acc[G::FR][G::FC];
-  if (w < 2 * P.n_w) {  // rows d, columns f
-    w = xcd_swz(w, 2 * P.n_w);
-    const bool up = w >= P.n_w;
-    w = up ? w - P.n_w : w;
-    const int d0 = w % nD * kT, f0 = w / nD * kT;
-    const Op A{P.x, P.D, P.D, P.M, nullptr}, B{up ? P.db : P.da, P.F, P.F, P.M, nullptr};
-    G::run(A, B, d0, f0, 0, P.M, st, acc);
-    put_tile<E, G>(acc, d0, f0, P.D, P.F, up ? P.dwu : P.dwg);
-    return;
-  }
-  w = xcd_swz(w - 2 * P.n_w, P.n_d);  // rows f, columns o
-  const int nO = (P.O + kT - 1) / kT;
-  const int o0 = w % nO * kT, f0 = w / nO * kT;
-  (void)nF;
-  const Op A{P.h, P.F, P.F, P.M, nullptr}, B{P.dy, P.O, P.O, P.M, nullptr};
-  G::run(A, B, f0, o0, 0, P.M, st, acc);
-  put_tile<E, G>(acc, f0, o0, P.F, P.O, P.dwd);
+  store8<E>(static_cast<typename E::T*>(P.out) + i, s);
 }
 
 int tiles(int n, int t = kT) { return (n + t - 1) / t; }
 
+// Slices.  A launch on 256 compute units takes at most whole rounds of its longest workgroup, and of workgroups
+// of several lengths, longest first, about the work of one unit and half the shortest; a k-step (32 deep in
+// bf16, 16 in float) takes 0.95 or 1.6 us, a workgroup 6 us more, sliced sums cost 5 us and their bytes at 3 TB/s
+// (written beside products, read again from the caches), within kPartBytes.  Tried are the depths that cut the longest product into 1 to 16.
+constexpr size_t kPartBytes = size_t{128} << 20;
+void plan(Products& Q, bool bf) {
+  const double step = bf ? 0.95 / 32 : 1.6 / 16;
+  int longest = 0;
+  for (int i = 0; i < Q.n; ++i) longest = std::max(longest, Q.p[i].A2 ? 2 * Q.p[i].kp : Q.p[i].kp);
+  double best = -1;
+  int best_s[4] = {1, 1, 1, 1};
+  for (int cut = 1; cut <= 16; ++cut) {
+    const int depth = std::max((longest + cut - 1) / cut, 128);
+    double work = 0, most = 0, least = 1e30, bytes = 0;
+    int s[4], count = 0;
+    for (int i = 0; i < Q.n; ++i) {
+      const Product& P = Q.p[i];
+      const int halves = P.A2 ? 2 : 1;
+      s[i] = std::max((P.kp * halves + depth - 1) / depth, 1);
+      if (P.A2 && !bf) s[i] = 2 * std::max((P.kp + depth - 1) / depth, 1);
+      const double len = static_cast<double>(P.kp) * halves / s[i] * step + 6;
+      work += len * s[i] * tiles(P.rows) * tiles(P.cols);
+      most = std::max(most, len);
+      least = std::min(least, len);
+      count += s[i] * tiles(P.rows) * tiles(P.cols);
+      if (s[i] > 1) bytes += 4.0 * s[i] * P.rows * P.cols;
+    }
+    // (a float product of two halves is sliced whatever its room: cut 1 stays)
+    if (cut > 1 && bytes > kPartBytes) break;
+    const double rounds = (count + 255) / 256 * most;
+    const double launch = Q.n == 1 ? rounds : std::min(rounds, std::max(work / 256 + least / 2, most));
+    const double t = launch + (bytes > 0 ? 5 + bytes / 3.0e6 : 0);
+    if (best < 0 || t < best) {
+      best = t;
+      for (int i = 0; i < Q.n; ++i) best_s[i] = s[i];
+    }
+  }
+  for (int i = 0; i < Q.n; ++i) {
+    Product& P = Q.p[i];
+    const int halves = P.A2 ? 2 : 1;
+    if (P.A2 && !bf) {  // slices end where the first half does
+      const int per = best_s[i] / 2;
+      P.depth = ((P.kp + per - 1) / per + 31) / 32 * 32;
+      P.slices = 2 * per;
+      if (P.depth * per != P.kp) P.kp = P.depth * per;
+    } else {
+      P.depth = ((P.kp * halves + best_s[i] - 1) / best_s[i] + 31) / 32 * 32;
+      P.slices = (P.kp * halves + P.depth - 1) / P.depth;
+    }
+  }
+}
+
+// Bytes of the sliced sums, and their places from `part` on.
+size_t place_parts(Products& Q, char* part) {
+  size_t at = 0;
+  for (int i = 0; i < Q.n; ++i) {
+    Product& P = Q.p[i];
+    P.part = reinterpret_cast<float*>(part + at);
+    if (P.slices > 1) at += align_up(static_cast<size_t>(P.slices) * P.rows * P.cols * 4, 256);
+  }
+  return at;
+}
+
+Product product(const void* A, int pa, const void* B, int pb, bool mc_b, int rows, int cols, int K, void* out) {
+  Product P{};
+  P.A = A;
+  P.B = B;
+  P.pa = pa;
+  P.pb = pb;
+  P.mc_b = mc_b;
+  P.rows = rows;
+  P.cols = cols;
+  P.K = K;
+  P.kp = (K + 31) / 32 * 32;
+  P.out = out;
+  return P;
+}
+
+template <class E, LL LA, bool KCB, bool MCB>
+hipError_t run_products(Products& Q, const char* name, hipStream_t stream) {
+  // longest first
+  std::stable_sort(Q.p, Q.p + Q.n, [](const Product& x, const Product& y) { return x.depth > y.depth; });
+  int total = 0;
+  int64_t joined = 0;
+  for (int i = 0; i < Q.n; ++i) {
+    Q.p[i].first = total;
+    total += tiles(Q.p[i].rows) * tiles(Q.p[i].cols) * Q.p[i].slices;
+    if (Q.p[i].slices > 1) joined = std::max(joined, static_cast<int64_t>(Q.p[i].rows) * Q.p[i].cols);
+  }
+  {
+    Prof pr(name, stream);
+    hipLaunchKernelGGL((ffn_products<E, LA, KCB, MCB>), dim3(total), dim3(512), 0, stream, Q);
+  }
+  if (joined > 0) {
+    Prof pr("ffn_join", stream);
+    hipLaunchKernelGGL(ffn_join<E>, dim3(static_cast<unsigned>((joined / 8 + 255) / 256), Q.n), dim3(256), 0, stream, Q);
+  }
+  return hipGetLastError();
+}
+
+Products down_products(const FfnArgs& q, const void* h, bool bf) {
+  Products Q{};
+  Q.n = 1;
+  Q.p[0] = product(q.wd, q.F, h, q.F, false, q.O, q.M, q.F, q.y);
+  plan(Q, bf);
+  return Q;
+}
+// The slices are those of all four, so that a gradient does not change with the others that are asked for.
+Products grad_products(const FfnArgs& q, const FfnGrads& g, const void* da, const void* db, const void* h, bool bf) {
+  Products Q{};
+  Q.n = 4;
+  Q.p[0] = product(q.wg, q.D, da, q.F, false, q.D, q.M, q.F, g.dx);
+  Q.p[0].A2 = q.wu;
+  Q.p[0].B2 = db;
+  Q.p[1] = product(q.x, q.D, da, q.F, true, q.D, q.F, q.M, g.dwg);
+  Q.p[2] = product(q.x, q.D, db, q.F, true, q.D, q.F, q.M, g.dwu);
+  Q.p[3] = product(h, q.F, g.dy, q.O, true, q.F, q.O, q.M, g.dwd);
+  plan(Q, bf);
+  return Q;
+}
+
 template <class E>
-hipError_t forward(const FfnArgs& q, void* h, hipStream_t stream) {
+hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
   using T = typename E::T;
+  if (q.M <= kFew) {
+    Prof pr("ffn_few", stream);
+    const FewArgs<E> p{static_cast<const T*>(q.x), static_cast<const T*>(q.wg), static_cast<const T*>(q.wu),
+                       static_cast<T*>(h), static_cast<T*>(q.a), static_cast<T*>(q.b), q.M, q.D, q.F};
+    if (q.act == kSilu) launch_few<E, 2, kSilu>(p, stream);
+    else launch_few<E, 2, kGelu>(p, stream);
+    const FewArgs<E> d{static_cast<const T*>(h), static_cast<const T*>(q.wd), nullptr, static_cast<T*>(q.y), nullptr,
+                       nullptr, q.M, q.F, q.O};
+    launch_few<E, 1, kSilu>(d, stream);
+    return hipGetLastError();
+  }
+  // The rows past the last whole tile go without tiles where that saves a round of the chip (M = 4,215, 512 x 2,048,
+  // float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
+  const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
+  const bool apart = rest > 0 && rest <= kFew && (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256;
+  const int m = apart ? q.M - rest : q.M;
   PairArgs<E> p{static_cast<const T*>(q.x),  static_cast<const T*>(q.wg), static_cast<const T*>(q.wu),
-                static_cast<T*>(h), static_cast<T*>(q.a), static_cast<T*>(q.b), q.M, q.D, q.F};
+                static_cast<T*>(h), static_cast<T*>(q.a), static_cast<T*>(q.b), m, q.D, q.F};
+  if (apart) {
+    Prof pr("ffn_few", stream);
+    const int64_t at = static_cast<int64_t>(m) * q.F;
+    const FewArgs<E> f{p.x + static_cast<int64_t>(m) * q.D, p.wg, p.wu, p.h + at, p.a ? p.a + at : nullptr,
+                       p.b ? p.b + at : nullptr, rest, q.D, q.F};
+    if (q.act == kSilu) launch_few<E, 2, kSilu>(f, stream);
+    else launch_few<E, 2, kGelu>(f, stream);
+  }
   {
     Prof pr("ffn_pair", stream);
-    const dim3 grid(grouped_grid(tiles(q.M), tiles(q.F, kT / 2)));
+    const dim3 grid(grouped_grid(tiles(m), nF));
     if (q.act == kSilu) hipLaunchKernelGGL((ffn_pair<E, kSilu>), grid, dim3(512), 0, stream, p);
     else hipLaunchKernelGGL((ffn_pair<E, kGelu>), grid, dim3(512), 0, stream, p);
   }
-  DownArgs<E> d{static_cast<const T*>(h), static_cast<const T*>(q.wd), static_cast<T*>(q.y), q.M, q.F, q.O};
-  Prof pr("ffn_down", stream);
-  hipLaunchKernelGGL((ffn_down<E>), dim3(grouped_grid(tiles(q.M), tiles(q.O))), dim3(512), 0, stream, d);
-  return hipGetLastError();
+  Products Q = down_products(q, h, E::kBf);
+  place_parts(Q, part);
+  return run_products<E, LL::KC, true, false>(Q, "ffn_down", stream);
 }
 
 template <class E>
@@ -340,42 +727,36 @@ hipError_t backward(const FfnArgs& q, const FfnGrads& g, char* ws, hipStream_t s
     if (q.act == kSilu) hipLaunchKernelGGL((ffn_back<E, kSilu>), grid, dim3(512), 0, stream, b);
     else hipLaunchKernelGGL((ffn_back<E, kGelu>), grid, dim3(512), 0, stream, b);
   }
-  GradArgs<E> p{};
-  p.x = static_cast<const T*>(q.x);
-  p.dy = static_cast<const T*>(g.dy);
-  p.wg = static_cast<const T*>(q.wg);
-  p.wu = static_cast<const T*>(q.wu);
-  p.da = da;
-  p.db = db;
-  p.h = h;
-  p.dx = static_cast<T*>(g.dx);
-  p.dwg = static_cast<T*>(g.dwg);
-  p.dwu = static_cast<T*>(g.dwu);
-  p.dwd = static_cast<T*>(g.dwd);
-  p.M = q.M;
-  p.D = q.D;
-  p.F = q.F;
-  p.O = q.O;
-  p.n_dx = g.dx ? tiles(q.M) * tiles(q.D) : 0;
-  p.n_w = g.dwg ? tiles(q.F) * tiles(q.D) : 0;
-  p.n_d = g.dwd ? tiles(q.F) * tiles(q.O) : 0;
-  const int total = p.n_dx + 2 * p.n_w + p.n_d;
-  if (total > 0) {
-    Prof pr("ffn_grads", stream);
-    hipLaunchKernelGGL((ffn_grads<E>), dim3(total), dim3(512), 0, stream, p);
-  }
-  return hipGetLastError();
+  Products Q = grad_products(q, g, da, db, h, E::kBf);
+  place_parts(Q, ws + 3 * n);
+  Q.n = static_cast<int>(std::remove_if(Q.p, Q.p + Q.n, [](const Product& P) { return !P.out; }) - Q.p);
+  if (Q.n == 0) return hipGetLastError();
+  return run_products<E, LL::MC, true, true>(Q, "ffn_grads", stream);
 }
 
 }  // namespace
 
-size_t ffn_workspace_bytes(int dtype, int M, int F, bool back) {
-  const size_t n = align_up(static_cast<size_t>(M > 0 ? M : 1) * F * (dtype == 1 ? 2 : 4), 256);
-  return back ? 3 * n : n;
+static size_t ffn_values_bytes(int dtype, int M, int F) {
+  return align_up(static_cast<size_t>(M > 0 ? M : 1) * F * (dtype == 1 ? 2 : 4), 256);
+}
+
+size_t ffn_workspace_bytes(int dtype, const FfnArgs& q, bool back) {
+  const size_t n = ffn_values_bytes(dtype, q.M, q.F);
+  if (q.M == 0) return n;
+  if (!back) {
+    if (q.M <= kFew) return n;
+    Products Q = down_products(q, nullptr, dtype == 1);
+    return n + place_parts(Q, nullptr);
+  }
+  FfnArgs w = q;
+  w.wu = &w;  // (that there is a second half)
+  Products Q = grad_products(w, FfnGrads{}, nullptr, nullptr, nullptr, dtype == 1);
+  return 3 * n + place_parts(Q, nullptr);
 }
 
 hipError_t launch_gated_ffn(int dtype, const FfnArgs& q, void* ws, hipStream_t stream) {
-  return dtype == 1 ? forward<B16>(q, ws, stream) : forward<F32>(q, ws, stream);
+  char* const part = static_cast<char*>(ws) + ffn_values_bytes(dtype, q.M, q.F);
+  return dtype == 1 ? forward<B16>(q, ws, part, stream) : forward<F32>(q, ws, part, stream);
 }
 
 hipError_t launch_gated_ffn_backward(int dtype, const FfnArgs& q, const FfnGrads& g, void* ws, hipStream_t stream) {

@@ -1308,7 +1308,12 @@ static bool ffn_args_ok(pctc_dtype dtype, int32_t M, int32_t D, int32_t F, int32
 
 size_t pctc_gated_ffn_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t F, int32_t O, int32_t backward) {
   if (!ffn_args_ok(dtype, M, D, F, O)) return 0;
-  return ffn_workspace_bytes(dtype == PCTC_BF16 ? 1 : 0, M, F, backward != 0);
+  FfnArgs q{};
+  q.M = M;
+  q.D = D;
+  q.F = F;
+  q.O = O;
+  return ffn_workspace_bytes(dtype == PCTC_BF16 ? 1 : 0, q, backward != 0);
 }
 
 // The block's inputs and outputs: aligned, there where they must be, and what is written apart from the rest.

@@ -367,7 +367,7 @@ struct FfnGrads {
   const void* dy;
   void *dx, *dwg, *dwu, *dwd;  // null: not wanted (dwg and dwu go together)
 };
-size_t ffn_workspace_bytes(int dtype, int M, int F, bool back);
+size_t ffn_workspace_bytes(int dtype, const FfnArgs& q, bool back);  // q: its sizes alone count
 hipError_t launch_gated_ffn(int dtype, const FfnArgs& q, void* ws, hipStream_t stream);
 hipError_t launch_gated_ffn_backward(int dtype, const FfnArgs& q, const FfnGrads& g, void* ws, hipStream_t stream);
 
