@@ -491,10 +491,10 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
  *   a = x Wg^T,  b = x Wu^T,  h = act(a) b,  y = h Wd^T          act: PCTC_SILU a / (1 + exp(-a)),
  *                                                                PCTC_GELU a (1 + erf(a / sqrt 2)) / 2
  *   x [M, D], w_gate and w_up [F, D], w_down [O, F], y [M, O], all device, dtype, 16-byte aligned.  M >= 0;
- *   D, F and O positive multiples of 8, at most PCTC_MAX_DIM.  Products are summed in float; a, b, h (and in the
- *   backward dh b act'(a) and dh act(a)) are rounded to dtype as operands of the next product, and every
+ *   D, F and O positive multiples of 8, at most PCTC_MAX_DIM.  Products are summed in float; h (and in the
+ *   backward dh b act'(a) and dh act(a)) is rounded to dtype as an operand of the next product, and every
  *   output once.
- *   gate, up [M, F]: a and b, kept for the backward; both NULL or neither.
+ *   gate, up: device float [M, F], a and b, kept for the backward; both NULL or neither.
  * pctc_gated_ffn_backward: from dy [M, O] and the forward's x, gate and up the gradients dx [M, D], dw_gate and
  *   dw_up [F, D] (both or neither) and dw_down [O, F]; those that are NULL are not formed.
  * What is written must not overlap another buffer of the call.  workspace: pctc_gated_ffn_workspace_size() bytes
@@ -503,10 +503,10 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
 enum { PCTC_SILU = 0, PCTC_GELU = 1 };
 size_t pctc_gated_ffn_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t F, int32_t O, int32_t backward);
 int32_t pctc_gated_ffn(pctc_dtype dtype, const void* x, int32_t M, int32_t D, const void* w_gate, const void* w_up,
-                       int32_t F, const void* w_down, int32_t O, int32_t activation, void* gate, void* up, void* y,
+                       int32_t F, const void* w_down, int32_t O, int32_t activation, float* gate, float* up, void* y,
                        void* workspace, size_t workspace_bytes, void* stream);
 int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x, int32_t M, int32_t D,
-                                const void* gate, const void* up, const void* w_gate, const void* w_up, int32_t F,
+                                const float* gate, const float* up, const void* w_gate, const void* w_up, int32_t F,
                                 const void* w_down, int32_t O, int32_t activation, void* dx, void* dw_gate,
                                 void* dw_up, void* dw_down, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -12,8 +12,10 @@
 //   ffn_back      dh, whose epilogue reads a and b and writes da, db and h (formed again);
 //   ffn_products  dx and the three weight gradients, which need only what is there by then, in one launch.
 // Every product is laid out with the output's contiguous dimension as the tile's rows, so that a lane's
-// accumulators are runs of 4 output values.  a, b, h, da and db are kept in the type of x: they are
-// operands of the next products.
+// accumulators are runs of 4 output values.  h, da and db have the type of x, being operands of the next
+// products; a and b are kept in float: rounded to bf16 they alone would make the gradients' error of two
+// roundings (an operand's and the result's, 0.0023) one of four (0.0035; 14 us of 1,770 saved at M = 2,567,
+// 4,096 x 10,240).
 // Bound by the matrix products, 6 M D F operations forward and 12 M D F backward, for few rows by reading the
 // weights.
 #include <algorithm>
@@ -28,7 +30,7 @@ namespace {
 
 using bf::LL;
 
-constexpr int kFew = 128;  // rows of x that the forward takes without tiles
+constexpr int kFew = 512;  // most rows of x that the forward takes without tiles
 constexpr int kT = 256;  // tile rows and columns
 constexpr int kWc = 4;   // wavefronts across a tile's columns (two across its rows)
 
@@ -97,6 +99,19 @@ __device__ __forceinline__ void act_grad(float a, float& f, float& d) {
   f = a * c;
   if constexpr (ACT == kSilu) d = fmaf(f, 1.f - c, c);
   else d = fmaf(a * 0.3989422804014327f, e, c);
+}
+
+// From dh, a and b: h, and da in a's place, db in b's.
+template <int ACT>
+__device__ __forceinline__ void back_values(const float (&dh)[8], float (&a)[8], float (&b)[8], float (&h)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float f, d;
+    act_grad<ACT>(a[e], f, d);
+    h[e] = f * b[e];
+    a[e] = dh[e] * b[e] * d;
+    b[e] = dh[e] * f;
+  }
 }
 
 // ---- eight consecutive values (16-byte aligned) --------------------------------------------
@@ -222,7 +237,8 @@ __device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* co
 template <class E>
 struct FewArgs {
   const typename E::T *x, *w0, *w1;
-  typename E::T *out, *a, *b;  // a and b null: not kept
+  typename E::T* out;
+  float *a, *b;  // null: not kept
   int M, K, R;
 };
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -340,8 +356,8 @@ __global__ void __launch_bounds__(WAVES * 64) ffn_few(FewArgs<E> P) {
       for (int e = 0; e < 4; ++e) h[e] = act<ACT>(v[0][e]) * v[1][e];
       store4<E>(P.out + at, h);
       if (P.a) {
-        store4<E>(P.a + at, v[0]);
-        store4<E>(P.b + at, v[1]);
+        store4<F32>(P.a + at, v[0]);
+        store4<F32>(P.b + at, v[1]);
       }
     } else {
       store4<E>(P.out + at, v[0]);
@@ -371,7 +387,8 @@ void launch_few(const FewArgs<E>& P, hipStream_t stream) {
 template <class E>
 struct PairArgs {
   const typename E::T *x, *wg, *wu;
-  typename E::T *h, *a, *b;  // a and b null: not kept
+  typename E::T* h;
+  float *a, *b;  // null: not kept
   int M, D, F;
 };
 
@@ -402,7 +419,7 @@ __global__ void __launch_bounds__(512, 1) ffn_pair(PairArgs<E> P) {
       h[e] = act<ACT>(block < 8 ? v[e] : o) * (block < 8 ? o : v[e]);
     }
     if (in && block < 8) store8<E>(P.h + at, h);
-    if (in && P.a) store8<E>((block < 8 ? P.a : P.b) + at, v);
+    if (in && P.a) store8<F32>((block < 8 ? P.a : P.b) + at, v);
   });
 }
 
@@ -410,7 +427,8 @@ __global__ void __launch_bounds__(512, 1) ffn_pair(PairArgs<E> P) {
 
 template <class E>
 struct BackArgs {
-  const typename E::T *dy, *wd, *a, *b;
+  const typename E::T *dy, *wd;
+  const float *a, *b;
   typename E::T *da, *db, *h;
   int M, F, O;
 };
@@ -429,7 +447,7 @@ __global__ void __launch_bounds__(512, 1) ffn_back(BackArgs<E> P) {
   const int wave = threadIdx.x >> 6;
   const int fw = ft * kT + wave / kWc * 128, mw = mt * kT + wave % kWc * 64;
   struct AB {
-    typename Raw<E>::Eight a, b;
+    Raw<F32>::Eight a, b;
   };
   // (places outside read the tile's first: no branch between the reads)
   by_columns<G, AB>(
@@ -439,16 +457,9 @@ __global__ void __launch_bounds__(512, 1) ffn_back(BackArgs<E> P) {
         if (f >= P.F || m >= P.M) return;
         const int64_t at = static_cast<int64_t>(m) * P.F + f;
         float a[8], b[8], h[8];
-        Raw<E>::values(x.a, a);
-        Raw<E>::values(x.b, b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float fa, ga;
-          act_grad<ACT>(a[e], fa, ga);
-          h[e] = fa * b[e];
-          a[e] = dh[e] * b[e] * ga;
-          b[e] = dh[e] * fa;
-        }
+        Raw<F32>::values(x.a, a);
+        Raw<F32>::values(x.b, b);
+        back_values<ACT>(dh, a, b, h);
         store8<E>(P.da + at, a);
         store8<E>(P.db + at, b);
         store8<E>(P.h + at, h);
@@ -456,8 +467,8 @@ __global__ void __launch_bounds__(512, 1) ffn_back(BackArgs<E> P) {
       [&](int block, int col, AB& x) {
         const int f = fw + block * 8, m = mw + col;
         const int64_t at = f < P.F && m < P.M ? static_cast<int64_t>(m) * P.F + f : 0;
-        x.a = *reinterpret_cast<const typename Raw<E>::Eight*>(P.a + at);
-        x.b = *reinterpret_cast<const typename Raw<E>::Eight*>(P.b + at);
+        x.a = *reinterpret_cast<const Raw<F32>::Eight*>(P.a + at);
+        x.b = *reinterpret_cast<const Raw<F32>::Eight*>(P.b + at);
       });
 }
 
@@ -466,7 +477,8 @@ __global__ void __launch_bounds__(512, 1) ffn_back(BackArgs<E> P) {
 // out[c][r] = sum over k of A[r][k] B[c][k] (+ A2[r][k] B2[c][k]), r < rows, c < cols, for up to four
 // products in one launch, each cut along k into `slices` of `depth` (a multiple of 32; the second operands' k
 // begins at kp, K rounded up to it).  A product of one slice is written as it is to be; of several, every
-// slice's float sums are written and ffn_join adds them in order.
+// slice's float sums are written and ffn_join adds them in order.  Without `out` the sums are always written,
+// for join_pair or join_back, which make something else of them.
 struct Product {
   const void *A, *B, *A2, *B2;  // A2 null: none
   void* out;
@@ -522,7 +534,7 @@ __global__ void __launch_bounds__(512, 1) ffn_products(Products Q) {
   }
   const int wave = threadIdx.x >> 6;
   const int rw = r0 + wave / kWc * 128, cw = c0 + wave % kWc * 64;
-  float* const part = P.slices > 1 ? P.part + static_cast<int64_t>(slice) * P.rows * P.cols : nullptr;
+  float* const part = P.slices > 1 || !P.out ? P.part + static_cast<int64_t>(slice) * P.rows * P.cols : nullptr;
   by_columns<GK>(acc, st, [&](int block, int col, const float (&v)[8]) {
     const int r = rw + block * 8, c = cw + col;
     if (r >= P.rows || c >= P.cols) return;
@@ -532,14 +544,9 @@ __global__ void __launch_bounds__(512, 1) ffn_products(Products Q) {
   });
 }
 
-// The sliced products' sums; blockIdx.y: product.
-template <class E>
-__global__ void __launch_bounds__(256) ffn_join(Products Q) {
-  const Product& P = Q.p[blockIdx.y];
+// Eight of a product's values from its slices' sums.
+__device__ __forceinline__ void joined(const Product& P, int64_t i, float (&s)[8]) {
   const int64_t n = static_cast<int64_t>(P.rows) * P.cols;
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
-  if (P.slices < 2 || i >= n) return;
-  float s[8];
   load8<F32>(P.part + i, s);
 #pragma unroll 4
   for (int k = 1; k < P.slices; ++k) {
@@ -548,7 +555,49 @@ __global__ void __launch_bounds__(256) ffn_join(Products Q) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[e] += v[e];
   }
+}
+
+// The sliced products' sums; blockIdx.y: product.
+template <class E>
+__global__ void __launch_bounds__(256) ffn_join(Products Q) {
+  const Product& P = Q.p[blockIdx.y];
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (P.slices < 2 || i >= static_cast<int64_t>(P.rows) * P.cols) return;
+  float s[8];
+  joined(P, i, s);
   store8<E>(static_cast<typename E::T*>(P.out) + i, s);
+}
+
+// Both projections' sums (products 0 and 1) to h, and a and b where they are kept.
+template <class E, int ACT>
+__global__ void __launch_bounds__(256) join_pair(Products Q, typename E::T* h, float* pa, float* pb) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (i >= static_cast<int64_t>(Q.p[0].rows) * Q.p[0].cols) return;
+  float a[8], b[8], v[8];
+  joined(Q.p[0], i, a);
+  joined(Q.p[1], i, b);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = act<ACT>(a[e]) * b[e];
+  store8<E>(h + i, v);
+  if (pa) {
+    store8<F32>(pa + i, a);
+    store8<F32>(pb + i, b);
+  }
+}
+
+// dh's sums to da, db and h.
+template <class E, int ACT>
+__global__ void __launch_bounds__(256) join_back(Products Q, BackArgs<E> P) {
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (i >= static_cast<int64_t>(P.M) * P.F) return;
+  float dh[8], a[8], b[8], h[8];
+  joined(Q.p[0], i, dh);
+  load8<F32>(P.a + i, a);
+  load8<F32>(P.b + i, b);
+  back_values<ACT>(dh, a, b, h);
+  store8<E>(P.da + i, a);
+  store8<E>(P.db + i, b);
+  store8<E>(P.h + i, h);
 }
 
 int tiles(int n, int t = kT) { return (n + t - 1) / t; }
@@ -558,8 +607,10 @@ int tiles(int n, int t = kT) { return (n + t - 1) / t; }
 // bf16, 16 in float) takes 0.95 or 1.6 us, a workgroup 6 us more, sliced sums cost 5 us and their bytes at 3 TB/s
 // (written beside products, read again from the caches), within kPartBytes.  Tried are the depths that cut the longest product into 1 to 16.
 constexpr size_t kPartBytes = size_t{128} << 20;
-void plan(Products& Q, bool bf) {
-  const double step = bf ? 0.95 / 32 : 1.6 / 16;
+double step_us(bool bf) { return bf ? 0.95 / 32 : 1.6 / 16; }  // per k
+// Returns the time by this model.  always_joined: one slice is joined too.
+double plan(Products& Q, bool bf, bool always_joined = false) {
+  const double step = step_us(bf);
   int longest = 0;
   for (int i = 0; i < Q.n; ++i) longest = std::max(longest, Q.p[i].A2 ? 2 * Q.p[i].kp : Q.p[i].kp);
   double best = -1;
@@ -578,7 +629,7 @@ void plan(Products& Q, bool bf) {
       most = std::max(most, len);
       least = std::min(least, len);
       count += s[i] * tiles(P.rows) * tiles(P.cols);
-      if (s[i] > 1) bytes += 4.0 * s[i] * P.rows * P.cols;
+      if (s[i] > 1 || always_joined) bytes += 4.0 * s[i] * P.rows * P.cols;
     }
     // (a float product of two halves is sliced whatever its room: cut 1 stays)
     if (cut > 1 && bytes > kPartBytes) break;
@@ -603,15 +654,16 @@ void plan(Products& Q, bool bf) {
       P.slices = (P.kp * halves + P.depth - 1) / P.depth;
     }
   }
+  return best;
 }
 
 // Bytes of the sliced sums, and their places from `part` on.
-size_t place_parts(Products& Q, char* part) {
+size_t place_parts(Products& Q, char* part, bool always_joined = false) {
   size_t at = 0;
   for (int i = 0; i < Q.n; ++i) {
     Product& P = Q.p[i];
     P.part = reinterpret_cast<float*>(part + at);
-    if (P.slices > 1) at += align_up(static_cast<size_t>(P.slices) * P.rows * P.cols * 4, 256);
+    if (P.slices > 1 || always_joined) at += align_up(static_cast<size_t>(P.slices) * P.rows * P.cols * 4, 256);
   }
   return at;
 }
@@ -636,19 +688,19 @@ hipError_t run_products(Products& Q, const char* name, hipStream_t stream) {
   // longest first
   std::stable_sort(Q.p, Q.p + Q.n, [](const Product& x, const Product& y) { return x.depth > y.depth; });
   int total = 0;
-  int64_t joined = 0;
+  int64_t most = 0;  // values to join
   for (int i = 0; i < Q.n; ++i) {
     Q.p[i].first = total;
     total += tiles(Q.p[i].rows) * tiles(Q.p[i].cols) * Q.p[i].slices;
-    if (Q.p[i].slices > 1) joined = std::max(joined, static_cast<int64_t>(Q.p[i].rows) * Q.p[i].cols);
+    if (Q.p[i].slices > 1 && Q.p[i].out) most = std::max(most, static_cast<int64_t>(Q.p[i].rows) * Q.p[i].cols);
   }
   {
     Prof pr(name, stream);
     hipLaunchKernelGGL((ffn_products<E, LA, KCB, MCB>), dim3(total), dim3(512), 0, stream, Q);
   }
-  if (joined > 0) {
+  if (most > 0) {
     Prof pr("ffn_join", stream);
-    hipLaunchKernelGGL(ffn_join<E>, dim3(static_cast<unsigned>((joined / 8 + 255) / 256), Q.n), dim3(256), 0, stream, Q);
+    hipLaunchKernelGGL(ffn_join<E>, dim3(static_cast<unsigned>((most / 8 + 255) / 256), Q.n), dim3(256), 0, stream, Q);
   }
   return hipGetLastError();
 }
@@ -660,6 +712,39 @@ Products down_products(const FfnArgs& q, const void* h, bool bf) {
   plan(Q, bf);
   return Q;
 }
+
+// How the projections are formed.  The times are those of plan()'s model, and for few rows what was measured:
+// the weights at 5.3 TB/s and as much again for every 40 rows (32 in float; bf16, 4,096 x 10,240, the whole
+// block: 1 row 52 us, 16 rows 68, 64 130, 128 210).
+enum class Pair { kFew, kTiles, kSliced };
+double few_us(const FfnArgs& q, bool bf, double weights) {
+  return 6 + weights * (bf ? 2 : 4) / 5.3e6 * (1 + q.M / (bf ? 40.0 : 32.0));
+}
+double tiles_us(int count, int K, bool bf) { return (count + 255) / 256 * (K * step_us(bf) + (bf ? 10 : 25)); }
+Pair pair_plan(const FfnArgs& q, bool bf, Products& Q) {
+  Q = Products{};
+  Q.n = 2;
+  Q.p[0] = product(q.wg, q.D, q.x, q.D, false, q.F, q.M, q.D, nullptr);
+  Q.p[1] = product(q.wu, q.D, q.x, q.D, false, q.F, q.M, q.D, nullptr);
+  const double sliced = plan(Q, bf, true), whole = tiles_us(tiles(q.M) * tiles(q.F, kT / 2), q.D, bf);
+  if (q.M <= kFew && few_us(q, bf, 2.0 * q.D * q.F) <= std::min(sliced, whole)) return Pair::kFew;
+  return sliced < whole ? Pair::kSliced : Pair::kTiles;
+}
+bool down_by_few(const FfnArgs& q, bool bf) {
+  if (q.M > kFew) return false;
+  Products Q{};
+  Q.n = 1;
+  Q.p[0] = product(nullptr, q.F, nullptr, q.F, false, q.O, q.M, q.F, nullptr);
+  return few_us(q, bf, static_cast<double>(q.O) * q.F) <= plan(Q, bf);
+}
+// dh by slices (then Q is their plan), or whole tiles with the activation's part in their epilogue.
+bool back_sliced(const FfnArgs& q, const void* dy, bool bf, Products& Q) {
+  Q = Products{};
+  Q.n = 1;
+  Q.p[0] = product(q.wd, q.F, dy, q.O, false, q.F, q.M, q.O, nullptr);
+  return plan(Q, bf, true) < tiles_us(tiles(q.M) * tiles(q.F), q.O, bf);
+}
+
 // The slices are those of all four, so that a gradient does not change with the others that are asked for.
 Products grad_products(const FfnArgs& q, const FfnGrads& g, const void* da, const void* db, const void* h, bool bf) {
   Products Q{};
@@ -677,39 +762,50 @@ Products grad_products(const FfnArgs& q, const FfnGrads& g, const void* da, cons
 template <class E>
 hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
   using T = typename E::T;
-  if (q.M <= kFew) {
+  T* const hh = static_cast<T*>(h);
+  float *const a = q.a, *const b = q.b;
+  const T *const x = static_cast<const T*>(q.x), *const wg = static_cast<const T*>(q.wg), *const wu = static_cast<const T*>(q.wu);
+  const bool silu = q.act == kSilu;
+  auto few = [&](int m0, int rows) {
     Prof pr("ffn_few", stream);
-    const FewArgs<E> p{static_cast<const T*>(q.x), static_cast<const T*>(q.wg), static_cast<const T*>(q.wu),
-                       static_cast<T*>(h), static_cast<T*>(q.a), static_cast<T*>(q.b), q.M, q.D, q.F};
-    if (q.act == kSilu) launch_few<E, 2, kSilu>(p, stream);
-    else launch_few<E, 2, kGelu>(p, stream);
-    const FewArgs<E> d{static_cast<const T*>(h), static_cast<const T*>(q.wd), nullptr, static_cast<T*>(q.y), nullptr,
-                       nullptr, q.M, q.F, q.O};
+    const int64_t at = static_cast<int64_t>(m0) * q.F;
+    const FewArgs<E> f{x + static_cast<int64_t>(m0) * q.D, wg, wu, hh + at, a ? a + at : nullptr, b ? b + at : nullptr,
+                       rows, q.D, q.F};
+    if (silu) launch_few<E, 2, kSilu>(f, stream);
+    else launch_few<E, 2, kGelu>(f, stream);
+  };
+  Products Q;
+  const Pair how = pair_plan(q, E::kBf, Q);
+  if (how == Pair::kFew) {
+    few(0, q.M);
+  } else if (how == Pair::kSliced) {
+    place_parts(Q, part, true);
+    const hipError_t e = run_products<E, LL::KC, true, false>(Q, "ffn_pair", stream);
+    if (e != hipSuccess) return e;
+    Prof pr("ffn_join", stream);
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(q.M) * q.F / 8 + 255) / 256));
+    if (silu) hipLaunchKernelGGL((join_pair<E, kSilu>), grid, dim3(256), 0, stream, Q, hh, a, b);
+    else hipLaunchKernelGGL((join_pair<E, kGelu>), grid, dim3(256), 0, stream, Q, hh, a, b);
+  } else {
+    // The rows past the last whole tile go without tiles where that saves a round of the chip (M = 4,215, 512 x
+    // 2,048, float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
+    const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
+    const bool apart = rest > 0 && rest <= kT / 2 && (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256;
+    const int m = apart ? q.M - rest : q.M;
+    if (apart) few(m, rest);
+    const PairArgs<E> p{x, wg, wu, hh, a, b, m, q.D, q.F};
+    Prof pr("ffn_pair", stream);
+    const dim3 grid(grouped_grid(tiles(m), nF));
+    if (silu) hipLaunchKernelGGL((ffn_pair<E, kSilu>), grid, dim3(512), 0, stream, p);
+    else hipLaunchKernelGGL((ffn_pair<E, kGelu>), grid, dim3(512), 0, stream, p);
+  }
+  if (down_by_few(q, E::kBf)) {
+    Prof pr("ffn_few", stream);
+    const FewArgs<E> d{hh, static_cast<const T*>(q.wd), nullptr, static_cast<T*>(q.y), nullptr, nullptr, q.M, q.F, q.O};
     launch_few<E, 1, kSilu>(d, stream);
     return hipGetLastError();
   }
-  // The rows past the last whole tile go without tiles where that saves a round of the chip (M = 4,215, 512 x 2,048,
-  // float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
-  const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
-  const bool apart = rest > 0 && rest <= kFew && (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256;
-  const int m = apart ? q.M - rest : q.M;
-  PairArgs<E> p{static_cast<const T*>(q.x),  static_cast<const T*>(q.wg), static_cast<const T*>(q.wu),
-                static_cast<T*>(h), static_cast<T*>(q.a), static_cast<T*>(q.b), m, q.D, q.F};
-  if (apart) {
-    Prof pr("ffn_few", stream);
-    const int64_t at = static_cast<int64_t>(m) * q.F;
-    const FewArgs<E> f{p.x + static_cast<int64_t>(m) * q.D, p.wg, p.wu, p.h + at, p.a ? p.a + at : nullptr,
-                       p.b ? p.b + at : nullptr, rest, q.D, q.F};
-    if (q.act == kSilu) launch_few<E, 2, kSilu>(f, stream);
-    else launch_few<E, 2, kGelu>(f, stream);
-  }
-  {
-    Prof pr("ffn_pair", stream);
-    const dim3 grid(grouped_grid(tiles(m), nF));
-    if (q.act == kSilu) hipLaunchKernelGGL((ffn_pair<E, kSilu>), grid, dim3(512), 0, stream, p);
-    else hipLaunchKernelGGL((ffn_pair<E, kGelu>), grid, dim3(512), 0, stream, p);
-  }
-  Products Q = down_products(q, h, E::kBf);
+  Q = down_products(q, h, E::kBf);
   place_parts(Q, part);
   return run_products<E, LL::KC, true, false>(Q, "ffn_down", stream);
 }
@@ -719,12 +815,21 @@ hipError_t backward(const FfnArgs& q, const FfnGrads& g, char* ws, hipStream_t s
   using T = typename E::T;
   const size_t n = align_up(static_cast<size_t>(q.M) * q.F * sizeof(T), 256);
   T *da = reinterpret_cast<T*>(ws), *db = reinterpret_cast<T*>(ws + n), *h = reinterpret_cast<T*>(ws + 2 * n);
-  BackArgs<E> b{static_cast<const T*>(g.dy), static_cast<const T*>(q.wd), static_cast<const T*>(q.a),
-                static_cast<const T*>(q.b), da, db, h, q.M, q.F, q.O};
-  {
+  const BackArgs<E> b{static_cast<const T*>(g.dy), static_cast<const T*>(q.wd), q.a, q.b, da, db, h, q.M, q.F, q.O};
+  const bool silu = q.act == kSilu;
+  Products B;
+  if (back_sliced(q, g.dy, E::kBf, B)) {
+    place_parts(B, ws + 3 * n, true);
+    const hipError_t e = run_products<E, LL::MC, true, true>(B, "ffn_back", stream);
+    if (e != hipSuccess) return e;
+    Prof pr("ffn_join", stream);
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(q.M) * q.F / 8 + 255) / 256));
+    if (silu) hipLaunchKernelGGL((join_back<E, kSilu>), grid, dim3(256), 0, stream, B, b);
+    else hipLaunchKernelGGL((join_back<E, kGelu>), grid, dim3(256), 0, stream, B, b);
+  } else {
     Prof pr("ffn_back", stream);
     const dim3 grid(grouped_grid(tiles(q.M), tiles(q.F)));
-    if (q.act == kSilu) hipLaunchKernelGGL((ffn_back<E, kSilu>), grid, dim3(512), 0, stream, b);
+    if (silu) hipLaunchKernelGGL((ffn_back<E, kSilu>), grid, dim3(512), 0, stream, b);
     else hipLaunchKernelGGL((ffn_back<E, kGelu>), grid, dim3(512), 0, stream, b);
   }
   Products Q = grad_products(q, g, da, db, h, E::kBf);
@@ -743,15 +848,22 @@ static size_t ffn_values_bytes(int dtype, int M, int F) {
 size_t ffn_workspace_bytes(int dtype, const FfnArgs& q, bool back) {
   const size_t n = ffn_values_bytes(dtype, q.M, q.F);
   if (q.M == 0) return n;
+  const bool bf = dtype == 1;
+  Products Q;
+  size_t part = 0;  // of one step at a time
   if (!back) {
-    if (q.M <= kFew) return n;
-    Products Q = down_products(q, nullptr, dtype == 1);
-    return n + place_parts(Q, nullptr);
+    if (pair_plan(q, bf, Q) == Pair::kSliced) part = place_parts(Q, nullptr, true);
+    if (!down_by_few(q, bf)) {
+      Q = down_products(q, nullptr, bf);
+      part = std::max(part, place_parts(Q, nullptr));
+    }
+    return n + part;
   }
+  if (back_sliced(q, nullptr, bf, Q)) part = place_parts(Q, nullptr, true);
   FfnArgs w = q;
   w.wu = &w;  // (that there is a second half)
-  Products Q = grad_products(w, FfnGrads{}, nullptr, nullptr, nullptr, dtype == 1);
-  return 3 * n + place_parts(Q, nullptr);
+  Q = grad_products(w, FfnGrads{}, nullptr, nullptr, nullptr, bf);
+  return 3 * n + std::max(part, place_parts(Q, nullptr));
 }
 
 hipError_t launch_gated_ffn(int dtype, const FfnArgs& q, void* ws, hipStream_t stream) {

@@ -1319,32 +1319,31 @@ size_t pctc_gated_ffn_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int
 // The block's inputs and outputs: aligned, there where they must be, and what is written apart from the rest.
 struct FfnBuffer {
   const void* p;
-  uint64_t values;
+  uint64_t bytes;
   bool needed, written;
 };
-static bool ffn_buffers_ok(pctc_dtype dtype, const FfnBuffer* b, int n) {
-  const uint64_t e = value_bytes(dtype);
+static bool ffn_buffers_ok(const FfnBuffer* b, int n) {
   for (int i = 0; i < n; ++i) {
-    if (b[i].values == 0) continue;
+    if (b[i].bytes == 0) continue;
     if ((b[i].needed && !b[i].p) || misaligned16(b[i].p)) return false;
     for (int j = 0; j < n; ++j)
-      if (j != i && b[i].written && (!b[j].written || j > i) && meets(b[i].p, e * b[i].values, b[j].p, e * b[j].values))
+      if (j != i && b[i].written && (!b[j].written || j > i) && meets(b[i].p, b[i].bytes, b[j].p, b[j].bytes))
         return false;
   }
   return true;
 }
 
 int32_t pctc_gated_ffn(pctc_dtype dtype, const void* x, int32_t M, int32_t D, const void* w_gate, const void* w_up,
-                       int32_t F, const void* w_down, int32_t O, int32_t activation, void* gate, void* up, void* y,
+                       int32_t F, const void* w_down, int32_t O, int32_t activation, float* gate, float* up, void* y,
                        void* workspace, size_t workspace_bytes, void* stream_ptr) {
   const size_t need = pctc_gated_ffn_workspace_size(dtype, M, D, F, O, 0);
   if (need == 0 || (activation != PCTC_SILU && activation != PCTC_GELU) || !gate != !up) return PCTC_EINVAL;
   if (M == 0) return PCTC_OK;
-  const uint64_t m = M, d = D, f = F, o = O;
+  const uint64_t e = value_bytes(dtype), m = M, d = e * D, f = F, o = e * O;
   const FfnBuffer b[] = {{x, m * d, true, false}, {w_gate, f * d, true, false}, {w_up, f * d, true, false},
-                         {w_down, o * f, true, false}, {gate, m * f, false, true}, {up, m * f, false, true},
+                         {w_down, o * f, true, false}, {gate, 4 * m * f, false, true}, {up, 4 * m * f, false, true},
                          {y, m * o, true, true}};
-  if (!ffn_buffers_ok(dtype, b, 7)) return PCTC_EINVAL;
+  if (!ffn_buffers_ok(b, 7)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (misaligned256(workspace)) return PCTC_EINVAL;
   const FfnArgs q{x, w_gate, w_up, w_down, gate, up, y, M, D, F, O, activation};
@@ -1354,21 +1353,21 @@ int32_t pctc_gated_ffn(pctc_dtype dtype, const void* x, int32_t M, int32_t D, co
 }
 
 int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x, int32_t M, int32_t D,
-                                const void* gate, const void* up, const void* w_gate, const void* w_up, int32_t F,
+                                const float* gate, const float* up, const void* w_gate, const void* w_up, int32_t F,
                                 const void* w_down, int32_t O, int32_t activation, void* dx, void* dw_gate,
                                 void* dw_up, void* dw_down, void* workspace, size_t workspace_bytes,
                                 void* stream_ptr) {
   const size_t need = pctc_gated_ffn_workspace_size(dtype, M, D, F, O, 1);
   if (need == 0 || (activation != PCTC_SILU && activation != PCTC_GELU) || !dw_gate != !dw_up) return PCTC_EINVAL;
-  const uint64_t m = M, d = D, f = F, o = O;
-  const FfnBuffer b[] = {{x, m * d, true, false}, {dy, m * o, true, false}, {gate, m * f, true, false},
-                         {up, m * f, true, false}, {w_gate, f * d, true, false}, {w_up, f * d, true, false},
+  const uint64_t e = value_bytes(dtype), m = M, d = e * D, f = F, o = e * O;
+  const FfnBuffer b[] = {{x, m * d, true, false}, {dy, m * o, true, false}, {gate, 4 * m * f, true, false},
+                         {up, 4 * m * f, true, false}, {w_gate, f * d, true, false}, {w_up, f * d, true, false},
                          {w_down, o * f, true, false}, {dx, m * d, false, true}, {dw_gate, f * d, false, true},
                          {dw_up, f * d, false, true}, {dw_down, o * f, false, true}};
-  if (!ffn_buffers_ok(dtype, b, 11)) return PCTC_EINVAL;
+  if (!ffn_buffers_ok(b, 11)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (misaligned256(workspace)) return PCTC_EINVAL;
-  const FfnArgs q{x, w_gate, w_up, w_down, const_cast<void*>(gate), const_cast<void*>(up), nullptr, M, D, F, O, activation};
+  const FfnArgs q{x, w_gate, w_up, w_down, const_cast<float*>(gate), const_cast<float*>(up), nullptr, M, D, F, O, activation};
   const FfnGrads g{dy, dx, dw_gate, dw_up, dw_down};
   PCTC_HIP(launch_gated_ffn_backward(dtype == PCTC_BF16 ? 1 : 0, q, g, workspace, static_cast<hipStream_t>(stream_ptr)));
   prof_flush();

@@ -359,7 +359,7 @@ hipError_t launch_clear(void* p, int64_t bytes, hipStream_t stream);
 // ---- gated feed-forward block (gated_ffn.hip) -------------------------------------------------
 struct FfnArgs {
   const void *x, *wg, *wu, *wd;  // [M][D], [F][D] twice, [O][F]
-  void *a, *b;                   // [M][F]: written by the forward (null: not kept), read by the backward
+  float *a, *b;                  // [M][F]: written by the forward (null: not kept), read by the backward
   void* y;                       // [M][O], forward
   int M, D, F, O, act;
 };

@@ -1157,7 +1157,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
               *, stream=None) -> Dict[str, Optional[torch.Tensor]]:
     """Gated feed-forward block y = (act(x w_gate^T) * (x w_up^T)) w_down^T of x [..., D], bfloat16 or float32,
     for activation "silu" or "gelu" (by the error function); D, F and O multiples of 8.  Returns y [..., O] and, with
-    keep, gate and up [..., F], the two projections, which the backward reads (else None)."""
+    keep, gate and up [..., F] (float32), the two projections, which the backward reads (else None)."""
     L = lib()
     x, wg, wu, wd, (M, D, F, O), dt, act = _ffn_args(x, w_gate, w_up, w_down, activation)
     dev, lead = x.device, x.shape[:-1]
@@ -1165,7 +1165,7 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     if nbytes == 0:
         _check(-1, "pctc_gated_ffn")
     y = _out(out, (*lead, O), x.dtype, dev)
-    a, b = (torch.empty((*lead, F), dtype=x.dtype, device=dev) for _ in range(2)) if keep else (None, None)
+    a, b = (torch.empty((*lead, F), dtype=torch.float32, device=dev) for _ in range(2)) if keep else (None, None)
     ws = _scratch(nbytes, dev)
     code = L.pctc_gated_ffn(dt, x.data_ptr(), M, D, wg.data_ptr(), wu.data_ptr(), F, wd.data_ptr(), O, act,
                             a.data_ptr() if keep else None, b.data_ptr() if keep else None, y.data_ptr(), ws.data_ptr(),
@@ -1184,9 +1184,9 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up
     L = lib()
     x, wg, wu, wd, (M, D, F, O), dt, act = _ffn_args(x, w_gate, w_up, w_down, activation)
     dev, lead = x.device, x.shape[:-1]
-    for t, n, what in ((dy, O, "dy"), (gate, F, "gate"), (up, F, "up")):
-        if t.dtype is not x.dtype or t.device != dev or tuple(t.shape) != (*lead, n):
-            raise PrunedCTCError(-1, f"{what} must be {x.dtype} {(*lead, n)} on {dev}")
+    for t, n, kind, what in ((dy, O, x.dtype, "dy"), (gate, F, torch.float32, "gate"), (up, F, torch.float32, "up")):
+        if t.dtype is not kind or t.device != dev or tuple(t.shape) != (*lead, n):
+            raise PrunedCTCError(-1, f"{what} must be {kind} {(*lead, n)} on {dev}")
     dy, gate, up = dy.contiguous(), gate.contiguous(), up.contiguous()
     nbytes = L.pctc_gated_ffn_workspace_size(dt, M, D, F, O, 1)
     if nbytes == 0:

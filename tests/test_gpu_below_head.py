@@ -447,7 +447,7 @@ def product_error(A, B, eA, eB, extra=0):
 
 
 def check_ffn(c, act, dtype, got, grads=None):
-    """Bounds carried through the block.  a, b: their products' errors and one rounding to the type (e).  The
+    """Bounds carried through the block.  a, b: their products' errors.  The
     activation's slope is at most 1.13 (and its derivative's at most 0.8), and it is itself computed to
     within 2^-20 of its argument (exponential, error function and division of a few units in the last place
     each).  Products of two factors: each one's error times the other."""
@@ -464,15 +464,14 @@ def check_ffn(c, act, dtype, got, grads=None):
         ef = 1.13 * ea + small * np.abs(w["gate"])
         return (ef * np.abs(w["up"]) + np.abs(f) * eb + ef * eb) * (1 + e) + (e + 2 * F) * np.abs(w["h"]) + 1e-37, ef
 
-    eh, _ = h_error(raw_a, raw_b)  # the forward's h comes from unrounded projections
+    eh, ef = h_error(raw_a, raw_b)
     within(got["y"], w["y"], product_error(w["h"], wd, eh, z(wd)) * (1 + e) + e * np.abs(w["y"]) + 1e-37, "y")
-    ea, eb = raw_a * (1 + e) + e * np.abs(w["gate"]), raw_b * (1 + e) + e * np.abs(w["up"])
+    ea, eb = raw_a, raw_b
     if got["gate"] is not None:
         within(got["gate"], w["gate"], ea, "gate")
         within(got["up"], w["up"], eb, "up")
     if grads is None:
         return
-    eh, ef = h_error(ea, eb)
     edf = 0.8 * ea + small * (1 + np.abs(w["gate"]))
     edh = product_error(dy, wd.T, z(dy), z(wd.T))
     up, dh = np.abs(w["up"]), np.abs(w["dh"])
