@@ -21,10 +21,12 @@ namespace pctc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRankTokens = 16384;
+constexpr int kRankTokens = 15360;  // their classes and the counts take 64 KB of LDS
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kMaxBits = 10, kMaxBins = 1 << kMaxBits;
 constexpr int kMaxTiles = 128;  // workgroups of a radix pass
+// Tokens that a wavefront of rank_tokens counts.
+__host__ __device__ __forceinline__ int rank_share(int N) { return ((N + kSortWaves - 1) / kSortWaves + 63) / 64 * 64; }
 
 typedef u32x4 __attribute__((aligned(2))) Piece;
 
@@ -125,28 +127,56 @@ embedding_kernel(const void* __restrict__ table, int V, int D, const void* __res
 
 // ---- sorting -------------------------------------------------------------------------------
 
+// Short workgroups run best (1.2 GB: 16 bytes a thread 187 us, 128 bytes 210); very long clears take more of
+// them in turn, so that a grid's threads stay below 2^32.
+__device__ __forceinline__ void clear_share(void* p, int64_t bytes, int64_t block, int64_t blocks, int threads) {
+  char* const q = static_cast<char*>(p);
+  for (int64_t i = (block * threads + threadIdx.x) * 16; i < bytes; i += blocks * threads * 16) {
+    if (bytes - i >= 16) __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<Piece*>(q + i));
+    else
+      for (int64_t b = i; b < bytes; b += 2) *reinterpret_cast<uint16_t*>(q + b) = 0;
+  }
+}
+
 // keys[p], perm[p]: class and place of the p-th token in the order of (class, place).  64 tokens a
-// workgroup, a lane each in every wavefront; wavefront w counts the tokens of its share that come
-// before.  The shares' keys are the same in every lane.
+// workgroup, a lane each in every wavefront; wavefront w counts the tokens of its share (a whole number
+// of 64, in LDS, the same in every lane) that come before.  Two instructions a compare: 11,458 tokens 10 us.
+// The workgroups past the first `ranks` clear `bytes` at `zero` meanwhile (1.2 GB take 187 us).
 template <bool I64>
 __global__ void __launch_bounds__(kSortThreads)
-rank_tokens(const void* __restrict__ tokens, int N, int V, int32_t* __restrict__ keys, int32_t* __restrict__ perm) {
+rank_tokens(const void* __restrict__ tokens, int N, int V, int32_t* __restrict__ keys, int32_t* __restrict__ perm,
+            int ranks, void* zero, int64_t bytes) {
+  extern __shared__ __attribute__((aligned(16))) int32_t shares[];
   __shared__ int32_t count[kSortWaves][64];
+  if (static_cast<int>(blockIdx.x) >= ranks) {
+    clear_share(zero, bytes, blockIdx.x - ranks, gridDim.x - ranks, kSortThreads);
+    return;
+  }
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g0 = blockIdx.x * 64, i = g0 + lane;
   const int own = i < N ? class_of<I64>(tokens, i, V) : V;
-  const int share = (N + kSortWaves - 1) / kSortWaves;
-  const int jb = min(N, wave * share), je = min(N, jb + share);
+  const int share = rank_share(N);
+  const int jb = wave * share, je = jb + share;
+  int32_t* const mine = shares + jb;
+  for (int j = jb + lane; j < je; j += 64) mine[j - jb] = j < N ? class_of<I64>(tokens, j, V) : 0x7fffffff;
+  __syncthreads();
   int before = 0;
   const int j1 = min(max(g0, jb), je), j2 = min(max(g0 + 64, jb), je);
-#pragma unroll 8
-  for (int j = jb; j < j1; ++j) before += class_of<I64>(tokens, j, V) <= own;
+  auto four = [&](int j) { return *reinterpret_cast<const int4*>(mine + (j - jb)); };
+#pragma unroll 4
+  for (int j = jb; j < j1; j += 4) {
+    const int4 k = four(j);
+    before += (k.x <= own) + (k.y <= own) + (k.z <= own) + (k.w <= own);
+  }
   for (int j = j1; j < j2; ++j) {
-    const int k = class_of<I64>(tokens, j, V);
+    const int k = mine[j - jb];
     before += k < own || (k == own && j < i);
   }
-#pragma unroll 8
-  for (int j = j2; j < je; ++j) before += class_of<I64>(tokens, j, V) < own;
+#pragma unroll 4
+  for (int j = j2; j < je; j += 4) {
+    const int4 k = four(j);
+    before += (k.x < own) + (k.y < own) + (k.z < own) + (k.w < own);
+  }
   count[wave][lane] = before;
   __syncthreads();
   if (wave == 0 && i < N) {
@@ -187,15 +217,29 @@ radix_count(SortPass P) {
   for (int d = threadIdx.x; d < bins; d += kSortThreads) P.hist[blockIdx.x * bins + d] = h[d];
 }
 
-// hist[b][d] becomes the first place of tile b's tokens of digit d.  One workgroup, a thread a digit.
+// A thread a digit: its tokens in all tiles and in those before, and a scan over the digits, give the first
+// place of the tile's tokens of the digit (at most kMaxTiles rows of counts, read from the caches; a launch
+// of its own for the scan took 5 us).  Each wavefront counts its own share of the tile by digit, the counts
+// become first places (over the wavefronts before it), and it goes through its share again in order, 64 tokens at a time: lanes of
+// the same digit are found by a ballot per bit.
+template <bool I64>
 __global__ void __launch_bounds__(kSortThreads)
-radix_scan(int32_t* hist, int bins, int tiles) {
+radix_place(SortPass P) {
+  __shared__ int32_t at[kSortWaves][kMaxBins];
   __shared__ int32_t wave_sum[kSortWaves];
-  const int d = threadIdx.x, lane = d & 63, wave = d >> 6;
-  int total = 0;
-  if (d < bins)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bins = 1 << P.bits;
+  static_assert(kSortThreads >= kMaxBins, "a thread a digit");
+  const int digit0 = threadIdx.x;
+  int total = 0, earlier = 0;
+  if (digit0 < bins) {
 #pragma unroll 16
-    for (int b = 0; b < tiles; ++b) total += hist[b * bins + d];
+    for (int t = 0; t < P.tiles; ++t) {
+      const int n = P.hist[t * bins + digit0];
+      total += n;
+      earlier += t < static_cast<int>(blockIdx.x) ? n : 0;
+    }
+  }
   int incl = total;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -203,35 +247,15 @@ radix_scan(int32_t* hist, int bins, int tiles) {
     if (lane >= o) incl += x;
   }
   if (lane == 63) wave_sum[wave] = incl;
-  __syncthreads();
-  int at = incl - total;
-  for (int w = 0; w < wave; ++w) at += wave_sum[w];
-  if (d < bins)
-#pragma unroll 16
-    for (int b = 0; b < tiles; ++b) {
-      const int n = hist[b * bins + d];
-      hist[b * bins + d] = at;
-      at += n;
-    }
-}
-
-// Each wavefront counts its own share of the tile by digit, the counts become first places (over the
-// wavefronts before it), and it goes through its share again in order, 64 tokens at a time: lanes of
-// the same digit are found by a ballot per bit.
-template <bool I64>
-__global__ void __launch_bounds__(kSortThreads)
-radix_place(SortPass P) {
-  __shared__ int32_t at[kSortWaves][kMaxBins];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int bins = 1 << P.bits;
   for (int d = threadIdx.x; d < kSortWaves * bins; d += kSortThreads) at[d / bins][d % bins] = 0;
   __syncthreads();
   const int share = P.tile / kSortWaves;
   const int b = blockIdx.x * P.tile + wave * share, e = min(P.N, b + share);
   for (int p = b + lane; p < e; p += 64) atomicAdd(&at[wave][(key_at<I64>(P, p) >> P.shift) & (bins - 1)], 1);
   __syncthreads();
-  if (static_cast<int>(threadIdx.x) < bins) {
-    int first = P.hist[blockIdx.x * bins + threadIdx.x];
+  if (digit0 < bins) {
+    int first = incl - total + earlier;
+    for (int w = 0; w < wave; ++w) first += wave_sum[w];
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
       const int n = at[w][threadIdx.x];
@@ -345,18 +369,16 @@ embedding_sum(SumArgs A) {
   else put_row<OBF>(A, c, d, s);
 }
 
-// The classes that lie in several ranges, by the range in which each begins.
+// The classes that lie in several ranges, by the range in which each begins (blockIdx.x).  32 lanes take
+// 8 columns each, and the ranges in eight runs, whose sums are added in order: a class that has most of the
+// tokens lies in hundreds of ranges.
 template <bool OBF>
 __global__ void __launch_bounds__(kThreads)
 embedding_join(SumArgs A) {
-  const int r = blockIdx.x * (kThreads / A.lanes) + threadIdx.x / A.lanes;
-  const int d = (blockIdx.y * A.lanes + threadIdx.x % A.lanes) * kVals;
-  if (r >= A.ranges - 1 || d >= A.D) return;
+  const int r = blockIdx.x;
   const int b = r * A.range, e = b + A.range;
-  const int c = A.keys[e - 1];
+  const int c = A.keys[e - 1];  // (r is not the last range)
   if (c >= A.V || A.keys[e] != c || (b > 0 && A.keys[b - 1] == c && A.keys[b] == c)) return;
-  float s[kVals];
-  load_vals<false>(A.part + (static_cast<int64_t>(r) * 2 + 1) * A.D + d, A.D - d, s);
   // the last range with the class: the first place past it by bisection (keys rise)
   int lo = e, hi = A.N;
   while (lo < hi) {
@@ -365,26 +387,40 @@ embedding_join(SumArgs A) {
     else hi = mid;
   }
   const int last = (lo - 1) / A.range;
+  constexpr int kRuns = kThreads / 32;
+  __shared__ float part[kRuns][32][kVals];
+  const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
+  const int d = (blockIdx.y * 32 + lane) * kVals;
+  const int per = (last - r + 1 + kRuns - 1) / kRuns;
+  float s[kVals] = {};
+  if (d < A.D) {
+    const int qb = r + run * per, qe = min(last + 1, qb + per);
 #pragma unroll 4
-  for (int q = r + 1; q <= last; ++q) {
-    float x[kVals];
-    load_vals<false>(A.part + static_cast<int64_t>(q) * 2 * A.D + d, A.D - d, x);
+    for (int q = qb; q < qe; ++q) {  // its first part is the second of range r, then the first of each
+      float x[kVals];
+      load_vals<false>(A.part + (static_cast<int64_t>(q) * 2 + (q == r)) * A.D + d, A.D - d, x);
 #pragma unroll
-    for (int k = 0; k < kVals; ++k) s[k] += x[k];
+      for (int k = 0; k < kVals; ++k) s[k] += x[k];
+    }
   }
+#pragma unroll
+  for (int k = 0; k < kVals; ++k) part[run][lane][k] = s[k];
+  __syncthreads();
+  if (run > 0 || d >= A.D) return;
+#pragma unroll
+  for (int g = 1; g < kRuns; ++g)
+#pragma unroll
+    for (int k = 0; k < kVals; ++k) s[k] += part[g][lane][k];
   put_row<OBF>(A, c, d, s);
 }
 
-__global__ void __launch_bounds__(kThreads)
-fill_zero(void* p, int64_t bytes) {
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 16;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads * 16;
-  char* q = static_cast<char*>(p);
-  for (int64_t k = i; k < bytes; k += step) {
-    if (bytes - k >= 16) __builtin_nontemporal_store(u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<Piece*>(q + k));
-    else
-      for (int64_t b = k; b < bytes; b += 2) *reinterpret_cast<uint16_t*>(q + b) = 0;
-  }
+__global__ void __launch_bounds__(kThreads) fill_zero(void* p, int64_t bytes) {
+  clear_share(p, bytes, blockIdx.x, gridDim.x, kThreads);
+}
+
+// Workgroups that clear.
+unsigned clear_blocks(int64_t bytes, int threads) {
+  return static_cast<unsigned>(std::min<int64_t>((bytes + threads * 16 - 1) / (threads * 16), (int64_t{1} << 31) / threads));
 }
 
 // Places of a range: as short as keeps its partial rows few beside the rows it reads.
@@ -419,8 +455,7 @@ Layout layout(int N, int D) {
 hipError_t launch_clear(void* p, int64_t bytes, hipStream_t stream) {
   Prof pr("clear", stream);
   if (bytes > 0)
-    hipLaunchKernelGGL(fill_zero, dim3(static_cast<unsigned>(std::min<int64_t>((bytes + 4095) / 4096, kMaxGrid))),
-                       dim3(kThreads), 0, stream, p, bytes);
+    hipLaunchKernelGGL(fill_zero, dim3(clear_blocks(bytes, kThreads)), dim3(kThreads), 0, stream, p, bytes);
   return hipGetLastError();
 }
 
@@ -446,18 +481,26 @@ hipError_t launch_embedding(int dtype, const void* table, int V, int D, const vo
 
 size_t embedding_backward_bytes(int N, int D) { return layout(N, D).total; }
 
-// Sorted keys and places at the start of the workspace.
-static hipError_t sort_tokens(const void* tokens, bool i64, int N, int V, char* ws, const Layout& L, hipStream_t stream) {
+// Sorted keys and places at the start of the workspace; `bytes` at `zero` are cleared too (0: nothing).
+static hipError_t sort_tokens(const void* tokens, bool i64, int N, int V, char* ws, const Layout& L, void* zero,
+                              int64_t bytes, hipStream_t stream) {
   auto at = [&](size_t o) { return reinterpret_cast<int32_t*>(ws + o); };
   if (N <= kRankTokens) {
     Prof pr("embedding_rank", stream);
-    const dim3 grid((N + 63) / 64);
+    const int ranks = (N + 63) / 64;
+    const dim3 grid(ranks + clear_blocks(bytes, kSortThreads));
+    const size_t lds = static_cast<size_t>(kSortWaves) * rank_share(N) * 4;
     if (i64)
-      hipLaunchKernelGGL(rank_tokens<true>, grid, dim3(kSortThreads), 0, stream, tokens, N, V, at(L.o_keys), at(L.o_perm));
+      hipLaunchKernelGGL(rank_tokens<true>, grid, dim3(kSortThreads), lds, stream, tokens, N, V, at(L.o_keys),
+                         at(L.o_perm), ranks, zero, bytes);
     else
-      hipLaunchKernelGGL(rank_tokens<false>, grid, dim3(kSortThreads), 0, stream, tokens, N, V, at(L.o_keys),
-                         at(L.o_perm));
+      hipLaunchKernelGGL(rank_tokens<false>, grid, dim3(kSortThreads), lds, stream, tokens, N, V, at(L.o_keys),
+                         at(L.o_perm), ranks, zero, bytes);
     return hipGetLastError();
+  }
+  if (bytes > 0) {
+    const hipError_t e = launch_clear(zero, bytes, stream);
+    if (e != hipSuccess) return e;
   }
   int bits = 1;
   while ((V >> bits) != 0) ++bits;  // keys reach V
@@ -469,7 +512,7 @@ static hipError_t sort_tokens(const void* tokens, bool i64, int N, int V, char* 
   P.V = V;
   P.bits = per;
   const int unit = 64 * kSortWaves;
-  P.tile = std::max(2 * unit, static_cast<int>((static_cast<int64_t>(N) + kMaxTiles * unit - 1) / (kMaxTiles * unit)) * unit);
+  P.tile = std::max(unit, static_cast<int>((static_cast<int64_t>(N) + kMaxTiles * unit - 1) / (kMaxTiles * unit)) * unit);
   P.tiles = (N + P.tile - 1) / P.tile;
   for (int q = 0; q < passes; ++q) {
     const bool last = q == passes - 1;
@@ -480,7 +523,6 @@ static hipError_t sort_tokens(const void* tokens, bool i64, int N, int V, char* 
     Prof pr("embedding_sort", stream);
     if (i64) hipLaunchKernelGGL(radix_count<true>, dim3(P.tiles), dim3(kSortThreads), 0, stream, P);
     else hipLaunchKernelGGL(radix_count<false>, dim3(P.tiles), dim3(kSortThreads), 0, stream, P);
-    hipLaunchKernelGGL(radix_scan, dim3(1), dim3(kSortThreads), 0, stream, P.hist, 1 << per, P.tiles);
     if (i64) hipLaunchKernelGGL(radix_place<true>, dim3(P.tiles), dim3(kSortThreads), 0, stream, P);
     else hipLaunchKernelGGL(radix_place<false>, dim3(P.tiles), dim3(kSortThreads), 0, stream, P);
     P.keys_in = P.keys_out;
@@ -492,14 +534,11 @@ static hipError_t sort_tokens(const void* tokens, bool i64, int N, int V, char* 
 hipError_t launch_embedding_backward(int dtype, const void* dy, const void* tokens, bool i64, int N, int V, int D,
                                      float scale, int out_dtype, void* dW, bool accumulate, void* workspace,
                                      hipStream_t stream) {
-  if (!accumulate) {
-    const hipError_t e = launch_clear(dW, static_cast<int64_t>(V) * D * (out_dtype == 1 ? 2 : 4), stream);
-    if (e != hipSuccess) return e;
-  }
-  if (N == 0) return hipGetLastError();
+  const int64_t bytes = accumulate ? 0 : static_cast<int64_t>(V) * D * (out_dtype == 1 ? 2 : 4);
+  if (N == 0) return bytes > 0 ? launch_clear(dW, bytes, stream) : hipSuccess;
   const Layout L = layout(N, D);
   char* ws = static_cast<char*>(workspace);
-  hipError_t e = sort_tokens(tokens, i64, N, V, ws, L, stream);
+  hipError_t e = sort_tokens(tokens, i64, N, V, ws, L, dW, bytes, stream);
   if (e != hipSuccess) return e;
   SumArgs A{};
   A.dy = dy;
@@ -531,8 +570,9 @@ hipError_t launch_embedding_backward(int dtype, const void* dy, const void* toke
   }
   if (A.ranges > 1) {
     Prof pr("embedding_join", stream);
-    if (out_dtype == 1) hipLaunchKernelGGL(embedding_join<true>, grid, dim3(kThreads), 0, stream, A);
-    else hipLaunchKernelGGL(embedding_join<false>, grid, dim3(kThreads), 0, stream, A);
+    const dim3 joins(A.ranges - 1, (D + 32 * kVals - 1) / (32 * kVals));
+    if (out_dtype == 1) hipLaunchKernelGGL(embedding_join<true>, joins, dim3(kThreads), 0, stream, A);
+    else hipLaunchKernelGGL(embedding_join<false>, joins, dim3(kThreads), 0, stream, A);
   }
   return hipGetLastError();
 }
