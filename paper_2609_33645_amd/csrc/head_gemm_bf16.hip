@@ -79,14 +79,17 @@ using GDw = bf::Gemm<kBR, kBC, kBK, LL::MC, LL::MC, 4, 2, 4, true>;
 template <class G, bool BIAS, int OCC>
 __global__ void __launch_bounds__(G::kThreads, OCC)
 lse_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __restrict__ W, const float* __restrict__ bias,
-                 int V, int P, int vper, float2* __restrict__ partials) {
+                 int V, int P, int vper, float2* __restrict__ partials, const int32_t* __restrict__ Mdev) {
   extern __shared__ float bsh[];  // BIAS: b over this partition's rows (vper, padded to whole tiles)
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   PCTC_STAGES_G(G)
+  if (Mdev) M = min(M, *Mdev);
   const int nMt = (M + TC - 1) / TC;
   // every frame tile of a vocabulary run on one XCD at about the same time: the run's W rows
   // are fetched once and shared through that XCD's L2
-  const int w = xcd_swz(blockIdx.x, gridDim.x);
+  const int works = Mdev ? nMt * P : gridDim.x;
+  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int w = xcd_swz(blockIdx.x, works);
   const int mt = w % nMt;
   const int p = w / nMt;
   if (p >= P) return;
@@ -175,14 +178,18 @@ template <bool HT, bool BIAS = false>
 __global__ void __launch_bounds__(512, 1)
 lse_partial_e_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ Ht, int Mp, int M, int D,
                    const uint16_t* __restrict__ W, const float* __restrict__ bias, int V, int P, int vper,
-                   float2* __restrict__ partials, uint16_t* __restrict__ E, int epitch, int eparts, int32_t* __restrict__ einv) {
+                   float2* __restrict__ partials, uint16_t* __restrict__ E, int epitch, int eparts, int32_t* __restrict__ einv,
+                   const int32_t* __restrict__ Mdev) {
   using G = std::conditional_t<HT, GMidTW, GMid>;
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   static_assert(FR == 4 && FC == 2 && G::NW == 8 && TR == 256, "waves of 128 vocabulary rows x 64 frames");
   PCTC_STAGES_G(G)
   __shared__ __attribute__((aligned(1024))) char stg_[G::NW * 4096];
+  if (Mdev) M = min(M, *Mdev);
   const int nMt = (M + TC - 1) / TC;
-  const int w = xcd_swz(blockIdx.x, gridDim.x);
+  const int works = Mdev ? nMt * P : gridDim.x;
+  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int w = xcd_swz(blockIdx.x, works);
   const int mt = w % nMt;
   const int p = w / nMt;
   if (einv && blockIdx.x == 0 && threadIdx.x == 0) *einv = 0;
@@ -434,7 +441,7 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
                   const float* __restrict__ bias, int c0, int cw, const float2* __restrict__ lam2,
                   const float* __restrict__ g, const int32_t* __restrict__ remap, const float* __restrict__ S, int ldS,
                   const float* __restrict__ G, int ldG, uint16_t* __restrict__ dZ, int chunk,
-                  float* __restrict__ dbpart) {
+                  float* __restrict__ dbpart, const int32_t* __restrict__ Mdev) {
   constexpr int FR = GG::FR, FC = GG::FC, TR = GG::kBR, TC = GG::kBC, NT = GG::kThreads;
   static_assert(TR == 256 && NT % TR == 0, "each thread owns one tile column");
   constexpr int WC = GG::NW / 2;        // column groups of 64 frames (the wave grid is 2 x WC)
@@ -444,10 +451,13 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
   constexpr int kGps = GG::kStageBytes / (32 * kPitch);
   static_assert(kGps >= 1 && (WC + kGps - 1) / kGps <= GG::kNS, "staging fits the stages");
   PCTC_STAGES_G(GG)
+  if (Mdev) M = min(M, *Mdev);
   const int nMt = (M + TC - 1) / TC;
   const int nVt = (cw + TR - 1) / TR;
+  const int works = !Mdev ? gridDim.x : nMt > 0 ? grouped_grid(nMt, nVt) : 0;
+  if (static_cast<int>(blockIdx.x) >= works) return;
   int mt, vt;
-  if (!grouped_tile(xcd_swz(blockIdx.x, gridDim.x), nMt, nVt, mt, vt)) return;
+  if (!grouped_tile(xcd_swz(blockIdx.x, works), nMt, nVt, mt, vt)) return;
   const int m0 = mt * TC;
   const int vl0 = vt * TR;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -583,9 +593,10 @@ __global__ void __launch_bounds__(512, 1)
 recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__ Hst, int Mp, int M, int D,
                    const uint16_t* __restrict__ W, int c0, int cw, int run, const float2* __restrict__ lam2,
                    const float* __restrict__ g, uint16_t* __restrict__ dZ, int chunk,
-                   const int32_t* __restrict__ only_if) {
+                   const int32_t* __restrict__ only_if, const int32_t* __restrict__ Mdev) {
   // only_if (the normaliser's E check flag): recompute only when its E cannot be used
   if (only_if && *only_if == 0) return;
+  if (Mdev) M = min(M, *Mdev);
   using G = std::conditional_t<HT, GMidT, GMid>;
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   static_assert(FR == 4 && FC == 2 && G::NW == 8 && TR == 256, "waves of 128 vocabulary rows x 64 frames");
@@ -594,7 +605,9 @@ recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__
   const int nMt = (M + TC - 1) / TC;
   const int nVt = (cw + TR - 1) / TR;
   // all frame tiles of a vocabulary run consecutive on one XCD (it fetches the run's W rows once)
-  const int w = xcd_swz(blockIdx.x, gridDim.x);
+  const int works = Mdev ? nMt * ((nVt + run - 1) / run) : gridDim.x;
+  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int w = xcd_swz(blockIdx.x, works);
   const int mt = w % nMt;
   const int vt0 = (w / nMt) * run;
   if (vt0 >= nVt) return;
@@ -707,7 +720,8 @@ template <class G, int OCC>
 __global__ void __launch_bounds__(G::kThreads, OCC)
 dh_gemm_bf16(const uint16_t* __restrict__ dZ, int M, int chunk, const uint16_t* __restrict__ W, int D, int c0, int cw,
              int slice, float* __restrict__ part, int gm, int accumulate, const int32_t* __restrict__ kdev,
-             const float* __restrict__ rowscale) {
+             const float* __restrict__ rowscale, const int32_t* __restrict__ Mdev) {
+  if (Mdev) M = min(M, *Mdev);
   // the first chunk writes its slices; later chunks (and an accumulating call) add to them
   const bool first = c0 == 0 && !accumulate;
   if (kdev) cw = min(cw, 2 * *kdev);  // union columns: [hi | lo] of the K classes the device found
@@ -716,7 +730,9 @@ dh_gemm_bf16(const uint16_t* __restrict__ dZ, int M, int chunk, const uint16_t* 
   const int nDt = (D + TC - 1) / TC;
   // Each XCD (a contiguous run of work ids) takes one block of a gm x (8 / gm) partition of
   // the frame x d tile grid: it reads dZ rows of its frame block and W columns of its d block
-  const int work = xcd_swz(blockIdx.x, gridDim.x);
+  const int works = Mdev ? nMt * nDt * ((cw + slice - 1) / slice) : gridDim.x;
+  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int work = xcd_swz(blockIdx.x, works);
   const int s = work / (nMt * nDt);
   int mt, dt;
   block_tile(work % (nMt * nDt), nMt, nDt, gm, mt, dt);
@@ -783,7 +799,9 @@ struct DwOp {
 // tiles, the rest P1's (the union columns' dW_u in the last chunk's launch).  O16: `out` holds bf16.
 template <bool O16>
 __global__ void __launch_bounds__(512, 1)
-dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int M, int D) {
+dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int M, int D,
+             const int32_t* __restrict__ Mdev) {
+  if (Mdev) M = min(M, *Mdev);  // (with none, zeros are written)
   using G = GDw;
   constexpr int FR = G::FR, FC = G::FC;
   PCTC_STAGES_G(G)
@@ -801,7 +819,7 @@ dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int 
   const int mb = z * P.mslice;
   const int mlen = min(M - mb, P.mslice);
   if (P.kdev) cw = min(cw, 2 * *P.kdev);
-  if (z >= P.nz || mlen <= 0 || v0 >= cw) return;
+  if (z >= P.nz || (mlen <= 0 && !Mdev) || v0 >= cw) return;
   float* const dW = P.out + static_cast<int64_t>(z) * P.zstride;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // A: Z viewed as rows v (columns of Z), k = frame; B: Hs viewed as rows d, k = frame
@@ -1082,7 +1100,7 @@ hipError_t launch_union_part_bf16(const float* G, int ldG, const int32_t* Kdev, 
       const int tiles = ((M + GUh::kBR - 1) / GUh::kBR) * ((D + GUh::kBC - 1) / GUh::kBC);
       Prof pr("union_dh", stream);
       hipLaunchKernelGGL((dh_gemm_bf16<GUh, 2>), dim3(tiles), dim3(GUh::kThreads), 0, stream, Gb, M, k2, WU2, D, 0,
-                         k2, k2, dH, dh_xcd_rows(M, D), 0, Kdev, nullptr);
+                         k2, k2, dH, dh_xcd_rows(M, D), 0, Kdev, nullptr, nullptr);
     }
   }
   if (want_dW && !dw_elsewhere) {
@@ -1090,7 +1108,8 @@ hipError_t launch_union_part_bf16(const float* G, int ldG, const int32_t* Kdev, 
     const DwOp p{Gb, k2, 0, k2, reinterpret_cast<float*>(sc + L.o_dwu), L.nz, L.mslice,
                  static_cast<int64_t>(k2) * D, Kdev};
     Prof pr("union_dw", stream);
-    hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles), dim3(GDw::kThreads), 0, stream, p, p, tiles, Hs, M, D);
+    hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles), dim3(GDw::kThreads), 0, stream, p, p, tiles, Hs, M, D,
+                       nullptr);
   }
   if (want_db) {
     const int mper = (M + kColSlices - 1) / kColSlices;
@@ -1110,7 +1129,7 @@ hipError_t launch_union_dh_bf16(const uint16_t* Gb, const int32_t* Kdev, int K_m
   const int tiles = ((M + GUh::kBR - 1) / GUh::kBR) * ((D + GUh::kBC - 1) / GUh::kBC);
   Prof pr("union_dh", stream);
   hipLaunchKernelGGL((dh_gemm_bf16<GUh, 2>), dim3(tiles), dim3(GUh::kThreads), 0, stream, Gb, M, k2, WU2, D, 0, k2,
-                     k2, dH, dh_xcd_rows(M, D), 1, Kdev, nullptr);
+                     k2, dH, dh_xcd_rows(M, D), 1, Kdev, nullptr, nullptr);
   return hipGetLastError();
 }
 
@@ -1214,7 +1233,7 @@ int lse_parts_any_m_bf16(int M, int D, int V) { return lse_split_bf16(M, D, V, S
 int amax_parts_bf16(int M, int D, int V) { return lse_split_bf16(M, D, V, SplitFor::kAmax).P; }
 
 hipError_t launch_lse_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                   float2* partials, int* P_out, hipStream_t stream, bool any_m) {
+                                   float2* partials, int* P_out, hipStream_t stream, bool any_m, const int32_t* Mdev) {
   const LseSplit sp = lse_split_bf16(M, D, V, any_m ? SplitFor::kAnyM : SplitFor::kLse);
   const int vper = sp.vper, Peff = sp.P;
   *P_out = Peff;
@@ -1225,10 +1244,10 @@ hipError_t launch_lse_partial_bf16(const uint16_t* H, int M, int D, const uint16
   const dim3 grid(sp.nM * Peff);
   if (bias) {
     hipLaunchKernelGGL((lse_partial_bf16<GMid, true, 1>), grid, dim3(GMid::kThreads), bsh, stream, H, M, D, W, bias,
-                       V, Peff, vper, partials);
+                       V, Peff, vper, partials, Mdev);
   } else {
     hipLaunchKernelGGL((lse_partial_bf16<GMid, false, 1>), grid, dim3(GMid::kThreads), 0, stream, H, M, D, W, bias,
-                       V, Peff, vper, partials);
+                       V, Peff, vper, partials, Mdev);
   }
   return hipGetLastError();
 }
@@ -1366,7 +1385,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  const int32_t* remap, const float* S, int ldS, uint16_t* dZ, int chunk, float* part,
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra, const ChunkE* ce,
-                                 const uint16_t* Hst, int Mp, uint16_t* dW16) {
+                                 const uint16_t* Hst, int Mp, uint16_t* dW16, const int32_t* Mdev) {
   // wide heads: one 8-wave 256 x 256 workgroup per CU (the long k loop hides the epilogue);
   // narrow heads: two 4-wave 256 x 128 workgroups per CU, so that one's epilogue (exp, pack,
   // staged stores: VALU-bound) overlaps the other's products
@@ -1374,12 +1393,14 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
   const int nMt = (M + (wide ? GWide::kBC : GFwd::kBC) - 1) / (wide ? GWide::kBC : GFwd::kBC);
   if (recompute) {
     const int nVt = (cw + kFR - 1) / kFR;
-    const dim3 grid(grouped_grid(nMt, nVt));
+    int works = grouped_grid(nMt, nVt);
+    for (int n = 1; Mdev && n < nMt; ++n) works = max(works, grouped_grid(n, nVt));  // whatever *Mdev is
+    const dim3 grid(works);
     // with ce the launch only recomputes when the normaliser's rows are unusable
     Prof pr(ce ? "recompute_check" : "recompute_dz", stream);
 #define PCTC_RECOMPUTE(GC, OCC, BI, DBI)                                                                             \
   hipLaunchKernelGGL((recompute_dz_bf16<GC, BI, DBI, OCC>), grid, dim3(GC::kThreads), 0, stream, Hs, M, D, W, bias, \
-                     c0, cw, lam2, g, remap, S, ldS, G, ldG, dZ, chunk, dbpart)
+                     c0, cw, lam2, g, remap, S, ldS, G, ldG, dZ, chunk, dbpart, Mdev)
 #define PCTC_RECOMPUTE_CFG(GC, OCC)           \
   if (bias) {                                 \
     if (db) PCTC_RECOMPUTE(GC, OCC, true, true);  \
@@ -1400,10 +1421,10 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
       const int nruns = (nVt + run - 1) / run;
       if (Hst)
         hipLaunchKernelGGL(recompute_run_bf16<true>, dim3(nMt2 * nruns), dim3(GMid::kThreads), 0, stream, Hs, Hst,
-                           Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr);
+                           Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr, Mdev);
       else
         hipLaunchKernelGGL(recompute_run_bf16<false>, dim3(nMt2 * nruns), dim3(GMid::kThreads), 0, stream, Hs, Hst,
-                           Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr);
+                           Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr, Mdev);
     } else {
       PCTC_RECOMPUTE_CFG(GFwd, 2)
     }
@@ -1419,7 +1440,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
     const int ns = (cw + slice - 1) / slice;
     Prof pr("dh_gemm", stream);
     hipLaunchKernelGGL((dh_gemm_bf16<GDh, 1>), dim3(tiles * ns), dim3(GDh::kThreads), 0, stream, dZ, M, chunk, W, D,
-                       c0, cw, slice, part, dh_xcd_rows(M, D), 0, nullptr, ce ? ce->rowscale : nullptr);
+                       c0, cw, slice, part, dh_xcd_rows(M, D), 0, nullptr, ce ? ce->rowscale : nullptr, Mdev);
   }
   if (want_dW) {
     const int nDt = (D + kBC - 1) / kBC;
@@ -1434,10 +1455,11 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
     Prof pr("dw_gemm", stream);
     if (dW16) {
       p0.out = reinterpret_cast<float*>(dW16);
-      hipLaunchKernelGGL(dw_gemm_bf16<true>, dim3(tiles0), dim3(GDw::kThreads), 0, stream, p0, p0, tiles0, Hs, M, D);
+      hipLaunchKernelGGL(dw_gemm_bf16<true>, dim3(tiles0), dim3(GDw::kThreads), 0, stream, p0, p0, tiles0, Hs, M, D,
+                         Mdev);
     } else {
       hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles0 + tiles1), dim3(GDw::kThreads), 0, stream, p0, p1, tiles0,
-                         ce ? ce->Hp : Hs, M, D);
+                         ce ? ce->Hp : Hs, M, D, Mdev);
     }
   }
   return hipGetLastError();
@@ -1464,7 +1486,7 @@ int lse_e_parts_bf16(int M, int D, int V, int chunk) {
 
 hipError_t launch_lse_partial_e_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                      float2* partials, int* P_out, uint16_t* E, int epitch, int eparts, int32_t* einv,
-                                     hipStream_t stream, const uint16_t* Ht, int Mp, bool any_m) {
+                                     hipStream_t stream, const uint16_t* Ht, int Mp, bool any_m, const int32_t* Mdev) {
   const LseSplit sp = lse_split_bf16(M, D, V, any_m ? SplitFor::kAnyM : SplitFor::kLse);
   *P_out = sp.P;
   const dim3 grid(sp.nM * sp.P), block(GMid::kThreads);
@@ -1473,13 +1495,13 @@ hipError_t launch_lse_partial_e_bf16(const uint16_t* H, int M, int D, const uint
     // the partition's bias takes the 32 KB that E is staged through
     if (!Ht || eparts > 0 || sp.vper * sizeof(float) > 32768) return hipErrorInvalidValue;
     hipLaunchKernelGGL((lse_partial_e_bf16<true, true>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V, sp.P,
-                       sp.vper, partials, E, epitch, 0, einv);
+                       sp.vper, partials, E, epitch, 0, einv, Mdev);
   } else if (Ht) {
     hipLaunchKernelGGL((lse_partial_e_bf16<true>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V, sp.P, sp.vper,
-                       partials, E, epitch, eparts, einv);
+                       partials, E, epitch, eparts, einv, Mdev);
   } else {
     hipLaunchKernelGGL((lse_partial_e_bf16<false>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V, sp.P, sp.vper,
-                       partials, E, epitch, eparts, einv);
+                       partials, E, epitch, eparts, einv, Mdev);
   }
   return hipGetLastError();
 }

@@ -165,6 +165,12 @@ struct DzTokens {
   const int32_t* token;
   const float* logp;
   const float* g;
+  const int32_t* Mdev = nullptr;  // how many frames there are (null: M)
+  // summed by the first chunk's launch: loss = sum of w_n losses_n over the n < N whose status is 0
+  const float *losses = nullptr, *weights = nullptr;
+  const int32_t* status = nullptr;
+  int N = 0;
+  double* loss = nullptr;
 };
 hipError_t launch_dz_tokens(int dtype, void* dZ, int pitch, int M, int c0, int cw, const DzTokens& t, float scale,
                             hipStream_t stream);
@@ -184,8 +190,11 @@ hipError_t head_bwd_f32(const float* H, int M, int D, const float* W, const floa
                         char* scratch, const BwdPlan& plan, hipStream_t stream, const DzTokens* tokens = nullptr);
 
 // ---- bf16 kernels on the direct-to-LDS engine (head_gemm_bf16.hip) ---------------------
+// Mdev (null: M) of the normaliser and the backward's chunks: how many of the M rows there are, on the device;
+// the pitches of the partial pairs and of dH's slices are then that number's.
 hipError_t launch_lse_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                   float2* partials, int* P_out, hipStream_t stream, bool any_m = false);
+                                   float2* partials, int* P_out, hipStream_t stream, bool any_m = false,
+                                   const int32_t* Mdev = nullptr);
 // Gz (may be null): also Gz[m * ldS + j] = 0 for j < *K (the lattice's G, before it is written).
 // Zd (may be null): write the selected logits in double (Zd[m * ldS + j]) instead of S; lam
 // is then not read (launch_lse_finalize subtracts it).
@@ -210,7 +219,8 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra = nullptr,
                                  const ChunkE* ce = nullptr, const uint16_t* Hst = nullptr, int Mp = 0,
-                                 uint16_t* dW16 = nullptr);  // dW16: dW is written there, rounded to bf16 (no extra, no ce)
+                                 uint16_t* dW16 = nullptr,  // dW is written there, rounded to bf16 (no extra, no ce)
+                                 const int32_t* Mdev = nullptr);
 // Partitions of the normaliser that can write E for a first chunk of `chunk` columns (0: none;
 // narrow heads with D a multiple of 128, chunk a multiple of the partition width).
 int lse_e_parts_bf16(int M, int D, int V, int chunk);
@@ -220,7 +230,8 @@ int lse_e_parts_bf16(int M, int D, int V, int chunk);
 // With bias (float [V]; needs Ht, eparts 0) the logits include it.
 hipError_t launch_lse_partial_e_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                      float2* partials, int* P_out, uint16_t* E, int epitch, int eparts, int32_t* einv,
-                                     hipStream_t stream, const uint16_t* Ht = nullptr, int Mp = 0, bool any_m = false);
+                                     hipStream_t stream, const uint16_t* Ht = nullptr, int Mp = 0, bool any_m = false,
+                                     const int32_t* Mdev = nullptr);
 size_t lse_ht_bytes_bf16(int M, int D);
 bool bias_reads_ht_bf16(int M, int D);
 // Partitions that a normaliser launch with any_m, and an argmax launch, of this shape write.
@@ -383,7 +394,8 @@ struct PolicyArgs {
 };
 struct PolicyLayout {
   BwdPlan bwd;
-  size_t o_lam, o_lam2, o_g, o_part, o_ht, o_dh, o_bwd, total;
+  size_t o_lam2, o_g, o_tok, o_lp, o_rows, o_inv, o_count, o_h, o_part, o_ht, o_dh, o_bwd, total;
+  bool ht;  // the normaliser reads H transposed
 };
 // grads: the call asks for gradients.
 PolicyLayout policy_layout(int dtype, int M, int D, int V, bool bias, bool grads, int chunk);

@@ -5,10 +5,11 @@
 //   g_m = w_m dloss_m / dlp_m,   dZ[m] = g_m (onehot(token_m) - p(m)),   dH = dZ W,  dW = dZ^T H
 //
 // The logits are not stored: the normaliser and the recomputed backward are those of the Pruned CTC
-// loss, whose union columns here are one class per frame.  Three small kernels come between: the tokens'
-// logits and losses (a wavefront a token; two rows of D values each), the loss, and in every chunk of
-// the backward the tokens' own entries of dZ.  Bound by the matrix products, 8 M V D operations
-// (the logits are formed twice).
+// loss, whose union columns here are one class per frame.  bf16 rows whose token is left out (prompts)
+// are left out of the products too: the counted rows are gathered, and every launch ends at their
+// number, which only the device knows.  Between the products: the tokens' normalisers, logits and losses (a
+// wavefront a token), and in every chunk of the backward the tokens' own entries of dZ, the sum of the
+// losses beside the first.  Bound by the matrix products, 8 M V D operations (the logits are formed twice).
 #include "pctc_internal.h"
 
 namespace pctc {
@@ -44,29 +45,133 @@ __device__ __forceinline__ float dot_share(const void* a, const void* b, int D, 
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// A wavefront a token: its logit (lanes' float sums joined in double), then the loss in double.
-template <bool BF>
+// counts[b]: counted tokens of the rows [kCountRows b, kCountRows (b + 1)).
+constexpr int kCountRows = 8192;
 __global__ void __launch_bounds__(kThreads)
-policy_tokens(const void* __restrict__ H, int M, int D, const void* __restrict__ W, const float* __restrict__ bias, int V,
-              const double* __restrict__ lam, PolicyArgs a, float* __restrict__ g) {
-  const int m = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (m >= M) return;
+policy_count(const int32_t* __restrict__ tokens, int M, int V, int32_t* __restrict__ counts) {
+  const int b = blockIdx.x * kCountRows, e = min(M, b + kCountRows);
+  int n = 0;
+  for (int m = b + threadIdx.x; m < e; m += kThreads) n += static_cast<uint32_t>(tokens[m]) < static_cast<uint32_t>(V);
+  __shared__ int sh[kThreads / 64];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) counts[blockIdx.x] = sh[0] + sh[1] + sh[2] + sh[3];
+}
+
+// The counted rows of H, one behind the other: Hc[j] = H[rows[j]], inv[m] = j (-1: left out), *count of
+// them; what a left out row reports.  A workgroup takes kGatherRows rows and counts those before by
+// itself (counts: in whole blocks, where there are many).
+constexpr int kGatherRows = 8;
+__global__ void __launch_bounds__(kThreads)
+policy_gather(const uint16_t* __restrict__ H, int M, int D, int V, PolicyArgs a, const int32_t* __restrict__ counts,
+              uint16_t* __restrict__ Hc, int32_t* __restrict__ rows, int32_t* __restrict__ inv, int32_t* __restrict__ count) {
+  const int m0 = blockIdx.x * kGatherRows;
+  auto counted = [&](int m) { return m < M && static_cast<uint32_t>(a.tokens[m]) < static_cast<uint32_t>(V); };
+  int n = 0, from = 0;
+  if (counts) {
+    const int blocks = m0 / kCountRows;
+    for (int b = threadIdx.x; b < blocks; b += kThreads) n += counts[b];
+    from = blocks * kCountRows;
+  }
+#pragma unroll 8
+  for (int m = from + threadIdx.x; m < m0; m += kThreads) n += counted(m);
+  __shared__ int sh[kThreads / 64];
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o, 64);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = n;
+  __syncthreads();
+  int j = sh[0] + sh[1] + sh[2] + sh[3];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  for (int r = 0; r < kGatherRows; ++r) {
+    const int m = m0 + r;
+    const bool in = counted(m);
+    if (wave == r % (kThreads / 64) && m < M) {
+      if (in) {
+        const uint16_t* src = H + static_cast<int64_t>(m) * D;
+        uint16_t* dst = Hc + static_cast<int64_t>(j) * D;
+#pragma unroll 4
+        for (int d = lane * 8; d < D; d += 512) *reinterpret_cast<u32x4*>(dst + d) = *reinterpret_cast<const u32x4*>(src + d);
+      }
+      if (lane == 0) {
+        inv[m] = in ? j : -1;
+        if (in) {
+          rows[j] = m;
+        } else {
+          a.logp[m] = a.losses[m] = 0.f;
+          a.status[m] = 1;
+        }
+      }
+    }
+    j += in;
+  }
+  if (m0 + kGatherRows >= M && threadIdx.x == 0) *count = j;
+}
+
+// Where the tokens kernel finds its rows and what it leaves for the backward, by place j in H.
+struct PolicyRows {
+  const int32_t* rows;   // [.]: the row of place j (null: j itself)
+  const int32_t* count;  // how many places (null: M)
+  const float2* partials;
+  int P;          // the normaliser's partial pairs (max, sum) of each place, [P][places]
+  float2* lam2;   // lambda log2(e) in two floats
+  float* g;
+  int32_t* token;
+  float* logp;
+};
+
+// A wavefront a place, 16 of them a workgroup (so that the lines of the partial pairs, 16 places each, are
+// read once).  lambda in double from the pairs; the token's logit from two rows of D values, lanes' float
+// sums joined in double; the loss in double.  mask (null: none): a row without a gradient is cleared there,
+// so that what is not finite in it reaches no product.
+template <bool BF>
+__global__ void __launch_bounds__(kLossThreads)
+policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const float* __restrict__ bias, int V,
+              PolicyRows R, PolicyArgs a, uint16_t* mask) {
+  const int n = R.count ? min(M, *R.count) : M;
+  const int j = blockIdx.x * (kLossThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (j >= n) return;
+  // lambda: the largest maximum is exact, each sum is scaled by the float exponential of an exact difference
+  constexpr int kPer = kMaxLseParts / 64;
+  float2 q[kPer];
+  float top = -INFINITY;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int p = lane + 64 * i;
+    q[i] = p < R.P ? R.partials[static_cast<int64_t>(p) * n + j] : make_float2(-INFINITY, 0.f);
+    nan |= (q[i].x != q[i].x) || (q[i].y != q[i].y);
+    top = fmaxf(top, q[i].x);
+  }
+  top = wave_max(top);
+  double sum = 0.0;
+  if (top != -INFINITY)
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (q[i].x != -INFINITY)
+        sum += static_cast<double>(q[i].y) *
+               static_cast<double>(fast_exp2(static_cast<float>(static_cast<double>(q[i].x) - top) * kLog2e));
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  double lam = top == -INFINITY ? -INFINITY : static_cast<double>(top) + log(sum);
+  if (__ballot(nan) != 0) lam = __longlong_as_double(0x7ff8000000000000LL);
+  const int m = R.rows ? R.rows[j] : j;
   const int tok = a.tokens[m];
   const bool counted = tok >= 0 && tok < V;
+  constexpr int kBytes = BF ? 2 : 4;
+  const char* const row = static_cast<const char*>(H) + static_cast<int64_t>(j) * D * kBytes;
   double z = 0.0;
   if (counted) {
-    constexpr int kBytes = BF ? 2 : 4;
-    z = dot_share<BF>(static_cast<const char*>(H) + static_cast<int64_t>(m) * D * kBytes,
-                      static_cast<const char*>(W) + static_cast<int64_t>(tok) * D * kBytes, D, lane);
+    z = dot_share<BF>(row, static_cast<const char*>(W) + static_cast<int64_t>(tok) * D * kBytes, D, lane);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) z += __shfl_xor(z, o, 64);
   }
-  if (lane != 0) return;
   float lp32 = 0.f, loss32 = 0.f, g32 = 0.f;
   int status = 1;  // left out
   if (counted) {
     if (bias) z += static_cast<double>(bias[tok]);
-    const double lp = z - lam[m];
+    const double lp = z - lam;
     const double A = a.adv[m], w = a.weights ? static_cast<double>(a.weights[m]) : 1.0;
     double loss = 0.0, c = 0.0;
     if (A != 0.0) {  // (a NaN is not)
@@ -93,36 +198,46 @@ policy_tokens(const void* __restrict__ H, int M, int D, const void* __restrict__
       loss32 = g32 = 0.f;
     }
   }
+  if (mask && g32 == 0.f) {
+    uint16_t* const out = mask + static_cast<int64_t>(j) * D;
+    for (int d = lane * 8; d < D; d += 512) *reinterpret_cast<u32x4*>(out + d) = u32x4{0u, 0u, 0u, 0u};
+  }
+  if (lane != 0) return;
+  const double l2 = lam * kLog2eD;
+  const float hi2 = static_cast<float>(l2);
+  R.lam2[j] = make_float2(hi2, static_cast<float>(l2 - static_cast<double>(hi2)));
+  R.g[j] = g32;
+  R.token[j] = tok;
+  R.logp[j] = lp32;
   a.logp[m] = lp32;
   a.losses[m] = loss32;
   a.status[m] = status;
-  g[m] = g32;
 }
 
-// loss = sum of w_m loss_m over the counted tokens, in double and a fixed order.
-__global__ void __launch_bounds__(kLossThreads)
-policy_sum(const float* __restrict__ losses, const float* __restrict__ weights, const int32_t* __restrict__ status,
-           int M, double* __restrict__ loss) {
-  __shared__ double sh[kLossThreads / 64];
+// The sum of w_n losses_n over the counted tokens, in double and a fixed order.
+__device__ __forceinline__ void sum_losses(const DzTokens& t) {
+  __shared__ double sh[kThreads / 64];
   double s = 0.0;
 #pragma unroll 4
-  for (int m = threadIdx.x; m < M; m += kLossThreads)
-    if (status[m] == 0) s += static_cast<double>(losses[m]) * (weights ? static_cast<double>(weights[m]) : 1.0);
+  for (int n = threadIdx.x; n < t.N; n += kThreads)
+    if (t.status[n] == 0) s += static_cast<double>(t.losses[n]) * (t.weights ? static_cast<double>(t.weights[n]) : 1.0);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    double t = 0.0;
-    for (int w = 0; w < kLossThreads / 64; ++w) t += sh[w];
-    *loss = t;
-  }
+  if (threadIdx.x == 0) *t.loss = ((sh[0] + sh[1]) + sh[2]) + sh[3];
 }
 
-// The tokens' own entries of a chunk: g (1 - p), 1 - p = -expm1(lp).
+// The tokens' own entries of a chunk: g (1 - p), 1 - p = -expm1(lp).  The last workgroup of a launch that sums
+// does nothing else.
 template <bool BF>
 __global__ void __launch_bounds__(kThreads)
 dz_tokens(void* __restrict__ dZ, int pitch, int M, int c0, int cw, DzTokens t, float scale) {
+  if (t.loss && blockIdx.x + 1 == gridDim.x) {
+    sum_losses(t);
+    return;
+  }
+  if (t.Mdev) M = min(M, *t.Mdev);
   const int m = blockIdx.x * kThreads + threadIdx.x;
   if (m >= M) return;
   const int v = t.token[m] - c0;
@@ -137,7 +252,9 @@ dz_tokens(void* __restrict__ dZ, int pitch, int M, int c0, int cw, DzTokens t, f
 // db of a bf16 chunk: column sums of dZ over slices of the frames, then over the slices.  32 lanes of 8
 // columns and 8 frames at a time.
 __global__ void __launch_bounds__(kThreads)
-db_slices(const uint16_t* __restrict__ dZ, int M, int pitch, int mper, float* __restrict__ part) {
+db_slices(const uint16_t* __restrict__ dZ, int M, int pitch, int mper, float* __restrict__ part,
+          const int32_t* __restrict__ Mdev) {
+  if (Mdev) M = min(M, *Mdev);
   __shared__ float x[8][kThreads];
   const int col = (threadIdx.x & 31) * 8, row = threadIdx.x >> 5;
   const int v = blockIdx.x * 256 + col;  // the pitch is a multiple of 256
@@ -169,14 +286,24 @@ db_join(const float* __restrict__ part, int slices, int pitch, int cw, uint16_t*
   db[v] = f32_to_bf16(s);
 }
 
-// dH = the split-K slices' sum, rounded to bf16; n a multiple of 8.
+// dH[m] = the split-K slices' sum of place inv[m], rounded to bf16 (zeros for a row that is left out).  n
+// values, a multiple of 4; the slices lie *count D values apart.
 __global__ void __launch_bounds__(kThreads)
-dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, uint16_t* __restrict__ dH) {
+dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, int D, const int32_t* __restrict__ inv,
+              const int32_t* __restrict__ count, uint16_t* __restrict__ dH) {
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
   if (i >= n) return;
-  float4 s = *reinterpret_cast<const float4*>(part + i);
+  const int m = static_cast<int>(i / D), j = inv[m];
+  if (j < 0) {
+    *reinterpret_cast<u32x2*>(dH + i) = u32x2{0u, 0u};
+    return;
+  }
+  const int64_t step = static_cast<int64_t>(*count) * D;
+  const float* at = part + static_cast<int64_t>(j) * D + (i - static_cast<int64_t>(m) * D);
+  float4 s = *reinterpret_cast<const float4*>(at);
+#pragma unroll 4
   for (int k = 1; k < splits; ++k) {
-    const float4 p = *reinterpret_cast<const float4*>(part + k * n + i);
+    const float4 p = *reinterpret_cast<const float4*>(at + k * step);
     s.x += p.x;
     s.y += p.y;
     s.z += p.z;
@@ -189,10 +316,12 @@ constexpr int kDbSlices = 16;
 
 }  // namespace
 
-hipError_t launch_dz_tokens(int dtype, void* dZ, int pitch, int M, int c0, int cw, const DzTokens& t, float scale,
+hipError_t launch_dz_tokens(int dtype, void* dZ, int pitch, int M, int c0, int cw, const DzTokens& tokens, float scale,
                             hipStream_t stream) {
   Prof pr("dz_tokens", stream);
-  const dim3 grid((M + kThreads - 1) / kThreads);
+  DzTokens t = tokens;
+  if (c0 > 0) t.loss = nullptr;
+  const dim3 grid((M + kThreads - 1) / kThreads + (t.loss ? 1 : 0));
   if (dtype == 1) hipLaunchKernelGGL(dz_tokens<true>, grid, dim3(kThreads), 0, stream, dZ, pitch, M, c0, cw, t, scale);
   else hipLaunchKernelGGL(dz_tokens<false>, grid, dim3(kThreads), 0, stream, dZ, pitch, M, c0, cw, t, scale);
   return hipGetLastError();
@@ -208,14 +337,20 @@ PolicyLayout policy_layout(int dtype, int M, int D, int V, bool bias, bool grads
     at += align_up(bytes, 256);
     return o;
   };
-  L.o_lam = take(m * sizeof(double));
   L.o_lam2 = take(m * sizeof(float2));
   L.o_g = take(m * sizeof(float));
+  L.o_tok = take(m * sizeof(int32_t));
+  L.o_lp = take(m * sizeof(float));
+  if (dtype == 1) {
+    L.o_rows = take(m * sizeof(int32_t));
+    L.o_inv = take(m * sizeof(int32_t));
+    L.o_count = take((m / kCountRows + 2) * sizeof(int32_t));
+    L.o_h = take(m * D * sizeof(uint16_t));
+  }
   const size_t fwd = at;
   L.o_part = take(lse_partial_bytes(M, D));
-  const bool ht = dtype == 1 && (bias ? bias_reads_ht_bf16(M, D) : frames_from_ht_bf16(M, D, V));
-  L.o_ht = take(ht ? lse_ht_bytes_bf16(M, D) : 0);
-  if (!ht) L.o_ht = 0;
+  L.ht = dtype == 1 && (bias ? bias_reads_ht_bf16(M, D) : frames_from_ht_bf16(M, D, V));
+  L.o_ht = take(L.ht ? lse_ht_bytes_bf16(M, D) : 0);
   if (grads) {
     // the backward's room is that of the normaliser, which is done
     const size_t end = at;
@@ -229,18 +364,19 @@ PolicyLayout policy_layout(int dtype, int M, int D, int V, bool bias, bool grads
   return L;
 }
 
-static hipError_t policy_bwd_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
-                                  const float2* lam2, const DzTokens& tokens, uint16_t* dH, uint16_t* dW, uint16_t* db,
-                                  char* scratch, const BwdPlan& plan, float* one, hipStream_t stream) {
+// Hc: the counted rows, those without a gradient cleared; tokens.Mdev of them.
+static hipError_t policy_bwd_bf16(uint16_t* Hc, int M, int D, const uint16_t* W, const float* bias, int V,
+                                  const float2* lam2, const DzTokens& tokens, const int32_t* inv, uint16_t* dH,
+                                  uint16_t* dW, uint16_t* db, char* scratch, const BwdPlan& plan, float* one,
+                                  hipStream_t stream) {
   uint16_t* dZ = reinterpret_cast<uint16_t*>(scratch);
-  uint16_t* Hs = bwd_hs(scratch, plan);
   uint16_t* Hst = bwd_hst(scratch, plan);
   float* part = one ? one : reinterpret_cast<float*>(scratch + plan.dz_bytes + plan.ht_bytes);
   float* dbpart = reinterpret_cast<float*>(scratch + plan.dz_bytes + plan.ht_bytes + plan.part_bytes + plan.lam2_bytes);
   const int chunk = plan.chunk;
-  hipError_t e = Hst ? launch_ht_build_bf16(H, M, D, tokens.g, Hs, Hst, plan.Mp, stream)
-                     : launch_hs_build_bf16(H, M, D, tokens.g, Hs, stream);
-  if (e != hipSuccess) return e;
+  hipError_t e;
+  // (rows behind the last counted one hold anything; their columns of the transpose reach no result)
+  if (Hst && (e = launch_ht_build_bf16(Hc, M, D, nullptr, nullptr, Hst, plan.Mp, stream)) != hipSuccess) return e;
   // slices of the dH product as in the Pruned CTC backward
   const int slice = (chunk / plan.splits + 63) / 64 * 64;
   const int nslices = ((chunk < V ? chunk : V) + slice - 1) / slice;
@@ -251,27 +387,28 @@ static hipError_t policy_bwd_bf16(const uint16_t* H, int M, int D, const uint16_
       sl = ((cw + nslices - 1) / nslices + 63) / 64 * 64;
       if (sl < 64) sl = 64;
     }
-    e = launch_bwd_chunk_bf16(Hs, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
-                              sl, true, false, false, nullptr, nullptr, nullptr, stream, nullptr, nullptr, Hst, plan.Mp);
+    e = launch_bwd_chunk_bf16(Hc, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
+                              sl, true, false, false, nullptr, nullptr, nullptr, stream, nullptr, nullptr, Hst, plan.Mp,
+                              nullptr, tokens.Mdev);
     if (e != hipSuccess) return e;
     if ((e = launch_dz_tokens(1, dZ, chunk, M, c0, cw, tokens, 1.f, stream)) != hipSuccess) return e;
     if (db) {
       Prof pr("db_colsum", stream);
       const int most = (M + 127) / 128 < kDbSlices ? (M + 127) / 128 : kDbSlices;  // (dbpart has a row per 128 frames)
       const int mper = ((M + most - 1) / most + 7) / 8 * 8, slices = (M + mper - 1) / mper, tiles = (cw + 255) / 256;
-      hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart);
+      hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart, tokens.Mdev);
       hipLaunchKernelGGL(db_join, dim3(tiles), dim3(kThreads), 0, stream, dbpart, slices, chunk, cw, db + c0);
     }
-    e = launch_bwd_chunk_bf16(Hs, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
+    e = launch_bwd_chunk_bf16(Hc, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
                               sl, false, dH != nullptr, dW != nullptr, nullptr, nullptr, nullptr, stream, nullptr, nullptr,
-                              Hst, plan.Mp, dW);
+                              Hst, plan.Mp, dW, tokens.Mdev);
     if (e != hipSuccess) return e;
   }
   if (dH) {
     const int64_t n = static_cast<int64_t>(M) * D;
     Prof pr("dh_reduce", stream);
     hipLaunchKernelGGL(dh_reduce_b16, dim3(static_cast<unsigned>((n / 4 + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                       stream, part, one ? 1 : nslices, n, dH);
+                       stream, part, one ? 1 : nslices, n, D, inv, tokens.Mdev, dH);
   }
   return hipGetLastError();
 }
@@ -286,29 +423,70 @@ hipError_t launch_policy_loss(int dtype, const void* H, int M, int D, const void
     if (dW && (e = launch_clear(dW, es * V * D, stream)) != hipSuccess) return e;
     return db ? launch_clear(db, es * V, stream) : hipSuccess;
   }
-  double* lam = reinterpret_cast<double*>(ws + L.o_lam);
+  const bool grads = dH || dW || db;
+  auto i32 = [&](size_t o) { return reinterpret_cast<int32_t*>(ws + o); };
+  auto f32 = [&](size_t o) { return reinterpret_cast<float*>(ws + o); };
+  float2* partials = reinterpret_cast<float2*>(ws + L.o_part);
   float2* lam2 = reinterpret_cast<float2*>(ws + L.o_lam2);
-  float* g = reinterpret_cast<float*>(ws + L.o_g);
-  e = launch_lse(dtype, H, M, D, W, bias, V, reinterpret_cast<float2*>(ws + L.o_part), lam, lam2, stream,
-                 L.o_ht ? reinterpret_cast<uint16_t*>(ws + L.o_ht) : nullptr);
-  if (e != hipSuccess) return e;
-  {
-    Prof pr("policy_tokens", stream);
-    const dim3 grid((M + kThreads / 64 - 1) / (kThreads / 64));
-    if (dtype == 1)
-      hipLaunchKernelGGL(policy_tokens<true>, grid, dim3(kThreads), 0, stream, H, M, D, W, bias, V, lam, a, g);
-    else hipLaunchKernelGGL(policy_tokens<false>, grid, dim3(kThreads), 0, stream, H, M, D, W, bias, V, lam, a, g);
-    hipLaunchKernelGGL(policy_sum, dim3(1), dim3(kLossThreads), 0, stream, a.losses, a.weights, a.status, M, a.loss);
+  PolicyRows R{nullptr, nullptr, partials, 0, lam2, f32(L.o_g), i32(L.o_tok), f32(L.o_lp)};
+  const dim3 grid((M + kLossThreads / 64 - 1) / (kLossThreads / 64));
+  DzTokens tokens{R.token, R.logp, R.g};
+  tokens.losses = a.losses;
+  tokens.weights = a.weights;
+  tokens.status = a.status;
+  tokens.N = M;
+  tokens.loss = a.loss;
+  if (dtype == 1) {
+    uint16_t* Hc = reinterpret_cast<uint16_t*>(ws + L.o_h);
+    const uint16_t* Wb = static_cast<const uint16_t*>(W);
+    int32_t *const count = i32(L.o_count), *const counts = count + 1;
+    const bool many = M > 4 * kCountRows;
+    {
+      Prof pr("policy_gather", stream);
+      if (many)
+        hipLaunchKernelGGL(policy_count, dim3((M + kCountRows - 1) / kCountRows), dim3(kThreads), 0, stream, a.tokens, M, V,
+                           counts);
+      hipLaunchKernelGGL(policy_gather, dim3((M + kGatherRows - 1) / kGatherRows), dim3(kThreads), 0, stream,
+                         static_cast<const uint16_t*>(H), M, D, V, a, many ? counts : nullptr, Hc, i32(L.o_rows),
+                         i32(L.o_inv), count);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (L.ht) {
+      uint16_t* Ht = reinterpret_cast<uint16_t*>(ws + L.o_ht);
+      const int Mp = (M + 63) / 64 * 64;
+      if ((e = launch_ht_build_bf16(Hc, M, D, nullptr, nullptr, Ht, Mp, stream)) != hipSuccess) return e;
+      e = launch_lse_partial_e_bf16(Hc, M, D, Wb, bias, V, partials, &R.P, nullptr, 0, 0, nullptr, stream, Ht, Mp, false,
+                                    count);
+    } else {
+      e = launch_lse_partial_bf16(Hc, M, D, Wb, bias, V, partials, &R.P, stream, false, count);
+    }
+    if (e != hipSuccess) return e;
+    R.rows = i32(L.o_rows);
+    R.count = tokens.Mdev = count;
+    {
+      Prof pr("policy_tokens", stream);
+      hipLaunchKernelGGL(policy_tokens<true>, grid, dim3(kLossThreads), 0, stream, Hc, M, D, W, bias, V, R, a,
+                         grads ? Hc : nullptr);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (grads)
+      return policy_bwd_bf16(Hc, M, D, Wb, bias, V, lam2, tokens, i32(L.o_inv), static_cast<uint16_t*>(dH),
+                             static_cast<uint16_t*>(dW), static_cast<uint16_t*>(db), ws + L.o_bwd, L.bwd,
+                             L.bwd.part_bytes == 0 ? f32(L.o_dh) : nullptr, stream);
+  } else {
+    if ((e = launch_lse_partials(0, H, M, D, W, bias, V, partials, &R.P, stream)) != hipSuccess) return e;
+    {
+      Prof pr("policy_tokens", stream);
+      hipLaunchKernelGGL(policy_tokens<false>, grid, dim3(kLossThreads), 0, stream, H, M, D, W, bias, V, R, a, nullptr);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (grads)
+      return head_bwd_f32(static_cast<const float*>(H), M, D, static_cast<const float*>(W), bias, V, lam2, nullptr, 0, R.g,
+                          nullptr, static_cast<float*>(dH), static_cast<float*>(dW), static_cast<float*>(db),
+                          ws + L.o_bwd, L.bwd, stream, &tokens);
   }
-  if ((e = hipGetLastError()) != hipSuccess || (!dH && !dW && !db)) return e;
-  const DzTokens tokens{a.tokens, a.logp, g};
-  if (dtype == 1)
-    return policy_bwd_bf16(static_cast<const uint16_t*>(H), M, D, static_cast<const uint16_t*>(W), bias, V, lam2, tokens,
-                           static_cast<uint16_t*>(dH), static_cast<uint16_t*>(dW), static_cast<uint16_t*>(db), ws + L.o_bwd,
-                           L.bwd, L.bwd.part_bytes == 0 ? reinterpret_cast<float*>(ws + L.o_dh) : nullptr, stream);
-  return head_bwd_f32(static_cast<const float*>(H), M, D, static_cast<const float*>(W), bias, V, lam2, nullptr, 0, g,
-                      nullptr, static_cast<float*>(dH), static_cast<float*>(dW), static_cast<float*>(db), ws + L.o_bwd,
-                      L.bwd, stream, &tokens);
+  // no chunk to sum beside
+  return launch_dz_tokens(dtype, nullptr, 0, 0, 0, 0, tokens, 1.f, stream);
 }
 
 }  // namespace pctc

@@ -393,7 +393,9 @@ def test_policy_loss_of_rows_that_are_not_finite(dtype):
         status = np.zeros(M, np.int32)
         status[bad] = code
         check_policy(c0, dtype, (0.2, 0.3), 0.0, got, status=status)
-        for k in ("loss", "losses", "dH", "dW") if dtype == "bf16" else ():
+        # (counted rows take a place in dW's sums, so that the others are added in other groups)
+        same = ("loss", "losses", "dH") + (("dW",) if code == pc.TOKEN_LEFT_OUT else ())
+        for k in same if dtype == "bf16" else ():
             assert torch.equal(got[k], want[k]), k
     # a ratio beyond every bound: clipped where that lowers the objective, left out where it does not
     adv3, old3 = torch.ones_like(adv), old.clone()
@@ -402,6 +404,24 @@ def test_policy_loss_of_rows_that_are_not_finite(dtype):
     got = args(H, t, adv3, old3)
     assert got["status"][7] == 0 and got["losses"][7] == -np.float32(1 + np.float64(np.float32(0.3))) and not got["dH"][7].any()
     assert got["status"][8] == pc.TOKEN_NONFINITE and got["losses"][8] == 0 and torch.isfinite(got["dW"].float()).all()
+
+
+@pytest.mark.parametrize("M,counted", [(1, 0), (300, 0), (300, 1), (700, 255), (700, 256), (700, 257), (700, 513), (40_000, 300),
+                                       (33_000, 32_999)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_policy_loss_of_few_counted_rows(M, counted, bias):
+    """Any share of the rows left out, in blocks and scattered."""
+    say("policy_loss few counted", M, counted, bias)
+    D, V = 128, 300
+    c = policy_case(M + counted, M, D, V, "bf16", bias)
+    r = np.random.default_rng(M + counted)
+    rows = np.sort(r.choice(M, counted, replace=False)) if counted % 2 else np.arange(M - counted, M)
+    t = np.full(M, -1)
+    t[rows] = np.abs(c["tokens"][rows]) % V
+    c.update(tokens=t, old=None)
+    got = policy_call(c, "bf16", (0.2, 0.3), 0.1, want_db=True, chunk=256)
+    check_policy(c, "bf16", (0.2, 0.3), 0.1, got, db=True)
+    assert counted or not any(got[k].any() for k in ("dH", "dW", "db", "loss"))
 
 
 def test_policy_loss_without_rows_and_in_a_graph():
