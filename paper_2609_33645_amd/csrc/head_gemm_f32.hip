@@ -441,6 +441,7 @@ db_reduce_f32(const float* __restrict__ dbpart, int slices, int chunk, int cw, f
   const int v = blockIdx.x * 256 + threadIdx.x;
   if (v >= cw) return;
   float s = 0.f;
+#pragma unroll 16
   for (int z = 0; z < slices; ++z) s += dbpart[static_cast<int64_t>(z) * chunk + v];
   db[v] = s * kDzUnscale;
 }

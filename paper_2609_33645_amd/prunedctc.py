@@ -1003,16 +1003,16 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
     if adv is None:
         raise PrunedCTCError(-1, "no advantages")
     lo, hi = (math.inf, math.inf) if clip is None else clip
-    dH = _out(dH_out, (M, D), H.dtype, dev, "dH_out") if want_dH else None
-    dW = _out(dW_out, (V, D), H.dtype, dev, "dW_out") if want_dW else None
-    db = torch.empty(V, dtype=H.dtype, device=dev) if want_db else None
+    dH = _out(dH_out, (M, D), H.dtype, H, "dH_out") if want_dH else None
+    dW = _out(dW_out, (V, D), H.dtype, H, "dW_out") if want_dW else None
+    db = H.new_empty(V) if want_db else None
     nbytes = int(L.pctc_policy_workspace_size(dt, M, D, V, int(bias is not None), int(want_dH or want_dW or want_db),
                                               int(chunk)))
     if nbytes == 0:
         _check(-1, "pctc_policy_loss")
-    loss = torch.empty(1, dtype=torch.float64, device=dev)
-    losses, logp = torch.empty((2, M), dtype=torch.float32, device=dev).unbind()
-    status = torch.empty(M, dtype=torch.int32, device=dev)
+    loss = H.new_empty(1, dtype=torch.float64)
+    losses, logp = H.new_empty((2, M), dtype=torch.float32).unbind()
+    status = H.new_empty(M, dtype=torch.int32)
     ws = _scratch(nbytes, dev)
     at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     code = L.pctc_policy_loss(dt, at(H), M, D, at(W), at(bias), V, at(tokens), at(adv), at(old), at(ref), at(w), float(lo),
@@ -1025,10 +1025,11 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
 
 # ---- below the head ----------------------------------------------------------------------
 
-def _out(out: Optional[torch.Tensor], shape, dtype: torch.dtype, dev: torch.device, what: str = "out") -> torch.Tensor:
-    """A new tensor, or the caller's, which must be one of that shape."""
+def _out(out: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.Tensor, what: str = "out") -> torch.Tensor:
+    """A new tensor, or the caller's, which must be one of that shape (on the device of `like`)."""
+    dev = like.device
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)  # (half the time of torch.empty with a device)
     if out.dtype is not dtype or tuple(out.shape) != tuple(shape) or out.device != dev or not out.is_contiguous():
         raise PrunedCTCError(-1, f"{what} must be contiguous {dtype} {tuple(shape)} on {dev}")
     return out
@@ -1062,7 +1063,7 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset=0, residual: Optional[t
         if offset.dtype is not torch.int64 or offset.numel() != 1 or offset.device != dev:
             raise PrunedCTCError(-1, f"offset must be a whole number or an int64 tensor of one on {dev}")
         counter, offset = offset, 0
-    y = _out(out, x.shape, x.dtype, dev)
+    y = _out(out, x.shape, x.dtype, x)
     code = lib().pctc_dropout(dt, x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(),
                               float(p), _u64(seed, "seed"), _u64(offset, "offset"),
                               None if counter is None else counter.data_ptr(), _raw_stream(dev))
@@ -1087,7 +1088,7 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out
     dt, dev, (V, D) = _dtype_code(table), table.device, table.shape
     table = table.contiguous()
     tokens, size = _token_args(tokens, dev)
-    y = _out(out, (*tokens.shape, D), table.dtype, dev)
+    y = _out(out, (*tokens.shape, D), table.dtype, table)
     code = lib().pctc_embedding(dt, table.data_ptr(), V, D, tokens.data_ptr(), size, tokens.numel(), float(scale),
                                 y.data_ptr(), _raw_stream(dev))
     if code:
@@ -1117,7 +1118,7 @@ def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, V: int, scale: fl
         raise PrunedCTCError(-1, f"unsupported dtype {kind}")
     if V < 1 or D < 1:
         raise PrunedCTCError(-1, "V and D must be positive")
-    dW = _out(out, (V, D), kind, dev)
+    dW = _out(out, (V, D), kind, dy)
     dy = dy.contiguous()
     L = lib()
     nbytes = L.pctc_embedding_backward_workspace_size(N, D)
@@ -1164,8 +1165,8 @@ def gated_ffn(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down:
     nbytes = L.pctc_gated_ffn_workspace_size(dt, M, D, F, O, 0)
     if nbytes == 0:
         _check(-1, "pctc_gated_ffn")
-    y = _out(out, (*lead, O), x.dtype, dev)
-    a, b = (torch.empty((*lead, F), dtype=torch.float32, device=dev) for _ in range(2)) if keep else (None, None)
+    y = _out(out, (*lead, O), x.dtype, x)
+    a, b = (x.new_empty((*lead, F), dtype=torch.float32) for _ in range(2)) if keep else (None, None)
     ws = _scratch(nbytes, dev)
     code = L.pctc_gated_ffn(dt, x.data_ptr(), M, D, wg.data_ptr(), wu.data_ptr(), F, wd.data_ptr(), O, act,
                             a.data_ptr() if keep else None, b.data_ptr() if keep else None, y.data_ptr(), ws.data_ptr(),
@@ -1200,6 +1201,74 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up
     if code:
         _check(code, "pctc_gated_ffn_backward")
     return dict(zip(("dx", "dw_gate", "dw_up", "dw_down"), (dx, *dws)))
+
+
+class Dropout(torch.autograd.Function):
+    """Autograd wrapper of dropout().  The mask is made again in the backward, from the counters of the forward (a
+    device tensor's value is copied: the caller may move it on before)."""
+
+    @staticmethod
+    def forward(ctx, x, p, seed, offset, residual):
+        ctx.p, ctx.seed, ctx.has_residual = p, seed, residual is not None
+        ctx.offset = offset.clone() if isinstance(offset, torch.Tensor) else offset
+        return dropout(x.detach(), p, seed, ctx.offset, None if residual is None else residual.detach())
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx = dropout(dy, ctx.p, ctx.seed, ctx.offset) if ctx.needs_input_grad[0] else None
+        return dx, None, None, None, dy if ctx.has_residual and ctx.needs_input_grad[4] else None
+
+
+class Embedding(torch.autograd.Function):
+    """Autograd wrapper of embedding(); the table's gradient has its type."""
+
+    @staticmethod
+    def forward(ctx, table, tokens, scale):
+        ctx.save_for_backward(tokens)
+        ctx.scale, ctx.V = scale, int(table.shape[0])
+        return embedding(table.detach(), tokens, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        return (embedding_backward(dy, *ctx.saved_tensors, ctx.V, ctx.scale) if ctx.needs_input_grad[0] else None), None, None
+
+
+class GatedFFN(torch.autograd.Function):
+    """Autograd wrapper of gated_ffn()."""
+
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, activation):
+        r = gated_ffn(x.detach(), w_gate.detach(), w_up.detach(), w_down.detach(), activation,
+                      keep=any(ctx.needs_input_grad[:4]))
+        ctx.activation = activation
+        ctx.save_for_backward(x, r["gate"], r["up"], w_gate, w_up, w_down)
+        return r["y"]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, gate, up, wg, wu, wd = (t.detach() for t in ctx.saved_tensors)
+        need = ctx.needs_input_grad
+        r = gated_ffn_backward(dy, x, gate, up, wg, wu, wd, ctx.activation, want_dx=need[0], want_dw=any(need[1:4]))
+        return r["dx"], *(r[k] if n else None for k, n in zip(("dw_gate", "dw_up", "dw_down"), need[1:4])), None
+
+
+def dropout_layer(x: torch.Tensor, p: float, seed: int, offset=0, residual: Optional[torch.Tensor] = None):
+    """dropout() with gradients for x and residual."""
+    return Dropout.apply(x, p, seed, offset, residual)
+
+
+def embedding_layer(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0):
+    """embedding() with a gradient for the table."""
+    return Embedding.apply(table, tokens, scale)
+
+
+def gated_ffn_layer(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                    activation: str = "silu"):
+    """gated_ffn()'s y with gradients for x and the weights."""
+    return GatedFFN.apply(x, w_gate, w_up, w_down, activation)
 
 
 # ---- kernel timing -----------------------------------------------------------------------

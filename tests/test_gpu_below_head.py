@@ -526,3 +526,168 @@ def test_gated_ffn(dtype, M, D, F_, O, act):
     dx, dw = back(want_dw=False), back(want_dx=False)
     assert torch.equal(dx["dx"], grads["dx"]) and dx["dw_gate"] is None and dw["dx"] is None
     assert all(torch.equal(dw[k], grads[k]) for k in ("dw_gate", "dw_up", "dw_down"))
+
+
+# ---- together ------------------------------------------------------------------------------
+
+def test_layers_in_autograd_against_the_formulas():
+    """tokens -> embedding -> dropout -> gated block with residual dropout -> head -> policy loss, the head tied to
+    the embedding: every gradient against the same chain in float64 (masks from the reference generator)."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("layers together")
+    torch.manual_seed(3)
+    V, D, F_, M, p = 211, 64, 136, 90, 0.2
+    E0, wg, wu, wd = (torch.randn(s, device="cuda") / s[1] ** 0.5 for s in ((V, D), (F_, D), (F_, D), (D, F_)))
+    leaves = [t.clone().requires_grad_() for t in (E0, wg, wu, wd)]
+    t = torch.randint(-1, V, (M,), device="cuda", dtype=torch.int32)
+    nxt, adv = torch.randint(-1, V, (M,), device="cuda"), torch.randn(M, device="cuda")
+    n = M * D
+    e = pc.embedding_layer(leaves[0], t, 2.0)
+    x = pc.dropout_layer(e, p, 77, 0)
+    y = pc.dropout_layer(pc.gated_ffn_layer(x, *leaves[1:], "gelu"), p, 77, n // 8, residual=x)
+    y.retain_grad()
+    out = pc.policy_loss(y.detach(), E0, nxt, adv)
+    grads = list(torch.autograd.grad(y, leaves, out["dH"], retain_graph=True))
+    # tied: the head's gradient and the embedding's in one buffer
+    de = torch.autograd.grad(y, e, out["dH"])[0]
+    tied = pc.embedding_backward(de, t, V, 2.0, out=out["dW"].clone(), accumulate=True)
+    k1, k2 = (dev(ref.kept(n, p, 77, o)).view(M, D) for o in (0, n // 8))
+    s = 65536 / ref.threshold(p)
+    L = [q.double().requires_grad_() for q in (E0, wg, wu, wd, E0)]
+    ok = (t >= 0)[:, None]
+    x = torch.where(k1, torch.where(ok, L[0][t.clamp(min=0).long()], 0.0) * 2.0 * s, 0.0)
+    a = x @ L[1].T
+    h = 0.5 * a * (1 + torch.erf(a / math.sqrt(2))) * (x @ L[2].T)
+    y64 = x + torch.where(k2, (h @ L[3].T) * s, 0.0)
+    lp = torch.log_softmax(y64 @ L[4].T, 1).gather(1, nxt.clamp(min=0)[:, None])[:, 0]
+    loss = -(torch.where(nxt >= 0, lp, 0.0) * adv).sum()  # (the gradient of r A at r = 1)
+    want = torch.autograd.grad(loss, L)
+    # float chains of a few hundred products of values of order one, against the largest of each gradient: 2e-5
+    for name, g, w in (*zip(("table", "gate", "up", "down"), grads, want), ("head", out["dW"], want[4]),
+                       ("tied", tied, want[0] + want[4])):
+        assert float((g.double() - w).abs().max()) <= 2e-5 * float(w.abs().max()), name
+
+
+def test_layers_only_form_what_is_asked():
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("layers asked")
+    x, w, wd = torch.randn(5, 16, device="cuda"), torch.randn(24, 16, device="cuda"), torch.randn(16, 24, device="cuda")
+    w2 = w.clone().requires_grad_()
+    y = pc.gated_ffn_layer(x, w, w2, wd)
+    (g,) = torch.autograd.grad(y.sum(), [w2])
+    full = pc.gated_ffn(x, w, w, wd, keep=True)
+    assert torch.equal(g, pc.gated_ffn_backward(torch.ones_like(x), x, full["gate"], full["up"], w, w, wd)["dw_up"])
+    # the mask of the backward is the forward's, wherever the caller's counter has gone
+    c = torch.tensor([5], device="cuda")
+    x.requires_grad_()
+    r = torch.randn(5, 16, device="cuda", requires_grad=True)
+    y = pc.dropout_layer(x, 0.5, 3, c, r)
+    c += 1000
+    gx, gr = torch.autograd.grad(y.sum(), [x, r])
+    assert torch.equal(gx, pc.dropout(torch.ones_like(x), 0.5, 3, 5)) and torch.equal(gr, torch.ones_like(r))
+
+
+@pytest.mark.parametrize("op", ["dropout", "embedding", "embedding_backward", "gated_ffn", "gated_ffn_backward", "policy_loss"])
+def test_on_a_given_stream_and_in_a_graph(op):
+    """The same bits on another stream (its inputs let go of at once) and from a captured graph replayed with eager
+    calls, other inputs and synchronizations between."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("streams and graphs", op)
+    torch.manual_seed(len(op))
+    M, D, F_, V = 200, 72, 136, 500
+    bf = torch.bfloat16
+    x, dy = (torch.randn(M, D, device="cuda").to(bf) for _ in range(2))
+    wg, wu = (torch.randn(F_, D, device="cuda").to(bf) for _ in range(2))
+    wd, W = torch.randn(D, F_, device="cuda").to(bf), torch.randn(V, D, device="cuda").to(bf)
+    t = torch.randint(-1, V, (M,), device="cuda", dtype=torch.int32)
+    adv = torch.randn(M, device="cuda")
+    a, b = (torch.randn(M, F_, device="cuda") for _ in range(2))
+    calls = {
+        "dropout": lambda x, **k: [pc.dropout(x, 0.3, 4, 9, residual=dy, **k)],
+        "embedding": lambda x, **k: [pc.embedding(x, t, 0.5, **k)],
+        "embedding_backward": lambda x, **k: [pc.embedding_backward(x, t, V, dtype=torch.float32, **k)],
+        "gated_ffn": lambda x, **k: list(pc.gated_ffn(x, wg, wu, wd, keep=True, **k).values()),
+        "gated_ffn_backward": lambda x, **k: list(pc.gated_ffn_backward(dy, x, a, b, wg, wu, wd, **k).values()),
+        "policy_loss": lambda x, **k: [v for v in pc.policy_loss(x, W, t, adv, **k).values() if v is not None],
+    }
+    call = calls[op]
+    want = call(x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    given = [call(x, stream=s) for _ in range(3)]
+    torch.cuda.current_stream().wait_stream(s)
+    for got in given:
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
+    # an input that the caller lets go of while the call's stream still has work before it
+    tmp = x.clone()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    got = call(tmp, stream=s)
+    del tmp
+    junk = [torch.full_like(x, 9.0) for _ in range(8)]
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
+    del junk
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call(x)
+    for i in range(4):
+        x.normal_()
+        t.copy_(torch.randint(-1, V, (M,), device="cuda"))
+        graph.replay()
+        want = call(x)
+        assert all(torch.equal(g, w) for g, w in zip(got, want)), i
+        torch.cuda.synchronize()
+
+
+def test_two_graphs_and_two_streams_at_once():
+    """Calls in flight on two streams, and two captured graphs replayed on them, do not share memory."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("two at once")
+    torch.manual_seed(1)
+    V, D, F_ = 3000, 128, 264
+    W = torch.randn(V, D, device="cuda").bfloat16()
+    w = [torch.randn(s, device="cuda").bfloat16() for s in ((F_, D), (F_, D), (D, F_))]
+
+    def step(x, t, adv):
+        y = pc.gated_ffn(x, *w, keep=True)
+        r = pc.policy_loss(y["y"], W, t, adv)
+        g = pc.gated_ffn_backward(r["dH"], x, y["gate"], y["up"], *w)
+        return [r["dW"], r["losses"], *g.values(), pc.embedding_backward(g["dx"], t, V)]
+
+    data = [(torch.randn(M, D, device="cuda").bfloat16(), torch.randint(-1, V, (M,), device="cuda", dtype=torch.int32),
+             torch.randn(M, device="cuda")) for M in (300, 900)]
+    want = [step(*d) for d in data]
+    streams = [torch.cuda.Stream() for _ in data]
+    graphs, outs = [], []
+    for d, s in zip(data, streams):
+        s.wait_stream(torch.cuda.current_stream())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(step(*d))
+        graphs.append(g)
+    for _ in range(3):
+        eager = []
+        for d, s, g in zip(data, streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+                eager.append(step(*d))
+        torch.cuda.synchronize()
+        for o, e, want_d in zip(outs, eager, want):
+            assert all(torch.equal(x, z) and torch.equal(y, z) for x, y, z in zip(o, e, want_d))
+
+
+def test_example_with_a_block_and_rewards():
+    """Runs, with finite losses and gradients; the streams still agree with the whole utterances."""
+    from paper_2609_33645_amd import fit_and_decode
+    say("example")
+    r = fit_and_decode.run(steps=12, beams=4, classes=60, N=3, block=72, policy=3)
+    for k in ("loss_first", "loss_last", "norm_max", "reward_first", "reward_last", "policy_norm_max"):
+        assert math.isfinite(r[k]), k
+    assert r["norm_max"] > 0 and r["policy_norm_max"] > 0
+    assert r["streams equal"] and r["predictor off by"] < 1e-3
