@@ -111,17 +111,17 @@ embedding_kernel(const void* __restrict__ table, int V, int D, const void* __res
                  int lanes, void* __restrict__ y) {
   constexpr int kPer = BF ? 8 : 4, kBytes = BF ? 2 : 4;
   const int rows = kThreads / lanes, sub = threadIdx.x / lanes, at = threadIdx.x % lanes;
-  const int64_t m = static_cast<int64_t>(blockIdx.x) * rows + sub;
-  if (m >= N) return;
-  const int c = class_of<I64>(tokens, m, V);
-  const char* src = static_cast<const char*>(table) + static_cast<int64_t>(c) * D * kBytes;
-  char* dst = static_cast<char*>(y) + m * D * kBytes;
-  for (int d = at * kPer; d < D; d += lanes * kPer) {
-    float v[kPer];
-    load_vals<BF>(src + static_cast<int64_t>(d) * kBytes, c < V ? D - d : 0, v);
+  for (int64_t m = static_cast<int64_t>(blockIdx.x) * rows + sub; m < N; m += static_cast<int64_t>(gridDim.x) * rows) {
+    const int c = class_of<I64>(tokens, m, V);
+    const char* src = static_cast<const char*>(table) + static_cast<int64_t>(c) * D * kBytes;
+    char* dst = static_cast<char*>(y) + m * D * kBytes;
+    for (int d = at * kPer; d < D; d += lanes * kPer) {
+      float v[kPer];
+      load_vals<BF>(src + static_cast<int64_t>(d) * kBytes, c < V ? D - d : 0, v);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) v[e] *= scale;
-    store_vals<BF>(dst + static_cast<int64_t>(d) * kBytes, D - d, v);
+      for (int e = 0; e < kPer; ++e) v[e] *= scale;
+      store_vals<BF>(dst + static_cast<int64_t>(d) * kBytes, D - d, v);
+    }
   }
 }
 
@@ -375,43 +375,46 @@ embedding_sum(SumArgs A) {
 template <bool OBF>
 __global__ void __launch_bounds__(kThreads)
 embedding_join(SumArgs A) {
-  const int r = blockIdx.x;
-  const int b = r * A.range, e = b + A.range;
-  const int c = A.keys[e - 1];  // (r is not the last range)
-  if (c >= A.V || A.keys[e] != c || (b > 0 && A.keys[b - 1] == c && A.keys[b] == c)) return;
-  // the last range with the class: the first place past it by bisection (keys rise)
-  int lo = e, hi = A.N;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (A.keys[mid] <= c) lo = mid + 1;
-    else hi = mid;
-  }
-  const int last = (lo - 1) / A.range;
   constexpr int kRuns = kThreads / 32;
   __shared__ float part[kRuns][32][kVals];
   const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
   const int d = (blockIdx.y * 32 + lane) * kVals;
-  const int per = (last - r + 1 + kRuns - 1) / kRuns;
-  float s[kVals] = {};
-  if (d < A.D) {
-    const int qb = r + run * per, qe = min(last + 1, qb + per);
-#pragma unroll 4
-    for (int q = qb; q < qe; ++q) {  // its first part is the second of range r, then the first of each
-      float x[kVals];
-      load_vals<false>(A.part + (static_cast<int64_t>(q) * 2 + (q == r)) * A.D + d, A.D - d, x);
-#pragma unroll
-      for (int k = 0; k < kVals; ++k) s[k] += x[k];
+  for (int r = blockIdx.x; r < A.ranges - 1; r += gridDim.x) {  // (the same for the whole workgroup)
+    const int b = r * A.range, e = b + A.range;
+    const int c = A.keys[e - 1];
+    if (c >= A.V || A.keys[e] != c || (b > 0 && A.keys[b - 1] == c && A.keys[b] == c)) continue;
+    // the last range with the class: the first place past it by bisection (keys rise)
+    int lo = e, hi = A.N;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (A.keys[mid] <= c) lo = mid + 1;
+      else hi = mid;
     }
+    const int last = (lo - 1) / A.range;
+    const int per = (last - r + 1 + kRuns - 1) / kRuns;
+    float s[kVals] = {};
+    if (d < A.D) {
+      const int qb = r + run * per, qe = min(last + 1, qb + per);
+#pragma unroll 4
+      for (int q = qb; q < qe; ++q) {  // its first part is the second of range r, then the first of each
+        float x[kVals];
+        load_vals<false>(A.part + (static_cast<int64_t>(q) * 2 + (q == r)) * A.D + d, A.D - d, x);
+#pragma unroll
+        for (int k = 0; k < kVals; ++k) s[k] += x[k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kVals; ++k) part[run][lane][k] = s[k];
+    __syncthreads();
+    if (run == 0 && d < A.D) {
+#pragma unroll
+      for (int g = 1; g < kRuns; ++g)
+#pragma unroll
+        for (int k = 0; k < kVals; ++k) s[k] += part[g][lane][k];
+      put_row<OBF>(A, c, d, s);
+    }
+    __syncthreads();  // before the next range's sums
   }
-#pragma unroll
-  for (int k = 0; k < kVals; ++k) part[run][lane][k] = s[k];
-  __syncthreads();
-  if (run > 0 || d >= A.D) return;
-#pragma unroll
-  for (int g = 1; g < kRuns; ++g)
-#pragma unroll
-    for (int k = 0; k < kVals; ++k) s[k] += part[g][lane][k];
-  put_row<OBF>(A, c, d, s);
 }
 
 __global__ void __launch_bounds__(kThreads) fill_zero(void* p, int64_t bytes) {
@@ -423,13 +426,17 @@ unsigned clear_blocks(int64_t bytes, int threads) {
   return static_cast<unsigned>(std::min<int64_t>((bytes + threads * 16 - 1) / (threads * 16), (int64_t{1} << 31) / threads));
 }
 
-// Places of a range: as short as keeps its partial rows few beside the rows it reads.
-int range_of(int N) { return N >= 16384 ? 32 : N >= 1024 ? 16 : 8; }
-
 int lanes_for(int pieces) {
   int l = 1;
   while (l < pieces && l < kThreads) l <<= 1;
   return l;
+}
+
+// Places of a range: as short as keeps its partial rows few beside the rows it reads; short where a row has
+// few lanes, and ranges alone fill the chip.
+int range_of(int N, int D) {
+  if (lanes_for((D + kVals - 1) / kVals) < 32) return 8;
+  return N >= 16384 ? 32 : N >= 1024 ? 16 : 8;
 }
 
 struct Layout {
@@ -444,7 +451,7 @@ Layout layout(int N, int D) {
   L.o_perm2 = 3 * n;
   L.o_hist = N > kRankTokens ? 4 * n : 2 * n;
   L.o_part = L.o_hist + (N > kRankTokens ? static_cast<size_t>(kMaxTiles) * kMaxBins * 4 : 0);
-  const int range = range_of(N);
+  const int range = range_of(N, D);
   const size_t ranges = static_cast<size_t>((static_cast<int64_t>(N) + range - 1) / range);
   L.total = L.o_part + align_up((ranges > 1 ? ranges : 0) * 2 * D * sizeof(float), 256);
   return L;
@@ -463,7 +470,7 @@ hipError_t launch_embedding(int dtype, const void* table, int V, int D, const vo
                             float scale, void* y, hipStream_t stream) {
   const int per = dtype == 1 ? 8 : 4;
   const int lanes = lanes_for((D + per - 1) / per), rows = kThreads / lanes;
-  const dim3 grid(static_cast<unsigned>((N + rows - 1) / rows));
+  const dim3 grid(static_cast<unsigned>(std::min((N + rows - 1) / rows, kMaxGrid)));
   Prof pr("embedding", stream);
 #define PCTC_EMBED(BF, I64)                                                                                      \
   hipLaunchKernelGGL((embedding_kernel<BF, I64>), grid, dim3(kThreads), 0, stream, table, V, D, tokens, N, scale, \
@@ -549,7 +556,7 @@ hipError_t launch_embedding_backward(int dtype, const void* dy, const void* toke
   A.N = N;
   A.V = V;
   A.D = D;
-  A.range = range_of(N);
+  A.range = range_of(N, D);
   A.ranges = (N + A.range - 1) / A.range;
   A.lanes = lanes_for((D + kVals - 1) / kVals);
   A.scale = scale;
@@ -570,7 +577,7 @@ hipError_t launch_embedding_backward(int dtype, const void* dy, const void* toke
   }
   if (A.ranges > 1) {
     Prof pr("embedding_join", stream);
-    const dim3 joins(A.ranges - 1, (D + 32 * kVals - 1) / (32 * kVals));
+    const dim3 joins(std::min(A.ranges - 1, 1 << 18), (D + 32 * kVals - 1) / (32 * kVals));
     if (out_dtype == 1) hipLaunchKernelGGL(embedding_join<true>, joins, dim3(kThreads), 0, stream, A);
     else hipLaunchKernelGGL(embedding_join<false>, joins, dim3(kThreads), 0, stream, A);
   }

@@ -1028,8 +1028,8 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
 def _out(out: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.Tensor, what: str = "out") -> torch.Tensor:
     """A new tensor, or the caller's, which must be one of that shape (on the device of `like`)."""
     dev = like.device
-    if out is None:
-        return like.new_empty(shape, dtype=dtype)  # (half the time of torch.empty with a device)
+    if out is None:  # (half the time of torch.empty with a device)
+        return torch.empty_like(like) if shape == like.shape and dtype is like.dtype else like.new_empty(shape, dtype=dtype)
     if out.dtype is not dtype or tuple(out.shape) != tuple(shape) or out.device != dev or not out.is_contiguous():
         raise PrunedCTCError(-1, f"{what} must be contiguous {dtype} {tuple(shape)} on {dev}")
     return out

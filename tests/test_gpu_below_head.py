@@ -528,6 +528,59 @@ def test_gated_ffn(dtype, M, D, F_, O, act):
     assert all(torch.equal(dw[k], grads[k]) for k in ("dw_gate", "dw_up", "dw_down"))
 
 
+def test_gated_ffn_without_rows_and_of_shapes():
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("gated_ffn shapes")
+    x, w, wd = torch.randn(6, 16, device="cuda"), torch.randn(24, 16, device="cuda"), torch.randn(8, 24, device="cuda")
+    r = pc.gated_ffn(x[:0], w, w, wd, keep=True)
+    assert r["y"].shape == (0, 8) and r["gate"].shape == (0, 24)
+    g = pc.gated_ffn_backward(r["y"], x[:0], r["gate"], r["up"], w, w, wd)
+    assert g["dx"].shape == (0, 16) and not any(g[k].any() for k in ("dw_gate", "dw_up", "dw_down"))
+    whole = pc.gated_ffn(x, w, w, wd, keep=True)
+    shaped = pc.gated_ffn(x.view(2, 3, 16), w, w, wd, keep=True)
+    assert shaped["y"].shape == (2, 3, 8) and torch.equal(shaped["y"].view(6, 8), whole["y"])
+    assert torch.equal(shaped["gate"].view(6, 24), whole["gate"])
+    out = torch.full((6, 8), 7.0, device="cuda")
+    assert pc.gated_ffn(x.T.contiguous().T, w, w.T.contiguous().T, wd, out=out)["y"] is out and torch.equal(out, whole["y"])
+    for bad in (lambda: pc.gated_ffn(x[:, :15], w[:, :15], w[:, :15], wd), lambda: pc.gated_ffn(x, w, w[:16], wd),
+                lambda: pc.gated_ffn(x, w, w, wd.bfloat16()), lambda: pc.gated_ffn(x, w, w, wd, out=x),
+                lambda: pc.gated_ffn_backward(x, x, whole["gate"], whole["up"], w, w, wd)):
+        with pytest.raises(pc.PrunedCTCError):
+            bad()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [5, 300])
+def test_gated_ffn_rows_do_not_meet(dtype, M):
+    """Infinities and NaN in one row of x stay in that row; values that drive the activation to its ends."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("gated_ffn nonfinite", dtype, M)
+    c = ffn_case(9, M, 64, 136, 72, dtype)
+    for act in ("silu", "gelu"):
+        want = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act)["y"]
+        x = c["x"].clone()
+        x[1], x[3] = math.nan, math.inf
+        got = pc.gated_ffn(x, c["wg"], c["wu"], c["wd"], act)["y"]
+        assert torch.isnan(got[1]).all() and not torch.isfinite(got[3]).all()
+        rest = [i for i in range(M) if i not in (1, 3)]
+        # (float tiles with such values are taken on other instructions)
+        assert torch.equal(got[rest], want[rest]) if dtype == "bf16" else torch.allclose(got[rest], want[rest], rtol=1e-5, atol=1e-5)
+        # act(-1e4) is zero, act(1e4) its argument
+        big = torch.full_like(c["x"][:2], 0.0)
+        big[0, 0], big[1, 0] = 1e4, -1e4
+        g = torch.zeros_like(c["wg"])
+        g[:, 0] = 1
+        u = torch.zeros_like(g)
+        u[:, 0] = 1e-4
+        r = pc.gated_ffn(big, g, u, torch.eye(136, device="cuda", dtype=x.dtype)[:72].contiguous(), act, keep=True)
+        assert torch.allclose(r["y"][0].float(), torch.tensor(1e4, device="cuda"), rtol=2e-2) and not r["y"][1].any()
+        d = pc.gated_ffn_backward(torch.ones_like(r["y"]), big, r["gate"], r["up"], g, u,
+                                  torch.eye(136, device="cuda", dtype=x.dtype)[:72].contiguous(), act)
+        assert all(torch.isfinite(v.float()).all() for v in d.values())
+
+
 # ---- together ------------------------------------------------------------------------------
 
 def test_layers_in_autograd_against_the_formulas():
