@@ -228,11 +228,11 @@ __device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* co
 
 // ---- few rows ------------------------------------------------------------------------------
 
-// The projections (MATS 2: the same rows of w0 and w1, then h = act(a) b) or a plain product (MATS 1) for up to
-// 16 NT rows of x.  A workgroup takes 16 rows of the weights, its wavefronts a share of k each, and adds the
-// shares up in order through LDS.  Weights and rows go from memory to the matrix instructions' registers
+// The projections (MATS 2: the same rows of w0 and w1, then h = act(a) b) or a plain product (MATS 1) for few
+// rows of x.  A workgroup takes 16 RB rows of the weights and 16 NT of x, its wavefronts a share of k each, and
+// adds the shares up in order through LDS.  Weights and rows go from memory to the matrix instructions' registers
 // (16 x 16, 16 bytes a lane: 64 bytes of each of 16 rows an instruction) without LDS: every weight is used by
-// one wavefront only, and what bounds the kernel is reading the weights.  Rows past R or M repeat the
+// one wavefront only, and what bounds the kernel is reading the weights (from 32 rows on, those and x from the caches).  Rows past R or M repeat the
 // last one; what they give is not written.
 template <class E>
 struct FewArgs {
@@ -254,36 +254,45 @@ __device__ __forceinline__ void few_step(const u32x4& w, const u32x4& x, f32x4& 
   }
 }
 
-template <class E, int MATS, int NT, int WAVES, int ACT>
-__global__ void __launch_bounds__(WAVES * 64) ffn_few(FewArgs<E> P) {
+template <class E, int MATS, int RB, int NT, int KS, int ACT>
+__global__ void __launch_bounds__(KS * 64) ffn_few(FewArgs<E> P) {
   using T = typename E::T;
   constexpr int kPer = E::kBf ? 8 : 4, kStep = 4 * kPer;  // values of a lane, k of a step
-  constexpr int U = NT >= 4 ? 2 : 4;                      // steps read ahead
-  __shared__ f32x4 sum[WAVES][MATS * NT][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
-  const int row = min(r0 + (lane & 15), P.R - 1), ko = (lane >> 4) * kPer;
-  const T* w[MATS];
-  w[0] = P.w0 + static_cast<int64_t>(row) * P.K + ko;
-  if constexpr (MATS == 2) w[1] = P.w1 + static_cast<int64_t>(row) * P.K + ko;
+  constexpr int U = MATS * RB + NT >= 6 ? 2 : 4;          // steps read ahead
+  constexpr int NA = MATS * RB * NT;                      // accumulators
+  __shared__ f32x4 sum[KS][NA][64];
+  const int lane = threadIdx.x & 63, ks = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = blockIdx.x * 16 * RB, m0 = blockIdx.y * 16 * NT;
+  const int ko = (lane >> 4) * kPer;
+  const T* w[MATS][RB];
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int64_t at = static_cast<int64_t>(min(r0 + 16 * b + (lane & 15), P.R - 1)) * P.K + ko;
+    w[0][b] = P.w0 + at;
+    if constexpr (MATS == 2) w[1][b] = P.w1 + at;
+  }
   const T* x[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) x[n] = P.x + static_cast<int64_t>(min(m0 + 16 * n + (lane & 15), P.M - 1)) * P.K + ko;
-  f32x4 acc[MATS][NT];
+  f32x4 acc[MATS][RB][NT];
 #pragma unroll
   for (int q = 0; q < MATS; ++q)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[q][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int share = (P.K + WAVES * kStep - 1) / (WAVES * kStep) * kStep;
-  const int kb = min(P.K, wave * share), ke = min(P.K, kb + share);
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) acc[q][b][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int share = (P.K + KS * kStep - 1) / (KS * kStep) * kStep;
+  const int kb = min(P.K, ks * share), ke = min(P.K, kb + share);
   auto piece = [](const T* p) { return *reinterpret_cast<const u32x4*>(p); };
   int k = kb;
-  u32x4 wv[2][MATS][U], xv[2][NT][U];
+  u32x4 wv[2][MATS][RB][U], xv[2][NT][U];
   auto read = [&](int s, int at) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
-      for (int q = 0; q < MATS; ++q) wv[s][q][u] = piece(w[q] + at + u * kStep);
+      for (int q = 0; q < MATS; ++q)
+#pragma unroll
+        for (int b = 0; b < RB; ++b) wv[s][q][b][u] = piece(w[q][b] + at + u * kStep);
 #pragma unroll
       for (int n = 0; n < NT; ++n) xv[s][n][u] = piece(x[n] + at + u * kStep);
     }
@@ -294,7 +303,9 @@ __global__ void __launch_bounds__(WAVES * 64) ffn_few(FewArgs<E> P) {
 #pragma unroll
       for (int q = 0; q < MATS; ++q)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) few_step<E>(wv[s][q][u], xv[s][n][u], acc[q][n]);
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) few_step<E>(wv[s][q][b][u], xv[s][n][u], acc[q][b][n]);
   };
   constexpr int kBlock = U * kStep;
   const int blocks = (ke - kb) / kBlock;
@@ -325,27 +336,31 @@ __global__ void __launch_bounds__(WAVES * 64) ffn_few(FewArgs<E> P) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) xt[n] = in ? piece(x[n] + k) : zero;
 #pragma unroll
-    for (int q = 0; q < MATS; ++q) {
-      const u32x4 wt = in ? piece(w[q] + k) : zero;
+    for (int q = 0; q < MATS; ++q)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) few_step<E>(wt, xt[n], acc[q][n]);
-    }
+      for (int b = 0; b < RB; ++b) {
+        const u32x4 wt = in ? piece(w[q][b] + k) : zero;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) few_step<E>(wt, xt[n], acc[q][b][n]);
+      }
   }
 #pragma unroll
   for (int q = 0; q < MATS; ++q)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) sum[wave][q * NT + n][lane] = acc[q][n];
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) sum[ks][(q * RB + b) * NT + n][lane] = acc[q][b][n];
   __syncthreads();
-  for (int i = threadIdx.x; i < NT * 64; i += WAVES * 64) {
-    const int n = i >> 6, l = i & 63;
-    const int m = m0 + 16 * n + (l & 15), r = r0 + 4 * (l >> 4);
+  for (int i = threadIdx.x; i < RB * NT * 64; i += KS * 64) {
+    const int l = i & 63, n = (i >> 6) % NT, b = (i >> 6) / NT;
+    const int m = m0 + 16 * n + (l & 15), r = r0 + 16 * b + 4 * (l >> 4);
     if (m >= P.M || r >= P.R) continue;
     float v[MATS][4] = {};
 #pragma unroll
-    for (int g = 0; g < WAVES; ++g)
+    for (int g = 0; g < KS; ++g)
 #pragma unroll
       for (int q = 0; q < MATS; ++q) {
-        const f32x4 s = sum[g][q * NT + n][l];
+        const f32x4 s = sum[g][(q * RB + b) * NT + n][l];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[q][e] += s[e];
       }
@@ -365,20 +380,38 @@ __global__ void __launch_bounds__(WAVES * 64) ffn_few(FewArgs<E> P) {
   }
 }
 
-// Rows of x a workgroup takes: all of them while that leaves workgroups for every compute unit twice; else
-// fewer, and the weights are read again from the caches.
+// How a launch is cut: 16 RB rows of the weights and 16 NT rows of x a workgroup, KS shares of k.  Rows of x are
+// read by every workgroup of other weights and weights by every one of other rows, from the caches; the least of
+// that which leaves a workgroup for every compute unit is best from 32 rows on (the most workgroups where none
+// does), and up to 16 rows, which memory bounds, 16 rows of weights.  The block of 1,024 x 4,096 in bf16, 128
+// rows: 31 us by the most workgroups, 24 so.
 template <class E, int MATS, int ACT>
 void launch_few(const FewArgs<E>& P, hipStream_t stream) {
-  const int nr = (P.R + 15) / 16;
-  int nt = P.M <= 16 ? 1 : P.M <= 32 ? 2 : P.M <= 64 ? 4 : 8;
-  while (nt > 1 && nr * ((P.M + 16 * nt - 1) / (16 * nt)) < 512) nt /= 2;
-  const dim3 grid(nr, (P.M + 16 * nt - 1) / (16 * nt));
-#define PCTC_FEW(NT, WAVES) \
-  hipLaunchKernelGGL((ffn_few<E, MATS, NT, WAVES, ACT>), grid, dim3(WAVES * 64), 0, stream, P)
-  if (nt == 1) PCTC_FEW(1, 8);
-  else if (nt == 2) PCTC_FEW(2, 8);
-  else if (nt == 4) PCTC_FEW(4, 8);
-  else PCTC_FEW(8, 4);
+  static const int cuts[5][2] = {{1, 1}, {1, 2}, {2, 2}, {1, 4}, {2, 4}};
+  int best = 0;
+  int64_t least = -1;
+  for (int c = 0; c < 5 && P.M > 16; ++c) {
+    const int rb = cuts[c][0], nt = cuts[c][1];
+    const int64_t nr = (P.R + 16 * rb - 1) / (16 * rb), nm = (P.M + 16 * nt - 1) / (16 * nt);
+    if (c > 0 && (nr * nm < 256 || 16 * (nt / 2) >= P.M)) continue;
+    const int64_t read = nr * P.M + nm * P.R * MATS;  // times K
+    if (least < 0 || read < least) {
+      least = read;
+      best = c;
+    }
+  }
+#define PCTC_FEW(C, RB, NT, KS)                                                                                     \
+  case C:                                                                                                           \
+    hipLaunchKernelGGL((ffn_few<E, MATS, RB, NT, KS, ACT>), dim3((P.R + 16 * RB - 1) / (16 * RB),                   \
+                       (P.M + 16 * NT - 1) / (16 * NT)), dim3(KS * 64), 0, stream, P);                              \
+    break
+  switch (best) {
+    PCTC_FEW(0, 1, 1, 8);
+    PCTC_FEW(1, 1, 2, 8);
+    PCTC_FEW(2, 2, 2, 8);
+    PCTC_FEW(3, 1, 4, 8);
+    PCTC_FEW(4, 2, 4, 4);
+  }
 #undef PCTC_FEW
 }
 
@@ -714,11 +747,11 @@ Products down_products(const FfnArgs& q, const void* h, bool bf) {
 }
 
 // How the projections are formed.  The times are those of plan()'s model, and for few rows what was measured:
-// the weights at 5.3 TB/s and as much again for every 40 rows (32 in float; bf16, 4,096 x 10,240, the whole
+// the weights at 5.3 TB/s and as much again for every 44 rows (36 in float; bf16, 4,096 x 10,240, the whole
 // block: 1 row 52 us, 16 rows 68, 64 130, 128 210).
 enum class Pair { kFew, kTiles, kSliced };
 double few_us(const FfnArgs& q, bool bf, double weights) {
-  return 6 + weights * (bf ? 2 : 4) / 5.3e6 * (1 + q.M / (bf ? 40.0 : 32.0));
+  return 6 + weights * (bf ? 2 : 4) / 5.3e6 * (1 + q.M / (bf ? 44.0 : 36.0));
 }
 double tiles_us(int count, int K, bool bf) { return (count + 255) / 256 * (K * step_us(bf) + (bf ? 10 : 25)); }
 Pair pair_plan(const FfnArgs& q, bool bf, Products& Q) {
