@@ -754,13 +754,23 @@ double few_us(const FfnArgs& q, bool bf, double weights) {
   return 6 + weights * (bf ? 2 : 4) / 5.3e6 * (1 + q.M / (bf ? 44.0 : 36.0));
 }
 double tiles_us(int count, int K, bool bf) { return (count + 255) / 256 * (K * step_us(bf) + (bf ? 10 : 25)); }
+// The rows past the last whole tile go without tiles where that saves a round of the chip (M = 4,215, 512 x 2,048,
+// float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
+int rows_apart(const FfnArgs& q) {
+  const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
+  const bool apart = rest > 0 && rest <= kT / 2 && q.M > kT && (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256;
+  return apart ? rest : 0;
+}
 Pair pair_plan(const FfnArgs& q, bool bf, Products& Q) {
   Q = Products{};
   Q.n = 2;
   Q.p[0] = product(q.wg, q.D, q.x, q.D, false, q.F, q.M, q.D, nullptr);
   Q.p[1] = product(q.wu, q.D, q.x, q.D, false, q.F, q.M, q.D, nullptr);
-  const double sliced = plan(Q, bf, true), whole = tiles_us(tiles(q.M) * tiles(q.F, kT / 2), q.D, bf);
-  if (q.M <= kFew && few_us(q, bf, 2.0 * q.D * q.F) <= std::min(sliced, whole)) return Pair::kFew;
+  const double weights = 2.0 * q.D * q.F, sliced = plan(Q, bf, true);
+  FfnArgs last = q;
+  last.M = rows_apart(q);
+  const double whole = tiles_us(tiles(q.M - last.M) * tiles(q.F, kT / 2), q.D, bf) + (last.M ? few_us(last, bf, weights) : 0);
+  if (q.M <= kFew && few_us(q, bf, weights) <= std::min(sliced, whole)) return Pair::kFew;
   return sliced < whole ? Pair::kSliced : Pair::kTiles;
 }
 bool down_by_few(const FfnArgs& q, bool bf) {
@@ -820,12 +830,8 @@ hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
     if (silu) hipLaunchKernelGGL((join_pair<E, kSilu>), grid, dim3(256), 0, stream, Q, hh, a, b);
     else hipLaunchKernelGGL((join_pair<E, kGelu>), grid, dim3(256), 0, stream, Q, hh, a, b);
   } else {
-    // The rows past the last whole tile go without tiles where that saves a round of the chip (M = 4,215, 512 x
-    // 2,048, float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
-    const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
-    const bool apart = rest > 0 && rest <= kT / 2 && (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256;
-    const int m = apart ? q.M - rest : q.M;
-    if (apart) few(m, rest);
+    const int rest = rows_apart(q), m = q.M - rest, nF = tiles(q.F, kT / 2);
+    if (rest > 0) few(m, rest);
     const PairArgs<E> p{x, wg, wu, hh, a, b, m, q.D, q.F};
     Prof pr("ffn_pair", stream);
     const dim3 grid(grouped_grid(tiles(m), nF));
