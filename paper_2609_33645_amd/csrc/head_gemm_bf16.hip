@@ -66,6 +66,14 @@ constexpr int kRcStores = 16;  // buffer stores per wave per 256 x 256 tile (rec
 using GUh = bf::Gemm<256, 128, 32, LL::KC, LL::MC, 3, 2, 2>;
 using GDw = bf::Gemm<kBR, kBC, kBK, LL::MC, LL::MC, 4, 2, 4, true>;
 
+// Launches with the kernels' DM: whether the number of rows comes from the device (the calls that know it ask
+// nothing of memory and skip no workgroup).
+template <class F>
+void rows_from(const int32_t* Mdev, F launch) {
+  if (Mdev) launch(std::true_type{});
+  else launch(std::false_type{});
+}
+
 }  // namespace
 
 #define PCTC_STAGES_G(G)                                                                  \
@@ -76,19 +84,19 @@ using GDw = bf::Gemm<kBR, kBC, kBK, LL::MC, LL::MC, 4, 2, 4, true>;
   char* const stx_[4] = {st0_, st1_, st2_, st3_};                                           \
   char* const(&st)[G::kNS] = *reinterpret_cast<char* const(*)[G::kNS]>(&stx_);
 
-template <class G, bool BIAS, int OCC>
+template <class G, bool BIAS, int OCC, bool DM = false>
 __global__ void __launch_bounds__(G::kThreads, OCC)
 lse_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __restrict__ W, const float* __restrict__ bias,
                  int V, int P, int vper, float2* __restrict__ partials, const int32_t* __restrict__ Mdev) {
   extern __shared__ float bsh[];  // BIAS: b over this partition's rows (vper, padded to whole tiles)
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   PCTC_STAGES_G(G)
-  if (Mdev) M = min(M, *Mdev);
+  if constexpr (DM) M = min(M, *Mdev);
   const int nMt = (M + TC - 1) / TC;
   // every frame tile of a vocabulary run on one XCD at about the same time: the run's W rows
   // are fetched once and shared through that XCD's L2
-  const int works = Mdev ? nMt * P : gridDim.x;
-  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int works = DM ? nMt * P : gridDim.x;
+  if (DM && static_cast<int>(blockIdx.x) >= works) return;
   const int w = xcd_swz(blockIdx.x, works);
   const int mt = w % nMt;
   const int p = w / nMt;
@@ -174,7 +182,7 @@ __device__ __forceinline__ void lse_e_update(const f32x16 (&a)[FR][FC], int j, f
 // sets it.
 // HT: the frames come from Ht [D][Mp] (the transposed head input) instead of H [M][D].
 // BIAS (HT, no E partitions): the accumulators start at b, which lies where E would be staged.
-template <bool HT, bool BIAS = false>
+template <bool HT, bool BIAS = false, bool DM = false>
 __global__ void __launch_bounds__(512, 1)
 lse_partial_e_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ Ht, int Mp, int M, int D,
                    const uint16_t* __restrict__ W, const float* __restrict__ bias, int V, int P, int vper,
@@ -185,10 +193,10 @@ lse_partial_e_bf16(const uint16_t* __restrict__ H, const uint16_t* __restrict__ 
   static_assert(FR == 4 && FC == 2 && G::NW == 8 && TR == 256, "waves of 128 vocabulary rows x 64 frames");
   PCTC_STAGES_G(G)
   __shared__ __attribute__((aligned(1024))) char stg_[G::NW * 4096];
-  if (Mdev) M = min(M, *Mdev);
+  if constexpr (DM) M = min(M, *Mdev);
   const int nMt = (M + TC - 1) / TC;
-  const int works = Mdev ? nMt * P : gridDim.x;
-  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int works = DM ? nMt * P : gridDim.x;
+  if (DM && static_cast<int>(blockIdx.x) >= works) return;
   const int w = xcd_swz(blockIdx.x, works);
   const int mt = w % nMt;
   const int p = w / nMt;
@@ -435,7 +443,7 @@ gather_s_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __re
 // 16-byte vectors.  DB: the staged (rounded) values are also summed
 // over the tile's frames, giving this tile's share of db = dZ^T 1 in
 // dbpart[frame tile][column].
-template <class GG, bool BIAS, bool DB, int OCC>
+template <class GG, bool BIAS, bool DB, int OCC, bool DM = false>
 __global__ void __launch_bounds__(GG::kThreads, OCC)
 recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t* __restrict__ W,
                   const float* __restrict__ bias, int c0, int cw, const float2* __restrict__ lam2,
@@ -451,11 +459,11 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
   constexpr int kGps = GG::kStageBytes / (32 * kPitch);
   static_assert(kGps >= 1 && (WC + kGps - 1) / kGps <= GG::kNS, "staging fits the stages");
   PCTC_STAGES_G(GG)
-  if (Mdev) M = min(M, *Mdev);
+  if constexpr (DM) M = min(M, *Mdev);
   const int nMt = (M + TC - 1) / TC;
   const int nVt = (cw + TR - 1) / TR;
-  const int works = !Mdev ? gridDim.x : nMt > 0 ? grouped_grid(nMt, nVt) : 0;
-  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int works = !DM ? gridDim.x : nMt > 0 ? grouped_grid(nMt, nVt) : 0;
+  if (DM && static_cast<int>(blockIdx.x) >= works) return;
   int mt, vt;
   if (!grouped_tile(xcd_swz(blockIdx.x, works), nMt, nVt, mt, vt)) return;
   const int m0 = mt * TC;
@@ -588,7 +596,7 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
 // count them and leave them in flight under the next tile's first products.
 
 // HT: the frames come from Hst [D][Mp] (Hs transposed) instead of Hs [M][D].
-template <bool HT>
+template <bool HT, bool DM = false>
 __global__ void __launch_bounds__(512, 1)
 recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__ Hst, int Mp, int M, int D,
                    const uint16_t* __restrict__ W, int c0, int cw, int run, const float2* __restrict__ lam2,
@@ -596,7 +604,7 @@ recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__
                    const int32_t* __restrict__ only_if, const int32_t* __restrict__ Mdev) {
   // only_if (the normaliser's E check flag): recompute only when its E cannot be used
   if (only_if && *only_if == 0) return;
-  if (Mdev) M = min(M, *Mdev);
+  if constexpr (DM) M = min(M, *Mdev);
   using G = std::conditional_t<HT, GMidT, GMid>;
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   static_assert(FR == 4 && FC == 2 && G::NW == 8 && TR == 256, "waves of 128 vocabulary rows x 64 frames");
@@ -605,8 +613,8 @@ recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__
   const int nMt = (M + TC - 1) / TC;
   const int nVt = (cw + TR - 1) / TR;
   // all frame tiles of a vocabulary run consecutive on one XCD (it fetches the run's W rows once)
-  const int works = Mdev ? nMt * ((nVt + run - 1) / run) : gridDim.x;
-  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int works = DM ? nMt * ((nVt + run - 1) / run) : gridDim.x;
+  if (DM && static_cast<int>(blockIdx.x) >= works) return;
   const int w = xcd_swz(blockIdx.x, works);
   const int mt = w % nMt;
   const int vt0 = (w / nMt) * run;
@@ -716,12 +724,12 @@ static int dh_xcd_rows(int M, int D) {
   return best;
 }
 
-template <class G, int OCC>
+template <class G, int OCC, bool DM = false>
 __global__ void __launch_bounds__(G::kThreads, OCC)
 dh_gemm_bf16(const uint16_t* __restrict__ dZ, int M, int chunk, const uint16_t* __restrict__ W, int D, int c0, int cw,
              int slice, float* __restrict__ part, int gm, int accumulate, const int32_t* __restrict__ kdev,
              const float* __restrict__ rowscale, const int32_t* __restrict__ Mdev) {
-  if (Mdev) M = min(M, *Mdev);
+  if constexpr (DM) M = min(M, *Mdev);
   // the first chunk writes its slices; later chunks (and an accumulating call) add to them
   const bool first = c0 == 0 && !accumulate;
   if (kdev) cw = min(cw, 2 * *kdev);  // union columns: [hi | lo] of the K classes the device found
@@ -730,8 +738,8 @@ dh_gemm_bf16(const uint16_t* __restrict__ dZ, int M, int chunk, const uint16_t* 
   const int nDt = (D + TC - 1) / TC;
   // Each XCD (a contiguous run of work ids) takes one block of a gm x (8 / gm) partition of
   // the frame x d tile grid: it reads dZ rows of its frame block and W columns of its d block
-  const int works = Mdev ? nMt * nDt * ((cw + slice - 1) / slice) : gridDim.x;
-  if (static_cast<int>(blockIdx.x) >= works) return;
+  const int works = DM ? nMt * nDt * ((cw + slice - 1) / slice) : gridDim.x;
+  if (DM && static_cast<int>(blockIdx.x) >= works) return;
   const int work = xcd_swz(blockIdx.x, works);
   const int s = work / (nMt * nDt);
   int mt, dt;
@@ -797,11 +805,11 @@ struct DwOp {
 
 // dW products of up to two operand sets in one launch: work ids below tiles0 take P0's output
 // tiles, the rest P1's (the union columns' dW_u in the last chunk's launch).  O16: `out` holds bf16.
-template <bool O16>
+template <bool O16, bool DM = false>
 __global__ void __launch_bounds__(512, 1)
 dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int M, int D,
              const int32_t* __restrict__ Mdev) {
-  if (Mdev) M = min(M, *Mdev);  // (with none, zeros are written)
+  if constexpr (DM) M = min(M, *Mdev);  // (with none, zeros are written)
   using G = GDw;
   constexpr int FR = G::FR, FC = G::FC;
   PCTC_STAGES_G(G)
@@ -819,7 +827,7 @@ dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int 
   const int mb = z * P.mslice;
   const int mlen = min(M - mb, P.mslice);
   if (P.kdev) cw = min(cw, 2 * *P.kdev);
-  if (z >= P.nz || (mlen <= 0 && !Mdev) || v0 >= cw) return;
+  if (z >= P.nz || (mlen <= 0 && !DM) || v0 >= cw) return;
   float* const dW = P.out + static_cast<int64_t>(z) * P.zstride;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // A: Z viewed as rows v (columns of Z), k = frame; B: Hs viewed as rows d, k = frame
@@ -1242,13 +1250,15 @@ hipError_t launch_lse_partial_bf16(const uint16_t* H, int M, int D, const uint16
   // every head on the 32-deep four-stage tiles (for wide heads each vocabulary tile is its own
   // partition; the 64-deep two-stage tiles measured 4% slower there)
   const dim3 grid(sp.nM * Peff);
-  if (bias) {
-    hipLaunchKernelGGL((lse_partial_bf16<GMid, true, 1>), grid, dim3(GMid::kThreads), bsh, stream, H, M, D, W, bias,
-                       V, Peff, vper, partials, Mdev);
-  } else {
-    hipLaunchKernelGGL((lse_partial_bf16<GMid, false, 1>), grid, dim3(GMid::kThreads), 0, stream, H, M, D, W, bias,
-                       V, Peff, vper, partials, Mdev);
-  }
+  rows_from(Mdev, [&](auto dm) {
+    if (bias) {
+      hipLaunchKernelGGL((lse_partial_bf16<GMid, true, 1, dm>), grid, dim3(GMid::kThreads), bsh, stream, H, M, D, W,
+                         bias, V, Peff, vper, partials, Mdev);
+    } else {
+      hipLaunchKernelGGL((lse_partial_bf16<GMid, false, 1, dm>), grid, dim3(GMid::kThreads), 0, stream, H, M, D, W,
+                         bias, V, Peff, vper, partials, Mdev);
+    }
+  });
   return hipGetLastError();
 }
 
@@ -1386,6 +1396,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra, const ChunkE* ce,
                                  const uint16_t* Hst, int Mp, uint16_t* dW16, const int32_t* Mdev) {
+  if (Mdev && want_dW && !dW16) return hipErrorInvalidValue;  // (only the bf16 dW takes its rows from the device)
   // wide heads: one 8-wave 256 x 256 workgroup per CU (the long k loop hides the epilogue);
   // narrow heads: two 4-wave 256 x 128 workgroups per CU, so that one's epilogue (exp, pack,
   // staged stores: VALU-bound) overlaps the other's products
@@ -1399,8 +1410,10 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
     // with ce the launch only recomputes when the normaliser's rows are unusable
     Prof pr(ce ? "recompute_check" : "recompute_dz", stream);
 #define PCTC_RECOMPUTE(GC, OCC, BI, DBI)                                                                             \
-  hipLaunchKernelGGL((recompute_dz_bf16<GC, BI, DBI, OCC>), grid, dim3(GC::kThreads), 0, stream, Hs, M, D, W, bias, \
-                     c0, cw, lam2, g, remap, S, ldS, G, ldG, dZ, chunk, dbpart, Mdev)
+  rows_from(Mdev, [&](auto dm) {                                                                                     \
+    hipLaunchKernelGGL((recompute_dz_bf16<GC, BI, DBI, OCC, dm>), grid, dim3(GC::kThreads), 0, stream, Hs, M, D, W,  \
+                       bias, c0, cw, lam2, g, remap, S, ldS, G, ldG, dZ, chunk, dbpart, Mdev);                       \
+  })
 #define PCTC_RECOMPUTE_CFG(GC, OCC)           \
   if (bias) {                                 \
     if (db) PCTC_RECOMPUTE(GC, OCC, true, true);  \
@@ -1419,12 +1432,14 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
       const int runs = max(1, min(nVt, kRcCus / nMt2));
       const int run = (nVt + runs - 1) / runs;
       const int nruns = (nVt + run - 1) / run;
-      if (Hst)
-        hipLaunchKernelGGL(recompute_run_bf16<true>, dim3(nMt2 * nruns), dim3(GMid::kThreads), 0, stream, Hs, Hst,
-                           Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr, Mdev);
-      else
-        hipLaunchKernelGGL(recompute_run_bf16<false>, dim3(nMt2 * nruns), dim3(GMid::kThreads), 0, stream, Hs, Hst,
-                           Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr, Mdev);
+      rows_from(Mdev, [&](auto dm) {
+        if (Hst)
+          hipLaunchKernelGGL((recompute_run_bf16<true, dm>), dim3(nMt2 * nruns), dim3(GMid::kThreads), 0, stream, Hs,
+                             Hst, Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr, Mdev);
+        else
+          hipLaunchKernelGGL((recompute_run_bf16<false, dm>), dim3(nMt2 * nruns), dim3(GMid::kThreads), 0, stream, Hs,
+                             Hst, Mp, M, D, W, c0, cw, run, lam2, g, dZ, chunk, ce ? ce->einv : nullptr, Mdev);
+      });
     } else {
       PCTC_RECOMPUTE_CFG(GFwd, 2)
     }
@@ -1439,8 +1454,10 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
     const int tiles = ((M + kBR - 1) / kBR) * ((D + kBC - 1) / kBC);
     const int ns = (cw + slice - 1) / slice;
     Prof pr("dh_gemm", stream);
-    hipLaunchKernelGGL((dh_gemm_bf16<GDh, 1>), dim3(tiles * ns), dim3(GDh::kThreads), 0, stream, dZ, M, chunk, W, D,
-                       c0, cw, slice, part, dh_xcd_rows(M, D), 0, nullptr, ce ? ce->rowscale : nullptr, Mdev);
+    rows_from(Mdev, [&](auto dm) {
+      hipLaunchKernelGGL((dh_gemm_bf16<GDh, 1, dm>), dim3(tiles * ns), dim3(GDh::kThreads), 0, stream, dZ, M, chunk, W,
+                         D, c0, cw, slice, part, dh_xcd_rows(M, D), 0, nullptr, ce ? ce->rowscale : nullptr, Mdev);
+    });
   }
   if (want_dW) {
     const int nDt = (D + kBC - 1) / kBC;
@@ -1455,11 +1472,13 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
     Prof pr("dw_gemm", stream);
     if (dW16) {
       p0.out = reinterpret_cast<float*>(dW16);
-      hipLaunchKernelGGL(dw_gemm_bf16<true>, dim3(tiles0), dim3(GDw::kThreads), 0, stream, p0, p0, tiles0, Hs, M, D,
-                         Mdev);
+      rows_from(Mdev, [&](auto dm) {
+        hipLaunchKernelGGL((dw_gemm_bf16<true, dm>), dim3(tiles0), dim3(GDw::kThreads), 0, stream, p0, p0, tiles0, Hs, M,
+                           D, Mdev);
+      });
     } else {
       hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles0 + tiles1), dim3(GDw::kThreads), 0, stream, p0, p1, tiles0,
-                         ce ? ce->Hp : Hs, M, D, Mdev);
+                         ce ? ce->Hp : Hs, M, D, nullptr);
     }
   }
   return hipGetLastError();
@@ -1491,18 +1510,20 @@ hipError_t launch_lse_partial_e_bf16(const uint16_t* H, int M, int D, const uint
   *P_out = sp.P;
   const dim3 grid(sp.nM * sp.P), block(GMid::kThreads);
   Prof pr("lse_partial", stream);
-  if (bias) {
-    // the partition's bias takes the 32 KB that E is staged through
-    if (!Ht || eparts > 0 || sp.vper * sizeof(float) > 32768) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((lse_partial_e_bf16<true, true>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V, sp.P,
-                       sp.vper, partials, E, epitch, 0, einv, Mdev);
-  } else if (Ht) {
-    hipLaunchKernelGGL((lse_partial_e_bf16<true>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V, sp.P, sp.vper,
-                       partials, E, epitch, eparts, einv, Mdev);
-  } else {
-    hipLaunchKernelGGL((lse_partial_e_bf16<false>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V, sp.P, sp.vper,
-                       partials, E, epitch, eparts, einv, Mdev);
-  }
+  // the partition's bias takes the 32 KB that E is staged through
+  if (bias && (!Ht || eparts > 0 || sp.vper * sizeof(float) > 32768)) return hipErrorInvalidValue;
+  rows_from(Mdev, [&](auto dm) {
+    if (bias) {
+      hipLaunchKernelGGL((lse_partial_e_bf16<true, true, dm>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V,
+                         sp.P, sp.vper, partials, E, epitch, 0, einv, Mdev);
+    } else if (Ht) {
+      hipLaunchKernelGGL((lse_partial_e_bf16<true, false, dm>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V,
+                         sp.P, sp.vper, partials, E, epitch, eparts, einv, Mdev);
+    } else {
+      hipLaunchKernelGGL((lse_partial_e_bf16<false, false, dm>), grid, block, 0, stream, H, Ht, Mp, M, D, W, bias, V,
+                         sp.P, sp.vper, partials, E, epitch, eparts, einv, Mdev);
+    }
+  });
   return hipGetLastError();
 }
 
