@@ -519,10 +519,11 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
  *   loss = sum over the counted rows of weights[m] losses[m];  dH, dW, db: its gradients
  * (where r A is the smaller the row's gradient is that of r A, else of the KL term alone).  The frame x
  * vocabulary logits are not stored: the backward recomputes them chunk by chunk as Pruned CTC's does.
- *   H, W, bias, D, V, chunk: as for pruned_ctc_fwd_bwd_ex (M rows, bias NULL for none).  M = 0 is allowed.
+ *   H, W, bias, D, V, chunk: as for pruned_ctc_fwd_bwd_ex (bias NULL for none).  0 <= M <= 2^25 rows, M D <= 2^33.
  *   tokens: device int32 [M]; advantages: device float [M].  old_logp NULL: the policy that sampled the tokens
  *   is this one (r = 1).  ref_logp NULL: no KL term.  weights NULL: 1.  All three device float [M].
- *   clip_lo, clip_hi >= 0 (+inf: not clipped), kl_weight finite and >= 0.
+ *   clip_lo, clip_hi >= 0 (+inf: not clipped), kl_weight finite and >= 0.  An advantage of 0 has no first term,
+ *   whatever old_logp is.
  *   loss: device double [1]; losses, logp: device float [M]; status: device int32 [M]: PCTC_TOKEN_COUNTED;
  *   PCTC_TOKEN_LEFT_OUT, a token outside [0, V) (a prompt's place), logp 0; PCTC_TOKEN_NONFINITE, a loss or
  *   gradient factor that is not finite.  Rows that are not counted have losses 0 and take no part in loss
@@ -530,7 +531,8 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
  *   dH [M, D], dW [V, D], db [V]: of the dtype of H, rounded once from float sums; each may be NULL, and with all
  *   three NULL only the losses are formed.
  *   workspace: pctc_policy_workspace_size() bytes (bias, grads: whether the call has a bias, asks for a
- *   gradient), 256-byte aligned.  Asynchronous; the result does not change from call to call.
+ *   gradient), 256-byte aligned.  What is written must not overlap another buffer of the call.  Asynchronous; the
+ *   result does not change from call to call.
  * ---------------------------------------------------------------------------------- */
 enum { PCTC_TOKEN_COUNTED = 0, PCTC_TOKEN_LEFT_OUT = 1, PCTC_TOKEN_NONFINITE = 2 };
 size_t pctc_policy_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t bias, int32_t grads,

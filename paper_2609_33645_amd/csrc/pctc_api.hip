@@ -1316,16 +1316,17 @@ size_t pctc_gated_ffn_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int
   return ffn_workspace_bytes(dtype == PCTC_BF16 ? 1 : 0, q, backward != 0);
 }
 
-// The block's inputs and outputs: aligned, there where they must be, and what is written apart from the rest.
-struct FfnBuffer {
+// A call's inputs and outputs: aligned, there where they must be, and what is written apart from the rest.
+struct Buffer {
   const void* p;
   uint64_t bytes;
   bool needed, written;
+  size_t align = 16;
 };
-static bool ffn_buffers_ok(const FfnBuffer* b, int n) {
+static bool buffers_ok(const Buffer* b, int n) {
   for (int i = 0; i < n; ++i) {
     if (b[i].bytes == 0) continue;
-    if ((b[i].needed && !b[i].p) || misaligned16(b[i].p)) return false;
+    if ((b[i].needed && !b[i].p) || misaligned_to(b[i].p, b[i].align)) return false;
     for (int j = 0; j < n; ++j)
       if (j != i && b[i].written && (!b[j].written || j > i) && meets(b[i].p, b[i].bytes, b[j].p, b[j].bytes))
         return false;
@@ -1340,10 +1341,10 @@ int32_t pctc_gated_ffn(pctc_dtype dtype, const void* x, int32_t M, int32_t D, co
   if (need == 0 || (activation != PCTC_SILU && activation != PCTC_GELU) || !gate != !up) return PCTC_EINVAL;
   if (M == 0) return PCTC_OK;
   const uint64_t e = value_bytes(dtype), m = M, d = e * D, f = F, o = e * O;
-  const FfnBuffer b[] = {{x, m * d, true, false}, {w_gate, f * d, true, false}, {w_up, f * d, true, false},
+  const Buffer b[] = {{x, m * d, true, false}, {w_gate, f * d, true, false}, {w_up, f * d, true, false},
                          {w_down, o * f, true, false}, {gate, 4 * m * f, false, true}, {up, 4 * m * f, false, true},
                          {y, m * o, true, true}};
-  if (!ffn_buffers_ok(b, 7)) return PCTC_EINVAL;
+  if (!buffers_ok(b, 7)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (misaligned256(workspace)) return PCTC_EINVAL;
   const FfnArgs q{x, w_gate, w_up, w_down, gate, up, y, M, D, F, O, activation};
@@ -1360,11 +1361,11 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
   const size_t need = pctc_gated_ffn_workspace_size(dtype, M, D, F, O, 1);
   if (need == 0 || (activation != PCTC_SILU && activation != PCTC_GELU) || !dw_gate != !dw_up) return PCTC_EINVAL;
   const uint64_t e = value_bytes(dtype), m = M, d = e * D, f = F, o = e * O;
-  const FfnBuffer b[] = {{x, m * d, true, false}, {dy, m * o, true, false}, {gate, 4 * m * f, true, false},
+  const Buffer b[] = {{x, m * d, true, false}, {dy, m * o, true, false}, {gate, 4 * m * f, true, false},
                          {up, 4 * m * f, true, false}, {w_gate, f * d, true, false}, {w_up, f * d, true, false},
                          {w_down, o * f, true, false}, {dx, m * d, false, true}, {dw_gate, f * d, false, true},
                          {dw_up, f * d, false, true}, {dw_down, o * f, false, true}};
-  if (!ffn_buffers_ok(b, 11)) return PCTC_EINVAL;
+  if (!buffers_ok(b, 11)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (misaligned256(workspace)) return PCTC_EINVAL;
   const FfnArgs q{x, w_gate, w_up, w_down, const_cast<float*>(gate), const_cast<float*>(up), nullptr, M, D, F, O, activation};
@@ -1376,9 +1377,15 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
 
 // ---- policy loss on the head -----------------------------------------------------------------
 
+constexpr int32_t kMaxPolicyRows = 1 << 25;
+constexpr int64_t kMaxPolicyValues = int64_t{1} << 33;
+
 size_t pctc_policy_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t bias, int32_t grads,
                                   int32_t chunk) {
-  if (!head_args_ok(dtype, D, V) || M < 0 || M > kMaxFrames || chunk < 0 || chunk % 256) return 0;
+  // (64 threads a row, and one for 4 values of dH, are counted in 32 bits)
+  if (!head_args_ok(dtype, D, V) || M < 0 || M > kMaxPolicyRows || static_cast<int64_t>(M) * D > kMaxPolicyValues ||
+      chunk < 0 || chunk % 256)
+    return 0;
   return policy_layout(dtype == PCTC_BF16 ? 1 : 0, M, D, V, bias != 0, grads != 0, chunk).total;
 }
 
@@ -1389,13 +1396,16 @@ int32_t pctc_policy_loss(pctc_dtype dtype, const void* H, int32_t M, int32_t D, 
                          void* db, void* workspace, size_t workspace_bytes, void* stream_ptr) {
   const bool grads = dH || dW || db;
   const size_t need = pctc_policy_workspace_size(dtype, M, D, V, bias != nullptr, grads, chunk);
-  if (need == 0 || !(clip_lo >= 0.f) || !(clip_hi >= 0.f) || !(kl_weight >= 0.f) || !(kl_weight < INFINITY) || !loss ||
-      !W || misaligned16(W) || misaligned16(H) || misaligned16(dH) || misaligned16(dW))
+  if (need == 0 || !(clip_lo >= 0.f) || !(clip_hi >= 0.f) || !(kl_weight >= 0.f) || !(kl_weight < INFINITY))
     return PCTC_EINVAL;
-  if (M > 0 && (!H || !tokens || !advantages || !losses || !logp || !status)) return PCTC_EINVAL;
-  const uint64_t e = value_bytes(dtype), nh = e * M * D, nw = e * V * D;
-  if (meets(dH, nh, H, nh) || meets(dH, nh, W, nw) || meets(dW, nw, H, nh) || meets(dW, nw, W, nw) || meets(dH, nh, dW, nw))
-    return PCTC_EINVAL;
+  const uint64_t e = value_bytes(dtype), m = M, v = V, d = e * D;
+  const Buffer b[] = {{H, m * d, true, false}, {W, v * d, true, false}, {bias, 4 * v, false, false, 4},
+                      {tokens, 4 * m, true, false, 4}, {advantages, 4 * m, true, false, 4},
+                      {old_logp, 4 * m, false, false, 4}, {ref_logp, 4 * m, false, false, 4},
+                      {weights, 4 * m, false, false, 4}, {loss, 8, true, true, 8}, {losses, 4 * m, true, true, 4},
+                      {logp, 4 * m, true, true, 4}, {status, 4 * m, true, true, 4}, {dH, m * d, false, true},
+                      {dW, v * d, false, true}, {db, v * e, false, true, e}};
+  if (!buffers_ok(b, 15)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (misaligned256(workspace)) return PCTC_EINVAL;
   const int dt = dtype == PCTC_BF16 ? 1 : 0;

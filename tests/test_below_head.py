@@ -138,7 +138,16 @@ def test_policy_refusals_and_sizes():
                 dict(W=p[1] + 8), dict(dH=p[8] + 8), dict(dW=p[9] + 8), dict(dH=p[0]), dict(dH=p[1] + 16), dict(dW=p[1]),
                 dict(dW=p[8] + 1024), dict(ws=p[10] + 16)):
         assert call(**bad) == -1, bad
-    assert call(ws=None) == call(bytes=1000) == -4
+    # what is written may meet nothing else of the call; floats lie on their size
+    full = dict(bias=p[11], old=p[12], ref=p[13], w=p[14], db=p[15])
+    for bad in (dict(logp=p[12]), dict(losses=p[3]), dict(losses=p[6] + 36), dict(status=p[2]), dict(loss=p[5] + 32),
+                dict(db=p[11]), dict(db=p[9] + 64), dict(losses=p[14]), dict(logp=p[13] + 4), dict(status=p[8] + 4),
+                dict(loss=p[4] + 4), dict(logp=p[6] + 2), dict(bias=p[11] + 2), dict(old=p[12] + 1), dict(db=p[15] + 1)):
+        assert call(**{**full, **bad}) == -1, bad
+    assert call(**full, bytes=1000) == -4  # (nothing else is wrong with it)
+    # rows and values whose threads 32 bits would not count
+    assert size(1, 1 << 25, 64, 300, 0, 1, 0) > 0 and size(1, (1 << 25) + 1, 64, 300, 0, 1, 0) == 0
+    assert size(1, 1 << 23, 1024, 300, 0, 1, 0) > 0 and size(1, (1 << 23) + 1, 1024, 300, 0, 1, 0) == 0
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
