@@ -804,12 +804,9 @@ struct DwOp {
 };
 
 // dW products of up to two operand sets in one launch: work ids below tiles0 take P0's output
-// tiles, the rest P1's (the union columns' dW_u in the last chunk's launch).  O16: `out` holds bf16.
-template <bool O16, bool DM = false>
+// tiles, the rest P1's (the union columns' dW_u in the last chunk's launch).
 __global__ void __launch_bounds__(512, 1)
-dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int M, int D,
-             const int32_t* __restrict__ Mdev) {
-  if constexpr (DM) M = min(M, *Mdev);  // (with none, zeros are written)
+dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int M, int D) {
   using G = GDw;
   constexpr int FR = G::FR, FC = G::FC;
   PCTC_STAGES_G(G)
@@ -827,7 +824,7 @@ dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int 
   const int mb = z * P.mslice;
   const int mlen = min(M - mb, P.mslice);
   if (P.kdev) cw = min(cw, 2 * *P.kdev);
-  if (z >= P.nz || (mlen <= 0 && !DM) || v0 >= cw) return;
+  if (z >= P.nz || mlen <= 0 || v0 >= cw) return;
   float* const dW = P.out + static_cast<int64_t>(z) * P.zstride;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // A: Z viewed as rows v (columns of Z), k = frame; B: Hs viewed as rows d, k = frame
@@ -844,11 +841,7 @@ dw_gemm_bf16(DwOp P0, DwOp P1, int tiles0, const uint16_t* __restrict__ Hs, int 
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int v = v0 + G::row_of(wave, lane, i, r);
-        const int64_t at = static_cast<int64_t>(P.c0 + v) * D + d;
-        if (v < cw) {
-          if constexpr (O16) reinterpret_cast<uint16_t*>(dW)[at] = static_cast<uint16_t>(pack_bf16x2(acc[i][j][r], 0.f));
-          else dW[at] = acc[i][j][r];
-        }
+        if (v < cw) dW[static_cast<int64_t>(P.c0 + v) * D + d] = acc[i][j][r];
       }
     }
 }
@@ -1116,8 +1109,7 @@ hipError_t launch_union_part_bf16(const float* G, int ldG, const int32_t* Kdev, 
     const DwOp p{Gb, k2, 0, k2, reinterpret_cast<float*>(sc + L.o_dwu), L.nz, L.mslice,
                  static_cast<int64_t>(k2) * D, Kdev};
     Prof pr("union_dw", stream);
-    hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles), dim3(GDw::kThreads), 0, stream, p, p, tiles, Hs, M, D,
-                       nullptr);
+    hipLaunchKernelGGL(dw_gemm_bf16, dim3(tiles), dim3(GDw::kThreads), 0, stream, p, p, tiles, Hs, M, D);
   }
   if (want_db) {
     const int mper = (M + kColSlices - 1) / kColSlices;
@@ -1395,8 +1387,8 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  const int32_t* remap, const float* S, int ldS, uint16_t* dZ, int chunk, float* part,
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra, const ChunkE* ce,
-                                 const uint16_t* Hst, int Mp, uint16_t* dW16, const int32_t* Mdev) {
-  if (Mdev && want_dW && !dW16) return hipErrorInvalidValue;  // (only the bf16 dW takes its rows from the device)
+                                 const uint16_t* Hst, int Mp, const int32_t* Mdev) {
+  if (Mdev && want_dW) return hipErrorInvalidValue;  // (dW's kernel takes M rows)
   // wide heads: one 8-wave 256 x 256 workgroup per CU (the long k loop hides the epilogue);
   // narrow heads: two 4-wave 256 x 128 workgroups per CU, so that one's epilogue (exp, pack,
   // staged stores: VALU-bound) overlaps the other's products
@@ -1462,7 +1454,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
   if (want_dW) {
     const int nDt = (D + kBC - 1) / kBC;
     const int tiles0 = ((cw + kBR - 1) / kBR) * nDt;
-    DwOp p0{dZ, chunk, c0, cw, dW, 1, M, 0, nullptr};
+    const DwOp p0{dZ, chunk, c0, cw, dW, 1, M, 0, nullptr};
     DwOp p1 = p0;
     int tiles1 = 0;
     if (extra && extra->Z) {  // the union columns' dW_u, in this launch's last round
@@ -1470,16 +1462,8 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
       tiles1 = ((extra->cols + kBR - 1) / kBR) * nDt;
     }
     Prof pr("dw_gemm", stream);
-    if (dW16) {
-      p0.out = reinterpret_cast<float*>(dW16);
-      rows_from(Mdev, [&](auto dm) {
-        hipLaunchKernelGGL((dw_gemm_bf16<true, dm>), dim3(tiles0), dim3(GDw::kThreads), 0, stream, p0, p0, tiles0, Hs, M,
-                           D, Mdev);
-      });
-    } else {
-      hipLaunchKernelGGL(dw_gemm_bf16<false>, dim3(tiles0 + tiles1), dim3(GDw::kThreads), 0, stream, p0, p1, tiles0,
-                         ce ? ce->Hp : Hs, M, D, nullptr);
-    }
+    hipLaunchKernelGGL(dw_gemm_bf16, dim3(tiles0 + tiles1), dim3(GDw::kThreads), 0, stream, p0, p1, tiles0,
+                       ce ? ce->Hp : Hs, M, D);
   }
   return hipGetLastError();
 }

@@ -330,4 +330,63 @@ __device__ __forceinline__ void amax_store_partials(float (&bv)[G::FC], int (&bi
   }
 }
 
+// A wavefront's accumulators (128 tile rows x 64 columns) as rows of the output: 32 columns at a time go
+// through its own 16 KB of the drained stages (16-byte slots XORed with the column, so that neither
+// writes nor reads meet in a bank), and come back 8 consecutive tile rows a lane, 16 lanes a column, so that
+// memory is read and written in lines.  Straight from the accumulators a store is 32 pieces of 16 bytes: the
+// epilogue of ffn_back then took longer than its product (M = 2,567, 4,096 x 10,240: 419 us, now 238).
+// fn(block, col, v, x): tile rows 8 block .. 8 block + 7 of the wavefront's 128, column col of its 64; x is what
+// pre(block, col, x) read for these places, for 32 columns before any of them is used, so that many
+// reads are in flight (there is one workgroup on a compute unit, whose products are over).
+// A wavefront's LDS accesses are ordered; no barrier is needed.
+struct Nothing {};
+template <class G, class X = Nothing, class Fn, class Pre>
+__device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* const (&st)[4], Fn&& fn, Pre&& pre) {
+  static_assert(G::FR == 4 && G::FC == 2, "128 x 64");
+  int lane = threadIdx.x & 63;
+  // opaque: what is derived from it is not kept in registers through the product (it would spill there)
+  asm volatile("" : "+v"(lane));
+  const int wave = threadIdx.x >> 6;
+  char* const base = (wave < 2 ? st[0] : wave < 4 ? st[1] : wave < 6 ? st[2] : st[3]) + (wave & 1) * 16384;
+  constexpr int NB = sizeof(X) > 32 ? 4 : 8;  // places a lane reads ahead
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int c = lane & 31;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int slot = 8 * i + 2 * q + (lane >> 5);  // tile rows 4 slot ..
+        *reinterpret_cast<float4*>(base + c * 512 + ((slot ^ (c & 31)) << 4)) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+      }
+    const int block = lane & 15;
+#pragma unroll
+    for (int t0 = 0; t0 < 8; t0 += NB) {
+      X x[NB];
+#pragma unroll
+      for (int t = 0; t < NB; ++t) pre(block, 32 * j + 4 * (t0 + t) + (lane >> 4), x[t]);
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        const int col = 4 * (t0 + t) + (lane >> 4);
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float4 y = *reinterpret_cast<const float4*>(base + col * 512 + (((2 * block + h) ^ (col & 31)) << 4));
+          v[4 * h] = y.x;
+          v[4 * h + 1] = y.y;
+          v[4 * h + 2] = y.z;
+          v[4 * h + 3] = y.w;
+        }
+        fn(block, 32 * j + col, v, x[t]);
+      }
+    }
+  }
+}
+template <class G, class Fn>
+__device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* const (&st)[4], Fn&& fn) {
+  by_columns<G>(acc, st, [&](int block, int col, const float (&v)[8], const Nothing&) { fn(block, col, v); },
+                [](int, int, Nothing&) {});
+}
+
 }  // namespace pctc

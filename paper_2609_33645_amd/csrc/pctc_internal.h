@@ -171,7 +171,20 @@ struct DzTokens {
   const int32_t* status = nullptr;
   int N = 0;
   double* loss = nullptr;
+  // what the rounding of the own entries took off, by class of the chunk (null: not kept; bf16): OwnFirst
+  // [chunk] and OwnRest [chunk][kOwnMost - 1]
+  struct OwnFirst* first = nullptr;
+  struct OwnRest* rest = nullptr;
 };
+struct __attribute__((aligned(16))) OwnFirst {
+  int count, row;  // tokens of the class (at most kOwnMost kept), the first one's row and its rest
+  float rest;
+};
+struct OwnRest {
+  int row;
+  float rest;
+};
+constexpr int kOwnMost = 16;
 hipError_t launch_dz_tokens(int dtype, void* dZ, int pitch, int M, int c0, int cw, const DzTokens& t, float scale,
                             hipStream_t stream);
 
@@ -219,7 +232,6 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra = nullptr,
                                  const ChunkE* ce = nullptr, const uint16_t* Hst = nullptr, int Mp = 0,
-                                 uint16_t* dW16 = nullptr,  // dW is written there, rounded to bf16 (no extra, no ce)
                                  const int32_t* Mdev = nullptr);
 // Partitions of the normaliser that can write E for a first chunk of `chunk` columns (0: none;
 // narrow heads with D a multiple of 128, chunk a multiple of the partition width).
@@ -394,7 +406,7 @@ struct PolicyArgs {
 };
 struct PolicyLayout {
   BwdPlan bwd;
-  size_t o_lam2, o_g, o_tok, o_lp, o_rows, o_inv, o_count, o_h, o_part, o_ht, o_dh, o_bwd, total;
+  size_t o_lam2, o_g, o_tok, o_lp, o_rows, o_inv, o_count, o_h, o_part, o_ht, o_dh, o_own, o_bwd, total;
   bool ht;  // the normaliser reads H transposed
 };
 // grads: the call asks for gradients.

@@ -10,6 +10,8 @@
 // number, which only the device knows.  Between the products: the tokens' normalisers, logits and losses (a
 // wavefront a token), and in every chunk of the backward the tokens' own entries of dZ, the sum of the
 // losses beside the first.  Bound by the matrix products, 8 M V D operations (the logits are formed twice).
+#include "gemm_bf16.h"
+#include "head_tiles.h"
 #include "pctc_internal.h"
 
 namespace pctc {
@@ -231,8 +233,49 @@ __device__ __forceinline__ void sum_losses(const DzTokens& t) {
 // A token's own entry of dZ: g (1 - p), 1 - p = -expm1(lp).
 __device__ __forceinline__ float own_entry(const DzTokens& t, int j) { return -expm1f(t.logp[j]) * t.g[j]; }
 
-// The tokens' own entries of a chunk.  The last workgroup of a launch that sums
-// does nothing else.
+__device__ __forceinline__ float own_rest(const DzTokens& t, int j) {
+  if (t.g[j] == 0.f) return 0.f;
+  const float x = own_entry(t, j);
+  return x - bf16_to_f32(f32_to_bf16(x));
+}
+
+// The tokens of 256 classes, a lane a class: the first kOwnMost of each in the order of their rows, with what the
+// rounding took off their entries.  A wavefront stops after kOwnWave tokens of its 64 classes: where there
+// are more the roundings average out, and a class may have them all.
+constexpr int kOwnWave = 512;
+__device__ __forceinline__ void list_tokens(const DzTokens& t, int M, int c0, int tile) {
+  const int lane = threadIdx.x & 63;
+  const int cls = tile * 256 + threadIdx.x, lo = c0 + cls - lane;  // of the chunk; this wavefront's first class
+  OwnRest* const more = t.rest + static_cast<int64_t>(cls) * (kOwnMost - 1);
+  OwnFirst first{0, 0, 0.f};
+  int seen = 0;
+  constexpr int kAhead = 8;
+  for (int m0 = 0; m0 < M && seen < kOwnWave; m0 += 64 * kAhead) {
+    int at[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) at[k] = m0 + 64 * k + lane < M ? t.token[m0 + 64 * k + lane] - lo : -1;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      uint64_t hits = __ballot(static_cast<unsigned>(at[k]) < 64u);
+      for (; hits; hits &= hits - 1, ++seen) {
+        const int b = __builtin_ctzll(hits);
+        if (__builtin_amdgcn_readlane(at[k], b) == lane) {
+          const int m = m0 + 64 * k + b;
+          if (first.count == 0) first.row = m;
+          else if (first.count < kOwnMost) more[first.count - 1].row = m;
+          ++first.count;
+        }
+      }
+    }
+  }
+  first.count = min(first.count, kOwnMost);
+  if (first.count > 0) first.rest = own_rest(t, first.row);
+  for (int e = 1; e < first.count; ++e) more[e - 1].rest = own_rest(t, more[e - 1].row);
+  t.first[cls] = first;
+}
+
+// The tokens' own entries of a chunk.  Of a launch that sums the last workgroup does nothing else, and of one
+// that lists them the ceil(cw / 256) before it.
 template <bool BF>
 __global__ void __launch_bounds__(kThreads)
 dz_tokens(void* __restrict__ dZ, int pitch, int M, int c0, int cw, DzTokens t, float scale) {
@@ -240,7 +283,12 @@ dz_tokens(void* __restrict__ dZ, int pitch, int M, int c0, int cw, DzTokens t, f
     sum_losses(t);
     return;
   }
+  const int rows = (M + kThreads - 1) / kThreads;
   if (t.Mdev) M = min(M, *t.Mdev);
+  if (static_cast<int>(blockIdx.x) >= rows) {
+    if constexpr (BF) list_tokens(t, M, c0, blockIdx.x - rows);
+    return;
+  }
   const int m = blockIdx.x * kThreads + threadIdx.x;
   if (m >= M) return;
   const int v = t.token[m] - c0;
@@ -252,12 +300,11 @@ dz_tokens(void* __restrict__ dZ, int pitch, int M, int c0, int cw, DzTokens t, f
   else static_cast<float*>(dZ)[at] = x;
 }
 
-// db of a bf16 chunk: column sums of dZ over slices of the frames, then over the slices.  32 lanes of 8
-// columns and 8 frames at a time.
+// db of a bf16 chunk: column sums of dZ, with what the rounding took off the own entries, over slices of the
+// frames, then over the slices.  32 lanes of 8 columns and 8 frames at a time.
 __global__ void __launch_bounds__(kThreads)
-db_slices(const uint16_t* __restrict__ dZ, int M, int pitch, int mper, float* __restrict__ part,
-          const int32_t* __restrict__ Mdev) {
-  if (Mdev) M = min(M, *Mdev);
+db_slices(const uint16_t* __restrict__ dZ, int M, int pitch, int mper, float* __restrict__ part, int c0, DzTokens t) {
+  M = min(M, *t.Mdev);
   __shared__ float x[8][kThreads];
   const int col = (threadIdx.x & 31) * 8, row = threadIdx.x >> 5;
   const int v = blockIdx.x * 256 + col;  // the pitch is a multiple of 256
@@ -271,14 +318,20 @@ db_slices(const uint16_t* __restrict__ dZ, int M, int pitch, int mper, float* __
       s[2 * e] += __uint_as_float(w[e] << 16);
       s[2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
     }
+    const int own = t.token[m] - c0 - v;
+    if (static_cast<unsigned>(own) < 8u) {
+      const float r = own_rest(t, m);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += e == own ? r : 0.f;
+    }
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[row][col + e] = s[e];
   __syncthreads();
-  float t = 0.f;
+  float total = 0.f;
 #pragma unroll
-  for (int r = 0; r < 8; ++r) t += x[r][threadIdx.x];
-  part[static_cast<int64_t>(blockIdx.y) * pitch + blockIdx.x * 256 + threadIdx.x] = t;
+  for (int r = 0; r < 8; ++r) total += x[r][threadIdx.x];
+  part[static_cast<int64_t>(blockIdx.y) * pitch + blockIdx.x * 256 + threadIdx.x] = total;
 }
 __global__ void __launch_bounds__(kThreads)
 db_join(const float* __restrict__ part, int slices, int pitch, int cw, uint16_t* __restrict__ db) {
@@ -326,6 +379,51 @@ dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, int D, cons
   *reinterpret_cast<u32x2*>(dH + i) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
 }
 
+// dW of a bf16 chunk: tiles of 256 values of a row x 256 classes, so that the accumulators leave in lines, each
+// class with what the rounding took off its tokens' own entries times their rows of H, before its one rounding
+// to bf16 (0.0023 -> 0.0017 of dW's norm; of few rows one rounding may be most of the error: 40 rows of 100
+// classes, up to 0.0034).
+__global__ void __launch_bounds__(512, 1)
+policy_dw(const uint16_t* __restrict__ dZ, int pitch, int M, const uint16_t* __restrict__ H, int D, int c0, int cw,
+          uint16_t* __restrict__ dW, DzTokens t) {
+  using G = bf::Gemm<256, 256, 32, bf::LL::MC, bf::LL::MC, 4, 2, 4, true>;
+  __shared__ __attribute__((aligned(1024))) char st0[G::kStageBytes];
+  __shared__ __attribute__((aligned(1024))) char st1[G::kStageBytes];
+  __shared__ __attribute__((aligned(1024))) char st2[G::kStageBytes];
+  __shared__ __attribute__((aligned(1024))) char st3[G::kStageBytes];
+  char* const st[4] = {st0, st1, st2, st3};
+  M = min(M, *t.Mdev);  // (with none, zeros are written)
+  const int nDt = (D + 255) / 256;
+  const int w = xcd_swz(blockIdx.x, gridDim.x);
+  const int d0 = w % nDt * 256, v0 = w / nDt * 256;
+  const bf::GOp A{H, D, D, M, nullptr}, B{dZ, pitch, cw, M, nullptr};
+  f32x16 acc[G::FR][G::FC];
+  G::run_pp(A, B, d0, v0, 0, M, st, acc);
+  const int wave = threadIdx.x >> 6;
+  const int dw = d0 + wave / 4 * 128, vw = v0 + wave % 4 * 64;
+  by_columns<G, OwnFirst>(
+      acc, st,
+      [&](int block, int col, float (&s)[8], const OwnFirst& own) {
+        const int d = dw + block * 8, v = vw + col;
+        if (v >= cw || d >= D) return;
+        auto add = [&](int row, float rest) {
+          const u32x4 h = *reinterpret_cast<const u32x4*>(H + static_cast<int64_t>(row) * D + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[2 * e] = fmaf(rest, __uint_as_float(h[e] << 16), s[2 * e]);
+            s[2 * e + 1] = fmaf(rest, __uint_as_float(h[e] & 0xffff0000u), s[2 * e + 1]);
+          }
+        };
+        if (own.count > 0) add(own.row, own.rest);
+        const OwnRest* const more = t.rest + static_cast<int64_t>(v) * (kOwnMost - 1);
+#pragma unroll 4
+        for (int e = 1; e < own.count; ++e) add(more[e - 1].row, more[e - 1].rest);
+        *reinterpret_cast<u32x4*>(dW + static_cast<int64_t>(c0 + v) * D + d) =
+            u32x4{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]), pack_bf16x2(s[4], s[5]), pack_bf16x2(s[6], s[7])};
+      },
+      [&](int, int col, OwnFirst& own) { own = t.first[vw + col]; });
+}
+
 constexpr int kDbSlices = 16;
 
 }  // namespace
@@ -335,7 +433,7 @@ hipError_t launch_dz_tokens(int dtype, void* dZ, int pitch, int M, int c0, int c
   Prof pr("dz_tokens", stream);
   DzTokens t = tokens;
   if (c0 > 0) t.loss = nullptr;
-  const dim3 grid((M + kThreads - 1) / kThreads + (t.loss ? 1 : 0));
+  const dim3 grid((M + kThreads - 1) / kThreads + (t.first ? (cw + 255) / 256 : 0) + (t.loss ? 1 : 0));
   if (dtype == 1) hipLaunchKernelGGL(dz_tokens<true>, grid, dim3(kThreads), 0, stream, dZ, pitch, M, c0, cw, t, scale);
   else hipLaunchKernelGGL(dz_tokens<false>, grid, dim3(kThreads), 0, stream, dZ, pitch, M, c0, cw, t, scale);
   return hipGetLastError();
@@ -371,6 +469,7 @@ PolicyLayout policy_layout(int dtype, int M, int D, int V, bool bias, bool grads
     at = fwd;
     // one slice of the dH product has no room of its own in the plan
     L.o_dh = take(dtype == 1 && L.bwd.part_bytes == 0 ? m * D * sizeof(float) : 0);
+    L.o_own = take(dtype == 1 ? L.bwd.chunk * (sizeof(OwnFirst) + (kOwnMost - 1) * sizeof(OwnRest)) : 0);
     L.o_bwd = take(L.bwd.total);
     at = at > end ? at : end;
   }
@@ -384,7 +483,8 @@ static hipError_t policy_bwd_bf16(uint16_t* Hc, int M, int D, const uint16_t* W,
                                   uint16_t* dW, uint16_t* db, char* scratch, const BwdPlan& plan, float* one,
                                   hipStream_t stream) {
   uint16_t* dZ = reinterpret_cast<uint16_t*>(scratch);
-  uint16_t* Hst = bwd_hst(scratch, plan);
+  // the recompute reads the frames transposed where that pays for its launch (with a bias it never does)
+  uint16_t* Hst = !bias && frames_from_ht_bf16(M, D, V) ? bwd_hst(scratch, plan) : nullptr;
   float* part = one ? one : reinterpret_cast<float*>(scratch + plan.dz_bytes + plan.ht_bytes);
   float* dbpart = reinterpret_cast<float*>(scratch + plan.dz_bytes + plan.ht_bytes + plan.part_bytes + plan.lam2_bytes);
   const int chunk = plan.chunk;
@@ -403,20 +503,25 @@ static hipError_t policy_bwd_bf16(uint16_t* Hc, int M, int D, const uint16_t* W,
     }
     e = launch_bwd_chunk_bf16(Hc, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
                               sl, true, false, false, nullptr, nullptr, nullptr, stream, nullptr, nullptr, Hst, plan.Mp,
-                              nullptr, tokens.Mdev);
+                              tokens.Mdev);
     if (e != hipSuccess) return e;
     if ((e = launch_dz_tokens(1, dZ, chunk, M, c0, cw, tokens, 1.f, stream)) != hipSuccess) return e;
     if (db) {
       Prof pr("db_colsum", stream);
       const int most = (M + 127) / 128 < kDbSlices ? (M + 127) / 128 : kDbSlices;  // (dbpart has a row per 128 frames)
       const int mper = ((M + most - 1) / most + 7) / 8 * 8, slices = (M + mper - 1) / mper, tiles = (cw + 255) / 256;
-      hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart, tokens.Mdev);
+      hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart, c0, tokens);
       hipLaunchKernelGGL(db_join, dim3(tiles), dim3(kThreads), 0, stream, dbpart, slices, chunk, cw, db + c0);
     }
     e = launch_bwd_chunk_bf16(Hc, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
-                              sl, false, dH != nullptr, dW != nullptr, nullptr, nullptr, nullptr, stream, nullptr, nullptr,
-                              Hst, plan.Mp, dW, tokens.Mdev);
+                              sl, false, dH != nullptr, false, nullptr, nullptr, nullptr, stream, nullptr, nullptr, Hst,
+                              plan.Mp, tokens.Mdev);
     if (e != hipSuccess) return e;
+    if (dW) {
+      Prof pr("dw_gemm", stream);
+      const dim3 grid((cw + 255) / 256 * ((D + 255) / 256));
+      hipLaunchKernelGGL(policy_dw, grid, dim3(512), 0, stream, dZ, chunk, M, Hc, D, c0, cw, dW, tokens);
+    }
   }
   if (dH) {
     const int64_t n = static_cast<int64_t>(M) * D;
@@ -483,6 +588,10 @@ hipError_t launch_policy_loss(int dtype, const void* H, int M, int D, const void
                          grads ? Hc : nullptr);
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (dW) {
+      tokens.first = reinterpret_cast<OwnFirst*>(ws + L.o_own);
+      tokens.rest = reinterpret_cast<OwnRest*>(tokens.first + L.bwd.chunk);
+    }
     if (grads)
       return policy_bwd_bf16(Hc, M, D, Wb, bias, V, lam2, tokens, i32(L.o_inv), static_cast<uint16_t*>(dH),
                              static_cast<uint16_t*>(dW), static_cast<uint16_t*>(db), ws + L.o_bwd, L.bwd,

@@ -120,9 +120,9 @@ def test_policy_refusals_and_sizes():
                 (1, 1, 64, 1, 0, 1, 0), (1, 1, 64, 524_289, 0, 1, 0), (1, 1, 64, 300, 0, 1, 100), (1, 1, 64, 300, 0, 1, -256),
                 (1, (1 << 30) + 1, 64, 300, 0, 1, 0)):
         assert size(*bad) == 0, bad
-    # the gradients' room does not grow with the vocabulary
+    # the gradients' room does not grow with the vocabulary (chunks differ by up to 10,240 columns of 136 bytes)
     big = [size(1, 4000, 512, V, 0, 1, 0) for V in (150_000, 180_000, 400_000)]
-    assert max(big) - min(big) < 1 << 20
+    assert max(big) - min(big) < 2 << 20
     p = [OK + i * BIG for i in range(16)]
     good = dict(dtype=1, H=p[0], M=10, D=64, W=p[1], bias=None, V=300, tokens=p[2], adv=p[3], old=None, ref=None, w=None, lo=0.2,
                 hi=0.2, kl=0.0, chunk=0, loss=p[4], losses=p[5], logp=p[6], status=p[7], dH=p[8], dW=p[9], db=None, ws=p[10],

@@ -266,14 +266,15 @@ def policy_call(c, dtype, clip, kl, **kw):
                           d(c["bias"]), clip=clip, kl_weight=kl, **kw)
 
 
-def check_policy(c, dtype, clip, kl, got, db=False, status=None):
+def check_policy(c, dtype, clip, kl, got, db=False, status=None, own_rounded=True):
     """Errors to first order.  A logit: (D + 2) 2^-24 of the sum of its terms' magnitudes; lambda: the largest logit's
     error and 2e-5, the normaliser's bar.  From these the token's log probability (one rounding more), its
     ratio and KL factor, hence g; a probability by its logit's and lambda's errors and the exponential's
     2^-21; dZ by these and one rounding to the products' type (of the token's own entry: of g (1 - p), whose p
     is off by the log probability's error).  Products: magnitudes times the roundings of their sums, at most one
     per 16 terms on the matrix cores and one per slice, taken as one per term; a rounding at the end.
-    float32 products drop 2^-24 of each term and round six times per 16 terms: the same bound."""
+    float32 products drop 2^-24 of each term and round six times per 16 terms: the same bound.
+    own_rounded False: the rounding of the tokens' own entries is made good in the gradients."""
     lo, hi = clip
     w = ref.policy(c["H"], c["W"], c["bias"], c["tokens"], c["adv"], c["old"], c["ref"], c["w"], lo, hi, kl)
     M, V = w["p"].shape
@@ -301,7 +302,8 @@ def check_policy(c, dtype, clip, kl, got, db=False, status=None):
     edz = g * ep + eg[:, None] * w["p"] + e * np.abs(w["dZ"])
     rows = np.nonzero(ok)[0]
     own = (rows, t[rows])
-    edz[own] = (g[rows, 0] * w["p"][own] * elp[rows] * 1.01 + eg[rows] * (1 - w["p"][own]) + (e + 4 * F) * np.abs(w["dZ"][own]))
+    edz[own] = (g[rows, 0] * w["p"][own] * elp[rows] * 1.01 + eg[rows] * (1 - w["p"][own])
+                + ((e if own_rounded else 0) + 4 * F) * np.abs(w["dZ"][own]))
     dz = np.abs(w["dZ"]) + edz
     aW, aH = np.abs(c["W"]), np.abs(c["H"])
     out = E[dtype]
@@ -347,6 +349,35 @@ def test_policy_loss_of_nearly_certain_tokens(dtype):
     c["old"], c["ref"] = (lp - 0.05).astype(np.float32), (lp + 0.1).astype(np.float32)
     w = check_policy(c, dtype, (0.2, 0.2), 0.05, policy_call(c, dtype, (0.2, 0.2), 0.05))
     assert np.median(w["p"][np.nonzero(ok)[0], c["tokens"][ok]]) > 0.95  # (the inputs are what they are meant to be)
+
+
+@pytest.mark.parametrize("M,D,V,chunk,bias", [(1, 64, 300, 0, True), (1, 8, 2, 0, False), (3, 72, 700, 256, True),
+                                              (40, 64, 100, 0, True), (40, 200, 1000, 512, False), (331, 512, 5000, 0, True)])
+def test_policy_loss_of_few_tokens_a_class(M, D, V, chunk, bias):
+    """In bf16 what the rounding of a token's own entry of dZ takes off is made good in all three gradients: of few
+    rows one such rounding may be most of the error."""
+    say("policy_loss few tokens a class", M, D, V, chunk, bias)
+    c = policy_case(3 * M + V, M, D, V, "bf16", bias)
+    if M < 4:  # (all of them count)
+        c["tokens"] = np.abs(c["tokens"]) % V
+    live = c["tokens"][(c["tokens"] >= 0) & (c["tokens"] < V)]
+    assert len(live) and np.bincount(live).max() <= 16
+    got = policy_call(c, "bf16", (0.2, 0.3), 0.07, chunk=chunk, want_db=True)
+    check_policy(c, "bf16", (0.2, 0.3), 0.07, got, db=True, own_rounded=False)
+
+
+@pytest.mark.parametrize("M,V,classes", [(700, 300, 1), (900, 300, 2), (700, 600, 30), (1500, 130, 130), (2100, 256, 64)])
+def test_policy_loss_of_many_tokens_a_class(M, V, classes):
+    """More tokens of a class than are made good one by one, and more than a wavefront goes through."""
+    say("policy_loss many tokens a class", M, V, classes)
+    c = policy_case(M + classes, M, 64, V, "bf16", True)
+    ids = np.random.default_rng(classes).permutation(V)[:classes]
+    c.update(tokens=ids[np.arange(M) % classes], old=None, ref=None)
+    got = policy_call(c, "bf16", (0.2, 0.3), 0.0, want_db=True, chunk=256)
+    check_policy(c, "bf16", (0.2, 0.3), 0.0, got, db=True)
+    again = policy_call(c, "bf16", (0.2, 0.3), 0.0, want_db=True, chunk=256)
+    import torch
+    assert all(torch.equal(got[k], again[k]) for k in ("dH", "dW", "db"))
 
 
 @pytest.mark.parametrize("drop", ["old", "ref", "w", "old ref w", "clip"])
