@@ -724,12 +724,11 @@ static int dh_xcd_rows(int M, int D) {
   return best;
 }
 
-template <class G, int OCC, bool DM = false>
+template <class G, int OCC>
 __global__ void __launch_bounds__(G::kThreads, OCC)
 dh_gemm_bf16(const uint16_t* __restrict__ dZ, int M, int chunk, const uint16_t* __restrict__ W, int D, int c0, int cw,
              int slice, float* __restrict__ part, int gm, int accumulate, const int32_t* __restrict__ kdev,
-             const float* __restrict__ rowscale, const int32_t* __restrict__ Mdev) {
-  if constexpr (DM) M = min(M, *Mdev);
+             const float* __restrict__ rowscale) {
   // the first chunk writes its slices; later chunks (and an accumulating call) add to them
   const bool first = c0 == 0 && !accumulate;
   if (kdev) cw = min(cw, 2 * *kdev);  // union columns: [hi | lo] of the K classes the device found
@@ -738,9 +737,7 @@ dh_gemm_bf16(const uint16_t* __restrict__ dZ, int M, int chunk, const uint16_t* 
   const int nDt = (D + TC - 1) / TC;
   // Each XCD (a contiguous run of work ids) takes one block of a gm x (8 / gm) partition of
   // the frame x d tile grid: it reads dZ rows of its frame block and W columns of its d block
-  const int works = DM ? nMt * nDt * ((cw + slice - 1) / slice) : gridDim.x;
-  if (DM && static_cast<int>(blockIdx.x) >= works) return;
-  const int work = xcd_swz(blockIdx.x, works);
+  const int work = xcd_swz(blockIdx.x, gridDim.x);
   const int s = work / (nMt * nDt);
   int mt, dt;
   block_tile(work % (nMt * nDt), nMt, nDt, gm, mt, dt);
@@ -1101,7 +1098,7 @@ hipError_t launch_union_part_bf16(const float* G, int ldG, const int32_t* Kdev, 
       const int tiles = ((M + GUh::kBR - 1) / GUh::kBR) * ((D + GUh::kBC - 1) / GUh::kBC);
       Prof pr("union_dh", stream);
       hipLaunchKernelGGL((dh_gemm_bf16<GUh, 2>), dim3(tiles), dim3(GUh::kThreads), 0, stream, Gb, M, k2, WU2, D, 0,
-                         k2, k2, dH, dh_xcd_rows(M, D), 0, Kdev, nullptr, nullptr);
+                         k2, k2, dH, dh_xcd_rows(M, D), 0, Kdev, nullptr);
     }
   }
   if (want_dW && !dw_elsewhere) {
@@ -1129,7 +1126,7 @@ hipError_t launch_union_dh_bf16(const uint16_t* Gb, const int32_t* Kdev, int K_m
   const int tiles = ((M + GUh::kBR - 1) / GUh::kBR) * ((D + GUh::kBC - 1) / GUh::kBC);
   Prof pr("union_dh", stream);
   hipLaunchKernelGGL((dh_gemm_bf16<GUh, 2>), dim3(tiles), dim3(GUh::kThreads), 0, stream, Gb, M, k2, WU2, D, 0, k2,
-                     k2, dH, dh_xcd_rows(M, D), 1, Kdev, nullptr, nullptr);
+                     k2, dH, dh_xcd_rows(M, D), 1, Kdev, nullptr);
   return hipGetLastError();
 }
 
@@ -1388,7 +1385,7 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
                                  int slice, bool recompute, bool want_dH, bool want_dW, float* dW, float* db,
                                  float* dbpart, hipStream_t stream, const DwExtra* extra, const ChunkE* ce,
                                  const uint16_t* Hst, int Mp, const int32_t* Mdev) {
-  if (Mdev && want_dW) return hipErrorInvalidValue;  // (dW's kernel takes M rows)
+  if (Mdev && (want_dH || want_dW)) return hipErrorInvalidValue;  // (their kernels take M rows)
   // wide heads: one 8-wave 256 x 256 workgroup per CU (the long k loop hides the epilogue);
   // narrow heads: two 4-wave 256 x 128 workgroups per CU, so that one's epilogue (exp, pack,
   // staged stores: VALU-bound) overlaps the other's products
@@ -1446,10 +1443,8 @@ hipError_t launch_bwd_chunk_bf16(const uint16_t* Hs, int M, int D, const uint16_
     const int tiles = ((M + kBR - 1) / kBR) * ((D + kBC - 1) / kBC);
     const int ns = (cw + slice - 1) / slice;
     Prof pr("dh_gemm", stream);
-    rows_from(Mdev, [&](auto dm) {
-      hipLaunchKernelGGL((dh_gemm_bf16<GDh, 1, dm>), dim3(tiles * ns), dim3(GDh::kThreads), 0, stream, dZ, M, chunk, W,
-                         D, c0, cw, slice, part, dh_xcd_rows(M, D), 0, nullptr, ce ? ce->rowscale : nullptr, Mdev);
-    });
+    hipLaunchKernelGGL((dh_gemm_bf16<GDh, 1>), dim3(tiles * ns), dim3(GDh::kThreads), 0, stream, dZ, M, chunk, W, D,
+                       c0, cw, slice, part, dh_xcd_rows(M, D), 0, nullptr, ce ? ce->rowscale : nullptr);
   }
   if (want_dW) {
     const int nDt = (D + kBC - 1) / kBC;

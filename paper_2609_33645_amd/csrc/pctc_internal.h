@@ -203,8 +203,8 @@ hipError_t head_bwd_f32(const float* H, int M, int D, const float* W, const floa
                         char* scratch, const BwdPlan& plan, hipStream_t stream, const DzTokens* tokens = nullptr);
 
 // ---- bf16 kernels on the direct-to-LDS engine (head_gemm_bf16.hip) ---------------------
-// Mdev (null: M) of the normaliser and the backward's chunks: how many of the M rows there are, on the device;
-// the pitches of the partial pairs and of dH's slices are then that number's.
+// Mdev (null: M) of the normaliser and of a chunk's recompute: how many of the M rows there are, on the device; the
+// pitch of the partial pairs is then that number's.
 hipError_t launch_lse_partial_bf16(const uint16_t* H, int M, int D, const uint16_t* W, const float* bias, int V,
                                    float2* partials, int* P_out, hipStream_t stream, bool any_m = false,
                                    const int32_t* Mdev = nullptr);

@@ -291,6 +291,8 @@ dz_tokens(void* __restrict__ dZ, int pitch, int M, int c0, int cw, DzTokens t, f
   }
   const int m = blockIdx.x * kThreads + threadIdx.x;
   if (m >= M) return;
+  if constexpr (BF)  // the columns that dH's 16-byte pieces hold past the last class (exp(-lambda) may be infinite)
+    for (int v = cw; v < (cw + 7) / 8 * 8; ++v) static_cast<uint16_t*>(dZ)[static_cast<int64_t>(m) * pitch + v] = 0;
   const int v = t.token[m] - c0;
   const float g = t.g[m];
   if (v < 0 || v >= cw || g == 0.f) return;
@@ -379,6 +381,62 @@ dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, int D, cons
   *reinterpret_cast<u32x2*>(dH + i) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
 }
 
+#define PCTC_POLICY_STAGES(G)                                            \
+  __shared__ __attribute__((aligned(1024))) char st0[G::kStageBytes];    \
+  __shared__ __attribute__((aligned(1024))) char st1[G::kStageBytes];    \
+  __shared__ __attribute__((aligned(1024))) char st2[G::kStageBytes];    \
+  __shared__ __attribute__((aligned(1024))) char st3[G::kStageBytes];    \
+  char* const st[4] = {st0, st1, st2, st3};
+
+// A chunk's share of dH by slices of `slice` of its columns: part[slice][frame][D], written by the first chunk (add
+// false), added to by the others.  Tiles of 256 values of a row x 256 frames, which leave in lines: 331 frames, D =
+// 512, 5,000 columns 18 us, where the fused call's kernel, whose tiles lie the other way and leave by single values,
+// takes 31; large products are the same (1,925 frames, D = 4,096, 50,688 columns 636 and 641).
+__global__ void __launch_bounds__(512, 1)
+policy_dh(const uint16_t* __restrict__ dZ, int pitch, int M, const uint16_t* __restrict__ W, int D, int cw, int slice,
+          bool add, float* __restrict__ part, const int32_t* __restrict__ Mdev) {
+  using G = bf::Gemm<256, 256, 32, bf::LL::MC, bf::LL::KC, 4, 2, 4, true>;
+  PCTC_POLICY_STAGES(G)
+  M = min(M, *Mdev);
+  const int nM = (M + 255) / 256, nD = (D + 255) / 256;
+  const int works = nM * nD * gridDim.y;
+  const int id = blockIdx.y * gridDim.x + blockIdx.x;
+  if (id >= works) return;
+  const int w = xcd_swz(id, works);
+  const int s = w / (nM * nD), rest = w % (nM * nD);
+  const int d0 = (nD <= nM ? rest % nD : rest / nM) * 256, m0 = (nD <= nM ? rest / nD : rest % nM) * 256;
+  const int kb = s * slice, ke = min(cw, kb + slice);
+  if (add && kb >= ke) return;
+  const bf::GOp A{W, D, D, cw, nullptr}, B{dZ, pitch, M, cw, nullptr};
+  f32x16 acc[G::FR][G::FC];
+  G::run_pp(A, B, d0, m0, kb, ke, st, acc);
+  const int wave = threadIdx.x >> 6;
+  const int dw = d0 + wave / 4 * 128, mw = m0 + wave % 4 * 64;
+  float* const out = part + static_cast<int64_t>(s) * M * D;
+  struct __attribute__((aligned(16))) Eight {
+    float4 a, b;
+  };
+  auto place = [&](int block, int col) {
+    const int d = dw + block * 8, m = mw + col;
+    return d < D && m < M ? static_cast<int64_t>(m) * D + d : int64_t{-1};
+  };
+  by_columns<G, Eight>(
+      acc, st,
+      [&](int block, int col, const float (&v)[8], const Eight& x) {
+        const int64_t at = place(block, col);
+        if (at < 0) return;
+        float4* const o = reinterpret_cast<float4*>(out + at);
+        o[0] = make_float4(v[0] + x.a.x, v[1] + x.a.y, v[2] + x.a.z, v[3] + x.a.w);
+        o[1] = make_float4(v[4] + x.b.x, v[5] + x.b.y, v[6] + x.b.z, v[7] + x.b.w);
+      },
+      [&](int block, int col, Eight& x) {
+        const int64_t at = place(block, col);
+        x = Eight{make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+        if (add)  // (places outside read the first: no branch between the reads)
+          x = *reinterpret_cast<const Eight*>(out + (at < 0 ? 0 : at));
+      });
+}
+
 // dW of a bf16 chunk: tiles of 256 values of a row x 256 classes, so that the accumulators leave in lines, each
 // class with what the rounding took off its tokens' own entries times their rows of H, before its one rounding
 // to bf16 (0.0023 -> 0.0017 of dW's norm; of few rows one rounding may be most of the error: 40 rows of 100
@@ -387,11 +445,7 @@ __global__ void __launch_bounds__(512, 1)
 policy_dw(const uint16_t* __restrict__ dZ, int pitch, int M, const uint16_t* __restrict__ H, int D, int c0, int cw,
           uint16_t* __restrict__ dW, DzTokens t) {
   using G = bf::Gemm<256, 256, 32, bf::LL::MC, bf::LL::MC, 4, 2, 4, true>;
-  __shared__ __attribute__((aligned(1024))) char st0[G::kStageBytes];
-  __shared__ __attribute__((aligned(1024))) char st1[G::kStageBytes];
-  __shared__ __attribute__((aligned(1024))) char st2[G::kStageBytes];
-  __shared__ __attribute__((aligned(1024))) char st3[G::kStageBytes];
-  char* const st[4] = {st0, st1, st2, st3};
+  PCTC_POLICY_STAGES(G)
   M = min(M, *t.Mdev);  // (with none, zeros are written)
   const int nDt = (D + 255) / 256;
   const int w = xcd_swz(blockIdx.x, gridDim.x);
@@ -513,10 +567,12 @@ static hipError_t policy_bwd_bf16(uint16_t* Hc, int M, int D, const uint16_t* W,
       hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart, c0, tokens);
       hipLaunchKernelGGL(db_join, dim3(tiles), dim3(kThreads), 0, stream, dbpart, slices, chunk, cw, db + c0);
     }
-    e = launch_bwd_chunk_bf16(Hc, M, D, W, bias, c0, cw, lam2, nullptr, 0, tokens.g, nullptr, nullptr, 0, dZ, chunk, part,
-                              sl, false, dH != nullptr, false, nullptr, nullptr, nullptr, stream, nullptr, nullptr, Hst,
-                              plan.Mp, tokens.Mdev);
-    if (e != hipSuccess) return e;
+    if (dH) {
+      Prof pr("dh_gemm", stream);
+      const dim3 grid((M + 255) / 256 * ((D + 255) / 256), (cw + sl - 1) / sl);
+      hipLaunchKernelGGL(policy_dh, grid, dim3(512), 0, stream, dZ, chunk, M, W + static_cast<int64_t>(c0) * D, D, cw, sl,
+                         c0 > 0, part, tokens.Mdev);
+    }
     if (dW) {
       Prof pr("dw_gemm", stream);
       const dim3 grid((cw + 255) / 256 * ((D + 255) / 256));

@@ -366,6 +366,19 @@ def test_policy_loss_of_few_tokens_a_class(M, D, V, chunk, bias):
     check_policy(c, "bf16", (0.2, 0.3), 0.07, got, db=True, own_rounded=False)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shift", [-300.0, 250.0])
+@pytest.mark.parametrize("V", [301, 304])
+def test_policy_loss_of_logits_far_from_zero(dtype, shift, V):
+    """A bias that all classes share changes nothing, also where exp(-lambda) is infinite or zero and the last
+    class ends inside a piece of 16 bytes."""
+    say("policy_loss far from zero", dtype, shift, V)
+    c = policy_case(V, 60, 64, V, dtype, True)
+    c["bias"] = (c["bias"] + np.float32(shift)).astype(np.float32)
+    got = policy_call(c, dtype, (0.2, 0.3), 0.07, want_db=True)
+    check_policy(c, dtype, (0.2, 0.3), 0.07, got, db=True)
+
+
 @pytest.mark.parametrize("M,V,classes", [(700, 300, 1), (900, 300, 2), (700, 600, 30), (1500, 130, 130), (2100, 256, 64)])
 def test_policy_loss_of_many_tokens_a_class(M, V, classes):
     """More tokens of a class than are made good one by one, and more than a wavefront goes through."""
