@@ -10,7 +10,7 @@
 // number, which only the device knows.  Between the products: the tokens' normalisers, logits and losses (a
 // wavefront a token), and in every chunk of the backward the tokens' own entries of dZ, the sum of the
 // losses beside the first.  Bound by the matrix products, 8 M V D operations (the logits are formed twice).
-#include "gemm_bf16.h"
+#include "gemm_f32.h"
 #include "head_tiles.h"
 #include "pctc_internal.h"
 
@@ -123,16 +123,96 @@ struct PolicyRows {
   float* logp;
 };
 
+// A logit as the normaliser's products give it, to the bit: the same matrix instructions over the same k, for 32
+// rows of H and of W at once, of whose 32 x 32 products the diagonal is wanted.  h, w: this lane's rows (lane mod 32);
+// start: the bias of the class (in bf16 the sums start from it, in float it is added).  Lanes whose half does not hold
+// their column's return another.
+template <bool BF>
+__device__ __forceinline__ float tile_logit(const void* h, const void* w, float start, int D, int lane) {
+  f32x16 acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = BF ? start : 0.f;
+  const int ko = 8 * (lane >> 5);
+  if constexpr (BF) {
+    constexpr int U = 8;
+    const uint16_t *a = static_cast<const uint16_t*>(w) + ko, *b = static_cast<const uint16_t*>(h) + ko;
+    for (int k0 = 0; k0 < D; k0 += 16 * U) {
+      u32x4 x[U], y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = k0 + 16 * u + ko < D;
+        x[u] = in ? *reinterpret_cast<const u32x4*>(a + k0 + 16 * u) : u32x4{0u, 0u, 0u, 0u};
+        y[u] = in ? *reinterpret_cast<const u32x4*>(b + k0 + 16 * u) : u32x4{0u, 0u, 0u, 0u};
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[u]), __builtin_bit_cast(bf16x8, y[u]), acc, 0, 0, 0);
+    }
+  } else {
+    constexpr int U = 4;
+    const float *a = static_cast<const float*>(w) + ko, *b = static_cast<const float*>(h) + ko;
+    for (int k0 = 0; k0 < D; k0 += 16 * U) {
+      f3::f32x4 x[U][2], y[U][2];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = k0 + 16 * u + ko < D;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          x[u][e] = in ? *reinterpret_cast<const f3::f32x4*>(a + k0 + 16 * u + 4 * e) : f3::f32x4{0.f, 0.f, 0.f, 0.f};
+          y[u][e] = in ? *reinterpret_cast<const f3::f32x4*>(b + k0 + 16 * u + 4 * e) : f3::f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        f3::Tri p, q;
+        f3::split4<0>(x[u][0], p);
+        f3::split4<1>(x[u][1], p);
+        f3::split4<0>(y[u][0], q);
+        f3::split4<1>(y[u][1], q);
+#pragma unroll
+        for (int i = 2; i >= 0; --i)
+#pragma unroll
+          for (int e = i; e >= 0; --e) {
+            bf16x8 f, g;
+            __builtin_memcpy(&f, p.d[e], 16);
+            __builtin_memcpy(&g, q.d[i - e], 16);
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, g, acc, 0, 0, 0);
+          }
+      }
+    }
+  }
+  const int c = lane & 31, at = 4 * (c >> 3) + (c & 3);
+  float z = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z = r == at ? acc[r] : z;
+  return BF ? z : z + start;
+}
+
 // A wavefront a place, 16 of them a workgroup (so that the lines of the partial pairs, 16 places each, are
 // read once).  lambda in double from the pairs; the token's logit from two rows of D values, lanes' float
-// sums joined in double; the loss in double.  mask (null: none): a row without a gradient is cleared there,
-// so that what is not finite in it reaches no product.
+// sums joined in double; the loss in double.  The normaliser's products round that logit otherwise; lambda is
+// corrected by what the difference makes of the token's own share of it (tile_logit), so that the log probability of a
+// nearly certain token is right.  mask (null: none): a row without a gradient is cleared there, so that what is
+// not finite in it reaches no product.
 template <bool BF>
 __global__ void __launch_bounds__(kLossThreads)
 policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const float* __restrict__ bias, int V,
               PolicyRows R, PolicyArgs a, uint16_t* mask) {
   const int n = R.count ? min(M, *R.count) : M;
-  const int j = blockIdx.x * (kLossThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  constexpr int kPlaces = kLossThreads / 64;
+  const int j0 = blockIdx.x * kPlaces, j = j0 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (j0 >= n) return;
+  constexpr int kBytes = BF ? 2 : 4;
+  __shared__ float tile[kPlaces];
+  if (threadIdx.x < 64) {
+    const int c = lane & 31, q = min(j0 + (c & (kPlaces - 1)), n - 1);
+    const int t0 = a.tokens[R.rows ? R.rows[q] : q], t = t0 >= 0 && t0 < V ? t0 : 0;
+    const float z = tile_logit<BF>(static_cast<const char*>(H) + static_cast<int64_t>(q) * D * kBytes,
+                                   static_cast<const char*>(W) + static_cast<int64_t>(t) * D * kBytes, bias ? bias[t] : 0.f, D,
+                                   lane);
+    if (c < kPlaces && (lane >> 5) == ((c >> 2) & 1)) tile[c] = z;
+  }
+  __syncthreads();
   if (j >= n) return;
   // lambda: the largest maximum is exact, each sum is scaled by the float exponential of an exact difference
   constexpr int kPer = kMaxLseParts / 64;
@@ -161,7 +241,6 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
   const int m = R.rows ? R.rows[j] : j;
   const int tok = a.tokens[m];
   const bool counted = tok >= 0 && tok < V;
-  constexpr int kBytes = BF ? 2 : 4;
   const char* const row = static_cast<const char*>(H) + static_cast<int64_t>(j) * D * kBytes;
   double z = 0.0;
   if (counted) {
@@ -173,6 +252,8 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
   int status = 1;  // left out
   if (counted) {
     if (bias) z += static_cast<double>(bias[tok]);
+    const double zt = tile[threadIdx.x >> 6], off = z - zt;
+    if (fabs(off) < 1.0 && lam - lam == 0.0) lam += log1p(exp(zt - lam) * expm1(off));
     const double lp = z - lam;
     const double A = a.adv[m], w = a.weights ? static_cast<double>(a.weights[m]) : 1.0;
     double loss = 0.0, c = 0.0;
