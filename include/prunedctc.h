@@ -492,8 +492,8 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
  *                                                                PCTC_GELU a (1 + erf(a / sqrt 2)) / 2
  *   x [M, D], w_gate and w_up [F, D], w_down [O, F], y [M, O], all device, dtype, 16-byte aligned.  M >= 0;
  *   D, F and O positive multiples of 8, at most PCTC_MAX_DIM.  Products are summed in float; h (and in the
- *   backward dh b act'(a) and dh act(a)) is rounded to dtype as an operand of the next product, and every
- *   output once.
+ *   backward dh b act'(a) and dh act(a)) is rounded to dtype as an operand of the next product (in the forward of up
+ *   to 8 rows carried on in two parts), and every output once.
  *   gate, up: device float [M, F], a and b, kept for the backward; both NULL or neither.
  * pctc_gated_ffn_backward: from dy [M, O] and the forward's x, gate and up the gradients dx [M, D], dw_gate and
  *   dw_up [F, D] (both or neither) and dw_down [O, F]; those that are NULL are not formed.

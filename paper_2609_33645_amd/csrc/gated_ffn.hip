@@ -31,6 +31,7 @@ namespace {
 using bf::LL;
 
 constexpr int kFew = 512;  // most rows of x that the forward takes without tiles
+constexpr int kLoRows = 8;  // most rows whose h is kept in two parts
 constexpr int kT = 256;  // tile rows and columns
 constexpr int kWc = 4;   // wavefronts across a tile's columns (two across its rows)
 
@@ -173,14 +174,19 @@ __device__ __forceinline__ void load8(const typename E::T* p, float (&v)[8]) {
 // rows of x.  A workgroup takes 16 RB rows of the weights and 16 NT of x, its wavefronts a share of k each, and
 // adds the shares up in order through LDS.  Weights and rows go from memory to the matrix instructions' registers
 // (16 x 16, 16 bytes a lane: 64 bytes of each of 16 rows an instruction) without LDS: every weight is used by
-// one wavefront only, and what bounds the kernel is reading the weights (from 32 rows on, those and x from the caches).  Rows past R or M repeat the
-// last one; what they give is not written.
+// one wavefront only, and what bounds the kernel is reading the weights (from 32 rows on, those and x from the caches).
+// Rows past R or M repeat the last one; what they give is not written.  LO (bf16, at most 8 rows): h in two parts, the
+// second what the rounding of the first leaves, which takes the columns of the matrix instruction that 8 rows leave
+// free: y is off by its own rounding alone (0.0024 -> 0.0017 of its norm), for nothing (one row of 4,096 x 10,240; as
+// rows and instructions of their own, 52 -> 56 us).
 template <class E>
 struct FewArgs {
   const typename E::T *x, *w0, *w1;
   typename E::T* out;
   float *a, *b;  // null: not kept
   int M, K, R;
+  const typename E::T* xlo = nullptr;  // LO: what the rounding of x left
+  typename E::T* lo = nullptr;         // LO: what the rounding of h leaves
 };
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
@@ -195,7 +201,7 @@ __device__ __forceinline__ void few_step(const u32x4& w, const u32x4& x, f32x4& 
   }
 }
 
-template <class E, int MATS, int RB, int NT, int KS, int ACT>
+template <class E, int MATS, int RB, int NT, int KS, int ACT, bool LO = false>
 __global__ void __launch_bounds__(KS * 64) ffn_few(FewArgs<E> P) {
   using T = typename E::T;
   constexpr int kPer = E::kBf ? 8 : 4, kStep = 4 * kPer;  // values of a lane, k of a step
@@ -215,6 +221,9 @@ __global__ void __launch_bounds__(KS * 64) ffn_few(FewArgs<E> P) {
   const T* x[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) x[n] = P.x + static_cast<int64_t>(min(m0 + 16 * n + (lane & 15), P.M - 1)) * P.K + ko;
+  constexpr bool kLoX = LO && MATS == 1;
+  if constexpr (kLoX)
+    x[0] = ((lane & 8) ? P.xlo : P.x) + static_cast<int64_t>(min(lane & 7, P.M - 1)) * P.K + ko;
   f32x4 acc[MATS][RB][NT];
 #pragma unroll
   for (int q = 0; q < MATS; ++q)
@@ -304,6 +313,11 @@ __global__ void __launch_bounds__(KS * 64) ffn_few(FewArgs<E> P) {
         const f32x4 s = sum[g][(q * RB + b) * NT + n][l];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[q][e] += s[e];
+        if constexpr (kLoX) {
+          const f32x4 t = sum[g][(q * RB + b) * NT + n][l + 8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[q][e] += t[e];
+        }
       }
     const int64_t at = static_cast<int64_t>(m) * P.R + r;
     if constexpr (MATS == 2) {
@@ -311,6 +325,11 @@ __global__ void __launch_bounds__(KS * 64) ffn_few(FewArgs<E> P) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) h[e] = act<ACT>(v[0][e]) * v[1][e];
       store4<E>(P.out + at, h);
+      if constexpr (LO) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] -= bf16_to_f32(f32_to_bf16(h[e]));
+        store4<E>(P.lo + at, h);
+      }
       if (P.a) {
         store4<F32>(P.a + at, v[0]);
         store4<F32>(P.b + at, v[1]);
@@ -339,6 +358,12 @@ void launch_few(const FewArgs<E>& P, hipStream_t stream) {
     if (least < 0 || read < least) {
       least = read;
       best = c;
+    }
+  }
+  if constexpr (E::kBf) {
+    if (P.xlo || P.lo) {  // (at most kLoRows rows)
+      hipLaunchKernelGGL((ffn_few<E, MATS, 1, 1, 8, ACT, true>), dim3((P.R + 15) / 16), dim3(512), 0, stream, P);
+      return;
     }
   }
 #define PCTC_FEW(C, RB, NT, KS)                                                                                     \
@@ -743,6 +768,12 @@ Products grad_products(const FfnArgs& q, const FfnGrads& g, const void* da, cons
   return Q;
 }
 
+// h in two parts: for the rows that the matrix instruction holds twice, if both products go without tiles.
+bool two_parts(const FfnArgs& q, bool bf) {
+  Products Q;
+  return bf && q.M <= kLoRows && pair_plan(q, bf, Q) == Pair::kFew && down_by_few(q, bf);
+}
+
 template <class E>
 hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
   using T = typename E::T;
@@ -750,11 +781,13 @@ hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
   float *const a = q.a, *const b = q.b;
   const T *const x = static_cast<const T*>(q.x), *const wg = static_cast<const T*>(q.wg), *const wu = static_cast<const T*>(q.wu);
   const bool silu = q.act == kSilu;
+  T* const lo = two_parts(q, E::kBf) ? reinterpret_cast<T*>(part) : nullptr;
   auto few = [&](int m0, int rows) {
     Prof pr("ffn_few", stream);
     const int64_t at = static_cast<int64_t>(m0) * q.F;
-    const FewArgs<E> f{x + static_cast<int64_t>(m0) * q.D, wg, wu, hh + at, a ? a + at : nullptr, b ? b + at : nullptr,
-                       rows, q.D, q.F};
+    FewArgs<E> f{x + static_cast<int64_t>(m0) * q.D, wg, wu, hh + at, a ? a + at : nullptr, b ? b + at : nullptr,
+                 rows, q.D, q.F};
+    f.lo = lo;
     if (silu) launch_few<E, 2, kSilu>(f, stream);
     else launch_few<E, 2, kGelu>(f, stream);
   };
@@ -781,7 +814,8 @@ hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
   }
   if (down_by_few(q, E::kBf)) {
     Prof pr("ffn_few", stream);
-    const FewArgs<E> d{hh, static_cast<const T*>(q.wd), nullptr, static_cast<T*>(q.y), nullptr, nullptr, q.M, q.F, q.O};
+    FewArgs<E> d{hh, static_cast<const T*>(q.wd), nullptr, static_cast<T*>(q.y), nullptr, nullptr, q.M, q.F, q.O};
+    d.xlo = lo;
     launch_few<E, 1, kSilu>(d, stream);
     return hipGetLastError();
   }
@@ -832,6 +866,7 @@ size_t ffn_workspace_bytes(int dtype, const FfnArgs& q, bool back) {
   Products Q;
   size_t part = 0;  // of one step at a time
   if (!back) {
+    if (two_parts(q, bf)) return 2 * n;
     if (pair_plan(q, bf, Q) == Pair::kSliced) part = place_parts(Q, nullptr, true);
     if (!down_by_few(q, bf)) {
       Q = down_products(q, nullptr, bf);
