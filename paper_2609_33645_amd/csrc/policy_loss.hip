@@ -19,7 +19,7 @@ namespace pctc {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kLossThreads = 1024;
+constexpr int kLossThreads = 512;
 
 // Sum of products of this lane's pieces of two rows of D values (a multiple of 8), 16 bytes at a time.
 template <bool BF>
@@ -134,7 +134,7 @@ __device__ __forceinline__ float tile_logit(const void* h, const void* w, float 
   for (int r = 0; r < 16; ++r) acc[r] = BF ? start : 0.f;
   const int ko = 8 * (lane >> 5);
   if constexpr (BF) {
-    constexpr int U = 8;
+    constexpr int U = 16;
     const uint16_t *a = static_cast<const uint16_t*>(w) + ko, *b = static_cast<const uint16_t*>(h) + ko;
     for (int k0 = 0; k0 < D; k0 += 16 * U) {
       u32x4 x[U], y[U];
@@ -151,24 +151,26 @@ __device__ __forceinline__ float tile_logit(const void* h, const void* w, float 
   } else {
     constexpr int U = 4;
     const float *a = static_cast<const float*>(w) + ko, *b = static_cast<const float*>(h) + ko;
-    for (int k0 = 0; k0 < D; k0 += 16 * U) {
-      f3::f32x4 x[U][2], y[U][2];
+    f3::f32x4 x[2][U][2], y[2][U][2];
+    auto read = [&](int s, int k0) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const bool in = k0 + 16 * u + ko < D;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          x[u][e] = in ? *reinterpret_cast<const f3::f32x4*>(a + k0 + 16 * u + 4 * e) : f3::f32x4{0.f, 0.f, 0.f, 0.f};
-          y[u][e] = in ? *reinterpret_cast<const f3::f32x4*>(b + k0 + 16 * u + 4 * e) : f3::f32x4{0.f, 0.f, 0.f, 0.f};
+          x[s][u][e] = in ? *reinterpret_cast<const f3::f32x4*>(a + k0 + 16 * u + 4 * e) : f3::f32x4{0.f, 0.f, 0.f, 0.f};
+          y[s][u][e] = in ? *reinterpret_cast<const f3::f32x4*>(b + k0 + 16 * u + 4 * e) : f3::f32x4{0.f, 0.f, 0.f, 0.f};
         }
       }
+    };
+    auto use = [&](int s) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         f3::Tri p, q;
-        f3::split4<0>(x[u][0], p);
-        f3::split4<1>(x[u][1], p);
-        f3::split4<0>(y[u][0], q);
-        f3::split4<1>(y[u][1], q);
+        f3::split4<0>(x[s][u][0], p);
+        f3::split4<1>(x[s][u][1], p);
+        f3::split4<0>(y[s][u][0], q);
+        f3::split4<1>(y[s][u][1], q);
 #pragma unroll
         for (int i = 2; i >= 0; --i)
 #pragma unroll
@@ -179,6 +181,13 @@ __device__ __forceinline__ float tile_logit(const void* h, const void* w, float 
             acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, g, acc, 0, 0, 0);
           }
       }
+    };
+    read(0, 0);
+    for (int k0 = 0; k0 < D; k0 += 32 * U) {  // (k past D: zeros, which change nothing)
+      read(1, k0 + 16 * U);
+      use(0);
+      read(0, k0 + 32 * U);
+      use(1);
     }
   }
   const int c = lane & 31, at = 4 * (c >> 3) + (c & 3);
@@ -188,8 +197,7 @@ __device__ __forceinline__ float tile_logit(const void* h, const void* w, float 
   return BF ? z : z + start;
 }
 
-// A wavefront a place, 16 of them a workgroup (so that the lines of the partial pairs, 16 places each, are
-// read once).  lambda in double from the pairs; the token's logit from two rows of D values, lanes' float
+// A wavefront a place, eight of them a workgroup.  lambda in double from the pairs; the token's logit from two rows of D values, lanes' float
 // sums joined in double; the loss in double.  The normaliser's products round that logit otherwise; lambda is
 // corrected by what the difference makes of the token's own share of it (tile_logit), so that the log probability of a
 // nearly certain token is right.  mask (null: none): a row without a gradient is cleared there, so that what is
