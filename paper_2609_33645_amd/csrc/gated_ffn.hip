@@ -604,7 +604,8 @@ int tiles(int n, int t = kT) { return (n + t - 1) / t; }
 // Slices.  A launch on 256 compute units takes at most whole rounds of its longest workgroup, and of workgroups
 // of several lengths, longest first, about the work of one unit and half the shortest; a k-step (32 deep in
 // bf16, 16 in float) takes 0.95 or 1.6 us, a workgroup 6 us more, sliced sums cost 5 us and their bytes at 3 TB/s
-// (written beside products, read again from the caches), within kPartBytes.  Tried are the depths that cut the longest product into 1 to 16.
+// (written beside products, read again from the caches), within kPartBytes.  Tried are the depths that cut the
+// longest product into 1 to 16.
 constexpr size_t kPartBytes = size_t{128} << 20;
 double step_us(bool bf) { return bf ? 0.95 / 32 : 1.6 / 16; }  // per k
 // Returns the time by this model.  always_joined: one slice is joined too.
