@@ -1204,7 +1204,8 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up
 
 
 class Dropout(torch.autograd.Function):
-    """Autograd wrapper of dropout().  The mask is made again in the backward, from the counters of the forward (a
+    """Autograd wrapper of dropout().  (For a backward that is captured into a graph, here as for any operator: no
+    graph recorded outside the capture may still hold the same leaves.)  The mask is made again in the backward, from the counters of the forward (a
     device tensor's value is copied: the caller may move it on before)."""
 
     @staticmethod
