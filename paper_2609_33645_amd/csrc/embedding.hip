@@ -282,10 +282,10 @@ radix_place(SortPass P) {
       P.keys_out[to] = key;
       P.perm_out[to] = from;
       // the last lane of a digit moves its counter on, once every lane has read it
-      __builtin_amdgcn_wave_barrier();
+      wave_exchange();
       if ((same >> lane) == 1) at[wave][digit] = to + 1;
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_exchange();  // before the next 64 read it
   }
 }
 

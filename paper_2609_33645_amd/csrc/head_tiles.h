@@ -338,7 +338,7 @@ __device__ __forceinline__ void amax_store_partials(float (&bv)[G::FC], int (&bi
 // fn(block, col, v, x): tile rows 8 block .. 8 block + 7 of the wavefront's 128, column col of its 64; x is what
 // pre(block, col, x) read for these places, for 32 columns before any of them is used, so that many
 // reads are in flight (there is one workgroup on a compute unit, whose products are over).
-// A wavefront's LDS accesses are ordered; no barrier is needed.
+// The 16 KB are one wavefront's: its exchanges need no barrier of the workgroup.
 struct Nothing {};
 template <class G, class X = Nothing, class Fn, class Pre>
 __device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* const (&st)[4], Fn&& fn, Pre&& pre) {
@@ -352,6 +352,7 @@ __device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* co
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int c = lane & 31;
+    wave_exchange();  // (the columns before have been read)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -360,6 +361,7 @@ __device__ __forceinline__ void by_columns(f32x16 (&acc)[G::FR][G::FC], char* co
         *reinterpret_cast<float4*>(base + c * 512 + ((slot ^ (c & 31)) << 4)) =
             make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
       }
+    wave_exchange();
     const int block = lane & 15;
 #pragma unroll
     for (int t0 = 0; t0 < 8; t0 += NB) {

@@ -39,6 +39,14 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float fast_log2(float x) { return __builtin_amdgcn_logf(x); }
 
+// What a lane wrote to the LDS before is there for the wavefront's other lanes after: its LDS operations run in program
+// order, and the fence keeps the compiler from reordering them or from taking a lane's own value for what it
+// reads.  No instruction of its own.
+__device__ __forceinline__ void wave_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Value of lane (l ^ 32): the other half of the wavefront.
 __device__ __forceinline__ float swap_halves(float x) {
   return __shfl_xor(x, 32, 64);
