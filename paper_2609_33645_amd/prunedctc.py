@@ -1026,10 +1026,11 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
 # ---- below the head ----------------------------------------------------------------------
 
 def _out(out: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.Tensor, what: str = "out") -> torch.Tensor:
-    """A new tensor, or the caller's, which must be one of that shape (on the device of `like`)."""
+    """A new contiguous tensor, or the caller's, which must be one of that shape (on the device of `like`)."""
     dev = like.device
-    if out is None:  # (half the time of torch.empty with a device)
-        return torch.empty_like(like) if shape == like.shape and dtype is like.dtype else like.new_empty(shape, dtype=dtype)
+    if out is None:  # (half the time of torch.empty with a device; empty_like keeps the strides of what is not contiguous)
+        same = shape == like.shape and dtype is like.dtype and like.is_contiguous()
+        return torch.empty_like(like) if same else like.new_empty(shape, dtype=dtype)
     if out.dtype is not dtype or tuple(out.shape) != tuple(shape) or out.device != dev or not out.is_contiguous():
         raise PrunedCTCError(-1, f"{what} must be contiguous {dtype} {tuple(shape)} on {dev}")
     return out
@@ -1118,8 +1119,8 @@ def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, V: int, scale: fl
         raise PrunedCTCError(-1, f"unsupported dtype {kind}")
     if V < 1 or D < 1:
         raise PrunedCTCError(-1, "V and D must be positive")
-    dW = _out(out, (V, D), kind, dy)
     dy = dy.contiguous()
+    dW = _out(out, (V, D), kind, dy)
     L = lib()
     nbytes = L.pctc_embedding_backward_workspace_size(N, D)
     if nbytes == 0:

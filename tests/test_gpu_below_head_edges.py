@@ -44,3 +44,51 @@ def test_embedding_backward_of_whole_numbers(N, V):
         np.add.at(want, t[ok], dy[ok].astype(np.float64))
         got = pc.embedding_backward(dev(dy), torch.from_numpy(t).cuda(), V)
         assert np.array_equal(host(got), want)
+
+
+# ---- layouts -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,D", [(7, 5), (300, 40), (130, 1)])
+def test_embedding_backward_of_a_transposed_gradient_with_the_tables_shape(dtype, N, D):
+    """As many tokens as classes: a new dW has dy's shape, but not its strides."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("embedding_backward transposed", dtype, N, D)
+    r = np.random.default_rng(N)
+    t = r.integers(-1, N, size=N)
+    tokens = torch.from_numpy(t).cuda()
+    dy = dev(r.normal(size=(D, N)).astype(np.float32), dtype).T
+    got = pc.embedding_backward(dy, tokens, N, 0.7)
+    assert got.is_contiguous()
+    check_grad(dy, t, N, 0.7, got)
+    base = torch.randn(D, N, device="cuda").to(kind(dtype)).T.contiguous()
+    acc = pc.embedding_backward(dy, tokens, N, 0.7, out=base.clone(), accumulate=True)
+    check_grad(dy, t, N, 0.7, acc, host(base))
+    table = torch.randn(N, D, device="cuda").to(kind(dtype)).requires_grad_()
+    y = pc.embedding_layer(table, tokens, 0.7)
+    (grad,) = torch.autograd.grad(y.t(), [table], dy.T)
+    assert grad.is_contiguous() and torch.equal(grad, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_transposed_operands_whose_results_have_their_shape(dtype):
+    """The same of every other new result: dropout's, the lookup's, the block's and its gradients', the policy loss's."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("transposed operands", dtype)
+    n = 64
+    torch.manual_seed(2)
+    a, b, c, d, e = (torch.randn(n, n, device="cuda").to(kind(dtype)).T for _ in range(5))
+    t = torch.randperm(n, device="cuda")
+    adv = torch.randn(n, device="cuda")
+
+    def calls(a, b, c, d, e):
+        f = pc.gated_ffn(a, b, c, d, keep=True)
+        return [pc.dropout(a, 0.3, 1, residual=b), pc.embedding(a, t), f["y"], f["gate"], f["up"],
+                *pc.gated_ffn_backward(e, a, f["gate"].T.contiguous().T, f["up"], b, c, d).values(),
+                *pc.policy_loss(a, b, t, adv, want_db=True).values()]
+
+    got, want = calls(a, b, c, d, e), calls(*(x.contiguous() for x in (a, b, c, d, e)))
+    for i, (g, w) in enumerate(zip(got, want)):
+        assert g.is_contiguous() and torch.equal(g, w), i
