@@ -527,7 +527,7 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
  *   loss: device double [1]; losses, logp: device float [M]; status: device int32 [M]: PCTC_TOKEN_COUNTED;
  *   PCTC_TOKEN_LEFT_OUT, a token outside [0, V) (a prompt's place), logp 0; PCTC_TOKEN_NONFINITE, a loss or
  *   gradient factor that is not finite.  Rows that are not counted have losses 0 and take no part in loss
- *   or gradients (their dH rows are zero).
+ *   or gradients (their dH rows are zero), also where W or the bias is not finite.
  *   dH [M, D], dW [V, D], db [V]: of the dtype of H, rounded once from float sums; each may be NULL, and with all
  *   three NULL only the losses are formed.
  *   workspace: pctc_policy_workspace_size() bytes (bias, grads: whether the call has a bias, asks for a

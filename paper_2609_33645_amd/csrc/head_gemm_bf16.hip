@@ -66,6 +66,14 @@ constexpr int kRcStores = 16;  // buffer stores per wave per 256 x 256 tile (rec
 using GUh = bf::Gemm<256, 128, 32, LL::KC, LL::MC, 3, 2, 2>;
 using GDw = bf::Gemm<kBR, kBC, kBK, LL::MC, LL::MC, 4, 2, 4, true>;
 
+// Two values of -g p in bf16 with g's sign, `sg`.  DM: zeros for a frame with g = 0 (live 0) also where its logits are no
+// numbers, as a head that is not finite makes them (without DM such frames' products are finite).
+template <bool DM>
+__device__ __forceinline__ uint32_t signed_pair(float x, float y, uint32_t sg, uint32_t live) {
+  const uint32_t w = pack_bf16x2(x, y) ^ sg;
+  return DM ? w & live : w;
+}
+
 // Launches with the kernels' DM: whether the number of rows comes from the device (the calls that know it ask
 // nothing of memory and skip no workgroup).
 template <class F>
@@ -487,7 +495,7 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
   // the exponent offset ll takes g_m's magnitude (+inf on excluded frames, whose products
   // are finite: the values are zeros) and sg its sign, applied to a packed bf16 pair
   float ll[FC];
-  uint32_t sg[FC];
+  uint32_t sg[FC], live[FC];
 #pragma unroll
   for (int j = 0; j < FC; ++j) {
     const int m = m0 + GG::col_of(wave, lane, j);
@@ -495,6 +503,7 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
     const float2 l2 = (m < M) ? lam2[m] : make_float2(0.f, 0.f);
     ll[j] = (gm != 0.f) ? (l2.x + l2.y) - fast_log2(fabsf(gm)) : INFINITY;
     sg[j] = (gm > 0.f) ? 0x80008000u : 0u;
+    live[j] = (gm != 0.f) ? ~0u : 0u;
   }
   const GOp A{W + static_cast<int64_t>(c0) * D, D, cw, D, nullptr};
   const GOp B{Hs, D, M, D, nullptr};
@@ -528,7 +537,7 @@ recompute_dz_bf16(const uint16_t* __restrict__ Hs, int M, int D, const uint16_t*
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = fast_exp2(fmaf(acc[i][j][4 * q + e], kLog2e, -ll[j]));
         *reinterpret_cast<u32x2*>(stage + (lane & 31) * kPitch + rl0 * 2) =
-            u32x2{pack_bf16x2(v[0], v[1]) ^ sg[j], pack_bf16x2(v[2], v[3]) ^ sg[j]};
+            u32x2{signed_pair<DM>(v[0], v[1], sg[j], live[j]), signed_pair<DM>(v[2], v[3], sg[j], live[j])};
       }
     __syncthreads();
     if (nunion > 0) {
@@ -626,7 +635,7 @@ recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__
   const int wr = wave / (G::NW / 2), wc = wave % (G::NW / 2);
   // -g_m p = -sign(g_m) 2^(z log2(e) - (lambda_m log2(e) - log2|g_m|)), as in recompute_dz_bf16
   float ll[FC];
-  uint32_t sg[FC];
+  uint32_t sg[FC], live[FC];
 #pragma unroll
   for (int j = 0; j < FC; ++j) {
     const int m = m0 + G::col_of(wave, lane, j);
@@ -634,6 +643,7 @@ recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__
     const float2 l2 = (m < M) ? lam2[m] : make_float2(0.f, 0.f);
     ll[j] = (gm != 0.f) ? (l2.x + l2.y) - fast_log2(fabsf(gm)) : INFINITY;
     sg[j] = (gm > 0.f) ? 0x80008000u : 0u;
+    live[j] = (gm != 0.f) ? ~0u : 0u;
   }
   const GOp A{W + static_cast<int64_t>(c0) * D, D, cw, D, nullptr};
   const GOp B = HT ? GOp{Hst, Mp, M, D, nullptr} : GOp{Hs, D, M, D, nullptr};
@@ -661,7 +671,8 @@ recompute_run_bf16(const uint16_t* __restrict__ Hs, const uint16_t* __restrict__
           for (int e = 0; e < 4; ++e) v[e] = fast_exp2(fmaf(a[ib + il][j][4 * q + e], kLog2e, -ll[j]));
           const int c = 32 * il + 8 * q + 4 * hl;  // 4 consecutive vocabulary columns of frame rf
           const int off = rf * 128 + (((c >> 3) ^ (rf & 7)) << 4) + (((c >> 2) & 1) << 3);
-          *reinterpret_cast<u32x2*>(stg + off) = u32x2{pack_bf16x2(v[0], v[1]) ^ sg[j], pack_bf16x2(v[2], v[3]) ^ sg[j]};
+          *reinterpret_cast<u32x2*>(stg + off) =
+              u32x2{signed_pair<DM>(v[0], v[1], sg[j], live[j]), signed_pair<DM>(v[2], v[3], sg[j], live[j])};
         }
 #pragma unroll
       for (int t = 0; t < 4; ++t) {  // lanes 8 f.. 8 f + 7 take frame row f + 8 t

@@ -312,8 +312,12 @@ struct ProductsF32 {
   int nz, mslice, nw;  // nw: dW workgroups (0: no dW)
   float *dW, *wpart;   // dW: row c0
   bool dw_first;       // dW's workgroups first
+  const float* g;      // LIVE: [M]
 };
 
+// LIVE: the rows of dH whose g is 0 are zeros also where W is not finite.  (By a mask of the rows, read before the
+// product: reading g at every store took 5% of 1,600 rows, D = 512, 5,000 columns.)
+template <bool LIVE>
 __global__ void __launch_bounds__(512, 1) products_f32(ProductsF32 P) {
   PCTC_F3_STAGES
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -334,7 +338,24 @@ __global__ void __launch_bounds__(512, 1) products_f32(ProductsF32 P) {
     // a sum that the union columns made large loses more (1.4e-5 against 1.4e-6 at V = 180,000)
     const GOp A{P.dZ, P.chunk, P.M, P.cw, nullptr};
     const GOp B{P.W, P.D, P.D, P.cw, nullptr};
+    uint64_t live[2] = {~uint64_t{0}, ~uint64_t{0}};  // the wavefront's 128 rows
+    if constexpr (LIVE) {
+      static_assert(GH::FR == 4, "128 rows");
+      const int m = m0 + (wave / GH::WC) * 128 + lane;
+      live[0] = __ballot(m < P.M && P.g[min(m, P.M - 1)] != 0.f);
+      live[1] = __ballot(m + 64 < P.M && P.g[min(m + 64, P.M - 1)] != 0.f);
+    }
     GH::run(A, B, m0, d0, kb, ke, st, acc);
+    if (LIVE && (live[0] & live[1]) != ~uint64_t{0}) {
+#pragma unroll
+      for (int i = 0; i < GH::FR; ++i) {
+        const uint32_t rows = static_cast<uint32_t>(live[i >> 1] >> (32 * (i & 1))) >> (4 * (lane >> 5));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int j = 0; j < GH::FC; ++j) acc[i][j][r] = (rows >> (8 * (r >> 2) + (r & 3)) & 1) ? acc[i][j][r] : 0.f;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < GH::FR; ++i)
 #pragma unroll
@@ -631,9 +652,11 @@ hipError_t head_bwd_f32(const float* H, int M, int D, const float* W, const floa
       p.dW = dW ? dW + static_cast<int64_t>(c0) * D : nullptr;
       p.wpart = wpart;
       p.dw_first = mslice > p.slice;
+      p.g = g;
       {
         Prof pr("products", stream);
-        hipLaunchKernelGGL(products_f32, dim3(p.nh + p.nw), dim3(512), 0, stream, p);
+        if (tokens) hipLaunchKernelGGL(products_f32<true>, dim3(p.nh + p.nw), dim3(512), 0, stream, p);
+        else hipLaunchKernelGGL(products_f32<false>, dim3(p.nh + p.nw), dim3(512), 0, stream, p);
       }
       if (dW && nz > 1) {
         const int64_t n = static_cast<int64_t>(cw) * D;

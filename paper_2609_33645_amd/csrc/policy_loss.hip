@@ -436,7 +436,8 @@ db_join(const float* __restrict__ part, int slices, int pitch, int cw, uint16_t*
 }
 
 // dH[m] = the split-K slices' sum of place inv[m], and what the rounding to bf16 took off the token's own entry
-// times its row of W, rounded to bf16 (zeros for a row that is left out).  The own entry is the largest of
+// times its row of W, rounded to bf16 (zeros for a row that is left out or has no gradient: 0 times a value of W that is
+// not finite is none).  The own entry is the largest of
 // its row of dZ by far: with its rounding in, the row's error is that of two roundings (0.0025 of dH's norm),
 // without it of one (0.0017).  n values, a multiple of 4; the slices lie *t.Mdev D values apart.
 __global__ void __launch_bounds__(kThreads)
@@ -445,7 +446,7 @@ dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, int D, cons
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
   if (i >= n) return;
   const int m = static_cast<int>(i / D), j = inv[m];
-  if (j < 0) {
+  if (j < 0 || t.g[j] == 0.f) {
     *reinterpret_cast<u32x2*>(dH + i) = u32x2{0u, 0u};
     return;
   }
@@ -461,14 +462,12 @@ dh_reduce_b16(const float* __restrict__ part, int splits, int64_t n, int D, cons
     s.z += p.z;
     s.w += p.w;
   }
-  if (t.g[j] != 0.f) {
-    const float x = own_entry(t, j), rest = x - bf16_to_f32(f32_to_bf16(x));
-    const u32x2 w = *reinterpret_cast<const u32x2*>(W + static_cast<int64_t>(t.token[j]) * D + d);
-    s.x = fmaf(rest, __uint_as_float(w[0] << 16), s.x);
-    s.y = fmaf(rest, __uint_as_float(w[0] & 0xffff0000u), s.y);
-    s.z = fmaf(rest, __uint_as_float(w[1] << 16), s.z);
-    s.w = fmaf(rest, __uint_as_float(w[1] & 0xffff0000u), s.w);
-  }
+  const float x = own_entry(t, j), rest = x - bf16_to_f32(f32_to_bf16(x));
+  const u32x2 w = *reinterpret_cast<const u32x2*>(W + static_cast<int64_t>(t.token[j]) * D + d);
+  s.x = fmaf(rest, __uint_as_float(w[0] << 16), s.x);
+  s.y = fmaf(rest, __uint_as_float(w[0] & 0xffff0000u), s.y);
+  s.z = fmaf(rest, __uint_as_float(w[1] << 16), s.z);
+  s.w = fmaf(rest, __uint_as_float(w[1] & 0xffff0000u), s.w);
   *reinterpret_cast<u32x2*>(dH + i) = u32x2{pack_bf16x2(s.x, s.y), pack_bf16x2(s.z, s.w)};
 }
 

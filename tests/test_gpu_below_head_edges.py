@@ -92,3 +92,54 @@ def test_transposed_operands_whose_results_have_their_shape(dtype):
     got, want = calls(a, b, c, d, e), calls(*(x.contiguous() for x in (a, b, c, d, e)))
     for i, (g, w) in enumerate(zip(got, want)):
         assert g.is_contiguous() and torch.equal(g, w), i
+
+
+# ---- heads that are not finite -------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V,chunk", [(40, 64, 300, 0), (300, 512, 900, 256), (130, 2048, 700, 512), (520, 128, 3000, 0)])
+@pytest.mark.parametrize("bad", ["inf", "nan", "bias inf", "bias nan"])
+def test_policy_loss_of_a_head_that_is_not_finite(dtype, M, D, V, chunk, bad):
+    """Every row meets the class: none is counted, and none has a part in any gradient."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss head not finite", dtype, M, D, V, chunk, bad)
+    c = policy_case(M + V, M, D, V, dtype, "bias" in bad)
+    value = math.inf if "inf" in bad else math.nan
+    if "bias" in bad:
+        c["bias"][V // 2] = value
+    else:
+        c["W"][V // 2] = value
+    got = policy_call(c, dtype, (0.2, 0.3), 0.07, chunk=chunk, want_db=True)
+    ok = (c["tokens"] >= 0) & (c["tokens"] < V)
+    assert (got["status"].cpu().numpy() == np.where(ok, pc.TOKEN_NONFINITE, pc.TOKEN_LEFT_OUT)).all()
+    for k in ("loss", "losses", "dH", "dW", "db"):
+        assert not torch.isnan(got[k].float()).any() and not got[k].any(), k
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V", [(90, 64, 300), (300, 512, 900)])
+def test_policy_loss_of_a_class_that_some_rows_rule_out(dtype, M, D, V):
+    """An infinite value in W that gives some rows a logit of -inf (p = 0, they count) and others +inf (they do
+    not): these have no part in dW, db and their rows of dH."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss class ruled out", dtype, M, D, V)
+    c = policy_case(M, M, D, V, dtype)
+    c["tokens"] = np.abs(c["tokens"]) % (V - 1)
+    c["H"][:, 0] = np.where(np.arange(M) % 3 == 0, 1.0, -1.0)
+    c["W"][V - 1, 0] = math.inf
+    c["ref"] = c["old"] = None
+    got = policy_call(c, dtype, (0.2, 0.3), 0.0, want_db=True)
+    out = np.arange(M) % 3 == 0
+    assert (got["status"].cpu().numpy() == np.where(out, pc.TOKEN_NONFINITE, pc.TOKEN_COUNTED)).all()
+    assert not got["dH"][dev(out)].any()
+    # without that class and those rows
+    few = dict(c, H=c["H"][~out], W=c["W"][:-1], tokens=c["tokens"][~out], adv=c["adv"][~out], w=c["w"][~out])
+    want = policy_call(few, dtype, (0.2, 0.3), 0.0, want_db=True)
+    for k in ("losses", "logp"):
+        assert torch.allclose(got[k][dev(~out)], want[k], rtol=1e-5, atol=1e-5), k
+    for k in ("dW", "db"):
+        g, w = got[k][:-1].float(), want[k].float()
+        assert torch.isfinite(g).all() and float((g - w).norm()) <= 0.01 * float(w.norm()), k
+        assert not got[k][-1].any(), k
