@@ -327,7 +327,10 @@ __global__ void __launch_bounds__(KS * 64) ffn_few(FewArgs<E> P) {
       store4<E>(P.out + at, h);
       if constexpr (LO) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] -= bf16_to_f32(f32_to_bf16(h[e]));
+        for (int e = 0; e < 4; ++e) {
+          const float rest = h[e] - bf16_to_f32(f32_to_bf16(h[e]));
+          h[e] = rest - rest == 0.f ? rest : 0.f;  // (an infinite h has none: it would undo the first part)
+        }
         store4<E>(P.lo + at, h);
       }
       if (P.a) {

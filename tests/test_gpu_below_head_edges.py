@@ -143,3 +143,27 @@ def test_policy_loss_of_a_class_that_some_rows_rule_out(dtype, M, D, V):
         g, w = got[k][:-1].float(), want[k].float()
         assert torch.isfinite(g).all() and float((g - w).norm()) <= 0.01 * float(w.norm()), k
         assert not got[k][-1].any(), k
+
+
+# ---- the block's ends ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [1, 3, 8, 9, 300])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gated_ffn_of_a_hidden_unit_that_overflows(dtype, M, act):
+    """One unit of one row is infinite: the row is infinite with the signs of its weights, the others are as they were."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("gated_ffn overflow", dtype, M, act)
+    c = ffn_case(M, M, 64, 264, 72, dtype)
+    c["wg"][:, 0] = c["wu"][:, 0] = 0
+    want = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act)["y"]
+    c["wg"][5, 0] = c["wu"][5, 0] = 1
+    c["x"][:, 0] = 0
+    quiet = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act)["y"]
+    assert torch.equal(quiet, want)
+    c["x"][0, 0] = 2.0 ** 65
+    y = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act)["y"]
+    assert c["wd"][:, 5].all() and torch.equal(y[0], torch.copysign(torch.full_like(y[0], math.inf), c["wd"][:, 5]))
+    # (float tiles with such values are taken on other instructions, which round otherwise)
+    assert torch.equal(y[1:], want[1:]) if dtype == "bf16" else torch.allclose(y[1:], want[1:], rtol=1e-5, atol=1e-5)
