@@ -968,6 +968,12 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float, out: Optional
 
 # ---- policy loss -------------------------------------------------------------------------
 
+def _sizes_fit(*sizes: int) -> None:
+    """The library's sizes are int32; ctypes would cut a larger one off."""
+    if max(sizes) >= 2 ** 31 or min(sizes) < -2 ** 31:
+        raise PrunedCTCError(-1, "a size does not fit 32 bits")
+
+
 def _per_token(x: Optional[torch.Tensor], M: int, dev: torch.device, what: str) -> Optional[torch.Tensor]:
     if x is None:
         return None
@@ -991,6 +997,7 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
     Returns loss (float64 [1]), losses and logp (float32 [M]), status (int32 [M], TOKEN_*) and, of the type
     of H, dH [M, D], dW [V, D] and with want_db db [V].  dH_out / dW_out: the caller's tensors for them."""
     L = lib()
+    _sizes_fit(*H.shape, *W.shape, int(chunk))
     H, W, bias, dt = _head_args(H, W, bias)
     (M, D), V, dev = H.shape, int(W.shape[0]), H.device
     if tokens.numel() != M or tokens.dtype not in (torch.int32, torch.int64) or tokens.device != dev:
@@ -1087,6 +1094,7 @@ def embedding(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out
     if table.dim() != 2 or not table.is_cuda:
         raise PrunedCTCError(-1, "table must be a device tensor [V, D]")
     dt, dev, (V, D) = _dtype_code(table), table.device, table.shape
+    _sizes_fit(V, D)
     table = table.contiguous()
     tokens, size = _token_args(tokens, dev)
     y = _out(out, (*tokens.shape, D), table.dtype, table)
@@ -1119,6 +1127,7 @@ def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, V: int, scale: fl
         raise PrunedCTCError(-1, f"unsupported dtype {kind}")
     if V < 1 or D < 1:
         raise PrunedCTCError(-1, "V and D must be positive")
+    _sizes_fit(V, D)
     dy = dy.contiguous()
     dW = _out(out, (V, D), kind, dy)
     L = lib()
@@ -1149,6 +1158,7 @@ def _ffn_args(x, w_gate, w_up, w_down, activation):
     if tuple(w_gate.shape) != (F, D) or w_up.shape != w_gate.shape or w_down.shape[1] != F:
         raise PrunedCTCError(-1, "w_gate and w_up must be [F, D], w_down [O, F]")
     M = x.numel() // D if D else 0
+    _sizes_fit(M, D, F, O)
     return x.contiguous(), w_gate.contiguous(), w_up.contiguous(), w_down.contiguous(), (M, D, F, O), dt, \
         _ACTIVATIONS[activation]
 

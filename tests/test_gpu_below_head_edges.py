@@ -167,3 +167,30 @@ def test_gated_ffn_of_a_hidden_unit_that_overflows(dtype, M, act):
     assert c["wd"][:, 5].all() and torch.equal(y[0], torch.copysign(torch.full_like(y[0], math.inf), c["wd"][:, 5]))
     # (float tiles with such values are taken on other instructions, which round otherwise)
     assert torch.equal(y[1:], want[1:]) if dtype == "bf16" else torch.allclose(y[1:], want[1:], rtol=1e-5, atol=1e-5)
+
+
+# ---- sizes ---------------------------------------------------------------------------------------
+
+def test_sizes_that_int32_does_not_hold():
+    """Refused before anything is copied or allocated (2^32 + 8 rows were once taken as 8)."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("sizes past int32")
+    n = 2 ** 32 + 8
+    many = torch.zeros(1, 8, device="cuda", dtype=torch.bfloat16).expand(n, 8)
+    w, t = torch.zeros(16, 8, device="cuda", dtype=torch.bfloat16), torch.zeros(8, device="cuda", dtype=torch.int64)
+    tall, few = many[:, :1], torch.zeros(8, 1, device="cuda", dtype=torch.bfloat16)
+    wide = torch.zeros(8, 1, device="cuda", dtype=torch.bfloat16).expand(8, n)
+    rows = torch.zeros(1, device="cuda").expand(n)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    for call in (lambda: pc.gated_ffn(many, w, w, w.T), lambda: pc.gated_ffn(w, many, many, many.T),
+                 lambda: pc.gated_ffn(w, w, w, w[:, :1].T[:, :1].expand(n, 16)), lambda: pc.embedding(tall, t), lambda: pc.embedding(wide, t),
+                 lambda: pc.embedding_backward(few, t, n), lambda: pc.embedding_backward(wide, t, 8),
+                 lambda: pc.policy_loss(many, w, rows, rows), lambda: pc.policy_loss(w, many, t, t.float()),
+                 lambda: pc.policy_loss(w[:8], w, t, t.float(), chunk=2 ** 32 + 256)):
+        with pytest.raises(pc.PrunedCTCError) as e:
+            call()
+        assert e.value.code == -1
+    assert torch.cuda.max_memory_allocated() - before < 1 << 20
