@@ -523,7 +523,7 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
  *   tokens: device int32 [M]; advantages: device float [M].  old_logp NULL: the policy that sampled the tokens
  *   is this one (r = 1).  ref_logp NULL: no KL term.  weights NULL: 1.  All three device float [M].
  *   clip_lo, clip_hi >= 0 (+inf: not clipped), kl_weight finite and >= 0.  An advantage of 0 has no first term,
- *   whatever old_logp is.
+ *   whatever old_logp is, and a kl_weight of 0 no KL term, whatever ref_logp is.
  *   loss: device double [1]; losses, logp: device float [M]; status: device int32 [M]: PCTC_TOKEN_COUNTED;
  *   PCTC_TOKEN_LEFT_OUT, a token outside [0, V) (a prompt's place), logp 0; PCTC_TOKEN_NONFINITE, a loss or
  *   gradient factor that is not finite.  Rows that are not counted have losses 0 and take no part in loss

@@ -275,7 +275,7 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
       loss = -cut;
       c = flat ? 0.0 : -A * r;
     }
-    if (a.ref_logp) {
+    if (a.ref_logp && a.kl != 0.f) {  // (0 times an infinite difference is not zero)
       const double d = static_cast<double>(a.ref_logp[m]) - lp, x = expm1(d);
       loss += static_cast<double>(a.kl) * (x - d);
       c -= static_cast<double>(a.kl) * x;

@@ -194,3 +194,19 @@ def test_sizes_that_int32_does_not_hold():
             call()
         assert e.value.code == -1
     assert torch.cuda.max_memory_allocated() - before < 1 << 20
+
+
+# ---- terms without weight and refusals -----------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_policy_loss_with_a_kl_weight_of_zero(dtype):
+    """No KL term, whatever the reference is (0 times infinity would take rows out)."""
+    import torch
+    say("policy_loss kl 0", dtype)
+    c = policy_case(4, 60, 64, 200, dtype)
+    want = policy_call(dict(c, ref=None), dtype, (0.2, 0.3), 0.0, want_db=True)
+    refs = c["ref"].copy()
+    refs[::4], refs[1::4], refs[2::4] = -math.inf, math.nan, 1e4
+    for x in (c["ref"], refs):
+        got = policy_call(dict(c, ref=x), dtype, (0.2, 0.3), 0.0, want_db=True)
+        assert all(torch.equal(got[k], want[k]) for k in want)
