@@ -1009,7 +1009,10 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
         (advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights")))
     if adv is None:
         raise PrunedCTCError(-1, "no advantages")
-    lo, hi = (math.inf, math.inf) if clip is None else clip
+    try:
+        lo, hi = (math.inf, math.inf) if clip is None else map(float, clip)
+    except (TypeError, ValueError):
+        raise PrunedCTCError(-1, "clip must be None or how far below and above 1 the ratio counts") from None
     dH = _out(dH_out, (M, D), H.dtype, H, "dH_out") if want_dH else None
     dW = _out(dW_out, (V, D), H.dtype, H, "dW_out") if want_dW else None
     db = H.new_empty(V) if want_db else None
@@ -1022,8 +1025,8 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
     status = H.new_empty(M, dtype=torch.int32)
     ws = _scratch(nbytes, dev)
     at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    code = L.pctc_policy_loss(dt, at(H), M, D, at(W), at(bias), V, at(tokens), at(adv), at(old), at(ref), at(w), float(lo),
-                              float(hi), float(kl_weight), int(chunk), at(loss), at(losses), at(logp), at(status), at(dH),
+    code = L.pctc_policy_loss(dt, at(H), M, D, at(W), at(bias), V, at(tokens), at(adv), at(old), at(ref), at(w), lo,
+                              hi, float(kl_weight), int(chunk), at(loss), at(losses), at(logp), at(status), at(dH),
                               at(dW), at(db), at(ws), ws.numel(), _raw_stream(dev))
     if code:
         _check(code, "pctc_policy_loss")

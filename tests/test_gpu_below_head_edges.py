@@ -210,3 +210,16 @@ def test_policy_loss_with_a_kl_weight_of_zero(dtype):
     for x in (c["ref"], refs):
         got = policy_call(dict(c, ref=x), dtype, (0.2, 0.3), 0.0, want_db=True)
         assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+def test_policy_loss_refuses_what_is_no_clip():
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss clip")
+    H, W = torch.randn(4, 8, device="cuda"), torch.randn(16, 8, device="cuda")
+    t, adv = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.ones(4, device="cuda")
+    for clip in (0.2, (0.2,), (0.1, 0.2, 0.3), "ab", (None, 0.2), (-0.1, 0.2), (0.1, math.nan)):
+        with pytest.raises(pc.PrunedCTCError) as e:
+            pc.policy_loss(H, W, t, adv, clip=clip)
+        assert e.value.code == -1, clip
+    assert pc.policy_loss(H, W, t, adv, clip=[0.1, math.inf])["loss"].isfinite()
