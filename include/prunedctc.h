@@ -475,7 +475,7 @@ int32_t pctc_clip_grad_norm(int32_t ntensors, const void* const* grads, void* co
  *   out_dtype.  1 <= V <= PCTC_MAX_VOCAB, 1 <= D <= PCTC_MAX_DIM, 0 <= N <= 2^30, scale finite.
  *   workspace: pctc_embedding_backward_workspace_size() bytes, 256-byte aligned.
  *
- * What is written must not overlap an input but as said.  All are asynchronous.
+ * What is written, the workspace among it, must not overlap an input but as said.  All are asynchronous.
  * ---------------------------------------------------------------------------------- */
 int32_t pctc_dropout(pctc_dtype dtype, const void* x, const void* residual, void* y, int64_t n, double p,
                      uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* stream);
@@ -497,7 +497,7 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
  *   gate, up: device float [M, F], a and b, kept for the backward; both NULL or neither.
  * pctc_gated_ffn_backward: from dy [M, O] and the forward's x, gate and up the gradients dx [M, D], dw_gate and
  *   dw_up [F, D] (both or neither) and dw_down [O, F]; those that are NULL are not formed.
- * What is written must not overlap another buffer of the call.  workspace: pctc_gated_ffn_workspace_size() bytes
+ * What is written, the workspace among it, must not overlap another buffer of the call.  workspace: pctc_gated_ffn_workspace_size() bytes
  * (backward 0 or 1), 256-byte aligned.  Asynchronous; the result does not change from call to call.
  * ---------------------------------------------------------------------------------- */
 enum { PCTC_SILU = 0, PCTC_GELU = 1 };
@@ -531,7 +531,7 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
  *   dH [M, D], dW [V, D], db [V]: of the dtype of H, rounded once from float sums; each may be NULL, and with all
  *   three NULL only the losses are formed.
  *   workspace: pctc_policy_workspace_size() bytes (bias, grads: whether the call has a bias, asks for a
- *   gradient), 256-byte aligned.  What is written must not overlap another buffer of the call.  Asynchronous; the
+ *   gradient), 256-byte aligned.  What is written, the workspace among it, must not overlap another buffer of the call.  Asynchronous; the
  *   result does not change from call to call.
  * ---------------------------------------------------------------------------------- */
 enum { PCTC_TOKEN_COUNTED = 0, PCTC_TOKEN_LEFT_OUT = 1, PCTC_TOKEN_NONFINITE = 2 };

@@ -1292,7 +1292,10 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
       return PCTC_EINVAL;
     const size_t need = pctc_embedding_backward_workspace_size(N, D);
     if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
-    if (misaligned256(workspace) || meets(workspace, need, dW, bytes)) return PCTC_EINVAL;
+    if (misaligned256(workspace) || meets(workspace, need, dW, bytes) ||
+        meets(workspace, need, dy, static_cast<uint64_t>(N) * D * e) ||
+        meets(workspace, need, tokens, static_cast<uint64_t>(N) * token_bytes))
+      return PCTC_EINVAL;
   }
   PCTC_HIP(launch_embedding_backward(dtype == PCTC_BF16 ? 1 : 0, dy, tokens, token_bytes == 8, static_cast<int>(N), V, D,
                                      scale, out_dtype == PCTC_BF16 ? 1 : 0, dW, accumulate != 0, workspace,
@@ -1334,6 +1337,14 @@ static bool buffers_ok(const Buffer* b, int n) {
   return true;
 }
 
+// The workspace is written too.
+static bool workspace_ok(const void* workspace, size_t need, const Buffer* b, int n) {
+  if (misaligned256(workspace)) return false;
+  for (int i = 0; i < n; ++i)
+    if (meets(workspace, need, b[i].p, b[i].bytes)) return false;
+  return true;
+}
+
 int32_t pctc_gated_ffn(pctc_dtype dtype, const void* x, int32_t M, int32_t D, const void* w_gate, const void* w_up,
                        int32_t F, const void* w_down, int32_t O, int32_t activation, float* gate, float* up, void* y,
                        void* workspace, size_t workspace_bytes, void* stream_ptr) {
@@ -1346,7 +1357,7 @@ int32_t pctc_gated_ffn(pctc_dtype dtype, const void* x, int32_t M, int32_t D, co
                          {y, m * o, true, true}};
   if (!buffers_ok(b, 7)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
-  if (misaligned256(workspace)) return PCTC_EINVAL;
+  if (!workspace_ok(workspace, need, b, 7)) return PCTC_EINVAL;
   const FfnArgs q{x, w_gate, w_up, w_down, gate, up, y, M, D, F, O, activation};
   PCTC_HIP(launch_gated_ffn(dtype == PCTC_BF16 ? 1 : 0, q, workspace, static_cast<hipStream_t>(stream_ptr)));
   prof_flush();
@@ -1367,7 +1378,7 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
                          {dw_up, f * d, false, true}, {dw_down, o * f, false, true}};
   if (!buffers_ok(b, 11)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
-  if (misaligned256(workspace)) return PCTC_EINVAL;
+  if (!workspace_ok(workspace, need, b, 11)) return PCTC_EINVAL;
   const FfnArgs q{x, w_gate, w_up, w_down, const_cast<float*>(gate), const_cast<float*>(up), nullptr, M, D, F, O, activation};
   const FfnGrads g{dy, dx, dw_gate, dw_up, dw_down};
   PCTC_HIP(launch_gated_ffn_backward(dtype == PCTC_BF16 ? 1 : 0, q, g, workspace, static_cast<hipStream_t>(stream_ptr)));
@@ -1407,7 +1418,7 @@ int32_t pctc_policy_loss(pctc_dtype dtype, const void* H, int32_t M, int32_t D, 
                       {dW, v * d, false, true}, {db, v * e, false, true, e}};
   if (!buffers_ok(b, 15)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
-  if (misaligned256(workspace)) return PCTC_EINVAL;
+  if (!workspace_ok(workspace, need, b, 15)) return PCTC_EINVAL;
   const int dt = dtype == PCTC_BF16 ? 1 : 0;
   const PolicyArgs a{tokens, advantages, old_logp, ref_logp, weights, clip_lo, clip_hi, kl_weight, loss, losses, logp, status};
   PCTC_HIP(launch_policy_loss(dt, H, M, D, W, bias, V, a, dH, dW, db, static_cast<char*>(workspace),

@@ -216,3 +216,30 @@ def test_entry_points_check_their_tensors():
                  lambda: pc.dropout(x.half(), 0.1, 1)):
         with pytest.raises(pc.PrunedCTCError):
             call()
+
+
+@built
+def test_a_workspace_that_meets_another_buffer_is_refused():
+    """It is written: over an input it would change what the call reads, over an output what it gives."""
+    lib = _lib()
+    p = [OK + i * BIG for i in range(17)]
+    room = 1 << 34
+    # (name, arguments of which pointers may be any, the workspace's place, its size)
+    calls = {
+        "embedding_backward": (lib.pctc_embedding_backward, [1, p[0], p[1], 4, 50, 10, 8, 1.0, 0, p[2], 0, p[16], room, None], 11,
+                               lib.pctc_embedding_backward_workspace_size(50, 8)),
+        "gated_ffn": (lib.pctc_gated_ffn, [1, p[0], 10, 64, p[1], p[2], 128, p[3], 72, 0, p[4], p[5], p[6], p[16], room, None], 13,
+                      lib.pctc_gated_ffn_workspace_size(1, 10, 64, 128, 72, 0)),
+        "gated_ffn_backward": (lib.pctc_gated_ffn_backward, [1, p[0], p[1], 10, 64, p[2], p[3], p[4], p[5], 128, p[6], 72, 1, p[7],
+                                                             p[8], p[9], p[10], p[16], room, None], 17,
+                               lib.pctc_gated_ffn_workspace_size(1, 10, 64, 128, 72, 1)),
+        "policy_loss": (lib.pctc_policy_loss, [1, p[0], 10, 64, p[1], p[2], 300, p[3], p[4], p[5], p[6], p[7], 0.2, 0.2, 0.1, 0,
+                                               p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[16], room, None], 23,
+                        lib.pctc_policy_workspace_size(1, 10, 64, 300, 1, 1, 0)),
+    }
+    for name, (f, args, at, need) in calls.items():
+        assert need > 0
+        for q in [a for a in args if isinstance(a, int) and a >= OK and a != p[16]]:
+            for ws in (q, q - (need - 1) // 256 * 256):  # at its start, and ending behind it
+                args[at] = ws
+                assert f(*args) == -1, (name, p.index(q), ws - q)
