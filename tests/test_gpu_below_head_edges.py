@@ -223,3 +223,98 @@ def test_policy_loss_refuses_what_is_no_clip():
             pc.policy_loss(H, W, t, adv, clip=clip)
         assert e.value.code == -1, clip
     assert pc.policy_loss(H, W, t, adv, clip=[0.1, math.inf])["loss"].isfinite()
+
+
+# ---- every way the block goes --------------------------------------------------------------------
+
+def launches(call):
+    """What the call gives, and how often it launched each of the library's kernels."""
+    from paper_2609_33645_amd import prunedctc as pc
+    pc.prof_reset()
+    pc.prof_enable(True)
+    try:
+        r = call()
+    finally:
+        pc.prof_enable(False)
+    counts = {k: v["launches"] for k, v in pc.prof_read().items()}
+    pc.prof_reset()
+    return r, counts
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,F_,O,way", [
+    (513, 136, 64, 8, "sliced"), (600, 1032, 128, 72, "sliced"), (700, 2056, 72, 264, "sliced"),
+    (1061, 8, 4104, 8, "tiles"), (1290, 24, 4104, 16, "tiles"),
+    (1061, 72, 8184, 40, "apart"), (1152, 16, 8192, 8, "apart"), (2085, 136, 4040, 72, "apart"), (4215, 512, 2048, 512, "apart")])
+def test_gated_ffn_by_every_way(dtype, M, D, F_, O, way):
+    """Projections in slices of k that are joined (sums of 4 bytes for each of 2 M F values in the workspace, and no
+    other join: F is too short to cut), in whole tiles over more than one round of the chip (no room for such
+    sums), and in whole tiles with the last rows apart (the one launch of few rows that a call of more than 512 makes).
+    Everything is checked, the last rows with all the others."""
+    from paper_2609_33645_amd import prunedctc as pc
+    say("gated_ffn ways", dtype, M, D, F_, O, way)
+    act = "gelu" if (M + D) % 2 else "silu"
+    c = ffn_case(M + D, M, D, F_, O, dtype)
+    got, n = launches(lambda: pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act, keep=True))
+    room = pc.lib().pctc_gated_ffn_workspace_size(1 if dtype == "bf16" else 0, M, D, F_, O, 0)
+    sums = room - M * F_ * (2 if dtype == "bf16" else 4)
+    assert n["ffn_pair"] == 1 and n["ffn_down"] == 1
+    assert n.get("ffn_few", 0) == (1 if way == "apart" else 0)
+    assert (sums >= 8 * M * F_ and n["ffn_join"] == 1) if way == "sliced" else sums < 8 * M * F_
+    grads, n = launches(lambda: pc.gated_ffn_backward(c["dy"], c["x"], got["gate"], got["up"], c["wg"], c["wu"], c["wd"], act))
+    assert n["ffn_back"] == 1 and n["ffn_grads"] == 1
+    check_ffn(c, act, dtype, got, grads)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,F_", [(1061, 8200), (1152, 8192)])
+def test_gated_ffn_backward_in_whole_tiles(dtype, M, F_):
+    """dh by whole tiles with the activation in their epilogue, more than one round of the chip in float32: there is no
+    room for the sums of slices."""
+    from paper_2609_33645_amd import prunedctc as pc
+    say("gated_ffn back tiles", dtype, M, F_)
+    size = 2 if dtype == "bf16" else 4
+    room = pc.lib().pctc_gated_ffn_workspace_size(1 if dtype == "bf16" else 0, M, 8, F_, 8, 1)
+    assert room - 3 * M * F_ * size < 4 * M * F_
+    c = ffn_case(M, M, 8, F_, 8, dtype)
+    for act in ("silu", "gelu"):
+        got = pc.gated_ffn(c["x"], c["wg"], c["wu"], c["wd"], act, keep=True)
+        grads = pc.gated_ffn_backward(c["dy"], c["x"], got["gate"], got["up"], c["wg"], c["wu"], c["wd"], act)
+        check_ffn(c, act, dtype, got, grads)
+
+
+# ---- frames read from H transposed, of a number that only the device knows -----------------------
+
+@pytest.mark.parametrize("M,D,V,bias,counted", [(2300, 512, 600, True, 700), (2049, 640, 700, True, 1), (2200, 1920, 300, True, 2200),
+                                                (2304, 512, 500, True, 0), (2100, 1024, 40_000, False, 600),
+                                                (2064, 1024, 38_000, False, 2050)])
+def test_policy_loss_from_transposed_rows(M, D, V, bias, counted):
+    """The counted rows are gathered into memory that held NaN, transposed with what lies behind them, and the rows
+    that are left out hold NaN themselves: none of it reaches a result.  Checked on the counted rows alone."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss transposed", M, D, V, bias, counted)
+    r = np.random.default_rng(M + V)
+    rows = np.sort(r.choice(M, counted, replace=False))
+    few = policy_case(M + V, counted, D, V, "bf16", bias)
+    few["tokens"] = np.abs(few["tokens"]) % V
+    c = dict(few, H=np.full((M, D), math.nan), tokens=np.where(r.random(M) < 0.5, -1, V))
+    for k in ("adv", "old", "ref", "w"):
+        c[k] = np.full(M, math.nan, np.float32)
+    for k in ("H", "tokens", "adv", "old", "ref", "w"):
+        c[k][rows] = few[k]
+    junk = torch.full((pc.lib().pctc_policy_workspace_size(1, M, D, V, int(bias), 1, 0) // 2 + 4096,), math.nan, device="cuda",
+                      dtype=torch.bfloat16)
+    del junk
+    got, n = launches(lambda: policy_call(c, "bf16", (0.2, 0.3), 0.07, want_db=True))
+    assert n["ht_build"] == (1 if bias else 2)  # (the normaliser's frames, and without a bias the recompute's)
+    at = dev(rows)
+    out = torch.ones(M, dtype=torch.bool, device="cuda")
+    out[at] = False
+    assert (got["status"][out] == pc.TOKEN_LEFT_OUT).all()
+    assert not any(got[k][out].any() for k in ("losses", "logp", "dH"))
+    if counted:
+        part = {k: got[k][at] for k in ("losses", "logp", "status", "dH")}
+        check_policy(few, "bf16", (0.2, 0.3), 0.07, dict(got, **part), db=True)
+    else:
+        assert not any(got[k].any() for k in ("loss", "dW", "db"))
