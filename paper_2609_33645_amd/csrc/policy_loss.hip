@@ -224,7 +224,9 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
   }
   __syncthreads();
   if (j >= n) return;
-  // lambda: the largest maximum is exact, each sum is scaled by the float exponential of an exact difference
+  // lambda: the largest maximum is exact, each sum is scaled by the float exponential of an exact difference, and by
+  // what the normaliser's rounding of max log2(e) put into each of its exponents (beside logits of 2,000 that is
+  // 8.5e-5 of the sum, and so much of a certain token's log probability)
   constexpr int kPer = kMaxLseParts / 64;
   float2 q[kPer];
   float top = -INFINITY;
@@ -241,9 +243,12 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
   if (top != -INFINITY)
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
-      if (q[i].x != -INFINITY)
-        sum += static_cast<double>(q[i].y) *
+      if (q[i].x != -INFINITY) {
+        const float ms = q[i].x * kLog2e;
+        const double r = static_cast<double>(fmaf(q[i].x, kLog2e, -ms)) * kLn2D;  // exact, then exp(-r) to r^4 / 24
+        sum += static_cast<double>(q[i].y) * (1.0 - r * (1.0 - r * (0.5 - r / 6.0))) *
                static_cast<double>(fast_exp2(static_cast<float>(static_cast<double>(q[i].x) - top) * kLog2e));
+      }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
   double lam = top == -INFINITY ? -INFINITY : static_cast<double>(top) + log(sum);

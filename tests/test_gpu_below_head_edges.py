@@ -318,3 +318,36 @@ def test_policy_loss_from_transposed_rows(M, D, V, bias, counted):
         check_policy(few, "bf16", (0.2, 0.3), 0.07, dict(got, **part), db=True)
     else:
         assert not any(got[k].any() for k in ("loss", "dW", "db"))
+
+
+# ---- log probabilities of certain tokens ---------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V", [(9, 72, 300), (331, 512, 5000), (100, 2048, 700), (70, 4096, 1500), (2300, 512, 600), (2100, 1024, 38_000)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_policy_loss_of_certain_tokens_to_the_last_bits(dtype, M, D, V, bias):
+    """Logits of about 2,000 with a token that has all of the probability: its log probability is -sum exp(z_v - z_t),
+    below V exp(-gap).  The normaliser's sum is then that token's exponential, of an instruction that is off by at
+    most a unit in the last place, 2^-23 of 1, and twice that with the roundings of the float sums behind
+    it; lambda's own logit of the token lies 1.2e-4 from the next float, and the loss has to take the rounding that
+    gave it off again to the bit.  In double three sums of |z| are rounded besides."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("policy_loss certain bits", dtype, M, D, V, bias)
+    g = torch.Generator(device="cuda").manual_seed(M + D)
+    W = torch.randn(V, D, device="cuda", generator=g).to(kind(dtype))
+    t = torch.randint(0, V, (M,), device="cuda", generator=g)
+    H = (W[t].float() * (2000 / D) + torch.randn(M, D, device="cuda", generator=g)).to(kind(dtype))
+    b = torch.randn(V, device="cuda", generator=g) if bias else None
+    z = H.double() @ W.double().T + (0 if b is None else b.double())
+    own = z.gather(1, t[:, None])[:, 0]
+    gap = float((own - z.scatter(1, t[:, None], -math.inf).max(1).values).min())
+    assert gap > 40 and 1024 < float(own.median()) < 4096  # (the inputs are what they are meant to be)
+    got = pc.policy_loss(H, W, t, torch.ones(M, device="cuda"), bias=b, want_db=True)
+    tol = 2.0 ** -22 + 4 * 2.0 ** -53 * float(own.max()) + V * math.exp(-gap)
+    assert float(got["logp"].abs().max()) <= tol
+    assert torch.equal(got["losses"], torch.full_like(got["losses"], -1.0))
+    # dZ is g = -1 times at most tol + V exp(-gap) in any place; a class has at most M tokens
+    most = 2 * (tol + V * math.exp(-gap))
+    assert float(got["dH"].abs().max()) <= most * float(W.abs().max()) * 2
+    assert float(got["dW"].abs().max()) <= most * float(H.abs().max()) * M and float(got["db"].abs().max()) <= most * M
