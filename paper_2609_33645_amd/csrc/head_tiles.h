@@ -98,6 +98,16 @@ __device__ __forceinline__ void mask_rows_inf(f32x16 (&acc)[FR][FC], int v0, int
     }
 }
 
+// What the exponents of log2(e) z are taken relative to: the maximum's, but none below that of -1e9, so that a column
+// whose rows are all masked yet adds nothing, by a bias of -inf, of -1e30 or of the type's lowest value; and by how much
+// it is off log2(e) times that maximum, exactly.  (That rounding enters every exponent: 64 at 1e9, beyond every
+// exponential's range from 3e9 on.)
+constexpr float kLseFloor = -1e9f;
+__device__ __forceinline__ float lse_reference(float max) { return fmaxf(max, kLseFloor) * kLog2e; }
+__device__ __forceinline__ float lse_rounding(float max) {
+  return fmaf(fmaxf(max, kLseFloor), kLog2e, -lse_reference(max));
+}
+
 // Online log-sum-exp update of the running (max, sum) of this lane's frames with one
 // tile of logits (bias included; out-of-range rows already -inf).
 template <int FR, int FC, class G>
@@ -112,8 +122,7 @@ __device__ __forceinline__ void lse_tile_update(const f32x16 (&acc)[FR][FC], flo
       for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, acc[i][j][r]);
     tmax = fmaxf(tmax, swap_halves(tmax));
     const float nmax = fmaxf(run_max[j], tmax);
-    // a column with no finite logit yet (rows masked by a -inf bias) adds nothing
-    const float ms = (nmax == -INFINITY) ? 0.f : nmax * kLog2e;
+    const float ms = lse_reference(nmax);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < FR; ++i)
@@ -151,8 +160,7 @@ __device__ __forceinline__ void lse_block_update(const f32x16 (&acc)[FR][FC], fl
       }
     tmax = fmaxf(tmax, swap_halves(tmax));
     const float nmax = fmaxf(run_max[j], tmax);
-    // a column with no finite logit yet (rows masked by a -inf bias) adds nothing
-    const float ms = (nmax == -INFINITY) ? 0.f : nmax * kLog2e;
+    const float ms = lse_reference(nmax);
     float s = 0.f;
     if (__builtin_expect(__any(fabsf(nmax) > 1e37f && nmax > -INFINITY), 0)) {
       // a column of masked classes only, the mask a type's lowest value: its products with log2(e)
@@ -172,7 +180,7 @@ __device__ __forceinline__ void lse_block_update(const f32x16 (&acc)[FR][FC], fl
           s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         }
       // ms is nmax log2(e) rounded; its rounding, up to 1e-6 at a logit of 20, is taken off the sum again
-      if (nmax > -INFINITY) s *= fast_exp2(-fmaf(nmax, kLog2e, -ms));
+      s *= fast_exp2(-lse_rounding(nmax));
     }
     s += swap_halves(s);
     const float scale = (run_max[j] == -INFINITY) ? 0.f : fast_exp2((run_max[j] - nmax) * kLog2e);

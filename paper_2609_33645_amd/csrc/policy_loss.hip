@@ -244,8 +244,7 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
 #pragma unroll
     for (int i = 0; i < kPer; ++i)
       if (q[i].x != -INFINITY) {
-        const float ms = q[i].x * kLog2e;
-        const double r = static_cast<double>(fmaf(q[i].x, kLog2e, -ms)) * kLn2D;  // exact, then exp(-r) to r^4 / 24
+        const double r = static_cast<double>(lse_rounding(q[i].x)) * kLn2D;  // exp(-r) to r^4 / 24
         sum += static_cast<double>(q[i].y) * (1.0 - r * (1.0 - r * (0.5 - r / 6.0))) *
                static_cast<double>(fast_exp2(static_cast<float>(static_cast<double>(q[i].x) - top) * kLog2e));
       }

@@ -351,3 +351,58 @@ def test_policy_loss_of_certain_tokens_to_the_last_bits(dtype, M, D, V, bias):
     most = 2 * (tol + V * math.exp(-gap))
     assert float(got["dH"].abs().max()) <= most * float(W.abs().max()) * 2
     assert float(got["dW"].abs().max()) <= most * float(H.abs().max()) * M and float(got["db"].abs().max()) <= most * M
+
+
+# ---- classes masked by the bias ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V", [(90, 64, 700), (300, 512, 1500), (2100, 512, 1100), (60, 2048, 1030)])
+@pytest.mark.parametrize("where", ["first", "last", "middle", "scattered"])
+def test_policy_loss_of_masked_classes(dtype, M, D, V, where):
+    """A mask of minus infinity, of the type's lowest value and of -1e30 over whole tiles of classes: the same bits, and
+    what the loss gives without these classes."""
+    import torch
+    say("policy_loss masked classes", dtype, M, D, V, where)
+    masked = {"first": np.arange(V) < 520, "last": np.arange(V) >= V - 520, "middle": (np.arange(V) >= 100) & (np.arange(V) < 620),
+              "scattered": np.arange(V) % 3 == 0}[where]
+    keep = np.nonzero(~masked)[0]
+    few = policy_case(M + V, M, D, len(keep), dtype, True)
+    live = (few["tokens"] >= 0) & (few["tokens"] < len(keep))
+    W = np.random.default_rng(V).normal(size=(V, D)) / math.sqrt(D)
+    W[keep] = few["W"]
+    tokens = np.where(live, keep[np.where(live, few["tokens"], 0)], -1)
+    got = []
+    for low in (-math.inf, float(np.finfo(np.float32).min), -1e30):
+        b = np.full(V, low, np.float32)
+        b[keep] = few["bias"]
+        got.append(policy_call(dict(few, W=W, bias=b, tokens=tokens), dtype, (0.2, 0.3), 0.07, want_db=True))
+    for other in got[1:]:
+        assert all(torch.equal(other[k], got[0][k]) for k in got[0])
+    at = dev(keep)
+    part = {k: got[0][k][at] for k in ("dW", "db")}
+    check_policy(few, dtype, (0.2, 0.3), 0.07, dict(got[0], **part), db=True)
+    off = dev(masked)
+    assert not got[0]["dW"][off].any() and not got[0]["db"][off].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,D,V", [(50, 64, 1500), (300, 512, 1500), (2100, 512, 1100), (60, 2048, 1100)])
+def test_other_calls_on_the_head_with_masked_classes(dtype, M, D, V):
+    """The same of Pruned CTC, whose normaliser it is, and of the frame candidates."""
+    import torch
+    from paper_2609_33645_amd import prunedctc as pc
+    say("masked classes elsewhere", dtype, M, D, V)
+    g = torch.Generator(device="cuda").manual_seed(M)
+    H, W = (torch.randn(n, D, device="cuda", generator=g).to(kind(dtype)) / D ** 0.25 for n in (M, V))
+    b = torch.randn(V, device="cuda", generator=g)
+    y = torch.arange(1, 11, dtype=torch.int32, device="cuda")
+    want = None
+    for low in (-math.inf, float(np.finfo(np.float32).min), -1e30, -1e9):
+        b[100:1000] = low
+        r = pc.pruned_ctc_fwd_bwd(H, W, y, [M], [10], 0, beam=100.0, bias=b, want_db=True)
+        c = pc.frame_candidates(H, W, 8, 0, b)
+        got = {**{k: r[k] for k in ("loss", "loss_per_utt", "status", "dH", "dW", "db")}, **c}
+        if want is None:
+            want = got
+            assert r["status"].item() == pc.UTT_OK and all(torch.isfinite(v.double()).all() for v in got.values())
+        assert all(torch.equal(got[k], want[k]) for k in want), (low, [k for k in want if not torch.equal(got[k], want[k])])
