@@ -497,8 +497,9 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
  *   gate, up: device float [M, F], a and b, kept for the backward; both NULL or neither.
  * pctc_gated_ffn_backward: from dy [M, O] and the forward's x, gate and up the gradients dx [M, D], dw_gate and
  *   dw_up [F, D] (both or neither) and dw_down [O, F]; those that are NULL are not formed.
- * What is written, the workspace among it, must not overlap another buffer of the call.  workspace: pctc_gated_ffn_workspace_size() bytes
- * (backward 0 or 1), 256-byte aligned.  Asynchronous; the result does not change from call to call.
+ * What is written, the workspace among it, must not overlap another buffer of the call.
+ * workspace: pctc_gated_ffn_workspace_size() bytes (backward 0 or 1), 256-byte aligned.  Asynchronous; the result
+ * does not change from call to call.
  * ---------------------------------------------------------------------------------- */
 enum { PCTC_SILU = 0, PCTC_GELU = 1 };
 size_t pctc_gated_ffn_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t F, int32_t O, int32_t backward);
@@ -531,8 +532,8 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
  *   dH [M, D], dW [V, D], db [V]: of the dtype of H, rounded once from float sums; each may be NULL, and with all
  *   three NULL only the losses are formed.
  *   workspace: pctc_policy_workspace_size() bytes (bias, grads: whether the call has a bias, asks for a
- *   gradient), 256-byte aligned.  What is written, the workspace among it, must not overlap another buffer of the call.  Asynchronous; the
- *   result does not change from call to call.
+ *   gradient), 256-byte aligned.  What is written, the workspace among it, must not overlap another buffer of the
+ *   call.  Asynchronous; the result does not change from call to call.
  * ---------------------------------------------------------------------------------- */
 enum { PCTC_TOKEN_COUNTED = 0, PCTC_TOKEN_LEFT_OUT = 1, PCTC_TOKEN_NONFINITE = 2 };
 size_t pctc_policy_workspace_size(pctc_dtype dtype, int32_t M, int32_t D, int32_t V, int32_t bias, int32_t grads,

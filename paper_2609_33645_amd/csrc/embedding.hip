@@ -220,8 +220,8 @@ radix_count(SortPass P) {
 // A thread a digit: its tokens in all tiles and in those before, and a scan over the digits, give the first
 // place of the tile's tokens of the digit (at most kMaxTiles rows of counts, read from the caches; a launch
 // of its own for the scan took 5 us).  Each wavefront counts its own share of the tile by digit, the counts
-// become first places (over the wavefronts before it), and it goes through its share again in order, 64 tokens at a time: lanes of
-// the same digit are found by a ballot per bit.
+// become first places (over the wavefronts before it), and it goes through its share again in order, 64
+// tokens at a time: lanes of the same digit are found by a ballot per bit.
 template <bool I64>
 __global__ void __launch_bounds__(kSortThreads)
 radix_place(SortPass P) {
@@ -424,7 +424,8 @@ __global__ void __launch_bounds__(kThreads) fill_zero(void* p, int64_t bytes) {
 
 // Workgroups that clear.
 unsigned clear_blocks(int64_t bytes, int threads) {
-  return static_cast<unsigned>(std::min<int64_t>((bytes + threads * 16 - 1) / (threads * 16), (int64_t{1} << 31) / threads));
+  const int64_t each = threads * 16;
+  return static_cast<unsigned>(std::min<int64_t>((bytes + each - 1) / each, (int64_t{1} << 31) / threads));
 }
 
 int lanes_for(int pieces) {

@@ -193,7 +193,8 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 template <class E>
 __device__ __forceinline__ void few_step(const u32x4& w, const u32x4& x, f32x4& acc) {
   if constexpr (E::kBf) {
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0,
+                                                  0, 0);
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)  // k in another order, the same for both operands
@@ -514,7 +515,8 @@ __global__ void __launch_bounds__(512, 1) ffn_products(Products Q) {
   const int r0 = rt * kT, c0 = ct * kT;
   const int kb = slice * P.depth, ke = kb + P.depth;
   f32x16 acc[GK::FR][GK::FC];
-  const Op A{static_cast<const T*>(P.A), P.pa, P.rows, P.K, nullptr}, B{static_cast<const T*>(P.B), P.pb, P.cols, P.K, nullptr};
+  const Op A{static_cast<const T*>(P.A), P.pa, P.rows, P.K, nullptr};
+  const Op B{static_cast<const T*>(P.B), P.pb, P.cols, P.K, nullptr};
   if (MCB && (!KCB || P.mc_b)) {
     if constexpr (E::kBf) GM::run_pp(A, B, r0, c0, kb, min(ke, P.K), st, acc);
     else GM::run(A, B, r0, c0, kb, min(ke, P.K), st, acc);
@@ -728,8 +730,8 @@ double tiles_us(int count, int K, bool bf) { return (count + 255) / 256 * (K * s
 // float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
 int rows_apart(const FfnArgs& q) {
   const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
-  const bool apart = rest > 0 && rest <= kT / 2 && q.M > kT && (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256;
-  return apart ? rest : 0;
+  if (rest == 0 || rest > kT / 2 || q.M <= kT) return 0;
+  return (q.M / kT * nF + 255) / 256 < (tiles(q.M) * nF + 255) / 256 ? rest : 0;
 }
 Pair pair_plan(const FfnArgs& q, bool bf, Products& Q) {
   Q = Products{};
@@ -739,7 +741,8 @@ Pair pair_plan(const FfnArgs& q, bool bf, Products& Q) {
   const double weights = 2.0 * q.D * q.F, sliced = plan(Q, bf, true);
   FfnArgs last = q;
   last.M = rows_apart(q);
-  const double whole = tiles_us(tiles(q.M - last.M) * tiles(q.F, kT / 2), q.D, bf) + (last.M ? few_us(last, bf, weights) : 0);
+  double whole = tiles_us(tiles(q.M - last.M) * tiles(q.F, kT / 2), q.D, bf);
+  if (last.M) whole += few_us(last, bf, weights);
   if (q.M <= kFew && few_us(q, bf, weights) <= std::min(sliced, whole)) return Pair::kFew;
   return sliced < whole ? Pair::kSliced : Pair::kTiles;
 }
@@ -783,7 +786,8 @@ hipError_t forward(const FfnArgs& q, void* h, char* part, hipStream_t stream) {
   using T = typename E::T;
   T* const hh = static_cast<T*>(h);
   float *const a = q.a, *const b = q.b;
-  const T *const x = static_cast<const T*>(q.x), *const wg = static_cast<const T*>(q.wg), *const wu = static_cast<const T*>(q.wu);
+  const T *const x = static_cast<const T*>(q.x);
+  const T *const wg = static_cast<const T*>(q.wg), *const wu = static_cast<const T*>(q.wu);
   const bool silu = q.act == kSilu;
   T* const lo = two_parts(q, E::kBf) ? reinterpret_cast<T*>(part) : nullptr;
   auto few = [&](int m0, int rows) {

@@ -94,8 +94,9 @@ void rows_from(const int32_t* Mdev, F launch) {
 
 template <class G, bool BIAS, int OCC, bool DM = false>
 __global__ void __launch_bounds__(G::kThreads, OCC)
-lse_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __restrict__ W, const float* __restrict__ bias,
-                 int V, int P, int vper, float2* __restrict__ partials, const int32_t* __restrict__ Mdev) {
+lse_partial_bf16(const uint16_t* __restrict__ H, int M, int D, const uint16_t* __restrict__ W,
+                 const float* __restrict__ bias, int V, int P, int vper, float2* __restrict__ partials,
+                 const int32_t* __restrict__ Mdev) {
   extern __shared__ float bsh[];  // BIAS: b over this partition's rows (vper, padded to whole tiles)
   constexpr int FR = G::FR, FC = G::FC, TR = G::kBR, TC = G::kBC;
   PCTC_STAGES_G(G)

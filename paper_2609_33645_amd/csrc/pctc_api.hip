@@ -1265,7 +1265,8 @@ int32_t pctc_embedding(pctc_dtype dtype, const void* table, int32_t V, int32_t D
   if (!table || !tokens || !y || misaligned_to(table, e) || misaligned_to(y, e) || misaligned_to(tokens, token_bytes))
     return PCTC_EINVAL;
   const uint64_t bytes = static_cast<uint64_t>(N) * D * e;
-  if (meets(y, bytes, table, static_cast<uint64_t>(V) * D * e) || meets(y, bytes, tokens, static_cast<uint64_t>(N) * token_bytes))
+  if (meets(y, bytes, table, static_cast<uint64_t>(V) * D * e) ||
+      meets(y, bytes, tokens, static_cast<uint64_t>(N) * token_bytes))
     return PCTC_EINVAL;
   PCTC_HIP(launch_embedding(dtype == PCTC_BF16 ? 1 : 0, table, V, D, tokens, token_bytes == 8, N, scale, y,
                             static_cast<hipStream_t>(stream_ptr)));
@@ -1288,13 +1289,12 @@ int32_t pctc_embedding_backward(pctc_dtype dtype, const void* dy, const void* to
   if (!dW || misaligned_to(dW, o)) return PCTC_EINVAL;
   if (N > 0) {
     if (!dy || !tokens || misaligned_to(dy, e) || misaligned_to(tokens, token_bytes)) return PCTC_EINVAL;
-    if (meets(dW, bytes, dy, static_cast<uint64_t>(N) * D * e) || meets(dW, bytes, tokens, static_cast<uint64_t>(N) * token_bytes))
-      return PCTC_EINVAL;
+    const uint64_t rows = static_cast<uint64_t>(N) * D * e, ids = static_cast<uint64_t>(N) * token_bytes;
+    if (meets(dW, bytes, dy, rows) || meets(dW, bytes, tokens, ids)) return PCTC_EINVAL;
     const size_t need = pctc_embedding_backward_workspace_size(N, D);
     if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
-    if (misaligned256(workspace) || meets(workspace, need, dW, bytes) ||
-        meets(workspace, need, dy, static_cast<uint64_t>(N) * D * e) ||
-        meets(workspace, need, tokens, static_cast<uint64_t>(N) * token_bytes))
+    if (misaligned256(workspace) || meets(workspace, need, dW, bytes) || meets(workspace, need, dy, rows) ||
+        meets(workspace, need, tokens, ids))
       return PCTC_EINVAL;
   }
   PCTC_HIP(launch_embedding_backward(dtype == PCTC_BF16 ? 1 : 0, dy, tokens, token_bytes == 8, static_cast<int>(N), V, D,
@@ -1379,7 +1379,8 @@ int32_t pctc_gated_ffn_backward(pctc_dtype dtype, const void* dy, const void* x,
   if (!buffers_ok(b, 11)) return PCTC_EINVAL;
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (!workspace_ok(workspace, need, b, 11)) return PCTC_EINVAL;
-  const FfnArgs q{x, w_gate, w_up, w_down, const_cast<float*>(gate), const_cast<float*>(up), nullptr, M, D, F, O, activation};
+  const FfnArgs q{x, w_gate, w_up, w_down, const_cast<float*>(gate), const_cast<float*>(up), nullptr, M, D, F, O,
+                  activation};
   const FfnGrads g{dy, dx, dw_gate, dw_up, dw_down};
   PCTC_HIP(launch_gated_ffn_backward(dtype == PCTC_BF16 ? 1 : 0, q, g, workspace, static_cast<hipStream_t>(stream_ptr)));
   prof_flush();
@@ -1420,7 +1421,8 @@ int32_t pctc_policy_loss(pctc_dtype dtype, const void* H, int32_t M, int32_t D, 
   if (!workspace || workspace_bytes < need) return PCTC_EWORKSPACE;
   if (!workspace_ok(workspace, need, b, 15)) return PCTC_EINVAL;
   const int dt = dtype == PCTC_BF16 ? 1 : 0;
-  const PolicyArgs a{tokens, advantages, old_logp, ref_logp, weights, clip_lo, clip_hi, kl_weight, loss, losses, logp, status};
+  const PolicyArgs a{tokens, advantages, old_logp, ref_logp, weights, clip_lo, clip_hi, kl_weight, loss, losses, logp,
+                     status};
   PCTC_HIP(launch_policy_loss(dt, H, M, D, W, bias, V, a, dH, dW, db, static_cast<char*>(workspace),
                               policy_layout(dt, M, D, V, bias != nullptr, grads, chunk),
                               static_cast<hipStream_t>(stream_ptr)));

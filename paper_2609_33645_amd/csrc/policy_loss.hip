@@ -68,7 +68,8 @@ policy_count(const int32_t* __restrict__ tokens, int M, int V, int32_t* __restri
 constexpr int kGatherRows = 8;
 __global__ void __launch_bounds__(kThreads)
 policy_gather(const uint16_t* __restrict__ H, int M, int D, int V, PolicyArgs a, const int32_t* __restrict__ counts,
-              uint16_t* __restrict__ Hc, int32_t* __restrict__ rows, int32_t* __restrict__ inv, int32_t* __restrict__ count) {
+              uint16_t* __restrict__ Hc, int32_t* __restrict__ rows, int32_t* __restrict__ inv,
+              int32_t* __restrict__ count) {
   const int m0 = blockIdx.x * kGatherRows;
   auto counted = [&](int m) { return m < M && static_cast<uint32_t>(a.tokens[m]) < static_cast<uint32_t>(V); };
   int n = 0, from = 0;
@@ -94,7 +95,8 @@ policy_gather(const uint16_t* __restrict__ H, int M, int D, int V, PolicyArgs a,
         const uint16_t* src = H + static_cast<int64_t>(m) * D;
         uint16_t* dst = Hc + static_cast<int64_t>(j) * D;
 #pragma unroll 4
-        for (int d = lane * 8; d < D; d += 512) *reinterpret_cast<u32x4*>(dst + d) = *reinterpret_cast<const u32x4*>(src + d);
+        for (int d = lane * 8; d < D; d += 512)
+          *reinterpret_cast<u32x4*>(dst + d) = *reinterpret_cast<const u32x4*>(src + d);
       }
       if (lane == 0) {
         inv[m] = in ? j : -1;
@@ -218,8 +220,8 @@ policy_tokens(const void* H, int M, int D, const void* __restrict__ W, const flo
     const int c = lane & 31, q = min(j0 + (c & (kPlaces - 1)), n - 1);
     const int t0 = a.tokens[R.rows ? R.rows[q] : q], t = t0 >= 0 && t0 < V ? t0 : 0;
     const float z = tile_logit<BF>(static_cast<const char*>(H) + static_cast<int64_t>(q) * D * kBytes,
-                                   static_cast<const char*>(W) + static_cast<int64_t>(t) * D * kBytes, bias ? bias[t] : 0.f, D,
-                                   lane);
+                                   static_cast<const char*>(W) + static_cast<int64_t>(t) * D * kBytes,
+                                   bias ? bias[t] : 0.f, D, lane);
     if (c < kPlaces && (lane >> 5) == ((c >> 2) & 1)) tile[c] = z;
   }
   __syncthreads();
@@ -658,7 +660,8 @@ static hipError_t policy_bwd_bf16(uint16_t* Hc, int M, int D, const uint16_t* W,
       Prof pr("db_colsum", stream);
       const int most = (M + 127) / 128 < kDbSlices ? (M + 127) / 128 : kDbSlices;  // (dbpart has a row per 128 frames)
       const int mper = ((M + most - 1) / most + 7) / 8 * 8, slices = (M + mper - 1) / mper, tiles = (cw + 255) / 256;
-      hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart, c0, tokens);
+      hipLaunchKernelGGL(db_slices, dim3(tiles, slices), dim3(kThreads), 0, stream, dZ, M, chunk, mper, dbpart, c0,
+                         tokens);
       hipLaunchKernelGGL(db_join, dim3(tiles), dim3(kThreads), 0, stream, dbpart, slices, chunk, cw, db + c0);
     }
     if (dH) {
@@ -713,8 +716,8 @@ hipError_t launch_policy_loss(int dtype, const void* H, int M, int D, const void
     {
       Prof pr("policy_gather", stream);
       if (many)
-        hipLaunchKernelGGL(policy_count, dim3((M + kCountRows - 1) / kCountRows), dim3(kThreads), 0, stream, a.tokens, M, V,
-                           counts);
+        hipLaunchKernelGGL(policy_count, dim3((M + kCountRows - 1) / kCountRows), dim3(kThreads), 0, stream, a.tokens, M,
+                           V, counts);
       hipLaunchKernelGGL(policy_gather, dim3((M + kGatherRows - 1) / kGatherRows), dim3(kThreads), 0, stream,
                          static_cast<const uint16_t*>(H), M, D, V, a, many ? counts : nullptr, Hc, i32(L.o_rows),
                          i32(L.o_inv), count);
@@ -754,8 +757,8 @@ hipError_t launch_policy_loss(int dtype, const void* H, int M, int D, const void
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (grads)
-      return head_bwd_f32(static_cast<const float*>(H), M, D, static_cast<const float*>(W), bias, V, lam2, nullptr, 0, R.g,
-                          nullptr, static_cast<float*>(dH), static_cast<float*>(dW), static_cast<float*>(db),
+      return head_bwd_f32(static_cast<const float*>(H), M, D, static_cast<const float*>(W), bias, V, lam2, nullptr, 0,
+                          R.g, nullptr, static_cast<float*>(dH), static_cast<float*>(dW), static_cast<float*>(db),
                           ws + L.o_bwd, L.bwd, stream, &tokens);
   }
   // no chunk to sum beside

@@ -214,8 +214,10 @@ def run(steps: int = 300, beams: int = 8, classes: int = 200, seed: int = 0, N: 
         W, b, losses, norms = fit(Hd, yd, T, U, classes, steps)
     more = {}
     if policy:
-        W, rewards, pnorms = reinforce(through_block(Hd, below), W, b, T, np.split(y, np.cumsum(U)[:-1]), policy, seed=seed)
-        more = {"reward_first": float(rewards[0]), "reward_last": float(rewards[-1]), "policy_norm_max": float(pnorms.max())}
+        ref = np.split(y, np.cumsum(U)[:-1])
+        W, rewards, pnorms = reinforce(through_block(Hd, below), W, b, T, ref, policy, seed=seed)
+        more = {"reward_first": float(rewards[0]), "reward_last": float(rewards[-1]),
+                "policy_norm_max": float(pnorms.max())}
     H, y, T, U = speak(rng, E, N, noise=3.0)
     H, Ed = torch.from_numpy(H).to(dev), torch.from_numpy(E).to(dev)
     H = through_block(H, below)

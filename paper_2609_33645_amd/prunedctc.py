@@ -155,8 +155,8 @@ def lib() -> ctypes.CDLL:
     L.pctc_gated_ffn.argtypes = [c_i32, c_p, c_i32, c_i32, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_p, c_p, c_p, c_p, c_sz,
                                  c_p]
     L.pctc_gated_ffn.restype = c_i32
-    L.pctc_gated_ffn_backward.argtypes = [c_i32, c_p, c_p, c_i32, c_i32, c_p, c_p, c_p, c_p, c_i32, c_p, c_i32, c_i32, c_p,
-                                          c_p, c_p, c_p, c_p, c_sz, c_p]
+    L.pctc_gated_ffn_backward.argtypes = [c_i32, c_p, c_p, c_i32, c_i32, c_p, c_p, c_p, c_p, c_i32, c_p, c_i32, c_i32,
+                                          c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
     L.pctc_gated_ffn_backward.restype = c_i32
     L.pctc_policy_workspace_size.argtypes = [c_i32] * 7
     L.pctc_policy_workspace_size.restype = c_sz
@@ -1038,7 +1038,7 @@ def policy_loss(H: torch.Tensor, W: torch.Tensor, tokens: torch.Tensor, advantag
 def _out(out: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.Tensor, what: str = "out") -> torch.Tensor:
     """A new contiguous tensor, or the caller's, which must be one of that shape (on the device of `like`)."""
     dev = like.device
-    if out is None:  # (half the time of torch.empty with a device; empty_like keeps the strides of what is not contiguous)
+    if out is None:  # (half the time of torch.empty with a device; but what is not contiguous keeps its strides there)
         same = shape == like.shape and dtype is like.dtype and like.is_contiguous()
         return torch.empty_like(like) if same else like.new_empty(shape, dtype=dtype)
     if out.dtype is not dtype or tuple(out.shape) != tuple(shape) or out.device != dev or not out.is_contiguous():
@@ -1075,8 +1075,8 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset=0, residual: Optional[t
             raise PrunedCTCError(-1, f"offset must be a whole number or an int64 tensor of one on {dev}")
         counter, offset = offset, 0
     y = _out(out, x.shape, x.dtype, x)
-    code = lib().pctc_dropout(dt, x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(), x.numel(),
-                              float(p), _u64(seed, "seed"), _u64(offset, "offset"),
+    code = lib().pctc_dropout(dt, x.data_ptr(), None if residual is None else residual.data_ptr(), y.data_ptr(),
+                              x.numel(), float(p), _u64(seed, "seed"), _u64(offset, "offset"),
                               None if counter is None else counter.data_ptr(), _raw_stream(dev))
     if code:
         _check(code, "pctc_dropout")
@@ -1218,9 +1218,10 @@ def gated_ffn_backward(dy: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, up
 
 
 class Dropout(torch.autograd.Function):
-    """Autograd wrapper of dropout().  (For a backward that is captured into a graph, here as for any operator: no
-    graph recorded outside the capture may still hold the same leaves.)  The mask is made again in the backward, from the counters of the forward (a
-    device tensor's value is copied: the caller may move it on before)."""
+    """Autograd wrapper of dropout().  The mask is made again in the backward, from the counters of the forward (a
+    device tensor's value is copied: the caller may move it on before).  For this layer and those below, as
+    for any operator: while a backward is captured into a graph, no autograd graph recorded outside the
+    capture may still hold the same leaves."""
 
     @staticmethod
     def forward(ctx, x, p, seed, offset, residual):
@@ -1247,7 +1248,8 @@ class Embedding(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        return (embedding_backward(dy, *ctx.saved_tensors, ctx.V, ctx.scale) if ctx.needs_input_grad[0] else None), None, None
+        (tokens,) = ctx.saved_tensors
+        return embedding_backward(dy, tokens, ctx.V, ctx.scale) if ctx.needs_input_grad[0] else None, None, None
 
 
 class GatedFFN(torch.autograd.Function):
