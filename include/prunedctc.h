@@ -148,7 +148,7 @@ int32_t pruned_ctc_fwd_bwd(pctc_dtype dtype, const void* H, int32_t D, const voi
  * dL/deta = db[blank]; App. C normalises losses by the batch's target-token count,
  * which is w_n = 1 / sum_n U_n).
  *
- * bias        device float [V] or NULL: logits are H W^T + 1 b^T.
+ * bias        device float [V] or NULL: logits are H W^T + 1 b^T.  -inf, or any value of -1e9 or less, masks a class.
  * utt_weight  device float [N] or NULL (all 1): loss = sum_n w_n L_n over the included
  *             utterances, and dH, dW, db are the gradients of that sum.  loss_per_utt
  *             still receives the unweighted L_n.  A zero weight excludes the utterance

@@ -98,7 +98,7 @@ __device__ __forceinline__ void store8(void* p, int64_t i, int left, const float
 }
 
 // Two groups of 8 values a thread, all read before the generator runs, past the caches (nothing is read again).  Bound by
-// memory: 11,458 x 4,096 in bf16 31 us, with a residual 46 (6.0 TB/s); 331 x 512 3.2.
+// memory: 11,458 x 4,096 in bf16 31 us, with a residual 46 (6.1 TB/s); 331 x 512 3.0.
 // x, residual and y may be the same memory: a thread reads its values before it writes them.
 template <bool BF, bool RES>
 __global__ void __launch_bounds__(kThreads)

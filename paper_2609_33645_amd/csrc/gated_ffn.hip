@@ -727,7 +727,7 @@ double few_us(const FfnArgs& q, bool bf, double weights) {
 }
 double tiles_us(int count, int K, bool bf) { return (count + 255) / 256 * (K * step_us(bf) + (bf ? 10 : 25)); }
 // The rows past the last whole tile go without tiles where that saves a round of the chip (M = 4,215, 512 x 2,048,
-// float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 113 and 15 for the rest).
+// float: 17 x 16 tiles are two rounds, 182 us, 16 x 16 one, 116 and 12 for the rest).
 int rows_apart(const FfnArgs& q) {
   const int nF = tiles(q.F, kT / 2), rest = q.M % kT;
   if (rest == 0 || rest > kT / 2 || q.M <= kT) return 0;

@@ -342,7 +342,7 @@ __device__ __forceinline__ void amax_store_partials(float (&bv)[G::FC], int (&bi
 // through its own 16 KB of the drained stages (16-byte slots XORed with the column, so that neither
 // writes nor reads meet in a bank), and come back 8 consecutive tile rows a lane, 16 lanes a column, so that
 // memory is read and written in lines.  Straight from the accumulators a store is 32 pieces of 16 bytes: the
-// epilogue of ffn_back then took longer than its product (M = 2,567, 4,096 x 10,240: 419 us, now 238).
+// epilogue of ffn_back then took longer than its product (M = 2,567, 4,096 x 10,240: 419 us, now 255).
 // fn(block, col, v, x): tile rows 8 block .. 8 block + 7 of the wavefront's 128, column col of its 64; x is what
 // pre(block, col, x) read for these places, for 32 columns before any of them is used, so that many
 // reads are in flight (there is one workgroup on a compute unit, whose products are over).

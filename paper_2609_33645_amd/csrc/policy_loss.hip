@@ -204,7 +204,7 @@ __device__ __forceinline__ float tile_logit(const void* h, const void* w, float 
 // rows of D values, lanes' float sums joined in double; the loss in double.  The normaliser's products round that
 // logit otherwise; lambda is corrected by what the difference makes of the token's own share of it (tile_logit), so
 // that the log probability of a nearly certain token is right (losses 1.4e-6 -> 2e-7 off 64 bits, fp32 gradients
-// 3e-6 -> 4e-7; the first wavefront's sums take 3 us of 331 rows at D = 512, 11 in float, 20 of 1,925 at D = 4,096).
+// 3e-6 -> 3e-7; the first wavefront's sums take 3 us of 331 rows at D = 512, 11 in float, 20 of 1,925 at D = 4,096).
 // mask (null: none): a row without a gradient is cleared there, so that what is not finite in it reaches no product.
 template <bool BF>
 __global__ void __launch_bounds__(kLossThreads)
